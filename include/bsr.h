@@ -298,6 +298,83 @@ bsr_status_t bsr_plan_get_order(bsr_plan_t plan, int *order, int *call, int n, i
 /* bsr_plan_destroy -- release the graph and the workspaces. NULL is a no-op. */
 void bsr_plan_destroy(bsr_plan_t plan);
 
+/*
+ * ---- The residual step between two blocks
+ *
+ * A transformer layer adds the output of a block (of bsr_spmm, of a
+ * feed-forward block) to its residual stream; a norm may stand before and
+ * after the block, a gate and a scale at its end:
+ *
+ *   t[n]  = post(y[n])
+ *   h'[n] = alpha * h[n] + scale * gate[n / gate_tokens] * t[n]
+ *   z[n]  = pre(h'[n])                       (the next block's input)
+ *
+ * post and pre: BSR_NORM_NONE (the row itself), BSR_NORM_LAYER
+ * (x - mean) / sqrt(var + eps) * w + b with the biased variance, or BSR_NORM_RMS
+ * x / sqrt(mean(x^2) + eps) * w + b. All arithmetic is in fp32; h' and z are
+ * rounded once each, z is made from the unrounded h'.
+ */
+typedef enum { BSR_NORM_NONE = 0, BSR_NORM_LAYER = 1, BSR_NORM_RMS = 2 } bsr_norm_t;
+
+typedef struct {
+    int64_t D;             /* features, 1 .. 16384 (else BSR_ERR_SHAPE) */
+    int64_t gate_tokens;   /* consecutive tokens that share a row of the gate: >= 1 with a gate, else unused */
+    bsr_dtype_t block_dt;  /* element type of y, z, gate and their gradients */
+    bsr_dtype_t stream_dt; /* element type of h, h' and their gradients: block_dt, or BSR_F32 beside bf16 blocks */
+    bsr_norm_t post, pre;
+    float post_eps, pre_eps;
+    float alpha;
+    const float *scale;            /* device fp32 [D], or NULL for 1 */
+    const float *post_w, *post_b;  /* device fp32 [D], or NULL for 1 and 0; NULL without the norm */
+    const float *pre_w, *pre_b;
+} bsr_residual_norm_t;
+
+/*
+ * bsr_residual_norm -- h' and z from y and h.
+ *
+ * y, h     device, [N, D] row-major, 16-byte aligned. h NULL: no stream yet (0).
+ * gate     device, [ceil(N / gate_tokens), D], 16-byte aligned, or NULL for 1.
+ * h_out    receives h', or NULL where only z is wanted.
+ * z        receives z; NULL if and only if pre is BSR_NORM_NONE (then h_out is needed).
+ * A plain norm of y: h, gate and h_out NULL, post BSR_NORM_NONE.
+ * h_out may be h and z may be y (the same addresses); outputs overlap nothing
+ * else (BSR_ERR_INVALID_ARG). Device buffers only. N == 0 is a no-op.
+ * Asynchronous on `stream`; allocates nothing. The current device's buffers.
+ */
+bsr_status_t bsr_residual_norm(const bsr_residual_norm_t *p, const void *y, const void *h, const void *gate, void *h_out,
+                               void *z, int64_t N, void *stream);
+
+/* The gradients of the parameters; each device, or NULL where not wanted (and
+ * NULL where the parameter is absent). dgate has the gate's shape and type. */
+typedef struct {
+    void *dgate;
+    float *dscale, *dpost_w, *dpost_b, *dpre_w, *dpre_b;
+} bsr_residual_norm_grads_t;
+
+/* Bytes of workspace of a backward call of N tokens (0 for N == 0), with or
+ * without a gate of p->gate_tokens tokens a row. */
+bsr_status_t bsr_residual_norm_workspace(const bsr_residual_norm_t *p, int64_t N, size_t *bytes);
+
+/*
+ * bsr_residual_norm_backward -- the gradients of y, h and the parameters, from
+ * y, the h' that the forward call returned and the gradients of h' and z.
+ *
+ * h_out    the forward call's h'; needed if pre is a norm, else unused.
+ * dh_out   the gradient of h' from what else reads it, or NULL for 0.
+ * dz       the gradient of z; NULL if and only if pre is BSR_NORM_NONE.
+ * dy, dh   receive the gradients of y and h; each may be NULL. dh may be dh_out,
+ *          dy may be y or dz (the same addresses); else nothing overlaps.
+ * grads    written, not added to (zeros for N == 0); NULL: none wanted.
+ * ws       device, 16-byte aligned, of at least the bytes that
+ *          bsr_residual_norm_workspace gives (else BSR_ERR_CAPACITY); used until
+ *          the call's kernels have run.
+ * Sums over tokens are added in a fixed order: the same call gives the same bits.
+ */
+bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void *y, const void *h_out, const void *gate,
+                                        const void *dh_out, const void *dz, void *dy, void *dh,
+                                        const bsr_residual_norm_grads_t *grads, int64_t N, void *ws, size_t ws_bytes,
+                                        void *stream);
+
 /* bsr_destroy -- release what the handle owns (not the borrowed arrays). NULL is a no-op. */
 void bsr_destroy(bsr_handle_t h);
 

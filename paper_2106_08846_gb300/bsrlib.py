@@ -34,7 +34,27 @@ BSR_BF16 = 1
 _DT = {torch.float32: BSR_F32, torch.bfloat16: BSR_BF16}
 _TORCH_DT = {BSR_F32: torch.float32, BSR_BF16: torch.bfloat16}
 
+BSR_NORM_NONE = 0
+BSR_NORM_LAYER = 1
+BSR_NORM_RMS = 2
+
+_NORM = {"none": BSR_NORM_NONE, "layer": BSR_NORM_LAYER, "rms": BSR_NORM_RMS}
+
 _lib = None
+
+
+class _ResidualNorm(ctypes.Structure):
+    """bsr_residual_norm_t"""
+    _fields_ = [("D", ctypes.c_int64), ("gate_tokens", ctypes.c_int64), ("block_dt", ctypes.c_int),
+                ("stream_dt", ctypes.c_int), ("post", ctypes.c_int), ("pre", ctypes.c_int), ("post_eps", ctypes.c_float),
+                ("pre_eps", ctypes.c_float), ("alpha", ctypes.c_float), ("scale", ctypes.c_void_p),
+                ("post_w", ctypes.c_void_p), ("post_b", ctypes.c_void_p), ("pre_w", ctypes.c_void_p),
+                ("pre_b", ctypes.c_void_p)]
+
+
+class _ResidualNormGrads(ctypes.Structure):
+    """bsr_residual_norm_grads_t"""
+    _fields_ = [(k, ctypes.c_void_p) for k in ("dgate", "dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")]
 
 
 class BsrError(RuntimeError):
@@ -82,6 +102,14 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.bsr_get_schedule.restype = U
         lib.bsr_get_call_info.argtypes = [P, I64, ctypes.c_char_p, ctypes.c_size_t]
         lib.bsr_get_call_info.restype = U
+        RN = ctypes.POINTER(_ResidualNorm)
+        lib.bsr_residual_norm.argtypes = [RN, P, P, P, P, P, I64, P]
+        lib.bsr_residual_norm.restype = U
+        lib.bsr_residual_norm_workspace.argtypes = [RN, I64, ctypes.POINTER(ctypes.c_size_t)]
+        lib.bsr_residual_norm_workspace.restype = U
+        lib.bsr_residual_norm_backward.argtypes = [RN, P, P, P, P, P, P, P, ctypes.POINTER(_ResidualNormGrads), I64, P,
+                                                   ctypes.c_size_t, P]
+        lib.bsr_residual_norm_backward.restype = U
         lib.bsr_destroy.argtypes = [P]
         lib.bsr_destroy.restype = None
         lib.bsr_status_str.argtypes = [U]
@@ -364,6 +392,105 @@ def bsr_get_call_info(h: Handle, N: int) -> str:
 
 def bsr_destroy(h: Handle) -> None:
     h.destroy()
+
+
+def _workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    """Scratch of one call, from torch's allocator: handed out again only to work that comes after the call on its stream."""
+    if nbytes == 0:
+        return None
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if stream is not None:
+        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+        ws.record_stream(s)
+        s.wait_stream(torch.cuda.current_stream(device))   # (its last user may still be at work there)
+    return ws
+
+
+def _check_rows(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
+    if t is None:
+        return
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}")
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous, of shape {list(shape)}")
+
+
+def _residual_norm(y, stream_dt, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps):
+    """The checked bsr_residual_norm_t of a call."""
+    if post not in _NORM or pre not in _NORM:
+        raise ValueError("post and pre are 'none', 'layer' or 'rms'")
+    if y.dim() != 2:
+        raise ValueError("y must be [N, D]")
+    N, D = y.shape
+    for name, w in (("scale", scale), ("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b)):
+        if w is not None:
+            _check_rows(name, w, (D,), torch.float32)
+    if gate is not None:
+        if gate_tokens < 1:
+            raise ValueError("gate_tokens must be at least 1")
+        _check_rows("gate", gate, (-(-N // gate_tokens), D), y.dtype)
+    return _ResidualNorm(D, gate_tokens if gate is not None else 0, dtype_code(y.dtype), dtype_code(stream_dt), _NORM[post],
+                         _NORM[pre], eps, eps if pre_eps is None else pre_eps, alpha, _ptr(scale), _ptr(post_w), _ptr(post_b),
+                         _ptr(pre_w), _ptr(pre_b))
+
+
+def bsr_residual_norm(y: torch.Tensor, h: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+                      gate_tokens: int = 1, scale: Optional[torch.Tensor] = None, alpha: float = 1.0, post: str = "none",
+                      post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None, pre: str = "none",
+                      pre_w: Optional[torch.Tensor] = None, pre_b: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                      pre_eps: Optional[float] = None, h_out: Optional[torch.Tensor] = None,
+                      z: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(h_out, z): h_out = alpha h + scale * gate * post(y) and z = pre(h_out)
+    (None if pre is "none"), for rows y [N, D] of a block's output and h of the
+    residual stream (None: no stream yet). gate has a row for each gate_tokens
+    tokens; eps is both norms', or post's beside pre_eps. h_out may be h and z may
+    be y (see include/bsr.h)."""
+    st = (h if h is not None else h_out if h_out is not None else y).dtype
+    p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
+    if h_out is None:
+        h_out = torch.empty(y.shape, dtype=st, device=y.device)
+    if z is None and pre != "none":
+        z = torch.empty_like(y)
+    for name, t, dt in (("y", y, y.dtype), ("h", h, st), ("h_out", h_out, st), ("z", z, y.dtype)):
+        _check_rows(name, t, y.shape, dt)
+    st = (_lib or load()).bsr_residual_norm(p, y.data_ptr(), _ptr(h), _ptr(gate), h_out.data_ptr(), _ptr(z), y.shape[0],
+                                            _stream(stream))
+    if st:
+        _check(st, "bsr_residual_norm")
+    return h_out, z
+
+
+def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], dh_out: Optional[torch.Tensor],
+                               dz: Optional[torch.Tensor], *, gate: Optional[torch.Tensor] = None, gate_tokens: int = 1,
+                               scale: Optional[torch.Tensor] = None, alpha: float = 1.0, post: str = "none",
+                               post_w: Optional[torch.Tensor] = None, post_b: Optional[torch.Tensor] = None,
+                               pre: str = "none", pre_w: Optional[torch.Tensor] = None,
+                               pre_b: Optional[torch.Tensor] = None, eps: float = 1e-5, pre_eps: Optional[float] = None,
+                               dy: Optional[torch.Tensor] = None, dh: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """Gradients of bsr_residual_norm, whose arguments it takes with the h_out
+    that it returned (needed if pre is a norm) and the gradients of h_out (None: 0)
+    and of z (None if pre is "none"): "dy", "dh", and of each parameter given
+    "dgate", "dscale", "dpost_w", "dpost_b", "dpre_w" and "dpre_b"."""
+    st = next((t.dtype for t in (h_out, dh_out, dh) if t is not None), y.dtype)
+    p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
+    out = {"dy": torch.empty_like(y) if dy is None else dy,
+           "dh": torch.empty(y.shape, dtype=st, device=y.device) if dh is None else dh}
+    for name, t, dt in (("y", y, y.dtype), ("h_out", h_out, st), ("dh_out", dh_out, st), ("dz", dz, y.dtype),
+                        ("dy", out["dy"], y.dtype), ("dh", out["dh"], st)):
+        _check_rows(name, t, y.shape, dt)
+    grads = _ResidualNormGrads()
+    for name, w in (("dgate", gate), ("dscale", scale), ("dpost_w", post_w), ("dpost_b", post_b), ("dpre_w", pre_w),
+                    ("dpre_b", pre_b)):
+        if w is not None:
+            out[name] = torch.empty_like(w)
+            setattr(grads, name, out[name].data_ptr())
+    lib, n = _lib or load(), ctypes.c_size_t(0)
+    _check(lib.bsr_residual_norm_workspace(p, y.shape[0], ctypes.byref(n)), "bsr_residual_norm_workspace")
+    ws = _workspace(n.value, y.device, stream)
+    _check(lib.bsr_residual_norm_backward(p, y.data_ptr(), _ptr(h_out), _ptr(gate), _ptr(dh_out), _ptr(dz),
+                                          out["dy"].data_ptr(), out["dh"].data_ptr(), grads, y.shape[0], _ptr(ws), n.value,
+                                          _stream(stream)), "bsr_residual_norm_backward")
+    return out
 
 
 def parse_schedule(text: str) -> dict:

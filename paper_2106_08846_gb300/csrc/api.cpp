@@ -17,24 +17,12 @@
 #include <vector>
 
 #include "bsr_internal.h"
+#include "host.h"
 #include "schedule.h"
 
 namespace bsr {
 
 namespace {
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
 
 std::mutex g_cache_mu;
 std::unordered_map<uint64_t, std::vector<std::weak_ptr<Schedule>>> g_cache;
@@ -59,27 +47,6 @@ bool same_key(const Schedule &s, int device, bsr_dtype_t dt, int R, int C, int64
               const std::vector<int32_t> &indptr, const std::vector<int32_t> &indices) {
     return s.device == device && s.dt == dt && s.R == R && s.C == C && s.M == M && s.K == K &&
            s.indptr == indptr && s.indices == indices;
-}
-
-enum PtrKind { PK_DEVICE, PK_HOST, PK_BAD };
-
-// Where a pointer lives, relative to the handle's device.
-PtrKind classify(const void *p, int device) {
-    cudaPointerAttributes at;
-    cudaError_t e = cudaPointerGetAttributes(&at, p);
-    if (e != cudaSuccess) { cudaGetLastError(); return PK_BAD; }
-    switch (at.type) {
-        case cudaMemoryTypeDevice: return at.device == device ? PK_DEVICE : PK_BAD;
-        case cudaMemoryTypeManaged: return PK_DEVICE;
-        case cudaMemoryTypeHost:
-        case cudaMemoryTypeUnregistered: return PK_HOST;
-        default: return PK_BAD;
-    }
-}
-
-bool overlaps(const void *a, size_t na, const void *b, size_t nb) {
-    uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return na && nb && x < y + nb && y < x + na;
 }
 
 bsr_status_t grow(void **buf, size_t *cap, size_t need) {
