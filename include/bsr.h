@@ -375,6 +375,57 @@ bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void
                                         const bsr_residual_norm_grads_t *grads, int64_t N, void *ws, size_t ws_bytes,
                                         void *stream);
 
+/*
+ * ---- The gated feed-forward block
+ *
+ *   G = X Wg' + bg,  U = X Wu' + bu,  H = act(G) * U      (elementwise)
+ *
+ * with dense weights: the paper prunes a transformer's attention projections,
+ * its feed-forward weights stay dense. H is what a down projection (bsr_spmm)
+ * takes. X [N, K], Wg and Wu [F, K], H [N, F], row-major, element type dt; bg and
+ * bu fp32 [F] or NULL. Sums are held in fp32 and G and U are not rounded before
+ * H is. Sizes: F, K in 1 .. 2^20, N in 0 .. 2^31 - 1, N F and N K below 2^40.
+ */
+typedef enum {
+    BSR_ACT_SILU = 0,      /* g / (1 + e^-g) */
+    BSR_ACT_GELU = 1,      /* g Phi(g), Phi the normal distribution (erf) */
+    BSR_ACT_GELU_TANH = 2, /* g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2 */
+    BSR_ACT_RELU = 3,      /* max(g, 0) */
+    BSR_ACT_SIGMOID = 4    /* 1 / (1 + e^-g) */
+} bsr_act_t;
+
+/* Bytes of workspace of a call of N tokens; `backward` 0 or 1. May be 0. */
+bsr_status_t bsr_gated_workspace(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, int backward, size_t *bytes);
+
+/*
+ * bsr_gated -- H from X.
+ *
+ * X, Wg, Wu, H: device, 16-byte aligned; H overlaps no other buffer.
+ * ws       device, 16-byte aligned, of at least the bytes that bsr_gated_workspace
+ *          gives (else BSR_ERR_CAPACITY); used until the call's kernels have run.
+ * Asynchronous on `stream`; allocates nothing; reads the weights as they are when
+ * its kernels run. N == 0 is a no-op. Device buffers of the current device only.
+ */
+bsr_status_t bsr_gated(const void *X, const void *Wg, const void *Wu, const float *bg, const float *bu, void *H, int64_t N,
+                       int64_t F, int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * bsr_gated_backward -- the gradients from dH [N, F], with G and U computed again
+ * from the forward call's arguments:
+ *
+ *   dG = dH U act'(G), dU = dH act(G)       (relu'(0) = 0)
+ *   dX = dG Wg + dU Wu, dWg = dG' X, dWu = dU' X, dbg = sum_n dG, dbu = sum_n dU
+ *
+ * dX [N, K], dWg and dWu [F, K] (element type dt, 16-byte aligned), dbg and dbu
+ * fp32 [F]: written, not added to; each NULL where not wanted, but dWg and dWu
+ * both or neither, and dbg or dbu only beside bg or bu. For N == 0 the weights'
+ * gradients are zeros. No output overlaps another buffer. For BSR_BF16, dG and dU
+ * are rounded to bf16 as operands of dX, dWg and dWu (not for dbg and dbu).
+ */
+bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, const float *bg, const float *bu,
+                                const void *dH, void *dX, void *dWg, void *dWu, float *dbg, float *dbu, int64_t N, int64_t F,
+                                int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream);
+
 /* bsr_destroy -- release what the handle owns (not the borrowed arrays). NULL is a no-op. */
 void bsr_destroy(bsr_handle_t h);
 

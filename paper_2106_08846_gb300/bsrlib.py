@@ -38,6 +38,14 @@ BSR_NORM_NONE = 0
 BSR_NORM_LAYER = 1
 BSR_NORM_RMS = 2
 
+BSR_ACT_SILU = 0
+BSR_ACT_GELU = 1
+BSR_ACT_GELU_TANH = 2
+BSR_ACT_RELU = 3
+BSR_ACT_SIGMOID = 4
+
+_ACT = {"silu": BSR_ACT_SILU, "gelu": BSR_ACT_GELU, "gelu_tanh": BSR_ACT_GELU_TANH, "relu": BSR_ACT_RELU,
+        "sigmoid": BSR_ACT_SIGMOID}
 _NORM = {"none": BSR_NORM_NONE, "layer": BSR_NORM_LAYER, "rms": BSR_NORM_RMS}
 
 _lib = None
@@ -110,6 +118,12 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.bsr_residual_norm_backward.argtypes = [RN, P, P, P, P, P, P, P, ctypes.POINTER(_ResidualNormGrads), I64, P,
                                                    ctypes.c_size_t, P]
         lib.bsr_residual_norm_backward.restype = U
+        lib.bsr_gated_workspace.argtypes = [I64, I64, I64, U, I, ctypes.POINTER(ctypes.c_size_t)]
+        lib.bsr_gated_workspace.restype = U
+        lib.bsr_gated.argtypes = [P, P, P, P, P, P, I64, I64, I64, U, I, P, ctypes.c_size_t, P]
+        lib.bsr_gated.restype = U
+        lib.bsr_gated_backward.argtypes = [P] * 11 + [I64, I64, I64, U, I, P, ctypes.c_size_t, P]
+        lib.bsr_gated_backward.restype = U
         lib.bsr_destroy.argtypes = [P]
         lib.bsr_destroy.restype = None
         lib.bsr_status_str.argtypes = [U]
@@ -490,6 +504,72 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
     _check(lib.bsr_residual_norm_backward(p, y.data_ptr(), _ptr(h_out), _ptr(gate), _ptr(dh_out), _ptr(dz),
                                           out["dy"].data_ptr(), out["dh"].data_ptr(), grads, y.shape[0], _ptr(ws), n.value,
                                           _stream(stream)), "bsr_residual_norm_backward")
+    return out
+
+
+def _check_gated(X, Wg, Wu, bg, bu, act: str) -> Tuple[int, int, int, int]:
+    """The checks of a gated block's inputs; (N, F, K, type)."""
+    if act not in _ACT:
+        raise ValueError("act is one of " + ", ".join(_ACT))
+    dt = dtype_code(X.dtype)
+    if X.dim() != 2 or Wg.dim() != 2:
+        raise ValueError("X must be [N, K] and Wg and Wu [F, K]")
+    (N, K), F = X.shape, Wg.shape[0]
+    _check_rows("X", X, (N, K), X.dtype)
+    _check_rows("Wg", Wg, (F, K), X.dtype)
+    _check_rows("Wu", Wu, (F, K), X.dtype)
+    _check_rows("bg", bg, (F,), torch.float32)
+    _check_rows("bu", bu, (F,), torch.float32)
+    return N, F, K, dt
+
+
+def _gated_workspace(N, F, K, dt, backward, device, stream):
+    n = ctypes.c_size_t(0)
+    _check((_lib or load()).bsr_gated_workspace(N, F, K, dt, backward, ctypes.byref(n)), "bsr_gated_workspace")
+    return _workspace(n.value, device, stream), n.value
+
+
+def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor] = None,
+              bu: Optional[torch.Tensor] = None, act: str = "silu", H: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """H = act(X Wg' + bg) * (X Wu' + bu): the gated feed-forward block of X
+    [N, K] with dense weights [F, K]; act is "silu", "gelu" (erf), "gelu_tanh",
+    "relu" or "sigmoid"."""
+    N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
+    if H is None:
+        H = torch.empty((N, F), dtype=X.dtype, device=X.device)
+    _check_rows("H", H, (N, F), X.dtype)
+    ws, n = _gated_workspace(N, F, K, dt, 0, X.device, stream)
+    st = _lib.bsr_gated(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), H.data_ptr(), N, F, K, dt, _ACT[act],
+                        _ptr(ws), n, _stream(stream))
+    if st:
+        _check(st, "bsr_gated")
+    return H
+
+
+def bsr_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[torch.Tensor],
+                       bu: Optional[torch.Tensor], dH: torch.Tensor, act: str = "silu",
+                       dX: Optional[torch.Tensor] = None, dWg: Optional[torch.Tensor] = None,
+                       dWu: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """Gradients of bsr_gated from that of its result: "dX", "dWg", "dWu", and
+    "dbg" and "dbu" where the biases are given. G and U are computed again;
+    nothing is kept from the forward call."""
+    N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
+    out = {"dX": torch.empty_like(X) if dX is None else dX, "dWg": torch.empty_like(Wg) if dWg is None else dWg,
+           "dWu": torch.empty_like(Wu) if dWu is None else dWu}
+    _check_rows("dH", dH, (N, F), X.dtype)
+    _check_rows("dX", out["dX"], (N, K), X.dtype)
+    _check_rows("dWg", out["dWg"], (F, K), X.dtype)
+    _check_rows("dWu", out["dWu"], (F, K), X.dtype)
+    if bg is not None:
+        out["dbg"] = torch.empty_like(bg)
+    if bu is not None:
+        out["dbu"] = torch.empty_like(bu)
+    ws, n = _gated_workspace(N, F, K, dt, 1, X.device, stream)
+    _check(_lib.bsr_gated_backward(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), dH.data_ptr(),
+                                   out["dX"].data_ptr(), out["dWg"].data_ptr(), out["dWu"].data_ptr(), _ptr(out.get("dbg")),
+                                   _ptr(out.get("dbu")), N, F, K, dt, _ACT[act], _ptr(ws), n, _stream(stream)),
+           "bsr_gated_backward")
     return out
 
 

@@ -1,0 +1,56 @@
+// Activations of the gated feed-forward block and their derivatives, in fp32.
+#pragma once
+
+#include "bsr.h"
+
+namespace bsr {
+
+// 1 / (1 + e^-x); FAST: the hardware's exponential and reciprocal, whose
+// relative error of about 2^-21 is lost in a result rounded to bf16.
+template <bool FAST>
+__device__ __forceinline__ float logistic(float x) {
+    if constexpr (FAST) return __fdividef(1.f, 1.f + __expf(-x));
+    else return 1.f / (1.f + expf(-x));
+}
+
+constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+
+// act(g); the tanh form of GELU as g / (1 + e^-2u), which is the same.
+template <bool FAST>
+__device__ __forceinline__ float activate(int act, float g) {
+    switch (act) {
+        case BSR_ACT_SILU: return g * logistic<FAST>(g);
+        case BSR_ACT_GELU: return g * (FAST ? fmaf(0.5f, erff(0.70710678f * g), 0.5f) : normcdff(g));
+        case BSR_ACT_GELU_TANH: return g * logistic<FAST>(2.f * kGeluA * g * fmaf(kGeluB * g, g, 1.f));
+        case BSR_ACT_RELU: return g > 0.f ? g : (g != g ? g : 0.f);
+        default: return logistic<FAST>(g);
+    }
+}
+
+// act(g) and act'(g).
+template <bool FAST>
+__device__ __forceinline__ float2 activate_slope(int act, float g) {
+    switch (act) {
+        case BSR_ACT_SILU: {
+            const float p = logistic<FAST>(g);
+            return make_float2(g * p, p * fmaf(g, 1.f - p, 1.f));
+        }
+        case BSR_ACT_GELU: {
+            const float p = FAST ? fmaf(0.5f, erff(0.70710678f * g), 0.5f) : normcdff(g);
+            const float density = 0.3989422804f * (FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g));
+            return make_float2(g * p, fmaf(g, density, p));
+        }
+        case BSR_ACT_GELU_TANH: {
+            const float p = logistic<FAST>(2.f * kGeluA * g * fmaf(kGeluB * g, g, 1.f));
+            return make_float2(g * p, fmaf(g * p * (1.f - p), 2.f * kGeluA * fmaf(3.f * kGeluB * g, g, 1.f), p));
+        }
+        case BSR_ACT_RELU: return make_float2(g > 0.f ? g : (g != g ? g : 0.f), g > 0.f ? 1.f : (g != g ? g : 0.f));
+        default: {
+            const float p = logistic<FAST>(g);
+            return make_float2(p, p * (1.f - p));
+        }
+    }
+}
+
+}  // namespace bsr

@@ -4,6 +4,7 @@
 #include <cmath>
 
 #include "bsr_internal.h"
+#include "gated.h"
 #include "host.h"
 #include "residual_norm.h"
 
@@ -89,6 +90,17 @@ void add_params(Buffers &b, const bsr_residual_norm_t *p) {
     for (const float *w : {p->scale, p->post_w, p->post_b, p->pre_w, p->pre_b}) b.in(w, (size_t)p->D * 4, 4);
 }
 
+constexpr int64_t kGatedMost = (int64_t)1 << 20;
+
+bsr_status_t check_gated(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt) {
+    if (!known(dt)) return BSR_ERR_UNSUPPORTED;
+    if (N < 0) return BSR_ERR_INVALID_ARG;
+    if (F < 1 || K < 1 || F > kGatedMost || K > kGatedMost || N > INT32_MAX || N * std::max(F, K) >= (int64_t)1 << 40)
+        return BSR_ERR_SHAPE;
+    return BSR_OK;
+}
+bool known(bsr_act_t a) { return a >= BSR_ACT_SILU && a <= BSR_ACT_SIGMOID; }
+
 }  // namespace
 
 extern "C" {
@@ -156,6 +168,74 @@ bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void
     if ((st = b.check()) != BSR_OK) return st;
     const RnBackward a{q, y, h_out, gate, dh_out, dz, dy, dh, g, N, static_cast<float *>(ws)};
     return launched(launch_residual_norm_backward(a, static_cast<cudaStream_t>(stream)));
+}
+
+bsr_status_t bsr_gated_workspace(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, int backward, size_t *bytes) {
+    if (!bytes) return BSR_ERR_INVALID_ARG;
+    *bytes = 0;
+    const bsr_status_t st = check_gated(N, F, K, dt);
+    if (st == BSR_OK) *bytes = (size_t)gated_workspace(N, F, K, dt, backward != 0);
+    return st;
+}
+
+bsr_status_t bsr_gated(const void *X, const void *Wg, const void *Wu, const float *bg, const float *bu, void *H, int64_t N,
+                       int64_t F, int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream) {
+    bsr_status_t st = check_gated(N, F, K, dt);
+    if (st != BSR_OK) return st;
+    if (!known(act)) return BSR_ERR_UNSUPPORTED;
+    if (N == 0) return BSR_OK;
+    if (!X || !Wg || !Wu || !H) return BSR_ERR_INVALID_ARG;
+    const size_t es = dtype_size(dt), need = (size_t)gated_workspace(N, F, K, dt, false);
+    if (need > ws_bytes) return BSR_ERR_CAPACITY;
+    if (need && !ws) return BSR_ERR_INVALID_ARG;
+    Buffers b;
+    b.in(X, (size_t)N * K * es);
+    for (const void *w : {Wg, Wu}) b.in(w, (size_t)F * K * es);
+    for (const float *v : {bg, bu}) b.in(v, (size_t)F * 4, 4);
+    b.out(H, (size_t)N * F * es);
+    b.out(ws, need);
+    if ((st = b.check()) != BSR_OK) return st;
+    GatedCall c = {X, Wg, Wu, bg, bu, N, F, K, dt, act, ws};
+    c.H = H;
+    return launched(launch_gated(c, static_cast<cudaStream_t>(stream)));
+}
+
+bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, const float *bg, const float *bu,
+                                const void *dH, void *dX, void *dWg, void *dWu, float *dbg, float *dbu, int64_t N, int64_t F,
+                                int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream) {
+    bsr_status_t st = check_gated(N, F, K, dt);
+    if (st != BSR_OK) return st;
+    if (!known(act)) return BSR_ERR_UNSUPPORTED;
+    if (!dWg != !dWu || (dbg && !bg) || (dbu && !bu)) return BSR_ERR_INVALID_ARG;
+    const size_t es = dtype_size(dt), need = (size_t)gated_workspace(N, F, K, dt, true);
+    Buffers b;
+    for (void *w : {dWg, dWu}) b.out(w, (size_t)F * K * es);
+    for (float *v : {dbg, dbu}) b.out(v, (size_t)F * 4, 4);
+    if (N > 0) {
+        if (!X || !Wg || !Wu || !dH) return BSR_ERR_INVALID_ARG;
+        if (need > ws_bytes) return BSR_ERR_CAPACITY;
+        if (need && !ws) return BSR_ERR_INVALID_ARG;
+        b.in(X, (size_t)N * K * es);
+        for (const void *w : {Wg, Wu}) b.in(w, (size_t)F * K * es);
+        for (const float *v : {bg, bu}) b.in(v, (size_t)F * 4, 4);
+        b.in(dH, (size_t)N * F * es);
+        b.out(dX, (size_t)N * K * es);
+        b.out(ws, need);
+    }
+    if ((st = b.check()) != BSR_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (N == 0) {   // sums of nothing
+        for (void *w : {dWg, dWu})
+            if (w && cudaMemsetAsync(w, 0, (size_t)F * K * es, s) != cudaSuccess) return launched(cudaErrorUnknown);
+        for (float *v : {dbg, dbu})
+            if (v && cudaMemsetAsync(v, 0, (size_t)F * 4, s) != cudaSuccess) return launched(cudaErrorUnknown);
+        return BSR_OK;
+    }
+    GatedCall c = {X, Wg, Wu, bg, bu, N, F, K, dt, act, ws};
+    c.dH = dH;
+    c.dX = dX, c.dWg = dWg, c.dWu = dWu;
+    c.dbg = dbg, c.dbu = dbu;
+    return launched(launch_gated_backward(c, s));
 }
 
 }  // extern "C"

@@ -52,3 +52,26 @@ def test_residual_norm_refusals(lib):
         g = b._ResidualNormGrads()
         setattr(g, name, 256)
         assert backward(op(), grads=g) == b.BSR_ERR_INVALID_ARG
+
+
+def test_gated_refusals(lib):
+    from paper_2106_08846_gb300 import bsrlib as b
+    d, e = ctypes.c_void_p(256), ctypes.c_void_p(1 << 30)
+    n = ctypes.c_size_t(7)
+    for N, F, K, dt, want in ((4, 64, 64, 2, b.BSR_ERR_UNSUPPORTED), (-1, 64, 64, 0, b.BSR_ERR_INVALID_ARG),
+                              (4, 0, 64, 0, b.BSR_ERR_SHAPE), (4, 64, 0, 0, b.BSR_ERR_SHAPE),
+                              (4, (1 << 20) + 1, 64, 0, b.BSR_ERR_SHAPE), (1 << 31, 64, 64, 0, b.BSR_ERR_SHAPE),
+                              (1 << 30, 64, 1 << 20, 0, b.BSR_ERR_SHAPE)):
+        assert lib.bsr_gated_workspace(N, F, K, dt, 0, ctypes.byref(n)) == want and n.value == 0
+        assert lib.bsr_gated(d, d, d, None, None, e, N, F, K, dt, 0, d, 1 << 40, None) == want
+        assert lib.bsr_gated_backward(d, d, d, None, None, d, e, None, None, None, None, N, F, K, dt, 0, d, 1 << 40, None) == want
+    assert lib.bsr_gated_workspace(4, 64, 64, 0, 0, None) == b.BSR_ERR_INVALID_ARG
+    for bad in (-1, 5):
+        assert lib.bsr_gated(d, d, d, None, None, e, 4, 64, 64, 0, bad, d, 1 << 40, None) == b.BSR_ERR_UNSUPPORTED
+    assert lib.bsr_gated(None, d, d, None, None, e, 4, 64, 64, 0, 0, d, 1 << 40, None) == b.BSR_ERR_INVALID_ARG
+    assert lib.bsr_gated(None, None, None, None, None, None, 0, 64, 64, 0, 0, None, 0, None) == b.BSR_OK
+
+    def backward(dWg=None, dWu=None, dbg=None, bg=None, dH=d):
+        return lib.bsr_gated_backward(d, d, d, bg, None, dH, e, dWg, dWu, dbg, None, 4, 64, 64, 0, 0, d, 1 << 40, None)
+
+    assert backward(dH=None) == backward(dWg=e) == backward(dWu=e) == backward(dbg=e) == b.BSR_ERR_INVALID_ARG
