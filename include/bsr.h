@@ -384,7 +384,13 @@ bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void
  * its feed-forward weights stay dense. H is what a down projection (bsr_spmm)
  * takes. X [N, K], Wg and Wu [F, K], H [N, F], row-major, element type dt; bg and
  * bu fp32 [F] or NULL. Sums are held in fp32 and G and U are not rounded before
- * H is. Sizes: F, K in 1 .. 2^20, N in 0 .. 2^31 - 1, N F and N K below 2^40.
+ * H is. Sizes: F, K in 1 .. 2^20, N in 0 .. 2^30, N F and N K below 2^38.
+ *
+ * fp32 operands run on the tensor cores as three bf16 parts each, whose sum they
+ * are, and a product as the six part products that are not below 2^-24 of it,
+ * added in fp32: |dG| <= 1e-5 (sum |x||w| + |b|), as for bsr_spmm. A token whose
+ * fp32 activations are not finite gives NaN where plain arithmetic might give an
+ * infinity.
  */
 typedef enum {
     BSR_ACT_SILU = 0,      /* g / (1 + e^-g) */
@@ -420,11 +426,19 @@ bsr_status_t bsr_gated(const void *X, const void *Wg, const void *Wu, const floa
  * fp32 [F]: written, not added to; each NULL where not wanted, but dWg and dWu
  * both or neither, and dbg or dbu only beside bg or bu. For N == 0 the weights'
  * gradients are zeros. No output overlaps another buffer. For BSR_BF16, dG and dU
- * are rounded to bf16 as operands of dX, dWg and dWu (not for dbg and dbu).
+ * are rounded as operands of dX, dWg and dWu (not for dbg and dbu): to bf16, and up
+ * to 128 tokens to 16 bits.
  */
 bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, const float *bg, const float *bu,
                                 const void *dH, void *dX, void *dWg, void *dWu, float *dbg, float *dbu, int64_t N, int64_t F,
                                 int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * bsr_check_status -- synchronise the current device and return the first error
+ * that a kernel of bsr_gated or bsr_gated_backward recorded there
+ * (BSR_ERR_TIMEOUT when a bounded wait gave up), then clear it. BSR_OK if none.
+ */
+bsr_status_t bsr_check_status(void);
 
 /* bsr_destroy -- release what the handle owns (not the borrowed arrays). NULL is a no-op. */
 void bsr_destroy(bsr_handle_t h);

@@ -124,6 +124,8 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.bsr_gated.restype = U
         lib.bsr_gated_backward.argtypes = [P] * 11 + [I64, I64, I64, U, I, P, ctypes.c_size_t, P]
         lib.bsr_gated_backward.restype = U
+        lib.bsr_check_status.argtypes = []
+        lib.bsr_check_status.restype = U
         lib.bsr_destroy.argtypes = [P]
         lib.bsr_destroy.restype = None
         lib.bsr_status_str.argtypes = [U]
@@ -390,6 +392,11 @@ def bsr_plan_create(handles, Xs, biases, Ys, Ns=None, independent: bool = False)
 
 def bsr_check_device_status(h: Handle) -> int:
     return load().bsr_check_device_status(h.ptr)
+
+
+def bsr_check_status() -> int:
+    """The first error that a kernel of bsr_gated or bsr_gated_backward recorded on the current device (synchronises it)."""
+    return load().bsr_check_status()
 
 
 def bsr_get_schedule(h: Handle) -> str:

@@ -7,13 +7,17 @@
 //   dG = dH U act'(G),  dU = dH act(G)
 //   dX = dG Wg + dU Wu,  dWg = dG' X,  dWu = dU' X,  dbg = sum dG,  dbu = sum dU
 //
-// in fp32 multiply-adds on 64 x 64 tiles staged through shared memory.
+// The products run on the tensor cores (gated_mma.cu). dG and dU stand side by
+// side in the workspace as one bf16 matrix [N, 2 Fp], so that dX is one product
+// over 2 Fp columns and dWg and dWu are one product of 2 Fp rows. Operands that
+// the copy engine cannot read in place are laid out first: fp32 ones as three
+// bf16 parts, bf16 ones whose rows do not start on 16-byte boundaries padded.
 #include <algorithm>
 
-#include "act.cuh"
 #include "bsr_internal.h"
 #include "elem.cuh"
 #include "gated.h"
+#include "gated_mma.h"
 #include "launch.cuh"
 #include "ptx.cuh"
 
@@ -21,137 +25,216 @@ namespace bsr {
 
 namespace {
 
-constexpr int T = 64, KS = 16;
-
-// One operand element (r, k) at p[r * rs + k * ks].
-template <typename E>
-struct Operand {
-    const E *p;
-    int64_t rs, ks, rows;
+// One matrix to lay out: rows x K values to parts of rows x Kp.
+struct Source {
+    const void *src;
+    uint16_t *dst;
+    int64_t rows;
+};
+struct Sources {
+    Source m[3];
+    int64_t K, Kp;
+    int vec;   // K is a multiple of 8 (rows start on 16-byte boundaries)
 };
 
-// acc (+)= A B' for a 64 x 64 tile at (m0, n0); 256 threads, 4 x 4 values each.
-template <typename A, typename B>
-__device__ __forceinline__ void tile_product(float (&acc)[4][4], Operand<A> a, Operand<B> b, int64_t K, int64_t m0, int64_t n0) {
-    __shared__ float as[KS][T + 1], bs[KS][T + 1];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int64_t k0 = 0; k0 < K; k0 += KS) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < T * KS; e += 256) {
-            // neighbours along the contiguous side
-            const int ra = a.ks == 1 ? e / KS : e % T, ka = a.ks == 1 ? e % KS : e / T;
-            as[ka][ra] = m0 + ra < a.rows && k0 + ka < K ? to_f32(a.p[(m0 + ra) * a.rs + (k0 + ka) * a.ks]) : 0.f;
-            const int rb = b.ks == 1 ? e / KS : e % T, kb = b.ks == 1 ? e % KS : e / T;
-            bs[kb][rb] = n0 + rb < b.rows && k0 + kb < K ? to_f32(b.p[(n0 + rb) * b.rs + (k0 + kb) * b.ks]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < KS; k++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = fmaf(as[k][ty + 16 * i], bs[k][tx + 16 * j], acc[i][j]);
-    }
-}
+__device__ __forceinline__ uint16_t cut(float x) { return (uint16_t)(__float_as_uint(x) >> 16); }
 
-template <typename E, bool BACK>
-__global__ void __launch_bounds__(256) k_gated(const __grid_constant__ GatedCall c, float *dG, float *dU) {
+// Eight columns a thread. fp32: three parts, cut off and not rounded, so that
+// none overflows; a value that is not finite goes into the first part alone.
+template <typename T>
+__global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources a) {
+    constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
-    const int64_t n0 = (int64_t)blockIdx.y * T, f0 = (int64_t)blockIdx.x * T;
-    float g[4][4] = {}, u[4][4] = {};
-    const Operand<E> x{static_cast<const E *>(c.X), c.K, 1, c.N};
-    tile_product(g, x, Operand<E>{static_cast<const E *>(c.Wg), c.K, 1, c.F}, c.K, n0, f0);
-    tile_product(u, x, Operand<E>{static_cast<const E *>(c.Wu), c.K, 1, c.F}, c.K, n0, f0);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) {
-            const int64_t n = n0 + ty + 16 * i, f = f0 + tx + 16 * j, at = n * c.F + f;
-            if (n >= c.N || f >= c.F) continue;
-            const float gv = g[i][j] + (c.bg ? c.bg[f] : 0.f), uv = u[i][j] + (c.bu ? c.bu[f] : 0.f);
-            if constexpr (BACK) {
-                const float d = to_f32(static_cast<const E *>(c.dH)[at]);
-                const float2 a = activate_slope<false>(c.act, gv);
-                dG[at] = d * uv * a.y;
-                dU[at] = d * a.x;
+    const Source m = a.m[blockIdx.y];
+    const int64_t eights = a.Kp / 8, total = m.rows * eights;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / eights, c = (i - row * eights) * 8;
+        const T *src = static_cast<const T *>(m.src) + row * a.K + c;
+        uint16_t out[PARTS][8];
+        if constexpr (PARTS == 1) {
+#pragma unroll
+            for (int j = 0; j < 8; j++) out[0][j] = c + j < a.K ? __ldg(src + j) : (uint16_t)0;
+        } else {
+            float v[8];
+            if (a.vec) {
+                const float4 p = __ldg(reinterpret_cast<const float4 *>(src)), q = __ldg(reinterpret_cast<const float4 *>(src) + 1);
+                v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
             } else {
-                static_cast<E *>(c.H)[at] = from_f32<E>(activate<false>(c.act, gv) * uv);
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[j] = c + j < a.K ? __ldg(src + j) : 0.f;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; j++) {
+                const bool finite = (__float_as_uint(v[j]) & 0x7f800000u) != 0x7f800000u;
+                const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u), r = finite ? v[j] - hi : 0.f;
+                out[0][j] = finite ? cut(hi) : from_f32<uint16_t>(v[j]);
+                out[1][j] = cut(r);
+                out[2][j] = cut(r - __uint_as_float(__float_as_uint(r) & 0xffff0000u));
             }
         }
-}
-
-// out[m, n] = A0 B0' + A1 B1' (K columns each; A1.p may be NULL), row-major with n_cols columns
-template <typename E>
-__global__ void __launch_bounds__(256) k_product(Operand<float> a0, Operand<E> b0, Operand<float> a1, Operand<E> b1, int64_t K,
-                                                 E *out) {
-    ptx::pdl_launch_dependents();
-    ptx::pdl_wait();
-    const int64_t m0 = (int64_t)blockIdx.y * T, n0 = (int64_t)blockIdx.x * T;
-    float acc[4][4] = {};
-    tile_product(acc, a0, b0, K, m0, n0);
-    if (a1.p) tile_product(acc, a1, b1, K, m0, n0);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) {
-            const int64_t m = m0 + ty + 16 * i, n = n0 + tx + 16 * j;
-            if (m < a0.rows && n < b0.rows) out[m * b0.rows + n] = from_f32<E>(acc[i][j]);
+#pragma unroll
+        for (int p = 0; p < PARTS; p++) {
+            uint32_t w[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) w[j] = out[p][2 * j] | (uint32_t)out[p][2 * j + 1] << 16;
+            *reinterpret_cast<uint4 *>(m.dst + ((int64_t)p * m.rows + row) * a.Kp + c) = make_uint4(w[0], w[1], w[2], w[3]);
         }
+    }
 }
 
-// out[f] = sum over n of d[n, f], a column a thread
-__global__ void __launch_bounds__(256) k_column_sums(const float *d, int64_t N, int64_t F, float *out) {
+// dbg and dbu: the sums of the 2 Fp columns of `sums` [n, 2 Fp], 32 columns a
+// CTA: 32 x 8 threads, each every eighth row, then the eight.
+__global__ void __launch_bounds__(256) k_bias_sums(const float *sums, int64_t n, int64_t F, int64_t Fp, float *dbg, float *dbu) {
+    __shared__ float part[8][33];
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
-    const int64_t f = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (f >= F) return;
+    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
     float s = 0.f;
-    for (int64_t n = 0; n < N; n++) s += d[n * F + f];
-    out[f] = s;
+    for (int64_t k = threadIdx.y; k < n; k += 8) s += sums[k * 2 * Fp + c];
+    part[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    if (threadIdx.y) return;
+    s = 0.f;
+    for (int k = 0; k < 8; k++) s += part[k][threadIdx.x];
+    float *out = c < Fp ? dbg : dbu;
+    const int64_t f = c < Fp ? c : c - Fp;
+    if (out && f < F) out[f] = s;
 }
 
-unsigned tiles(int64_t n) { return (unsigned)((n + T - 1) / T); }
+int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-template <typename E>
-cudaError_t forward(const GatedCall &c, cudaStream_t s) {
-    return launch_kernel(k_gated<E, false>, dim3(tiles(c.F), tiles(c.N)), dim3(256), 0, s, c, (float *)nullptr, (float *)nullptr);
-}
+// The workspace of a call, and its products.
+struct Plan {
+    int parts, d_parts;   // bf16 matrices to an operand, and to dG and dU
+    bool lay_out;
+    int64_t Kp, Fp;
+    int64_t x_at, wg_at, wu_at, d_at, sums_at, parts_at, bytes;
+    GatedMma main, dx, dw;
+};
 
-template <typename E>
-cudaError_t backward(const GatedCall &c, cudaStream_t s) {
-    float *dG = static_cast<float *>(c.ws), *dU = dG + c.N * c.F;
-    const E *X = static_cast<const E *>(c.X), *Wg = static_cast<const E *>(c.Wg), *Wu = static_cast<const E *>(c.Wu);
-    cudaError_t e = cudaSuccess;
-    if (c.N > 0) e = launch_kernel(k_gated<E, true>, dim3(tiles(c.F), tiles(c.N)), dim3(256), 0, s, c, dG, dU);
-    if (e == cudaSuccess && c.dX && c.N > 0)
-        e = launch_kernel(k_product<E>, dim3(tiles(c.K), tiles(c.N)), dim3(256), 0, s, Operand<float>{dG, c.F, 1, c.N},
-                          Operand<E>{Wg, 1, c.K, c.K}, Operand<float>{dU, c.F, 1, c.N}, Operand<E>{Wu, 1, c.K, c.K}, c.F,
-                          static_cast<E *>(c.dX));
-    for (int i = 0; i < 2; i++) {
-        const float *d = i ? dU : dG;
-        void *dW = i ? c.dWu : c.dWg;
-        float *db = i ? c.dbu : c.dbg;
-        if (e == cudaSuccess && dW)
-            e = launch_kernel(k_product<E>, dim3(tiles(c.K), tiles(c.F)), dim3(256), 0, s, Operand<float>{d, 1, c.F, c.F},
-                              Operand<E>{X, 1, c.K, c.K}, Operand<float>{nullptr, 1, 1, 0}, Operand<E>{nullptr, 1, 1, 0}, c.N,
-                              static_cast<E *>(dW));
-        if (e == cudaSuccess && db)
-            e = launch_kernel(k_column_sums, dim3((unsigned)((c.F + 255) / 256)), dim3(256), 0, s, d, c.N, c.F, db);
+// Up to this many tokens the weights' and their gradients' bytes bound the
+// products, and a second part of dG and dU, which keeps 16 of their bits, costs
+// next to nothing; a gradient of few tokens is a sum of few terms, in which
+// roundings to 8 bits do not average out.
+constexpr int64_t kFewTokens = 128;
+
+Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
+    Plan p = {};
+    p.parts = dt == BSR_F32 ? 3 : 1;
+    p.d_parts = dt == BSR_F32 ? 3 : N <= kFewTokens ? 2 : 1;
+    p.lay_out = dt == BSR_F32 || K % 8 != 0;
+    p.Kp = round_up(K, 8);
+    p.Fp = backward ? round_up(F, 64) : F;
+    auto take = [&](int64_t bytes) {
+        const int64_t at = p.bytes;
+        p.bytes += round_up(bytes, 256);
+        return at;
+    };
+    if (p.lay_out) {
+        p.x_at = take(p.parts * N * p.Kp * 2);
+        p.wg_at = take(p.parts * F * p.Kp * 2);
+        p.wu_at = take(p.parts * F * p.Kp * 2);
     }
-    return e;
+    GatedMma &m = p.main;
+    m.mode = backward ? GM_BACKWARD : GM_FORWARD;
+    m.a.planes = p.parts;
+    m.M = N, m.N = F, m.K = K, m.Fp = p.Fp;
+    plan_gated_mma(m);
+    if (!backward) return p;
+    p.d_at = take(p.d_parts * N * 2 * p.Fp * 2);
+    p.sums_at = take((N + 31) / 32 * 2 * p.Fp * 4);
+    GatedMma &x = p.dx, &w = p.dw;
+    x.mode = w.mode = GM_PRODUCT;
+    x.a.planes = w.a.planes = m.d_planes = p.d_parts;
+    x.M = N, x.N = K, x.K = 2 * p.Fp;
+    x.b_side = true;
+    x.b_seam = p.Fp;
+    x.row_seam = x.out_rows = N;
+    w.M = 2 * p.Fp, w.N = K, w.K = N;
+    w.a_side = w.b_side = true;
+    w.row_seam = p.Fp, w.out_rows = F;
+    plan_gated_mma(x);
+    plan_gated_mma(w);
+    int64_t most = 0;
+    for (const GatedMma *g : {&x, &w})
+        if (g->splits > 1) most = std::max(most, g->splits * g->M * g->part_ld * 4);
+    p.parts_at = take(most);
+    return p;
+}
+
+// The operands X, Wg and Wu as the tensor cores read them.
+cudaError_t operands(const GatedCall &c, const Plan &p, Planes (&m)[3], cudaStream_t s) {
+    const void *src[3] = {c.X, c.Wg, c.Wu};
+    const int64_t rows[3] = {c.N, c.F, c.F}, at[3] = {p.x_at, p.wg_at, p.wu_at};
+    Sources a;
+    a.K = c.K, a.Kp = p.Kp;
+    a.vec = c.K % 8 == 0;
+    for (int i = 0; i < 3; i++) {
+        uint16_t *dst = reinterpret_cast<uint16_t *>(static_cast<unsigned char *>(c.ws) + at[i]);
+        a.m[i] = Source{src[i], dst, rows[i]};
+        m[i] = Planes{p.lay_out ? dst : static_cast<const uint16_t *>(src[i]), rows[i], p.lay_out ? p.Kp : c.K, p.lay_out ? p.Kp : c.K,
+                      p.parts};
+    }
+    if (!p.lay_out) return cudaSuccess;
+    const int64_t blocks = (std::max(c.N, c.F) * (p.Kp / 8) + 255) / 256;
+    const dim3 grid((unsigned)std::min<int64_t>(blocks, 2048), 3);
+    return c.dt == BSR_F32 ? launch_kernel(k_lay_out<float>, grid, dim3(256), 0, s, a)
+                           : launch_kernel(k_lay_out<uint16_t>, grid, dim3(256), 0, s, a);
 }
 
 }  // namespace
 
 int64_t gated_workspace(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
-    return backward ? 2 * N * F * 4 : 0;
+    return N == 0 ? 0 : plan_of(N, F, K, dt, backward).bytes;
 }
 
 cudaError_t launch_gated(const GatedCall &c, cudaStream_t s) {
-    return c.dt == BSR_F32 ? forward<float>(c, s) : forward<uint16_t>(c, s);
+    Plan p = plan_of(c.N, c.F, c.K, c.dt, false);
+    Planes m[3];
+    cudaError_t e = operands(c, p, m, s);
+    if (e != cudaSuccess) return e;
+    GatedMma &g = p.main;
+    g.dt = c.dt;
+    g.a = m[0], g.b0 = m[1], g.b1 = m[2];
+    g.bg = c.bg, g.bu = c.bu;
+    g.act = c.act;
+    g.H = c.H;
+    return launch_gated_mma(g, s);
 }
 
 cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
-    return c.dt == BSR_F32 ? backward<float>(c, s) : backward<uint16_t>(c, s);
+    Plan p = plan_of(c.N, c.F, c.K, c.dt, true);
+    unsigned char *ws = static_cast<unsigned char *>(c.ws);
+    Planes m[3];
+    cudaError_t e = operands(c, p, m, s);
+    if (e != cudaSuccess) return e;
+    GatedMma &g = p.main;
+    g.dt = p.dx.dt = p.dw.dt = c.dt;
+    g.a = m[0], g.b0 = m[1], g.b1 = m[2];
+    g.bg = c.bg, g.bu = c.bu;
+    g.act = c.act;
+    g.dH = c.dH;
+    g.D = reinterpret_cast<uint16_t *>(ws + p.d_at);
+    g.sums = c.dbg || c.dbu ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
+    e = launch_gated_mma(g, s);
+    const Planes d{g.D, c.N, 2 * p.Fp, 2 * p.Fp, p.d_parts};
+    if (e == cudaSuccess && c.dX) {
+        p.dx.a = d, p.dx.b0 = m[1], p.dx.b1 = m[2];
+        p.dx.out0 = p.dx.out1 = c.dX;
+        p.dx.parts = reinterpret_cast<float *>(ws + p.parts_at);
+        e = launch_gated_mma(p.dx, s);
+    }
+    if (e == cudaSuccess && c.dWg) {
+        p.dw.a = d, p.dw.b0 = m[0];
+        p.dw.out0 = c.dWg, p.dw.out1 = c.dWu;
+        p.dw.parts = reinterpret_cast<float *>(ws + p.parts_at);
+        e = launch_gated_mma(p.dw, s);
+    }
+    if (e == cudaSuccess && g.sums)
+        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 8), 0, s, (const float *)g.sums, (c.N + 31) / 32, c.F,
+                          p.Fp, c.dbg, c.dbu);
+    return e;
 }
 
 }  // namespace bsr

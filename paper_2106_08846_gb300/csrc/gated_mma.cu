@@ -1,0 +1,794 @@
+// The products of the gated feed-forward block on the tensor cores.
+//
+// One kernel for three of them: G and U with the activation and the product (or
+// its derivatives) on the way out, and the plain products of the backward pass.
+// A cluster of two CTAs works on a tile of 256 rows by 2 `half` columns; in the
+// gated modes one CTA loads `half` rows of Wg and the other of Wu, so that the
+// same thread finds G and U of a feature in its tensor-memory lane.
+//
+//   warp 0     A tiles by TMA (128-byte swizzle), 128 rows x 64 of K a CTA
+//   warp 1     B tiles, `half` rows x 64
+//   warp 2     MMAs (M = 256, N = 2 half, K = 16) of the pair's first CTA
+//   warps 4-11 epilogue: 32 rows and half of the columns each, straight from
+//              tensor memory to global memory
+//
+// Persistent: one CTA per SM; two accumulator buffers of 256 columns let a
+// tile's epilogue overlap the next tile's MMAs.
+//
+// Operands stored with K along rows (weights for dX; dG, dU and X for the
+// weights' gradients) are read in place: TMA boxes of 64 x 64 and descriptors
+// with M or N contiguous.
+//
+// fp32 operands come as three bf16 parts whose sum they are (8 bits of the
+// significand each), and a product is the six of nine part products that are not
+// below 2^-24 of it (bf16 products may have an A of two parts). The tensor cores' fp32 accumulation drops bits with every
+// addition, so the small products of 256 columns of K come first and the
+// accumulators are added to registers after every 256 columns.
+//
+// Every wait is bounded by the global timer; a timeout is recorded, stops every
+// role, lets the issued copies and MMAs finish, frees the tensor memory and
+// returns.
+#include <algorithm>
+#include <atomic>
+#include <cstdlib>
+
+#include "act.cuh"
+#include "bsr_internal.h"
+#include "elem.cuh"
+#include "gated_mma.h"
+#include "launch.cuh"
+#include "ptx.cuh"
+#include "status.cuh"
+#include "tcgen05.cuh"
+
+namespace bsr {
+
+namespace {
+
+constexpr int KC = 64;                        // columns of K per chunk
+constexpr uint32_t kABytes = 128 * 128;       // a CTA's A tile
+constexpr int kEpiWarps = 8, kEpiWarp0 = 4, kMmaWarp = 2;
+constexpr int kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kStages = 8;
+constexpr uint32_t kBiasBytes = kEpiWarps * 128 * 4;
+constexpr uint32_t kMaxSmem = 227 * 1024 - 1024;
+constexpr uint32_t kAccCols = 256;
+constexpr int kDrainChunks = 4;               // fp32: columns of K between additions to registers, in chunks
+constexpr int kPairs = 6;
+constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
+
+__device__ int g_status;
+
+struct Args {
+    CUtensorMap a, b0, b1;
+    int64_t M, N;             // rows; columns (gated modes: features)
+    unsigned tiles_n, units;
+    int splits, chunks, seam; // chunks of K in all; the chunk from which b1 is read
+    int half, ns;
+    int pairs;                // pairs of parts that are multiplied
+    uint32_t stage_bytes, idesc;
+    int a_side, b_side;
+    const float *bg, *bu;
+    int act;
+    const void *dH;
+    void *out0, *out1;        // gated forward: H in out0
+    uint16_t *D;
+    int d_planes;
+    int64_t Fp;
+    float *sums;
+    int64_t row_seam, out_rows;
+    float *parts;
+    int64_t part_ld;
+    int vec;                  // output (and dH) rows start on 32-byte boundaries
+    uint64_t wait_ns;
+    int stall_chunk;          // test hook: this step of each unit is never loaded by warp 0 (-1: none)
+};
+
+struct Unit {
+    int64_t m0, n0;   // first row, first column (gated modes: feature)
+    int c0, c1;       // chunks
+    int split;
+};
+
+template <int MODE>
+__device__ __forceinline__ Unit unit_at(const Args &a, unsigned v) {
+    Unit u;
+    u.split = 0;
+    if (MODE == GM_PRODUCT && a.splits > 1) {
+        u.split = (int)(v % (unsigned)a.splits);
+        v /= (unsigned)a.splits;
+    }
+    const unsigned tm = v / a.tiles_n, tn = v - tm * a.tiles_n;
+    u.m0 = (int64_t)tm * 256;
+    u.n0 = (int64_t)tn * (MODE == GM_PRODUCT ? 2 * a.half : a.half);
+    u.c0 = (int)((int64_t)a.chunks * u.split / a.splits);
+    u.c1 = (int)((int64_t)a.chunks * (u.split + 1) / a.splits);
+    return u;
+}
+
+// The steps of a unit: a block of chunks after another (fp32: of kDrainChunks;
+// bf16: all of them), and a block's chunks once for each pair of parts, the
+// smallest products first.
+template <bool F32>
+struct Steps {
+    int c, c1, b0, left;   // chunk, end; the block's first chunk, and the pairs of parts after this one
+    __device__ __forceinline__ void start(const Args &a, const Unit &u) {
+        c = b0 = u.c0;
+        c1 = u.c1;
+        left = a.pairs - 1;
+    }
+    __device__ __forceinline__ bool done() const { return b0 >= c1; }
+    __device__ __forceinline__ int block_end() const { return F32 ? min(b0 + kDrainChunks, c1) : c1; }
+    // moves on; true at a block's end
+    __device__ __forceinline__ bool next(const Args &a) {
+        c++;
+        if (c < block_end()) return false;
+        if (left > 0) {
+            left--;
+            c = b0;
+            return false;
+        }
+        left = a.pairs - 1;
+        c = b0 = block_end();
+        return true;
+    }
+    // three parts: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0); two of A: (1,0) (0,0)
+    __device__ __forceinline__ int a_part() const { return F32 ? (0x210100 >> (4 * left)) & 3 : left; }
+    __device__ __forceinline__ int b_part() const { return F32 ? (0x012010 >> (4 * left)) & 3 : 0; }
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// 16 values to row p (column c of `cols`): at once where `vec` and all are there.
+__device__ __forceinline__ void store16(uint16_t *row, int64_t c, int64_t cols, bool vec, const float (&v)[16]) {
+    if (vec && c + 16 <= cols) {
+        uint32_t r[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) r[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        ptx::st_global_32(row + c, r);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; j++)
+            if (c + j < cols) row[c + j] = from_f32<uint16_t>(v[j]);
+    }
+}
+__device__ __forceinline__ void store16(float *row, int64_t c, int64_t cols, bool vec, const float (&v)[16]) {
+    if (vec && c + 16 <= cols) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            uint32_t r[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) r[j] = __float_as_uint(v[8 * h + j]);
+            ptx::st_global_32(row + c + 8 * h, r);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; j++)
+            if (c + j < cols) row[c + j] = v[j];
+    }
+}
+// 16 values of a row; 0 past its end
+__device__ __forceinline__ void load16(const uint16_t *row, int64_t c, int64_t cols, bool vec, float (&v)[16]) {
+    if (vec && c + 16 <= cols) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(row + c) + h);
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                v[8 * h + 2 * j] = __uint_as_float(w[j] << 16);
+                v[8 * h + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; j++) v[j] = c + j < cols ? to_f32(__ldg(row + c + j)) : 0.f;
+    }
+}
+__device__ __forceinline__ void load16(const float *row, int64_t c, int64_t cols, bool vec, float (&v)[16]) {
+    if (vec && c + 16 <= cols) {
+#pragma unroll
+        for (int h = 0; h < 4; h++) {
+            const float4 q = __ldg(reinterpret_cast<const float4 *>(row + c) + h);
+            v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; j++) v[j] = c + j < cols ? __ldg(row + c + j) : 0.f;
+    }
+}
+
+// Sums of 16 values over a warp's lanes: lane l gets that of value l % 16.
+__device__ __forceinline__ float lane_sums(const float (&v)[16]) {
+    const int lane = threadIdx.x & 31;
+    float a[8], b[4], c[2];
+#pragma unroll
+    for (int j = 0; j < 8; j++) {   // lanes with bit 3 keep the upper eight
+        const float mine = lane & 8 ? v[j + 8] : v[j], other = lane & 8 ? v[j] : v[j + 8];
+        a[j] = mine + __shfl_xor_sync(0xffffffffu, other, 8);
+    }
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const float mine = lane & 4 ? a[j + 4] : a[j], other = lane & 4 ? a[j] : a[j + 4];
+        b[j] = mine + __shfl_xor_sync(0xffffffffu, other, 4);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        const float mine = lane & 2 ? b[j + 2] : b[j], other = lane & 2 ? b[j] : b[j + 2];
+        c[j] = mine + __shfl_xor_sync(0xffffffffu, other, 2);
+    }
+    const float mine = lane & 1 ? c[1] : c[0], other = lane & 1 ? c[0] : c[1];
+    const float s = mine + __shfl_xor_sync(0xffffffffu, other, 1);
+    return s + __shfl_xor_sync(0xffffffffu, s, 16);
+}
+
+// The three bf16 parts of a finite fp32 value, cut off and not rounded, so that
+// none overflows: their sum is the value.
+__device__ __forceinline__ void parts_of(float x, float (&p)[3]) {
+    p[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
+    if (!finite) p[0] = x;   // (an infinity, or a NaN of which the cut could make one)
+    const float r = finite ? x - p[0] : 0.f;
+    p[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
+    p[2] = r - p[1];
+}
+
+// Puts out 16 columns of this thread's row: gated modes G in v and U in w of
+// features f ..; GM_PRODUCT columns c .. in v and c + 16 .. in w.
+template <int MODE, typename T>
+__device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, int64_t c, float (&v)[16], float (&w)[16],
+                                    const float *bias_g, const float *bias_u, const float (&d)[16]) {
+    constexpr bool FAST = sizeof(T) == 2;
+    if constexpr (MODE != GM_PRODUCT) {
+        if (a.bg) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 b = *reinterpret_cast<const float4 *>(bias_g + j);
+                v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
+            }
+        }
+        if (a.bu) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                const float4 b = *reinterpret_cast<const float4 *>(bias_u + j);
+                w[j] += b.x, w[j + 1] += b.y, w[j + 2] += b.z, w[j + 3] += b.w;
+            }
+        }
+    }
+    if constexpr (MODE == GM_FORWARD) {
+        with_act(a.act, [&](auto tag) {
+#pragma unroll
+            for (int j = 0; j < 16; j++) v[j] = activate<decltype(tag)::value, FAST>(v[j]) * w[j];
+        });
+        if (row < a.M) store16(static_cast<T *>(a.out0) + row * a.N, c, a.N, a.vec, v);
+    } else if constexpr (MODE == GM_BACKWARD) {
+        with_act(a.act, [&](auto tag) {
+#pragma unroll
+            for (int j = 0; j < 16; j++) {
+                const float2 s = activate_slope<decltype(tag)::value, FAST>(v[j]);
+                v[j] = d[j] * w[j] * s.y;
+                w[j] = d[j] * s.x;
+            }
+        });
+        if (row >= a.M) {   // (the sums below)
+#pragma unroll
+            for (int j = 0; j < 16; j++) v[j] = w[j] = 0.f;
+        }
+        if (a.sums && c < a.Fp) {
+            const float sg = lane_sums(v), su = lane_sums(w);
+            const int lane = threadIdx.x & 31;
+            float *at = a.sums + (row >> 5) * 2 * a.Fp + c;
+            if ((row & ~(int64_t)31) < a.M) at[lane < 16 ? lane : a.Fp + lane - 16] = lane < 16 ? sg : su;
+        }
+        if (row < a.M && c < a.Fp) {
+            uint16_t *at = a.D + row * 2 * a.Fp + c;
+            if constexpr (FAST) {
+                store16(at, 0, 16, true, v);
+                store16(at + a.Fp, 0, 16, true, w);
+                if (a.d_planes == 2) {   // what the rounding left
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {
+                        v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+                        w[j] -= __bfloat162float(__float2bfloat16_rn(w[j]));
+                    }
+                    at += 2 * a.Fp * a.M;
+                    store16(at, 0, 16, true, v);
+                    store16(at + a.Fp, 0, 16, true, w);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2; k++) {
+                    float p[3][16];
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {
+                        float q[3];
+                        parts_of(k ? w[j] : v[j], q);
+                        p[0][j] = q[0], p[1][j] = q[1], p[2][j] = q[2];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 3; i++) store16(at + k * a.Fp + i * 2 * a.Fp * a.M, 0, 16, true, p[i]);
+                }
+            }
+        }
+    } else {
+        if (row >= a.M) return;
+        if (a.splits > 1) {
+            float *at = a.parts + ((int64_t)u.split * a.M + row) * a.part_ld;
+            store16(at, c, a.part_ld, true, v);
+            store16(at, c + 16, a.part_ld, true, w);
+            return;
+        }
+        const bool second = row >= a.row_seam;
+        const int64_t r = second ? row - a.row_seam : row;
+        if (r >= a.out_rows) return;
+        T *out = static_cast<T *>(second ? a.out1 : a.out0) + r * a.N;
+        store16(out, c, a.N, a.vec, v);
+        store16(out, c + 16, a.N, a.vec, w);
+    }
+}
+
+template <int MODE, typename T>
+__global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant__ Args a) {
+    constexpr bool F32 = sizeof(T) == 4;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char *base = ptx::align_smem(smem_raw);
+    const int ns = a.ns;
+    const uint32_t stage_bytes = a.stage_bytes;
+    float *bias_s = reinterpret_cast<float *>(base + (size_t)ns * stage_bytes);
+    __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], done;
+    __shared__ int stop, loads[2][2];   // loads[producer][CTA of the pair]: loads issued
+    __shared__ int freed, handed;       // commits issued to `empty` and to `acc_full`
+    __shared__ uint32_t tmem_s;
+
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_rank();
+    const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < ns; s++) {
+            ptx::mbar_init(&full[s], 2);   // the producers' arrivals, and their bytes
+            ptx::mbar_init(&empty[s], 1);
+        }
+        for (int i = 0; i < 2; i++) {
+            ptx::mbar_init(&acc_full[i], 1);
+            ptx::mbar_init(&acc_empty[i], 2 * kEpiWarps);
+        }
+        ptx::mbar_init(&done, 1);
+        stop = freed = handed = 0;
+        loads[0][0] = loads[0][1] = loads[1][0] = loads[1][1] = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, 2 * kAccCols);
+    tc5::fence_before();
+    __syncthreads();
+    ptx::cluster_barrier();   // the other CTA's barriers exist
+    tc5::fence_after();
+    ptx::pdl_launch_dependents();   // (after the allocation: ptx.cuh)
+    const uint32_t tmem = tmem_s;
+    const bool elected = ptx::elect_one();
+    // stops every role of this pair; a timeout is recorded
+    auto halt = [&]() {
+        if (elected) {
+            if (!aborted(&stop)) set_status(&g_status, DEV_TIMEOUT);
+            atomicExch(&stop, 1);
+            ptx::store_cluster(ptx::map_to_cta(&stop, rank ^ 1), 1);
+        }
+    };
+
+    // ---- producers: warp 0 A tiles, warp 1 B tiles
+    const int prod = warp;
+    unsigned v = pair;
+    Unit un = {};
+    Steps<F32> st = {};
+    int s = 0, issued = 0;
+    uint32_t phase = 1;     // the parity of `empty` that a first use of a stage passes at once
+    uint32_t stalled = 0;   // test hook: stages whose load was left out
+    const uint32_t bytes = prod ? 2 * (uint32_t)a.half * 128 : 2 * kABytes;   // of both CTAs
+    const uint32_t dst0 = ptx::smem_addr(base) + (prod ? kABytes : 0), bar0 = ptx::smem_addr(&full[0]);
+    const uint32_t first0 = ptx::map_to_cta(&full[0], 0);   // `full` of the pair's first CTA
+    auto load_step = [&]() {
+        if (prod == 0 && a.stall_chunk >= 0 && st.c == a.stall_chunk) {   // never loaded: its consumer times out
+            stalled |= 1u << s;
+        } else if (elected) {
+            const uint32_t dst = dst0 + s * stage_bytes, bar = first0 + 8 * s;
+            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, bytes);
+            if (prod == 0) {
+                const int m = (int)(un.m0 + rank * 128), k = st.c * KC;
+                if (a.a_side) {
+                    ptx::tma_load_3d_pair_at(dst, &a.a, m, k, st.a_part(), bar);
+                    ptx::tma_load_3d_pair_at(dst + 8192, &a.a, m + 64, k, st.a_part(), bar);
+                } else {
+                    ptx::tma_load_3d_pair_at(dst, &a.a, k, m, st.a_part(), bar);
+                }
+            } else if (MODE != GM_PRODUCT) {
+                ptx::tma_load_3d_pair_at(dst, rank ? &a.b1 : &a.b0, st.c * KC, (int)un.n0, st.b_part(), bar);
+            } else {
+                const bool second = a.seam && st.c >= a.seam;
+                const int n = (int)(un.n0 + rank * a.half), k = (second ? st.c - a.seam : st.c) * KC;
+                const CUtensorMap *map = second ? &a.b1 : &a.b0;
+                if (a.b_side) {
+                    for (int j = 0; j < a.half; j += 64)
+                        ptx::tma_load_3d_pair_at(dst + 128 * j, map, n + j, k, st.b_part(), bar);
+                } else {
+                    ptx::tma_load_3d_pair_at(dst, map, k, n, st.b_part(), bar);
+                }
+            }
+        }
+        issued++;
+        if (++s == ns) {
+            s = 0;
+            phase ^= 1;
+        }
+        st.next(a);
+        if (!st.done()) return true;
+        v += pairs;
+        if (v >= a.units) return false;
+        un = unit_at<MODE>(a, v);
+        st.start(a, un);
+        return true;
+    };
+    bool more = false;
+    if (warp < 2) {
+        if (elected) {
+            ptx::prefetch_tensormap(prod ? &a.b0 : &a.a);
+            if (prod) ptx::prefetch_tensormap(&a.b1);
+        }
+        more = v < a.units;
+        if (more) {
+            un = unit_at<MODE>(a, v);
+            st.start(a, un);
+        }
+        ptx::pdl_wait();   // every operand may be an earlier kernel's output
+        while (more) {
+            const bool got = wait_or_abort(&empty[s], phase, a.wait_ns, &stop);
+            if (!__all_sync(0xffffffffu, got && !aborted(&stop))) {
+                halt();
+                break;
+            }
+            more = load_step();
+        }
+        if (elected) {
+            loads[prod][rank] = issued;
+            ptx::store_cluster(ptx::map_to_cta(&loads[prod][rank], rank ^ 1), (uint32_t)issued);
+        }
+    } else if (warp == kMmaWarp) {
+        if (rank == 0) {
+            int ab = 0, n_freed = 0, n_handed = 0;
+            uint32_t fphase = 0, aphase = 1;
+            bool ok = true;
+            const uint32_t smem0 = ptx::smem_addr(base);
+            const uint64_t ad0 = a.a_side ? tc5::desc_sw128_mn(smem0, 8192) : tc5::desc_sw128(smem0);
+            const uint64_t bd0 = a.b_side ? tc5::desc_sw128_mn(smem0 + kABytes, 8192) : tc5::desc_sw128(smem0 + kABytes);
+            // 16 of K: two groups of eight 128-byte rows, or 32 bytes along the rows
+            const uint32_t a_step = a.a_side ? 128 : 2, b_step = a.b_side ? 128 : 2;
+            ptx::pdl_wait();   // the waits below are bounded from here on
+            for (; ok && v < a.units; v += pairs) {
+                un = unit_at<MODE>(a, v);
+                st.start(a, un);
+                while (ok && !st.done()) {   // a block of steps into one accumulator buffer
+                    const uint32_t d = tmem + (uint32_t)ab * kAccCols;
+                    ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[ab], aphase, a.wait_ns, &stop));
+                    tc5::fence_after();
+                    uint32_t acc = 0;
+                    for (bool last = false; ok && !last;) {
+                        ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
+                        if (!ok) break;
+                        tc5::fence_after();
+                        if (elected) {
+                            const uint64_t ad = ad0 + (uint64_t)((s * stage_bytes) >> 4), bd = bd0 + (uint64_t)((s * stage_bytes) >> 4);
+#pragma unroll
+                            for (int j = 0; j < KC / 16; j++)
+                                tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, a.idesc, acc | (j > 0));
+                            tc5::commit_pair(&empty[s]);
+                        }
+                        __syncwarp();
+                        acc = 1;
+                        n_freed++;
+                        if (++s == ns) {
+                            s = 0;
+                            fphase ^= 1;
+                        }
+                        last = st.next(a);
+                    }
+                    if (!ok) break;
+                    if (elected) tc5::commit_pair(&acc_full[ab]);
+                    __syncwarp();
+                    n_handed++;
+                    ab ^= 1;
+                    if (ab == 0) aphase ^= 1;
+                }
+                if (!ok) halt();
+            }
+            // every MMA issued has completed before the tensor memory is freed
+            if (elected) {
+                tc5::commit_pair(&done);
+                freed = n_freed;
+                handed = n_handed;
+                ptx::store_cluster(ptx::map_to_cta(&freed, 1), (uint32_t)n_freed);
+                ptx::store_cluster(ptx::map_to_cta(&handed, 1), (uint32_t)n_handed);
+            }
+            __syncwarp();
+            ptx::mbar_wait_bounded(&done, 0, kDrainNs);
+        }
+    } else if (warp >= kEpiWarp0) {
+        const int q = warp & 3, hc = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., half hc of the columns
+        float *bs = bias_s + (warp - kEpiWarp0) * 128;
+        const int pieces = a.half / 32;   // of 2 x 16 columns
+        // columns of a piece's two sixteens in the accumulators: G and U of the same features, or neighbours
+        const int col0 = MODE == GM_PRODUCT ? hc * a.half : hc * (a.half / 2), step = MODE == GM_PRODUCT ? 32 : 16,
+                  other = MODE == GM_PRODUCT ? 16 : a.half;
+        ptx::pdl_wait();   // the outputs and dH may be an earlier kernel's
+        int ab = 0;
+        uint32_t fphase = 0;
+        bool ok = true;
+        for (; ok && v < a.units; v += pairs) {
+            un = unit_at<MODE>(a, v);
+            const int64_t row = un.m0 + rank * 128 + 32 * q + lane;
+            if (MODE != GM_PRODUCT && (a.bg || a.bu)) {
+                __syncwarp();   // (the last unit's biases have been read)
+                for (int j = lane; j < a.half / 2; j += 32) {
+                    const int64_t f = un.n0 + col0 + j;
+                    bs[j] = a.bg && f < a.N ? __ldg(a.bg + f) : 0.f;
+                    bs[64 + j] = a.bu && f < a.N ? __ldg(a.bu + f) : 0.f;
+                }
+                __syncwarp();
+            }
+            float g[4][16], w[4][16];   // (fp32: the sums of the blocks so far)
+            if constexpr (F32) {
+#pragma unroll
+                for (int p = 0; p < 4; p++)
+#pragma unroll
+                    for (int j = 0; j < 16; j++) g[p][j] = w[p][j] = 0.f;
+            }
+            const int blocks = F32 ? (un.c1 - un.c0 + kDrainChunks - 1) / kDrainChunks : 1;
+            for (int b = 0; ok && b < blocks; b++) {
+                const uint64_t limit = a.wait_ns * (uint64_t)((un.c1 - un.c0) * a.pairs + 2);
+                ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, limit, &stop));
+                if (!ok) {
+                    halt();
+                    break;
+                }
+                tc5::fence_after();
+                const uint32_t tm = tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16);
+#pragma unroll
+                for (int p = 0; p < 4; p++) {
+                    if (p >= pieces) break;
+                    float d[16] = {};
+                    const int64_t c = un.n0 + col0 + p * step;
+                    if (MODE == GM_BACKWARD && !F32 && row < a.M)
+                        load16(static_cast<const T *>(a.dH) + row * a.N, c, a.N, a.vec, d);
+                    uint32_t r0[16], r1[16];
+                    tc5::ld16(tm + col0 + p * step, r0);
+                    tc5::ld16(tm + col0 + p * step + other, r1);
+                    tc5::ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
+                        asm volatile("" : "+r"(r0[j]));
+                        asm volatile("" : "+r"(r1[j]));
+                    }
+                    if (p == pieces - 1) {   // the last columns are in registers
+                        tc5::fence_before();
+                        __syncwarp();
+                        if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(&acc_empty[ab], 0));
+                    }
+                    if constexpr (F32) {
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            g[p][j] += __uint_as_float(r0[j]);
+                            w[p][j] += __uint_as_float(r1[j]);
+                        }
+                    } else {
+                        float x[16], y[16];
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {
+                            x[j] = __uint_as_float(r0[j]);
+                            y[j] = __uint_as_float(r1[j]);
+                        }
+                        put<MODE, T>(a, un, row, c, x, y, bs + 16 * p, bs + 64 + 16 * p, d);
+                    }
+                }
+                ab ^= 1;
+                if (ab == 0) fphase ^= 1;
+            }
+            if constexpr (F32) {
+                if (ok) {
+#pragma unroll
+                    for (int p = 0; p < 4; p++) {
+                        if (p >= pieces) break;
+                        float d[16] = {};
+                        const int64_t c = un.n0 + col0 + p * step;
+                        if (MODE == GM_BACKWARD && row < a.M)
+                            load16(static_cast<const T *>(a.dH) + row * a.N, c, a.N, a.vec, d);
+                        put<MODE, T>(a, un, row, c, g[p], w[p], bs + 16 * p, bs + 64 + 16 * p, d);
+                    }
+                }
+            }
+        }
+    }
+    // every MMA completed (the issuer waited for `done`), and neither CTA reads
+    // or signals the other's shared memory any more
+    auto meet = [&]() {
+        __syncwarp();
+        ptx::cluster_barrier();
+    };
+    tc5::fence_before();
+    meet();
+    if (aborted(&stop)) {
+        // (the same for both CTAs.) The loads that only some of the producers
+        // issued are completed by the others, so that every barrier phase can
+        // finish, and the CTA whose barriers count the bytes waits for the last
+        // ns of them (older ones were consumed): no copy outlives the CTAs
+        if (warp < 2) {
+            int most = 0;
+            for (int p = 0; p < 2; p++)
+                for (int r = 0; r < 2; r++) most = max(most, loads[p][r]);
+            while (more && issued < most) more = load_step();
+            for (int i = max(0, issued - ns); rank == 0 && i < issued; i++)
+                if (!((stalled >> (i % ns)) & 1)) ptx::mbar_wait_bounded(&full[i % ns], (uint32_t)(i / ns) & 1, kDrainNs);
+        }
+        meet();
+    }
+    if (warp == kMmaWarp) {
+        // a commit arrives by itself, at both CTAs: each waits for the last
+        // arrival at every barrier of its own before it gives up its tensor
+        // memory and its shared memory (a barrier a lane)
+        uint64_t *bar = nullptr;
+        int last = 0;   // the phase of the last arrival
+        if (lane < ns && lane < freed) {
+            bar = &empty[lane];
+            last = (freed - 1 - lane) / ns;
+        } else if (lane >= 29 && lane - 29 < min(2, handed)) {
+            bar = &acc_full[lane - 29];
+            last = (handed - 1 - (lane - 29)) / 2;
+        } else if (lane == 31) {
+            bar = &done;
+        }
+        if (bar) ptx::mbar_wait_bounded(bar, (uint32_t)last & 1, kDrainNs);
+        __syncwarp();
+        tc5::fence_after();
+        tc5::dealloc_pair(tmem, 2 * kAccCols);
+    }
+}
+
+// The sum of a split product's parts, in their order, four columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) k_join_parts(const float *parts, int64_t M, int64_t N, int64_t ld, int splits, int64_t row_seam,
+                                                    int64_t out_rows, void *out0, void *out1) {
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    const int64_t fours = (N + 3) / 4, total = M * fours;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t row = i / fours, c = (i - row * fours) * 4;
+        const bool second = row >= row_seam;
+        const int64_t r = second ? row - row_seam : row;
+        if (r >= out_rows) continue;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < splits; k++) {
+            const float4 p = *reinterpret_cast<const float4 *>(parts + ((int64_t)k * M + row) * ld + c);
+            s.x += p.x, s.y += p.y, s.z += p.z, s.w += p.w;
+        }
+        T *out = static_cast<T *>(second ? out1 : out0) + r * N + c;
+        const float v[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            if (c + j < N) out[j] = from_f32<T>(v[j]);
+    }
+}
+
+// `side`: boxes of 64 columns x 64 rows; else of 64 columns x `rows` rows.
+cudaError_t encode(const Planes &m, bool side, int rows, CUtensorMap *map) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows, (cuuint64_t)m.planes};
+    const cuuint64_t strides[2] = {(cuuint64_t)m.ld * 2, (cuuint64_t)m.ld * 2 * (cuuint64_t)m.rows};
+    const cuuint32_t box[3] = {64, (cuuint32_t)(side ? 64 : rows), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t *>(m.p), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
+int pairs_of_sms() {
+    int dev = 0, n = 152;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        cudaGetLastError();
+    return std::max(1, n / 2);
+}
+
+template <int MODE, typename T>
+cudaError_t launch(const GatedMma &g, cudaStream_t s) {
+    Args a = {};
+    a.M = g.M, a.N = g.N;
+    a.half = g.half;
+    a.splits = g.splits;
+    a.chunks = (int)((g.K + KC - 1) / KC);
+    a.seam = (int)(g.b_seam / KC);
+    a.tiles_n = (unsigned)(MODE == GM_PRODUCT ? (g.N + 2 * g.half - 1) / (2 * g.half) : (g.Fp + g.half - 1) / g.half);
+    const int64_t units = (g.M + 255) / 256 * a.tiles_n * g.splits;
+    if (units > INT32_MAX) return cudaErrorInvalidConfiguration;
+    a.units = (unsigned)units;
+    a.stage_bytes = kABytes + (uint32_t)g.half * 128;
+    a.pairs = g.a.planes == 3 ? kPairs : g.a.planes;
+    a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 2048 - kBiasBytes) / a.stage_bytes);
+    a.idesc = tc5::idesc(false, 256, 2 * g.half) | (g.a_side ? tc5::kIdescAmn : 0) | (g.b_side ? tc5::kIdescBmn : 0);
+    a.a_side = g.a_side, a.b_side = g.b_side;
+    a.bg = g.bg, a.bu = g.bu;
+    a.act = g.act;
+    a.dH = g.dH;
+    a.out0 = MODE == GM_FORWARD ? g.H : g.out0;
+    a.out1 = g.out1;
+    a.D = g.D, a.d_planes = g.d_planes;
+    a.Fp = g.Fp;
+    a.sums = g.sums;
+    a.row_seam = g.row_seam, a.out_rows = g.out_rows;
+    a.parts = g.parts, a.part_ld = g.part_ld;
+    // 32-byte stores: base addresses and rows of 32-byte multiples
+    a.vec = g.N * (int64_t)sizeof(T) % 32 == 0 &&
+            (reinterpret_cast<uintptr_t>(a.out0) | reinterpret_cast<uintptr_t>(a.out1) | reinterpret_cast<uintptr_t>(g.dH)) % 32 == 0;
+    const char *limit = std::getenv("BSR_WAIT_LIMIT_NS"), *stall = std::getenv("BSR_TEST_STALL_CHUNK");
+    a.wait_ns = limit ? std::strtoull(limit, nullptr, 10) : 1000000000ull;
+    a.stall_chunk = stall ? std::atoi(stall) : -1;
+    cudaError_t e = encode(g.a, g.a_side, 128, &a.a);
+    if (e == cudaSuccess) e = encode(g.b0, g.b_side, g.half, &a.b0);
+    if (e == cudaSuccess) e = encode(g.b1.p ? g.b1 : g.b0, g.b_side, g.half, &a.b1);
+    static std::atomic<uint64_t> attr_set{0};
+    if (e == cudaSuccess) e = allow_smem(k_gated_mma<MODE, T>, kMaxSmem, attr_set);
+    if (e != cudaSuccess) return e;
+    const unsigned grid = 2 * (unsigned)std::min<int64_t>(units, pairs_of_sms());
+    e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(kThreads), a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
+    if (e != cudaSuccess || g.splits == 1) return e;
+    const int64_t fours = g.M * ((g.N + 3) / 4);
+    return launch_kernel(k_join_parts<T>, dim3((unsigned)std::min<int64_t>((fours + 255) / 256, 8 * 2 * pairs_of_sms())), dim3(256), 0,
+                         s, (const float *)g.parts, g.M, g.N, g.part_ld, g.splits, g.row_seam, g.out_rows, g.out0, g.out1);
+}
+
+}  // namespace
+
+void plan_gated_mma(GatedMma &g) {
+    const int64_t pairs = pairs_of_sms(), steps = (g.K + KC - 1) / KC * (g.a.planes == 3 ? kPairs : g.a.planes), tm = (g.M + 255) / 256;
+    const bool product = g.mode == GM_PRODUCT;
+    double best = 0;
+    for (int half : {128, 64, 32}) {
+        if (product && half < 64) break;   // (a box of 64 columns)
+        const int64_t tn = product ? (g.N + 2 * half - 1) / (2 * half) : (g.Fp + half - 1) / half;
+        // SM cycles of a step: 512 of MMAs at 256 columns; narrower tiles wait for shared memory
+        const double step = std::max(512.0 * half / 128, 256.0);
+        for (int splits = 1; splits <= (product ? 16 : 1); splits++) {
+            if (splits > 1 && steps < 8 * splits) break;
+            const double waves = (double)((tm * tn * splits + pairs - 1) / pairs);
+            // a unit's start and end; the parts are written and read again, and a launch added
+            const double t = waves * ((double)(steps + splits - 1) / splits * step + 1500) +
+                             (splits > 1 ? 5000.0 + (double)g.M * g.N * 8 * splits / 4000 : 0);
+            if (best == 0 || t < best) {
+                best = t;
+                g.half = half;
+                g.splits = splits;
+                g.part_ld = tn * 2 * half;
+            }
+        }
+    }
+}
+
+cudaError_t launch_gated_mma(const GatedMma &g, cudaStream_t s) {
+    const bool f32 = g.dt == BSR_F32;
+    switch (g.mode) {
+        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, s) : launch<GM_FORWARD, uint16_t>(g, s);
+        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, s) : launch<GM_BACKWARD, uint16_t>(g, s);
+        default: return f32 ? launch<GM_PRODUCT, float>(g, s) : launch<GM_PRODUCT, uint16_t>(g, s);
+    }
+}
+
+cudaError_t gated_mma_status(int *code) {
+    const int ok = DEV_OK;
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(code, g_status, sizeof ok);
+    if (e == cudaSuccess && *code != ok) e = cudaMemcpyToSymbol(g_status, &ok, sizeof ok);
+    return e;
+}
+
+}  // namespace bsr

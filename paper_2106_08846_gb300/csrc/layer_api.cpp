@@ -5,6 +5,7 @@
 
 #include "bsr_internal.h"
 #include "gated.h"
+#include "gated_mma.h"
 #include "host.h"
 #include "residual_norm.h"
 
@@ -95,7 +96,7 @@ constexpr int64_t kGatedMost = (int64_t)1 << 20;
 bsr_status_t check_gated(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt) {
     if (!known(dt)) return BSR_ERR_UNSUPPORTED;
     if (N < 0) return BSR_ERR_INVALID_ARG;
-    if (F < 1 || K < 1 || F > kGatedMost || K > kGatedMost || N > INT32_MAX || N * std::max(F, K) >= (int64_t)1 << 40)
+    if (F < 1 || K < 1 || F > kGatedMost || K > kGatedMost || N > (int64_t)1 << 30 || N * std::max(F, K) >= (int64_t)1 << 38)
         return BSR_ERR_SHAPE;
     return BSR_OK;
 }
@@ -236,6 +237,12 @@ bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, c
     c.dX = dX, c.dWg = dWg, c.dWu = dWu;
     c.dbg = dbg, c.dbu = dbu;
     return launched(launch_gated_backward(c, s));
+}
+
+bsr_status_t bsr_check_status(void) {
+    int code = DEV_OK;
+    const bsr_status_t st = launched(gated_mma_status(&code));
+    return st == BSR_OK && code == DEV_TIMEOUT ? BSR_ERR_TIMEOUT : st;
 }
 
 }  // extern "C"

@@ -168,6 +168,15 @@ __device__ __forceinline__ void tma_load_2d_pair_at(uint32_t dst, const CUtensor
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// As tma_load_2d_pair_at, of a 3-D tensor.
+__device__ __forceinline__ void tma_load_3d_pair_at(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z,
+                                                   uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
+        "[%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
 // 32 bytes to global memory by one thread (32-byte aligned).
 __device__ __forceinline__ void st_global_32(void *p, const uint32_t (&v)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),

@@ -25,12 +25,23 @@ __device__ __forceinline__ uint64_t desc_sw128(uint32_t addr) {
            (2ull << 61);
 }
 
+// The same for an operand whose M (or N) side is contiguous: TMA boxes of 64
+// values of that side x 64 of K, 128-byte rows of one k each (8-row groups 1024
+// bytes apart along K), `side` bytes between boxes along M or N.
+__device__ __forceinline__ uint64_t desc_sw128_mn(uint32_t addr, uint32_t side) {
+    return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)(side >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | (1ull << 46) |
+           (2ull << 61);
+}
+
 // Instruction descriptor: fp32 accumulator, A and B K-major, A/B format 2
 // (tf32) or 1 (bf16), N / 8 and M / 16.
 __host__ __device__ constexpr uint32_t idesc(bool tf32, int M, int N) {
     return (1u << 4) | ((tf32 ? 2u : 1u) << 7) | ((tf32 ? 2u : 1u) << 10) | ((uint32_t)(N >> 3) << 17) |
            ((uint32_t)(M >> 4) << 24);
 }
+
+// bits of the instruction descriptor for operands contiguous along M and N
+constexpr uint32_t kIdescAmn = 1u << 15, kIdescBmn = 1u << 16;
 
 // D (tensor memory) (+)= A (shared-memory descriptor) x B (descriptor)
 template <bool TF32>
