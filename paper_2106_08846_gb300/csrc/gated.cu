@@ -156,10 +156,7 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
     w.row_seam = p.Fp, w.out_rows = F;
     plan_gated_mma(x);
     plan_gated_mma(w);
-    int64_t most = 0;
-    for (const GatedMma *g : {&x, &w})
-        if (g->splits > 1) most = std::max(most, g->splits * g->M * g->part_ld * 4);
-    p.parts_at = take(most);
+    p.parts_at = take(std::max(x.part_bytes, w.part_bytes));
     return p;
 }
 

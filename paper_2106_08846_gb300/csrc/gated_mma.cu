@@ -6,14 +6,22 @@
 // gated modes one CTA loads `half` rows of Wg and the other of Wu, so that the
 // same thread finds G and U of a feature in its tensor-memory lane.
 //
-//   warp 0     A tiles by TMA (128-byte swizzle), 128 rows x 64 of K a CTA
-//   warp 1     B tiles, `half` rows x 64
-//   warp 2     MMAs (M = 256, N = 2 half, K = 16) of the pair's first CTA
-//   warps 4-11 epilogue: 32 rows and half of the columns each, straight from
-//              tensor memory to global memory
+//   warps 0, 1, 3  producers, a step each in turn: the step's A tiles (128 rows
+//                  x 64 of K a CTA) and B tiles (`half` rows x 64) by TMA
+//                  (128-byte swizzle) into a stage of the ring
+//   warp 2         MMAs (M = 256, N = 2 half, K = 16) of the pair's first CTA
+//   warps 4-11     epilogue: 32 rows and half of the columns each, straight
+//                  from tensor memory to global memory
+//
+// A step is 128 columns of K (fp32: 64): 1024 (3072) SM cycles of MMAs at 256
+// columns. Waiting for a stage, one load of 64 columns and moving on take a
+// producer about 740 cycles; with 64 columns a step and one warp each for A and
+// B, the producers were the bound (8192 tokens of 1024 features into 4096, bf16:
+// 95 us, the MMAs 62).
 //
 // Persistent: one CTA per SM; two accumulator buffers of 256 columns let a
-// tile's epilogue overlap the next tile's MMAs.
+// tile's epilogue overlap the next tile's MMAs. Plain products split the K of
+// the tiles that would fill the last round only in part.
 //
 // Operands stored with K along rows (weights for dX; dG, dU and X for the
 // weights' gradients) are read in place: TMA boxes of 64 x 64 and descriptors
@@ -21,9 +29,9 @@
 //
 // fp32 operands come as three bf16 parts whose sum they are (8 bits of the
 // significand each), and a product is the six of nine part products that are not
-// below 2^-24 of it (bf16 products may have an A of two parts). The tensor cores' fp32 accumulation drops bits with every
-// addition, so the small products of 256 columns of K come first and the
-// accumulators are added to registers after every 256 columns.
+// below 2^-24 of it (bf16 products may have an A of two parts). The tensor cores'
+// fp32 accumulation drops bits with every addition, so the small products of a
+// step come first and the accumulators are added to registers after every step.
 //
 // Every wait is bounded by the global timer; a timeout is recorded, stops every
 // role, lets the issued copies and MMAs finish, frees the tensor memory and
@@ -53,8 +61,7 @@ constexpr int kStages = 8;
 constexpr uint32_t kBiasBytes = kEpiWarps * 128 * 4;
 constexpr uint32_t kMaxSmem = 227 * 1024 - 1024;
 constexpr uint32_t kAccCols = 256;
-constexpr int kDrainChunks = 4;               // fp32: columns of K between additions to registers, in chunks
-constexpr int kPairs = 6;
+constexpr int kProducers = 3;
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
 
 __device__ int g_status;
@@ -62,11 +69,12 @@ __device__ int g_status;
 struct Args {
     CUtensorMap a, b0, b1;
     int64_t M, N;             // rows; columns (gated modes: features)
-    unsigned tiles_n, units;
-    int splits, chunks, seam; // chunks of K in all; the chunk from which b1 is read
+    unsigned tiles_n, whole, units;   // tiles along N; units that are whole tiles (they come first)
+    int splits;               // units of every other tile
+    int chunks, steps, seam;  // chunks of K, steps of a tile; the chunk from which b1 is read
     int half, ns;
-    int pairs;                // pairs of parts that are multiplied
     uint32_t stage_bytes, idesc;
+    int a_tiles, b_tiles;     // in a stage
     int a_side, b_side;
     const float *bg, *bu;
     int act;
@@ -78,64 +86,47 @@ struct Args {
     float *sums;
     int64_t row_seam, out_rows;
     float *parts;
-    int64_t part_ld;
     int vec;                  // output (and dH) rows start on 32-byte boundaries
     uint64_t wait_ns;
-    int stall_chunk;          // test hook: this step of each unit is never loaded by warp 0 (-1: none)
+    int stall_step;           // test hook: this step of each tile is never loaded (-1: none)
 };
 
 struct Unit {
     int64_t m0, n0;   // first row, first column (gated modes: feature)
-    int c0, c1;       // chunks
-    int split;
+    int i0, i1;       // steps
+    int part;         // index of the unit's part, -1 for a whole tile
 };
 
 template <int MODE>
 __device__ __forceinline__ Unit unit_at(const Args &a, unsigned v) {
     Unit u;
-    u.split = 0;
-    if (MODE == GM_PRODUCT && a.splits > 1) {
-        u.split = (int)(v % (unsigned)a.splits);
-        v /= (unsigned)a.splits;
+    u.part = -1;
+    u.i0 = 0;
+    u.i1 = a.steps;
+    if (MODE == GM_PRODUCT && v >= a.whole) {
+        u.part = (int)(v - a.whole);
+        const unsigned tile = (unsigned)u.part / (unsigned)a.splits, k = (unsigned)u.part - tile * (unsigned)a.splits;
+        v = a.whole + tile;
+        u.i0 = (int)((int64_t)a.steps * k / a.splits);
+        u.i1 = (int)((int64_t)a.steps * (k + 1) / a.splits);
     }
     const unsigned tm = v / a.tiles_n, tn = v - tm * a.tiles_n;
     u.m0 = (int64_t)tm * 256;
     u.n0 = (int64_t)tn * (MODE == GM_PRODUCT ? 2 * a.half : a.half);
-    u.c0 = (int)((int64_t)a.chunks * u.split / a.splits);
-    u.c1 = (int)((int64_t)a.chunks * (u.split + 1) / a.splits);
     return u;
 }
 
-// The steps of a unit: a block of chunks after another (fp32: of kDrainChunks;
-// bf16: all of them), and a block's chunks once for each pair of parts, the
-// smallest products first.
+// The products of a step, the smallest first: tiles of A and B. fp32: parts
+// (2,0) (1,1) (0,2) (1,0) (0,1) (0,0) of one chunk; bf16: two chunks, or one
+// chunk with two parts of A.
 template <bool F32>
-struct Steps {
-    int c, c1, b0, left;   // chunk, end; the block's first chunk, and the pairs of parts after this one
-    __device__ __forceinline__ void start(const Args &a, const Unit &u) {
-        c = b0 = u.c0;
-        c1 = u.c1;
-        left = a.pairs - 1;
-    }
-    __device__ __forceinline__ bool done() const { return b0 >= c1; }
-    __device__ __forceinline__ int block_end() const { return F32 ? min(b0 + kDrainChunks, c1) : c1; }
-    // moves on; true at a block's end
-    __device__ __forceinline__ bool next(const Args &a) {
-        c++;
-        if (c < block_end()) return false;
-        if (left > 0) {
-            left--;
-            c = b0;
-            return false;
-        }
-        left = a.pairs - 1;
-        c = b0 = block_end();
-        return true;
-    }
-    // three parts: (2,0) (1,1) (0,2) (1,0) (0,1) (0,0); two of A: (1,0) (0,0)
-    __device__ __forceinline__ int a_part() const { return F32 ? (0x210100 >> (4 * left)) & 3 : left; }
-    __device__ __forceinline__ int b_part() const { return F32 ? (0x012010 >> (4 * left)) & 3 : 0; }
-};
+__device__ __forceinline__ int a_tile_of(const Args &a, int i, int n) {
+    return F32 ? (0x001012 >> (4 * i)) & 3 : a.b_tiles == 1 ? n - 1 - i : i;
+}
+template <bool F32>
+__device__ __forceinline__ int b_tile_of(const Args &a, int i) {
+    return F32 ? (0x010210 >> (4 * i)) & 3 : a.b_tiles == 1 ? 0 : i;
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
@@ -315,13 +306,13 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
             }
         }
     } else {
-        if (row >= a.M) return;
-        if (a.splits > 1) {
-            float *at = a.parts + ((int64_t)u.split * a.M + row) * a.part_ld;
-            store16(at, c, a.part_ld, true, v);
-            store16(at, c + 16, a.part_ld, true, w);
+        if (u.part >= 0) {   // [256][2 half] of this unit
+            float *at = a.parts + ((int64_t)u.part * 256 + (row - u.m0)) * 2 * a.half + (c - u.n0);
+            store16(at, 0, 32, true, v);
+            store16(at, 16, 32, true, w);
             return;
         }
+        if (row >= a.M) return;
         const bool second = row >= a.row_seam;
         const int64_t r = second ? row - a.row_seam : row;
         if (r >= a.out_rows) return;
@@ -337,19 +328,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
     const int ns = a.ns;
-    const uint32_t stage_bytes = a.stage_bytes;
+    const uint32_t stage_bytes = a.stage_bytes, b_at = a.a_tiles * kABytes, b_bytes = (uint32_t)a.half * 128;
     float *bias_s = reinterpret_cast<float *>(base + (size_t)ns * stage_bytes);
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], done;
-    __shared__ int stop, loads[2][2];   // loads[producer][CTA of the pair]: loads issued
-    __shared__ int freed, handed;       // commits issued to `empty` and to `acc_full`
+    __shared__ int stop, loads[kProducers][2];   // loads[producer][CTA of the pair]: steps loaded
+    __shared__ int freed, handed;                // commits issued to `empty` and to `acc_full`
     __shared__ uint32_t tmem_s;
 
+    // (a shuffle, so that the warp index and what follows from it is uniform)
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     if (threadIdx.x == 0) {
         for (int s = 0; s < ns; s++) {
-            ptx::mbar_init(&full[s], 2);   // the producers' arrivals, and their bytes
+            ptx::mbar_init(&full[s], 1);   // a producer's arrival, and its bytes
             ptx::mbar_init(&empty[s], 1);
         }
         for (int i = 0; i < 2; i++) {
@@ -358,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
         }
         ptx::mbar_init(&done, 1);
         stop = freed = handed = 0;
-        loads[0][0] = loads[0][1] = loads[1][0] = loads[1][1] = 0;
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, 2 * kAccCols);
@@ -378,69 +369,81 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
         }
     };
 
-    // ---- producers: warp 0 A tiles, warp 1 B tiles
-    const int prod = warp;
+    // ---- producers: the pair's steps prod, prod + np, ... No more producers
+    // than stages: one that waits for step g - ns to be consumed has to know that
+    // step g - 2 ns was, or the stage's barrier, which tells phases apart by their
+    // parity, would let it pass a round early; its last wait, for step
+    // g - np - ns, tells it so if np <= ns.
+    const int prod = warp < kMmaWarp ? warp : kMmaWarp, np = min(kProducers, ns);
+    const bool producer = warp < kEpiWarp0 && warp != kMmaWarp && prod < np;
     unsigned v = pair;
     Unit un = {};
-    Steps<F32> st = {};
-    int s = 0, issued = 0;
-    uint32_t phase = 1;     // the parity of `empty` that a first use of a stage passes at once
-    uint32_t stalled = 0;   // test hook: stages whose load was left out
-    const uint32_t bytes = prod ? 2 * (uint32_t)a.half * 128 : 2 * kABytes;   // of both CTAs
-    const uint32_t dst0 = ptx::smem_addr(base) + (prod ? kABytes : 0), bar0 = ptx::smem_addr(&full[0]);
+    int i = 0, s = prod % ns, issued = 0;
+    uint32_t phase = 1 ^ ((prod / ns) & 1);   // the parity of `empty` that a first use of a stage passes at once
+    uint32_t stalled = 0;                     // test hook: stages whose load was left out
+    const uint32_t smem0 = ptx::smem_addr(base), bar0 = ptx::smem_addr(&full[0]);
     const uint32_t first0 = ptx::map_to_cta(&full[0], 0);   // `full` of the pair's first CTA
+    // to the unit of step i, which may lie beyond this one's last; false: none left
+    auto seek = [&]() {
+        while (i >= un.i1) {
+            const int over = i - un.i1;
+            v += pairs;
+            if (v >= a.units) return false;
+            un = unit_at<MODE>(a, v);
+            i = un.i0 + over;
+        }
+        return true;
+    };
     auto load_step = [&]() {
-        if (prod == 0 && a.stall_chunk >= 0 && st.c == a.stall_chunk) {   // never loaded: its consumer times out
+        if (i == a.stall_step) {   // never loaded: its consumer times out
             stalled |= 1u << s;
         } else if (elected) {
-            const uint32_t dst = dst0 + s * stage_bytes, bar = first0 + 8 * s;
-            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, bytes);
-            if (prod == 0) {
-                const int m = (int)(un.m0 + rank * 128), k = st.c * KC;
+            const uint32_t dst = smem0 + s * stage_bytes, bar = first0 + 8 * s;
+            const bool chunks2 = !F32 && a.b_tiles == 2;
+            const int c0 = chunks2 ? 2 * i : i;
+            // a tile's last step may have one chunk only
+            const int na = chunks2 ? min(2, a.chunks - c0) : a.a_tiles, nb = chunks2 ? na : a.b_tiles;
+            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (na * kABytes + nb * b_bytes));
+            const int m = (int)(un.m0 + rank * 128);
+            for (int t = 0; t < na; t++) {
+                const int k = (chunks2 ? c0 + t : c0) * KC, part = chunks2 ? 0 : t;
+                const uint32_t to = dst + t * kABytes;
                 if (a.a_side) {
-                    ptx::tma_load_3d_pair_at(dst, &a.a, m, k, st.a_part(), bar);
-                    ptx::tma_load_3d_pair_at(dst + 8192, &a.a, m + 64, k, st.a_part(), bar);
+                    ptx::tma_load_3d_pair_at(to, &a.a, m, k, part, bar);
+                    ptx::tma_load_3d_pair_at(to + 8192, &a.a, m + 64, k, part, bar);
                 } else {
-                    ptx::tma_load_3d_pair_at(dst, &a.a, k, m, st.a_part(), bar);
+                    ptx::tma_load_3d_pair_at(to, &a.a, k, m, part, bar);
                 }
-            } else if (MODE != GM_PRODUCT) {
-                ptx::tma_load_3d_pair_at(dst, rank ? &a.b1 : &a.b0, st.c * KC, (int)un.n0, st.b_part(), bar);
-            } else {
-                const bool second = a.seam && st.c >= a.seam;
-                const int n = (int)(un.n0 + rank * a.half), k = (second ? st.c - a.seam : st.c) * KC;
-                const CUtensorMap *map = second ? &a.b1 : &a.b0;
-                if (a.b_side) {
-                    for (int j = 0; j < a.half; j += 64)
-                        ptx::tma_load_3d_pair_at(dst + 128 * j, map, n + j, k, st.b_part(), bar);
+            }
+            const int n = (int)(un.n0 + (MODE == GM_PRODUCT ? rank * a.half : 0));
+            for (int t = 0; t < nb; t++) {
+                const int c = chunks2 ? c0 + t : c0, part = chunks2 ? 0 : t;
+                const uint32_t to = dst + b_at + t * b_bytes;
+                if (MODE != GM_PRODUCT) {
+                    ptx::tma_load_3d_pair_at(to, rank ? &a.b1 : &a.b0, c * KC, n, part, bar);
                 } else {
-                    ptx::tma_load_3d_pair_at(dst, map, k, n, st.b_part(), bar);
+                    const bool second = a.seam && c >= a.seam;
+                    const int k = (second ? c - a.seam : c) * KC;
+                    const CUtensorMap *map = second ? &a.b1 : &a.b0;
+                    for (int j = 0; j < a.half; j += 64) ptx::tma_load_3d_pair_at(to + 128 * j, map, n + j, k, part, bar);
                 }
             }
         }
         issued++;
-        if (++s == ns) {
-            s = 0;
-            phase ^= 1;
-        }
-        st.next(a);
-        if (!st.done()) return true;
-        v += pairs;
-        if (v >= a.units) return false;
-        un = unit_at<MODE>(a, v);
-        st.start(a, un);
-        return true;
+        for (s += np; s >= ns; s -= ns) phase ^= 1;
+        i += np;
+        return seek();
     };
     bool more = false;
-    if (warp < 2) {
+    if (producer) {
         if (elected) {
-            ptx::prefetch_tensormap(prod ? &a.b0 : &a.a);
-            if (prod) ptx::prefetch_tensormap(&a.b1);
+            ptx::prefetch_tensormap(&a.a);
+            ptx::prefetch_tensormap(&a.b0);
+            ptx::prefetch_tensormap(&a.b1);
         }
-        more = v < a.units;
-        if (more) {
-            un = unit_at<MODE>(a, v);
-            st.start(a, un);
-        }
+        un = unit_at<MODE>(a, v);
+        i = un.i0 + prod;
+        more = seek();
         ptx::pdl_wait();   // every operand may be an earlier kernel's output
         while (more) {
             const bool got = wait_or_abort(&empty[s], phase, a.wait_ns, &stop);
@@ -459,46 +462,51 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
             int ab = 0, n_freed = 0, n_handed = 0;
             uint32_t fphase = 0, aphase = 1;
             bool ok = true;
-            const uint32_t smem0 = ptx::smem_addr(base);
+            s = 0;
             const uint64_t ad0 = a.a_side ? tc5::desc_sw128_mn(smem0, 8192) : tc5::desc_sw128(smem0);
-            const uint64_t bd0 = a.b_side ? tc5::desc_sw128_mn(smem0 + kABytes, 8192) : tc5::desc_sw128(smem0 + kABytes);
+            const uint64_t bd0 = a.b_side ? tc5::desc_sw128_mn(smem0 + b_at, 8192) : tc5::desc_sw128(smem0 + b_at);
             // 16 of K: two groups of eight 128-byte rows, or 32 bytes along the rows
             const uint32_t a_step = a.a_side ? 128 : 2, b_step = a.b_side ? 128 : 2;
             ptx::pdl_wait();   // the waits below are bounded from here on
             for (; ok && v < a.units; v += pairs) {
                 un = unit_at<MODE>(a, v);
-                st.start(a, un);
-                while (ok && !st.done()) {   // a block of steps into one accumulator buffer
+                for (i = un.i0; ok && i < un.i1; i++) {
                     const uint32_t d = tmem + (uint32_t)ab * kAccCols;
-                    ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[ab], aphase, a.wait_ns, &stop));
-                    tc5::fence_after();
-                    uint32_t acc = 0;
-                    for (bool last = false; ok && !last;) {
-                        ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
+                    if (F32 || i == un.i0) {   // into a fresh accumulator buffer
+                        ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[ab], aphase, a.wait_ns, &stop));
                         if (!ok) break;
-                        tc5::fence_after();
-                        if (elected) {
-                            const uint64_t ad = ad0 + (uint64_t)((s * stage_bytes) >> 4), bd = bd0 + (uint64_t)((s * stage_bytes) >> 4);
+                    }
+                    ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
+                    if (!ok) break;
+                    tc5::fence_after();
+                    if (elected) {
+                        const uint64_t at = (uint64_t)((s * stage_bytes) >> 4);
+                        const int n = F32 ? 6 : a.b_tiles == 1 ? a.a_tiles : min(2, a.chunks - 2 * i);
+#pragma unroll
+                        for (int t = 0; t < (F32 ? 6 : 2); t++) {
+                            if (t >= n) break;
+                            const uint64_t ad = ad0 + at + a_tile_of<F32>(a, t, n) * (kABytes >> 4);
+                            const uint64_t bd = bd0 + at + b_tile_of<F32>(a, t) * (b_bytes >> 4);
 #pragma unroll
                             for (int j = 0; j < KC / 16; j++)
-                                tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, a.idesc, acc | (j > 0));
-                            tc5::commit_pair(&empty[s]);
+                                tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, a.idesc,
+                                                 (!F32 && i > un.i0) | (t > 0) | (j > 0));
                         }
-                        __syncwarp();
-                        acc = 1;
-                        n_freed++;
-                        if (++s == ns) {
-                            s = 0;
-                            fphase ^= 1;
-                        }
-                        last = st.next(a);
+                        tc5::commit_pair(&empty[s]);
                     }
-                    if (!ok) break;
-                    if (elected) tc5::commit_pair(&acc_full[ab]);
                     __syncwarp();
-                    n_handed++;
-                    ab ^= 1;
-                    if (ab == 0) aphase ^= 1;
+                    n_freed++;
+                    if (++s == ns) {
+                        s = 0;
+                        fphase ^= 1;
+                    }
+                    if (F32 || i + 1 == un.i1) {
+                        if (elected) tc5::commit_pair(&acc_full[ab]);
+                        __syncwarp();
+                        n_handed++;
+                        ab ^= 1;
+                        if (ab == 0) aphase ^= 1;
+                    }
                 }
                 if (!ok) halt();
             }
@@ -536,74 +544,88 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
                 }
                 __syncwarp();
             }
-            float g[4][16], w[4][16];   // (fp32: the sums of the blocks so far)
-            if constexpr (F32) {
+            const T *dh = static_cast<const T *>(a.dH) + row * a.N;
+            const bool mine = MODE == GM_BACKWARD && row < a.M;
+            const uint64_t limit = a.wait_ns * (uint64_t)(un.i1 - un.i0 + 2);
+            // waits for the next accumulator buffer; its columns of this warp's lanes
+            auto wait_acc = [&]() {
+                ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, limit, &stop));
+                if (!ok) halt();
+                tc5::fence_after();
+                return tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16) + col0;
+            };
+            // hands the buffer back, its last columns being in registers
+            auto hand_back = [&]() {
+                tc5::fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(&acc_empty[ab], 0));
+                ab ^= 1;
+                if (ab == 0) fphase ^= 1;
+            };
+            if constexpr (!F32) {
+                // a piece ahead: accumulators and dH on their way while one is put out
+                uint32_t r[2][16];
+                float d[16] = {};
+                if (mine) load16(dh, un.n0 + col0, a.N, a.vec, d);
+                const uint32_t tm = wait_acc();
+                if (!ok) break;
+                tc5::ld16(tm, r[0]);
+                tc5::ld16(tm + other, r[1]);
+#pragma unroll 1
+                for (int p = 0; p < pieces; p++) {
+                    float x[16], y[16], dp[16];
+                    tc5::ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
+                        asm volatile("" : "+r"(r[0][j]));
+                        asm volatile("" : "+r"(r[1][j]));
+                        x[j] = __uint_as_float(r[0][j]);
+                        y[j] = __uint_as_float(r[1][j]);
+                        dp[j] = d[j];
+                    }
+                    if (p + 1 < pieces) {
+                        tc5::ld16(tm + (p + 1) * step, r[0]);
+                        tc5::ld16(tm + (p + 1) * step + other, r[1]);
+                        if (mine) load16(dh, un.n0 + col0 + (p + 1) * step, a.N, a.vec, d);
+                    } else {
+                        hand_back();
+                    }
+                    put<MODE, T>(a, un, row, un.n0 + col0 + p * step, x, y, bs + 16 * p, bs + 64 + 16 * p, dp);
+                }
+            } else {
+                float g[4][16], w[4][16];   // the sums of the steps so far
 #pragma unroll
                 for (int p = 0; p < 4; p++)
 #pragma unroll
                     for (int j = 0; j < 16; j++) g[p][j] = w[p][j] = 0.f;
-            }
-            const int blocks = F32 ? (un.c1 - un.c0 + kDrainChunks - 1) / kDrainChunks : 1;
-            for (int b = 0; ok && b < blocks; b++) {
-                const uint64_t limit = a.wait_ns * (uint64_t)((un.c1 - un.c0) * a.pairs + 2);
-                ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, limit, &stop));
-                if (!ok) {
-                    halt();
-                    break;
+                for (int b = un.i0; b < un.i1; b++) {
+                    const uint32_t tm = wait_acc();
+                    if (!ok) break;
+#pragma unroll
+                    for (int p = 0; p < 4; p++) {
+                        if (p >= pieces) break;
+                        uint32_t r0[16], r1[16];
+                        tc5::ld16(tm + p * step, r0);
+                        tc5::ld16(tm + p * step + other, r1);
+                        tc5::ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; j++) {   // (as above)
+                            asm volatile("" : "+r"(r0[j]));
+                            asm volatile("" : "+r"(r1[j]));
+                            g[p][j] += __uint_as_float(r0[j]);
+                            w[p][j] += __uint_as_float(r1[j]);
+                        }
+                    }
+                    hand_back();
                 }
-                tc5::fence_after();
-                const uint32_t tm = tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16);
+                if (!ok) break;
 #pragma unroll
                 for (int p = 0; p < 4; p++) {
                     if (p >= pieces) break;
                     float d[16] = {};
                     const int64_t c = un.n0 + col0 + p * step;
-                    if (MODE == GM_BACKWARD && !F32 && row < a.M)
-                        load16(static_cast<const T *>(a.dH) + row * a.N, c, a.N, a.vec, d);
-                    uint32_t r0[16], r1[16];
-                    tc5::ld16(tm + col0 + p * step, r0);
-                    tc5::ld16(tm + col0 + p * step + other, r1);
-                    tc5::ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
-                        asm volatile("" : "+r"(r0[j]));
-                        asm volatile("" : "+r"(r1[j]));
-                    }
-                    if (p == pieces - 1) {   // the last columns are in registers
-                        tc5::fence_before();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(&acc_empty[ab], 0));
-                    }
-                    if constexpr (F32) {
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            g[p][j] += __uint_as_float(r0[j]);
-                            w[p][j] += __uint_as_float(r1[j]);
-                        }
-                    } else {
-                        float x[16], y[16];
-#pragma unroll
-                        for (int j = 0; j < 16; j++) {
-                            x[j] = __uint_as_float(r0[j]);
-                            y[j] = __uint_as_float(r1[j]);
-                        }
-                        put<MODE, T>(a, un, row, c, x, y, bs + 16 * p, bs + 64 + 16 * p, d);
-                    }
-                }
-                ab ^= 1;
-                if (ab == 0) fphase ^= 1;
-            }
-            if constexpr (F32) {
-                if (ok) {
-#pragma unroll
-                    for (int p = 0; p < 4; p++) {
-                        if (p >= pieces) break;
-                        float d[16] = {};
-                        const int64_t c = un.n0 + col0 + p * step;
-                        if (MODE == GM_BACKWARD && row < a.M)
-                            load16(static_cast<const T *>(a.dH) + row * a.N, c, a.N, a.vec, d);
-                        put<MODE, T>(a, un, row, c, g[p], w[p], bs + 16 * p, bs + 64 + 16 * p, d);
-                    }
+                    if (mine) load16(dh, c, a.N, a.vec, d);
+                    put<MODE, T>(a, un, row, c, g[p], w[p], bs + 16 * p, bs + 64 + 16 * p, d);
                 }
             }
         }
@@ -617,17 +639,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
     tc5::fence_before();
     meet();
     if (aborted(&stop)) {
-        // (the same for both CTAs.) The loads that only some of the producers
-        // issued are completed by the others, so that every barrier phase can
-        // finish, and the CTA whose barriers count the bytes waits for the last
-        // ns of them (older ones were consumed): no copy outlives the CTAs
-        if (warp < 2) {
-            int most = 0;
-            for (int p = 0; p < 2; p++)
-                for (int r = 0; r < 2; r++) most = max(most, loads[p][r]);
-            while (more && issued < most) more = load_step();
-            for (int i = max(0, issued - ns); rank == 0 && i < issued; i++)
-                if (!((stalled >> (i % ns)) & 1)) ptx::mbar_wait_bounded(&full[i % ns], (uint32_t)(i / ns) & 1, kDrainNs);
+        // (the same for both CTAs.) The loads that only one CTA's producer
+        // issued are completed by the other's, so that every barrier phase can
+        // finish, and the CTA whose barriers count the bytes waits for those
+        // that no later load of their stage shows to be complete: no copy
+        // outlives the CTAs
+        if (producer) {
+            int most[kProducers];
+            for (int p = 0; p < np; p++) most[p] = max(loads[p][0], loads[p][1]);
+            while (more && issued < most[prod]) more = load_step();
+            for (int k = max(0, issued - ns); rank == 0 && k < issued; k++) {
+                const int g = prod + np * k, later = g + ns;
+                if (later / np >= most[later % np] && !((stalled >> (g % ns)) & 1))
+                    ptx::mbar_wait_bounded(&full[g % ns], (uint32_t)(g / ns) & 1, kDrainNs);
+            }
         }
         meet();
     }
@@ -653,28 +678,31 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
     }
 }
 
-// The sum of a split product's parts, in their order, four columns a thread.
+// The split tiles: the sum of a tile's parts, in their order, four columns a
+// thread; blockIdx.y is the tile after the whole ones.
 template <typename T>
-__global__ void __launch_bounds__(256) k_join_parts(const float *parts, int64_t M, int64_t N, int64_t ld, int splits, int64_t row_seam,
-                                                    int64_t out_rows, void *out0, void *out1) {
+__global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args a) {
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
-    const int64_t fours = (N + 3) / 4, total = M * fours;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / fours, c = (i - row * fours) * 4;
-        const bool second = row >= row_seam;
-        const int64_t r = second ? row - row_seam : row;
-        if (r >= out_rows) continue;
-        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < splits; k++) {
-            const float4 p = *reinterpret_cast<const float4 *>(parts + ((int64_t)k * M + row) * ld + c);
-            s.x += p.x, s.y += p.y, s.z += p.z, s.w += p.w;
+    const int fours = a.half / 2, width = 2 * a.half;
+    for (unsigned tile = blockIdx.y; tile < (a.units - a.whole) / (unsigned)a.splits; tile += gridDim.y) {
+        const unsigned tm = (a.whole + tile) / a.tiles_n, tn = a.whole + tile - tm * a.tiles_n;
+        const int e = blockIdx.x * 256 + threadIdx.x, r = e / fours, x = (e - r * fours) * 4;
+        const int64_t row = (int64_t)tm * 256 + r, c = (int64_t)tn * width + x;
+        if (r >= 256 || row >= a.M || c >= a.N) continue;
+        const bool second = row >= a.row_seam;
+        const int64_t at = second ? row - a.row_seam : row;
+        if (at >= a.out_rows) continue;
+        float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < a.splits; k++) {
+            const float4 p = *reinterpret_cast<const float4 *>(a.parts + ((int64_t)(tile * a.splits + k) * 256 + r) * width + x);
+            t.x += p.x, t.y += p.y, t.z += p.z, t.w += p.w;
         }
-        T *out = static_cast<T *>(second ? out1 : out0) + r * N + c;
-        const float v[4] = {s.x, s.y, s.z, s.w};
+        T *out = static_cast<T *>(second ? a.out1 : a.out0) + at * a.N + c;
+        const float f[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (c + j < N) out[j] = from_f32<T>(v[j]);
+            if (c + j < a.N) out[j] = from_f32<T>(f[j]);
     }
 }
 
@@ -700,21 +728,29 @@ int pairs_of_sms() {
     return std::max(1, n / 2);
 }
 
+// A stage's tiles and bytes.
+void stage_of(const GatedMma &g, int half, int *a_tiles, int *b_tiles, uint32_t *bytes) {
+    *a_tiles = g.a.planes == 3 ? 3 : 2;
+    *b_tiles = g.a.planes == 3 ? 3 : g.a.planes == 2 ? 1 : 2;
+    *bytes = *a_tiles * kABytes + *b_tiles * (uint32_t)half * 128;
+}
+
 template <int MODE, typename T>
 cudaError_t launch(const GatedMma &g, cudaStream_t s) {
     Args a = {};
     a.M = g.M, a.N = g.N;
     a.half = g.half;
-    a.splits = g.splits;
     a.chunks = (int)((g.K + KC - 1) / KC);
+    a.steps = g.steps;
     a.seam = (int)(g.b_seam / KC);
-    a.tiles_n = (unsigned)(MODE == GM_PRODUCT ? (g.N + 2 * g.half - 1) / (2 * g.half) : (g.Fp + g.half - 1) / g.half);
-    const int64_t units = (g.M + 255) / 256 * a.tiles_n * g.splits;
+    a.tiles_n = (unsigned)g.tiles_n;
+    a.splits = g.splits;
+    const int64_t units = g.whole + (g.tiles - g.whole) * g.splits;
     if (units > INT32_MAX) return cudaErrorInvalidConfiguration;
+    a.whole = (unsigned)g.whole;
     a.units = (unsigned)units;
-    a.stage_bytes = kABytes + (uint32_t)g.half * 128;
-    a.pairs = g.a.planes == 3 ? kPairs : g.a.planes;
-    a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 2048 - kBiasBytes) / a.stage_bytes);
+    stage_of(g, g.half, &a.a_tiles, &a.b_tiles, &a.stage_bytes);
+    a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 1024 - kBiasBytes) / a.stage_bytes);
     a.idesc = tc5::idesc(false, 256, 2 * g.half) | (g.a_side ? tc5::kIdescAmn : 0) | (g.b_side ? tc5::kIdescBmn : 0);
     a.a_side = g.a_side, a.b_side = g.b_side;
     a.bg = g.bg, a.bu = g.bu;
@@ -726,13 +762,13 @@ cudaError_t launch(const GatedMma &g, cudaStream_t s) {
     a.Fp = g.Fp;
     a.sums = g.sums;
     a.row_seam = g.row_seam, a.out_rows = g.out_rows;
-    a.parts = g.parts, a.part_ld = g.part_ld;
+    a.parts = g.parts;
     // 32-byte stores: base addresses and rows of 32-byte multiples
     a.vec = g.N * (int64_t)sizeof(T) % 32 == 0 &&
             (reinterpret_cast<uintptr_t>(a.out0) | reinterpret_cast<uintptr_t>(a.out1) | reinterpret_cast<uintptr_t>(g.dH)) % 32 == 0;
     const char *limit = std::getenv("BSR_WAIT_LIMIT_NS"), *stall = std::getenv("BSR_TEST_STALL_CHUNK");
     a.wait_ns = limit ? std::strtoull(limit, nullptr, 10) : 1000000000ull;
-    a.stall_chunk = stall ? std::atoi(stall) : -1;
+    a.stall_step = stall ? std::atoi(stall) : -1;
     cudaError_t e = encode(g.a, g.a_side, 128, &a.a);
     if (e == cudaSuccess) e = encode(g.b0, g.b_side, g.half, &a.b0);
     if (e == cudaSuccess) e = encode(g.b1.p ? g.b1 : g.b0, g.b_side, g.half, &a.b1);
@@ -741,34 +777,40 @@ cudaError_t launch(const GatedMma &g, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(units, pairs_of_sms());
     e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(kThreads), a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
-    if (e != cudaSuccess || g.splits == 1) return e;
-    const int64_t fours = g.M * ((g.N + 3) / 4);
-    return launch_kernel(k_join_parts<T>, dim3((unsigned)std::min<int64_t>((fours + 255) / 256, 8 * 2 * pairs_of_sms())), dim3(256), 0,
-                         s, (const float *)g.parts, g.M, g.N, g.part_ld, g.splits, g.row_seam, g.out_rows, g.out0, g.out1);
+    if (MODE != GM_PRODUCT || e != cudaSuccess || g.whole == g.tiles) return e;
+    return launch_kernel(k_join_parts<T>, dim3((unsigned)g.half / 2, (unsigned)std::min<int64_t>(g.tiles - g.whole, 65535)), dim3(256), 0, s,
+                         a);
 }
 
 }  // namespace
 
 void plan_gated_mma(GatedMma &g) {
-    const int64_t pairs = pairs_of_sms(), steps = (g.K + KC - 1) / KC * (g.a.planes == 3 ? kPairs : g.a.planes), tm = (g.M + 255) / 256;
-    const bool product = g.mode == GM_PRODUCT;
+    const int64_t pairs = pairs_of_sms(), tm = (g.M + 255) / 256, chunks = (g.K + KC - 1) / KC;
+    const bool product = g.mode == GM_PRODUCT, f32 = g.a.planes == 3;
+    g.steps = (int)(g.a.planes == 1 ? (chunks + 1) / 2 : chunks);
+    const int mmas = f32 ? 6 : 2;   // groups of four to a step
     double best = 0;
     for (int half : {128, 64, 32}) {
         if (product && half < 64) break;   // (a box of 64 columns)
-        const int64_t tn = product ? (g.N + 2 * half - 1) / (2 * half) : (g.Fp + half - 1) / half;
-        // SM cycles of a step: 512 of MMAs at 256 columns; narrower tiles wait for shared memory
-        const double step = std::max(512.0 * half / 128, 256.0);
-        for (int splits = 1; splits <= (product ? 16 : 1); splits++) {
-            if (splits > 1 && steps < 8 * splits) break;
-            const double waves = (double)((tm * tn * splits + pairs - 1) / pairs);
+        const int64_t tn = product ? (g.N + 2 * half - 1) / (2 * half) : (g.Fp + half - 1) / half, tiles = tm * tn;
+        // SM cycles of a step: 512 for four MMAs of 256 columns; narrower tiles wait for shared memory
+        const double step = mmas * std::max(512.0 * half / 128, 256.0);
+        for (int splits = 1; splits <= (product ? 16 : 1) && splits <= g.steps; splits++) {
+            // whole tiles as long as they fill all pairs
+            const int64_t whole = splits == 1 ? tiles : tiles / pairs * pairs;
+            const double rest = (double)(((tiles - whole) * splits + pairs - 1) / pairs);
             // a unit's start and end; the parts are written and read again, and a launch added
-            const double t = waves * ((double)(steps + splits - 1) / splits * step + 1500) +
-                             (splits > 1 ? 5000.0 + (double)g.M * g.N * 8 * splits / 4000 : 0);
+            double t = (double)((whole + pairs - 1) / pairs) * (g.steps * step + 1500);
+            if (splits > 1)
+                t += rest * ((double)(g.steps + splits - 1) / splits * step + 1500) + 5000 +
+                     (double)(tiles - whole) * splits * 256 * 2 * half * 8 / 4000;
             if (best == 0 || t < best) {
                 best = t;
                 g.half = half;
                 g.splits = splits;
-                g.part_ld = tn * 2 * half;
+                g.tiles = tiles, g.tiles_n = tn;
+                g.whole = whole;
+                g.part_bytes = (tiles - whole) * splits * 256 * 2 * half * 4;
             }
         }
     }

@@ -43,14 +43,14 @@ struct GatedMma {
     // GM_PRODUCT: rows below row_seam go to out0, those from it on to out1, `out_rows` in each
     void *out0, *out1;
     int64_t row_seam, out_rows;
-    float *parts;             // splits x M x part_ld, where splits > 1
+    float *parts;             // part_bytes
     // chosen by plan_gated_mma
-    int half, splits;
-    int64_t part_ld;
+    int half, steps, splits;
+    int64_t tiles, tiles_n, whole, part_bytes;
 };
 
-// Chooses the tile width and, for GM_PRODUCT, into how many parts K is split
-// (half, splits, part_ld), from the sizes.
+// Chooses, from the sizes, the tile width, the steps of a tile and, for
+// GM_PRODUCT, which tiles have their K split into how many parts.
 void plan_gated_mma(GatedMma &g);
 cudaError_t launch_gated_mma(const GatedMma &g, cudaStream_t s);
 
