@@ -108,9 +108,11 @@ int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
     int parts, d_parts;   // bf16 matrices to an operand, and to dG and dU
     bool lay_out;
+    int first;            // where dX stands in `grads`
     int64_t Kp, Fp;
     int64_t x_at, wg_at, wu_at, d_at, sums_at, parts_at, bytes;
-    GatedMma main, dx, dw;
+    GatedMma main, grads[2];   // dX; dWg and dWu
+    GatedPlan main_plan, grads_plan;
 };
 
 // Up to this many tokens the weights' and their gradients' bytes bound the
@@ -119,7 +121,7 @@ struct Plan {
 // roundings to 8 bits do not average out.
 constexpr int64_t kFewTokens = 128;
 
-Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
+Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, bool dx = true, bool dw = true) {
     Plan p = {};
     p.parts = dt == BSR_F32 ? 3 : 1;
     p.d_parts = dt == BSR_F32 ? 3 : N <= kFewTokens ? 2 : 1;
@@ -140,23 +142,27 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
     m.mode = backward ? GM_BACKWARD : GM_FORWARD;
     m.a.planes = p.parts;
     m.M = N, m.N = F, m.K = K, m.Fp = p.Fp;
-    plan_gated_mma(m);
+    p.main_plan = plan_gated_mma(&m, 1);
     if (!backward) return p;
     p.d_at = take(p.d_parts * N * 2 * p.Fp * 2);
     p.sums_at = take((N + 31) / 32 * 2 * p.Fp * 4);
-    GatedMma &x = p.dx, &w = p.dw;
+    GatedMma &x = p.grads[0], &w = p.grads[1];
     x.mode = w.mode = GM_PRODUCT;
     x.a.planes = w.a.planes = m.d_planes = p.d_parts;
     x.M = N, x.N = K, x.K = 2 * p.Fp;
-    x.b_side = true;
     x.b_seam = p.Fp;
     x.row_seam = x.out_rows = N;
     w.M = 2 * p.Fp, w.N = K, w.K = N;
-    w.a_side = w.b_side = true;
+    w.a_side = true;
     w.row_seam = p.Fp, w.out_rows = F;
-    plan_gated_mma(x);
-    plan_gated_mma(w);
-    p.parts_at = take(std::max(x.part_bytes, w.part_bytes));
+    // the one with the longer sums first: the tiles of the last round are split
+    p.first = x.K >= w.K ? 0 : 1;
+    if (p.first) std::swap(x, w);
+    p.parts_at = p.bytes;
+    if (dx || dw) {
+        p.grads_plan = plan_gated_mma(dx && dw ? p.grads : &p.grads[(dx ? 0 : 1) ^ p.first], dx + dw);
+        take(p.grads_plan.part_bytes);
+    }
     return p;
 }
 
@@ -183,7 +189,11 @@ cudaError_t operands(const GatedCall &c, const Plan &p, Planes (&m)[3], cudaStre
 }  // namespace
 
 int64_t gated_workspace(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
-    return N == 0 ? 0 : plan_of(N, F, K, dt, backward).bytes;
+    if (N == 0) return 0;
+    int64_t most = plan_of(N, F, K, dt, backward).bytes;
+    if (backward)   // (less is needed where only some gradients are wanted, but for the parts of another split)
+        for (int one = 0; one < 2; one++) most = std::max(most, plan_of(N, F, K, dt, true, one == 0, one == 1).bytes);
+    return most;
 }
 
 cudaError_t launch_gated(const GatedCall &c, cudaStream_t s) {
@@ -197,37 +207,32 @@ cudaError_t launch_gated(const GatedCall &c, cudaStream_t s) {
     g.bg = c.bg, g.bu = c.bu;
     g.act = c.act;
     g.H = c.H;
-    return launch_gated_mma(g, s);
+    return launch_gated_mma(&g, p.main_plan, s);
 }
 
 cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
-    Plan p = plan_of(c.N, c.F, c.K, c.dt, true);
+    const bool dx = c.dX, dw = c.dWg;
+    Plan p = plan_of(c.N, c.F, c.K, c.dt, true, dx, dw);
     unsigned char *ws = static_cast<unsigned char *>(c.ws);
     Planes m[3];
     cudaError_t e = operands(c, p, m, s);
     if (e != cudaSuccess) return e;
-    GatedMma &g = p.main;
-    g.dt = p.dx.dt = p.dw.dt = c.dt;
+    GatedMma &g = p.main, &x = p.grads[p.first], &w = p.grads[1 - p.first];
+    g.dt = x.dt = w.dt = c.dt;
     g.a = m[0], g.b0 = m[1], g.b1 = m[2];
     g.bg = c.bg, g.bu = c.bu;
     g.act = c.act;
     g.dH = c.dH;
     g.D = reinterpret_cast<uint16_t *>(ws + p.d_at);
     g.sums = c.dbg || c.dbu ? reinterpret_cast<float *>(ws + p.sums_at) : nullptr;
-    e = launch_gated_mma(g, s);
-    const Planes d{g.D, c.N, 2 * p.Fp, 2 * p.Fp, p.d_parts};
-    if (e == cudaSuccess && c.dX) {
-        p.dx.a = d, p.dx.b0 = m[1], p.dx.b1 = m[2];
-        p.dx.out0 = p.dx.out1 = c.dX;
-        p.dx.parts = reinterpret_cast<float *>(ws + p.parts_at);
-        e = launch_gated_mma(p.dx, s);
-    }
-    if (e == cudaSuccess && c.dWg) {
-        p.dw.a = d, p.dw.b0 = m[0];
-        p.dw.out0 = c.dWg, p.dw.out1 = c.dWu;
-        p.dw.parts = reinterpret_cast<float *>(ws + p.parts_at);
-        e = launch_gated_mma(p.dw, s);
-    }
+    e = launch_gated_mma(&g, p.main_plan, s);
+    x.a = w.a = Planes{g.D, c.N, 2 * p.Fp, 2 * p.Fp, p.d_parts};
+    x.b0 = m[1], x.b1 = m[2];
+    x.out0 = x.out1 = c.dX;
+    w.b0 = m[0];
+    w.out0 = c.dWg, w.out1 = c.dWu;
+    p.grads_plan.parts = reinterpret_cast<float *>(ws + p.parts_at);
+    if (e == cudaSuccess && (dx || dw)) e = launch_gated_mma(dx && dw ? p.grads : dx ? &x : &w, p.grads_plan, s);
     if (e == cudaSuccess && g.sums)
         e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 8), 0, s, (const float *)g.sums, (c.N + 31) / 32, c.F,
                           p.Fp, c.dbg, c.dbu);

@@ -6,22 +6,24 @@
 // gated modes one CTA loads `half` rows of Wg and the other of Wu, so that the
 // same thread finds G and U of a feature in its tensor-memory lane.
 //
-//   warps 0, 1, 3  producers, a step each in turn: the step's A tiles (128 rows
-//                  x 64 of K a CTA) and B tiles (`half` rows x 64) by TMA
-//                  (128-byte swizzle) into a stage of the ring
+//   warps 0, 1, 3  producers, a step each in turn: 64 columns of K, the A tile
+//                  (128 rows a CTA) and the B tile (`half` rows) by TMA (128-byte
+//                  swizzle) into a stage of the ring
 //   warp 2         MMAs (M = 256, N = 2 half, K = 16) of the pair's first CTA
-//   warps 4-11     epilogue: 32 rows and half of the columns each, straight
-//                  from tensor memory to global memory
+//   warps 4 ..     epilogue, 16 (fp32: 8) warps: 32 rows and a share of the
+//                  columns each, straight from tensor memory to global memory
 //
-// A step is 128 columns of K (fp32: 64): 1024 (3072) SM cycles of MMAs at 256
-// columns. Waiting for a stage, one load of 64 columns and moving on take a
-// producer about 740 cycles; with 64 columns a step and one warp each for A and
-// B, the producers were the bound (8192 tokens of 1024 features into 4096, bf16:
-// 95 us, the MMAs 62).
+// A step is 512 SM cycles of MMAs at 256 columns (fp32: 3072). Waiting for a
+// stage, its loads and moving on take a producer about 750 cycles, so one warp
+// for A and one for B were the bound (8192 tokens of 1024 features into 4096,
+// bf16: 95 us, the MMAs 62). Stages of 128 columns were too few to cover the
+// loads' latency (89 us).
 //
 // Persistent: one CTA per SM; two accumulator buffers of 256 columns let a
-// tile's epilogue overlap the next tile's MMAs. Plain products split the K of
-// the tiles that would fill the last round only in part.
+// tile's epilogue overlap the next tile's MMAs. The epilogue waits for its loads
+// and stores, a row a lane, more than it computes, hence the many warps. Two
+// plain products may share a launch, and those tiles that would fill the last
+// round only in part have their K split.
 //
 // Operands stored with K along rows (weights for dX; dG, dU and X for the
 // weights' gradients) are read in place: TMA boxes of 64 x 64 and descriptors
@@ -38,6 +40,7 @@
 // returns.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <cstdlib>
 
 #include "act.cuh"
@@ -55,10 +58,11 @@ namespace {
 
 constexpr int KC = 64;                        // columns of K per chunk
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's A tile
-constexpr int kEpiWarps = 8, kEpiWarp0 = 4, kMmaWarp = 2;
-constexpr int kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kEpiWarp0 = 4, kMmaWarp = 2;
+constexpr int epi_warps(bool f32) { return f32 ? 8 : 16; }
+constexpr int threads_of(bool f32) { return 32 * (kEpiWarp0 + epi_warps(f32)); }
 constexpr int kStages = 8;
-constexpr uint32_t kBiasBytes = kEpiWarps * 128 * 4;
+constexpr uint32_t kBiasBytes = 8 * 128 * 4;  // a warp's share of bg and bu: 64 (fp32), 32 features
 constexpr uint32_t kMaxSmem = 227 * 1024 - 1024;
 constexpr uint32_t kAccCols = 256;
 constexpr int kProducers = 3;
@@ -66,27 +70,35 @@ constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs alrea
 
 __device__ int g_status;
 
-struct Args {
+// One product.
+struct Job {
     CUtensorMap a, b0, b1;
     int64_t M, N;             // rows; columns (gated modes: features)
-    unsigned tiles_n, whole, units;   // tiles along N; units that are whole tiles (they come first)
-    int splits;               // units of every other tile
-    int chunks, steps, seam;  // chunks of K, steps of a tile; the chunk from which b1 is read
-    int half, ns;
-    uint32_t stage_bytes, idesc;
-    int a_tiles, b_tiles;     // in a stage
+    unsigned tiles_n;         // tiles along N
+    int steps, seam;          // steps of a tile; the step from which b1 is read
+    uint32_t idesc;
     int a_side, b_side;
+    void *out0, *out1;        // gated forward: H in out0
+    int64_t row_seam, out_rows;
+    int vec;                  // output (and dH) rows start on 32-byte boundaries
+};
+
+struct Args {
+    Job job[2];
+    unsigned second;          // the second job's first tile
+    unsigned whole, units;    // units that are whole tiles (they come first)
+    int splits;               // units of every other tile
+    int half, ns;
+    uint32_t stage_bytes;
+    int a_tiles, b_tiles;     // in a stage
     const float *bg, *bu;
     int act;
     const void *dH;
-    void *out0, *out1;        // gated forward: H in out0
     uint16_t *D;
     int d_planes;
     int64_t Fp;
     float *sums;
-    int64_t row_seam, out_rows;
     float *parts;
-    int vec;                  // output (and dH) rows start on 32-byte boundaries
     uint64_t wait_ns;
     int stall_step;           // test hook: this step of each tile is never loaded (-1: none)
 };
@@ -95,37 +107,44 @@ struct Unit {
     int64_t m0, n0;   // first row, first column (gated modes: feature)
     int i0, i1;       // steps
     int part;         // index of the unit's part, -1 for a whole tile
+    int job;
 };
 
 template <int MODE>
 __device__ __forceinline__ Unit unit_at(const Args &a, unsigned v) {
     Unit u;
     u.part = -1;
-    u.i0 = 0;
-    u.i1 = a.steps;
+    unsigned k = 0;
     if (MODE == GM_PRODUCT && v >= a.whole) {
         u.part = (int)(v - a.whole);
-        const unsigned tile = (unsigned)u.part / (unsigned)a.splits, k = (unsigned)u.part - tile * (unsigned)a.splits;
+        const unsigned tile = (unsigned)u.part / (unsigned)a.splits;
+        k = (unsigned)u.part - tile * (unsigned)a.splits;
         v = a.whole + tile;
-        u.i0 = (int)((int64_t)a.steps * k / a.splits);
-        u.i1 = (int)((int64_t)a.steps * (k + 1) / a.splits);
     }
-    const unsigned tm = v / a.tiles_n, tn = v - tm * a.tiles_n;
+    u.job = MODE == GM_PRODUCT && v >= a.second;
+    if (u.job) v -= a.second;
+    const Job &j = a.job[u.job];
+    u.i0 = 0;
+    u.i1 = j.steps;
+    if (MODE == GM_PRODUCT && u.part >= 0) {
+        u.i0 = (int)((int64_t)j.steps * k / a.splits);
+        u.i1 = (int)((int64_t)j.steps * (k + 1) / a.splits);
+    }
+    const unsigned tm = v / j.tiles_n, tn = v - tm * j.tiles_n;
     u.m0 = (int64_t)tm * 256;
     u.n0 = (int64_t)tn * (MODE == GM_PRODUCT ? 2 * a.half : a.half);
     return u;
 }
 
-// The products of a step, the smallest first: tiles of A and B. fp32: parts
-// (2,0) (1,1) (0,2) (1,0) (0,1) (0,0) of one chunk; bf16: two chunks, or one
-// chunk with two parts of A.
+// The products of a step, the smallest first: parts of A and B. fp32: (2,0) (1,1)
+// (0,2) (1,0) (0,1) (0,0); two parts of A: (1,0) (0,0).
 template <bool F32>
-__device__ __forceinline__ int a_tile_of(const Args &a, int i, int n) {
-    return F32 ? (0x001012 >> (4 * i)) & 3 : a.b_tiles == 1 ? n - 1 - i : i;
+__device__ __forceinline__ int a_tile_of(int i, int n) {
+    return F32 ? (0x001012 >> (4 * i)) & 3 : n - 1 - i;
 }
 template <bool F32>
-__device__ __forceinline__ int b_tile_of(const Args &a, int i) {
-    return F32 ? (0x010210 >> (4 * i)) & 3 : a.b_tiles == 1 ? 0 : i;
+__device__ __forceinline__ int b_tile_of(int i) {
+    return F32 ? (0x010210 >> (4 * i)) & 3 : 0;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -231,7 +250,7 @@ __device__ __forceinline__ void parts_of(float x, float (&p)[3]) {
 // Puts out 16 columns of this thread's row: gated modes G in v and U in w of
 // features f ..; GM_PRODUCT columns c .. in v and c + 16 .. in w.
 template <int MODE, typename T>
-__device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, int64_t c, float (&v)[16], float (&w)[16],
+__device__ __forceinline__ void put(const Args &a, const Job &job, const Unit &u, int64_t row, int64_t c, float (&v)[16], float (&w)[16],
                                     const float *bias_g, const float *bias_u, const float (&d)[16]) {
     constexpr bool FAST = sizeof(T) == 2;
     if constexpr (MODE != GM_PRODUCT) {
@@ -255,7 +274,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
 #pragma unroll
             for (int j = 0; j < 16; j++) v[j] = activate<decltype(tag)::value, FAST>(v[j]) * w[j];
         });
-        if (row < a.M) store16(static_cast<T *>(a.out0) + row * a.N, c, a.N, a.vec, v);
+        if (row < job.M) store16(static_cast<T *>(job.out0) + row * job.N, c, job.N, job.vec, v);
     } else if constexpr (MODE == GM_BACKWARD) {
         with_act(a.act, [&](auto tag) {
 #pragma unroll
@@ -265,7 +284,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
                 w[j] = d[j] * s.x;
             }
         });
-        if (row >= a.M) {   // (the sums below)
+        if (row >= job.M) {   // (the sums below)
 #pragma unroll
             for (int j = 0; j < 16; j++) v[j] = w[j] = 0.f;
         }
@@ -273,9 +292,9 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
             const float sg = lane_sums(v), su = lane_sums(w);
             const int lane = threadIdx.x & 31;
             float *at = a.sums + (row >> 5) * 2 * a.Fp + c;
-            if ((row & ~(int64_t)31) < a.M) at[lane < 16 ? lane : a.Fp + lane - 16] = lane < 16 ? sg : su;
+            if ((row & ~(int64_t)31) < job.M) at[lane < 16 ? lane : a.Fp + lane - 16] = lane < 16 ? sg : su;
         }
-        if (row < a.M && c < a.Fp) {
+        if (row < job.M && c < a.Fp) {
             uint16_t *at = a.D + row * 2 * a.Fp + c;
             if constexpr (FAST) {
                 store16(at, 0, 16, true, v);
@@ -286,7 +305,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
                         v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
                         w[j] -= __bfloat162float(__float2bfloat16_rn(w[j]));
                     }
-                    at += 2 * a.Fp * a.M;
+                    at += 2 * a.Fp * job.M;
                     store16(at, 0, 16, true, v);
                     store16(at + a.Fp, 0, 16, true, w);
                 }
@@ -301,7 +320,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
                         p[0][j] = q[0], p[1][j] = q[1], p[2][j] = q[2];
                     }
 #pragma unroll
-                    for (int i = 0; i < 3; i++) store16(at + k * a.Fp + i * 2 * a.Fp * a.M, 0, 16, true, p[i]);
+                    for (int i = 0; i < 3; i++) store16(at + k * a.Fp + i * 2 * a.Fp * job.M, 0, 16, true, p[i]);
                 }
             }
         }
@@ -312,19 +331,20 @@ __device__ __forceinline__ void put(const Args &a, const Unit &u, int64_t row, i
             store16(at, 16, 32, true, w);
             return;
         }
-        if (row >= a.M) return;
-        const bool second = row >= a.row_seam;
-        const int64_t r = second ? row - a.row_seam : row;
-        if (r >= a.out_rows) return;
-        T *out = static_cast<T *>(second ? a.out1 : a.out0) + r * a.N;
-        store16(out, c, a.N, a.vec, v);
-        store16(out, c + 16, a.N, a.vec, w);
+        if (row >= job.M) return;
+        const bool second = row >= job.row_seam;
+        const int64_t r = second ? row - job.row_seam : row;
+        if (r >= job.out_rows) return;
+        T *out = static_cast<T *>(second ? job.out1 : job.out0) + r * job.N;
+        store16(out, c, job.N, job.vec, v);
+        store16(out, c + 16, job.N, job.vec, w);
     }
 }
 
 template <int MODE, typename T>
-__global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(const __grid_constant__ Args a) {
     constexpr bool F32 = sizeof(T) == 4;
+    constexpr int kEpiWarps = epi_warps(F32);
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
     const int ns = a.ns;
@@ -398,34 +418,28 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
         if (i == a.stall_step) {   // never loaded: its consumer times out
             stalled |= 1u << s;
         } else if (elected) {
+            const Job &job = a.job[un.job];
             const uint32_t dst = smem0 + s * stage_bytes, bar = first0 + 8 * s;
-            const bool chunks2 = !F32 && a.b_tiles == 2;
-            const int c0 = chunks2 ? 2 * i : i;
-            // a tile's last step may have one chunk only
-            const int na = chunks2 ? min(2, a.chunks - c0) : a.a_tiles, nb = chunks2 ? na : a.b_tiles;
-            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (na * kABytes + nb * b_bytes));
-            const int m = (int)(un.m0 + rank * 128);
-            for (int t = 0; t < na; t++) {
-                const int k = (chunks2 ? c0 + t : c0) * KC, part = chunks2 ? 0 : t;
+            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (a.a_tiles * kABytes + a.b_tiles * b_bytes));
+            const int m = (int)(un.m0 + rank * 128), n = (int)(un.n0 + (MODE == GM_PRODUCT ? rank * a.half : 0));
+            const bool second = MODE == GM_PRODUCT && job.seam && i >= job.seam;
+            const int k = i * KC, kb = second ? (i - job.seam) * KC : k;
+            const CUtensorMap *map = (MODE == GM_PRODUCT ? second : rank) ? &job.b1 : &job.b0;
+            for (int t = 0; t < a.a_tiles; t++) {
                 const uint32_t to = dst + t * kABytes;
-                if (a.a_side) {
-                    ptx::tma_load_3d_pair_at(to, &a.a, m, k, part, bar);
-                    ptx::tma_load_3d_pair_at(to + 8192, &a.a, m + 64, k, part, bar);
+                if (MODE == GM_PRODUCT && job.a_side) {
+                    ptx::tma_load_3d_pair_at(to, &job.a, m, k, t, bar);
+                    ptx::tma_load_3d_pair_at(to + 8192, &job.a, m + 64, k, t, bar);
                 } else {
-                    ptx::tma_load_3d_pair_at(to, &a.a, k, m, part, bar);
+                    ptx::tma_load_3d_pair_at(to, &job.a, k, m, t, bar);
                 }
             }
-            const int n = (int)(un.n0 + (MODE == GM_PRODUCT ? rank * a.half : 0));
-            for (int t = 0; t < nb; t++) {
-                const int c = chunks2 ? c0 + t : c0, part = chunks2 ? 0 : t;
+            for (int t = 0; t < a.b_tiles; t++) {
                 const uint32_t to = dst + b_at + t * b_bytes;
-                if (MODE != GM_PRODUCT) {
-                    ptx::tma_load_3d_pair_at(to, rank ? &a.b1 : &a.b0, c * KC, n, part, bar);
+                if (MODE == GM_PRODUCT) {   // (b_side: every plain product's)
+                    for (int j = 0; j < a.half; j += 64) ptx::tma_load_3d_pair_at(to + 128 * j, map, n + j, kb, t, bar);
                 } else {
-                    const bool second = a.seam && c >= a.seam;
-                    const int k = (second ? c - a.seam : c) * KC;
-                    const CUtensorMap *map = second ? &a.b1 : &a.b0;
-                    for (int j = 0; j < a.half; j += 64) ptx::tma_load_3d_pair_at(to + 128 * j, map, n + j, k, part, bar);
+                    ptx::tma_load_3d_pair_at(to, map, kb, n, t, bar);
                 }
             }
         }
@@ -437,9 +451,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
     bool more = false;
     if (producer) {
         if (elected) {
-            ptx::prefetch_tensormap(&a.a);
-            ptx::prefetch_tensormap(&a.b0);
-            ptx::prefetch_tensormap(&a.b1);
+            for (int j = 0; j < (MODE == GM_PRODUCT ? 2 : 1); j++) {
+                ptx::prefetch_tensormap(&a.job[j].a);
+                ptx::prefetch_tensormap(&a.job[j].b0);
+                ptx::prefetch_tensormap(&a.job[j].b1);
+            }
         }
         un = unit_at<MODE>(a, v);
         i = un.i0 + prod;
@@ -463,13 +479,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
             uint32_t fphase = 0, aphase = 1;
             bool ok = true;
             s = 0;
-            const uint64_t ad0 = a.a_side ? tc5::desc_sw128_mn(smem0, 8192) : tc5::desc_sw128(smem0);
-            const uint64_t bd0 = a.b_side ? tc5::desc_sw128_mn(smem0 + b_at, 8192) : tc5::desc_sw128(smem0 + b_at);
-            // 16 of K: two groups of eight 128-byte rows, or 32 bytes along the rows
-            const uint32_t a_step = a.a_side ? 128 : 2, b_step = a.b_side ? 128 : 2;
             ptx::pdl_wait();   // the waits below are bounded from here on
             for (; ok && v < a.units; v += pairs) {
                 un = unit_at<MODE>(a, v);
+                const Job &job = a.job[un.job];
+                const bool a_side = MODE == GM_PRODUCT && job.a_side, b_side = MODE == GM_PRODUCT;
+                const uint64_t ad0 = a_side ? tc5::desc_sw128_mn(smem0, 8192) : tc5::desc_sw128(smem0);
+                const uint64_t bd0 = b_side ? tc5::desc_sw128_mn(smem0 + b_at, 8192) : tc5::desc_sw128(smem0 + b_at);
+                // 16 of K: two groups of eight 128-byte rows, or 32 bytes along the rows
+                const uint32_t a_step = a_side ? 128 : 2, b_step = b_side ? 128 : 2, idesc = job.idesc;
                 for (i = un.i0; ok && i < un.i1; i++) {
                     const uint32_t d = tmem + (uint32_t)ab * kAccCols;
                     if (F32 || i == un.i0) {   // into a fresh accumulator buffer
@@ -481,15 +499,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
                     tc5::fence_after();
                     if (elected) {
                         const uint64_t at = (uint64_t)((s * stage_bytes) >> 4);
-                        const int n = F32 ? 6 : a.b_tiles == 1 ? a.a_tiles : min(2, a.chunks - 2 * i);
+                        const int n = F32 ? 6 : a.a_tiles;
 #pragma unroll
                         for (int t = 0; t < (F32 ? 6 : 2); t++) {
                             if (t >= n) break;
-                            const uint64_t ad = ad0 + at + a_tile_of<F32>(a, t, n) * (kABytes >> 4);
-                            const uint64_t bd = bd0 + at + b_tile_of<F32>(a, t) * (b_bytes >> 4);
+                            const uint64_t ad = ad0 + at + a_tile_of<F32>(t, n) * (kABytes >> 4);
+                            const uint64_t bd = bd0 + at + b_tile_of<F32>(t) * (b_bytes >> 4);
 #pragma unroll
                             for (int j = 0; j < KC / 16; j++)
-                                tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, a.idesc,
+                                tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, idesc,
                                                  (!F32 && i > un.i0) | (t > 0) | (j > 0));
                         }
                         tc5::commit_pair(&empty[s]);
@@ -522,30 +540,32 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
             ptx::mbar_wait_bounded(&done, 0, kDrainNs);
         }
     } else if (warp >= kEpiWarp0) {
-        const int q = warp & 3, hc = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., half hc of the columns
-        float *bs = bias_s + (warp - kEpiWarp0) * 128;
-        const int pieces = a.half / 32;   // of 2 x 16 columns
-        // columns of a piece's two sixteens in the accumulators: G and U of the same features, or neighbours
-        const int col0 = MODE == GM_PRODUCT ? hc * a.half : hc * (a.half / 2), step = MODE == GM_PRODUCT ? 32 : 16,
-                  other = MODE == GM_PRODUCT ? 16 : a.half;
+        constexpr int kShares = kEpiWarps / 4, kMost = 8 / kShares;   // the columns' shares; most pieces of one
+        const int q = warp & 3, hc = (warp - kEpiWarp0) >> 2;          // tensor-memory lanes 32 q .., share hc
+        float *bs = bias_s + (warp - kEpiWarp0) * (kMost * 32);
+        // pieces of 2 x 16 columns: G and U of the same features, or neighbours; the share's first in the accumulators
+        const int all = a.half / 16, pieces = min((all + kShares - 1) / kShares, max(0, all - hc * ((all + kShares - 1) / kShares)));
+        const int step = MODE == GM_PRODUCT ? 32 : 16, other = MODE == GM_PRODUCT ? 16 : a.half;
+        const int col0 = hc * ((all + kShares - 1) / kShares) * step;
         ptx::pdl_wait();   // the outputs and dH may be an earlier kernel's
         int ab = 0;
         uint32_t fphase = 0;
         bool ok = true;
         for (; ok && v < a.units; v += pairs) {
             un = unit_at<MODE>(a, v);
+            const Job &job = a.job[un.job];
             const int64_t row = un.m0 + rank * 128 + 32 * q + lane;
             if (MODE != GM_PRODUCT && (a.bg || a.bu)) {
                 __syncwarp();   // (the last unit's biases have been read)
-                for (int j = lane; j < a.half / 2; j += 32) {
+                for (int j = lane; j < 16 * pieces; j += 32) {
                     const int64_t f = un.n0 + col0 + j;
-                    bs[j] = a.bg && f < a.N ? __ldg(a.bg + f) : 0.f;
-                    bs[64 + j] = a.bu && f < a.N ? __ldg(a.bu + f) : 0.f;
+                    bs[j] = a.bg && f < job.N ? __ldg(a.bg + f) : 0.f;
+                    bs[16 * kMost + j] = a.bu && f < job.N ? __ldg(a.bu + f) : 0.f;
                 }
                 __syncwarp();
             }
-            const T *dh = static_cast<const T *>(a.dH) + row * a.N;
-            const bool mine = MODE == GM_BACKWARD && row < a.M;
+            const T *dh = static_cast<const T *>(a.dH) + row * job.N;
+            const bool mine = MODE == GM_BACKWARD && row < job.M;
             const uint64_t limit = a.wait_ns * (uint64_t)(un.i1 - un.i0 + 2);
             // waits for the next accumulator buffer; its columns of this warp's lanes
             auto wait_acc = [&]() {
@@ -563,46 +583,40 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
                 if (ab == 0) fphase ^= 1;
             };
             if constexpr (!F32) {
-                // a piece ahead: accumulators and dH on their way while one is put out
-                uint32_t r[2][16];
                 float d[16] = {};
-                if (mine) load16(dh, un.n0 + col0, a.N, a.vec, d);
+                if (mine && pieces > 0) load16(dh, un.n0 + col0, job.N, job.vec, d);
                 const uint32_t tm = wait_acc();
                 if (!ok) break;
-                tc5::ld16(tm, r[0]);
-                tc5::ld16(tm + other, r[1]);
+                if (pieces == 0) hand_back();
 #pragma unroll 1
                 for (int p = 0; p < pieces; p++) {
-                    float x[16], y[16], dp[16];
+                    uint32_t r0[16], r1[16];
+                    tc5::ld16(tm + p * step, r0);
+                    tc5::ld16(tm + p * step + other, r1);
+                    if (mine && p > 0) load16(dh, un.n0 + col0 + p * step, job.N, job.vec, d);
                     tc5::ld_wait();
+                    float x[16], y[16];
 #pragma unroll
                     for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
-                        asm volatile("" : "+r"(r[0][j]));
-                        asm volatile("" : "+r"(r[1][j]));
-                        x[j] = __uint_as_float(r[0][j]);
-                        y[j] = __uint_as_float(r[1][j]);
-                        dp[j] = d[j];
+                        asm volatile("" : "+r"(r0[j]));
+                        asm volatile("" : "+r"(r1[j]));
+                        x[j] = __uint_as_float(r0[j]);
+                        y[j] = __uint_as_float(r1[j]);
                     }
-                    if (p + 1 < pieces) {
-                        tc5::ld16(tm + (p + 1) * step, r[0]);
-                        tc5::ld16(tm + (p + 1) * step + other, r[1]);
-                        if (mine) load16(dh, un.n0 + col0 + (p + 1) * step, a.N, a.vec, d);
-                    } else {
-                        hand_back();
-                    }
-                    put<MODE, T>(a, un, row, un.n0 + col0 + p * step, x, y, bs + 16 * p, bs + 64 + 16 * p, dp);
+                    if (p + 1 == pieces) hand_back();
+                    put<MODE, T>(a, job, un, row, un.n0 + col0 + p * step, x, y, bs + 16 * p, bs + 16 * kMost + 16 * p, d);
                 }
             } else {
-                float g[4][16], w[4][16];   // the sums of the steps so far
+                float g[kMost][16], w[kMost][16];   // the sums of the steps so far
 #pragma unroll
-                for (int p = 0; p < 4; p++)
+                for (int p = 0; p < kMost; p++)
 #pragma unroll
                     for (int j = 0; j < 16; j++) g[p][j] = w[p][j] = 0.f;
                 for (int b = un.i0; b < un.i1; b++) {
                     const uint32_t tm = wait_acc();
                     if (!ok) break;
 #pragma unroll
-                    for (int p = 0; p < 4; p++) {
+                    for (int p = 0; p < kMost; p++) {
                         if (p >= pieces) break;
                         uint32_t r0[16], r1[16];
                         tc5::ld16(tm + p * step, r0);
@@ -619,13 +633,21 @@ __global__ void __launch_bounds__(kThreads, 1) k_gated_mma(const __grid_constant
                     hand_back();
                 }
                 if (!ok) break;
-#pragma unroll
-                for (int p = 0; p < 4; p++) {
-                    if (p >= pieces) break;
-                    float d[16] = {};
+                // one copy of the code for all pieces: unrolled, it came from beyond the
+                // instruction caches (37000 cycles a unit of the backward pass)
+#pragma unroll 1
+                for (int p = 0; p < pieces; p++) {
+                    float d[16] = {}, x[16], y[16];
                     const int64_t c = un.n0 + col0 + p * step;
-                    if (mine) load16(dh, c, a.N, a.vec, d);
-                    put<MODE, T>(a, un, row, c, g[p], w[p], bs + 16 * p, bs + 64 + 16 * p, d);
+                    if (mine) load16(dh, c, job.N, job.vec, d);
+#pragma unroll
+                    for (int j = 0; j < 16; j++) {
+                        x[j] = g[0][j], y[j] = w[0][j];
+#pragma unroll
+                        for (int k = 1; k < kMost; k++)
+                            if (p == k) x[j] = g[k][j], y[j] = w[k][j];
+                    }
+                    put<MODE, T>(a, job, un, row, c, x, y, bs + 16 * p, bs + 16 * kMost + 16 * p, d);
                 }
             }
         }
@@ -686,23 +708,24 @@ __global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args
     ptx::pdl_wait();
     const int fours = a.half / 2, width = 2 * a.half;
     for (unsigned tile = blockIdx.y; tile < (a.units - a.whole) / (unsigned)a.splits; tile += gridDim.y) {
-        const unsigned tm = (a.whole + tile) / a.tiles_n, tn = a.whole + tile - tm * a.tiles_n;
+        const Unit un = unit_at<GM_PRODUCT>(a, a.whole + tile * (unsigned)a.splits);
+        const Job &job = a.job[un.job];
         const int e = blockIdx.x * 256 + threadIdx.x, r = e / fours, x = (e - r * fours) * 4;
-        const int64_t row = (int64_t)tm * 256 + r, c = (int64_t)tn * width + x;
-        if (r >= 256 || row >= a.M || c >= a.N) continue;
-        const bool second = row >= a.row_seam;
-        const int64_t at = second ? row - a.row_seam : row;
-        if (at >= a.out_rows) continue;
+        const int64_t row = un.m0 + r, c = un.n0 + x;
+        if (r >= 256 || row >= job.M || c >= job.N) continue;
+        const bool second = row >= job.row_seam;
+        const int64_t at = second ? row - job.row_seam : row;
+        if (at >= job.out_rows) continue;
         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < a.splits; k++) {
-            const float4 p = *reinterpret_cast<const float4 *>(a.parts + ((int64_t)(tile * a.splits + k) * 256 + r) * width + x);
+            const float4 p = *reinterpret_cast<const float4 *>(a.parts + ((int64_t)(un.part + k) * 256 + r) * width + x);
             t.x += p.x, t.y += p.y, t.z += p.z, t.w += p.w;
         }
-        T *out = static_cast<T *>(second ? a.out1 : a.out0) + at * a.N + c;
+        T *out = static_cast<T *>(second ? job.out1 : job.out0) + at * job.N + c;
         const float f[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
         for (int j = 0; j < 4; j++)
-            if (c + j < a.N) out[j] = from_f32<T>(f[j]);
+            if (c + j < job.N) out[j] = from_f32<T>(f[j]);
     }
 }
 
@@ -728,100 +751,127 @@ int pairs_of_sms() {
     return std::max(1, n / 2);
 }
 
-// A stage's tiles and bytes.
-void stage_of(const GatedMma &g, int half, int *a_tiles, int *b_tiles, uint32_t *bytes) {
-    *a_tiles = g.a.planes == 3 ? 3 : 2;
-    *b_tiles = g.a.planes == 3 ? 3 : g.a.planes == 2 ? 1 : 2;
-    *bytes = *a_tiles * kABytes + *b_tiles * (uint32_t)half * 128;
+// One job's arguments.
+template <int MODE, typename T>
+cudaError_t job_of(const GatedMma &g, const GatedShape &sh, Job &j) {
+    j.M = g.M, j.N = g.N;
+    j.tiles_n = (unsigned)sh.tiles_n;
+    j.steps = sh.steps;
+    j.seam = (int)(g.b_seam / KC);
+    j.idesc = tc5::idesc(false, 256, 2 * sh.half) | (g.a_side ? tc5::kIdescAmn : 0) | (MODE == GM_PRODUCT ? tc5::kIdescBmn : 0);
+    j.a_side = g.a_side;
+    j.out0 = MODE == GM_FORWARD ? g.H : g.out0;
+    j.out1 = g.out1;
+    j.row_seam = g.row_seam, j.out_rows = g.out_rows;
+    // 32-byte stores: base addresses and rows of 32-byte multiples
+    j.vec = g.N * (int64_t)sizeof(T) % 32 == 0 &&
+            (reinterpret_cast<uintptr_t>(j.out0) | reinterpret_cast<uintptr_t>(j.out1) | reinterpret_cast<uintptr_t>(g.dH)) % 32 == 0;
+    cudaError_t e = encode(g.a, g.a_side, 128, &j.a);
+    if (e == cudaSuccess) e = encode(g.b0, MODE == GM_PRODUCT, sh.half, &j.b0);
+    if (e == cudaSuccess) e = encode(g.b1.p ? g.b1 : g.b0, MODE == GM_PRODUCT, sh.half, &j.b1);
+    return e;
 }
 
 template <int MODE, typename T>
-cudaError_t launch(const GatedMma &g, cudaStream_t s) {
+cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
     Args a = {};
-    a.M = g.M, a.N = g.N;
-    a.half = g.half;
-    a.chunks = (int)((g.K + KC - 1) / KC);
-    a.steps = g.steps;
-    a.seam = (int)(g.b_seam / KC);
-    a.tiles_n = (unsigned)g.tiles_n;
-    a.splits = g.splits;
-    const int64_t units = g.whole + (g.tiles - g.whole) * g.splits;
+    const int64_t units = p.whole + (p.tiles - p.whole) * p.splits;
     if (units > INT32_MAX) return cudaErrorInvalidConfiguration;
-    a.whole = (unsigned)g.whole;
+    a.second = (unsigned)p.second;
+    a.whole = (unsigned)p.whole;
     a.units = (unsigned)units;
-    stage_of(g, g.half, &a.a_tiles, &a.b_tiles, &a.stage_bytes);
+    a.splits = p.splits;
+    a.half = p.half;
+    a.a_tiles = g->a.planes;
+    a.b_tiles = g->a.planes == 3 ? 3 : 1;
+    a.stage_bytes = a.a_tiles * kABytes + a.b_tiles * (uint32_t)p.half * 128;
     a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 1024 - kBiasBytes) / a.stage_bytes);
-    a.idesc = tc5::idesc(false, 256, 2 * g.half) | (g.a_side ? tc5::kIdescAmn : 0) | (g.b_side ? tc5::kIdescBmn : 0);
-    a.a_side = g.a_side, a.b_side = g.b_side;
-    a.bg = g.bg, a.bu = g.bu;
-    a.act = g.act;
-    a.dH = g.dH;
-    a.out0 = MODE == GM_FORWARD ? g.H : g.out0;
-    a.out1 = g.out1;
-    a.D = g.D, a.d_planes = g.d_planes;
-    a.Fp = g.Fp;
-    a.sums = g.sums;
-    a.row_seam = g.row_seam, a.out_rows = g.out_rows;
-    a.parts = g.parts;
-    // 32-byte stores: base addresses and rows of 32-byte multiples
-    a.vec = g.N * (int64_t)sizeof(T) % 32 == 0 &&
-            (reinterpret_cast<uintptr_t>(a.out0) | reinterpret_cast<uintptr_t>(a.out1) | reinterpret_cast<uintptr_t>(g.dH)) % 32 == 0;
+    a.bg = g->bg, a.bu = g->bu;
+    a.act = g->act;
+    a.dH = g->dH;
+    a.D = g->D, a.d_planes = g->d_planes;
+    a.Fp = g->Fp;
+    a.sums = g->sums;
+    a.parts = p.parts;
     const char *limit = std::getenv("BSR_WAIT_LIMIT_NS"), *stall = std::getenv("BSR_TEST_STALL_CHUNK");
     a.wait_ns = limit ? std::strtoull(limit, nullptr, 10) : 1000000000ull;
     a.stall_step = stall ? std::atoi(stall) : -1;
-    cudaError_t e = encode(g.a, g.a_side, 128, &a.a);
-    if (e == cudaSuccess) e = encode(g.b0, g.b_side, g.half, &a.b0);
-    if (e == cudaSuccess) e = encode(g.b1.p ? g.b1 : g.b0, g.b_side, g.half, &a.b1);
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < 2 && e == cudaSuccess; i++) {
+        const int k = i < p.jobs ? i : 0;
+        e = job_of<MODE, T>(g[k], p.shape[k], a.job[i]);
+    }
     static std::atomic<uint64_t> attr_set{0};
     if (e == cudaSuccess) e = allow_smem(k_gated_mma<MODE, T>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(units, pairs_of_sms());
-    e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(kThreads), a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
-    if (MODE != GM_PRODUCT || e != cudaSuccess || g.whole == g.tiles) return e;
-    return launch_kernel(k_join_parts<T>, dim3((unsigned)g.half / 2, (unsigned)std::min<int64_t>(g.tiles - g.whole, 65535)), dim3(256), 0, s,
+    e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(threads_of(sizeof(T) == 4)),
+                        a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
+    if (MODE != GM_PRODUCT || e != cudaSuccess || p.whole == p.tiles) return e;
+    return launch_kernel(k_join_parts<T>, dim3((unsigned)p.half / 2, (unsigned)std::min<int64_t>(p.tiles - p.whole, 65535)), dim3(256), 0, s,
                          a);
 }
 
 }  // namespace
 
-void plan_gated_mma(GatedMma &g) {
-    const int64_t pairs = pairs_of_sms(), tm = (g.M + 255) / 256, chunks = (g.K + KC - 1) / KC;
-    const bool product = g.mode == GM_PRODUCT, f32 = g.a.planes == 3;
-    g.steps = (int)(g.a.planes == 1 ? (chunks + 1) / 2 : chunks);
-    const int mmas = f32 ? 6 : 2;   // groups of four to a step
-    double best = 0;
+GatedPlan plan_gated_mma(const GatedMma *g, int n) {
+    const int64_t pairs = pairs_of_sms();
+    const bool product = g->mode == GM_PRODUCT;
+    const int groups = g->a.planes == 3 ? 6 : g->a.planes;   // of four MMAs to a step
+    GatedPlan best = {};
+    double best_t = 0;
     for (int half : {128, 64, 32}) {
         if (product && half < 64) break;   // (a box of 64 columns)
-        const int64_t tn = product ? (g.N + 2 * half - 1) / (2 * half) : (g.Fp + half - 1) / half, tiles = tm * tn;
-        // SM cycles of a step: 512 for four MMAs of 256 columns; narrower tiles wait for shared memory
-        const double step = mmas * std::max(512.0 * half / 128, 256.0);
-        for (int splits = 1; splits <= (product ? 16 : 1) && splits <= g.steps; splits++) {
-            // whole tiles as long as they fill all pairs
-            const int64_t whole = splits == 1 ? tiles : tiles / pairs * pairs;
-            const double rest = (double)(((tiles - whole) * splits + pairs - 1) / pairs);
-            // a unit's start and end; the parts are written and read again, and a launch added
-            double t = (double)((whole + pairs - 1) / pairs) * (g.steps * step + 1500);
-            if (splits > 1)
-                t += rest * ((double)(g.steps + splits - 1) / splits * step + 1500) + 5000 +
-                     (double)(tiles - whole) * splits * 256 * 2 * half * 8 / 4000;
-            if (best == 0 || t < best) {
-                best = t;
-                g.half = half;
-                g.splits = splits;
-                g.tiles = tiles, g.tiles_n = tn;
-                g.whole = whole;
-                g.part_bytes = (tiles - whole) * splits * 256 * 2 * half * 4;
+        GatedPlan p = {};
+        p.jobs = n;
+        p.half = half;
+        for (int i = 0; i < n; i++) {
+            GatedShape &sh = p.shape[i];
+            sh.half = half;
+            sh.steps = (int)((g[i].K + KC - 1) / KC);
+            sh.tiles_n = product ? (g[i].N + 2 * half - 1) / (2 * half) : (g[i].Fp + half - 1) / half;
+            if (i == 1) p.second = p.tiles;
+            p.tiles += (g[i].M + 255) / 256 * sh.tiles_n;
+        }
+        if (n == 1) p.second = p.tiles;
+        // SM cycles of a step: 512 for four MMAs of 256 columns; narrower tiles wait for their loads
+        const double step = groups * std::max(512.0 * half / 128, 400.0);
+        auto steps_at = [&](int64_t tile) { return p.shape[tile >= p.second].steps; };
+        // whole tiles as long as they fill all pairs, a round of units after another
+        const int64_t full = p.tiles / pairs * pairs;
+        double rounds = 0;
+        for (int64_t at = 0; at < full; at += pairs) {
+            rounds += std::max(steps_at(at), steps_at(at + pairs - 1)) * step + 1500;
+            if (steps_at(at) == steps_at(full - 1)) {   // (and so on to the end)
+                rounds += (double)((full - at) / pairs - 1) * (steps_at(at) * step + 1500);
+                break;
+            }
+        }
+        const int most = full < p.tiles ? std::max(steps_at(full), steps_at(p.tiles - 1)) : 0;
+        const int least = full < p.tiles ? std::min(steps_at(full), steps_at(p.tiles - 1)) : 1;
+        for (int splits = 1; splits <= (product ? 16 : 1) && splits <= least; splits++) {
+            const double units = (double)((p.tiles - full) * splits);
+            double t = rounds + std::ceil(units / (double)pairs) * (std::ceil((double)most / splits) * step + 1500);
+            // the parts are written and read again, and a launch added
+            if (splits > 1) t += 5000 + units * 256 * 2 * half * 8 / 4000;
+            if (best_t == 0 || t < best_t) {
+                best_t = t;
+                best = p;
+                best.splits = splits;
+                best.whole = splits == 1 ? p.tiles : full;
+                best.part_bytes = (p.tiles - best.whole) * splits * 256 * 2 * half * 4;
             }
         }
     }
+    return best;
 }
 
-cudaError_t launch_gated_mma(const GatedMma &g, cudaStream_t s) {
-    const bool f32 = g.dt == BSR_F32;
-    switch (g.mode) {
-        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, s) : launch<GM_FORWARD, uint16_t>(g, s);
-        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, s) : launch<GM_BACKWARD, uint16_t>(g, s);
-        default: return f32 ? launch<GM_PRODUCT, float>(g, s) : launch<GM_PRODUCT, uint16_t>(g, s);
+cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
+    const bool f32 = g->dt == BSR_F32;
+    switch (g->mode) {
+        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, p, s) : launch<GM_FORWARD, uint16_t>(g, p, s);
+        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, p, s) : launch<GM_BACKWARD, uint16_t>(g, p, s);
+        default: return f32 ? launch<GM_PRODUCT, float>(g, p, s) : launch<GM_PRODUCT, uint16_t>(g, p, s);
     }
 }
 

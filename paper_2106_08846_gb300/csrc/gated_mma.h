@@ -28,7 +28,8 @@ struct GatedMma {
     int mode;
     bsr_dtype_t dt;           // of the outputs and dH
     Planes a, b0, b1;
-    bool a_side, b_side;      // the operand is stored [K, M] (or [K, N]), M (or N) contiguous; else [M, K]
+    // GM_PRODUCT: B is stored [K, N], N contiguous; with a_side A is stored [K, M], M contiguous. Else [M, K], [N, K].
+    bool a_side;
     int64_t M, N, K;          // sizes of the product; gated modes: M tokens, N features
     int64_t b_seam;           // GM_PRODUCT: from this k on, the columns of A meet b1 (0: b0 only)
     // gated modes
@@ -43,16 +44,26 @@ struct GatedMma {
     // GM_PRODUCT: rows below row_seam go to out0, those from it on to out1, `out_rows` in each
     void *out0, *out1;
     int64_t row_seam, out_rows;
-    float *parts;             // part_bytes
-    // chosen by plan_gated_mma
-    int half, steps, splits;
-    int64_t tiles, tiles_n, whole, part_bytes;
 };
 
-// Chooses, from the sizes, the tile width, the steps of a tile and, for
-// GM_PRODUCT, which tiles have their K split into how many parts.
-void plan_gated_mma(GatedMma &g);
-cudaError_t launch_gated_mma(const GatedMma &g, cudaStream_t s);
+struct GatedShape {
+    int half, steps;
+    int64_t tiles_n;
+};
+// How products run: the tile width, and which tiles (the last, of all products')
+// have their K split into how many parts.
+struct GatedPlan {
+    int jobs, half, splits;
+    GatedShape shape[2];
+    int64_t tiles, second, whole;   // tiles; the second product's first; those that are not split
+    int64_t part_bytes;
+    float *parts;                   // part_bytes of workspace
+};
+
+// The plan of g, or of two GM_PRODUCTs (as many parts each) in one launch, from
+// the modes and sizes.
+GatedPlan plan_gated_mma(const GatedMma *g, int n);
+cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s);
 
 // The first error that a kernel of this file recorded on the current device
 // since the last call; synchronises the device.
