@@ -5,12 +5,11 @@
 
 namespace bsr {
 
-// 1 / (1 + e^-x); FAST: the hardware's exponential and reciprocal, whose
-// relative error of about 2^-21 is lost in a result rounded to bf16.
+// 1 / (1 + e^-x); FAST: the hardware's exponential, whose relative error of about
+// 2^-21 is lost in a result rounded to bf16.
 template <bool FAST>
 __device__ __forceinline__ float logistic(float x) {
-    if constexpr (FAST) return __fdividef(1.f, 1.f + __expf(-x));
-    else return 1.f / (1.f + expf(-x));
+    return __fdividef(1.f, 1.f + (FAST ? __expf(-x) : expf(-x)));
 }
 
 constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)

@@ -11,7 +11,8 @@
 // side in the workspace as one bf16 matrix [N, 2 Fp], so that dX is one product
 // over 2 Fp columns and dWg and dWu are one product of 2 Fp rows. Operands that
 // the copy engine cannot read in place are laid out first: fp32 ones as three
-// bf16 parts, bf16 ones whose rows do not start on 16-byte boundaries padded.
+// bf16 parts, bf16 ones padded whose rows do not start on 16-byte boundaries or
+// whose weights are not whole groups of 32 rows.
 #include <algorithm>
 
 #include "bsr_internal.h"
@@ -29,7 +30,7 @@ namespace {
 struct Source {
     const void *src;
     uint16_t *dst;
-    int64_t rows;
+    int64_t rows, padded;   // rows, and those of a part (zeros past the matrix)
 };
 struct Sources {
     Source m[3];
@@ -47,22 +48,23 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const Source m = a.m[blockIdx.y];
-    const int64_t eights = a.Kp / 8, total = m.rows * eights;
+    const int64_t eights = a.Kp / 8, total = m.padded * eights;
     for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t row = i / eights, c = (i - row * eights) * 8;
         const T *src = static_cast<const T *>(m.src) + row * a.K + c;
+        const bool there = row < m.rows;
         uint16_t out[PARTS][8];
         if constexpr (PARTS == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) out[0][j] = c + j < a.K ? __ldg(src + j) : (uint16_t)0;
+            for (int j = 0; j < 8; j++) out[0][j] = there && c + j < a.K ? __ldg(src + j) : (uint16_t)0;
         } else {
             float v[8];
-            if (a.vec) {
+            if (a.vec && there) {
                 const float4 p = __ldg(reinterpret_cast<const float4 *>(src)), q = __ldg(reinterpret_cast<const float4 *>(src) + 1);
                 v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; j++) v[j] = c + j < a.K ? __ldg(src + j) : 0.f;
+                for (int j = 0; j < 8; j++) v[j] = there && c + j < a.K ? __ldg(src + j) : 0.f;
             }
 #pragma unroll
             for (int j = 0; j < 8; j++) {
@@ -78,7 +80,7 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; j++) w[j] = out[p][2 * j] | (uint32_t)out[p][2 * j + 1] << 16;
-            *reinterpret_cast<uint4 *>(m.dst + ((int64_t)p * m.rows + row) * a.Kp + c) = make_uint4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<uint4 *>(m.dst + ((int64_t)p * m.padded + row) * a.Kp + c) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
 }
@@ -109,7 +111,7 @@ struct Plan {
     int parts, d_parts;   // bf16 matrices to an operand, and to dG and dU
     bool lay_out;
     int first;            // where dX stands in `grads`
-    int64_t Kp, Fp;
+    int64_t Kp, Fp, Fr;   // padded sizes; the weights' rows
     int64_t x_at, wg_at, wu_at, d_at, sums_at, parts_at, bytes;
     GatedMma main, grads[2];   // dX; dWg and dWu
     GatedPlan main_plan, grads_plan;
@@ -125,7 +127,8 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     Plan p = {};
     p.parts = dt == BSR_F32 ? 3 : 1;
     p.d_parts = dt == BSR_F32 ? 3 : N <= kFewTokens ? 2 : 1;
-    p.lay_out = dt == BSR_F32 || K % 8 != 0;
+    p.lay_out = dt == BSR_F32 || K % 8 != 0 || F % 32 != 0;
+    p.Fr = p.lay_out ? round_up(F, backward ? 64 : 32) : F;
     p.Kp = round_up(K, 8);
     p.Fp = backward ? round_up(F, 64) : F;
     auto take = [&](int64_t bytes) {
@@ -135,8 +138,8 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     };
     if (p.lay_out) {
         p.x_at = take(p.parts * N * p.Kp * 2);
-        p.wg_at = take(p.parts * F * p.Kp * 2);
-        p.wu_at = take(p.parts * F * p.Kp * 2);
+        p.wg_at = take(p.parts * p.Fr * p.Kp * 2);
+        p.wu_at = take(p.parts * p.Fr * p.Kp * 2);
     }
     GatedMma &m = p.main;
     m.mode = backward ? GM_BACKWARD : GM_FORWARD;
@@ -145,7 +148,7 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     p.main_plan = plan_gated_mma(&m, 1);
     if (!backward) return p;
     p.d_at = take(p.d_parts * N * 2 * p.Fp * 2);
-    p.sums_at = take((N + 31) / 32 * 2 * p.Fp * 4);
+    p.sums_at = take((N + 15) / 16 * 2 * p.Fp * 4);
     GatedMma &x = p.grads[0], &w = p.grads[1];
     x.mode = w.mode = GM_PRODUCT;
     x.a.planes = w.a.planes = m.d_planes = p.d_parts;
@@ -169,14 +172,14 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
 // The operands X, Wg and Wu as the tensor cores read them.
 cudaError_t operands(const GatedCall &c, const Plan &p, Planes (&m)[3], cudaStream_t s) {
     const void *src[3] = {c.X, c.Wg, c.Wu};
-    const int64_t rows[3] = {c.N, c.F, c.F}, at[3] = {p.x_at, p.wg_at, p.wu_at};
+    const int64_t rows[3] = {c.N, c.F, c.F}, padded[3] = {c.N, p.Fr, p.Fr}, at[3] = {p.x_at, p.wg_at, p.wu_at};
     Sources a;
     a.K = c.K, a.Kp = p.Kp;
     a.vec = c.K % 8 == 0;
     for (int i = 0; i < 3; i++) {
         uint16_t *dst = reinterpret_cast<uint16_t *>(static_cast<unsigned char *>(c.ws) + at[i]);
-        a.m[i] = Source{src[i], dst, rows[i]};
-        m[i] = Planes{p.lay_out ? dst : static_cast<const uint16_t *>(src[i]), rows[i], p.lay_out ? p.Kp : c.K, p.lay_out ? p.Kp : c.K,
+        a.m[i] = Source{src[i], dst, rows[i], padded[i]};
+        m[i] = Planes{p.lay_out ? dst : static_cast<const uint16_t *>(src[i]), padded[i], p.lay_out ? p.Kp : c.K, p.lay_out ? p.Kp : c.K,
                       p.parts};
     }
     if (!p.lay_out) return cudaSuccess;
@@ -234,7 +237,7 @@ cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
     p.grads_plan.parts = reinterpret_cast<float *>(ws + p.parts_at);
     if (e == cudaSuccess && (dx || dw)) e = launch_gated_mma(dx && dw ? p.grads : dx ? &x : &w, p.grads_plan, s);
     if (e == cudaSuccess && g.sums)
-        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 8), 0, s, (const float *)g.sums, (c.N + 31) / 32, c.F,
+        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 8), 0, s, (const float *)g.sums, (c.N + 15) / 16, c.F,
                           p.Fp, c.dbg, c.dbu);
     return e;
 }

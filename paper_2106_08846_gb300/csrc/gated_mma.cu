@@ -25,6 +25,16 @@
 // plain products may share a launch, and those tiles that would fill the last
 // round only in part have their K split.
 //
+// The accumulators leave tensor memory so that a thread has two runs of eight
+// features, of two rows, and the four threads beside it the next ones: 64 (fp32:
+// 128) contiguous bytes of a row, eight rows an instruction. A row a lane took 61
+// cycles an instruction of 32 bytes a lane, in the way of the MMAs' reads of
+// shared memory (backward pass, 8192 tokens of 1024 into 4096: 12900 cycles a tile
+// of 8200 cycles of MMAs). To that end the weights' rows are loaded in another
+// order: row 8 i + 2 q + e of 32 is feature 8 q + 2 i + e (i, q < 4, e < 2), a box
+// of a five-dimensional tensor. (The plain products' epilogue, a row a lane, is
+// hidden behind their longer sums.)
+//
 // Operands stored with K along rows (weights for dX; dG, dU and X for the
 // weights' gradients) are read in place: TMA boxes of 64 x 64 and descriptors
 // with M or N contiguous.
@@ -77,10 +87,11 @@ struct Job {
     unsigned tiles_n;         // tiles along N
     int steps, seam;          // steps of a tile; the step from which b1 is read
     uint32_t idesc;
-    int a_side, b_side;
+    int a_side;
+    int groups;               // gated modes: groups of 32 rows of a part of B
     void *out0, *out1;        // gated forward: H in out0
     int64_t row_seam, out_rows;
-    int vec;                  // output (and dH) rows start on 32-byte boundaries
+    int vec;                  // output (and dH) rows take wide stores (and loads)
 };
 
 struct Args {
@@ -181,59 +192,75 @@ __device__ __forceinline__ void store16(float *row, int64_t c, int64_t cols, boo
             if (c + j < cols) row[c + j] = v[j];
     }
 }
-// 16 values of a row; 0 past its end
-__device__ __forceinline__ void load16(const uint16_t *row, int64_t c, int64_t cols, bool vec, float (&v)[16]) {
-    if (vec && c + 16 <= cols) {
+// Eight values of a row as they lie in memory: 16 bytes of bf16, 32 of fp32.
+template <typename T>
+struct Eight {
+    uint32_t w[2 * sizeof(T)];
+};
+__device__ __forceinline__ void unpack(const Eight<uint16_t> &r, float (&v)[8]) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4 *>(row + c) + h);
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++) {
-                v[8 * h + 2 * j] = __uint_as_float(w[j] << 16);
-                v[8 * h + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; j++) v[j] = c + j < cols ? to_f32(__ldg(row + c + j)) : 0.f;
+    for (int j = 0; j < 4; j++) {
+        v[2 * j] = __uint_as_float(r.w[j] << 16);
+        v[2 * j + 1] = __uint_as_float(r.w[j] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void load16(const float *row, int64_t c, int64_t cols, bool vec, float (&v)[16]) {
-    if (vec && c + 16 <= cols) {
+__device__ __forceinline__ void unpack(const Eight<float> &r, float (&v)[8]) {
 #pragma unroll
-        for (int h = 0; h < 4; h++) {
-            const float4 q = __ldg(reinterpret_cast<const float4 *>(row + c) + h);
-            v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
+    for (int j = 0; j < 8; j++) v[j] = __uint_as_float(r.w[j]);
+}
+__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {   // (16-byte aligned)
+    *reinterpret_cast<uint4 *>(p) =
+        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {   // (32-byte aligned)
+    uint32_t r[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) r[j] = __float_as_uint(v[j]);
+    ptx::st_global_32(p, r);
+}
+
+// dH of row `row` from feature c on; 0 past the matrix.
+template <typename T>
+__device__ __forceinline__ void fetch(const Args &a, const Job &job, int64_t row, int64_t c, Eight<T> &r) {
+    const T *p = static_cast<const T *>(a.dH) + row * job.N + c;
+    if (row < job.M && job.vec && c + 8 <= job.N) {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; h++) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + h);
+            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
         }
     } else {
+        constexpr int per = 4 / sizeof(T);   // values to a word
 #pragma unroll
-        for (int j = 0; j < 16; j++) v[j] = c + j < cols ? __ldg(row + c + j) : 0.f;
+        for (int j = 0; j < 2 * (int)sizeof(T); j++) {
+            r.w[j] = 0;
+#pragma unroll
+            for (int h = 0; h < per; h++)
+                if (row < job.M && c + per * j + h < job.N) {
+                    if constexpr (per == 2) r.w[j] |= (uint32_t)__ldg(p + 2 * j + h) << (16 * h);
+                    else r.w[j] = __float_as_uint(__ldg(p + j));
+                }
+        }
     }
 }
 
-// Sums of 16 values over a warp's lanes: lane l gets that of value l % 16.
-__device__ __forceinline__ float lane_sums(const float (&v)[16]) {
+// Sums of eight values over the lanes with the same lane % 4: lane l gets that of
+// value l / 4.
+__device__ __forceinline__ float row_sums(const float (&v)[8]) {
     const int lane = threadIdx.x & 31;
-    float a[8], b[4], c[2];
+    float b[4], c[2];
 #pragma unroll
-    for (int j = 0; j < 8; j++) {   // lanes with bit 3 keep the upper eight
-        const float mine = lane & 8 ? v[j + 8] : v[j], other = lane & 8 ? v[j] : v[j + 8];
-        a[j] = mine + __shfl_xor_sync(0xffffffffu, other, 8);
-    }
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const float mine = lane & 4 ? a[j + 4] : a[j], other = lane & 4 ? a[j] : a[j + 4];
-        b[j] = mine + __shfl_xor_sync(0xffffffffu, other, 4);
+    for (int j = 0; j < 4; j++) {   // lanes with bit 4 keep the upper four
+        const float mine = lane & 16 ? v[j + 4] : v[j], other = lane & 16 ? v[j] : v[j + 4];
+        b[j] = mine + __shfl_xor_sync(0xffffffffu, other, 16);
     }
 #pragma unroll
     for (int j = 0; j < 2; j++) {
-        const float mine = lane & 2 ? b[j + 2] : b[j], other = lane & 2 ? b[j] : b[j + 2];
-        c[j] = mine + __shfl_xor_sync(0xffffffffu, other, 2);
+        const float mine = lane & 8 ? b[j + 2] : b[j], other = lane & 8 ? b[j] : b[j + 2];
+        c[j] = mine + __shfl_xor_sync(0xffffffffu, other, 8);
     }
-    const float mine = lane & 1 ? c[1] : c[0], other = lane & 1 ? c[0] : c[1];
-    const float s = mine + __shfl_xor_sync(0xffffffffu, other, 1);
-    return s + __shfl_xor_sync(0xffffffffu, s, 16);
+    const float mine = lane & 4 ? c[1] : c[0], other = lane & 4 ? c[0] : c[1];
+    return mine + __shfl_xor_sync(0xffffffffu, other, 4);
 }
 
 // The three bf16 parts of a finite fp32 value, cut off and not rounded, so that
@@ -247,98 +274,126 @@ __device__ __forceinline__ void parts_of(float x, float (&p)[3]) {
     p[2] = r - p[1];
 }
 
-// Puts out 16 columns of this thread's row: gated modes G in v and U in w of
-// features f ..; GM_PRODUCT columns c .. in v and c + 16 .. in w.
+// Puts out G and U (v and w: eight features from c on of rows `row` and row + 8)
+// of a gated mode: H, or dG and dU.
 template <int MODE, typename T>
-__device__ __forceinline__ void put(const Args &a, const Job &job, const Unit &u, int64_t row, int64_t c, float (&v)[16], float (&w)[16],
-                                    const float *bias_g, const float *bias_u, const float (&d)[16]) {
+__device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t row, int64_t c, float (&v)[2][8], float (&w)[2][8],
+                                          const float *bias_g, const float *bias_u, const Eight<T> (&dh)[2]) {
     constexpr bool FAST = sizeof(T) == 2;
-    if constexpr (MODE != GM_PRODUCT) {
-        if (a.bg) {
+    if (a.bg || a.bu) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                const float4 b = *reinterpret_cast<const float4 *>(bias_g + j);
-                v[j] += b.x, v[j + 1] += b.y, v[j + 2] += b.z, v[j + 3] += b.w;
-            }
-        }
-        if (a.bu) {
+        for (int j = 0; j < 8; j += 4) {
+            const float4 g = *reinterpret_cast<const float4 *>(bias_g + j), u = *reinterpret_cast<const float4 *>(bias_u + j);
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                const float4 b = *reinterpret_cast<const float4 *>(bias_u + j);
-                w[j] += b.x, w[j + 1] += b.y, w[j + 2] += b.z, w[j + 3] += b.w;
+            for (int h = 0; h < 2; h++) {
+                v[h][j] += g.x, v[h][j + 1] += g.y, v[h][j + 2] += g.z, v[h][j + 3] += g.w;
+                w[h][j] += u.x, w[h][j + 1] += u.y, w[h][j + 2] += u.z, w[h][j + 3] += u.w;
             }
         }
     }
     if constexpr (MODE == GM_FORWARD) {
         with_act(a.act, [&](auto tag) {
 #pragma unroll
-            for (int j = 0; j < 16; j++) v[j] = activate<decltype(tag)::value, FAST>(v[j]) * w[j];
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int j = 0; j < 8; j++) v[h][j] = activate<decltype(tag)::value, FAST>(v[h][j]) * w[h][j];
         });
-        if (row < job.M) store16(static_cast<T *>(job.out0) + row * job.N, c, job.N, job.vec, v);
-    } else if constexpr (MODE == GM_BACKWARD) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            if (row + 8 * h >= job.M) continue;
+            T *out = static_cast<T *>(job.out0) + (row + 8 * h) * job.N + c;
+            if (job.vec && c + 8 <= job.N) {
+                store8(out, v[h]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    if (c + j < job.N) out[j] = from_f32<T>(v[h][j]);
+            }
+        }
+    } else {
+        float d[2][8];
+#pragma unroll
+        for (int h = 0; h < 2; h++) unpack(dh[h], d[h]);
         with_act(a.act, [&](auto tag) {
 #pragma unroll
-            for (int j = 0; j < 16; j++) {
-                const float2 s = activate_slope<decltype(tag)::value, FAST>(v[j]);
-                v[j] = d[j] * w[j] * s.y;
-                w[j] = d[j] * s.x;
-            }
-        });
-        if (row >= job.M) {   // (the sums below)
+            for (int h = 0; h < 2; h++)
 #pragma unroll
-            for (int j = 0; j < 16; j++) v[j] = w[j] = 0.f;
-        }
-        if (a.sums && c < a.Fp) {
-            const float sg = lane_sums(v), su = lane_sums(w);
+                for (int j = 0; j < 8; j++) {
+                    const float2 s = activate_slope<decltype(tag)::value, FAST>(v[h][j]);
+                    v[h][j] = d[h][j] * w[h][j] * s.y;
+                    w[h][j] = d[h][j] * s.x;
+                }
+        });
+        if (c >= a.Fp) return;   // (all lanes of a warp, or none: c's eights of 32 features)
+        if (a.sums) {
+            float g[8], u[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) {   // (rows past the matrix: dH is 0 there, but 0 times what they hold need not be)
+                g[j] = (row < job.M ? v[0][j] : 0.f) + (row + 8 < job.M ? v[1][j] : 0.f);
+                u[j] = (row < job.M ? w[0][j] : 0.f) + (row + 8 < job.M ? w[1][j] : 0.f);
+            }
+            const float sg = row_sums(g), su = row_sums(u);
             const int lane = threadIdx.x & 31;
-            float *at = a.sums + (row >> 5) * 2 * a.Fp + c;
-            if ((row & ~(int64_t)31) < job.M) at[lane < 16 ? lane : a.Fp + lane - 16] = lane < 16 ? sg : su;
+            // the sixteen rows' sums: feature c + lane / 4 of this lane's eight
+            const int64_t first = row - (lane >> 2);
+            if (first < job.M) {
+                float *at = a.sums + (first >> 4) * 2 * a.Fp + c + (lane >> 2);
+                at[0] = sg;
+                at[a.Fp] = su;
+            }
         }
-        if (row < job.M && c < a.Fp) {
-            uint16_t *at = a.D + row * 2 * a.Fp + c;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            if (row + 8 * h >= job.M) continue;
+            uint16_t *at = a.D + (row + 8 * h) * 2 * a.Fp + c;
             if constexpr (FAST) {
-                store16(at, 0, 16, true, v);
-                store16(at + a.Fp, 0, 16, true, w);
+                store8(at, v[h]);
+                store8(at + a.Fp, w[h]);
                 if (a.d_planes == 2) {   // what the rounding left
 #pragma unroll
-                    for (int j = 0; j < 16; j++) {
-                        v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
-                        w[j] -= __bfloat162float(__float2bfloat16_rn(w[j]));
+                    for (int j = 0; j < 8; j++) {
+                        v[h][j] -= __bfloat162float(__float2bfloat16_rn(v[h][j]));
+                        w[h][j] -= __bfloat162float(__float2bfloat16_rn(w[h][j]));
                     }
                     at += 2 * a.Fp * job.M;
-                    store16(at, 0, 16, true, v);
-                    store16(at + a.Fp, 0, 16, true, w);
+                    store8(at, v[h]);
+                    store8(at + a.Fp, w[h]);
                 }
             } else {
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    float p[3][16];
+                    float p[3][8];
 #pragma unroll
-                    for (int j = 0; j < 16; j++) {
+                    for (int j = 0; j < 8; j++) {
                         float q[3];
-                        parts_of(k ? w[j] : v[j], q);
+                        parts_of(k ? w[h][j] : v[h][j], q);
                         p[0][j] = q[0], p[1][j] = q[1], p[2][j] = q[2];
                     }
 #pragma unroll
-                    for (int i = 0; i < 3; i++) store16(at + k * a.Fp + i * 2 * a.Fp * job.M, 0, 16, true, p[i]);
+                    for (int i = 0; i < 3; i++) store8(at + k * a.Fp + i * 2 * a.Fp * job.M, p[i]);
                 }
             }
         }
-    } else {
-        if (u.part >= 0) {   // [256][2 half] of this unit
-            float *at = a.parts + ((int64_t)u.part * 256 + (row - u.m0)) * 2 * a.half + (c - u.n0);
-            store16(at, 0, 32, true, v);
-            store16(at, 16, 32, true, w);
-            return;
-        }
-        if (row >= job.M) return;
-        const bool second = row >= job.row_seam;
-        const int64_t r = second ? row - job.row_seam : row;
-        if (r >= job.out_rows) return;
-        T *out = static_cast<T *>(second ? job.out1 : job.out0) + r * job.N;
-        store16(out, c, job.N, job.vec, v);
-        store16(out, c + 16, job.N, job.vec, w);
     }
+}
+
+// Puts out 2 x 16 columns, from c on, of this thread's row of a plain product.
+template <typename T>
+__device__ __forceinline__ void put_product(const Args &a, const Job &job, const Unit &u, int64_t row, int64_t c, const float (&v)[16],
+                                            const float (&w)[16]) {
+    if (u.part >= 0) {   // [256][2 half] of this unit
+        float *at = a.parts + ((int64_t)u.part * 256 + (row - u.m0)) * 2 * a.half + (c - u.n0);
+        store16(at, 0, 32, true, v);
+        store16(at, 16, 32, true, w);
+        return;
+    }
+    if (row >= job.M) return;
+    const bool second = row >= job.row_seam;
+    const int64_t r = second ? row - job.row_seam : row;
+    if (r >= job.out_rows) return;
+    T *out = static_cast<T *>(second ? job.out1 : job.out0) + r * job.N;
+    store16(out, c, job.N, job.vec, v);
+    store16(out, c + 16, job.N, job.vec, w);
 }
 
 template <int MODE, typename T>
@@ -438,8 +493,8 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 const uint32_t to = dst + b_at + t * b_bytes;
                 if (MODE == GM_PRODUCT) {   // (b_side: every plain product's)
                     for (int j = 0; j < a.half; j += 64) ptx::tma_load_3d_pair_at(to + 128 * j, map, n + j, kb, t, bar);
-                } else {
-                    ptx::tma_load_3d_pair_at(to, map, kb, n, t, bar);
+                } else {   // (a part's rows are whole groups of 32, and the parts lie behind one another)
+                    ptx::tma_load_5d_pair_at(to, map, kb, 0, 0, 0, n / 32 + t * job.groups, bar);
                 }
             }
         }
@@ -540,71 +595,118 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
             ptx::mbar_wait_bounded(&done, 0, kDrainNs);
         }
     } else if (warp >= kEpiWarp0) {
-        constexpr int kShares = kEpiWarps / 4, kMost = 8 / kShares;   // the columns' shares; most pieces of one
+        constexpr int kShares = kEpiWarps / 4, kMost = 8 / kShares;   // warps to 32 rows; most pieces of one
         const int q = warp & 3, hc = (warp - kEpiWarp0) >> 2;          // tensor-memory lanes 32 q .., share hc
         float *bs = bias_s + (warp - kEpiWarp0) * (kMost * 32);
-        // pieces of 2 x 16 columns: G and U of the same features, or neighbours; the share's first in the accumulators
-        const int all = a.half / 16, pieces = min((all + kShares - 1) / kShares, max(0, all - hc * ((all + kShares - 1) / kShares)));
-        const int step = MODE == GM_PRODUCT ? 32 : 16, other = MODE == GM_PRODUCT ? 16 : a.half;
-        const int col0 = hc * ((all + kShares - 1) / kShares) * step;
+        // this warp's pieces: gated modes, of 16 rows x 32 features (G and U), the
+        // rows' halves of a group of features behind each other; products, of 32 rows
+        // x 32 columns
+        const int all = a.half / 16, each = (all + kShares - 1) / kShares, first = hc * each,
+                  pieces = max(0, min(each, all - first));
         ptx::pdl_wait();   // the outputs and dH may be an earlier kernel's
         int ab = 0;
         uint32_t fphase = 0;
         bool ok = true;
+        // a piece's row and feature of this thread, gated modes
+        auto row_of = [&](const Unit &u, int p) { return u.m0 + rank * 128 + 32 * q + 16 * ((first + p) & 1) + (lane >> 2); };
+        auto col_of = [&](const Unit &u, int p) { return u.n0 + 32 * ((first + p) >> 1) + 8 * (lane & 3); };
+        // waits for the next accumulator buffer; its columns of this warp's lanes
+        auto wait_acc = [&](const Unit &u) {
+            const uint64_t limit = a.wait_ns * (uint64_t)(u.i1 - u.i0 + 2);
+            ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, limit, &stop));
+            if (!ok) halt();
+            tc5::fence_after();
+            return tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16);
+        };
+        // hands the buffer back, its last columns being in registers
+        auto hand_back = [&]() {
+            tc5::fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(&acc_empty[ab], 0));
+            ab ^= 1;
+            if (ab == 0) fphase ^= 1;
+        };
+        // a piece of the accumulators at tm
+        auto load_piece = [&](uint32_t tm, int p, uint32_t (&r0)[16], uint32_t (&r1)[16]) {
+            if constexpr (MODE == GM_PRODUCT) {
+                tc5::ld16(tm + 32 * (first + p), r0);
+                tc5::ld16(tm + 32 * (first + p) + 16, r1);
+            } else {
+                const uint32_t at = tm + ((uint32_t)(16 * ((first + p) & 1)) << 16) + 32 * ((first + p) >> 1);
+                tc5::ld_16x32(at, r0);
+                tc5::ld_16x32(at + a.half, r1);
+            }
+            tc5::ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
+                asm volatile("" : "+r"(r0[j]));
+                asm volatile("" : "+r"(r1[j]));
+            }
+        };
+        auto put = [&](const Job &job, int p, const float (&x)[16], const float (&y)[16], const Eight<T> (&dh)[2]) {
+            if constexpr (MODE == GM_PRODUCT) {
+                put_product<T>(a, job, un, un.m0 + rank * 128 + 32 * q + lane, un.n0 + 32 * (first + p), x, y);
+            } else {
+                float g[2][8], u[2][8];
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++) {
+                        g[h][j] = x[4 * (j / 2) + 2 * h + (j & 1)];
+                        u[h][j] = y[4 * (j / 2) + 2 * h + (j & 1)];
+                    }
+                const float *b = bs + 32 * (((first + p) >> 1) - (first >> 1)) + 8 * (lane & 3);
+                put_gated<MODE, T>(a, job, row_of(un, p), col_of(un, p), g, u, b, b + 16 * kMost, dh);
+            }
+        };
+        // bf16: dH of the unit to come (it is read from DRAM, 3000 cycles when the
+        // loads of the operands are in its way)
+        Eight<T> ahead[F32 ? 1 : kMost][2];
+        if constexpr (MODE == GM_BACKWARD && !F32) {
+            if (v < a.units) {
+                un = unit_at<MODE>(a, v);
+#pragma unroll
+                for (int p = 0; p < kMost; p++)
+#pragma unroll
+                    for (int h = 0; h < 2; h++)
+                        if (p < pieces) fetch(a, a.job[0], row_of(un, p) + 8 * h, col_of(un, p), ahead[p][h]);
+            }
+        }
         for (; ok && v < a.units; v += pairs) {
             un = unit_at<MODE>(a, v);
             const Job &job = a.job[un.job];
-            const int64_t row = un.m0 + rank * 128 + 32 * q + lane;
             if (MODE != GM_PRODUCT && (a.bg || a.bu)) {
                 __syncwarp();   // (the last unit's biases have been read)
-                for (int j = lane; j < 16 * pieces; j += 32) {
-                    const int64_t f = un.n0 + col0 + j;
+                for (int j = lane; j < 16 * kMost; j += 32) {
+                    const int64_t f = un.n0 + 32 * (first >> 1) + j;
                     bs[j] = a.bg && f < job.N ? __ldg(a.bg + f) : 0.f;
                     bs[16 * kMost + j] = a.bu && f < job.N ? __ldg(a.bu + f) : 0.f;
                 }
                 __syncwarp();
             }
-            const T *dh = static_cast<const T *>(a.dH) + row * job.N;
-            const bool mine = MODE == GM_BACKWARD && row < job.M;
-            const uint64_t limit = a.wait_ns * (uint64_t)(un.i1 - un.i0 + 2);
-            // waits for the next accumulator buffer; its columns of this warp's lanes
-            auto wait_acc = [&]() {
-                ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, limit, &stop));
-                if (!ok) halt();
-                tc5::fence_after();
-                return tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16) + col0;
-            };
-            // hands the buffer back, its last columns being in registers
-            auto hand_back = [&]() {
-                tc5::fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive_cluster(ptx::map_to_cta(&acc_empty[ab], 0));
-                ab ^= 1;
-                if (ab == 0) fphase ^= 1;
-            };
             if constexpr (!F32) {
-                float d[16] = {};
-                if (mine && pieces > 0) load16(dh, un.n0 + col0, job.N, job.vec, d);
-                const uint32_t tm = wait_acc();
+                const uint32_t tm = wait_acc(un);
                 if (!ok) break;
                 if (pieces == 0) hand_back();
-#pragma unroll 1
-                for (int p = 0; p < pieces; p++) {
+                const Unit next = MODE == GM_BACKWARD && v + pairs < a.units ? unit_at<MODE>(a, v + pairs) : un;
+#pragma unroll
+                for (int p = 0; p < kMost; p++) {
+                    if (p >= pieces) break;
                     uint32_t r0[16], r1[16];
-                    tc5::ld16(tm + p * step, r0);
-                    tc5::ld16(tm + p * step + other, r1);
-                    if (mine && p > 0) load16(dh, un.n0 + col0 + p * step, job.N, job.vec, d);
-                    tc5::ld_wait();
+                    load_piece(tm, p, r0, r1);
                     float x[16], y[16];
 #pragma unroll
-                    for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
-                        asm volatile("" : "+r"(r0[j]));
-                        asm volatile("" : "+r"(r1[j]));
-                        x[j] = __uint_as_float(r0[j]);
-                        y[j] = __uint_as_float(r1[j]);
-                    }
+                    for (int j = 0; j < 16; j++) x[j] = __uint_as_float(r0[j]), y[j] = __uint_as_float(r1[j]);
                     if (p + 1 == pieces) hand_back();
-                    put<MODE, T>(a, job, un, row, un.n0 + col0 + p * step, x, y, bs + 16 * p, bs + 16 * kMost + 16 * p, d);
+                    Eight<T> dh[2];
+                    if constexpr (MODE == GM_BACKWARD) {   // this unit's, on its way since the last one; the next unit's
+#pragma unroll
+                        for (int h = 0; h < 2; h++) {
+                            dh[h] = ahead[p][h];
+                            fetch(a, job, row_of(next, p) + 8 * h, col_of(next, p), ahead[p][h]);
+                        }
+                    }
+                    put(job, p, x, y, dh);
                 }
             } else {
                 float g[kMost][16], w[kMost][16];   // the sums of the steps so far
@@ -613,19 +715,15 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
 #pragma unroll
                     for (int j = 0; j < 16; j++) g[p][j] = w[p][j] = 0.f;
                 for (int b = un.i0; b < un.i1; b++) {
-                    const uint32_t tm = wait_acc();
+                    const uint32_t tm = wait_acc(un);
                     if (!ok) break;
 #pragma unroll
                     for (int p = 0; p < kMost; p++) {
                         if (p >= pieces) break;
                         uint32_t r0[16], r1[16];
-                        tc5::ld16(tm + p * step, r0);
-                        tc5::ld16(tm + p * step + other, r1);
-                        tc5::ld_wait();
+                        load_piece(tm, p, r0, r1);
 #pragma unroll
-                        for (int j = 0; j < 16; j++) {   // (as above)
-                            asm volatile("" : "+r"(r0[j]));
-                            asm volatile("" : "+r"(r1[j]));
+                        for (int j = 0; j < 16; j++) {
                             g[p][j] += __uint_as_float(r0[j]);
                             w[p][j] += __uint_as_float(r1[j]);
                         }
@@ -633,13 +731,15 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                     hand_back();
                 }
                 if (!ok) break;
-                // one copy of the code for all pieces: unrolled, it came from beyond the
-                // instruction caches (37000 cycles a unit of the backward pass)
+                // one copy of the code for all pieces
 #pragma unroll 1
                 for (int p = 0; p < pieces; p++) {
-                    float d[16] = {}, x[16], y[16];
-                    const int64_t c = un.n0 + col0 + p * step;
-                    if (mine) load16(dh, c, job.N, job.vec, d);
+                    float x[16], y[16];
+                    Eight<T> dh[2];
+                    if constexpr (MODE == GM_BACKWARD) {
+#pragma unroll
+                        for (int h = 0; h < 2; h++) fetch(a, job, row_of(un, p) + 8 * h, col_of(un, p), dh[h]);
+                    }
 #pragma unroll
                     for (int j = 0; j < 16; j++) {
                         x[j] = g[0][j], y[j] = w[0][j];
@@ -647,7 +747,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                         for (int k = 1; k < kMost; k++)
                             if (p == k) x[j] = g[k][j], y[j] = w[k][j];
                     }
-                    put<MODE, T>(a, job, un, row, c, x, y, bs + 16 * p, bs + 16 * kMost + 16 * p, d);
+                    put(job, p, x, y, dh);
                 }
             }
         }
@@ -744,6 +844,23 @@ cudaError_t encode(const Planes &m, bool side, int rows, CUtensorMap *map) {
                : cudaErrorInvalidValue;
 }
 
+// The weights of a gated mode: rows in groups of 32, a group's in the order that
+// the epilogue wants (row 8 i + 2 q + e of a box: 8 q + 2 i + e of the group).
+cudaError_t encode_weights(const Planes &m, int rows, CUtensorMap *map) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t ld = (cuuint64_t)m.ld * 2;
+    const cuuint64_t dims[5] = {(cuuint64_t)m.cols, 2, 4, 4, (cuuint64_t)(m.rows / 32 * m.planes)};
+    const cuuint64_t strides[4] = {ld, 8 * ld, 2 * ld, 32 * ld};
+    const cuuint32_t box[5] = {64, 2, 4, 4, (cuuint32_t)(rows / 32)};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<uint16_t *>(m.p), dims, strides, box, estr,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
 int pairs_of_sms() {
     int dev = 0, n = 152;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
@@ -763,12 +880,17 @@ cudaError_t job_of(const GatedMma &g, const GatedShape &sh, Job &j) {
     j.out0 = MODE == GM_FORWARD ? g.H : g.out0;
     j.out1 = g.out1;
     j.row_seam = g.row_seam, j.out_rows = g.out_rows;
-    // 32-byte stores: base addresses and rows of 32-byte multiples
-    j.vec = g.N * (int64_t)sizeof(T) % 32 == 0 &&
-            (reinterpret_cast<uintptr_t>(j.out0) | reinterpret_cast<uintptr_t>(j.out1) | reinterpret_cast<uintptr_t>(g.dH)) % 32 == 0;
+    // wide loads and stores: base addresses and rows of 32-byte multiples (16 do for eight bf16)
+    constexpr unsigned wide = MODE != GM_PRODUCT && sizeof(T) == 2 ? 16 : 32;
+    j.vec = g.N * sizeof(T) % wide == 0 &&
+            (reinterpret_cast<uintptr_t>(j.out0) | reinterpret_cast<uintptr_t>(j.out1) | reinterpret_cast<uintptr_t>(g.dH)) % wide == 0;
     cudaError_t e = encode(g.a, g.a_side, 128, &j.a);
-    if (e == cudaSuccess) e = encode(g.b0, MODE == GM_PRODUCT, sh.half, &j.b0);
-    if (e == cudaSuccess) e = encode(g.b1.p ? g.b1 : g.b0, MODE == GM_PRODUCT, sh.half, &j.b1);
+    j.groups = (int)(g.b0.rows / 32);
+    for (int i = 0; i < 2 && e == cudaSuccess; i++) {
+        const Planes &b = i && g.b1.p ? g.b1 : g.b0;
+        CUtensorMap *map = i ? &j.b1 : &j.b0;
+        e = MODE == GM_PRODUCT ? encode(b, true, 64, map) : encode_weights(b, sh.half, map);
+    }
     return e;
 }
 

@@ -12,7 +12,7 @@ namespace bsr {
 
 enum GatedMode : int {
     GM_FORWARD = 0,    // H = act(G) * U
-    GM_BACKWARD = 1,   // dG, dU (and sums of them over 32 tokens) from G, U and dH
+    GM_BACKWARD = 1,   // dG, dU (and sums of them over 16 tokens) from G, U and dH
     GM_PRODUCT = 2,    // a plain product: dX; dWg and dWu
 };
 
@@ -27,7 +27,7 @@ struct Planes {
 struct GatedMma {
     int mode;
     bsr_dtype_t dt;           // of the outputs and dH
-    Planes a, b0, b1;
+    Planes a, b0, b1;         // gated modes: Wg and Wu in b0 and b1, of whole groups of 32 rows (zeros past N)
     // GM_PRODUCT: B is stored [K, N], N contiguous; with a_side A is stored [K, M], M contiguous. Else [M, K], [N, K].
     bool a_side;
     int64_t M, N, K;          // sizes of the product; gated modes: M tokens, N features
@@ -40,7 +40,7 @@ struct GatedMma {
     int d_planes;
     uint16_t *D;              // d_planes of [M, 2 Fp]: dG, then dU from column Fp on
     int64_t Fp;
-    float *sums;              // [ceil(M / 32), 2 Fp], or NULL
+    float *sums;              // of 16 rows of dG and dU each, [ceil(M / 16), 2 Fp], or NULL
     // GM_PRODUCT: rows below row_seam go to out0, those from it on to out1, `out_rows` in each
     void *out0, *out1;
     int64_t row_seam, out_rows;

@@ -148,6 +148,13 @@ __device__ __forceinline__ void store_cluster(uint32_t addr, uint32_t v) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
+// The same with a release at the scope of the CTA: for a thread that only hands
+// back what it has read (tensor memory, ordered by tcgen05.fence), and whose
+// stores to global memory the other CTA does not read. The release at cluster
+// scope waits until they are done, 1700 cycles behind an epilogue's.
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t addr) {
+    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
 // mbar_arrive_expect_tx and tma_load_2d by shared-memory address.
 __device__ __forceinline__ void mbar_arrive_expect_tx_at(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -175,6 +182,15 @@ __device__ __forceinline__ void tma_load_3d_pair_at(uint32_t dst, const CUtensor
         "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], "
         "[%5];" ::"r"(dst),
         "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+// The same of a 5-D tensor.
+__device__ __forceinline__ void tma_load_5d_pair_at(uint32_t dst, const CUtensorMap *map, int32_t x0, int32_t x1, int32_t x2,
+                                                   int32_t x3, int32_t x4, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, "
+        "%5, %6}], [%7];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x0), "r"(x1), "r"(x2), "r"(x3), "r"(x4), "r"(bar)
         : "memory");
 }
 // 32 bytes to global memory by one thread (32-byte aligned).
