@@ -1,15 +1,67 @@
-// Activations of the gated feed-forward block and their derivatives, in fp32.
+// Activations of the gated feed-forward block and their derivatives, in fp32, two
+// values at a time: packed multiplies and adds take one instruction for both.
 #pragma once
+
+#include <cstdint>
 
 #include "bsr.h"
 
 namespace bsr {
 
+struct F2 {
+    unsigned long long v;
+};
+__device__ __forceinline__ F2 pack2(float a, float b) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack2(F2 x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 all2(float a) { return pack2(a, a); }
+template <typename F>
+__device__ __forceinline__ F2 each2(F2 x, F f) {
+    const float2 u = unpack2(x);
+    return pack2(f(u.x), f(u.y));
+}
+
 // 1 / (1 + e^-x); FAST: the hardware's exponential, whose relative error of about
 // 2^-21 is lost in a result rounded to bf16.
 template <bool FAST>
-__device__ __forceinline__ float logistic(float x) {
-    return __fdividef(1.f, 1.f + (FAST ? __expf(-x) : expf(-x)));
+__device__ __forceinline__ F2 logistic(F2 x) {
+    F2 e;
+    if constexpr (FAST) {
+        e = each2(mul2(x, all2(-1.4426950408889634f)), [](float t) {
+            float r;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+            return r;
+        });
+    } else {
+        e = each2(x, [](float t) { return expf(-t); });
+    }
+    return each2(add2(e, all2(1.f)), [](float t) {
+        float r;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+        return r;
+    });
 }
 
 constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)
@@ -17,38 +69,51 @@ constexpr float kGeluB = 0.044715f;
 
 // Phi(g), the normal distribution
 template <bool FAST>
-__device__ __forceinline__ float normal_cdf(float g) {
-    return FAST ? fmaf(0.5f, erff(0.70710678f * g), 0.5f) : normcdff(g);
+__device__ __forceinline__ F2 normal_cdf(F2 g) {
+    return each2(g, [](float t) { return FAST ? fmaf(0.5f, erff(0.70710678f * t), 0.5f) : normcdff(t); });
 }
 // the tanh form of GELU is g / (1 + e^-2u), which is the same; 2u
-__device__ __forceinline__ float gelu_2u(float g) { return 2.f * kGeluA * g * fmaf(kGeluB * g, g, 1.f); }
+__device__ __forceinline__ F2 gelu_2u(F2 g) {
+    return mul2(mul2(all2(2.f * kGeluA), g), fma2(mul2(all2(kGeluB), g), g, all2(1.f)));
+}
+__device__ __forceinline__ F2 relu(F2 g) {
+    return each2(g, [](float t) { return t > 0.f ? t : (t != t ? t : 0.f); });
+}
 
 template <int ACT, bool FAST>
-__device__ __forceinline__ float activate(float g) {
-    if constexpr (ACT == BSR_ACT_SILU) return g * logistic<FAST>(g);
-    else if constexpr (ACT == BSR_ACT_GELU) return g * normal_cdf<FAST>(g);
-    else if constexpr (ACT == BSR_ACT_GELU_TANH) return g * logistic<FAST>(gelu_2u(g));
-    else if constexpr (ACT == BSR_ACT_RELU) return g > 0.f ? g : (g != g ? g : 0.f);
+__device__ __forceinline__ F2 activate(F2 g) {
+    if constexpr (ACT == BSR_ACT_SILU) return mul2(g, logistic<FAST>(g));
+    else if constexpr (ACT == BSR_ACT_GELU) return mul2(g, normal_cdf<FAST>(g));
+    else if constexpr (ACT == BSR_ACT_GELU_TANH) return mul2(g, logistic<FAST>(gelu_2u(g)));
+    else if constexpr (ACT == BSR_ACT_RELU) return relu(g);
     else return logistic<FAST>(g);
 }
 
-// act(g) and act'(g).
+// act(g), and act'(g) in `slope`.
 template <int ACT, bool FAST>
-__device__ __forceinline__ float2 activate_slope(float g) {
+__device__ __forceinline__ F2 activate_slope(F2 g, F2 &slope) {
+    const F2 one = all2(1.f), minus = all2(-1.f);
     if constexpr (ACT == BSR_ACT_SILU) {
-        const float p = logistic<FAST>(g);
-        return make_float2(g * p, p * fmaf(g, 1.f - p, 1.f));
+        const F2 p = logistic<FAST>(g);
+        slope = mul2(p, fma2(g, fma2(p, minus, one), one));
+        return mul2(g, p);
     } else if constexpr (ACT == BSR_ACT_GELU) {
-        const float p = normal_cdf<FAST>(g), density = 0.3989422804f * (FAST ? __expf(-0.5f * g * g) : expf(-0.5f * g * g));
-        return make_float2(g * p, fmaf(g, density, p));
+        const F2 p = normal_cdf<FAST>(g);
+        const F2 density = each2(mul2(mul2(all2(-0.5f), g), g), [](float t) { return 0.3989422804f * (FAST ? __expf(t) : expf(t)); });
+        slope = fma2(g, density, p);
+        return mul2(g, p);
     } else if constexpr (ACT == BSR_ACT_GELU_TANH) {
-        const float p = logistic<FAST>(gelu_2u(g));
-        return make_float2(g * p, fmaf(g * p * (1.f - p), 2.f * kGeluA * fmaf(3.f * kGeluB * g, g, 1.f), p));
+        const F2 p = logistic<FAST>(gelu_2u(g)), a = mul2(g, p);
+        const F2 rise = mul2(all2(2.f * kGeluA), fma2(mul2(all2(3.f * kGeluB), g), g, one));
+        slope = fma2(mul2(a, fma2(p, minus, one)), rise, p);
+        return a;
     } else if constexpr (ACT == BSR_ACT_RELU) {
-        return make_float2(g > 0.f ? g : (g != g ? g : 0.f), g > 0.f ? 1.f : (g != g ? g : 0.f));
+        slope = each2(g, [](float t) { return t > 0.f ? 1.f : (t != t ? t : 0.f); });
+        return relu(g);
     } else {
-        const float p = logistic<FAST>(g);
-        return make_float2(p, p * (1.f - p));
+        const F2 p = logistic<FAST>(g);
+        slope = mul2(p, fma2(p, minus, one));
+        return p;
     }
 }
 

@@ -86,22 +86,23 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
 }
 
 // dbg and dbu: the sums of the 2 Fp columns of `sums` [n, 2 Fp], 32 columns a
-// CTA: 32 x 8 threads, each every eighth row, then the eight.
-__global__ void __launch_bounds__(256) k_bias_sums(const float *sums, int64_t n, int64_t F, int64_t Fp, float *dbg, float *dbu) {
-    __shared__ float part[8][33];
+// CTA: 32 x 32 threads, each every 32nd row, then the 32.
+__global__ void __launch_bounds__(1024) k_bias_sums(const float *sums, int64_t n, int64_t F, int64_t Fp, float *dbg, float *dbu) {
+    __shared__ float part[32][33];
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
     float s = 0.f;
-    for (int64_t k = threadIdx.y; k < n; k += 8) s += sums[k * 2 * Fp + c];
+#pragma unroll 8
+    for (int64_t k = threadIdx.y; k < n; k += 32) s += sums[k * 2 * Fp + c];
     part[threadIdx.y][threadIdx.x] = s;
     __syncthreads();
-    if (threadIdx.y) return;
-    s = 0.f;
-    for (int k = 0; k < 8; k++) s += part[k][threadIdx.x];
-    float *out = c < Fp ? dbg : dbu;
-    const int64_t f = c < Fp ? c : c - Fp;
-    if (out && f < F) out[f] = s;
+    s = part[threadIdx.x][threadIdx.y];   // column threadIdx.y, a row a lane
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.y, f = col < Fp ? col : col - Fp;
+    float *out = col < Fp ? dbg : dbu;
+    if (threadIdx.x == 0 && out && f < F) out[f] = s;
 }
 
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -110,7 +111,6 @@ int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
     int parts, d_parts;   // bf16 matrices to an operand, and to dG and dU
     bool lay_out;
-    int first;            // where dX stands in `grads`
     int64_t Kp, Fp, Fr;   // padded sizes; the weights' rows
     int64_t x_at, wg_at, wu_at, d_at, sums_at, parts_at, bytes;
     GatedMma main, grads[2];   // dX; dWg and dWu
@@ -148,7 +148,7 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     p.main_plan = plan_gated_mma(&m, 1);
     if (!backward) return p;
     p.d_at = take(p.d_parts * N * 2 * p.Fp * 2);
-    p.sums_at = take((N + 15) / 16 * 2 * p.Fp * 4);
+    p.sums_at = take((N + 31) / 32 * 2 * 2 * p.Fp * 4);
     GatedMma &x = p.grads[0], &w = p.grads[1];
     x.mode = w.mode = GM_PRODUCT;
     x.a.planes = w.a.planes = m.d_planes = p.d_parts;
@@ -158,12 +158,9 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     w.M = 2 * p.Fp, w.N = K, w.K = N;
     w.a_side = true;
     w.row_seam = p.Fp, w.out_rows = F;
-    // the one with the longer sums first: the tiles of the last round are split
-    p.first = x.K >= w.K ? 0 : 1;
-    if (p.first) std::swap(x, w);
     p.parts_at = p.bytes;
     if (dx || dw) {
-        p.grads_plan = plan_gated_mma(dx && dw ? p.grads : &p.grads[(dx ? 0 : 1) ^ p.first], dx + dw);
+        p.grads_plan = plan_gated_mma(dx ? &x : &w, dx + dw);
         take(p.grads_plan.part_bytes);
     }
     return p;
@@ -220,7 +217,7 @@ cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
     Planes m[3];
     cudaError_t e = operands(c, p, m, s);
     if (e != cudaSuccess) return e;
-    GatedMma &g = p.main, &x = p.grads[p.first], &w = p.grads[1 - p.first];
+    GatedMma &g = p.main, &x = p.grads[0], &w = p.grads[1];
     g.dt = x.dt = w.dt = c.dt;
     g.a = m[0], g.b0 = m[1], g.b1 = m[2];
     g.bg = c.bg, g.bu = c.bu;
@@ -235,9 +232,10 @@ cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
     w.b0 = m[0];
     w.out0 = c.dWg, w.out1 = c.dWu;
     p.grads_plan.parts = reinterpret_cast<float *>(ws + p.parts_at);
-    if (e == cudaSuccess && (dx || dw)) e = launch_gated_mma(dx && dw ? p.grads : dx ? &x : &w, p.grads_plan, s);
+    if (e == cudaSuccess && (dx || dw)) e = launch_gated_mma(dx ? &x : &w, p.grads_plan, s);
     if (e == cudaSuccess && g.sums)
-        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 8), 0, s, (const float *)g.sums, (c.N + 15) / 16, c.F,
+        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 32), 0, s, (const float *)g.sums,
+                          (c.N + 31) / 32 * (32 / sum_rows(p.main_plan, c.dt)), c.F,
                           p.Fp, c.dbg, c.dbu);
     return e;
 }

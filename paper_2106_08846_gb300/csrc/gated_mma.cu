@@ -85,6 +85,9 @@ struct Job {
     CUtensorMap a, b0, b1;
     int64_t M, N;             // rows; columns (gated modes: features)
     unsigned tiles_n;         // tiles along N
+    unsigned whole;           // tiles that are one unit (the first ones)
+    unsigned split_units;     // units of the others
+    int splits;               // of each of them
     int steps, seam;          // steps of a tile; the step from which b1 is read
     uint32_t idesc;
     int a_side;
@@ -96,9 +99,7 @@ struct Job {
 
 struct Args {
     Job job[2];
-    unsigned second;          // the second job's first tile
-    unsigned whole, units;    // units that are whole tiles (they come first)
-    int splits;               // units of every other tile
+    unsigned units;           // the jobs' whole tiles, then their split ones
     int half, ns;
     uint32_t stage_bytes;
     int a_tiles, b_tiles;     // in a stage
@@ -125,26 +126,39 @@ template <int MODE>
 __device__ __forceinline__ Unit unit_at(const Args &a, unsigned v) {
     Unit u;
     u.part = -1;
-    unsigned k = 0;
-    if (MODE == GM_PRODUCT && v >= a.whole) {
-        u.part = (int)(v - a.whole);
-        const unsigned tile = (unsigned)u.part / (unsigned)a.splits;
-        k = (unsigned)u.part - tile * (unsigned)a.splits;
-        v = a.whole + tile;
+    u.job = 0;
+    unsigned tile = v;
+    if (MODE == GM_PRODUCT) {
+        const unsigned w0 = a.job[0].whole, wholes = w0 + a.job[1].whole;
+        if (v < wholes) {
+            u.job = v >= w0;
+            if (u.job) tile -= w0;
+        } else {
+            u.part = (int)(v - wholes);
+            u.job = (unsigned)u.part >= a.job[0].split_units;
+            tile = (unsigned)u.part - (u.job ? a.job[0].split_units : 0);
+        }
     }
-    u.job = MODE == GM_PRODUCT && v >= a.second;
-    if (u.job) v -= a.second;
     const Job &j = a.job[u.job];
     u.i0 = 0;
     u.i1 = j.steps;
     if (MODE == GM_PRODUCT && u.part >= 0) {
-        u.i0 = (int)((int64_t)j.steps * k / a.splits);
-        u.i1 = (int)((int64_t)j.steps * (k + 1) / a.splits);
+        const unsigned s = (unsigned)j.splits, k = tile % s;
+        tile = j.whole + tile / s;
+        u.i0 = (int)((int64_t)j.steps * k / s);
+        u.i1 = (int)((int64_t)j.steps * (k + 1) / s);
     }
-    const unsigned tm = v / j.tiles_n, tn = v - tm * j.tiles_n;
+    const unsigned tm = tile / j.tiles_n, tn = tile - tm * j.tiles_n;
     u.m0 = (int64_t)tm * 256;
     u.n0 = (int64_t)tn * (MODE == GM_PRODUCT ? 2 * a.half : a.half);
     return u;
+}
+
+// The unit of a pair in a round of them: every second round is taken backwards,
+// so that who has a long unit in one has a short one in the next (the units come
+// longest first).
+__device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsigned pairs) {
+    return round * pairs + (round & 1 ? pairs - 1 - pair : pair);
 }
 
 // The products of a step, the smallest first: parts of A and B. fp32: (2,0) (1,1)
@@ -197,25 +211,26 @@ template <typename T>
 struct Eight {
     uint32_t w[2 * sizeof(T)];
 };
-__device__ __forceinline__ void unpack(const Eight<uint16_t> &r, float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 4; j++) {
-        v[2 * j] = __uint_as_float(r.w[j] << 16);
-        v[2 * j + 1] = __uint_as_float(r.w[j] & 0xffff0000u);
-    }
+__device__ __forceinline__ F2 two_of(const Eight<uint16_t> &r, int j) {
+    return pack2(__uint_as_float(r.w[j] << 16), __uint_as_float(r.w[j] & 0xffff0000u));
 }
-__device__ __forceinline__ void unpack(const Eight<float> &r, float (&v)[8]) {
-#pragma unroll
-    for (int j = 0; j < 8; j++) v[j] = __uint_as_float(r.w[j]);
+__device__ __forceinline__ F2 two_of(const Eight<float> &r, int j) {
+    return pack2(__uint_as_float(r.w[2 * j]), __uint_as_float(r.w[2 * j + 1]));
 }
-__device__ __forceinline__ void store8(uint16_t *p, const float (&v)[8]) {   // (16-byte aligned)
-    *reinterpret_cast<uint4 *>(p) =
-        make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+__device__ __forceinline__ uint32_t pack_bf16(F2 x) {
+    const float2 u = unpack2(x);
+    return pack_bf16(u.x, u.y);
 }
-__device__ __forceinline__ void store8(float *p, const float (&v)[8]) {   // (32-byte aligned)
+__device__ __forceinline__ void store8(uint16_t *p, const F2 (&v)[4]) {   // (16-byte aligned)
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0]), pack_bf16(v[1]), pack_bf16(v[2]), pack_bf16(v[3]));
+}
+__device__ __forceinline__ void store8(float *p, const F2 (&v)[4]) {   // (32-byte aligned)
     uint32_t r[8];
 #pragma unroll
-    for (int j = 0; j < 8; j++) r[j] = __float_as_uint(v[j]);
+    for (int j = 0; j < 4; j++) {
+        const float2 u = unpack2(v[j]);
+        r[2 * j] = __float_as_uint(u.x), r[2 * j + 1] = __float_as_uint(u.y);
+    }
     ptx::st_global_32(p, r);
 }
 
@@ -244,11 +259,16 @@ __device__ __forceinline__ void fetch(const Args &a, const Job &job, int64_t row
     }
 }
 
-// Sums of eight values over the lanes with the same lane % 4: lane l gets that of
-// value l / 4.
-__device__ __forceinline__ float row_sums(const float (&v)[8]) {
+// Sums of eight values, in pairs, over the lanes with the same lane % 4: lane l
+// gets that of value l / 4.
+__device__ __forceinline__ float row_sums(const F2 (&p)[4]) {
     const int lane = threadIdx.x & 31;
-    float b[4], c[2];
+    float v[8], b[4], c[2];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const float2 u = unpack2(p[j]);
+        v[2 * j] = u.x, v[2 * j + 1] = u.y;
+    }
 #pragma unroll
     for (int j = 0; j < 4; j++) {   // lanes with bit 4 keep the upper four
         const float mine = lane & 16 ? v[j + 4] : v[j], other = lane & 16 ? v[j] : v[j + 4];
@@ -274,20 +294,22 @@ __device__ __forceinline__ void parts_of(float x, float (&p)[3]) {
     p[2] = r - p[1];
 }
 
-// Puts out G and U (v and w: eight features from c on of rows `row` and row + 8)
-// of a gated mode: H, or dG and dU.
+// Puts out G and U (v and w: eight features from c on, in pairs, of rows `row` and
+// row + 8) of a gated mode: H, or dG and dU, whose sums over the rows are added to
+// sg and su.
 template <int MODE, typename T>
-__device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t row, int64_t c, float (&v)[2][8], float (&w)[2][8],
-                                          const float *bias_g, const float *bias_u, const Eight<T> (&dh)[2]) {
+__device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t row, int64_t c, F2 (&v)[2][4], F2 (&w)[2][4],
+                                          const float *bias_g, const float *bias_u, const Eight<T> (&dh)[2], F2 (&sg)[4],
+                                          F2 (&su)[4]) {
     constexpr bool FAST = sizeof(T) == 2;
     if (a.bg || a.bu) {
 #pragma unroll
-        for (int j = 0; j < 8; j += 4) {
-            const float4 g = *reinterpret_cast<const float4 *>(bias_g + j), u = *reinterpret_cast<const float4 *>(bias_u + j);
+        for (int j = 0; j < 4; j += 2) {
+            const float4 g = *reinterpret_cast<const float4 *>(bias_g + 2 * j), u = *reinterpret_cast<const float4 *>(bias_u + 2 * j);
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                v[h][j] += g.x, v[h][j + 1] += g.y, v[h][j + 2] += g.z, v[h][j + 3] += g.w;
-                w[h][j] += u.x, w[h][j + 1] += u.y, w[h][j + 2] += u.z, w[h][j + 3] += u.w;
+                v[h][j] = add2(v[h][j], pack2(g.x, g.y)), v[h][j + 1] = add2(v[h][j + 1], pack2(g.z, g.w));
+                w[h][j] = add2(w[h][j], pack2(u.x, u.y)), w[h][j + 1] = add2(w[h][j + 1], pack2(u.z, u.w));
             }
         }
     }
@@ -296,7 +318,7 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int j = 0; j < 8; j++) v[h][j] = activate<decltype(tag)::value, FAST>(v[h][j]) * w[h][j];
+                for (int j = 0; j < 4; j++) v[h][j] = mul2(activate<decltype(tag)::value, FAST>(v[h][j]), w[h][j]);
         });
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -306,42 +328,36 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
                 store8(out, v[h]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; j++)
-                    if (c + j < job.N) out[j] = from_f32<T>(v[h][j]);
+                for (int j = 0; j < 4; j++) {
+                    const float2 x = unpack2(v[h][j]);
+                    if (c + 2 * j < job.N) out[2 * j] = from_f32<T>(x.x);
+                    if (c + 2 * j + 1 < job.N) out[2 * j + 1] = from_f32<T>(x.y);
+                }
             }
         }
     } else {
-        float d[2][8];
-#pragma unroll
-        for (int h = 0; h < 2; h++) unpack(dh[h], d[h]);
         with_act(a.act, [&](auto tag) {
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
-                for (int j = 0; j < 8; j++) {
-                    const float2 s = activate_slope<decltype(tag)::value, FAST>(v[h][j]);
-                    v[h][j] = d[h][j] * w[h][j] * s.y;
-                    w[h][j] = d[h][j] * s.x;
+                for (int j = 0; j < 4; j++) {
+                    const F2 d = two_of(dh[h], j);
+                    F2 slope;
+                    const F2 act = activate_slope<decltype(tag)::value, FAST>(v[h][j], slope);
+                    v[h][j] = mul2(mul2(d, w[h][j]), slope);
+                    w[h][j] = mul2(d, act);
                 }
         });
-        if (c >= a.Fp) return;   // (all lanes of a warp, or none: c's eights of 32 features)
-        if (a.sums) {
-            float g[8], u[8];
+        // (rows past the matrix: dH is 0 there, and so is X, so G and U are finite
+        // unless the feature's weights or biases are not)
 #pragma unroll
-            for (int j = 0; j < 8; j++) {   // (rows past the matrix: dH is 0 there, but 0 times what they hold need not be)
-                g[j] = (row < job.M ? v[0][j] : 0.f) + (row + 8 < job.M ? v[1][j] : 0.f);
-                u[j] = (row < job.M ? w[0][j] : 0.f) + (row + 8 < job.M ? w[1][j] : 0.f);
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                sg[j] = add2(sg[j], v[h][j]);
+                su[j] = add2(su[j], w[h][j]);
             }
-            const float sg = row_sums(g), su = row_sums(u);
-            const int lane = threadIdx.x & 31;
-            // the sixteen rows' sums: feature c + lane / 4 of this lane's eight
-            const int64_t first = row - (lane >> 2);
-            if (first < job.M) {
-                float *at = a.sums + (first >> 4) * 2 * a.Fp + c + (lane >> 2);
-                at[0] = sg;
-                at[a.Fp] = su;
-            }
-        }
+        if (c >= a.Fp) return;
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             if (row + 8 * h >= job.M) continue;
@@ -350,11 +366,9 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
                 store8(at, v[h]);
                 store8(at + a.Fp, w[h]);
                 if (a.d_planes == 2) {   // what the rounding left
+                    auto rest = [](float x) { return x - __bfloat162float(__float2bfloat16_rn(x)); };
 #pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        v[h][j] -= __bfloat162float(__float2bfloat16_rn(v[h][j]));
-                        w[h][j] -= __bfloat162float(__float2bfloat16_rn(w[h][j]));
-                    }
+                    for (int j = 0; j < 4; j++) v[h][j] = each2(v[h][j], rest), w[h][j] = each2(w[h][j], rest);
                     at += 2 * a.Fp * job.M;
                     store8(at, v[h]);
                     store8(at + a.Fp, w[h]);
@@ -362,15 +376,19 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
             } else {
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    float p[3][8];
+                    uint32_t p[3][4];
 #pragma unroll
-                    for (int j = 0; j < 8; j++) {
-                        float q[3];
-                        parts_of(k ? w[h][j] : v[h][j], q);
-                        p[0][j] = q[0], p[1][j] = q[1], p[2][j] = q[2];
+                    for (int j = 0; j < 4; j++) {
+                        const float2 x = unpack2(k ? w[h][j] : v[h][j]);
+                        float lo[3], hi[3];
+                        parts_of(x.x, lo);
+                        parts_of(x.y, hi);
+#pragma unroll
+                        for (int i = 0; i < 3; i++) p[i][j] = pack_bf16(lo[i], hi[i]);
                     }
 #pragma unroll
-                    for (int i = 0; i < 3; i++) store8(at + k * a.Fp + i * 2 * a.Fp * job.M, p[i]);
+                    for (int i = 0; i < 3; i++)
+                        *reinterpret_cast<uint4 *>(at + k * a.Fp + i * 2 * a.Fp * job.M) = make_uint4(p[i][0], p[i][1], p[i][2], p[i][3]);
                 }
             }
         }
@@ -451,7 +469,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
     // g - np - ns, tells it so if np <= ns.
     const int prod = warp < kMmaWarp ? warp : kMmaWarp, np = min(kProducers, ns);
     const bool producer = warp < kEpiWarp0 && warp != kMmaWarp && prod < np;
-    unsigned v = pair;
+    unsigned round = 0, v = pair;
     Unit un = {};
     int i = 0, s = prod % ns, issued = 0;
     uint32_t phase = 1 ^ ((prod / ns) & 1);   // the parity of `empty` that a first use of a stage passes at once
@@ -462,7 +480,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
     auto seek = [&]() {
         while (i >= un.i1) {
             const int over = i - un.i1;
-            v += pairs;
+            v = unit_in(++round, pair, pairs);
             if (v >= a.units) return false;
             un = unit_at<MODE>(a, v);
             i = un.i0 + over;
@@ -535,7 +553,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
             bool ok = true;
             s = 0;
             ptx::pdl_wait();   // the waits below are bounded from here on
-            for (; ok && v < a.units; v += pairs) {
+            for (; ok && v < a.units; v = unit_in(++round, pair, pairs)) {
                 un = unit_at<MODE>(a, v);
                 const Job &job = a.job[un.job];
                 const bool a_side = MODE == GM_PRODUCT && job.a_side, b_side = MODE == GM_PRODUCT;
@@ -603,6 +621,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
         // x 32 columns
         const int all = a.half / 16, each = (all + kShares - 1) / kShares, first = hc * each,
                   pieces = max(0, min(each, all - first));
+        const bool both = each > 1;   // a warp has both halves of its groups
         ptx::pdl_wait();   // the outputs and dH may be an earlier kernel's
         int ab = 0;
         uint32_t fphase = 0;
@@ -643,20 +662,37 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 asm volatile("" : "+r"(r1[j]));
             }
         };
+        // sums of dG and dU over the rows of the pieces of one group of features
+        F2 sg[4], su[4];
         auto put = [&](const Job &job, int p, const float (&x)[16], const float (&y)[16], const Eight<T> (&dh)[2]) {
             if constexpr (MODE == GM_PRODUCT) {
                 put_product<T>(a, job, un, un.m0 + rank * 128 + 32 * q + lane, un.n0 + 32 * (first + p), x, y);
             } else {
-                float g[2][8], u[2][8];
+                F2 g[2][4], u[2][4];
 #pragma unroll
-                for (int j = 0; j < 8; j++)
+                for (int j = 0; j < 4; j++)
 #pragma unroll
                     for (int h = 0; h < 2; h++) {
-                        g[h][j] = x[4 * (j / 2) + 2 * h + (j & 1)];
-                        u[h][j] = y[4 * (j / 2) + 2 * h + (j & 1)];
+                        g[h][j] = pack2(x[4 * j + 2 * h], x[4 * j + 2 * h + 1]);
+                        u[h][j] = pack2(y[4 * j + 2 * h], y[4 * j + 2 * h + 1]);
                     }
+                const int64_t row = row_of(un, p), c = col_of(un, p);
                 const float *b = bs + 32 * (((first + p) >> 1) - (first >> 1)) + 8 * (lane & 3);
-                put_gated<MODE, T>(a, job, row_of(un, p), col_of(un, p), g, u, b, b + 16 * kMost, dh);
+                if (MODE == GM_BACKWARD && (!both || !(p & 1))) {
+#pragma unroll
+                    for (int j = 0; j < 4; j++) sg[j] = su[j] = all2(0.f);
+                }
+                put_gated<MODE, T>(a, job, row, c, g, u, b, b + 16 * kMost, dh, sg, su);
+                // the rows' sums: feature c + lane / 4 of this lane's eight
+                if (MODE == GM_BACKWARD && a.sums && (!both || (p & 1)) && c < a.Fp) {
+                    const float g1 = row_sums(sg), u1 = row_sums(su);
+                    const int64_t block = (un.m0 + rank * 128 + 32 * q) / 32;
+                    if (32 * block < job.M) {
+                        float *at = a.sums + ((both ? block : 2 * block + ((first + p) & 1)) * 2 * a.Fp) + c + (lane >> 2);
+                        at[0] = g1;
+                        at[a.Fp] = u1;
+                    }
+                }
             }
         };
         // bf16: dH of the unit to come (it is read from DRAM, 3000 cycles when the
@@ -672,7 +708,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                         if (p < pieces) fetch(a, a.job[0], row_of(un, p) + 8 * h, col_of(un, p), ahead[p][h]);
             }
         }
-        for (; ok && v < a.units; v += pairs) {
+        for (; ok && v < a.units; v = unit_in(++round, pair, pairs)) {
             un = unit_at<MODE>(a, v);
             const Job &job = a.job[un.job];
             if (MODE != GM_PRODUCT && (a.bg || a.bu)) {
@@ -688,7 +724,8 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 const uint32_t tm = wait_acc(un);
                 if (!ok) break;
                 if (pieces == 0) hand_back();
-                const Unit next = MODE == GM_BACKWARD && v + pairs < a.units ? unit_at<MODE>(a, v + pairs) : un;
+                const unsigned vn = unit_in(round + 1, pair, pairs);
+                const Unit next = MODE == GM_BACKWARD && vn < a.units ? unit_at<MODE>(a, vn) : un;
 #pragma unroll
                 for (int p = 0; p < kMost; p++) {
                     if (p >= pieces) break;
@@ -710,6 +747,13 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 }
             } else {
                 float g[kMost][16], w[kMost][16];   // the sums of the steps so far
+                if constexpr (MODE == GM_BACKWARD) {   // dH comes from DRAM: into L2 meanwhile
+                    for (int p = 0; p < pieces; p++)
+                        for (int h = 0; h < 2; h++) {
+                            const int64_t row = row_of(un, p) + 8 * h, c = col_of(un, p);
+                            if (row < job.M && c < job.N) ptx::prefetch_l2(static_cast<const T *>(a.dH) + row * job.N + c);
+                        }
+                }
 #pragma unroll
                 for (int p = 0; p < kMost; p++)
 #pragma unroll
@@ -731,23 +775,20 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                     hand_back();
                 }
                 if (!ok) break;
-                // one copy of the code for all pieces
+                // one copy of the code for all pieces (unrolled, it came from beyond the
+                // instruction caches), the sums handed on from piece to piece
 #pragma unroll 1
                 for (int p = 0; p < pieces; p++) {
-                    float x[16], y[16];
                     Eight<T> dh[2];
                     if constexpr (MODE == GM_BACKWARD) {
 #pragma unroll
                         for (int h = 0; h < 2; h++) fetch(a, job, row_of(un, p) + 8 * h, col_of(un, p), dh[h]);
                     }
+                    put(job, p, g[0], w[0], dh);
 #pragma unroll
-                    for (int j = 0; j < 16; j++) {
-                        x[j] = g[0][j], y[j] = w[0][j];
+                    for (int k = 0; k + 1 < kMost; k++)
 #pragma unroll
-                        for (int k = 1; k < kMost; k++)
-                            if (p == k) x[j] = g[k][j], y[j] = w[k][j];
-                    }
-                    put(job, p, x, y, dh);
+                        for (int j = 0; j < 16; j++) g[k][j] = g[k + 1][j], w[k][j] = w[k + 1][j];
                 }
             }
         }
@@ -801,14 +842,17 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
 }
 
 // The split tiles: the sum of a tile's parts, in their order, four columns a
-// thread; blockIdx.y is the tile after the whole ones.
+// thread; a tile to a blockIdx.y.
 template <typename T>
 __global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args a) {
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
     const int fours = a.half / 2, width = 2 * a.half;
-    for (unsigned tile = blockIdx.y; tile < (a.units - a.whole) / (unsigned)a.splits; tile += gridDim.y) {
-        const Unit un = unit_at<GM_PRODUCT>(a, a.whole + tile * (unsigned)a.splits);
+    const Job &j0 = a.job[0], &j1 = a.job[1];
+    const unsigned n0 = j0.split_units / (unsigned)j0.splits, n1 = j1.split_units / (unsigned)j1.splits;
+    for (unsigned tile = blockIdx.y; tile < n0 + n1; tile += gridDim.y) {
+        const unsigned part = tile < n0 ? tile * (unsigned)j0.splits : j0.split_units + (tile - n0) * (unsigned)j1.splits;
+        const Unit un = unit_at<GM_PRODUCT>(a, j0.whole + j1.whole + part);
         const Job &job = a.job[un.job];
         const int e = blockIdx.x * 256 + threadIdx.x, r = e / fours, x = (e - r * fours) * 4;
         const int64_t row = un.m0 + r, c = un.n0 + x;
@@ -817,7 +861,7 @@ __global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args
         const int64_t at = second ? row - job.row_seam : row;
         if (at >= job.out_rows) continue;
         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < a.splits; k++) {
+        for (int k = 0; k < job.splits; k++) {
             const float4 p = *reinterpret_cast<const float4 *>(a.parts + ((int64_t)(un.part + k) * 256 + r) * width + x);
             t.x += p.x, t.y += p.y, t.z += p.z, t.w += p.w;
         }
@@ -870,12 +914,15 @@ int pairs_of_sms() {
 
 // One job's arguments.
 template <int MODE, typename T>
-cudaError_t job_of(const GatedMma &g, const GatedShape &sh, Job &j) {
+cudaError_t job_of(const GatedMma &g, const GatedShape &sh, int half, Job &j) {
     j.M = g.M, j.N = g.N;
     j.tiles_n = (unsigned)sh.tiles_n;
+    j.whole = (unsigned)sh.whole;
+    j.splits = sh.splits;
+    j.split_units = (unsigned)((sh.tiles - sh.whole) * sh.splits);
     j.steps = sh.steps;
     j.seam = (int)(g.b_seam / KC);
-    j.idesc = tc5::idesc(false, 256, 2 * sh.half) | (g.a_side ? tc5::kIdescAmn : 0) | (MODE == GM_PRODUCT ? tc5::kIdescBmn : 0);
+    j.idesc = tc5::idesc(false, 256, 2 * half) | (g.a_side ? tc5::kIdescAmn : 0) | (MODE == GM_PRODUCT ? tc5::kIdescBmn : 0);
     j.a_side = g.a_side;
     j.out0 = MODE == GM_FORWARD ? g.H : g.out0;
     j.out1 = g.out1;
@@ -889,7 +936,7 @@ cudaError_t job_of(const GatedMma &g, const GatedShape &sh, Job &j) {
     for (int i = 0; i < 2 && e == cudaSuccess; i++) {
         const Planes &b = i && g.b1.p ? g.b1 : g.b0;
         CUtensorMap *map = i ? &j.b1 : &j.b0;
-        e = MODE == GM_PRODUCT ? encode(b, true, 64, map) : encode_weights(b, sh.half, map);
+        e = MODE == GM_PRODUCT ? encode(b, true, 64, map) : encode_weights(b, half, map);
     }
     return e;
 }
@@ -897,12 +944,8 @@ cudaError_t job_of(const GatedMma &g, const GatedShape &sh, Job &j) {
 template <int MODE, typename T>
 cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
     Args a = {};
-    const int64_t units = p.whole + (p.tiles - p.whole) * p.splits;
-    if (units > INT32_MAX) return cudaErrorInvalidConfiguration;
-    a.second = (unsigned)p.second;
-    a.whole = (unsigned)p.whole;
-    a.units = (unsigned)units;
-    a.splits = p.splits;
+    if (p.units > INT32_MAX) return cudaErrorInvalidConfiguration;
+    a.units = (unsigned)p.units;
     a.half = p.half;
     a.a_tiles = g->a.planes;
     a.b_tiles = g->a.planes == 3 ? 3 : 1;
@@ -919,19 +962,49 @@ cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
     a.wait_ns = limit ? std::strtoull(limit, nullptr, 10) : 1000000000ull;
     a.stall_step = stall ? std::atoi(stall) : -1;
     cudaError_t e = cudaSuccess;
-    for (int i = 0; i < 2 && e == cudaSuccess; i++) {
-        const int k = i < p.jobs ? i : 0;
-        e = job_of<MODE, T>(g[k], p.shape[k], a.job[i]);
+    for (int i = 0; i < p.jobs && e == cudaSuccess; i++) e = job_of<MODE, T>(g[p.order[i]], p.shape[i], p.half, a.job[i]);
+    if (p.jobs == 1) {   // (no units of its own)
+        a.job[1] = a.job[0];
+        a.job[1].whole = a.job[1].split_units = 0;
     }
     static std::atomic<uint64_t> attr_set{0};
     if (e == cudaSuccess) e = allow_smem(k_gated_mma<MODE, T>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
-    const unsigned grid = 2 * (unsigned)std::min<int64_t>(units, pairs_of_sms());
+    const unsigned grid = 2 * (unsigned)std::min<int64_t>(p.units, pairs_of_sms());
     e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(threads_of(sizeof(T) == 4)),
                         a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
-    if (MODE != GM_PRODUCT || e != cudaSuccess || p.whole == p.tiles) return e;
-    return launch_kernel(k_join_parts<T>, dim3((unsigned)p.half / 2, (unsigned)std::min<int64_t>(p.tiles - p.whole, 65535)), dim3(256), 0, s,
-                         a);
+    int64_t split = 0;
+    for (int i = 0; i < p.jobs; i++) split += p.shape[i].tiles - p.shape[i].whole;
+    if (MODE != GM_PRODUCT || e != cudaSuccess || split == 0) return e;
+    return launch_kernel(k_join_parts<T>, dim3((unsigned)p.half / 2, (unsigned)std::min<int64_t>(split, 65535)), dim3(256), 0, s, a);
+}
+
+// What a plan takes, in SM cycles: a round of units after another, the longest first.
+double cycles_of(const GatedPlan &p, int groups, int64_t pairs) {
+    // four MMAs of 256 columns take 512; narrower tiles wait for their loads
+    const double step = groups * std::max(512.0 * p.half / 128, 400.0);
+    int64_t count[4];
+    int length[4];
+    for (int i = 0; i < 2; i++) {
+        const GatedShape &sh = p.shape[i];
+        count[i] = i < p.jobs ? sh.whole : 0;
+        length[i] = sh.steps;
+        count[2 + i] = i < p.jobs ? (sh.tiles - sh.whole) * sh.splits : 0;
+        length[2 + i] = sh.splits ? (sh.steps + sh.splits - 1) / sh.splits : 0;
+    }
+    double t = 0;
+    int64_t over = 0;   // of the last kind's, into the round that is begun
+    for (int k = 0; k < 4; k++) {
+        const int64_t left = std::max<int64_t>(0, count[k] - over);
+        over = std::max<int64_t>(0, over - count[k]);
+        if (left == 0) continue;
+        const int64_t rounds = (left + pairs - 1) / pairs;
+        t += (double)rounds * (length[k] * step + 1500);   // (a unit's start and end)
+        over = rounds * pairs - left;
+    }
+    // the parts are written and read again, and a launch added
+    if (p.part_bytes) t += 5000 + (double)p.part_bytes * 2 / 4000;
+    return t;
 }
 
 }  // namespace
@@ -947,42 +1020,56 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n) {
         GatedPlan p = {};
         p.jobs = n;
         p.half = half;
+        double total = 0;
         for (int i = 0; i < n; i++) {
             GatedShape &sh = p.shape[i];
-            sh.half = half;
             sh.steps = (int)((g[i].K + KC - 1) / KC);
             sh.tiles_n = product ? (g[i].N + 2 * half - 1) / (2 * half) : (g[i].Fp + half - 1) / half;
-            if (i == 1) p.second = p.tiles;
-            p.tiles += (g[i].M + 255) / 256 * sh.tiles_n;
+            sh.tiles = (g[i].M + 255) / 256 * sh.tiles_n;
+            total += (double)sh.tiles * sh.steps;
         }
-        if (n == 1) p.second = p.tiles;
-        // SM cycles of a step: 512 for four MMAs of 256 columns; narrower tiles wait for their loads
-        const double step = groups * std::max(512.0 * half / 128, 400.0);
-        auto steps_at = [&](int64_t tile) { return p.shape[tile >= p.second].steps; };
-        // whole tiles as long as they fill all pairs, a round of units after another
-        const int64_t full = p.tiles / pairs * pairs;
-        double rounds = 0;
-        for (int64_t at = 0; at < full; at += pairs) {
-            rounds += std::max(steps_at(at), steps_at(at + pairs - 1)) * step + 1500;
-            if (steps_at(at) == steps_at(full - 1)) {   // (and so on to the end)
-                rounds += (double)((full - at) / pairs - 1) * (steps_at(at) * step + 1500);
-                break;
+        auto consider = [&](const int64_t (&whole)[2], const int (&splits)[2]) {
+            GatedPlan q = p;
+            q.units = 0;
+            q.part_bytes = 0;
+            // the job with the longer units first
+            const int l0 = (p.shape[0].steps + splits[0] - 1) / splits[0], l1 = n > 1 ? (p.shape[1].steps + splits[1] - 1) / splits[1] : 0;
+            q.order[0] = n > 1 && l1 > l0;
+            q.order[1] = 1 - q.order[0];
+            for (int i = 0; i < n; i++) {
+                GatedShape &sh = q.shape[i];
+                sh = p.shape[q.order[i]];
+                sh.splits = splits[q.order[i]];
+                sh.whole = sh.splits == 1 ? sh.tiles : whole[q.order[i]];
+                const int64_t parts = (sh.tiles - sh.whole) * sh.splits;
+                q.units += sh.whole + parts;
+                q.part_bytes += parts * 256 * 2 * half * 4;
             }
-        }
-        const int most = full < p.tiles ? std::max(steps_at(full), steps_at(p.tiles - 1)) : 0;
-        const int least = full < p.tiles ? std::min(steps_at(full), steps_at(p.tiles - 1)) : 1;
-        for (int splits = 1; splits <= (product ? 16 : 1) && splits <= least; splits++) {
-            const double units = (double)((p.tiles - full) * splits);
-            double t = rounds + std::ceil(units / (double)pairs) * (std::ceil((double)most / splits) * step + 1500);
-            // the parts are written and read again, and a launch added
-            if (splits > 1) t += 5000 + units * 256 * 2 * half * 8 / 4000;
+            const double t = cycles_of(q, groups, pairs);
             if (best_t == 0 || t < best_t) {
                 best_t = t;
-                best = p;
-                best.splits = splits;
-                best.whole = splits == 1 ? p.tiles : full;
-                best.part_bytes = (p.tiles - best.whole) * splits * 256 * 2 * half * 4;
+                best = q;
             }
+        };
+        consider({0, 0}, {1, 1});
+        if (!product) continue;
+        // every tile split into units of no more steps than the mean of a pair in so many rounds
+        for (int rounds = 1; rounds <= 6; rounds++) {
+            const double most = std::ceil(total / (double)pairs / rounds);
+            int splits[2] = {1, 1};
+            for (int i = 0; i < n; i++)
+                splits[i] = (int)std::min({16.0, (double)p.shape[i].steps, std::ceil(p.shape[i].steps / std::max(1.0, most))});
+            consider({0, 0}, splits);
+        }
+        // those tiles of the shorter sums that would fill the last round in part
+        const int last = n > 1 && p.shape[1].steps <= p.shape[0].steps;
+        const int64_t all = p.shape[0].tiles + (n > 1 ? p.shape[1].tiles : 0), rest = all % pairs;
+        for (int s = 2; s <= 16 && s <= p.shape[last].steps && rest <= p.shape[last].tiles; s++) {
+            int64_t whole[2] = {};
+            int splits[2] = {1, 1};
+            whole[last] = p.shape[last].tiles - rest;
+            splits[last] = s;
+            consider(whole, splits);
         }
     }
     return best;

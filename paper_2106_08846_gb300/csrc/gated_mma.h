@@ -12,7 +12,7 @@ namespace bsr {
 
 enum GatedMode : int {
     GM_FORWARD = 0,    // H = act(G) * U
-    GM_BACKWARD = 1,   // dG, dU (and sums of them over 16 tokens) from G, U and dH
+    GM_BACKWARD = 1,   // dG, dU (and sums of them over runs of tokens) from G, U and dH
     GM_PRODUCT = 2,    // a plain product: dX; dWg and dWu
 };
 
@@ -40,25 +40,28 @@ struct GatedMma {
     int d_planes;
     uint16_t *D;              // d_planes of [M, 2 Fp]: dG, then dU from column Fp on
     int64_t Fp;
-    float *sums;              // of 16 rows of dG and dU each, [ceil(M / 16), 2 Fp], or NULL
+    float *sums;              // of sum_rows rows of dG and dU each, [.., 2 Fp] (an even count of 16s), or NULL
     // GM_PRODUCT: rows below row_seam go to out0, those from it on to out1, `out_rows` in each
     void *out0, *out1;
     int64_t row_seam, out_rows;
 };
 
 struct GatedShape {
-    int half, steps;
-    int64_t tiles_n;
+    int steps, splits;               // of a tile: steps, and the parts of one that is not whole
+    int64_t tiles_n, tiles, whole;   // tiles along N; all; the first ones, which are not split
 };
-// How products run: the tile width, and which tiles (the last, of all products')
-// have their K split into how many parts.
+// How products run: the tile width, their order, and which tiles have their K
+// split into how many parts.
 struct GatedPlan {
-    int jobs, half, splits;
+    int jobs, half;
+    int order[2];                    // shape[i] is g[order[i]]'s
     GatedShape shape[2];
-    int64_t tiles, second, whole;   // tiles; the second product's first; those that are not split
-    int64_t part_bytes;
-    float *parts;                   // part_bytes of workspace
+    int64_t units, part_bytes;
+    float *parts;                    // part_bytes of workspace
 };
+
+// Rows of GatedMma::sums: one for so many rows of dG and dU.
+inline int sum_rows(const GatedPlan &p, bsr_dtype_t dt) { return p.half == 128 || (dt == BSR_F32 && p.half == 64) ? 32 : 16; }
 
 // The plan of g, or of two GM_PRODUCTs (as many parts each) in one launch, from
 // the modes and sizes.
