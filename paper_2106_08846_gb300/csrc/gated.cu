@@ -145,7 +145,7 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     m.mode = backward ? GM_BACKWARD : GM_FORWARD;
     m.a.planes = p.parts;
     m.M = N, m.N = F, m.K = K, m.Fp = p.Fp;
-    p.main_plan = plan_gated_mma(&m, 1);
+    p.main_plan = plan_gated_mma(&m, 1, 0);
     if (!backward) return p;
     p.d_at = take(p.d_parts * N * 2 * p.Fp * 2);
     p.sums_at = take((N + 31) / 32 * 2 * 2 * p.Fp * 4);
@@ -160,7 +160,9 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
     w.row_seam = p.Fp, w.out_rows = F;
     p.parts_at = p.bytes;
     if (dx || dw) {
-        p.grads_plan = plan_gated_mma(dx ? &x : &w, dx + dw);
+        // (where only some gradients are wanted: within the workspace of a call for all)
+        const int64_t most = dx && dw ? INT64_MAX : plan_gated_mma(&x, 2, INT64_MAX).part_bytes;
+        p.grads_plan = plan_gated_mma(dx ? &x : &w, dx + dw, most);
         take(p.grads_plan.part_bytes);
     }
     return p;
@@ -189,14 +191,12 @@ cudaError_t operands(const GatedCall &c, const Plan &p, Planes (&m)[3], cudaStre
 }  // namespace
 
 int64_t gated_workspace(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward) {
-    if (N == 0) return 0;
-    int64_t most = plan_of(N, F, K, dt, backward).bytes;
-    if (backward)   // (less is needed where only some gradients are wanted, but for the parts of another split)
-        for (int one = 0; one < 2; one++) most = std::max(most, plan_of(N, F, K, dt, true, one == 0, one == 1).bytes);
-    return most;
+    if (N == 0 || (!backward && N <= kGatedFew)) return 0;
+    return plan_of(N, F, K, dt, backward).bytes;
 }
 
 cudaError_t launch_gated(const GatedCall &c, cudaStream_t s) {
+    if (c.N <= kGatedFew) return launch_gated_few(c, s);
     Plan p = plan_of(c.N, c.F, c.K, c.dt, false);
     Planes m[3];
     cudaError_t e = operands(c, p, m, s);

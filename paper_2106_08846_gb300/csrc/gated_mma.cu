@@ -32,8 +32,8 @@
 // shared memory (backward pass, 8192 tokens of 1024 into 4096: 12900 cycles a tile
 // of 8200 cycles of MMAs). To that end the weights' rows are loaded in another
 // order: row 8 i + 2 q + e of 32 is feature 8 q + 2 i + e (i, q < 4, e < 2), a box
-// of a five-dimensional tensor. (The plain products' epilogue, a row a lane, is
-// hidden behind their longer sums.)
+// of a five-dimensional tensor. In plain products (bf16) the four threads exchange
+// their columns.
 //
 // Operands stored with K along rows (weights for dX; dG, dU and X for the
 // weights' gradients) are read in place: TMA boxes of 64 x 64 and descriptors
@@ -94,7 +94,7 @@ struct Job {
     int groups;               // gated modes: groups of 32 rows of a part of B
     void *out0, *out1;        // gated forward: H in out0
     int64_t row_seam, out_rows;
-    int vec;                  // output (and dH) rows take wide stores (and loads)
+    int align;                // bytes (at most 16) that output (and dH) rows are aligned to
 };
 
 struct Args {
@@ -178,34 +178,6 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return r;
 }
 
-// 16 values to row p (column c of `cols`): at once where `vec` and all are there.
-__device__ __forceinline__ void store16(uint16_t *row, int64_t c, int64_t cols, bool vec, const float (&v)[16]) {
-    if (vec && c + 16 <= cols) {
-        uint32_t r[8];
-#pragma unroll
-        for (int j = 0; j < 8; j++) r[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
-        ptx::st_global_32(row + c, r);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; j++)
-            if (c + j < cols) row[c + j] = from_f32<uint16_t>(v[j]);
-    }
-}
-__device__ __forceinline__ void store16(float *row, int64_t c, int64_t cols, bool vec, const float (&v)[16]) {
-    if (vec && c + 16 <= cols) {
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            uint32_t r[8];
-#pragma unroll
-            for (int j = 0; j < 8; j++) r[j] = __float_as_uint(v[8 * h + j]);
-            ptx::st_global_32(row + c + 8 * h, r);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; j++)
-            if (c + j < cols) row[c + j] = v[j];
-    }
-}
 // Eight values of a row as they lie in memory: 16 bytes of bf16, 32 of fp32.
 template <typename T>
 struct Eight {
@@ -221,42 +193,78 @@ __device__ __forceinline__ uint32_t pack_bf16(F2 x) {
     const float2 u = unpack2(x);
     return pack_bf16(u.x, u.y);
 }
-__device__ __forceinline__ void store8(uint16_t *p, const F2 (&v)[4]) {   // (16-byte aligned)
-    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(v[0]), pack_bf16(v[1]), pack_bf16(v[2]), pack_bf16(v[3]));
-}
-__device__ __forceinline__ void store8(float *p, const F2 (&v)[4]) {   // (32-byte aligned)
-    uint32_t r[8];
+template <typename T>
+__device__ __forceinline__ Eight<T> eight_of(const F2 (&v)[4]) {
+    Eight<T> r;
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        const float2 u = unpack2(v[j]);
-        r[2 * j] = __float_as_uint(u.x), r[2 * j + 1] = __float_as_uint(u.y);
+        if constexpr (sizeof(T) == 2) {
+            r.w[j] = pack_bf16(v[j]);
+        } else {
+            const float2 u = unpack2(v[j]);
+            r.w[2 * j] = __float_as_uint(u.x), r.w[2 * j + 1] = __float_as_uint(u.y);
+        }
     }
-    ptx::st_global_32(p, r);
+    return r;
+}
+// Eight values to p, n of which are there (the rest is past the row's end), in
+// stores as wide as the rows are aligned; and from p, 0 past the end.
+template <typename T>
+__device__ __forceinline__ void store8(T *p, int64_t n, int align, const Eight<T> &r) {
+    constexpr int words = 2 * sizeof(T);
+    if (n >= 8 && align == 16) {
+#pragma unroll
+        for (int h = 0; h < words / 4; h++)
+            reinterpret_cast<uint4 *>(p)[h] = make_uint4(r.w[4 * h], r.w[4 * h + 1], r.w[4 * h + 2], r.w[4 * h + 3]);
+    } else if (n >= 8 && align >= 8) {
+#pragma unroll
+        for (int h = 0; h < words / 2; h++) reinterpret_cast<uint2 *>(p)[h] = make_uint2(r.w[2 * h], r.w[2 * h + 1]);
+    } else if (n >= 8 && align >= 4) {
+#pragma unroll
+        for (int h = 0; h < words; h++) reinterpret_cast<uint32_t *>(p)[h] = r.w[h];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            if (j >= n) break;
+            if constexpr (sizeof(T) == 2) p[j] = (uint16_t)(r.w[j / 2] >> (16 * (j & 1)));
+            else p[j] = __uint_as_float(r.w[j]);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, int64_t n, int align, Eight<T> &r) {
+    constexpr int words = 2 * sizeof(T);
+    if (n >= 8 && align == 16) {
+#pragma unroll
+        for (int h = 0; h < words / 4; h++) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + h);
+            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
+        }
+    } else if (n >= 8 && align >= 8) {
+#pragma unroll
+        for (int h = 0; h < words / 2; h++) {
+            const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p) + h);
+            r.w[2 * h] = u.x, r.w[2 * h + 1] = u.y;
+        }
+    } else if (n >= 8 && align >= 4) {
+#pragma unroll
+        for (int h = 0; h < words; h++) r.w[h] = __ldg(reinterpret_cast<const uint32_t *>(p) + h);
+    } else {
+#pragma unroll
+        for (int j = 0; j < words; j++) r.w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            if (j >= n) break;
+            if constexpr (sizeof(T) == 2) r.w[j / 2] |= (uint32_t)__ldg(p + j) << (16 * (j & 1));
+            else r.w[j] = __float_as_uint(__ldg(p + j));
+        }
+    }
 }
 
 // dH of row `row` from feature c on; 0 past the matrix.
 template <typename T>
 __device__ __forceinline__ void fetch(const Args &a, const Job &job, int64_t row, int64_t c, Eight<T> &r) {
-    const T *p = static_cast<const T *>(a.dH) + row * job.N + c;
-    if (row < job.M && job.vec && c + 8 <= job.N) {
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; h++) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + h);
-            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
-        }
-    } else {
-        constexpr int per = 4 / sizeof(T);   // values to a word
-#pragma unroll
-        for (int j = 0; j < 2 * (int)sizeof(T); j++) {
-            r.w[j] = 0;
-#pragma unroll
-            for (int h = 0; h < per; h++)
-                if (row < job.M && c + per * j + h < job.N) {
-                    if constexpr (per == 2) r.w[j] |= (uint32_t)__ldg(p + 2 * j + h) << (16 * h);
-                    else r.w[j] = __float_as_uint(__ldg(p + j));
-                }
-        }
-    }
+    load8(static_cast<const T *>(a.dH) + row * job.N + c, row < job.M ? job.N - c : 0, job.align, r);
 }
 
 // Sums of eight values, in pairs, over the lanes with the same lane % 4: lane l
@@ -323,17 +331,7 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             if (row + 8 * h >= job.M) continue;
-            T *out = static_cast<T *>(job.out0) + (row + 8 * h) * job.N + c;
-            if (job.vec && c + 8 <= job.N) {
-                store8(out, v[h]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const float2 x = unpack2(v[h][j]);
-                    if (c + 2 * j < job.N) out[2 * j] = from_f32<T>(x.x);
-                    if (c + 2 * j + 1 < job.N) out[2 * j + 1] = from_f32<T>(x.y);
-                }
-            }
+            store8(static_cast<T *>(job.out0) + (row + 8 * h) * job.N + c, job.N - c, job.align, eight_of<T>(v[h]));
         }
     } else {
         with_act(a.act, [&](auto tag) {
@@ -363,15 +361,15 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
             if (row + 8 * h >= job.M) continue;
             uint16_t *at = a.D + (row + 8 * h) * 2 * a.Fp + c;
             if constexpr (FAST) {
-                store8(at, v[h]);
-                store8(at + a.Fp, w[h]);
+                store8(at, 8, 16, eight_of<uint16_t>(v[h]));
+                store8(at + a.Fp, 8, 16, eight_of<uint16_t>(w[h]));
                 if (a.d_planes == 2) {   // what the rounding left
                     auto rest = [](float x) { return x - __bfloat162float(__float2bfloat16_rn(x)); };
 #pragma unroll
                     for (int j = 0; j < 4; j++) v[h][j] = each2(v[h][j], rest), w[h][j] = each2(w[h][j], rest);
                     at += 2 * a.Fp * job.M;
-                    store8(at, v[h]);
-                    store8(at + a.Fp, w[h]);
+                    store8(at, 8, 16, eight_of<uint16_t>(v[h]));
+                    store8(at + a.Fp, 8, 16, eight_of<uint16_t>(w[h]));
                 }
             } else {
 #pragma unroll
@@ -395,23 +393,62 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
     }
 }
 
-// Puts out 2 x 16 columns, from c on, of this thread's row of a plain product.
+// Puts out 16 rows x 32 columns of a plain product, from row `row` (of this thread:
+// row and row + 8) and column c on; x as tc5::ld_16x32 leaves it.
 template <typename T>
-__device__ __forceinline__ void put_product(const Args &a, const Job &job, const Unit &u, int64_t row, int64_t c, const float (&v)[16],
-                                            const float (&w)[16]) {
+__device__ __forceinline__ void put_product(const Args &a, const Job &job, const Unit &u, int64_t row, int64_t c, const float (&x)[16]) {
+    const int q = threadIdx.x & 3;
     if (u.part >= 0) {   // [256][2 half] of this unit
-        float *at = a.parts + ((int64_t)u.part * 256 + (row - u.m0)) * 2 * a.half + (c - u.n0);
-        store16(at, 0, 32, true, v);
-        store16(at, 16, 32, true, w);
+        float *at = a.parts + ((int64_t)u.part * 256 + (row - u.m0)) * 2 * a.half + (c - u.n0) + 2 * q;
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                *reinterpret_cast<float2 *>(at + 8 * h * 2 * a.half + 8 * i) = make_float2(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]);
         return;
     }
-    if (row >= job.M) return;
-    const bool second = row >= job.row_seam;
-    const int64_t r = second ? row - job.row_seam : row;
-    if (r >= job.out_rows) return;
-    T *out = static_cast<T *>(second ? job.out1 : job.out0) + r * job.N;
-    store16(out, c, job.N, job.vec, v);
-    store16(out, c + 16, job.N, job.vec, w);
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        uint32_t w[4];   // bf16: two columns each
+        if constexpr (sizeof(T) == 2) {
+            // word i of lane j of four has columns 8 i + 2 j, + 1; word j of lane i will, so
+            // that a lane has eight columns: for each bit of i and j, the lanes that differ
+            // in it exchange the words that differ from the lane in it
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i] = pack_bf16(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]);
+#pragma unroll
+            for (int bit = 1; bit < 4; bit *= 2)
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if (i & bit) continue;
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, q & bit ? w[i] : w[i | bit], bit);
+                    if (q & bit) w[i] = got;
+                    else w[i | bit] = got;
+                }
+        }
+        const int64_t m = row + 8 * h;
+        const bool second = m >= job.row_seam;
+        const int64_t r = second ? m - job.row_seam : m;
+        if (m >= job.M || r >= job.out_rows) continue;
+        T *out = static_cast<T *>(second ? job.out1 : job.out0) + r * job.N;
+        if constexpr (sizeof(T) == 2) {
+            Eight<T> e;
+#pragma unroll
+            for (int i = 0; i < 4; i++) e.w[i] = w[i];
+            store8(out + c + 8 * q, job.N - (c + 8 * q), job.align, e);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const int64_t at = c + 8 * i + 2 * q;
+                if (at + 2 <= job.N && job.align >= 8) {
+                    *reinterpret_cast<float2 *>(out + at) = make_float2(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]);
+                } else {
+                    if (at < job.N) out[at] = x[4 * i + 2 * h];
+                    if (at + 1 < job.N) out[at + 1] = x[4 * i + 2 * h + 1];
+                }
+            }
+        }
+    }
 }
 
 template <int MODE, typename T>
@@ -648,8 +685,8 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
         // a piece of the accumulators at tm
         auto load_piece = [&](uint32_t tm, int p, uint32_t (&r0)[16], uint32_t (&r1)[16]) {
             if constexpr (MODE == GM_PRODUCT) {
-                tc5::ld16(tm + 32 * (first + p), r0);
-                tc5::ld16(tm + 32 * (first + p) + 16, r1);
+                tc5::ld_16x32(tm + 32 * (first + p), r0);
+                tc5::ld_16x32(tm + (16u << 16) + 32 * (first + p), r1);
             } else {
                 const uint32_t at = tm + ((uint32_t)(16 * ((first + p) & 1)) << 16) + 32 * ((first + p) >> 1);
                 tc5::ld_16x32(at, r0);
@@ -666,7 +703,9 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
         F2 sg[4], su[4];
         auto put = [&](const Job &job, int p, const float (&x)[16], const float (&y)[16], const Eight<T> (&dh)[2]) {
             if constexpr (MODE == GM_PRODUCT) {
-                put_product<T>(a, job, un, un.m0 + rank * 128 + 32 * q + lane, un.n0 + 32 * (first + p), x, y);
+                const int64_t row = un.m0 + rank * 128 + 32 * q + (lane >> 2), c = un.n0 + 32 * (first + p);
+                put_product<T>(a, job, un, row, c, x);
+                put_product<T>(a, job, un, row + 16, c, y);
             } else {
                 F2 g[2][4], u[2][4];
 #pragma unroll
@@ -927,10 +966,9 @@ cudaError_t job_of(const GatedMma &g, const GatedShape &sh, int half, Job &j) {
     j.out0 = MODE == GM_FORWARD ? g.H : g.out0;
     j.out1 = g.out1;
     j.row_seam = g.row_seam, j.out_rows = g.out_rows;
-    // wide loads and stores: base addresses and rows of 32-byte multiples (16 do for eight bf16)
-    constexpr unsigned wide = MODE != GM_PRODUCT && sizeof(T) == 2 ? 16 : 32;
-    j.vec = g.N * sizeof(T) % wide == 0 &&
-            (reinterpret_cast<uintptr_t>(j.out0) | reinterpret_cast<uintptr_t>(j.out1) | reinterpret_cast<uintptr_t>(g.dH)) % wide == 0;
+    const uintptr_t addresses = reinterpret_cast<uintptr_t>(j.out0) | reinterpret_cast<uintptr_t>(j.out1) |
+                                reinterpret_cast<uintptr_t>(g.dH) | (uintptr_t)(g.N * sizeof(T)) | 16;
+    j.align = (int)(addresses & (~addresses + 1));
     cudaError_t e = encode(g.a, g.a_side, 128, &j.a);
     j.groups = (int)(g.b0.rows / 32);
     for (int i = 0; i < 2 && e == cudaSuccess; i++) {
@@ -1009,7 +1047,7 @@ double cycles_of(const GatedPlan &p, int groups, int64_t pairs) {
 
 }  // namespace
 
-GatedPlan plan_gated_mma(const GatedMma *g, int n) {
+GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
     const int64_t pairs = pairs_of_sms();
     const bool product = g->mode == GM_PRODUCT;
     const int groups = g->a.planes == 3 ? 6 : g->a.planes;   // of four MMAs to a step
@@ -1045,6 +1083,7 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n) {
                 q.units += sh.whole + parts;
                 q.part_bytes += parts * 256 * 2 * half * 4;
             }
+            if (q.part_bytes > most_bytes) return;
             const double t = cycles_of(q, groups, pairs);
             if (best_t == 0 || t < best_t) {
                 best_t = t;

@@ -64,8 +64,8 @@ struct GatedPlan {
 inline int sum_rows(const GatedPlan &p, bsr_dtype_t dt) { return p.half == 128 || (dt == BSR_F32 && p.half == 64) ? 32 : 16; }
 
 // The plan of g, or of two GM_PRODUCTs (as many parts each) in one launch, from
-// the modes and sizes.
-GatedPlan plan_gated_mma(const GatedMma *g, int n);
+// the modes and sizes, with at most so many part_bytes.
+GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes);
 cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s);
 
 // The first error that a kernel of this file recorded on the current device
