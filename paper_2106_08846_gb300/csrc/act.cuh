@@ -1,47 +1,11 @@
 // Activations of the gated feed-forward block and their derivatives, in fp32, two
-// values at a time: packed multiplies and adds take one instruction for both.
+// values at a time.
 #pragma once
 
-#include <cstdint>
-
 #include "bsr.h"
+#include "pair.cuh"
 
 namespace bsr {
-
-struct F2 {
-    unsigned long long v;
-};
-__device__ __forceinline__ F2 pack2(float a, float b) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ float2 unpack2(F2 x) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
-    return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-    F2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-    return r;
-}
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-__device__ __forceinline__ F2 all2(float a) { return pack2(a, a); }
-template <typename F>
-__device__ __forceinline__ F2 each2(F2 x, F f) {
-    const float2 u = unpack2(x);
-    return pack2(f(u.x), f(u.y));
-}
 
 // 1 / (1 + e^-x); FAST: the hardware's exponential, whose relative error of about
 // 2^-21 is lost in a result rounded to bf16.
