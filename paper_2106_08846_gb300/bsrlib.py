@@ -65,6 +65,9 @@ class _ResidualNormGrads(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("dgate", "dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")]
 
 
+_PARAM_GRADS = ("dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")
+
+
 class BsrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -436,6 +439,11 @@ def _check_rows(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype)
         raise ValueError(f"{name} must be contiguous, of shape {list(shape)}")
 
 
+def _is_rows(t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> bool:
+    """Whether _check_rows passes (the calls' fast path: one test, the names only where it fails)."""
+    return t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous())
+
+
 def _residual_norm(y, stream_dt, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps):
     """The checked bsr_residual_norm_t of a call."""
     if post not in _NORM or pre not in _NORM:
@@ -443,16 +451,23 @@ def _residual_norm(y, stream_dt, gate, gate_tokens, scale, alpha, post, post_w, 
     if y.dim() != 2:
         raise ValueError("y must be [N, D]")
     N, D = y.shape
-    for name, w in (("scale", scale), ("post_w", post_w), ("post_b", post_b), ("pre_w", pre_w), ("pre_b", pre_b)):
-        if w is not None:
-            _check_rows(name, w, (D,), torch.float32)
-    if gate is not None:
+    f32, row = torch.float32, (D,)
+    ptrs = []
+    for w in (scale, post_w, post_b, pre_w, pre_b):
+        if w is None:
+            ptrs.append(None)
+            continue
+        if w.dtype is not f32 or w.shape != row or not w.is_contiguous():
+            raise TypeError("scale and the norms' weights and biases must be contiguous float32 tensors of D features")
+        ptrs.append(w.data_ptr())
+    if gate is None:
+        gate_tokens = 0
+    else:
         if gate_tokens < 1:
             raise ValueError("gate_tokens must be at least 1")
         _check_rows("gate", gate, (-(-N // gate_tokens), D), y.dtype)
-    return _ResidualNorm(D, gate_tokens if gate is not None else 0, dtype_code(y.dtype), dtype_code(stream_dt), _NORM[post],
-                         _NORM[pre], eps, eps if pre_eps is None else pre_eps, alpha, _ptr(scale), _ptr(post_w), _ptr(post_b),
-                         _ptr(pre_w), _ptr(pre_b))
+    return _ResidualNorm(D, gate_tokens, dtype_code(y.dtype), dtype_code(stream_dt), _NORM[post], _NORM[pre], eps,
+                         eps if pre_eps is None else pre_eps, alpha, *ptrs)
 
 
 def bsr_residual_norm(y: torch.Tensor, h: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
@@ -466,18 +481,21 @@ def bsr_residual_norm(y: torch.Tensor, h: Optional[torch.Tensor] = None, *, gate
     residual stream (None: no stream yet). gate has a row for each gate_tokens
     tokens; eps is both norms', or post's beside pre_eps. h_out may be h and z may
     be y (see include/bsr.h)."""
+    dt, shape = y.dtype, y.shape
     st = (h if h is not None else h_out if h_out is not None else y).dtype
     p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
     if h_out is None:
-        h_out = torch.empty(y.shape, dtype=st, device=y.device)
+        h_out = torch.empty(shape, dtype=st, device=y.device)
     if z is None and pre != "none":
         z = torch.empty_like(y)
-    for name, t, dt in (("y", y, y.dtype), ("h", h, st), ("h_out", h_out, st), ("z", z, y.dtype)):
-        _check_rows(name, t, y.shape, dt)
-    st = (_lib or load()).bsr_residual_norm(p, y.data_ptr(), _ptr(h), _ptr(gate), h_out.data_ptr(), _ptr(z), y.shape[0],
-                                            _stream(stream))
-    if st:
-        _check(st, "bsr_residual_norm")
+    if not (y.is_contiguous() and _is_rows(h, shape, st) and _is_rows(h_out, shape, st) and _is_rows(z, shape, dt)):
+        for name, t, d in (("y", y, dt), ("h", h, st), ("h_out", h_out, st), ("z", z, dt)):
+            _check_rows(name, t, shape, d)
+    status = (_lib or load()).bsr_residual_norm(p, y.data_ptr(), None if h is None else h.data_ptr(),
+                                                None if gate is None else gate.data_ptr(), h_out.data_ptr(),
+                                                None if z is None else z.data_ptr(), shape[0], _stream(stream))
+    if status:
+        _check(status, "bsr_residual_norm")
     return h_out, z
 
 
@@ -492,25 +510,44 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
     that it returned (needed if pre is a norm) and the gradients of h_out (None: 0)
     and of z (None if pre is "none"): "dy", "dh", and of each parameter given
     "dgate", "dscale", "dpost_w", "dpost_b", "dpre_w" and "dpre_b"."""
-    st = next((t.dtype for t in (h_out, dh_out, dh) if t is not None), y.dtype)
+    dt, shape, device = y.dtype, y.shape, y.device
+    st = next((t.dtype for t in (h_out, dh_out, dh) if t is not None), dt)
     p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
-    out = {"dy": torch.empty_like(y) if dy is None else dy,
-           "dh": torch.empty(y.shape, dtype=st, device=y.device) if dh is None else dh}
-    for name, t, dt in (("y", y, y.dtype), ("h_out", h_out, st), ("dh_out", dh_out, st), ("dz", dz, y.dtype),
-                        ("dy", out["dy"], y.dtype), ("dh", out["dh"], st)):
-        _check_rows(name, t, y.shape, dt)
-    grads = _ResidualNormGrads()
-    for name, w in (("dgate", gate), ("dscale", scale), ("dpost_w", post_w), ("dpost_b", post_b), ("dpre_w", pre_w),
-                    ("dpre_b", pre_b)):
-        if w is not None:
-            out[name] = torch.empty_like(w)
-            setattr(grads, name, out[name].data_ptr())
+    if dy is None:
+        dy = torch.empty_like(y)
+    if dh is None:
+        dh = torch.empty(shape, dtype=st, device=device)
+    if not (y.is_contiguous() and _is_rows(h_out, shape, st) and _is_rows(dh_out, shape, st) and _is_rows(dz, shape, dt)
+            and _is_rows(dy, shape, dt) and _is_rows(dh, shape, st)):
+        for name, t, d in (("y", y, dt), ("h_out", h_out, st), ("dh_out", dh_out, st), ("dz", dz, dt), ("dy", dy, dt),
+                           ("dh", dh, st)):
+            _check_rows(name, t, shape, d)
+    out = {"dy": dy, "dh": dh}
+    params = (scale, post_w, post_b, pre_w, pre_b)
+    ptrs, k = [None] * 6, 0
+    count = sum(w is not None for w in params)
+    if count:   # rows of one allocation
+        rows = torch.empty((count, shape[1]), dtype=torch.float32, device=device)
+        base, each = rows.data_ptr(), rows.unbind(0)
+        for i, name in enumerate(_PARAM_GRADS):
+            if params[i] is not None:
+                out[name] = each[k]
+                ptrs[1 + i] = base + 4 * shape[1] * k
+                k += 1
+    if gate is not None:
+        out["dgate"] = torch.empty_like(gate)
+        ptrs[0] = out["dgate"].data_ptr()
+    grads = _ResidualNormGrads(*ptrs)
     lib, n = _lib or load(), ctypes.c_size_t(0)
-    _check(lib.bsr_residual_norm_workspace(p, y.shape[0], ctypes.byref(n)), "bsr_residual_norm_workspace")
-    ws = _workspace(n.value, y.device, stream)
-    _check(lib.bsr_residual_norm_backward(p, y.data_ptr(), _ptr(h_out), _ptr(gate), _ptr(dh_out), _ptr(dz),
-                                          out["dy"].data_ptr(), out["dh"].data_ptr(), grads, y.shape[0], _ptr(ws), n.value,
-                                          _stream(stream)), "bsr_residual_norm_backward")
+    status = lib.bsr_residual_norm_workspace(p, shape[0], ctypes.byref(n))
+    if status:
+        _check(status, "bsr_residual_norm_workspace")
+    ws = _workspace(n.value, device, stream)
+    status = lib.bsr_residual_norm_backward(p, y.data_ptr(), _ptr(h_out), None if gate is None else gate.data_ptr(),
+                                            _ptr(dh_out), _ptr(dz), dy.data_ptr(), dh.data_ptr(), grads, shape[0], _ptr(ws),
+                                            n.value, _stream(stream))
+    if status:
+        _check(status, "bsr_residual_norm_backward")
     return out
 
 
@@ -518,21 +555,25 @@ def _check_gated(X, Wg, Wu, bg, bu, act: str) -> Tuple[int, int, int, int]:
     """The checks of a gated block's inputs; (N, F, K, type)."""
     if act not in _ACT:
         raise ValueError("act is one of " + ", ".join(_ACT))
-    dt = dtype_code(X.dtype)
+    xt = X.dtype
+    dt = dtype_code(xt)
     if X.dim() != 2 or Wg.dim() != 2:
         raise ValueError("X must be [N, K] and Wg and Wu [F, K]")
     (N, K), F = X.shape, Wg.shape[0]
-    _check_rows("X", X, (N, K), X.dtype)
-    _check_rows("Wg", Wg, (F, K), X.dtype)
-    _check_rows("Wu", Wu, (F, K), X.dtype)
-    _check_rows("bg", bg, (F,), torch.float32)
-    _check_rows("bu", bu, (F,), torch.float32)
+    if not (X.is_contiguous() and _is_rows(Wg, (F, K), xt) and _is_rows(Wu, (F, K), xt) and _is_rows(bg, (F,), torch.float32)
+            and _is_rows(bu, (F,), torch.float32)):
+        for name, t, shape in (("X", X, (N, K)), ("Wg", Wg, (F, K)), ("Wu", Wu, (F, K))):
+            _check_rows(name, t, shape, xt)
+        _check_rows("bg", bg, (F,), torch.float32)
+        _check_rows("bu", bu, (F,), torch.float32)
     return N, F, K, dt
 
 
 def _gated_workspace(N, F, K, dt, backward, device, stream):
     n = ctypes.c_size_t(0)
-    _check((_lib or load()).bsr_gated_workspace(N, F, K, dt, backward, ctypes.byref(n)), "bsr_gated_workspace")
+    status = (_lib or load()).bsr_gated_workspace(N, F, K, dt, backward, ctypes.byref(n))
+    if status:
+        _check(status, "bsr_gated_workspace")
     return _workspace(n.value, device, stream), n.value
 
 
@@ -545,12 +586,14 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[
     N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
     if H is None:
         H = torch.empty((N, F), dtype=X.dtype, device=X.device)
-    _check_rows("H", H, (N, F), X.dtype)
+    elif not _is_rows(H, (N, F), X.dtype):
+        _check_rows("H", H, (N, F), X.dtype)
     ws, n = _gated_workspace(N, F, K, dt, 0, X.device, stream)
-    st = _lib.bsr_gated(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), H.data_ptr(), N, F, K, dt, _ACT[act],
-                        _ptr(ws), n, _stream(stream))
-    if st:
-        _check(st, "bsr_gated")
+    status = _lib.bsr_gated(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), None if bg is None else bg.data_ptr(),
+                            None if bu is None else bu.data_ptr(), H.data_ptr(), N, F, K, dt, _ACT[act],
+                            None if ws is None else ws.data_ptr(), n, _stream(stream))
+    if status:
+        _check(status, "bsr_gated")
     return H
 
 
@@ -562,21 +605,23 @@ def bsr_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: 
     "dbg" and "dbu" where the biases are given. G and U are computed again;
     nothing is kept from the forward call."""
     N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
-    out = {"dX": torch.empty_like(X) if dX is None else dX, "dWg": torch.empty_like(Wg) if dWg is None else dWg,
-           "dWu": torch.empty_like(Wu) if dWu is None else dWu}
-    _check_rows("dH", dH, (N, F), X.dtype)
-    _check_rows("dX", out["dX"], (N, K), X.dtype)
-    _check_rows("dWg", out["dWg"], (F, K), X.dtype)
-    _check_rows("dWu", out["dWu"], (F, K), X.dtype)
-    if bg is not None:
-        out["dbg"] = torch.empty_like(bg)
-    if bu is not None:
-        out["dbu"] = torch.empty_like(bu)
+    xt, w = X.dtype, Wg.shape
+    dX = torch.empty_like(X) if dX is None else dX
+    dWg = torch.empty_like(Wg) if dWg is None else dWg
+    dWu = torch.empty_like(Wu) if dWu is None else dWu
+    if not (_is_rows(dH, (N, F), xt) and _is_rows(dX, X.shape, xt) and _is_rows(dWg, w, xt) and _is_rows(dWu, w, xt)):
+        for name, t, shape in (("dH", dH, (N, F)), ("dX", dX, X.shape), ("dWg", dWg, w), ("dWu", dWu, w)):
+            _check_rows(name, t, shape, xt)
+    out = {"dX": dX, "dWg": dWg, "dWu": dWu}
+    for name, b in (("dbg", bg), ("dbu", bu)):
+        if b is not None:
+            out[name] = torch.empty_like(b)
     ws, n = _gated_workspace(N, F, K, dt, 1, X.device, stream)
-    _check(_lib.bsr_gated_backward(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), dH.data_ptr(),
-                                   out["dX"].data_ptr(), out["dWg"].data_ptr(), out["dWu"].data_ptr(), _ptr(out.get("dbg")),
-                                   _ptr(out.get("dbu")), N, F, K, dt, _ACT[act], _ptr(ws), n, _stream(stream)),
-           "bsr_gated_backward")
+    status = _lib.bsr_gated_backward(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), dH.data_ptr(),
+                                     dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), _ptr(out.get("dbg")),
+                                     _ptr(out.get("dbu")), N, F, K, dt, _ACT[act], _ptr(ws), n, _stream(stream))
+    if status:
+        _check(status, "bsr_gated_backward")
     return out
 
 

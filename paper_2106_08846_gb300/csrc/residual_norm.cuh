@@ -1,0 +1,265 @@
+// What the kernels of the residual step share: how a row lies in the threads that
+// hold it, and sums over them.
+#pragma once
+
+#include "bsr_internal.h"
+#include "elem.cuh"
+#include "pair.cuh"
+#include "ptx.cuh"
+#include "residual_norm.h"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kMaxGroups = 8;     // rows in work per CTA
+
+// How a row lies in a group's NT threads: every NT-th feature to a thread, runs of
+// eight, or runs of eight with none past the row's end.
+enum Layout : int { SINGLES = 0, RUNS = 1, FULL = 2 };
+
+// Feature j of run i of thread t, and whether it is one.
+template <int L>
+__device__ __forceinline__ int feature(int i, int j, int t, int NT) {
+    return L != SINGLES ? 8 * (t + i * NT) + j : (8 * i + j) * NT + t;
+}
+template <int L>
+__device__ __forceinline__ bool inside(int i, int j, int t, int NT, int D) {
+    return L == FULL || feature<L>(i, j, t, NT) < D;
+}
+
+// A run of eight features, in pairs; as it lies in memory.
+struct Run {
+    F2 v[4];
+};
+template <typename T>
+struct Raw {
+    uint32_t w[2 * sizeof(T)];
+    __device__ __forceinline__ F2 two(int j) const {
+        if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+        else return pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    }
+    __device__ __forceinline__ Run run() const {
+        Run r;
+#pragma unroll
+        for (int j = 0; j < 4; j++) r.v[j] = two(j);
+        return r;
+    }
+};
+__device__ __forceinline__ Run all_run(float x) {
+    Run r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) r.v[j] = all2(x);
+    return r;
+}
+
+// Run i of a row; 0 past the row's end. CONST: of an array that the kernel does not write.
+template <typename T, int L, bool CONST>
+__device__ __forceinline__ Raw<T> load_run(const T *row, int D, int i, int t, int NT) {
+    Raw<T> r;
+    if constexpr (L != SINGLES) {
+        const int e = feature<L>(i, 0, t, NT);
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; h++) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (inside<L>(i, 0, t, NT, D)) {
+                const uint4 *p = reinterpret_cast<const uint4 *>(row + e) + h;
+                if constexpr (CONST) u = __ldg(p);
+                else   // a row, read once: the parameters keep their place in L1
+                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                                 : "l"(p)
+                                 : "memory");
+            }
+            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2 * (int)sizeof(T); j++) r.w[j] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int e = feature<L>(i, j, t, NT);
+            if (e < D) {
+                const T v = CONST ? __ldg(row + e) : row[e];
+                if constexpr (sizeof(T) == 4) r.w[j] = __float_as_uint(v);
+                else r.w[j / 2] |= (uint32_t)v << (16 * (j & 1));
+            }
+        }
+    }
+    return r;
+}
+template <typename T, int L>
+__device__ __forceinline__ Run load_const(const T *row, int D, int i, int t, int NT) {
+    return load_run<T, L, true>(row, D, i, t, NT).run();
+}
+template <typename T, int L>
+__device__ __forceinline__ void store_run(T *row, int D, int i, int t, int NT, const Run &r) {
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        const float2 u = unpack2(r.v[j]);
+        x[2 * j] = u.x, x[2 * j + 1] = u.y;
+    }
+    if constexpr (L != SINGLES) {
+        const int e = feature<L>(i, 0, t, NT);
+        if (!inside<L>(i, 0, t, NT, D)) return;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) reinterpret_cast<float4 *>(row + e)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+        } else {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; k++) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(x[2 * k + 1]), "f"(x[2 * k]));
+            *reinterpret_cast<uint4 *>(row + e) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int e = feature<L>(i, j, t, NT);
+            if (e < D) row[e] = from_f32<T>(x[j]);
+        }
+    }
+}
+
+// x - m where there is a feature (x is 0 elsewhere, and stays so)
+template <int L>
+__device__ __forceinline__ void centre(Run &x, float m, int D, int i, int t, int NT) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        if constexpr (L != SINGLES) x.v[j] = add2(x.v[j], all2(inside<L>(i, 0, t, NT, D) ? -m : 0.f));
+        else x.v[j] = add2(x.v[j], pack2(inside<L>(i, 2 * j, t, NT, D) ? -m : 0.f, inside<L>(i, 2 * j + 1, t, NT, D) ? -m : 0.f));
+    }
+}
+__device__ __forceinline__ float both(F2 x) {
+    const float2 u = unpack2(x);
+    return u.x + u.y;
+}
+
+// Sums over the NT threads of a group, the same in each of them. Lanes exchange
+// halves of the values until each has one to add up; the warps' sums meet in shared
+// memory, four warps to a group of words (of absent warps 0). Its two halves are used
+// in turn, so one barrier does: a half is written again only after the other half's
+// barrier. FOUR: at most four warps.
+template <bool FOUR>
+struct GroupSum {
+    float4 *words;   // [2][32]
+    int NT, id, turn;
+    __device__ __forceinline__ void init() {   // before the group's first barrier
+        for (int k = threadIdx.x; k < 64; k += NT) words[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (NT > 32) ptx::named_barrier(1 + id, NT);
+    }
+    template <int N>   // 1, 2 or 4
+    __device__ __forceinline__ void operator()(float (&v)[N]) {
+        const int lane = threadIdx.x & 31;
+        float a[N];
+#pragma unroll
+        for (int k = 0; k < N; k++) a[k] = v[k];
+#pragma unroll
+        for (int n = N, d = 16; n > 1; n /= 2, d /= 2) {
+#pragma unroll
+            for (int k = 0; k < n / 2; k++) {
+                const float mine = lane & d ? a[k + n / 2] : a[k], other = lane & d ? a[k] : a[k + n / 2];
+                a[k] = mine + __shfl_xor_sync(0xffffffffu, other, d);
+            }
+        }
+        constexpr int last = N == 4 ? 4 : N == 2 ? 8 : 16;
+#pragma unroll
+        for (int d = last; d > 0; d /= 2) a[0] += __shfl_xor_sync(0xffffffffu, a[0], d);
+        // value k is lane (32 / N) * (k's bits, the first exchange's the highest)
+        if (NT == 32) {
+#pragma unroll
+            for (int k = 0; k < N; k++) v[k] = __shfl_sync(0xffffffffu, a[0], 32 / N * k);
+            return;
+        }
+        // a warp's values side by side, but a value's four warps in one float4
+        float *w = reinterpret_cast<float *>(words + 32 * turn);
+        turn ^= 1;
+        const int warp = threadIdx.x >> 5;
+        if ((lane & (32 / N - 1)) == 0) w[16 * (warp >> 2) + 4 * (lane / (32 / N)) + (warp & 3)] = a[0];
+        ptx::named_barrier(1 + id, NT);
+        F2 s[N];
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const float4 u = reinterpret_cast<const float4 *>(w)[k];
+            s[k] = add2(pack2(u.x, u.y), pack2(u.z, u.w));
+        }
+        if (!FOUR)
+            for (int g = 1; g < (NT + 127) / 128; g++)
+#pragma unroll
+                for (int k = 0; k < N; k++) {
+                    const float4 u = reinterpret_cast<const float4 *>(w)[4 * g + k];
+                    s[k] = add2(s[k], add2(pack2(u.x, u.y), pack2(u.z, u.w)));
+                }
+#pragma unroll
+        for (int k = 0; k < N; k++) v[k] = both(s[k]);
+    }
+};
+
+// Normalises a row in place.
+template <int V, int L, typename Sum>
+__device__ __forceinline__ void normalise(Run (&x)[V], int how, float eps, int D, float over_d, int t, int NT, Sum &sum) {
+    F2 s;
+    float one[1];
+    if (how == BSR_NORM_LAYER) {
+        s = all2(0.f);
+#pragma unroll
+        for (int i = 0; i < V; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++) s = add2(s, x[i].v[j]);
+        one[0] = both(s);
+        sum(one);
+#pragma unroll
+        for (int i = 0; i < V; i++) centre<L>(x[i], one[0] * over_d, D, i, t, NT);
+    }
+    s = all2(0.f);
+#pragma unroll
+    for (int i = 0; i < V; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) s = fma2(x[i].v[j], x[i].v[j], s);
+    one[0] = both(s);
+    sum(one);
+    const F2 r = all2(rsqrtf(fmaf(one[0], over_d, eps)));
+#pragma unroll
+    for (int i = 0; i < V; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) x[i].v[j] = mul2(x[i].v[j], r);
+}
+// x * w + b with a parameter's row each, where there is one
+template <int V, int L>
+__device__ __forceinline__ void affine(Run (&x)[V], const float *w, const float *b, int D, int t, int NT) {
+    if (w) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const Run p = load_const<float, L>(w, D, i, t, NT);
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[i].v[j] = mul2(x[i].v[j], p.v[j]);
+        }
+    }
+    if (b) {
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            const Run p = load_const<float, L>(b, D, i, t, NT);
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[i].v[j] = add2(x[i].v[j], p.v[j]);
+        }
+    }
+}
+
+int sm_count() {
+    int dev = 0, n = 148;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+        cudaGetLastError();
+    return n;
+}
+
+bool aligned(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// The layout of rows of D features in V runs of NT threads.
+int layout_of(const bsr_residual_norm_t &p, int V, int NT) {
+    const bool runs = p.D % 8 == 0 && aligned(p.scale) && aligned(p.post_w) && aligned(p.post_b) && aligned(p.pre_w) && aligned(p.pre_b);
+    return !runs ? SINGLES : p.D == (int64_t)8 * V * NT ? FULL : RUNS;
+}
+
+}  // namespace
+
+}  // namespace bsr
