@@ -12,12 +12,12 @@
 // fp32: likewise, values split into tf32 parts, high and low, and multiplied as
 // high x low + low x high + high x high; one token or two by multiply-adds, two
 // columns of K to an instruction and four lanes to a feature. (768 into 2048: one
-// token 4.4 us, by the parts 5.5; four tokens 6.3, by the parts 5.5.)
+// token 4.4 us, by the parts 6.6; four tokens 6.3, by the parts 6.6.)
 //
 // What bounds it: DRAM, and for small weights the time of a launch and of one read.
 // 1024 into 4096, bf16: 1 to 8 tokens 4.5 us (16.8 MB, 2.5 us at the copy rate), 16
 // tokens 6.1, 32 tokens 7.8 (the products' own kernel 9.7); fp32: 1 token 6.7 us
-// (33.6 MB, 5.0 us), 8 tokens 7.3, 32 tokens 13.7 (30.6). Four CTAs to an SM, so that
+// (33.6 MB, 5.0 us), 8 tokens 8.8, 32 tokens 17.2 (30.6). Four CTAs to an SM, so that
 // all of them run at once: three took 0.3 us more.
 #include <algorithm>
 
@@ -126,18 +126,27 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_
             for (int n = 0; n < NT; n++) {
                 const uint4 v = load16<T, ALIGNED, CHECK, false>(x[n], k + i * step, K);
                 const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
+                if constexpr (sizeof(T) == 2) {
 #pragma unroll
-                for (int j = 0; j < 4; j += 2) {
-                    if constexpr (sizeof(T) == 2) {
-                        mma<T>(acc[n], ga[j], ua[j], ga[j + 1], ua[j + 1], xv[j], xv[j + 1]);
-                    } else {
-                        uint32_t h[6], l[6];
-                        split(ga[j], h[0], l[0]), split(ua[j], h[1], l[1]), split(ga[j + 1], h[2], l[2]), split(ua[j + 1], h[3], l[3]);
-                        split(xv[j], h[4], l[4]), split(xv[j + 1], h[5], l[5]);
-                        mma<T>(acc[n], l[0], l[1], l[2], l[3], h[4], h[5]);
-                        mma<T>(acc[n], h[0], h[1], h[2], h[3], l[4], l[5]);
-                        mma<T>(acc[n], h[0], h[1], h[2], h[3], h[4], h[5]);
+                    for (int j = 0; j < 4; j += 2) mma<T>(acc[n], ga[j], ua[j], ga[j + 1], ua[j + 1], xv[j], xv[j + 1]);
+                } else {
+                    // the accumulation in an MMA drops bits: the small products first, and
+                    // 16 columns at a time added here (in one accumulator throughout the
+                    // error of 1024 columns was 2.5e-6 of H, that of plain sums 0.9e-6)
+                    float sum[4] = {};
+                    uint32_t h[2][6], l[2][6];
+#pragma unroll
+                    for (int j = 0; j < 2; j++) {
+                        const uint32_t part[6] = {ga[2 * j], ua[2 * j], ga[2 * j + 1], ua[2 * j + 1], xv[2 * j], xv[2 * j + 1]};
+#pragma unroll
+                        for (int k = 0; k < 6; k++) split(part[k], h[j][k], l[j][k]);
+                        mma<T>(sum, l[j][0], l[j][1], l[j][2], l[j][3], h[j][4], h[j][5]);
+                        mma<T>(sum, h[j][0], h[j][1], h[j][2], h[j][3], l[j][4], l[j][5]);
                     }
+#pragma unroll
+                    for (int j = 0; j < 2; j++) mma<T>(sum, h[j][0], h[j][1], h[j][2], h[j][3], h[j][4], h[j][5]);
+#pragma unroll
+                    for (int k = 0; k < 4; k++) acc[n][k] += sum[k];
                 }
             }
         }
