@@ -123,7 +123,7 @@ struct Plan {
 // roundings to 8 bits do not average out.
 constexpr int64_t kFewTokens = 128;
 
-Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, bool dx = true, bool dw = true) {
+Plan make_plan(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, bool dx, bool dw) {
     Plan p = {};
     p.parts = dt == BSR_F32 ? 3 : 1;
     p.d_parts = dt == BSR_F32 ? 3 : N <= kFewTokens ? 2 : 1;
@@ -166,6 +166,28 @@ Plan plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, boo
         take(p.grads_plan.part_bytes);
     }
     return p;
+}
+
+// The plan of these sizes. Choosing tiles and parts takes 5 to 15 us, and a call
+// needs its plan twice (for its workspace too), so each thread keeps the last few.
+const Plan &plan_of(int64_t N, int64_t F, int64_t K, bsr_dtype_t dt, bool backward, bool dx = true, bool dw = true) {
+    struct Kept {
+        int64_t key[4];
+        Plan plan;
+    };
+    constexpr int kKept = 16;
+    thread_local Kept kept[kKept] = {};   // (N is at least 1 in a key)
+    thread_local int next = 0;
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) cudaGetLastError();
+    const int64_t key[4] = {N, F, K, (int64_t)device << 8 | (int64_t)dt << 3 | backward << 2 | dx << 1 | (int)dw};
+    for (const Kept &k : kept)
+        if (std::equal(key, key + 4, k.key)) return k.plan;
+    Kept &k = kept[next];
+    next = (next + 1) % kKept;
+    k.plan = make_plan(N, F, K, dt, backward, dx, dw);
+    std::copy(key, key + 4, k.key);
+    return k.plan;
 }
 
 // The operands X, Wg and Wu as the tensor cores read them.

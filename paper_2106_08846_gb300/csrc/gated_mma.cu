@@ -154,11 +154,11 @@ __device__ __forceinline__ Unit unit_at(const Args &a, unsigned v) {
     return u;
 }
 
-// The unit of a pair in a round of them: every second round is taken backwards,
-// so that who has a long unit in one has a short one in the next (the units come
-// longest first).
-__device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsigned pairs) {
-    return round * pairs + (round & 1 ? pairs - 1 - pair : pair);
+// The unit of a pair in a round of them: all rounds but the first are taken
+// backwards, so that who had a short unit there is the first to have one more (the
+// units come longest first).
+__host__ __device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsigned pairs) {
+    return round * pairs + (round ? pairs - 1 - pair : pair);
 }
 
 // The products of a step, the smallest first: parts of A and B. fp32: (2,0) (1,1)
@@ -1017,32 +1017,46 @@ cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
     return launch_kernel(k_join_parts<T>, dim3((unsigned)p.half / 2, (unsigned)std::min<int64_t>(split, 65535)), dim3(256), 0, s, a);
 }
 
-// What a plan takes, in SM cycles: a round of units after another, the longest first.
-double cycles_of(const GatedPlan &p, int groups, int64_t pairs) {
-    // four MMAs of 256 columns take 512; narrower tiles wait for their loads
-    const double step = groups * std::max(512.0 * p.half / 128, 400.0);
-    int64_t count[4];
-    int length[4];
-    for (int i = 0; i < 2; i++) {
-        const GatedShape &sh = p.shape[i];
-        count[i] = i < p.jobs ? sh.whole : 0;
-        length[i] = sh.steps;
-        count[2 + i] = i < p.jobs ? (sh.tiles - sh.whole) * sh.splits : 0;
-        length[2 + i] = sh.splits ? (sh.steps + sh.splits - 1) / sh.splits : 0;
-    }
-    double t = 0;
-    int64_t over = 0;   // of the last kind's, into the round that is begun
-    for (int k = 0; k < 4; k++) {
-        const int64_t left = std::max<int64_t>(0, count[k] - over);
-        over = std::max<int64_t>(0, over - count[k]);
-        if (left == 0) continue;
-        const int64_t rounds = (left + pairs - 1) / pairs;
-        t += (double)rounds * (length[k] * step + 1500);   // (a unit's start and end)
-        over = rounds * pairs - left;
-    }
+// What a plan takes, in SM cycles: the pair that has most to do, as unit_in hands
+// the units out. Gives up where that must be over `most`.
+double cycles_of(const GatedPlan &p, int groups, int pairs, double most) {
+    // four MMAs of 256 columns take 512; narrower tiles wait for their loads. 1500: a unit's start and end
+    const double step = groups * std::max(512.0 * p.half / 128, 400.0), unit = 1500;
     // the parts are written and read again, and a launch added
-    if (p.part_bytes) t += 5000 + (double)p.part_bytes * 2 / 4000;
-    return t;
+    const double join = p.part_bytes ? 5000 + (double)p.part_bytes * 2 / 4000 : 0;
+    int64_t count[4] = {};
+    double length[4] = {}, total = 0, longest = 0;
+    for (int i = 0; i < p.jobs; i++) {
+        const GatedShape &sh = p.shape[i];
+        count[i] = sh.whole;
+        length[i] = sh.steps * step + unit;
+        count[2 + i] = (sh.tiles - sh.whole) * sh.splits;
+        length[2 + i] = (sh.steps + sh.splits - 1) / sh.splits * step + unit;
+    }
+    for (int k = 0; k < 4; k++) {
+        total += (double)count[k] * length[k];
+        if (count[k]) longest = std::max(longest, length[k]);
+    }
+    const double least = std::max(total / pairs, longest) + join;
+    if (least >= most) return least;
+    // whole rounds of the first kind are the same for all
+    double base = 0;
+    int64_t taken = 0;
+    if (count[0] > pairs) {
+        const int64_t rounds = count[0] / pairs - 1;
+        base = (double)rounds * length[0];
+        taken = rounds * pairs;
+    }
+    constexpr int kMostPairs = 256;
+    double load[kMostPairs] = {};
+    pairs = std::min(pairs, kMostPairs);
+    unsigned v = 0;
+    for (int k = 0; k < 4; k++)
+        for (int64_t n = k == 0 ? taken : 0; n < count[k]; n++, v++) {
+            const unsigned round = v / pairs, at = v % pairs;
+            load[round ? pairs - 1 - at : at] += length[k];
+        }
+    return base + *std::max_element(load, load + pairs) + join;
 }
 
 }  // namespace
@@ -1058,14 +1072,13 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
         GatedPlan p = {};
         p.jobs = n;
         p.half = half;
-        double total = 0;
         for (int i = 0; i < n; i++) {
             GatedShape &sh = p.shape[i];
             sh.steps = (int)((g[i].K + KC - 1) / KC);
             sh.tiles_n = product ? (g[i].N + 2 * half - 1) / (2 * half) : (g[i].Fp + half - 1) / half;
             sh.tiles = (g[i].M + 255) / 256 * sh.tiles_n;
-            total += (double)sh.tiles * sh.steps;
         }
+        // the first `whole` tiles of each job as one unit, the others split
         auto consider = [&](const int64_t (&whole)[2], const int (&splits)[2]) {
             GatedPlan q = p;
             q.units = 0;
@@ -1084,7 +1097,7 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
                 q.part_bytes += parts * 256 * 2 * half * 4;
             }
             if (q.part_bytes > most_bytes) return;
-            const double t = cycles_of(q, groups, pairs);
+            const double t = cycles_of(q, groups, (int)pairs, best_t ? best_t : 1e300);
             if (best_t == 0 || t < best_t) {
                 best_t = t;
                 best = q;
@@ -1092,17 +1105,12 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
         };
         consider({0, 0}, {1, 1});
         if (!product) continue;
-        // every tile split into units of no more steps than the mean of a pair in so many rounds
-        for (int rounds = 1; rounds <= 6; rounds++) {
-            const double most = std::ceil(total / (double)pairs / rounds);
-            int splits[2] = {1, 1};
-            for (int i = 0; i < n; i++)
-                splits[i] = (int)std::min({16.0, (double)p.shape[i].steps, std::ceil(p.shape[i].steps / std::max(1.0, most))});
-            consider({0, 0}, splits);
-        }
-        // those tiles of the shorter sums that would fill the last round in part
+        for (int s0 : {1, 2, 3, 4, 5, 6, 8, 12, 16})
+            for (int s1 : {1, 2, 3, 4, 6, 8, 12, 16})
+                if (s0 + s1 > 2 && s0 <= p.shape[0].steps && (n > 1 ? s1 <= p.shape[1].steps : s1 == 1)) consider({0, 0}, {s0, s1});
+        // only those tiles of the shorter sums that would fill the last round in part
         const int last = n > 1 && p.shape[1].steps <= p.shape[0].steps;
-        const int64_t all = p.shape[0].tiles + (n > 1 ? p.shape[1].tiles : 0), rest = all % pairs;
+        const int64_t rest = (p.shape[0].tiles + (n > 1 ? p.shape[1].tiles : 0)) % pairs;
         for (int s = 2; s <= 16 && s <= p.shape[last].steps && rest <= p.shape[last].tiles; s++) {
             int64_t whole[2] = {};
             int splits[2] = {1, 1};
