@@ -37,9 +37,9 @@ k_residual_norm(const __grid_constant__ RnForward a, int64_t ahead) {
     ptx::pdl_wait();
     for (int64_t n = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; n < a.N; n += (int64_t)gridDim.x * blockDim.y) {
         Run x[V];
-        Raw<TS> h[V];
+        Raw<TS, L> h[V];
         {
-            Raw<TB> y[V];
+            Raw<TB, L> y[V];
 #pragma unroll
             for (int i = 0; i < V; i++) y[i] = load_run<TB, L, false>(static_cast<const TB *>(a.y) + n * D, D, i, t, NT);
             if (a.h) {

@@ -32,13 +32,24 @@ __device__ __forceinline__ bool inside(int i, int j, int t, int NT, int D) {
 struct Run {
     F2 v[4];
 };
-template <typename T>
+template <typename T, int L>
 struct Raw {
     uint32_t w[2 * sizeof(T)];
     __device__ __forceinline__ F2 two(int j) const {
         if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
         else return pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
     }
+    __device__ __forceinline__ Run run() const {
+        Run r;
+#pragma unroll
+        for (int j = 0; j < 4; j++) r.v[j] = two(j);
+        return r;
+    }
+};
+template <typename T>
+struct Raw<T, SINGLES> {   // (put together only when used: a load on its way is not waited for)
+    T v[8];
+    __device__ __forceinline__ F2 two(int j) const { return pack2(to_f32(v[2 * j]), to_f32(v[2 * j + 1])); }
     __device__ __forceinline__ Run run() const {
         Run r;
 #pragma unroll
@@ -55,8 +66,8 @@ __device__ __forceinline__ Run all_run(float x) {
 
 // Run i of a row; 0 past the row's end. CONST: of an array that the kernel does not write.
 template <typename T, int L, bool CONST>
-__device__ __forceinline__ Raw<T> load_run(const T *row, int D, int i, int t, int NT) {
-    Raw<T> r;
+__device__ __forceinline__ Raw<T, L> load_run(const T *row, int D, int i, int t, int NT) {
+    Raw<T, L> r;
     if constexpr (L != SINGLES) {
         const int e = feature<L>(i, 0, t, NT);
 #pragma unroll
@@ -75,15 +86,10 @@ __device__ __forceinline__ Raw<T> load_run(const T *row, int D, int i, int t, in
         }
     } else {
 #pragma unroll
-        for (int j = 0; j < 2 * (int)sizeof(T); j++) r.w[j] = 0;
-#pragma unroll
         for (int j = 0; j < 8; j++) {
             const int e = feature<L>(i, j, t, NT);
-            if (e < D) {
-                const T v = CONST ? __ldg(row + e) : row[e];
-                if constexpr (sizeof(T) == 4) r.w[j] = __float_as_uint(v);
-                else r.w[j / 2] |= (uint32_t)v << (16 * (j & 1));
-            }
+            r.v[j] = T(0);
+            if (e < D) r.v[j] = CONST ? __ldg(row + e) : row[e];
         }
     }
     return r;

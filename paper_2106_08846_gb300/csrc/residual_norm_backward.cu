@@ -40,13 +40,13 @@ struct RnBackwardArgs {
 };
 
 // The four rows of a token as they lie in memory.
-template <typename TB, typename TS, int V>
+template <typename TB, typename TS, int V, int L>
 struct Token {
-    Raw<TB> y[V], dz[V];
-    Raw<TS> h[V], dh[V];
+    Raw<TB, L> y[V], dz[V];
+    Raw<TS, L> h[V], dh[V];
 };
 template <typename TB, typename TS, int V, int L>
-__device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, int NT, Token<TB, TS, V> &k) {
+__device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, int NT, Token<TB, TS, V, L> &k) {
     const bool pre = a.p.pre != BSR_NORM_NONE;
     const int64_t at = n * D;
 #pragma unroll
@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         const int64_t row = u / args.split.slices;
         return row * args.split.span + (u - row * args.split.slices) * args.split.len;
     };
-    Token<TB, TS, V> next = {};
+    Token<TB, TS, V, L> next = {};
     if (KEEP && worker < args.split.units) load_token<TB, TS, V, L>(a, first_of(worker), D, t, NT, next);
     for (int64_t u = worker; u < args.split.units; u += args.split.workers) {
         const int64_t row = u / args.split.slices, n0 = first_of(u);
