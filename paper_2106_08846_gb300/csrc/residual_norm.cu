@@ -71,9 +71,11 @@ k_residual_norm(const __grid_constant__ RnForward a, int64_t ahead) {
         affine<V, L>(x, a.p.scale, nullptr, D, t, NT);
         if (a.h) {
 #pragma unroll
-            for (int i = 0; i < V; i++)
+            for (int i = 0; i < V; i++) {
+                const Run hr = h[i].run();
 #pragma unroll
-                for (int j = 0; j < 4; j++) x[i].v[j] = fma2(all2(a.p.alpha), h[i].two(j), x[i].v[j]);
+                for (int j = 0; j < 4; j++) x[i].v[j] = fma2(all2(a.p.alpha), hr.v[j], x[i].v[j]);
+            }
         }
         if (a.h_out) {
 #pragma unroll
@@ -96,7 +98,7 @@ cudaError_t forward_warps(const RnForward &a, cudaStream_t s) {
     const dim3 block(32, R), grid((unsigned)std::min<int64_t>((a.N + R - 1) / R, INT32_MAX));
     auto kernel = L == FULL   ? k_residual_norm<TB, TS, V, FULL, true>
                   : L == RUNS ? k_residual_norm<TB, TS, V, RUNS, true>
-                              : k_residual_norm<TB, TS, V, SINGLES, true>;
+                              : k_residual_norm<TB, TS, V, ANY, true>;
     return launch_kernel(kernel, grid, block, 0, s, a, (int64_t)sms * 24);   // (about the rows that run at once)
 }
 
@@ -106,7 +108,7 @@ cudaError_t forward_groups(const RnForward &a, cudaStream_t s) {
     const dim3 block(NT, R), grid((unsigned)std::min<int64_t>((a.N + R - 1) / R, INT32_MAX));
     auto kernel = L == FULL   ? k_residual_norm<TB, TS, V, FULL, false>
                   : L == RUNS ? k_residual_norm<TB, TS, V, RUNS, false>
-                              : k_residual_norm<TB, TS, V, SINGLES, false>;
+                              : k_residual_norm<TB, TS, V, ANY, false>;
     return launch_kernel(kernel, grid, block, 0, s, a, (int64_t)sm_count() * std::max(1, 1024 / NT));
 }
 

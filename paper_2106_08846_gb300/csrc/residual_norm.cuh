@@ -14,47 +14,68 @@ namespace {
 
 constexpr int kMaxGroups = 8;     // rows in work per CTA
 
-// How a row lies in a group's NT threads: every NT-th feature to a thread, runs of
-// eight, or runs of eight with none past the row's end.
-enum Layout : int { SINGLES = 0, RUNS = 1, FULL = 2 };
+// How rows lie in memory: anywhere, runs of eight on 16-byte boundaries, or such
+// with none past the row's end. A thread has V runs of eight features.
+enum Layout : int { ANY = 0, RUNS = 1, FULL = 2 };
 
 // Feature j of run i of thread t, and whether it is one.
-template <int L>
-__device__ __forceinline__ int feature(int i, int j, int t, int NT) {
-    return L != SINGLES ? 8 * (t + i * NT) + j : (8 * i + j) * NT + t;
-}
+__device__ __forceinline__ int feature(int i, int j, int t, int NT) { return 8 * (t + i * NT) + j; }
 template <int L>
 __device__ __forceinline__ bool inside(int i, int j, int t, int NT, int D) {
-    return L == FULL || feature<L>(i, j, t, NT) < D;
+    return L == FULL || feature(i, j, t, NT) < D;
 }
 
-// A run of eight features, in pairs; as it lies in memory.
+// A run of eight features, in pairs.
 struct Run {
     F2 v[4];
 };
+template <typename T>
+__device__ __forceinline__ Run run_of(const uint32_t (&w)[2 * sizeof(T)]) {
+    Run r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        if constexpr (sizeof(T) == 4) r.v[j] = pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+        else r.v[j] = pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    }
+    return r;
+}
+
+// A run as it is loaded: its words; or (ANY) the 16-byte blocks that hold it, the
+// place of its first byte in them and the values that are there. The blocks' other
+// bytes lie beside the run in memory, in a block that has a part of it.
 template <typename T, int L>
 struct Raw {
     uint32_t w[2 * sizeof(T)];
-    __device__ __forceinline__ F2 two(int j) const {
-        if constexpr (sizeof(T) == 4) return pack2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
-        else return pack2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
-    }
-    __device__ __forceinline__ Run run() const {
-        Run r;
-#pragma unroll
-        for (int j = 0; j < 4; j++) r.v[j] = two(j);
-        return r;
-    }
+    __device__ __forceinline__ Run run() const { return run_of<T>(w); }
 };
 template <typename T>
-struct Raw<T, SINGLES> {   // (put together only when used: a load on its way is not waited for)
-    T v[8];
-    __device__ __forceinline__ F2 two(int j) const { return pack2(to_f32(v[2 * j]), to_f32(v[2 * j + 1])); }
+struct Raw<T, ANY> {
+    uint32_t w[2 * sizeof(T) + 4];
+    int at, n;
     __device__ __forceinline__ Run run() const {
-        Run r;
+        constexpr int words = 2 * sizeof(T);
+        uint32_t a[words + 4], r[words];
 #pragma unroll
-        for (int j = 0; j < 4; j++) r.v[j] = two(j);
-        return r;
+        for (int k = 0; k < words + 4; k++) a[k] = w[k];
+        if (at & 4) {
+#pragma unroll
+            for (int k = 0; k < words + 3; k++) a[k] = a[k + 1];
+        }
+        if (at & 8) {
+#pragma unroll
+            for (int k = 0; k < words + 2; k++) a[k] = a[k + 2];
+        }
+#pragma unroll
+        for (int k = 0; k < words; k++) {
+            r[k] = sizeof(T) == 2 && (at & 2) ? __funnelshift_r(a[k], a[k + 1], 16) : a[k];
+            if constexpr (sizeof(T) == 4) {
+                if (k >= n) r[k] = 0;
+            } else {
+                if (2 * k >= n) r[k] = 0;
+                else if (2 * k + 1 >= n) r[k] &= 0xffffu;
+            }
+        }
+        return run_of<T>(r);
     }
 };
 __device__ __forceinline__ Run all_run(float x) {
@@ -64,32 +85,42 @@ __device__ __forceinline__ Run all_run(float x) {
     return r;
 }
 
-// Run i of a row; 0 past the row's end. CONST: of an array that the kernel does not write.
+// Run i of a row; 0 past the row's end. CONST: of an array that the kernel does not
+// write (a row that it may write is read once: the parameters keep their place in L1).
+template <bool CONST>
+__device__ __forceinline__ uint4 load_block(const void *p) {
+    uint4 u;
+    if constexpr (CONST)
+        u = __ldg(static_cast<const uint4 *>(p));
+    else
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                     : "l"(p)
+                     : "memory");
+    return u;
+}
 template <typename T, int L, bool CONST>
 __device__ __forceinline__ Raw<T, L> load_run(const T *row, int D, int i, int t, int NT) {
     Raw<T, L> r;
-    if constexpr (L != SINGLES) {
-        const int e = feature<L>(i, 0, t, NT);
+    const int e = feature(i, 0, t, NT);
+    if constexpr (L != ANY) {
 #pragma unroll
         for (int h = 0; h < (int)sizeof(T) / 2; h++) {
             uint4 u = make_uint4(0, 0, 0, 0);
-            if (inside<L>(i, 0, t, NT, D)) {
-                const uint4 *p = reinterpret_cast<const uint4 *>(row + e) + h;
-                if constexpr (CONST) u = __ldg(p);
-                else   // a row, read once: the parameters keep their place in L1
-                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                                 : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
-                                 : "l"(p)
-                                 : "memory");
-            }
+            if (inside<L>(i, 0, t, NT, D)) u = load_block<CONST>(row + e + 8 * h / (int)(sizeof(T) / 2));
             r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
         }
     } else {
+        const uintptr_t first = reinterpret_cast<uintptr_t>(row + e);
+        const char *block = reinterpret_cast<const char *>(first & ~(uintptr_t)15);
+        r.at = (int)(first & 15);
+        r.n = min(8, D - e);
+        const int bytes = r.at + r.n * (int)sizeof(T);   // of the blocks that the run needs
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int e = feature<L>(i, j, t, NT);
-            r.v[j] = T(0);
-            if (e < D) r.v[j] = CONST ? __ldg(row + e) : row[e];
+        for (int h = 0; h < (int)sizeof(T) / 2 + 1; h++) {
+            uint4 u = make_uint4(0, 0, 0, 0);
+            if (r.n > 0 && 16 * h < bytes) u = load_block<CONST>(block + 16 * h);
+            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
         }
     }
     return r;
@@ -100,29 +131,48 @@ __device__ __forceinline__ Run load_const(const T *row, int D, int i, int t, int
 }
 template <typename T, int L>
 __device__ __forceinline__ void store_run(T *row, int D, int i, int t, int NT, const Run &r) {
-    float x[8];
+    if (!inside<L>(i, 0, t, NT, D)) return;
+    T *const p = row + feature(i, 0, t, NT);
+    if constexpr (sizeof(T) == 4) {
+        float x[8];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-        const float2 u = unpack2(r.v[j]);
-        x[2 * j] = u.x, x[2 * j + 1] = u.y;
-    }
-    if constexpr (L != SINGLES) {
-        const int e = feature<L>(i, 0, t, NT);
-        if (!inside<L>(i, 0, t, NT, D)) return;
-        if constexpr (sizeof(T) == 4) {
+        for (int j = 0; j < 4; j++) {
+            const float2 u = unpack2(r.v[j]);
+            x[2 * j] = u.x, x[2 * j + 1] = u.y;
+        }
+        if constexpr (L != ANY) {
 #pragma unroll
-            for (int h = 0; h < 2; h++) reinterpret_cast<float4 *>(row + e)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+            for (int h = 0; h < 2; h++) reinterpret_cast<float4 *>(p)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
         } else {
-            uint32_t w[4];
+            const int n = D - feature(i, 0, t, NT);
 #pragma unroll
-            for (int k = 0; k < 4; k++) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(x[2 * k + 1]), "f"(x[2 * k]));
-            *reinterpret_cast<uint4 *>(row + e) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int j = 0; j < 8; j++)
+                if (j < n) p[j] = x[j];
         }
     } else {
+        uint32_t w[4];
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const int e = feature<L>(i, j, t, NT);
-            if (e < D) row[e] = from_f32<T>(x[j]);
+        for (int k = 0; k < 4; k++) {
+            const float2 u = unpack2(r.v[k]);
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[k]) : "f"(u.y), "f"(u.x));
+        }
+        if constexpr (L != ANY) {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+            const int n = D - feature(i, 0, t, NT);
+            if (n < 8) {
+#pragma unroll
+                for (int j = 0; j < 8; j++)
+                    if (j < n) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+            } else if (reinterpret_cast<uintptr_t>(p) & 2) {
+                p[0] = (uint16_t)w[0];
+#pragma unroll
+                for (int k = 0; k < 3; k++) *reinterpret_cast<uint32_t *>(p + 1 + 2 * k) = __funnelshift_r(w[k], w[k + 1], 16);
+                p[7] = (uint16_t)(w[3] >> 16);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; k++) *reinterpret_cast<uint32_t *>(p + 2 * k) = w[k];
+            }
         }
     }
 }
@@ -132,7 +182,7 @@ template <int L>
 __device__ __forceinline__ void centre(Run &x, float m, int D, int i, int t, int NT) {
 #pragma unroll
     for (int j = 0; j < 4; j++) {
-        if constexpr (L != SINGLES) x.v[j] = add2(x.v[j], all2(inside<L>(i, 0, t, NT, D) ? -m : 0.f));
+        if constexpr (L != ANY) x.v[j] = add2(x.v[j], all2(inside<L>(i, 0, t, NT, D) ? -m : 0.f));
         else x.v[j] = add2(x.v[j], pack2(inside<L>(i, 2 * j, t, NT, D) ? -m : 0.f, inside<L>(i, 2 * j + 1, t, NT, D) ? -m : 0.f));
     }
 }
@@ -263,7 +313,7 @@ bool aligned(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 // The layout of rows of D features in V runs of NT threads.
 int layout_of(const bsr_residual_norm_t &p, int V, int NT) {
     const bool runs = p.D % 8 == 0 && aligned(p.scale) && aligned(p.post_w) && aligned(p.post_b) && aligned(p.pre_w) && aligned(p.pre_b);
-    return !runs ? SINGLES : p.D == (int64_t)8 * V * NT ? FULL : RUNS;
+    return !runs ? ANY : p.D == (int64_t)8 * V * NT ? FULL : RUNS;
 }
 
 }  // namespace

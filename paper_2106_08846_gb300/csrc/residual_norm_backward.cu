@@ -76,7 +76,7 @@ enum Gate : int { NONE = 0, OF_RUNS = 1, OF_TOKENS = 2 };
 
 template <typename TB, typename TS, int V, int L, int THREADS, int GATE, bool BIAS>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_norm_backward(const __grid_constant__ RnBackwardArgs args) {
-    constexpr bool KEEP = V == 1;
+    constexpr bool KEEP = V == 1 && (L != ANY || THREADS == 128);
     extern __shared__ float4 unit_sums[];
     __shared__ float4 words[kMaxGroups][64];
     const RnBackward &a = args.b;
@@ -409,9 +409,9 @@ cudaError_t backward(const RnBackward &b, cudaStream_t s) {
     if (tokens && sh.V == 1) {
         kernel = threads <= 128 ? (L == FULL   ? k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_TOKENS, true>
                                    : L == RUNS ? k_residual_norm_backward<TB, TS, 1, RUNS, 128, OF_TOKENS, true>
-                                               : k_residual_norm_backward<TB, TS, 1, SINGLES, 128, OF_TOKENS, true>)
-                                : (L != SINGLES ? k_residual_norm_backward<TB, TS, 1, RUNS, 512, OF_TOKENS, true>
-                                                : k_residual_norm_backward<TB, TS, 1, SINGLES, 512, OF_TOKENS, true>);
+                                               : k_residual_norm_backward<TB, TS, 1, ANY, 128, OF_TOKENS, true>)
+                                : (L != ANY ? k_residual_norm_backward<TB, TS, 1, RUNS, 512, OF_TOKENS, true>
+                                                : k_residual_norm_backward<TB, TS, 1, ANY, 512, OF_TOKENS, true>);
     } else if (sh.V == 1 && threads <= 128) {
         if (L == FULL)
             kernel = gate ? (bias ? k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_RUNS, false>)
@@ -419,15 +419,15 @@ cudaError_t backward(const RnBackward &b, cudaStream_t s) {
         else if (L == RUNS)
             kernel = gate ? k_residual_norm_backward<TB, TS, 1, RUNS, 128, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 1, RUNS, 128, NONE, true>;
         else
-            kernel = k_residual_norm_backward<TB, TS, 1, SINGLES, 128, OF_RUNS, true>;
+            kernel = k_residual_norm_backward<TB, TS, 1, ANY, 128, OF_RUNS, true>;
     } else if (sh.V == 1) {
-        kernel = L == SINGLES ? k_residual_norm_backward<TB, TS, 1, SINGLES, 512, OF_RUNS, true>
+        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 1, ANY, 512, OF_RUNS, true>
                  : gate       ? k_residual_norm_backward<TB, TS, 1, RUNS, 512, OF_RUNS, true>
                               : k_residual_norm_backward<TB, TS, 1, RUNS, 512, NONE, true>;
     } else if (threads <= 512) {
-        kernel = L == SINGLES ? k_residual_norm_backward<TB, TS, 2, SINGLES, 512, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 512, OF_RUNS, true>;
+        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 2, ANY, 512, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 512, OF_RUNS, true>;
     } else {
-        kernel = L == SINGLES ? k_residual_norm_backward<TB, TS, 2, SINGLES, 1024, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 1024, OF_RUNS, true>;
+        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 2, ANY, 1024, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 1024, OF_RUNS, true>;
     }
     const size_t smem = (size_t)threads * 3 * 2 * sh.V * 16;   // (up to 192 KB, at 16384 features)
     if (smem > 32 * 1024) {   // (beside 8 KB that every kernel has)
