@@ -85,26 +85,6 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
     }
 }
 
-// dbg and dbu: the sums of the 2 Fp columns of `sums` [n, 2 Fp], 32 columns a
-// CTA: 32 x 32 threads, each every 32nd row, then the 32.
-__global__ void __launch_bounds__(1024) k_bias_sums(const float *sums, int64_t n, int64_t F, int64_t Fp, float *dbg, float *dbu) {
-    __shared__ float part[32][33];
-    ptx::pdl_launch_dependents();
-    ptx::pdl_wait();
-    const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x;
-    float s = 0.f;
-#pragma unroll 8
-    for (int64_t k = threadIdx.y; k < n; k += 32) s += sums[k * 2 * Fp + c];
-    part[threadIdx.y][threadIdx.x] = s;
-    __syncthreads();
-    s = part[threadIdx.x][threadIdx.y];   // column threadIdx.y, a row a lane
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    const int64_t col = (int64_t)blockIdx.x * 32 + threadIdx.y, f = col < Fp ? col : col - Fp;
-    float *out = col < Fp ? dbg : dbu;
-    if (threadIdx.x == 0 && out && f < F) out[f] = s;
-}
-
 int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // The workspace of a call, and its products.
@@ -254,12 +234,16 @@ cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
     w.b0 = m[0];
     w.out0 = c.dWg, w.out1 = c.dWu;
     p.grads_plan.parts = reinterpret_cast<float *>(ws + p.parts_at);
-    if (e == cudaSuccess && (dx || dw)) e = launch_gated_mma(dx ? &x : &w, p.grads_plan, s);
-    if (e == cudaSuccess && g.sums)
-        e = launch_kernel(k_bias_sums, dim3((unsigned)(2 * p.Fp / 32)), dim3(32, 32), 0, s, (const float *)g.sums,
-                          (c.N + 31) / 32 * (32 / sum_rows(p.main_plan, c.dt)), c.F,
-                          p.Fp, c.dbg, c.dbu);
-    return e;
+    GatedBias b;
+    if (g.sums) {
+        b.sums = g.sums;
+        b.rows = (c.N + 31) / 32 * (32 / sum_rows(p.main_plan, c.dt));
+        b.F = c.F, b.Fp = p.Fp;
+        b.dbg = c.dbg, b.dbu = c.dbu;
+    }
+    if (e != cudaSuccess) return e;
+    if (dx || dw) return launch_gated_mma(dx ? &x : &w, p.grads_plan, s, b);
+    return launch_gated_bias(b, s);
 }
 
 }  // namespace bsr

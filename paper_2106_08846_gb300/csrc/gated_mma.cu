@@ -880,25 +880,29 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
     }
 }
 
-// The split tiles: the sum of a tile's parts, in their order, four columns a
-// thread; a tile to a blockIdx.y.
+// What is left after the products, in one launch: the CTAs below `joins` add up
+// the parts of the split tiles, in their order, four columns a thread and half / 2
+// CTAs to a tile; those above sum the 2 Fp columns of dG's and dU's sums (n rows of
+// them), 32 columns a CTA, 32 x 8 threads, each every eighth row, then the eight.
 template <typename T>
-__global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args a) {
+__global__ void __launch_bounds__(256) k_gated_finish(const __grid_constant__ Args a, unsigned joins, int64_t n, int64_t F, float *dbg,
+                                                      float *dbu) {
+    __shared__ float part[8][33];
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
-    const int fours = a.half / 2, width = 2 * a.half;
-    const Job &j0 = a.job[0], &j1 = a.job[1];
-    const unsigned n0 = j0.split_units / (unsigned)j0.splits, n1 = j1.split_units / (unsigned)j1.splits;
-    for (unsigned tile = blockIdx.y; tile < n0 + n1; tile += gridDim.y) {
-        const unsigned part = tile < n0 ? tile * (unsigned)j0.splits : j0.split_units + (tile - n0) * (unsigned)j1.splits;
-        const Unit un = unit_at<GM_PRODUCT>(a, j0.whole + j1.whole + part);
+    if (blockIdx.x < joins) {
+        const int fours = a.half / 2, width = 2 * a.half;
+        const unsigned tile = blockIdx.x / (unsigned)fours;
+        const Job &j0 = a.job[0], &j1 = a.job[1];
+        const unsigned n0 = j0.split_units / (unsigned)j0.splits;
+        const unsigned first = tile < n0 ? tile * (unsigned)j0.splits : j0.split_units + (tile - n0) * (unsigned)j1.splits;
+        const Unit un = unit_at<GM_PRODUCT>(a, j0.whole + j1.whole + first);
         const Job &job = a.job[un.job];
-        const int e = blockIdx.x * 256 + threadIdx.x, r = e / fours, x = (e - r * fours) * 4;
+        const int e = (int)(blockIdx.x % (unsigned)fours) * 256 + threadIdx.x, r = e / fours, x = (e - r * fours) * 4;
         const int64_t row = un.m0 + r, c = un.n0 + x;
-        if (r >= 256 || row >= job.M || c >= job.N) continue;
         const bool second = row >= job.row_seam;
         const int64_t at = second ? row - job.row_seam : row;
-        if (at >= job.out_rows) continue;
+        if (row >= job.M || c >= job.N || at >= job.out_rows) return;
         float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int k = 0; k < job.splits; k++) {
             const float4 p = *reinterpret_cast<const float4 *>(a.parts + ((int64_t)(un.part + k) * 256 + r) * width + x);
@@ -909,7 +913,22 @@ __global__ void __launch_bounds__(256) k_join_parts(const __grid_constant__ Args
 #pragma unroll
         for (int j = 0; j < 4; j++)
             if (c + j < job.N) out[j] = from_f32<T>(f[j]);
+        return;
     }
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const int64_t c = (int64_t)(blockIdx.x - joins) * 32 + lane;
+    float s = 0.f;
+#pragma unroll 16
+    for (int64_t k = w; k < n; k += 8) s += a.sums[k * 2 * a.Fp + c];
+    part[w][lane] = s;
+    __syncthreads();
+    if (w) return;
+    s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; k++) s += part[k][lane];
+    const int64_t f = c < a.Fp ? c : c - a.Fp;
+    float *out = c < a.Fp ? dbg : dbu;
+    if (out && f < F) out[f] = s;
 }
 
 // `side`: boxes of 64 columns x 64 rows; else of 64 columns x `rows` rows.
@@ -979,8 +998,16 @@ cudaError_t job_of(const GatedMma &g, const GatedShape &sh, int half, Job &j) {
     return e;
 }
 
+template <typename T>
+cudaError_t finish(const Args &a, int64_t joins, const GatedBias &b, cudaStream_t s) {
+    const int64_t sums = b.sums ? 2 * b.Fp / 32 : 0;
+    if (joins + sums == 0) return cudaSuccess;
+    if (joins + sums > INT32_MAX) return cudaErrorInvalidConfiguration;
+    return launch_kernel(k_gated_finish<T>, dim3((unsigned)(joins + sums)), dim3(256), 0, s, a, (unsigned)joins, b.rows, b.F, b.dbg, b.dbu);
+}
+
 template <int MODE, typename T>
-cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
+cudaError_t launch(const GatedMma *g, const GatedPlan &p, const GatedBias &b, cudaStream_t s) {
     Args a = {};
     if (p.units > INT32_MAX) return cudaErrorInvalidConfiguration;
     a.units = (unsigned)p.units;
@@ -1011,10 +1038,12 @@ cudaError_t launch(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(p.units, pairs_of_sms());
     e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(threads_of(sizeof(T) == 4)),
                         a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
-    int64_t split = 0;
-    for (int i = 0; i < p.jobs; i++) split += p.shape[i].tiles - p.shape[i].whole;
-    if (MODE != GM_PRODUCT || e != cudaSuccess || split == 0) return e;
-    return launch_kernel(k_join_parts<T>, dim3((unsigned)p.half / 2, (unsigned)std::min<int64_t>(split, 65535)), dim3(256), 0, s, a);
+    if (MODE != GM_PRODUCT || e != cudaSuccess) return e;
+    int64_t joins = 0;
+    for (int i = 0; i < p.jobs; i++) joins += (p.shape[i].tiles - p.shape[i].whole) * (p.half / 2);
+    a.sums = const_cast<float *>(b.sums);
+    a.Fp = b.Fp;
+    return finish<T>(a, joins, b, s);
 }
 
 // What a plan takes, in SM cycles: the pair that has most to do, as unit_in hands
@@ -1122,13 +1151,20 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
     return best;
 }
 
-cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s) {
+cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s, const GatedBias &b) {
     const bool f32 = g->dt == BSR_F32;
     switch (g->mode) {
-        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, p, s) : launch<GM_FORWARD, uint16_t>(g, p, s);
-        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, p, s) : launch<GM_BACKWARD, uint16_t>(g, p, s);
-        default: return f32 ? launch<GM_PRODUCT, float>(g, p, s) : launch<GM_PRODUCT, uint16_t>(g, p, s);
+        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, p, b, s) : launch<GM_FORWARD, uint16_t>(g, p, b, s);
+        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, p, b, s) : launch<GM_BACKWARD, uint16_t>(g, p, b, s);
+        default: return f32 ? launch<GM_PRODUCT, float>(g, p, b, s) : launch<GM_PRODUCT, uint16_t>(g, p, b, s);
     }
+}
+
+cudaError_t launch_gated_bias(const GatedBias &b, cudaStream_t s) {
+    Args a = {};
+    a.sums = const_cast<float *>(b.sums);
+    a.Fp = b.Fp;
+    return finish<float>(a, 0, b, s);
 }
 
 cudaError_t gated_mma_status(int *code) {

@@ -66,7 +66,15 @@ inline int sum_rows(const GatedPlan &p, bsr_dtype_t dt) { return p.half == 128 |
 // The plan of g, or of two GM_PRODUCTs (as many parts each) in one launch, from
 // the modes and sizes, with at most so many part_bytes.
 GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes);
-cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s);
+// dbg and dbu from GM_BACKWARD's sums (NULL: not wanted): `rows` of them.
+struct GatedBias {
+    const float *sums = nullptr;
+    int64_t rows = 0, F = 0, Fp = 0;
+    float *dbg = nullptr, *dbu = nullptr;
+};
+// Runs them; GM_PRODUCTs also the biases' gradients, in their last launch.
+cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s, const GatedBias &b = GatedBias());
+cudaError_t launch_gated_bias(const GatedBias &b, cudaStream_t s);
 
 // The first error that a kernel of this file recorded on the current device
 // since the last call; synchronises the device.
