@@ -84,7 +84,7 @@ bsr_status_t check_residual(const bsr_residual_norm_t *p, int64_t N, bool gate) 
 }
 
 size_t gate_bytes(const bsr_residual_norm_t *p, int64_t N) {
-    return (size_t)((N + p->gate_tokens - 1) / p->gate_tokens) * p->D * dtype_size(p->block_dt);
+    return (N == 0 ? 0 : (size_t)((N - 1) / p->gate_tokens) + 1) * p->D * dtype_size(p->block_dt);
 }
 
 void add_params(Buffers &b, const bsr_residual_norm_t *p) {

@@ -112,13 +112,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
 #pragma unroll
             for (int i = 0; i < V; i++) unit_sum(k, i, 0) = unit_sum(k, i, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    // the tokens of a unit, and of the worker's next one
+    // the first token of a unit (of a last gate row's units some may lie past the last
+    // token: they add nothing, and nothing is read for them)
     auto first_of = [&](int64_t u) {
         const int64_t row = u / args.split.slices;
         return row * args.split.span + (u - row * args.split.slices) * args.split.len;
     };
     Token<TB, TS, V, L> next = {};
-    if (KEEP && worker < args.split.units) load_token<TB, TS, V, L>(a, first_of(worker), D, t, NT, next);
+    if (KEEP && worker < args.split.units && first_of(worker) < a.N) load_token<TB, TS, V, L>(a, first_of(worker), D, t, NT, next);
     for (int64_t u = worker; u < args.split.units; u += args.split.workers) {
         const int64_t row = u / args.split.slices, n0 = first_of(u);
         const int64_t n1 = min(min(n0 + args.split.len, (row + 1) * args.split.span), a.N);
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
                 dz[i] = next.dz[i].run();
             }
             const int64_t after = n + 1 < n1 ? n + 1 : later;
-            if (KEEP && after >= 0) load_token<TB, TS, V, L>(a, after, D, t, NT, next);
+            if (KEEP && after >= 0 && after < a.N) load_token<TB, TS, V, L>(a, after, D, t, NT, next);
             if (post_layer || pre_layer) {
                 F2 sh = all2(0.f), sy = all2(0.f);
 #pragma unroll

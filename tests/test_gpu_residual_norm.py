@@ -235,6 +235,15 @@ def test_backward_tokens(N, gate, block, stream):
     check_backward(*make(N, 72, block, stream, "layer", "rms", gate=gate, scale=N % 2 == 0))
 
 
+@pytest.mark.parametrize("block,stream", TYPES)
+def test_gate_rows_longer_than_the_tokens_left(block, stream):
+    # a last row of fewer tokens than the others, and one row for far more tokens than there are
+    for N, gate in ((600, 512), (1030, 1024), (50, 2**63 - 1)):
+        args = make(N, 264, block, stream, "rms", "layer", gate=gate, scale=True)
+        check_forward(*args)
+        check_backward(*args)
+
+
 def test_backward_repeats_to_the_bit_and_in_place_on_a_stream():
     s, p = make(3000, 768, "bf16", "f32", "rms", "layer", gate=700, scale=True)
     h_out = bsr.bsr_residual_norm(s["y"], s["h"], **p)[0]
