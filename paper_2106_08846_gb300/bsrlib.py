@@ -65,9 +65,6 @@ class _ResidualNormGrads(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("dgate", "dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")]
 
 
-_PARAM_GRADS = ("dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")
-
-
 class BsrError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -523,20 +520,14 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
                            ("dh", dh, st)):
             _check_rows(name, t, shape, d)
     out = {"dy": dy, "dh": dh}
-    params = (scale, post_w, post_b, pre_w, pre_b)
-    ptrs, k = [None] * 6, 0
-    count = sum(w is not None for w in params)
-    if count:   # rows of one allocation
-        rows = torch.empty((count, shape[1]), dtype=torch.float32, device=device)
-        base, each = rows.data_ptr(), rows.unbind(0)
-        for i, name in enumerate(_PARAM_GRADS):
-            if params[i] is not None:
-                out[name] = each[k]
-                ptrs[1 + i] = base + 4 * shape[1] * k
-                k += 1
-    if gate is not None:
-        out["dgate"] = torch.empty_like(gate)
-        ptrs[0] = out["dgate"].data_ptr()
+    ptrs = []
+    for name, w in (("dgate", gate), ("dscale", scale), ("dpost_w", post_w), ("dpost_b", post_b), ("dpre_w", pre_w),
+                    ("dpre_b", pre_b)):
+        if w is None:
+            ptrs.append(None)
+        else:   # (an allocation each: rows of one, as views, take the host twice as long)
+            out[name] = d = torch.empty_like(w)
+            ptrs.append(d.data_ptr())
     grads = _ResidualNormGrads(*ptrs)
     lib, n = _lib or load(), ctypes.c_size_t(0)
     status = lib.bsr_residual_norm_workspace(p, shape[0], ctypes.byref(n))
