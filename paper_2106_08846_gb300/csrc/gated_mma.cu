@@ -346,15 +346,17 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
                     w[h][j] = mul2(d, act);
                 }
         });
-        // (rows past the matrix: dH is 0 there, and so is X, so G and U are finite
-        // unless the feature's weights or biases are not)
+        // (no rows past the matrix: X and dH are 0 there, but a feature's weights and
+        // biases need not be finite)
 #pragma unroll
-        for (int h = 0; h < 2; h++)
+        for (int h = 0; h < 2; h++) {
+            if (row + 8 * h >= job.M) continue;
 #pragma unroll
             for (int j = 0; j < 4; j++) {
                 sg[j] = add2(sg[j], v[h][j]);
                 su[j] = add2(su[j], w[h][j]);
             }
+        }
         if (c >= a.Fp) return;
 #pragma unroll
         for (int h = 0; h < 2; h++) {

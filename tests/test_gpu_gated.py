@@ -188,6 +188,23 @@ def test_a_bad_token_leaves_the_others_alone(N, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_bias_gradients_of_features_that_are_not_finite(dtype):
+    s, dH = make(40, 96, 64, dtype)
+    dH = dH.abs() + 0.5
+    s["bg"][3] = float("inf")
+    got = bsr.bsr_gated_backward(s["X"], s["Wg"], s["Wu"], s["bg"], s["bu"], dH, act="relu")
+    assert got["dbu"][3] == float("inf")   # sum of dH relu(inf)
+    U = project(s["X"], s["Wu"], s["bu"])[0]
+    want = (dH.double() * U)[:, 3].sum()
+    assert abs(float(got["dbg"][3]) - float(want)) <= SUM * 40 * float((dH.double() * (U.abs() + 10)).max())
+    if dtype == "bf16":   # weights: every token's G is -inf, and relu of it 0 (fp32 parts give NaN)
+        s, dH = make(40, 96, 64, dtype)
+        s["X"], s["Wg"][5, 7] = s["X"].abs() + 0.5, -float("inf")
+        got = bsr.bsr_gated_backward(s["X"], s["Wg"], s["Wu"], s["bg"], s["bu"], dH, act="relu")
+        assert got["dbg"][5] == 0 and got["dbu"][5] == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N", [3, 700])
 def test_repeats_to_the_bit_on_another_stream(N, dtype):
     s, dH = make(N, 520, 328, dtype)
