@@ -7,34 +7,52 @@
 
 namespace bsr {
 
-// 1 / (1 + e^-x); FAST: the hardware's exponential, whose relative error of about
-// 2^-21 is lost in a result rounded to bf16.
+// e^(s x); FAST: the hardware's exponential, whose relative error of about 2^-21 is
+// lost in a result rounded to bf16.
 template <bool FAST>
-__device__ __forceinline__ F2 logistic(F2 x) {
-    F2 e;
-    if constexpr (FAST) {
-        e = each2(mul2(x, all2(-1.4426950408889634f)), [](float t) {
-            float r;
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
-            return r;
-        });
-    } else {
-        e = each2(x, [](float t) { return expf(-t); });
-    }
-    return each2(add2(e, all2(1.f)), [](float t) {
+__device__ __forceinline__ F2 exp_of(float s, F2 x) {
+    if constexpr (!FAST) return each2(x, [s](float t) { return expf(s * t); });
+    return each2(mul2(x, all2(s * 1.4426950408889634f)), [](float t) {
         float r;
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
         return r;
     });
+}
+__device__ __forceinline__ float reciprocal(float t) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+
+// 1 / (1 + e^-x)
+template <bool FAST>
+__device__ __forceinline__ F2 logistic(F2 x) {
+    return each2(add2(exp_of<FAST>(-1.f, x), all2(1.f)), reciprocal);
 }
 
 constexpr float kGeluA = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
-// Phi(g), the normal distribution
+// Phi(g), the normal distribution, and e^(-g^2 / 2), from which its density follows:
+// erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), for x >= 0, to 1.5e-7
+// (Abramowitz and Stegun 7.1.26; x = |g| / sqrt(2), and half of it for Phi). With the
+// exponential that the derivative takes anyway. (fp32, 1000 tokens of 768 into 2048:
+// 35.3 us, with normcdff 38.9; backward 129.8 and 138.0.)
 template <bool FAST>
-__device__ __forceinline__ F2 normal_cdf(F2 g) {
-    return each2(g, [](float t) { return FAST ? fmaf(0.5f, erff(0.70710678f * t), 0.5f) : normcdff(t); });
+__device__ __forceinline__ F2 normal_cdf(F2 g, F2 &e) {
+    e = exp_of<FAST>(-0.5f, mul2(g, g));
+    auto cdf = [](float x, float ex) {
+        const float t = reciprocal(fmaf(fabsf(x), 0.3275911f * 0.70710678f, 1.f));
+        float q = 0.5f * 1.061405429f;
+        q = fmaf(q, t, -0.5f * 1.453152027f);
+        q = fmaf(q, t, 0.5f * 1.421413741f);
+        q = fmaf(q, t, -0.5f * 0.284496736f);
+        q = fmaf(q, t, 0.5f * 0.254829592f);
+        q *= t * ex;
+        return x < 0.f ? q : 1.f - q;
+    };
+    const float2 x = unpack2(g), ex = unpack2(e);
+    return pack2(cdf(x.x, ex.x), cdf(x.y, ex.y));
 }
 // the tanh form of GELU is g / (1 + e^-2u), which is the same; 2u
 __device__ __forceinline__ F2 gelu_2u(F2 g) {
@@ -46,11 +64,18 @@ __device__ __forceinline__ F2 relu(F2 g) {
 
 template <int ACT, bool FAST>
 __device__ __forceinline__ F2 activate(F2 g) {
-    if constexpr (ACT == BSR_ACT_SILU) return mul2(g, logistic<FAST>(g));
-    else if constexpr (ACT == BSR_ACT_GELU) return mul2(g, normal_cdf<FAST>(g));
-    else if constexpr (ACT == BSR_ACT_GELU_TANH) return mul2(g, logistic<FAST>(gelu_2u(g)));
-    else if constexpr (ACT == BSR_ACT_RELU) return relu(g);
-    else return logistic<FAST>(g);
+    if constexpr (ACT == BSR_ACT_SILU) {
+        return mul2(g, logistic<FAST>(g));
+    } else if constexpr (ACT == BSR_ACT_GELU) {
+        F2 e;
+        return mul2(g, normal_cdf<FAST>(g, e));
+    } else if constexpr (ACT == BSR_ACT_GELU_TANH) {
+        return mul2(g, logistic<FAST>(gelu_2u(g)));
+    } else if constexpr (ACT == BSR_ACT_RELU) {
+        return relu(g);
+    } else {
+        return logistic<FAST>(g);
+    }
 }
 
 // act(g), and act'(g) in `slope`.
@@ -62,8 +87,8 @@ __device__ __forceinline__ F2 activate_slope(F2 g, F2 &slope) {
         slope = mul2(p, fma2(g, fma2(p, minus, one), one));
         return mul2(g, p);
     } else if constexpr (ACT == BSR_ACT_GELU) {
-        const F2 p = normal_cdf<FAST>(g);
-        const F2 density = each2(mul2(mul2(all2(-0.5f), g), g), [](float t) { return 0.3989422804f * (FAST ? __expf(t) : expf(t)); });
+        F2 e;
+        const F2 p = normal_cdf<FAST>(g, e), density = mul2(all2(0.3989422804f), e);   // (1 / sqrt(2 pi))
         slope = fma2(g, density, p);
         return mul2(g, p);
     } else if constexpr (ACT == BSR_ACT_GELU_TANH) {

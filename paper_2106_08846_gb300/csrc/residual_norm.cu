@@ -12,8 +12,11 @@
 // row on its way at once. Wider rows are a group of threads', eight or sixteen
 // features each.
 //
-// What bounds it: DRAM (y and h in, h' and z out): 16384 x 1024 bf16 26.8 us, 134 MB
-// at 74% of the copy rate.
+// What bounds it: DRAM (y and h in, h' and z out): 16384 x 1024 bf16 with a gate for
+// 512 tokens 25 us, 134 MB at 79% of the copy rate; 16384 x 768 fp32 41 us, 201 MB at
+// 72%; 4096 x 4096 bf16 33 us. One row of 1024: 2.6 us, the launch and one read's
+// latency. Rows that are no runs of eight on 16-byte boundaries pay for shifting them
+// into place and for stores of single words (16384 x 1193 bf16: 21% of the copy rate).
 #include <algorithm>
 
 #include "launch.cuh"
@@ -24,7 +27,7 @@ namespace bsr {
 namespace {
 
 // WARP: a warp to a row. Rows `ahead` further on are asked for into L2: registers
-// hold too few loads to keep DRAM busy (16384 x 1024 bf16: 29.4 us without).
+// hold too few loads to keep DRAM busy (16384 x 1024 bf16: 25.9 us without, 25.1 with).
 template <typename TB, typename TS, int V, int L, bool WARP>
 __global__ void __launch_bounds__(WARP ? 256 : 1024, WARP ? (V < 3 ? 4 : sizeof(TS) == 2 ? 3 : 2) : 1)
 k_residual_norm(const __grid_constant__ RnForward a, int64_t ahead) {

@@ -13,7 +13,10 @@
 // post norm's gradient. The groups' sums are added in a fixed order by a second
 // kernel, so results do not change from run to run.
 //
-// What bounds it: DRAM. y, h', dh', dz in, dy, dh out. MEASURED_BACKWARD
+// What bounds it: DRAM (y, h', dh', dz in, dy, dh out): 16384 x 1024, a bf16 block on an
+// fp32 stream with a gate for 512 tokens, 61 us, 302 MB at 73% of the copy rate; 16384 x
+// 768 fp32 65 us, 302 MB at 68%. Rows of more than 4096 features do not fit the
+// registers that a thread has for them: 12 to 24%.
 #include <algorithm>
 
 #include "launch.cuh"
@@ -314,8 +317,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
 }
 
 // Adds the workers' sums (blockIdx.y < kSums: one parameter's) or gate rows'
-// slices (`rows` of them to a blockIdx.y), 32 features a CTA: 32 x 32 threads, each
-// every so-manieth entry of a row, then those of a row.
+// slices (`rows` of them to a blockIdx.y), 32 features a CTA: 32 x 32 threads. The
+// threads of a feature take its entries in turn; their sums are added in their order.
 template <typename TB>
 __global__ void __launch_bounds__(1024) k_residual_norm_sums(const __grid_constant__ RnBackwardArgs args, int rows) {
     __shared__ float part[32][33];

@@ -158,6 +158,18 @@ def test_activations_over_their_range(act, N, dtype):
     check_backward(s, dH, act, dtype)
 
 
+@pytest.mark.parametrize("N", [2, 4000])
+def test_gelu_on_a_grid(N):
+    # G is x itself and U is 1. Phi: 7.5e-8 of the formula, and a few roundings of values below 1
+    x = torch.linspace(-12, 12, N, device="cuda")[:, None].contiguous()
+    W, none, one = torch.ones(32, 1, device="cuda"), torch.zeros(32, device="cuda"), torch.ones(32, device="cuda")
+    H = bsr.bsr_gated(x, W, W * 0, none, one, act="gelu").double()
+    want, slope = act64(x.double(), "gelu")
+    assert ((H - want).abs() <= 4e-7 * x.abs() + 2.0 ** -22 * want.abs()).all()
+    got = bsr.bsr_gated_backward(x, W, W * 0, none, one, torch.ones(N, 32, device="cuda"), act="gelu")
+    assert ((got["dX"].double() / 32 - slope).abs() <= 4e-7 * (1 + x.abs()) + SUM * slope.abs()).all()
+
+
 @pytest.mark.parametrize("dtype,N,F,K", [("bf16", 4096, 2048, 768), ("f32", 2048, 1024, 768), ("bf16", 2500, 4096, 1024)])
 def test_many_tiles(dtype, N, F, K):
     s, dH = make(N, F, K, dtype)
