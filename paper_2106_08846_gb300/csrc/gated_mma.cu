@@ -1060,8 +1060,12 @@ cudaError_t launch(const GatedMma *g, const GatedPlan &p, const GatedBias &b, cu
 // What a plan takes, in SM cycles: the pair that has most to do, as unit_in hands
 // the units out. Gives up where that must be over `most`.
 double cycles_of(const GatedPlan &p, int groups, int pairs, double most) {
-    // four MMAs of 256 columns take 512; narrower tiles wait for their loads. 1500: a unit's start and end
-    const double step = groups * std::max(512.0 * p.half / 128, 400.0), unit = 1500;
+    // four MMAs of 256 columns take 512; narrower tiles wait for their loads, 400 for each
+    // pair of tiles of A and B. A unit's start and end: 1500; of fp32 its epilogue too,
+    // whose registers the next unit's sums need
+    const bool f32 = groups == 6;
+    const int tiles = f32 ? 3 : groups;
+    const double step = std::max(groups * 512.0 * p.half / 128, tiles * 400.0), unit = f32 ? 12000.0 * p.half / 128 : 1500;
     // the parts are written and read again, and a launch added
     const double join = p.part_bytes ? 5000 + (double)p.part_bytes * 2 / 4000 : 0;
     int64_t count[4] = {};
