@@ -42,6 +42,10 @@
  *    MB + 1, KB and nnzb below 2^31.
  *  - One handle must not run bsr_spmm on two streams at once (the split-row
  *    workspace and staging buffers belong to the handle).
+ *  - bsr_residual_norm, bsr_gated and their backward calls have no handle: they
+ *    work on the current device and keep nothing between calls but the choice of
+ *    tiles for the last few sizes (per thread). Scratch memory is the caller's, a
+ *    buffer to each call in flight.
  */
 #ifndef BSR_H
 #define BSR_H
@@ -388,8 +392,8 @@ bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void
  *
  * fp32 operands run on the tensor cores as three bf16 parts each, whose sum they
  * are, and a product as the six part products that are not below 2^-24 of it,
- * added in fp32: |dG| <= 1e-5 (sum |x||w| + |b|), as for bsr_spmm. A token whose
- * fp32 activations are not finite gives NaN where plain arithmetic might give an
+ * added in fp32: |dG| <= 1e-5 (sum |x||w| + |b|), as for bsr_spmm. A sum with
+ * fp32 values that are not finite gives NaN where plain arithmetic might give an
  * infinity.
  */
 typedef enum {

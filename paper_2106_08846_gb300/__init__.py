@@ -1,8 +1,11 @@
-"""GB300 (sm_103a) block-sparse-row x dense product, Y = X W^T + b.
+"""GB300 (sm_103a) block-sparse-row x dense product, Y = X W^T + b, and the
+operators that stand between two products of a transformer layer.
 
 The product at the centre of "Algorithm to Compilation Co-design" (Section
 2.2): a pruned weight stored in BSR form (data, indices, indptr) multiplied
-with dense activations. The compute lives in libbsr_gb300.so (include/bsr.h);
+with dense activations; beside it the residual step with its norms
+(bsr_residual_norm) and the gated feed-forward block (bsr_gated), forward and
+backward. The compute lives in libbsr_gb300.so (include/bsr.h);
 this package is its ctypes binding and its build script.
 """
 from .bsrlib import (  # noqa: F401
