@@ -191,18 +191,27 @@ __device__ __forceinline__ float both(F2 x) {
     return u.x + u.y;
 }
 
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+
 // Sums over the NT threads of a group, the same in each of them. Lanes exchange
 // halves of the values until each has one to add up; the warps' sums meet in shared
 // memory, four warps to a group of words (of absent warps 0). Its two halves are used
 // in turn, so one barrier does: a half is written again only after the other half's
-// barrier. FOUR: at most four warps.
-template <bool FOUR>
+// barrier. FOUR: at most four warps. CLUSTER: a CTA's threads are the group's part in
+// it; the CTAs then write their sums into each other's shared memory, likewise in two
+// halves, and add them up in the order of their ranks.
+template <bool FOUR, bool CLUSTER = false>
 struct GroupSum {
-    float4 *words;   // [2][32]
+    float4 *words;   // [2][32]; CLUSTER: then [2][CTAs]
     int NT, id, turn;
     __device__ __forceinline__ void init() {   // before the group's first barrier
         for (int k = threadIdx.x; k < 64; k += NT) words[k] = make_float4(0.f, 0.f, 0.f, 0.f);
         if (NT > 32) ptx::named_barrier(1 + id, NT);
+        if (CLUSTER) ptx::cluster_barrier();   // the other CTAs have begun
     }
     template <int N>   // 1, 2 or 4
     __device__ __forceinline__ void operator()(float (&v)[N]) {
@@ -248,6 +257,23 @@ struct GroupSum {
                 }
 #pragma unroll
         for (int k = 0; k < N; k++) v[k] = both(s[k]);
+        if constexpr (CLUSTER) {
+            const uint32_t ctas = cluster_size();
+            float *const all = reinterpret_cast<float *>(words + 64 + 4 * turn);
+            if (threadIdx.x < ctas) {
+#pragma unroll
+                for (int k = 0; k < N; k++)
+                    ptx::store_cluster(ptx::map_to_cta(all + 4 * ptx::cluster_rank() + k, threadIdx.x), __float_as_uint(v[k]));
+            }
+            __syncwarp();
+            ptx::cluster_barrier();
+#pragma unroll
+            for (int k = 0; k < N; k++) {
+                float c = all[k];
+                for (uint32_t r = 1; r < ctas; r++) c += all[4 * r + k];
+                v[k] = c;
+            }
+        }
     }
 };
 

@@ -15,8 +15,9 @@
 //
 // What bounds it: DRAM (y, h', dh', dz in, dy, dh out): 16384 x 1024, a bf16 block on an
 // fp32 stream with a gate for 512 tokens, 61 us, 302 MB at 73% of the copy rate; 16384 x
-// 768 fp32 65 us, 302 MB at 68%. Rows of more than 4096 features do not fit the
-// registers that a thread has for them: 12 to 24%.
+// 768 fp32 65 us, 302 MB at 68%. Rows of more than 4096 features are a cluster's, whose
+// CTAs exchange their sums through distributed shared memory, which they wait for three
+// times a row: 27 to 30%.
 #include <algorithm>
 
 #include "launch.cuh"
@@ -40,26 +41,23 @@ struct RnBackwardArgs {
     RnSplit split;
     float *sums;        // [workers][kSums][D]
     float *gate_sums;   // [units][D], where a gate row has several slices
+    int ctas;           // to a row
 };
 
 // The four rows of a token as they lie in memory.
-template <typename TB, typename TS, int V, int L>
+template <typename TB, typename TS, int L>
 struct Token {
-    Raw<TB, L> y[V], dz[V];
-    Raw<TS, L> h[V], dh[V];
+    Raw<TB, L> y, dz;
+    Raw<TS, L> h, dh;
 };
-template <typename TB, typename TS, int V, int L>
-__device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, int NT, Token<TB, TS, V, L> &k) {
-    const bool pre = a.p.pre != BSR_NORM_NONE;
+template <typename TB, typename TS, int L>
+__device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, Token<TB, TS, L> &k) {
     const int64_t at = n * D;
-#pragma unroll
-    for (int i = 0; i < V; i++) {
-        k.y[i] = load_run<TB, L, false>(static_cast<const TB *>(a.y) + at, D, i, t, NT);
-        if (a.dh_out) k.dh[i] = load_run<TS, L, false>(static_cast<const TS *>(a.dh_out) + at, D, i, t, NT);
-        if (pre) {
-            k.h[i] = load_run<TS, L, true>(static_cast<const TS *>(a.h_out) + at, D, i, t, NT);
-            k.dz[i] = load_run<TB, L, false>(static_cast<const TB *>(a.dz) + at, D, i, t, NT);
-        }
+    k.y = load_run<TB, L, false>(static_cast<const TB *>(a.y) + at, D, 0, t, 0);
+    if (a.dh_out) k.dh = load_run<TS, L, false>(static_cast<const TS *>(a.dh_out) + at, D, 0, t, 0);
+    if (a.p.pre != BSR_NORM_NONE) {
+        k.h = load_run<TS, L, true>(static_cast<const TS *>(a.h_out) + at, D, 0, t, 0);
+        k.dz = load_run<TB, L, false>(static_cast<const TB *>(a.dz) + at, D, 0, t, 0);
     }
 }
 
@@ -67,53 +65,50 @@ __device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D
 // from two sums for each feature, Q = sum dH yh and S = sum dH: with t = yh w + b,
 // sum t dH = w Q + b S, from which the gate's gradient is scale times and the
 // scale's gate times that, and post_w's and post_b's are scale gate Q and
-// scale gate S. THREADS: the most of a CTA. KEEP: the next token is on its way in
-// registers (rows of more than 4096 features leave none for it). BIAS: whether there
-// may be one. GATE: none, a row of it for runs of tokens, or one for each token.
+// scale gate S. A thread has eight features. THREADS: the most of a CTA. CLUSTER: a
+// row is a cluster's (more than 4096 features). KEEP: the next token is on its way in
+// registers (odd rows, which take more, leave none for it in large CTAs). BIAS: whether
+// there may be one. GATE: none, a row of it for runs of tokens, or one for each token.
 // Without a gate all units are one. With one for each token, so they are: the gate
 // goes into dH before Q and S, and its own gradient is the token's. With runs, what
-// units add up to is held in shared memory (3 D values to a group), a thread's own
-// features each. At 128 registers four CTAs of 128 threads share an
-// SM: three, at 168, took 109 us for 16384 x 1024 of a bf16 block on an fp32 stream.
+// units add up to is held in shared memory (24 values to a thread). At 128 registers
+// four CTAs of 128 threads share an SM: three, at 168, took 109 us for 16384 x 1024 of
+// a bf16 block on an fp32 stream.
 enum Gate : int { NONE = 0, OF_RUNS = 1, OF_TOKENS = 2 };
 
-template <typename TB, typename TS, int V, int L, int THREADS, int GATE, bool BIAS>
+template <typename TB, typename TS, int L, int THREADS, int GATE, bool BIAS, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_norm_backward(const __grid_constant__ RnBackwardArgs args) {
-    constexpr bool KEEP = V == 1 && (L != ANY || THREADS == 128);
+    constexpr bool KEEP = L != ANY || THREADS == 128;
     extern __shared__ float4 unit_sums[];
-    __shared__ float4 words[kMaxGroups][64];
+    __shared__ float4 words[CLUSTER ? 2 : kMaxGroups][64];   // (CLUSTER: one group, and the CTAs' sums)
     const RnBackward &a = args.b;
-    const int t = threadIdx.x, NT = blockDim.x, D = (int)a.p.D;
+    const int NT = blockDim.x, D = (int)a.p.D;
+    const int t = (CLUSTER ? (int)ptx::cluster_rank() * NT : 0) + threadIdx.x;   // features 8 t ..
     const float over_d = 1.f / (float)D;
-    GroupSum<THREADS == 128> sum{words[threadIdx.y], NT, (int)threadIdx.y, 0};
+    GroupSum<THREADS == 128, CLUSTER> sum{words[threadIdx.y], NT, (int)threadIdx.y, 0};
     sum.init();
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();
-    const int64_t worker = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int64_t worker = CLUSTER ? blockIdx.x / (unsigned)args.ctas : (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const bool post = a.p.post != BSR_NORM_NONE, pre = a.p.pre != BSR_NORM_NONE;
     const bool post_layer = a.p.post == BSR_NORM_LAYER, pre_layer = a.p.pre == BSR_NORM_LAYER;
-    Run Q[V], S[V], dpre_w[V], dpre_b[V], pre_w[V], wc[V];   // wc: scale gate post_w
-    // dscale, dpost_w, dpost_b (k) of run i
-    float4 *const mine_s = unit_sums + (size_t)threadIdx.y * 3 * 2 * V * NT + t;
-    auto unit_sum = [&](int k, int i, int h) -> float4 & { return mine_s[((k * V + i) * 2 + h) * NT]; };
-    auto zero = [&](Run (&r)[V]) {
-#pragma unroll
-        for (int i = 0; i < V; i++) r[i] = all_run(0.f);
+    Run Q, S, dpre_w, dpre_b, pre_w, wc;   // wc: scale gate post_w
+    // dscale, dpost_w, dpost_b (k)
+    float4 *const mine_s = unit_sums + (size_t)threadIdx.y * 3 * 2 * NT + threadIdx.x;
+    auto unit_sum = [&](int k, int h) -> float4 & { return mine_s[(k * 2 + h) * NT]; };
+    auto param = [&](Run &r, const float *p, float absent) {
+        r = all_run(absent);
+        if (p) r = load_const<float, L>(p, D, 0, t, 0);
     };
-    auto param = [&](Run (&r)[V], const float *p, float absent) {
+    auto times = [&](Run &r, const Run &s) {
 #pragma unroll
-        for (int i = 0; i < V; i++) {
-            r[i] = all_run(absent);
-            if (p) r[i] = load_const<float, L>(p, D, i, t, NT);
-        }
+        for (int j = 0; j < 4; j++) r.v[j] = mul2(r.v[j], s.v[j]);
     };
-    zero(Q), zero(S), zero(dpre_w), zero(dpre_b);
-    if (KEEP) param(pre_w, a.p.pre_w, 1.f);
+    Q = S = dpre_w = dpre_b = all_run(0.f);
+    param(pre_w, a.p.pre_w, 1.f);
     if (GATE == OF_RUNS) {
 #pragma unroll
-        for (int k = 0; k < 3; k++)
-#pragma unroll
-            for (int i = 0; i < V; i++) unit_sum(k, i, 0) = unit_sum(k, i, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < 3; k++) unit_sum(k, 0) = unit_sum(k, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
     }
     // the first token of a unit (of a last gate row's units some may lie past the last
     // token: they add nothing, and nothing is read for them)
@@ -121,67 +116,45 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         const int64_t row = u / args.split.slices;
         return row * args.split.span + (u - row * args.split.slices) * args.split.len;
     };
-    Token<TB, TS, V, L> next = {};
-    if (KEEP && worker < args.split.units && first_of(worker) < a.N) load_token<TB, TS, V, L>(a, first_of(worker), D, t, NT, next);
+    Token<TB, TS, L> next = {};
+    if (KEEP && worker < args.split.units && first_of(worker) < a.N) load_token<TB, TS, L>(a, first_of(worker), D, t, next);
     for (int64_t u = worker; u < args.split.units; u += args.split.workers) {
         const int64_t row = u / args.split.slices, n0 = first_of(u);
         const int64_t n1 = min(min(n0 + args.split.len, (row + 1) * args.split.span), a.N);
         const int64_t later = u + args.split.workers < args.split.units ? first_of(u + args.split.workers) : -1;
         const TB *const gate_row = GATE == OF_RUNS && a.gate ? static_cast<const TB *>(a.gate) + row * D : nullptr;
-        auto times = [&](Run &r, const Run &s) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) r.v[j] = mul2(r.v[j], s.v[j]);
-        };
         param(wc, a.p.scale, 1.f);
-#pragma unroll
-        for (int i = 0; i < V; i++) {
-            if (gate_row) times(wc[i], load_const<TB, L>(gate_row, D, i, t, NT));
-            if (a.p.post_w) times(wc[i], load_const<float, L>(a.p.post_w, D, i, t, NT));
-        }
+        if (gate_row) times(wc, load_const<TB, L>(gate_row, D, 0, t, 0));
+        if (a.p.post_w) times(wc, load_const<float, L>(a.p.post_w, D, 0, t, 0));
         for (int64_t n = n0; n < n1; n++) {
-            Run y[V], hh[V], g[V], dz[V];
-            if (!KEEP) load_token<TB, TS, V, L>(a, n, D, t, NT, next);
-#pragma unroll
-            for (int i = 0; i < V; i++) {
-                y[i] = next.y[i].run();
-                hh[i] = next.h[i].run();
-                g[i] = next.dh[i].run();   // dH
-                dz[i] = next.dz[i].run();
-            }
+            if (!KEEP) load_token<TB, TS, L>(a, n, D, t, next);
+            Run y = next.y.run(), hh = next.h.run(), g = next.dh.run(), dz = next.dz.run();   // g: dH
             const int64_t after = n + 1 < n1 ? n + 1 : later;
-            if (KEEP && after >= 0 && after < a.N) load_token<TB, TS, V, L>(a, after, D, t, NT, next);
+            if (KEEP && after >= 0 && after < a.N) load_token<TB, TS, L>(a, after, D, t, next);
             if (post_layer || pre_layer) {
                 F2 sh = all2(0.f), sy = all2(0.f);
 #pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        sh = add2(sh, hh[i].v[j]);
-                        sy = add2(sy, y[i].v[j]);
-                    }
+                for (int j = 0; j < 4; j++) {
+                    sh = add2(sh, hh.v[j]);
+                    sy = add2(sy, y.v[j]);
+                }
                 float m[2] = {both(sh), both(sy)};
                 sum(m);
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    if (pre_layer) centre<L>(hh[i], m[0] * over_d, D, i, t, NT);
-                    if (post_layer) centre<L>(y[i], m[1] * over_d, D, i, t, NT);
-                }
+                if (pre_layer) centre<L>(hh, m[0] * over_d, D, 0, t, 0);
+                if (post_layer) centre<L>(y, m[1] * over_d, D, 0, t, 0);
             }
             float ry = 1.f;
             if (pre) {
-                if (!KEEP) param(pre_w, a.p.pre_w, 1.f);
                 F2 sh = all2(0.f), sy = all2(0.f), sa = all2(0.f), sx = all2(0.f);
 #pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const F2 aw = mul2(dz[i].v[j], pre_w[i].v[j]);
-                        sy = fma2(y[i].v[j], y[i].v[j], sy);
-                        sh = fma2(hh[i].v[j], hh[i].v[j], sh);
-                        sa = add2(sa, aw);
-                        sx = fma2(aw, hh[i].v[j], sx);
-                        if (BIAS) dpre_b[i].v[j] = add2(dpre_b[i].v[j], dz[i].v[j]);
-                    }
+                for (int j = 0; j < 4; j++) {
+                    const F2 aw = mul2(dz.v[j], pre_w.v[j]);
+                    sy = fma2(y.v[j], y.v[j], sy);
+                    sh = fma2(hh.v[j], hh.v[j], sh);
+                    sa = add2(sa, aw);
+                    sx = fma2(aw, hh.v[j], sx);
+                    if (BIAS) dpre_b.v[j] = add2(dpre_b.v[j], dz.v[j]);
+                }
                 float s[4] = {both(sh), both(sy), both(sa), both(sx)};
                 sum(s);
                 if (post) ry = rsqrtf(fmaf(s[1], over_d, a.p.post_eps));
@@ -189,129 +162,107 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
                 const float r = rsqrtf(fmaf(s[0], over_d, a.p.pre_eps));
                 const F2 r2 = all2(r), ma = all2(pre_layer ? -s[2] * over_d : 0.f), mx = all2(-s[3] * r * over_d);
 #pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        const F2 xh = mul2(hh[i].v[j], r2);
-                        dpre_w[i].v[j] = fma2(dz[i].v[j], xh, dpre_w[i].v[j]);
-                        g[i].v[j] = fma2(r2, fma2(xh, mx, fma2(dz[i].v[j], pre_w[i].v[j], ma)), g[i].v[j]);
-                    }
+                for (int j = 0; j < 4; j++) {
+                    const F2 xh = mul2(hh.v[j], r2);
+                    dpre_w.v[j] = fma2(dz.v[j], xh, dpre_w.v[j]);
+                    g.v[j] = fma2(r2, fma2(xh, mx, fma2(dz.v[j], pre_w.v[j], ma)), g.v[j]);
+                }
             } else if (post) {
                 F2 sy = all2(0.f);
 #pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) sy = fma2(y[i].v[j], y[i].v[j], sy);
+                for (int j = 0; j < 4; j++) sy = fma2(y.v[j], y.v[j], sy);
                 float s[1] = {both(sy)};
                 sum(s);
                 ry = rsqrtf(fmaf(s[0], over_d, a.p.post_eps));
             }
             if (a.dh) {
-                const F2 alpha = all2(a.p.alpha);
-#pragma unroll
-                for (int i = 0; i < V; i++) {
-                    Run out;
-#pragma unroll
-                    for (int j = 0; j < 4; j++) out.v[j] = mul2(alpha, g[i].v[j]);
-                    store_run<TS, L>(static_cast<TS *>(a.dh) + n * D, D, i, t, NT, out);
-                }
+                Run out = all_run(a.p.alpha);
+                times(out, g);
+                store_run<TS, L>(static_cast<TS *>(a.dh) + n * D, D, 0, t, 0, out);
             }
             const F2 ry2 = all2(ry);
             if constexpr (GATE == OF_TOKENS) {
+                const Run gate = load_const<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, 0, t, 0);
+                if (a.g.dgate) {   // scale t dH
+                    Run d = y;
+                    if (post) {
 #pragma unroll
-                for (int i = 0; i < V; i++) {
-                    const Run gate = load_const<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, i, t, NT);
-                    if (a.g.dgate) {   // scale t dH
-                        Run d = y[i];
-                        if (post) {
-#pragma unroll
-                            for (int j = 0; j < 4; j++) d.v[j] = mul2(d.v[j], ry2);
-                        }
-                        if (a.p.post_w) times(d, load_const<float, L>(a.p.post_w, D, i, t, NT));
-                        if (a.p.post_b) {
-                            const Run b = load_const<float, L>(a.p.post_b, D, i, t, NT);
-#pragma unroll
-                            for (int j = 0; j < 4; j++) d.v[j] = add2(d.v[j], b.v[j]);
-                        }
-                        if (a.p.scale) times(d, load_const<float, L>(a.p.scale, D, i, t, NT));
-                        times(d, g[i]);
-                        store_run<TB, L>(static_cast<TB *>(a.g.dgate) + n * D, D, i, t, NT, d);
+                        for (int j = 0; j < 4; j++) d.v[j] = mul2(d.v[j], ry2);
                     }
-                    times(g[i], gate);
+                    if (a.p.post_w) times(d, load_const<float, L>(a.p.post_w, D, 0, t, 0));
+                    if (a.p.post_b) {
+                        const Run b = load_const<float, L>(a.p.post_b, D, 0, t, 0);
+#pragma unroll
+                        for (int j = 0; j < 4; j++) d.v[j] = add2(d.v[j], b.v[j]);
+                    }
+                    if (a.p.scale) times(d, load_const<float, L>(a.p.scale, D, 0, t, 0));
+                    times(d, g);
+                    store_run<TB, L>(static_cast<TB *>(a.g.dgate) + n * D, D, 0, t, 0, d);
                 }
+                times(g, gate);
             }
             F2 sc = all2(0.f), sx = all2(0.f);
 #pragma unroll
-            for (int i = 0; i < V; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const F2 yh = post ? mul2(y[i].v[j], ry2) : y[i].v[j];
-                    Q[i].v[j] = fma2(g[i].v[j], yh, Q[i].v[j]);
-                    if (BIAS) S[i].v[j] = add2(S[i].v[j], g[i].v[j]);
-                    const F2 c = mul2(g[i].v[j], wc[i].v[j]);
-                    if (post) {
-                        sc = add2(sc, c);
-                        sx = fma2(c, yh, sx);
-                    }
-                    g[i].v[j] = c;
-                    y[i].v[j] = yh;
+            for (int j = 0; j < 4; j++) {
+                const F2 yh = post ? mul2(y.v[j], ry2) : y.v[j];
+                Q.v[j] = fma2(g.v[j], yh, Q.v[j]);
+                if (BIAS) S.v[j] = add2(S.v[j], g.v[j]);
+                const F2 c = mul2(g.v[j], wc.v[j]);
+                if (post) {
+                    sc = add2(sc, c);
+                    sx = fma2(c, yh, sx);
                 }
+                g.v[j] = c;
+                y.v[j] = yh;
+            }
             if (post) {
                 float s[2] = {both(sc), both(sx)};
                 sum(s);
                 const F2 mc = all2(post_layer ? -s[0] * over_d : 0.f), mx = all2(-s[1] * over_d);
 #pragma unroll
-                for (int i = 0; i < V; i++)
-#pragma unroll
-                    for (int j = 0; j < 4; j++) g[i].v[j] = mul2(ry2, fma2(y[i].v[j], mx, add2(g[i].v[j], mc)));
+                for (int j = 0; j < 4; j++) g.v[j] = mul2(ry2, fma2(y.v[j], mx, add2(g.v[j], mc)));
             }
-            if (a.dy) {
-#pragma unroll
-                for (int i = 0; i < V; i++) store_run<TB, L>(static_cast<TB *>(a.dy) + n * D, D, i, t, NT, g[i]);
-            }
+            if (a.dy) store_run<TB, L>(static_cast<TB *>(a.dy) + n * D, D, 0, t, 0, g);
         }
         if (GATE == OF_RUNS || later < 0) {   // what the unit (else: all of the worker's) adds to the gradients
             float *const out = args.sums + worker * kSums * D;
+            Run w = all_run(1.f), b = all_run(0.f), scale = all_run(1.f), gate = all_run(1.f), P, R;
+            if (a.p.post_w) w = load_const<float, L>(a.p.post_w, D, 0, t, 0);
+            if (a.p.post_b) b = load_const<float, L>(a.p.post_b, D, 0, t, 0);
+            if (a.p.scale) scale = load_const<float, L>(a.p.scale, D, 0, t, 0);
+            if (gate_row) gate = load_const<TB, L>(gate_row, D, 0, t, 0);
 #pragma unroll
-            for (int i = 0; i < V; i++) {
-                Run w = all_run(1.f), b = all_run(0.f), scale = all_run(1.f), gate = all_run(1.f), P, R;
-                if (a.p.post_w) w = load_const<float, L>(a.p.post_w, D, i, t, NT);
-                if (a.p.post_b) b = load_const<float, L>(a.p.post_b, D, i, t, NT);
-                if (a.p.scale) scale = load_const<float, L>(a.p.scale, D, i, t, NT);
-                if (gate_row) gate = load_const<TB, L>(gate_row, D, i, t, NT);
+            for (int j = 0; j < 4; j++) P.v[j] = fma2(w.v[j], Q.v[j], mul2(b.v[j], S.v[j]));
+            Run sg = scale;
+            times(sg, gate);
+            // dscale gate P, dpost_w scale gate Q, dpost_b scale gate S
 #pragma unroll
-                for (int j = 0; j < 4; j++) P.v[j] = fma2(w.v[j], Q[i].v[j], mul2(b.v[j], S[i].v[j]));
-                Run sg = scale;
-                times(sg, gate);
-                // dscale gate P, dpost_w scale gate Q, dpost_b scale gate S
+            for (int k = 0; k < 3; k++) {
+                R = k == 0 ? P : k == 1 ? Q : S;
+                times(R, k == 0 ? gate : sg);
+                if (GATE == OF_RUNS) {
 #pragma unroll
-                for (int k = 0; k < 3; k++) {
-                    R = k == 0 ? P : k == 1 ? Q[i] : S[i];
-                    times(R, k == 0 ? gate : sg);
-                    if (GATE == OF_RUNS) {
-#pragma unroll
-                        for (int h = 0; h < 2; h++) {
-                            float4 &s = unit_sum(k, i, h);
-                            const float4 old = s;
-                            R.v[2 * h] = add2(R.v[2 * h], pack2(old.x, old.y));
-                            R.v[2 * h + 1] = add2(R.v[2 * h + 1], pack2(old.z, old.w));
-                            const float2 lo = unpack2(R.v[2 * h]), hi = unpack2(R.v[2 * h + 1]);
-                            s = make_float4(lo.x, lo.y, hi.x, hi.y);
-                        }
+                    for (int h = 0; h < 2; h++) {
+                        float4 &s = unit_sum(k, h);
+                        const float4 old = s;
+                        R.v[2 * h] = add2(R.v[2 * h], pack2(old.x, old.y));
+                        R.v[2 * h + 1] = add2(R.v[2 * h + 1], pack2(old.z, old.w));
+                        const float2 lo = unpack2(R.v[2 * h]), hi = unpack2(R.v[2 * h + 1]);
+                        s = make_float4(lo.x, lo.y, hi.x, hi.y);
                     }
-                    if (later < 0 && (k == 0 ? a.g.dscale : k == 1 ? a.g.dpost_w : a.g.dpost_b)) store_run<float, L>(out + k * D, D, i, t, NT, R);
                 }
-                if (gate_row && a.g.dgate) {
-                    times(P, scale);
-                    if (args.gate_sums) store_run<float, L>(args.gate_sums + u * D, D, i, t, NT, P);
-                    else store_run<TB, L>(static_cast<TB *>(a.g.dgate) + row * D, D, i, t, NT, P);
-                }
-                if (later < 0) {
-                    if (a.g.dpre_w) store_run<float, L>(out + 3 * D, D, i, t, NT, dpre_w[i]);
-                    if (a.g.dpre_b) store_run<float, L>(out + 4 * D, D, i, t, NT, dpre_b[i]);
-                }
+                if (later < 0 && (k == 0 ? a.g.dscale : k == 1 ? a.g.dpost_w : a.g.dpost_b)) store_run<float, L>(out + k * D, D, 0, t, 0, R);
             }
-            zero(Q), zero(S);
+            if (gate_row && a.g.dgate) {
+                times(P, scale);
+                if (args.gate_sums) store_run<float, L>(args.gate_sums + u * D, D, 0, t, 0, P);
+                else store_run<TB, L>(static_cast<TB *>(a.g.dgate) + row * D, D, 0, t, 0, P);
+            }
+            if (later < 0) {
+                if (a.g.dpre_w) store_run<float, L>(out + 3 * D, D, 0, t, 0, dpre_w);
+                if (a.g.dpre_b) store_run<float, L>(out + 4 * D, D, 0, t, 0, dpre_b);
+            }
+            Q = S = all_run(0.f);
         }
     }
 }
@@ -362,28 +313,35 @@ __global__ void __launch_bounds__(1024) k_residual_norm_sums(const __grid_consta
     }
 }
 
-// Backward: runs of eight and threads of a group, and groups of a CTA.
+// Backward: CTAs to a row, threads of one that work on it, and rows of a CTA. A
+// thread has eight features: with sixteen, a row to a CTA, the sums did not fit its
+// registers (2000 x 8192 bf16 122 us, so 109; 1000 x 16384, a bf16 block on an fp32
+// stream, 349, so 143). More and smaller CTAs pay more for each other's sums (CTAs of
+// 256 threads: 112 and 238).
 struct RnShape {
-    int V, NT, R;
+    int C, NT, R;
 };
 RnShape shape_of(int64_t D) {
     RnShape s;
-    s.V = D > 4096 ? 2 : 1;
-    s.NT = (int)((D + 8 * s.V - 1) / (8 * s.V) + 31) / 32 * 32;
+    s.C = D > 8192 ? 4 : D > 4096 ? 2 : 1;
+    s.NT = (int)((D + 8 * s.C - 1) / (8 * s.C) + 31) / 32 * 32;
     s.R = s.NT == 32 ? 4 : s.NT == 64 ? 2 : 1;
     return s;
 }
 
 bool any_sum(const bsr_residual_norm_grads_t &g) { return g.dscale || g.dpost_w || g.dpost_b || g.dpre_w || g.dpre_b; }
 
-// Whether the gate has a row for each token (wide rows have no kernel for it: runs of one).
-bool of_tokens(const bsr_residual_norm_t &p) { return p.gate_tokens == 1 && shape_of(p.D).V == 1; }
+// Whether the gate has a row for each token.
+bool of_tokens(const bsr_residual_norm_t &p) { return p.gate_tokens == 1; }
 
 RnSplit split_of(const bsr_residual_norm_t &p, int64_t N) {
     const RnShape sh = shape_of(p.D);
-    // groups that an SM holds at once, by the backward kernel's registers
-    // (128 a thread, and warps are given them four at a time)
-    const int64_t most = (int64_t)sm_count() * std::max(1, 512 / ((sh.NT * sh.R + 127) / 128 * 128)) * sh.R;
+    // groups that run at once, by the backward kernel's registers (128 a thread, and
+    // warps are given them four at a time); clusters of four do not fill all parts of
+    // the GPU (36 of 38)
+    const int64_t sms = sm_count();
+    const int64_t most = sh.C == 1 ? sms * std::max(1, 512 / ((sh.NT * sh.R + 127) / 128 * 128)) * sh.R
+                                   : std::max<int64_t>(1, sh.C == 2 ? sms / 2 : sms / 4 * 15 / 16);
     RnSplit s;
     s.span = p.gate_tokens > 0 && !of_tokens(p) ? std::min<int64_t>(p.gate_tokens, N) : N;
     const int64_t rows = (N + s.span - 1) / s.span, len = std::max<int64_t>(1, (N + most - 1) / most);
@@ -404,41 +362,43 @@ cudaError_t backward(const RnBackward &b, cudaStream_t s) {
     a.sums = b.ws;
     a.gate_sums = b.gate && b.g.dgate && !tokens && a.split.slices > 1 ? b.ws + a.split.workers * kSums * b.p.D : nullptr;
     const RnShape sh = shape_of(b.p.D);
-    const int L = layout_of(b.p, sh.V, sh.NT), threads = sh.NT * sh.R;
-    const dim3 block(sh.NT, sh.R), grid((unsigned)((a.split.workers + sh.R - 1) / sh.R));
+    const int L = layout_of(b.p, sh.C, sh.NT), threads = sh.NT * sh.R;
+    const dim3 block(sh.NT, sh.R), grid((unsigned)((a.split.workers + sh.R - 1) / sh.R * sh.C));
+    a.ctas = sh.C;
     const bool gate = b.gate, bias = b.p.post_b || b.p.pre_b;
     // a kernel of its own for what is common: without a gate, and full rows without a bias
     using K = void (*)(RnBackwardArgs);
     K kernel;
-    if (tokens && sh.V == 1) {
-        kernel = threads <= 128 ? (L == FULL   ? k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_TOKENS, true>
-                                   : L == RUNS ? k_residual_norm_backward<TB, TS, 1, RUNS, 128, OF_TOKENS, true>
-                                               : k_residual_norm_backward<TB, TS, 1, ANY, 128, OF_TOKENS, true>)
-                                : (L != ANY ? k_residual_norm_backward<TB, TS, 1, RUNS, 512, OF_TOKENS, true>
-                                                : k_residual_norm_backward<TB, TS, 1, ANY, 512, OF_TOKENS, true>);
-    } else if (sh.V == 1 && threads <= 128) {
+    if (sh.C > 1) {
+        kernel = tokens ? (L == ANY ? k_residual_norm_backward<TB, TS, ANY, 512, OF_TOKENS, true, true>
+                                    : k_residual_norm_backward<TB, TS, RUNS, 512, OF_TOKENS, true, true>)
+                        : (L == ANY ? k_residual_norm_backward<TB, TS, ANY, 512, OF_RUNS, true, true>
+                                    : k_residual_norm_backward<TB, TS, RUNS, 512, OF_RUNS, true, true>);
+    } else if (tokens) {
+        kernel = threads <= 128 ? (L == FULL   ? k_residual_norm_backward<TB, TS, FULL, 128, OF_TOKENS, true, false>
+                                   : L == RUNS ? k_residual_norm_backward<TB, TS, RUNS, 128, OF_TOKENS, true, false>
+                                               : k_residual_norm_backward<TB, TS, ANY, 128, OF_TOKENS, true, false>)
+                                : (L != ANY ? k_residual_norm_backward<TB, TS, RUNS, 512, OF_TOKENS, true, false>
+                                            : k_residual_norm_backward<TB, TS, ANY, 512, OF_TOKENS, true, false>);
+    } else if (threads <= 128) {
         if (L == FULL)
-            kernel = gate ? (bias ? k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 1, FULL, 128, OF_RUNS, false>)
-                          : (bias ? k_residual_norm_backward<TB, TS, 1, FULL, 128, NONE, true> : k_residual_norm_backward<TB, TS, 1, FULL, 128, NONE, false>);
+            kernel = gate ? (bias ? k_residual_norm_backward<TB, TS, FULL, 128, OF_RUNS, true, false> : k_residual_norm_backward<TB, TS, FULL, 128, OF_RUNS, false, false>)
+                          : (bias ? k_residual_norm_backward<TB, TS, FULL, 128, NONE, true, false> : k_residual_norm_backward<TB, TS, FULL, 128, NONE, false, false>);
         else if (L == RUNS)
-            kernel = gate ? k_residual_norm_backward<TB, TS, 1, RUNS, 128, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 1, RUNS, 128, NONE, true>;
+            kernel = gate ? k_residual_norm_backward<TB, TS, RUNS, 128, OF_RUNS, true, false> : k_residual_norm_backward<TB, TS, RUNS, 128, NONE, true, false>;
         else
-            kernel = k_residual_norm_backward<TB, TS, 1, ANY, 128, OF_RUNS, true>;
-    } else if (sh.V == 1) {
-        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 1, ANY, 512, OF_RUNS, true>
-                 : gate       ? k_residual_norm_backward<TB, TS, 1, RUNS, 512, OF_RUNS, true>
-                              : k_residual_norm_backward<TB, TS, 1, RUNS, 512, NONE, true>;
-    } else if (threads <= 512) {
-        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 2, ANY, 512, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 512, OF_RUNS, true>;
+            kernel = k_residual_norm_backward<TB, TS, ANY, 128, OF_RUNS, true, false>;
     } else {
-        kernel = L == ANY ? k_residual_norm_backward<TB, TS, 2, ANY, 1024, OF_RUNS, true> : k_residual_norm_backward<TB, TS, 2, RUNS, 1024, OF_RUNS, true>;
+        kernel = L == ANY ? k_residual_norm_backward<TB, TS, ANY, 512, OF_RUNS, true, false>
+                 : gate   ? k_residual_norm_backward<TB, TS, RUNS, 512, OF_RUNS, true, false>
+                          : k_residual_norm_backward<TB, TS, RUNS, 512, NONE, true, false>;
     }
-    const size_t smem = (size_t)threads * 3 * 2 * sh.V * 16;   // (up to 192 KB, at 16384 features)
+    const size_t smem = (size_t)threads * 3 * 2 * 16;   // (up to 48 KB)
     if (smem > 32 * 1024) {   // (beside 8 KB that every kernel has)
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
-    cudaError_t e = launch_kernel(kernel, grid, block, smem, s, a);
+    cudaError_t e = launch_clusters(kernel, sh.C, grid, block, smem, s, a);
     if (e != cudaSuccess || (!any_sum(b.g) && !a.gate_sums)) return e;
     int rows = 1;   // gate rows to a CTA: as many as leave a thread eight slices at most
     while (rows < 32 && 2 * rows * a.split.slices <= 256) rows *= 2;

@@ -236,6 +236,14 @@ def test_backward_tokens(N, gate, block, stream):
 
 
 @pytest.mark.parametrize("block,stream", TYPES)
+@pytest.mark.parametrize("D,gate", [(4104, 0), (5120, 30), (8192, 1), (8191, 16), (8200, 0), (12288, 64), (16384, 1), (16383, 50)])
+def test_backward_wide_rows(D, gate, block, stream):
+    # several rows to each group of threads that works on them
+    check_backward(*make(200, D, block, stream, "layer", "rms", gate=gate, scale=True))
+    check_backward(*make(151, D, block, stream, "rms", "layer", gate=gate, bias=False))
+
+
+@pytest.mark.parametrize("block,stream", TYPES)
 def test_gate_rows_longer_than_the_tokens_left(block, stream):
     # a last row of fewer tokens than the others, and one row for far more tokens than there are
     for N, gate in ((600, 512), (1030, 1024), (50, 2**63 - 1)):
