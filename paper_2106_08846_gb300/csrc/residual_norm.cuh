@@ -277,44 +277,59 @@ struct GroupSum {
     }
 };
 
-// Normalises a row in place.
-template <int V, int L, typename Sum>
-__device__ __forceinline__ void normalise(Run (&x)[V], int how, float eps, int D, float over_d, int t, int NT, Sum &sum) {
-    F2 s;
-    float one[1];
+__device__ __forceinline__ void times(Run &r, const Run &s) {
+#pragma unroll
+    for (int j = 0; j < 4; j++) r.v[j] = mul2(r.v[j], s.v[j]);
+}
+
+// Normalises rows in place.
+template <int V, int L, int ROWS, typename Sum>
+__device__ __forceinline__ void normalise(Run (&x)[ROWS][V], int how, float eps, int D, float over_d, int t, int NT, Sum &sum) {
+    float s[ROWS];
     if (how == BSR_NORM_LAYER) {
-        s = all2(0.f);
+#pragma unroll
+        for (int k = 0; k < ROWS; k++) {
+            F2 c = all2(0.f);
+#pragma unroll
+            for (int i = 0; i < V; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) c = add2(c, x[k][i].v[j]);
+            s[k] = both(c);
+        }
+        sum(s);
+#pragma unroll
+        for (int k = 0; k < ROWS; k++)
+#pragma unroll
+            for (int i = 0; i < V; i++) centre<L>(x[k][i], s[k] * over_d, D, i, t, NT);
+    }
+#pragma unroll
+    for (int k = 0; k < ROWS; k++) {
+        F2 c = all2(0.f);
 #pragma unroll
         for (int i = 0; i < V; i++)
 #pragma unroll
-            for (int j = 0; j < 4; j++) s = add2(s, x[i].v[j]);
-        one[0] = both(s);
-        sum(one);
-#pragma unroll
-        for (int i = 0; i < V; i++) centre<L>(x[i], one[0] * over_d, D, i, t, NT);
+            for (int j = 0; j < 4; j++) c = fma2(x[k][i].v[j], x[k][i].v[j], c);
+        s[k] = both(c);
     }
-    s = all2(0.f);
+    sum(s);
 #pragma unroll
-    for (int i = 0; i < V; i++)
+    for (int k = 0; k < ROWS; k++) {
+        const F2 r = all2(rsqrtf(fmaf(s[k], over_d, eps)));
 #pragma unroll
-        for (int j = 0; j < 4; j++) s = fma2(x[i].v[j], x[i].v[j], s);
-    one[0] = both(s);
-    sum(one);
-    const F2 r = all2(rsqrtf(fmaf(one[0], over_d, eps)));
+        for (int i = 0; i < V; i++)
 #pragma unroll
-    for (int i = 0; i < V; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++) x[i].v[j] = mul2(x[i].v[j], r);
+            for (int j = 0; j < 4; j++) x[k][i].v[j] = mul2(x[k][i].v[j], r);
+    }
 }
 // x * w + b with a parameter's row each, where there is one
-template <int V, int L>
-__device__ __forceinline__ void affine(Run (&x)[V], const float *w, const float *b, int D, int t, int NT) {
+template <int V, int L, int ROWS>
+__device__ __forceinline__ void affine(Run (&x)[ROWS][V], const float *w, const float *b, int D, int t, int NT) {
     if (w) {
 #pragma unroll
         for (int i = 0; i < V; i++) {
             const Run p = load_const<float, L>(w, D, i, t, NT);
 #pragma unroll
-            for (int j = 0; j < 4; j++) x[i].v[j] = mul2(x[i].v[j], p.v[j]);
+            for (int k = 0; k < ROWS; k++) times(x[k][i], p);
         }
     }
     if (b) {
@@ -322,7 +337,9 @@ __device__ __forceinline__ void affine(Run (&x)[V], const float *w, const float 
         for (int i = 0; i < V; i++) {
             const Run p = load_const<float, L>(b, D, i, t, NT);
 #pragma unroll
-            for (int j = 0; j < 4; j++) x[i].v[j] = add2(x[i].v[j], p.v[j]);
+            for (int k = 0; k < ROWS; k++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) x[k][i].v[j] = add2(x[k][i].v[j], p.v[j]);
         }
     }
 }

@@ -100,10 +100,6 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         r = all_run(absent);
         if (p) r = load_const<float, L>(p, D, 0, t, 0);
     };
-    auto times = [&](Run &r, const Run &s) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) r.v[j] = mul2(r.v[j], s.v[j]);
-    };
     Q = S = dpre_w = dpre_b = all_run(0.f);
     param(pre_w, a.p.pre_w, 1.f);
     if (GATE == OF_RUNS) {
