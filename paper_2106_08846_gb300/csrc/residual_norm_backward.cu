@@ -44,13 +44,13 @@ struct RnBackwardArgs {
     int ctas;           // to a row
 };
 
-// The four rows of a token as they lie in memory.
+// The rows of a token as they lie in memory; GATE: its own gate too.
 template <typename TB, typename TS, int L>
 struct Token {
-    Raw<TB, L> y, dz;
+    Raw<TB, L> y, dz, gate;
     Raw<TS, L> h, dh;
 };
-template <typename TB, typename TS, int L>
+template <bool GATE, typename TB, typename TS, int L>
 __device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, Token<TB, TS, L> &k) {
     const int64_t at = n * D;
     k.y = load_run<TB, L, false>(static_cast<const TB *>(a.y) + at, D, 0, t, 0);
@@ -59,6 +59,7 @@ __device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D
         k.h = load_run<TS, L, true>(static_cast<const TS *>(a.h_out) + at, D, 0, t, 0);
         k.dz = load_run<TB, L, false>(static_cast<const TB *>(a.dz) + at, D, 0, t, 0);
     }
+    if (GATE) k.gate = load_run<TB, L, true>(static_cast<const TB *>(a.gate) + at, D, 0, t, 0);
 }
 
 // What a unit of tokens of one gate row adds to the parameters' gradients follows
@@ -79,6 +80,10 @@ enum Gate : int { NONE = 0, OF_RUNS = 1, OF_TOKENS = 2 };
 template <typename TB, typename TS, int L, int THREADS, int GATE, bool BIAS, bool CLUSTER>
 __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_norm_backward(const __grid_constant__ RnBackwardArgs args) {
     constexpr bool KEEP = L != ANY || THREADS == 128;
+    // a token's own gate is on its way with its rows, but for fp32 streams of bf16 blocks
+    // and odd rows, where it would cost more spills than it hides (16384 x 1024 bf16 67.3
+    // us without, 62.8 with; 8000 x 2048 of a bf16 block on an fp32 stream 71.9 and 81.9)
+    constexpr bool GATE_AHEAD = GATE == OF_TOKENS && L != ANY && sizeof(TB) == sizeof(TS);
     extern __shared__ float4 unit_sums[];
     __shared__ float4 words[CLUSTER ? 2 : kMaxGroups][64];   // (CLUSTER: one group, and the CTAs' sums)
     const RnBackward &a = args.b;
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         return row * args.split.span + (u - row * args.split.slices) * args.split.len;
     };
     Token<TB, TS, L> next = {};
-    if (KEEP && worker < args.split.units && first_of(worker) < a.N) load_token<TB, TS, L>(a, first_of(worker), D, t, next);
+    if (KEEP && worker < args.split.units && first_of(worker) < a.N) load_token<GATE_AHEAD>(a, first_of(worker), D, t, next);
     for (int64_t u = worker; u < args.split.units; u += args.split.workers) {
         const int64_t row = u / args.split.slices, n0 = first_of(u);
         const int64_t n1 = min(min(n0 + args.split.len, (row + 1) * args.split.span), a.N);
@@ -123,10 +128,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         if (gate_row) times(wc, load_const<TB, L>(gate_row, D, 0, t, 0));
         if (a.p.post_w) times(wc, load_const<float, L>(a.p.post_w, D, 0, t, 0));
         for (int64_t n = n0; n < n1; n++) {
-            if (!KEEP) load_token<TB, TS, L>(a, n, D, t, next);
+            if (!KEEP) load_token<GATE_AHEAD>(a, n, D, t, next);
             Run y = next.y.run(), hh = next.h.run(), g = next.dh.run(), dz = next.dz.run();   // g: dH
+            Run gate;
+            if (GATE_AHEAD) gate = next.gate.run();
             const int64_t after = n + 1 < n1 ? n + 1 : later;
-            if (KEEP && after >= 0 && after < a.N) load_token<TB, TS, L>(a, after, D, t, next);
+            if (KEEP && after >= 0 && after < a.N) load_token<GATE_AHEAD>(a, after, D, t, next);
             if (post_layer || pre_layer) {
                 F2 sh = all2(0.f), sy = all2(0.f);
 #pragma unroll
@@ -178,7 +185,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
             }
             const F2 ry2 = all2(ry);
             if constexpr (GATE == OF_TOKENS) {
-                const Run gate = load_const<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, 0, t, 0);
+                if (!GATE_AHEAD) gate = load_const<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, 0, t, 0);
                 if (a.g.dgate) {   // scale t dH
                     Run d = y;
                     if (post) {
