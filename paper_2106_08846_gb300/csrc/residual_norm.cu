@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_residual_norm(const __grid_co
             for (int k = 0; k < ROWS; k++) {
                 if (ROWS > 1 && n + k >= a.N) break;
 #pragma unroll
-                for (int i = 0; i < V; i++) store_run<std::remove_pointer_t<decltype(to)>, L>(to + (n + k) * D, D, i, t, NT, x[k][i]);
+                for (int i = 0; i < V; i++) store_run<std::remove_pointer_t<decltype(to)>, L, THREADS / 32>(to + (n + k) * D, D, i, t, NT, x[k][i]);
             }
         };
         if (a.h_out) store(static_cast<TS *>(a.h_out));

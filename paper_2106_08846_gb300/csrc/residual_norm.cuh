@@ -129,27 +129,44 @@ template <typename T, int L>
 __device__ __forceinline__ Run load_const(const T *row, int D, int i, int t, int NT) {
     return load_run<T, L, true>(row, D, i, t, NT).run();
 }
-template <typename T, int L>
+// A warp's kilobyte of shared memory; WARPS: the most of a CTA.
+template <int WARPS>
+__device__ __forceinline__ float *stage() {
+    __shared__ float4 words[WARPS][64];
+    return reinterpret_cast<float *>(words[(threadIdx.y * blockDim.x + threadIdx.x) >> 5]);
+}
+// By whole warps. ANY: a warp's fp32 runs, which are contiguous, change lanes through
+// shared memory, so that an instruction's stores lie side by side: a lane's eight
+// values one by one cost a write of their 32-byte sector each (3000 x 771 fp32 30.0 us,
+// so 26.3). bf16 runs go in four stores and lose by the detour (5000 x 1193 32.3 and 34.9).
+template <typename T, int L, int WARPS>
 __device__ __forceinline__ void store_run(T *row, int D, int i, int t, int NT, const Run &r) {
-    if (!inside<L>(i, 0, t, NT, D)) return;
+    const int lane = threadIdx.x & 31, left = D - feature(i, 0, t, NT);   // values of the row from this lane's on
     T *const p = row + feature(i, 0, t, NT);
-    if constexpr (sizeof(T) == 4) {
-        float x[8];
+    if constexpr (sizeof(T) == 4 && L == ANY) {
+        const int all = left + 8 * lane;   // from the warp's first on
+        if (all <= 0) return;
+        float *const buf = stage<WARPS>();
+        __syncwarp();   // (the last run has been read)
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const float2 u = unpack2(r.v[j]);
-            x[2 * j] = u.x, x[2 * j + 1] = u.y;
+        for (int h = 0; h < 2; h++) {
+            const float2 u = unpack2(r.v[2 * h]), w = unpack2(r.v[2 * h + 1]);
+            reinterpret_cast<float4 *>(buf)[2 * lane + h] = make_float4(u.x, u.y, w.x, w.y);
         }
-        if constexpr (L != ANY) {
+        __syncwarp();
+        T *const first = p - 8 * lane;
 #pragma unroll
-            for (int h = 0; h < 2; h++) reinterpret_cast<float4 *>(p)[h] = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-        } else {
-            const int n = D - feature(i, 0, t, NT);
+        for (int j = 0; j < 8; j++)
+            if (32 * j + lane < all) first[32 * j + lane] = buf[32 * j + lane];
+    } else if constexpr (sizeof(T) == 4) {
+        if (!inside<L>(i, 0, t, NT, D)) return;
 #pragma unroll
-            for (int j = 0; j < 8; j++)
-                if (j < n) p[j] = x[j];
+        for (int h = 0; h < 2; h++) {
+            const float2 u = unpack2(r.v[2 * h]), w = unpack2(r.v[2 * h + 1]);
+            reinterpret_cast<float4 *>(p)[h] = make_float4(u.x, u.y, w.x, w.y);
         }
     } else {
+        if (!inside<L>(i, 0, t, NT, D)) return;
         uint32_t w[4];
 #pragma unroll
         for (int k = 0; k < 4; k++) {
@@ -158,21 +175,18 @@ __device__ __forceinline__ void store_run(T *row, int D, int i, int t, int NT, c
         }
         if constexpr (L != ANY) {
             *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else if (left < 8) {
+#pragma unroll
+            for (int j = 0; j < 8; j++)
+                if (j < left) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+        } else if (reinterpret_cast<uintptr_t>(p) & 2) {
+            p[0] = (uint16_t)w[0];
+#pragma unroll
+            for (int k = 0; k < 3; k++) *reinterpret_cast<uint32_t *>(p + 1 + 2 * k) = __funnelshift_r(w[k], w[k + 1], 16);
+            p[7] = (uint16_t)(w[3] >> 16);
         } else {
-            const int n = D - feature(i, 0, t, NT);
-            if (n < 8) {
 #pragma unroll
-                for (int j = 0; j < 8; j++)
-                    if (j < n) p[j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
-            } else if (reinterpret_cast<uintptr_t>(p) & 2) {
-                p[0] = (uint16_t)w[0];
-#pragma unroll
-                for (int k = 0; k < 3; k++) *reinterpret_cast<uint32_t *>(p + 1 + 2 * k) = __funnelshift_r(w[k], w[k + 1], 16);
-                p[7] = (uint16_t)(w[3] >> 16);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; k++) *reinterpret_cast<uint32_t *>(p + 2 * k) = w[k];
-            }
+            for (int k = 0; k < 4; k++) *reinterpret_cast<uint32_t *>(p + 2 * k) = w[k];
         }
     }
 }

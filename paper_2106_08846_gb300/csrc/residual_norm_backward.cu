@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
             if (a.dh) {
                 Run out = all_run(a.p.alpha);
                 times(out, g);
-                store_run<TS, L>(static_cast<TS *>(a.dh) + n * D, D, 0, t, 0, out);
+                store_run<TS, L, THREADS / 32>(static_cast<TS *>(a.dh) + n * D, D, 0, t, 0, out);
             }
             const F2 ry2 = all2(ry);
             if constexpr (GATE == OF_TOKENS) {
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
                     }
                     if (a.p.scale) times(d, load_const<float, L>(a.p.scale, D, 0, t, 0));
                     times(d, g);
-                    store_run<TB, L>(static_cast<TB *>(a.g.dgate) + n * D, D, 0, t, 0, d);
+                    store_run<TB, L, THREADS / 32>(static_cast<TB *>(a.g.dgate) + n * D, D, 0, t, 0, d);
                 }
                 times(g, gate);
             }
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
 #pragma unroll
                 for (int j = 0; j < 4; j++) g.v[j] = mul2(ry2, fma2(y.v[j], mx, add2(g.v[j], mc)));
             }
-            if (a.dy) store_run<TB, L>(static_cast<TB *>(a.dy) + n * D, D, 0, t, 0, g);
+            if (a.dy) store_run<TB, L, THREADS / 32>(static_cast<TB *>(a.dy) + n * D, D, 0, t, 0, g);
         }
         if (GATE == OF_RUNS || later < 0) {   // what the unit (else: all of the worker's) adds to the gradients
             float *const out = args.sums + worker * kSums * D;
@@ -254,16 +254,16 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
                         s = make_float4(lo.x, lo.y, hi.x, hi.y);
                     }
                 }
-                if (later < 0 && (k == 0 ? a.g.dscale : k == 1 ? a.g.dpost_w : a.g.dpost_b)) store_run<float, L>(out + k * D, D, 0, t, 0, R);
+                if (later < 0 && (k == 0 ? a.g.dscale : k == 1 ? a.g.dpost_w : a.g.dpost_b)) store_run<float, L, THREADS / 32>(out + k * D, D, 0, t, 0, R);
             }
             if (gate_row && a.g.dgate) {
                 times(P, scale);
-                if (args.gate_sums) store_run<float, L>(args.gate_sums + u * D, D, 0, t, 0, P);
-                else store_run<TB, L>(static_cast<TB *>(a.g.dgate) + row * D, D, 0, t, 0, P);
+                if (args.gate_sums) store_run<float, L, THREADS / 32>(args.gate_sums + u * D, D, 0, t, 0, P);
+                else store_run<TB, L, THREADS / 32>(static_cast<TB *>(a.g.dgate) + row * D, D, 0, t, 0, P);
             }
             if (later < 0) {
-                if (a.g.dpre_w) store_run<float, L>(out + 3 * D, D, 0, t, 0, dpre_w);
-                if (a.g.dpre_b) store_run<float, L>(out + 4 * D, D, 0, t, 0, dpre_b);
+                if (a.g.dpre_w) store_run<float, L, THREADS / 32>(out + 3 * D, D, 0, t, 0, dpre_w);
+                if (a.g.dpre_b) store_run<float, L, THREADS / 32>(out + 4 * D, D, 0, t, 0, dpre_b);
             }
             Q = S = all_run(0.f);
         }
@@ -397,7 +397,7 @@ cudaError_t backward(const RnBackward &b, cudaStream_t s) {
                           : k_residual_norm_backward<TB, TS, RUNS, 512, NONE, true, false>;
     }
     const size_t smem = (size_t)threads * 3 * 2 * 16;   // (up to 48 KB)
-    if (smem > 32 * 1024) {   // (beside 8 KB that every kernel has)
+    if (smem > 24 * 1024) {   // (beside up to 24 KB that a kernel has)
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
