@@ -13,7 +13,7 @@
 //   warps 4 ..     epilogue, 16 (fp32: 8) warps: 32 rows and a share of the
 //                  columns each, straight from tensor memory to global memory
 //
-// A step is 512 SM cycles of MMAs at 256 columns (fp32: 3072). Waiting for a
+// A step is 512 SM cycles of MMAs at 256 columns (fp32: six times that). Waiting for a
 // stage, its loads and moving on take a producer about 750 cycles, so one warp
 // for A and one for B were the bound (8192 tokens of 1024 features into 4096,
 // bf16: 95 us, the MMAs 62). Stages of 128 columns were too few to cover the
