@@ -84,6 +84,17 @@ __device__ __forceinline__ Run all_run(float x) {
     for (int j = 0; j < 4; j++) r.v[j] = all2(x);
     return r;
 }
+// x in run i of a row, 0 past the row's end.
+template <int L>
+__device__ __forceinline__ Run row_run(float x, int D, int i, int t, int NT) {
+    Run r = all_run(inside<L>(i, 0, t, NT, D) ? x : 0.f);
+    if constexpr (L == ANY) {
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+            r.v[j] = pack2(inside<L>(i, 2 * j, t, NT, D) ? x : 0.f, inside<L>(i, 2 * j + 1, t, NT, D) ? x : 0.f);
+    }
+    return r;
+}
 
 // Run i of a row; 0 past the row's end. CONST: of an array that the kernel does not
 // write (a row that it may write is read once: the parameters keep their place in L1).

@@ -101,12 +101,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
     // dscale, dpost_w, dpost_b (k)
     float4 *const mine_s = unit_sums + (size_t)threadIdx.y * 3 * 2 * NT + threadIdx.x;
     auto unit_sum = [&](int k, int h) -> float4 & { return mine_s[(k * 2 + h) * NT]; };
-    auto param = [&](Run &r, const float *p, float absent) {
-        r = all_run(absent);
-        if (p) r = load_const<float, L>(p, D, 0, t, 0);
+    // a parameter, 1 where there is none; past the row's end 0: dH is not 0 there, but
+    // what the LayerNorm's gradient takes out of the row, which no sum may take in again
+    auto param = [&](Run &r, const float *p) {
+        r = p ? load_const<float, L>(p, D, 0, t, 0) : row_run<L>(1.f, D, 0, t, 0);
     };
     Q = S = dpre_w = dpre_b = all_run(0.f);
-    param(pre_w, a.p.pre_w, 1.f);
+    param(pre_w, a.p.pre_w);
     if (GATE == OF_RUNS) {
 #pragma unroll
         for (int k = 0; k < 3; k++) unit_sum(k, 0) = unit_sum(k, 1) = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -124,7 +125,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         const int64_t n1 = min(min(n0 + args.split.len, (row + 1) * args.split.span), a.N);
         const int64_t later = u + args.split.workers < args.split.units ? first_of(u + args.split.workers) : -1;
         const TB *const gate_row = GATE == OF_RUNS && a.gate ? static_cast<const TB *>(a.gate) + row * D : nullptr;
-        param(wc, a.p.scale, 1.f);
+        param(wc, a.p.scale);
         if (gate_row) times(wc, load_const<TB, L>(gate_row, D, 0, t, 0));
         if (a.p.post_w) times(wc, load_const<float, L>(a.p.post_w, D, 0, t, 0));
         for (int64_t n = n0; n < n1; n++) {
