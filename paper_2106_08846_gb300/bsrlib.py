@@ -4,6 +4,9 @@ Argument marshalling only: every step of the product and of the BSR
 conversion runs in libbsr_gb300.so. torch supplies device memory, streams and
 tensors; tensors cross as ``data_ptr()`` and streams as their ``cuda_stream``.
 There is no CPU fallback: if the library is missing, loading raises.
+With a `stream` other than the current one, outputs that a call makes itself are
+made on the current stream and written after what it still does; they may be used
+there once it has waited for `stream`.
 """
 from __future__ import annotations
 
@@ -161,6 +164,38 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _stream_object(stream, device):
+    """The torch stream of a call's `stream` argument (a Stream, or its handle as a number)."""
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(int(stream), device=device) if int(stream) else torch.cuda.default_stream(device)
+
+
+def _lend(stream, device, *tensors) -> None:
+    """Lets `stream` write tensors that a call has just made. Their memory is the
+    current stream's: work of the call waits for what that stream still does with
+    it, and it is handed out again only after the call's work."""
+    if stream is None:
+        return
+    s, current = _stream_object(stream, device), torch.cuda.current_stream(device)
+    if s.cuda_stream == current.cuda_stream:
+        return
+    s.wait_stream(current)
+    for t in tensors:
+        t.record_stream(s)
+
+
+def _workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
+    """Scratch of one call, from torch's allocator and of the call's own stream: it
+    waits for nobody else, and is handed out again only to later work of that stream."""
+    if nbytes == 0:
+        return None
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_stream_object(stream, device)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def dtype_code(dtype: torch.dtype) -> int:
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}: float32 or bfloat16")
@@ -184,12 +219,14 @@ def bsr_from_dense(W: torch.Tensor, R: int, C: int, threshold: float = 0.0, stre
     indptr = torch.empty(M // R + 1, dtype=torch.int32, device=W.device)
     nnzb = ctypes.c_int64(0)
     s = _stream(stream)
+    _lend(stream, W.device, indptr)
     _check(lib.bsr_from_dense(_ptr(W), M, K, R, C, threshold, dt, _ptr(indptr), None, None, 0,
                               ctypes.byref(nnzb), s), "bsr_from_dense(query)")
     n = nnzb.value
     indices = torch.empty(max(n, 0), dtype=torch.int32, device=W.device)
     data = torch.empty((max(n, 0), R, C), dtype=W.dtype, device=W.device)
     if n > 0:
+        _lend(stream, W.device, indices, data)
         _check(lib.bsr_from_dense(_ptr(W), M, K, R, C, threshold, dt, _ptr(indptr), _ptr(indices),
                                   _ptr(data), n, ctypes.byref(nnzb), s), "bsr_from_dense")
     return indptr, indices, data
@@ -214,6 +251,8 @@ class Handle:
         if Y is None:
             Y = torch.empty((X.shape[0], self.M), dtype=X.dtype, device=X.device,
                             pin_memory=not X.is_cuda)
+            if X.is_cuda:
+                _lend(stream, X.device, Y)
         bsr_spmm(self, X, bias, Y, X.shape[0], stream)
         return Y
 
@@ -415,18 +454,6 @@ def bsr_destroy(h: Handle) -> None:
     h.destroy()
 
 
-def _workspace(nbytes: int, device, stream) -> Optional[torch.Tensor]:
-    """Scratch of one call, from torch's allocator: handed out again only to work that comes after the call on its stream."""
-    if nbytes == 0:
-        return None
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
-        ws.record_stream(s)
-        s.wait_stream(torch.cuda.current_stream(device))   # (its last user may still be at work there)
-    return ws
-
-
 def _check_rows(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype) -> None:
     if t is None:
         return
@@ -481,13 +508,18 @@ def bsr_residual_norm(y: torch.Tensor, h: Optional[torch.Tensor] = None, *, gate
     dt, shape = y.dtype, y.shape
     st = (h if h is not None else h_out if h_out is not None else y).dtype
     p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
+    made = []
     if h_out is None:
         h_out = torch.empty(shape, dtype=st, device=y.device)
+        made.append(h_out)
     if z is None and pre != "none":
         z = torch.empty_like(y)
+        made.append(z)
     if not (y.is_contiguous() and _is_rows(h, shape, st) and _is_rows(h_out, shape, st) and _is_rows(z, shape, dt)):
         for name, t, d in (("y", y, dt), ("h", h, st), ("h_out", h_out, st), ("z", z, dt)):
             _check_rows(name, t, shape, d)
+    if made:
+        _lend(stream, y.device, *made)
     status = (_lib or load()).bsr_residual_norm(p, y.data_ptr(), None if h is None else h.data_ptr(),
                                                 None if gate is None else gate.data_ptr(), h_out.data_ptr(),
                                                 None if z is None else z.data_ptr(), shape[0], _stream(stream))
@@ -510,10 +542,13 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
     dt, shape, device = y.dtype, y.shape, y.device
     st = next((t.dtype for t in (h_out, dh_out, dh) if t is not None), dt)
     p = _residual_norm(y, st, gate, gate_tokens, scale, alpha, post, post_w, post_b, pre, pre_w, pre_b, eps, pre_eps)
+    made = []
     if dy is None:
         dy = torch.empty_like(y)
+        made.append(dy)
     if dh is None:
         dh = torch.empty(shape, dtype=st, device=device)
+        made.append(dh)
     if not (y.is_contiguous() and _is_rows(h_out, shape, st) and _is_rows(dh_out, shape, st) and _is_rows(dz, shape, dt)
             and _is_rows(dy, shape, dt) and _is_rows(dh, shape, st)):
         for name, t, d in (("y", y, dt), ("h_out", h_out, st), ("dh_out", dh_out, st), ("dz", dz, dt), ("dy", dy, dt),
@@ -527,6 +562,7 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
             ptrs.append(None)
         else:   # (an allocation each: rows of one, as views, take the host twice as long)
             out[name] = d = torch.empty_like(w)
+            made.append(d)
             ptrs.append(d.data_ptr())
     grads = _ResidualNormGrads(*ptrs)
     lib, n = _lib or load(), ctypes.c_size_t(0)
@@ -534,6 +570,8 @@ def bsr_residual_norm_backward(y: torch.Tensor, h_out: Optional[torch.Tensor], d
     if status:
         _check(status, "bsr_residual_norm_workspace")
     ws = _workspace(n.value, device, stream)
+    if made:
+        _lend(stream, device, *made)
     status = lib.bsr_residual_norm_backward(p, y.data_ptr(), _ptr(h_out), None if gate is None else gate.data_ptr(),
                                             _ptr(dh_out), _ptr(dz), dy.data_ptr(), dh.data_ptr(), grads, shape[0], _ptr(ws),
                                             n.value, _stream(stream))
@@ -577,6 +615,7 @@ def bsr_gated(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: Optional[
     N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
     if H is None:
         H = torch.empty((N, F), dtype=X.dtype, device=X.device)
+        _lend(stream, X.device, H)
     elif not _is_rows(H, (N, F), X.dtype):
         _check_rows("H", H, (N, F), X.dtype)
     ws, n = _gated_workspace(N, F, K, dt, 0, X.device, stream)
@@ -597,9 +636,16 @@ def bsr_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: 
     nothing is kept from the forward call."""
     N, F, K, dt = _check_gated(X, Wg, Wu, bg, bu, act)
     xt, w = X.dtype, Wg.shape
-    dX = torch.empty_like(X) if dX is None else dX
-    dWg = torch.empty_like(Wg) if dWg is None else dWg
-    dWu = torch.empty_like(Wu) if dWu is None else dWu
+    made = []
+    if dX is None:
+        dX = torch.empty_like(X)
+        made.append(dX)
+    if dWg is None:
+        dWg = torch.empty_like(Wg)
+        made.append(dWg)
+    if dWu is None:
+        dWu = torch.empty_like(Wu)
+        made.append(dWu)
     if not (_is_rows(dH, (N, F), xt) and _is_rows(dX, X.shape, xt) and _is_rows(dWg, w, xt) and _is_rows(dWu, w, xt)):
         for name, t, shape in (("dH", dH, (N, F)), ("dX", dX, X.shape), ("dWg", dWg, w), ("dWu", dWu, w)):
             _check_rows(name, t, shape, xt)
@@ -607,6 +653,9 @@ def bsr_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: 
     for name, b in (("dbg", bg), ("dbu", bu)):
         if b is not None:
             out[name] = torch.empty_like(b)
+            made.append(out[name])
+    if made:
+        _lend(stream, X.device, *made)
     ws, n = _gated_workspace(N, F, K, dt, 1, X.device, stream)
     status = _lib.bsr_gated_backward(X.data_ptr(), Wg.data_ptr(), Wu.data_ptr(), _ptr(bg), _ptr(bu), dH.data_ptr(),
                                      dX.data_ptr(), dWg.data_ptr(), dWu.data_ptr(), _ptr(out.get("dbg")),
