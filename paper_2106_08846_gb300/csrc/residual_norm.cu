@@ -54,12 +54,12 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_residual_norm(const __grid_co
 #pragma unroll
             for (int k = 0; k < ROWS; k++)
 #pragma unroll
-                for (int i = 0; i < V; i++) y[k][i] = load_run<TB, L, false>(static_cast<const TB *>(a.y) + row_of(k) * D, D, i, t, NT);
+                for (int i = 0; i < V; i++) y[k][i] = load_run<TB, L, false>(static_cast<const TB *>(a.y) + row_of(k) * D, D, i, t, NT, row_at_end<L>(a.N - 1 - row_of(k), D));
             if (a.h) {
 #pragma unroll
                 for (int k = 0; k < ROWS; k++)
 #pragma unroll
-                    for (int i = 0; i < V; i++) h[k][i] = load_run<TS, L, false>(static_cast<const TS *>(a.h) + row_of(k) * D, D, i, t, NT);
+                    for (int i = 0; i < V; i++) h[k][i] = load_run<TS, L, false>(static_cast<const TS *>(a.h) + row_of(k) * D, D, i, t, NT, row_at_end<L>(a.N - 1 - row_of(k), D));
             }
             if (n + ahead < a.N) {
                 const int64_t at = (n + ahead) * D;
@@ -83,12 +83,14 @@ __global__ void __launch_bounds__(THREADS, CTAS) k_residual_norm(const __grid_co
             auto gate_of = [&](int64_t row) {
                 return a.N >> 32 ? row / a.p.gate_tokens : (int64_t)((uint32_t)row / (uint32_t)a.p.gate_tokens);
             };
+            const int64_t gates = L == ANY ? gate_of(a.N - 1) + 1 : 0;   // the gate's rows
             const int64_t first = gate_of(row_of(0)), last = ROWS == 1 ? first : gate_of(row_of(ROWS - 1));
 #pragma unroll
             for (int i = 0; i < V; i++) {
-                const Run p = load_const<TB, L>(gate + first * D, D, i, t, NT);
+                const Run p = load_gate<TB, L>(gate + first * D, D, i, t, NT, row_at_end<L>(gates - 1 - first, D));
                 times(x[0][i], p);
-                if (ROWS == 2) times(x[ROWS - 1][i], last == first ? p : load_const<TB, L>(gate + last * D, D, i, t, NT));
+                if (ROWS == 2)
+                    times(x[ROWS - 1][i], last == first ? p : load_gate<TB, L>(gate + last * D, D, i, t, NT, row_at_end<L>(gates - 1 - last, D)));
             }
         }
         affine<V, L>(x, a.p.scale, nullptr, D, t, NT);

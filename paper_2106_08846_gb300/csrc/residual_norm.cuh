@@ -7,6 +7,7 @@
 #include "pair.cuh"
 #include "ptx.cuh"
 #include "residual_norm.h"
+#include "run_blocks.h"
 
 namespace bsr {
 
@@ -42,7 +43,7 @@ __device__ __forceinline__ Run run_of(const uint32_t (&w)[2 * sizeof(T)]) {
 
 // A run as it is loaded: its words; or (ANY) the 16-byte blocks that hold it, the
 // place of its first byte in them and the values that are there. The blocks' other
-// bytes lie beside the run in memory, in a block that has a part of it.
+// bytes lie beside the run in its array.
 template <typename T, int L>
 struct Raw {
     uint32_t w[2 * sizeof(T)];
@@ -110,8 +111,12 @@ __device__ __forceinline__ uint4 load_block(const void *p) {
                      : "memory");
     return u;
 }
+__device__ __forceinline__ uint32_t load_value(const float *p) { return *reinterpret_cast<const uint32_t *>(p); }
+__device__ __forceinline__ uint32_t load_value(const uint16_t *p) { return *p; }
+// ANY: at_end, where at_array_end holds for the row, whose last runs are then read value by
+// value (by its blocks the call would read up to 14 bytes past y, h and the others).
 template <typename T, int L, bool CONST>
-__device__ __forceinline__ Raw<T, L> load_run(const T *row, int D, int i, int t, int NT) {
+__device__ __forceinline__ Raw<T, L> load_run(const T *row, int D, int i, int t, int NT, bool at_end) {
     Raw<T, L> r;
     const int e = feature(i, 0, t, NT);
     if constexpr (L != ANY) {
@@ -123,22 +128,44 @@ __device__ __forceinline__ Raw<T, L> load_run(const T *row, int D, int i, int t,
         }
     } else {
         const uintptr_t first = reinterpret_cast<uintptr_t>(row + e);
-        const char *block = reinterpret_cast<const char *>(first & ~(uintptr_t)15);
-        r.at = (int)(first & 15);
+        const char *const blocks = reinterpret_cast<const char *>(first & ~(uintptr_t)15);
         r.n = min(8, D - e);
-        const int bytes = r.at + r.n * (int)sizeof(T);   // of the blocks that the run needs
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2 + 1; h++) {
-            uint4 u = make_uint4(0, 0, 0, 0);
-            if (r.n > 0 && 16 * h < bytes) u = load_block<CONST>(block + 16 * h);
-            r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
-        }
+        r.at = read_run<sizeof(T)>(
+            r.w, (int)(first & 15), r.n, at_end && at_row_end(D - e),
+            [&](int k, uint32_t *w) {
+                const uint4 u = load_block<CONST>(blocks + 16 * k);
+                w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+            },
+            [&](int j) { return load_value(row + e + j); });
     }
     return r;
 }
+// A run of a parameter, which may begin on any boundary of 4 bytes (ANY).
+template <int L>
+__device__ __forceinline__ Run load_param(const float *p, int D, int i, int t, int NT) {
+    if constexpr (L != ANY) {
+        return load_run<float, L, true>(p, D, i, t, NT, false).run();
+    } else {
+        uint32_t w[8];
+        const int e = feature(i, 0, t, NT), n = D - e;
+        read_run<4>(
+            w, 0, n, n < 8 || reinterpret_cast<uintptr_t>(p) % 16 != 0,
+            [&](int k, uint32_t *v) {
+                const uint4 u = load_block<true>(p + e + 4 * k);
+                v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
+            },
+            [&](int j) { return load_value(p + e + j); });
+        return run_of<float>(w);
+    }
+}
+// A run of a gate's row.
 template <typename T, int L>
-__device__ __forceinline__ Run load_const(const T *row, int D, int i, int t, int NT) {
-    return load_run<T, L, true>(row, D, i, t, NT).run();
+__device__ __forceinline__ Run load_gate(const T *row, int D, int i, int t, int NT, bool at_end) {
+    return load_run<T, L, true>(row, D, i, t, NT, at_end).run();
+}
+template <int L>
+__device__ __forceinline__ bool row_at_end(int64_t rows, int D) {
+    return L == ANY && at_array_end(rows, D);
 }
 // A warp's kilobyte of shared memory; WARPS: the most of a CTA.
 template <int WARPS>
@@ -352,7 +379,7 @@ __device__ __forceinline__ void affine(Run (&x)[ROWS][V], const float *w, const 
     if (w) {
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            const Run p = load_const<float, L>(w, D, i, t, NT);
+            const Run p = load_param<L>(w, D, i, t, NT);
 #pragma unroll
             for (int k = 0; k < ROWS; k++) times(x[k][i], p);
         }
@@ -360,7 +387,7 @@ __device__ __forceinline__ void affine(Run (&x)[ROWS][V], const float *w, const 
     if (b) {
 #pragma unroll
         for (int i = 0; i < V; i++) {
-            const Run p = load_const<float, L>(b, D, i, t, NT);
+            const Run p = load_param<L>(b, D, i, t, NT);
 #pragma unroll
             for (int k = 0; k < ROWS; k++)
 #pragma unroll

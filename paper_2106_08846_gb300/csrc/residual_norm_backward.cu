@@ -53,13 +53,14 @@ struct Token {
 template <bool GATE, typename TB, typename TS, int L>
 __device__ __forceinline__ void load_token(const RnBackward &a, int64_t n, int D, int t, Token<TB, TS, L> &k) {
     const int64_t at = n * D;
-    k.y = load_run<TB, L, false>(static_cast<const TB *>(a.y) + at, D, 0, t, 0);
-    if (a.dh_out) k.dh = load_run<TS, L, false>(static_cast<const TS *>(a.dh_out) + at, D, 0, t, 0);
+    const bool at_end = row_at_end<L>(a.N - 1 - n, D);
+    k.y = load_run<TB, L, false>(static_cast<const TB *>(a.y) + at, D, 0, t, 0, at_end);
+    if (a.dh_out) k.dh = load_run<TS, L, false>(static_cast<const TS *>(a.dh_out) + at, D, 0, t, 0, at_end);
     if (a.p.pre != BSR_NORM_NONE) {
-        k.h = load_run<TS, L, true>(static_cast<const TS *>(a.h_out) + at, D, 0, t, 0);
-        k.dz = load_run<TB, L, false>(static_cast<const TB *>(a.dz) + at, D, 0, t, 0);
+        k.h = load_run<TS, L, true>(static_cast<const TS *>(a.h_out) + at, D, 0, t, 0, at_end);
+        k.dz = load_run<TB, L, false>(static_cast<const TB *>(a.dz) + at, D, 0, t, 0, at_end);
     }
-    if (GATE) k.gate = load_run<TB, L, true>(static_cast<const TB *>(a.gate) + at, D, 0, t, 0);
+    if (GATE) k.gate = load_run<TB, L, true>(static_cast<const TB *>(a.gate) + at, D, 0, t, 0, at_end);
 }
 
 // What a unit of tokens of one gate row adds to the parameters' gradients follows
@@ -104,7 +105,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
     // a parameter, 1 where there is none; past the row's end 0: dH is not 0 there, but
     // what the LayerNorm's gradient takes out of the row, which no sum may take in again
     auto param = [&](Run &r, const float *p) {
-        r = p ? load_const<float, L>(p, D, 0, t, 0) : row_run<L>(1.f, D, 0, t, 0);
+        r = p ? load_param<L>(p, D, 0, t, 0) : row_run<L>(1.f, D, 0, t, 0);
     };
     Q = S = dpre_w = dpre_b = all_run(0.f);
     param(pre_w, a.p.pre_w);
@@ -124,10 +125,11 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         const int64_t row = u / args.split.slices, n0 = first_of(u);
         const int64_t n1 = min(min(n0 + args.split.len, (row + 1) * args.split.span), a.N);
         const int64_t later = u + args.split.workers < args.split.units ? first_of(u + args.split.workers) : -1;
+        const int64_t gate_rows = L == ANY ? args.split.units / args.split.slices : 0;
         const TB *const gate_row = GATE == OF_RUNS && a.gate ? static_cast<const TB *>(a.gate) + row * D : nullptr;
         param(wc, a.p.scale);
-        if (gate_row) times(wc, load_const<TB, L>(gate_row, D, 0, t, 0));
-        if (a.p.post_w) times(wc, load_const<float, L>(a.p.post_w, D, 0, t, 0));
+        if (gate_row) times(wc, load_gate<TB, L>(gate_row, D, 0, t, 0, row_at_end<L>(gate_rows - 1 - row, D)));
+        if (a.p.post_w) times(wc, load_param<L>(a.p.post_w, D, 0, t, 0));
         for (int64_t n = n0; n < n1; n++) {
             if (!KEEP) load_token<GATE_AHEAD>(a, n, D, t, next);
             Run y = next.y.run(), hh = next.h.run(), g = next.dh.run(), dz = next.dz.run();   // g: dH
@@ -186,20 +188,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
             }
             const F2 ry2 = all2(ry);
             if constexpr (GATE == OF_TOKENS) {
-                if (!GATE_AHEAD) gate = load_const<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, 0, t, 0);
+                if (!GATE_AHEAD) gate = load_gate<TB, L>(static_cast<const TB *>(a.gate) + n * D, D, 0, t, 0, row_at_end<L>(a.N - 1 - n, D));
                 if (a.g.dgate) {   // scale t dH
                     Run d = y;
                     if (post) {
 #pragma unroll
                         for (int j = 0; j < 4; j++) d.v[j] = mul2(d.v[j], ry2);
                     }
-                    if (a.p.post_w) times(d, load_const<float, L>(a.p.post_w, D, 0, t, 0));
+                    if (a.p.post_w) times(d, load_param<L>(a.p.post_w, D, 0, t, 0));
                     if (a.p.post_b) {
-                        const Run b = load_const<float, L>(a.p.post_b, D, 0, t, 0);
+                        const Run b = load_param<L>(a.p.post_b, D, 0, t, 0);
 #pragma unroll
                         for (int j = 0; j < 4; j++) d.v[j] = add2(d.v[j], b.v[j]);
                     }
-                    if (a.p.scale) times(d, load_const<float, L>(a.p.scale, D, 0, t, 0));
+                    if (a.p.scale) times(d, load_param<L>(a.p.scale, D, 0, t, 0));
                     times(d, g);
                     store_run<TB, L, THREADS / 32>(static_cast<TB *>(a.g.dgate) + n * D, D, 0, t, 0, d);
                 }
@@ -231,10 +233,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == 128 ? 4 : 1) k_residual_no
         if (GATE == OF_RUNS || later < 0) {   // what the unit (else: all of the worker's) adds to the gradients
             float *const out = args.sums + worker * kSums * D;
             Run w = all_run(1.f), b = all_run(0.f), scale = all_run(1.f), gate = all_run(1.f), P, R;
-            if (a.p.post_w) w = load_const<float, L>(a.p.post_w, D, 0, t, 0);
-            if (a.p.post_b) b = load_const<float, L>(a.p.post_b, D, 0, t, 0);
-            if (a.p.scale) scale = load_const<float, L>(a.p.scale, D, 0, t, 0);
-            if (gate_row) gate = load_const<TB, L>(gate_row, D, 0, t, 0);
+            if (a.p.post_w) w = load_param<L>(a.p.post_w, D, 0, t, 0);
+            if (a.p.post_b) b = load_param<L>(a.p.post_b, D, 0, t, 0);
+            if (a.p.scale) scale = load_param<L>(a.p.scale, D, 0, t, 0);
+            if (gate_row) gate = load_gate<TB, L>(gate_row, D, 0, t, 0, row_at_end<L>(gate_rows - 1 - row, D));
 #pragma unroll
             for (int j = 0; j < 4; j++) P.v[j] = fma2(w.v[j], Q.v[j], mul2(b.v[j], S.v[j]));
             Run sg = scale;
