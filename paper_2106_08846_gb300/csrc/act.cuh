@@ -103,8 +103,10 @@ __device__ __forceinline__ F2 activate_slope(F2 g, F2 &slope) {
         slope = each2(g, [](float t) { return t > 0.f ? 1.f : (t != t ? t : 0.f); });
         return relu(g);
     } else {
-        const F2 p = logistic<FAST>(g);
-        slope = mul2(p, fma2(p, minus, one));
+        // 1 - p as e^-g p, not as a difference, of which nothing is left from g = 17 on (where
+        // e^-g overflows p is 0, and so is the slope)
+        const F2 e = exp_of<FAST>(-1.f, g), p = each2(add2(e, one), reciprocal);
+        slope = mul2(p, each2(mul2(e, p), [](float q) { return fminf(q, 1.f); }));
         return p;
     }
 }

@@ -41,3 +41,23 @@ def test_gelu(N, dtype):
     close(H, x * cdf, x.abs() * cdf, rel + (2.0 ** -8 if dtype == "bf16" else 0.0))
     close(dU, x * cdf, x.abs() * cdf, rel)
     close(dG, cdf + x * density, cdf + x.abs() * density, rel)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 5, 64])
+def test_sigmoid(N, dtype):
+    g = torch.linspace(-80, 80, 1024, device="cuda")
+    H, dG, dU = on_a_grid(g, "sigmoid", dtype, N)
+    p, q = torch.sigmoid(g.double()), torch.sigmoid(-g.double())
+    rel = NEAR[dtype]
+    close(H, p, p, rel + (2.0 ** -8 if dtype == "bf16" else 0.0))
+    close(dU, p, p, rel)
+    close(dG, p * q, p * q, rel)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sigmoid_where_the_exponential_overflows(dtype):
+    g = torch.tensor([-3e38, -1e4, -100.0, -89.0, 89.0, 100.0, 1e4, 3e38], device="cuda").repeat(8)
+    H, dG, dU = on_a_grid(g, "sigmoid", dtype, 40)
+    want = (g > 0).double()
+    assert ((H - want).abs() <= 1e-37).all() and ((dU - want).abs() <= 1e-37).all() and (dG.abs() <= 1e-37).all()
