@@ -9,10 +9,10 @@
 // and of Wu, so that a thread finds G and U of a feature side by side; its eight
 // columns are tokens. The 16 bytes of a lane hold its part of two MMAs: which
 // columns of K meet in one is free, as long as weights and activations agree.
-// fp32: likewise, values split into tf32 parts, high and low, and multiplied as
-// high x low + low x high + high x high; one token or two by multiply-adds, two
-// columns of K to an instruction and four lanes to a feature. (768 into 2048: one
-// token 4.4 us, by the parts 6.6; four tokens 6.3, by the parts 6.6.)
+// fp32: likewise, values split into the three bf16 parts whose sum they are, and a product
+// as the six part products that are not below 2^-24 of it; one token or two by
+// multiply-adds, two columns of K to an instruction and four lanes to a feature. (768 into
+// 2048: one token 4.4 us, by parts 6.6; four tokens 6.3, by parts 6.6.)
 //
 // What bounds it: DRAM, and for small weights the time of a launch and of one read.
 // 1024 into 4096, bf16: 1 to 8 tokens 4.5 us (16.8 MB, 2.5 us at the copy rate), 16
@@ -35,21 +35,32 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kAhead = 4;   // 16-byte reads of either weight on their way at a time
 
-template <typename T>
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    if constexpr (sizeof(T) == 2)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                     : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// A tf32 high part (cut off) and the rest.
-__device__ __forceinline__ void split(uint32_t x, uint32_t &hi, uint32_t &lo) {
-    hi = x & 0xffffe000u;
-    lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
+// Two values as bf16, rounded to nearest, one that would overflow to the largest.
+__device__ __forceinline__ uint32_t pack_finite(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// The three bf16 parts of four fp32 values, in pairs (p[k]: part k of both pairs): each
+// the rounding of what the parts before it left, at most 2^-8 of them; their sum is the
+// value. (Of an infinity the last part is one.)
+__device__ __forceinline__ void split(const uint4 &v, uint32_t (&p)[3][2]) {
+    float x[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+#pragma unroll
+        for (int k = 0; k < 2; k++) {
+            p[k][h] = pack_finite(x[2 * h], x[2 * h + 1]);
+            x[2 * h] -= __uint_as_float(p[k][h] << 16);
+            x[2 * h + 1] -= __uint_as_float(p[k][h] & 0xffff0000u);
+        }
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2][h]) : "f"(x[2 * h + 1]), "f"(x[2 * h]));
+    }
 }
 
 // 16 bytes of a row from column k on; where CHECK, 0 past column K. Rows start on
@@ -121,32 +132,33 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_
         }
 #pragma unroll
         for (int i = 0; i < kAhead; i++) {
-            const uint32_t ga[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, ua[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t ga[4] = {a[i].x, a[i].y, a[i].z, a[i].w}, ua[4] = {b[i].x, b[i].y, b[i].z, b[i].w};
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                const uint4 v = load16<T, ALIGNED, CHECK, false>(x[n], k + i * step, K);
-                const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
-                if constexpr (sizeof(T) == 2) {
+                for (int n = 0; n < NT; n++) {
+                    const uint4 v = load16<T, ALIGNED, CHECK, false>(x[n], k + i * step, K);
+                    const uint32_t xv[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int j = 0; j < 4; j += 2) mma<T>(acc[n], ga[j], ua[j], ga[j + 1], ua[j + 1], xv[j], xv[j + 1]);
-                } else {
+                    for (int j = 0; j < 4; j += 2) mma(acc[n], ga[j], ua[j], ga[j + 1], ua[j + 1], xv[j], xv[j + 1]);
+                }
+            } else {
+                uint32_t g[3][2], u[3][2];
+                split(a[i], g);
+                split(b[i], u);
+#pragma unroll
+                for (int n = 0; n < NT; n++) {
+                    uint32_t xv[3][2];
+                    split(load16<T, ALIGNED, CHECK, false>(x[n], k + i * step, K), xv);
                     // the accumulation in an MMA drops bits: the small products first, and
                     // 16 columns at a time added here (in one accumulator throughout the
                     // error of 1024 columns was 2.5e-6 of H, that of plain sums 0.9e-6)
                     float sum[4] = {};
-                    uint32_t h[2][6], l[2][6];
 #pragma unroll
-                    for (int j = 0; j < 2; j++) {
-                        const uint32_t part[6] = {ga[2 * j], ua[2 * j], ga[2 * j + 1], ua[2 * j + 1], xv[2 * j], xv[2 * j + 1]};
+                    for (int p = 2; p >= 0; p--)
 #pragma unroll
-                        for (int k = 0; k < 6; k++) split(part[k], h[j][k], l[j][k]);
-                        mma<T>(sum, l[j][0], l[j][1], l[j][2], l[j][3], h[j][4], h[j][5]);
-                        mma<T>(sum, h[j][0], h[j][1], h[j][2], h[j][3], l[j][4], l[j][5]);
-                    }
+                        for (int w = p; w >= 0; w--) mma(sum, g[w][0], u[w][0], g[w][1], u[w][1], xv[p - w][0], xv[p - w][1]);
 #pragma unroll
-                    for (int j = 0; j < 2; j++) mma<T>(sum, h[j][0], h[j][1], h[j][2], h[j][3], h[j][4], h[j][5]);
-#pragma unroll
-                    for (int k = 0; k < 4; k++) acc[n][k] += sum[k];
+                    for (int j = 0; j < 4; j++) acc[n][j] += sum[j];
                 }
             }
         }
