@@ -16,10 +16,10 @@
 #include <algorithm>
 
 #include "bsr_internal.h"
-#include "elem.cuh"
 #include "gated.h"
 #include "gated_mma.h"
 #include "launch.cuh"
+#include "parts.cuh"
 #include "ptx.cuh"
 
 namespace bsr {
@@ -38,10 +38,7 @@ struct Sources {
     int vec;   // K is a multiple of 8 (rows start on 16-byte boundaries)
 };
 
-__device__ __forceinline__ uint16_t cut(float x) { return (uint16_t)(__float_as_uint(x) >> 16); }
-
-// Eight columns a thread. fp32: three parts, cut off and not rounded, so that
-// none overflows; a value that is not finite goes into the first part alone.
+// Eight columns a thread; fp32: their three parts.
 template <typename T>
 __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources a) {
     constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
@@ -53,10 +50,13 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
         const int64_t row = i / eights, c = (i - row * eights) * 8;
         const T *src = static_cast<const T *>(m.src) + row * a.K + c;
         const bool there = row < m.rows;
-        uint16_t out[PARTS][8];
+        uint32_t w[PARTS][4];
         if constexpr (PARTS == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) out[0][j] = there && c + j < a.K ? __ldg(src + j) : (uint16_t)0;
+            for (int j = 0; j < 8; j++) {
+                const uint32_t v = there && c + j < a.K ? __ldg(src + j) : (uint16_t)0;
+                w[0][j / 2] = j & 1 ? w[0][j / 2] | v << 16 : v;
+            }
         } else {
             float v[8];
             if (a.vec && there) {
@@ -67,21 +67,16 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
                 for (int j = 0; j < 8; j++) v[j] = there && c + j < a.K ? __ldg(src + j) : 0.f;
             }
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                const bool finite = (__float_as_uint(v[j]) & 0x7f800000u) != 0x7f800000u;
-                const float hi = __uint_as_float(__float_as_uint(v[j]) & 0xffff0000u), r = finite ? v[j] - hi : 0.f;
-                out[0][j] = finite ? cut(hi) : from_f32<uint16_t>(v[j]);
-                out[1][j] = cut(r);
-                out[2][j] = cut(r - __uint_as_float(__float_as_uint(r) & 0xffff0000u));
+            for (int j = 0; j < 4; j++) {
+                uint32_t p[3];
+                parts_of(v[2 * j], v[2 * j + 1], p);
+#pragma unroll
+                for (int k = 0; k < 3; k++) w[k][j] = p[k];
             }
         }
 #pragma unroll
-        for (int p = 0; p < PARTS; p++) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; j++) w[j] = out[p][2 * j] | (uint32_t)out[p][2 * j + 1] << 16;
-            *reinterpret_cast<uint4 *>(m.dst + ((int64_t)p * m.padded + row) * a.Kp + c) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
+        for (int p = 0; p < PARTS; p++)
+            *reinterpret_cast<uint4 *>(m.dst + ((int64_t)p * m.padded + row) * a.Kp + c) = make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]);
     }
 }
 

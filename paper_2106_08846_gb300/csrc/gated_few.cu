@@ -26,6 +26,7 @@
 #include "elem.cuh"
 #include "gated.h"
 #include "launch.cuh"
+#include "parts.cuh"
 #include "ptx.cuh"
 
 namespace bsr {
@@ -40,27 +41,13 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// Two values as bf16, rounded to nearest, one that would overflow to the largest.
-__device__ __forceinline__ uint32_t pack_finite(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.satfinite.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-// The three bf16 parts of four fp32 values, in pairs (p[k]: part k of both pairs): each
-// the rounding of what the parts before it left, at most 2^-8 of them; their sum is the
-// value. (Of an infinity the last part is one.)
+// The parts of four fp32 values, in pairs (p[k]: part k of both pairs).
 __device__ __forceinline__ void split(const uint4 &v, uint32_t (&p)[3][2]) {
-    float x[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+    uint32_t a[3], b[3];
+    parts_of(__uint_as_float(v.x), __uint_as_float(v.y), a);
+    parts_of(__uint_as_float(v.z), __uint_as_float(v.w), b);
 #pragma unroll
-    for (int h = 0; h < 2; h++) {
-#pragma unroll
-        for (int k = 0; k < 2; k++) {
-            p[k][h] = pack_finite(x[2 * h], x[2 * h + 1]);
-            x[2 * h] -= __uint_as_float(p[k][h] << 16);
-            x[2 * h + 1] -= __uint_as_float(p[k][h] & 0xffff0000u);
-        }
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[2][h]) : "f"(x[2 * h + 1]), "f"(x[2 * h]));
-    }
+    for (int k = 0; k < 3; k++) p[k][0] = a[k], p[k][1] = b[k];
 }
 
 // 16 bytes of a row from column k on; where CHECK, 0 past column K. Rows start on

@@ -49,8 +49,8 @@
 // with M or N contiguous.
 //
 // fp32 operands come as three bf16 parts whose sum they are (8 bits of the
-// significand each), and a product is the six of nine part products that are not
-// below 2^-24 of it (bf16 products may have an A of two parts). The tensor cores'
+// significand each, rounded to nearest), and a product is the six of nine part
+// products that are not below 2^-24 of it (bf16 products may have an A of two parts). The tensor cores'
 // fp32 accumulation drops bits with every addition, so the small products of a
 // step come first and the accumulators are added to registers after every step.
 //
@@ -67,6 +67,7 @@
 #include "elem.cuh"
 #include "gated_mma.h"
 #include "launch.cuh"
+#include "parts.cuh"
 #include "ptx.cuh"
 #include "status.cuh"
 #include "tcgen05.cuh"
@@ -300,17 +301,6 @@ __device__ __forceinline__ float row_sums(const F2 (&p)[4]) {
     return mine + __shfl_xor_sync(0xffffffffu, other, 4);
 }
 
-// The three bf16 parts of a finite fp32 value, cut off and not rounded, so that
-// none overflows: their sum is the value.
-__device__ __forceinline__ void parts_of(float x, float (&p)[3]) {
-    p[0] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    const bool finite = (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u;
-    if (!finite) p[0] = x;   // (an infinity, or a NaN of which the cut could make one)
-    const float r = finite ? x - p[0] : 0.f;
-    p[1] = __uint_as_float(__float_as_uint(r) & 0xffff0000u);
-    p[2] = r - p[1];
-}
-
 // Puts out G and U (v and w: eight features from c on, in pairs, of rows `row` and
 // row + 8) of a gated mode: H, or dG and dU, whose sums over the rows are added to
 // sg and su.
@@ -385,19 +375,15 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
             } else {
 #pragma unroll
                 for (int k = 0; k < 2; k++) {
-                    uint32_t p[3][4];
+                    uint32_t p[4][3];
 #pragma unroll
                     for (int j = 0; j < 4; j++) {
                         const float2 x = unpack2(k ? w[h][j] : v[h][j]);
-                        float lo[3], hi[3];
-                        parts_of(x.x, lo);
-                        parts_of(x.y, hi);
-#pragma unroll
-                        for (int i = 0; i < 3; i++) p[i][j] = pack_bf16(lo[i], hi[i]);
+                        parts_of(x.x, x.y, p[j]);
                     }
 #pragma unroll
                     for (int i = 0; i < 3; i++)
-                        *reinterpret_cast<uint4 *>(at + k * a.Fp + i * 2 * a.Fp * job.M) = make_uint4(p[i][0], p[i][1], p[i][2], p[i][3]);
+                        *reinterpret_cast<uint4 *>(at + k * a.Fp + i * 2 * a.Fp * job.M) = make_uint4(p[0][i], p[1][i], p[2][i], p[3][i]);
                 }
             }
         }

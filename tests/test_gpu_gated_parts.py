@@ -34,7 +34,28 @@ def test_few_tokens(N, K):
     assert float(err.max()) <= ONE, float(err.max())
 
 
-@pytest.mark.parametrize("N", [3, 20])
+@pytest.mark.parametrize("N", [33, 300])
+def test_more_tokens(N):
+    X, W, one = values(N, 1, N), values(520, 1, 7), torch.ones(520, device="cuda")
+    H = bsr.bsr_gated(X, torch.zeros_like(W), W, one, None, act="relu")
+    want = exact(X, W)
+    err = ((H.double() - want).abs() / want.abs())
+    assert float(err.max()) <= ONE, float(err.max())
+
+
+@pytest.mark.parametrize("N", [1, 33, 300])
+def test_gradients(N):
+    """F = 1, Wg = 0 and G = 1: dU = dH, dX = dH Wu; of one token dWu = dH X."""
+    X, Wu, one = values(N, 200, N), values(1, 200, 5), torch.ones(1, device="cuda")
+    dH = values(N, 1, 3)
+    got = bsr.bsr_gated_backward(X, torch.zeros_like(Wu), Wu, one, None, dH, act="relu")
+    pairs = [(got["dX"], exact(dH, Wu.T))] + ([(got["dWu"], exact(dH, X.T))] if N == 1 else [])
+    for x, want in pairs:
+        err = ((x.double() - want).abs() / want.abs())
+        assert torch.isfinite(x).all() and float(err.max()) <= ONE, float(err.max())
+
+
+@pytest.mark.parametrize("N", [3, 20, 40])
 def test_large_and_infinite_values(N):
     big = torch.finfo(torch.float32).max
     X = torch.tensor([[big, 0.0, 0.0], [-big, 0.0, 0.0], [float("inf"), 0.0, 0.0]], device="cuda").repeat(-(-N // 3), 1)[:N].contiguous()
