@@ -86,6 +86,11 @@ constexpr uint32_t kBiasBytes = 8 * 128 * 4;  // a warp's share of bg and bu: 64
 constexpr uint32_t kMaxSmem = 227 * 1024 - 1024;
 constexpr uint32_t kAccCols = 256;
 constexpr int kProducers = 3;
+// Steps of a bf16 product's unit at most: the accumulators lose about 7e-9 of a sum of
+// one sign with each column, always towards zero, over so many (16384 columns) 2^-13, a
+// sixteenth of the most that a bf16 result is rounded by; longer sums are split, their
+// parts added in fp32.
+constexpr int kMostSteps = 256;
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
 
 __device__ int g_status;
@@ -1133,11 +1138,16 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
                 best = q;
             }
         };
-        consider({0, 0}, {1, 1});
+        // a sum's parts at least
+        int least[2] = {1, 1};
+        for (int i = 0; i < n && product && groups != 6; i++) least[i] = (p.shape[i].steps + kMostSteps - 1) / kMostSteps;
+        consider({0, 0}, least);
         if (!product) continue;
         for (int s0 : {1, 2, 3, 4, 5, 6, 8, 12, 16})
             for (int s1 : {1, 2, 3, 4, 6, 8, 12, 16})
-                if (s0 + s1 > 2 && s0 <= p.shape[0].steps && (n > 1 ? s1 <= p.shape[1].steps : s1 == 1)) consider({0, 0}, {s0, s1});
+                if (s0 + s1 > 2 && s0 <= p.shape[0].steps && (n > 1 ? s1 <= p.shape[1].steps : s1 == 1))
+                    consider({0, 0}, {std::max(s0, least[0]), std::max(s1, least[1])});
+        if (least[0] + least[1] > 2) continue;
         // only those tiles of the shorter sums that would fill the last round in part
         const int last = n > 1 && p.shape[1].steps <= p.shape[0].steps;
         const int64_t rest = (p.shape[0].tiles + (n > 1 ? p.shape[1].tiles : 0)) % pairs;

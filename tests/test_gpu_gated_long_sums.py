@@ -1,0 +1,48 @@
+"""Gradients of the gated block's bf16 weights over very many tokens: sums of one
+sign, from which an accumulator that drops bits takes more with every token."""
+import math
+
+import pytest
+import torch
+
+import paper_2106_08846_gb300 as bsr
+
+pytestmark = pytest.mark.gpu
+BF16 = torch.bfloat16
+
+
+def positive(g, *shape):
+    return torch.rand(*shape, device="cuda", generator=g) + 0.5
+
+
+@pytest.mark.parametrize("N", [65536, 1 << 20, (1 << 19) + 100])
+def test_weights_of_many_tokens(N):
+    F = K = 64
+    g = torch.Generator(device="cuda").manual_seed(N)
+    X, dH = (positive(g, N, K) * positive(g, K)).to(BF16), (positive(g, N, F) * positive(g, F)).to(BF16)
+    Wg, Wu = positive(g, F, K).to(BF16), positive(g, F, K).to(BF16)
+    got = bsr.bsr_gated_backward(X, Wg, Wu, None, None, dH, act="relu")
+    x, d = X.double(), dH.double()
+    dU = d * (x @ Wg.double().T)
+    dG = d * (x @ Wu.double().T)
+    want = {"dWg": dG.T @ x, "dWu": dU.T @ x}
+    for k, w in want.items():
+        off = got[k].double() / w - 1
+        # a 32nd of the most that one is rounded by, for what accumulators lose, and the mean of results' and operands' roundings, spread over an
+        # octave and more by the factors above: at most 2^-9 each (2-norm), five times that of their mean
+        assert abs(float(off.mean())) <= 2.0 ** -14 + 5 * 2.0 ** -9 / math.sqrt(off.numel()), (k, float(off.mean()))
+        assert float(off.abs().max()) <= 2.0 ** -8 + 2.0 ** -10
+
+
+def test_a_long_inner_sum():
+    """dX, over 2 x 70000 features."""
+    N, F, K = 64, 70000, 32
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X, dH = positive(g, N, K).to(BF16), (positive(g, N, F) * positive(g, N, 1)).to(BF16)
+    Wg, Wu = ((positive(g, F, K) * positive(g, K)).to(BF16) for _ in range(2))
+    dX = bsr.bsr_gated_backward(X, Wg, Wu, None, None, dH, act="relu")["dX"]
+    x, d = X.double(), dH.double()
+    want = (d * (x @ Wu.double().T)) @ Wg.double() + (d * (x @ Wg.double().T)) @ Wu.double()
+    off = dX.double() / want - 1
+    assert abs(float(off.mean())) <= 2.0 ** -14 + 5 * 2.0 ** -9 / math.sqrt(off.numel()), float(off.mean())
+    assert float(off.abs().max()) <= 2.0 ** -8 + 2.0 ** -10
