@@ -232,7 +232,7 @@ cudaError_t launch_gated_backward(const GatedCall &c, cudaStream_t s) {
     GatedBias b;
     if (g.sums) {
         b.sums = g.sums;
-        b.rows = (c.N + 31) / 32 * (32 / sum_rows(p.main_plan, c.dt));
+        b.rows = (c.N + 31) / 32 * (32 / sum_rows(p.main_plan));
         b.F = c.F, b.Fp = p.Fp;
         b.dbg = c.dbg, b.dbu = c.dbu;
     }

@@ -80,22 +80,33 @@ __device__ __forceinline__ uint4 load16(const T *row, int k, int K) {
 
 // Calls body(k, checked) for this lane's columns k of each kAhead reads of a warp:
 // kAhead spans of 64 bytes, kWarps spans apart; `checked` (a compile-time constant)
-// where some may lie past K.
+// where some may lie past K. LONG: calls pause() after every kPause whole ones.
 template <bool B>
 struct Checked {
     static constexpr bool value = B;
 };
-template <typename T, typename F>
-__device__ __forceinline__ void along_k(int K, F body) {
-    constexpr int span = 64 / sizeof(T), stride = kAhead * kWarps * span;
+constexpr int kPause = 8;
+template <typename T>
+constexpr int kStride = kAhead * kWarps * 64 / (int)sizeof(T);   // columns of a call of body, of all warps
+template <typename T, bool LONG, typename F, typename P>
+__device__ __forceinline__ void along_k(int K, F body, P pause) {
+    constexpr int span = 64 / sizeof(T), stride = kStride<T>;
     const int lane0 = (threadIdx.x >> 5) * span + (threadIdx.x & 3) * (16 / (int)sizeof(T));
-    int k0 = 0;
-    for (; k0 + stride <= K; k0 += stride) body(k0 + lane0, Checked<false>{});
+    int k0 = 0, until = kPause * stride;
+    for (; k0 + stride <= K; k0 += stride) {
+        if (LONG && k0 == until) {
+            pause();
+            until += kPause * stride;
+        }
+        body(k0 + lane0, Checked<false>{});
+    }
     if (k0 < K) body(k0 + lane0, Checked<true>{});
 }
 
-// NT eights of tokens.
-template <typename T, int NT, bool ALIGNED>
+// NT eights of tokens. LONG (bf16): K of more than kPause strides. The accumulation drops
+// bits (7e-9 of a sum of one sign with a column), so a long sum goes on in shared memory.
+// (In short ones the test alone took 0.3 us, for 8 tokens of 1024 into 4096.)
+template <typename T, int NT, bool ALIGNED, bool LONG>
 __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_gated_few(const __grid_constant__ GatedCall c) {
     constexpr int step = kWarps * 64 / sizeof(T);
     __shared__ float4 sums[kWarps][NT][32];
@@ -108,8 +119,19 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_
 #pragma unroll
     for (int n = 0; n < NT; n++) x[n] = static_cast<const T *>(c.X) + std::min<int64_t>(8 * n + g, c.N - 1) * c.K;
     float acc[NT][4] = {};
+    bool kept = false;   // whether `sums` has what came before acc
+    auto keep = [&]() {
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            float4 &s = sums[warp][n][lane];
+            const float4 old = LONG && kept ? s : make_float4(0.f, 0.f, 0.f, 0.f);
+            s = make_float4(old.x + acc[n][0], old.y + acc[n][1], old.z + acc[n][2], old.w + acc[n][3]);
+#pragma unroll
+            for (int j = 0; j < 4; j++) acc[n][j] = 0.f;
+        }
+    };
     ptx::pdl_wait();
-    along_k<T>(K, [&](int k, auto checked) {
+    along_k<T, LONG>(K, [&](int k, auto checked) {
         constexpr bool CHECK = decltype(checked)::value;
         uint4 a[kAhead], b[kAhead];
 #pragma unroll
@@ -149,9 +171,11 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_
                 }
             }
         }
+    }, [&]() {
+        keep();
+        kept = true;
     });
-#pragma unroll
-    for (int n = 0; n < NT; n++) sums[warp][n][lane] = make_float4(acc[n][0], acc[n][1], acc[n][2], acc[n][3]);
+    keep();
     __syncthreads();
     // feature lane / 4 and tokens 2 (lane % 4), + 1 of each eight: G in x, y, U in z, w
     for (int e = threadIdx.x; e < NT * 32; e += 32 * kWarps) {
@@ -191,7 +215,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) k_gated_few_f32(const __grid_c
 #pragma unroll
     for (int n = 0; n < TOKENS; n++) G[n] = U[n] = all2(0.f);
     ptx::pdl_wait();
-    along_k<float>(K, [&](int k, auto checked) {
+    along_k<float, false>(K, [&](int k, auto checked) {
         constexpr bool CHECK = decltype(checked)::value;
         uint4 a[kAhead], b[kAhead];
 #pragma unroll
@@ -213,7 +237,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) k_gated_few_f32(const __grid_c
                 if (n + 1 < tokens) x += K;   // (past the last token: its own row again)
             }
         }
-    });
+    }, []() {});
 #pragma unroll
     for (int n = 0; n < TOKENS; n++) {
         const float2 gs = unpack2(G[n]), us = unpack2(U[n]);
@@ -239,8 +263,12 @@ __global__ void __launch_bounds__(32 * kWarps, 4) k_gated_few_f32(const __grid_c
 
 template <typename T, int NT>
 cudaError_t launch(const GatedCall &c, cudaStream_t s) {
-    return launch_kernel(c.K * sizeof(T) % 16 == 0 ? k_gated_few<T, NT, true> : k_gated_few<T, NT, false>,
-                         dim3((unsigned)((c.F + 7) / 8)), dim3(32 * kWarps), 0, s, c);
+    const bool aligned = c.K * sizeof(T) % 16 == 0;
+    auto kernel = aligned ? k_gated_few<T, NT, true, false> : k_gated_few<T, NT, false, false>;
+    if constexpr (sizeof(T) == 2) {
+        if (c.K > kPause * kStride<T>) kernel = aligned ? k_gated_few<T, NT, true, true> : k_gated_few<T, NT, false, true>;
+    }
+    return launch_kernel(kernel, dim3((unsigned)((c.F + 7) / 8)), dim3(32 * kWarps), 0, s, c);
 }
 template <int TOKENS>
 cudaError_t launch_f32(const GatedCall &c, cudaStream_t s) {

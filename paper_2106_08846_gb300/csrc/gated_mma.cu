@@ -10,7 +10,7 @@
 //                  (128 rows a CTA) and the B tile (`half` rows) by TMA (128-byte
 //                  swizzle) into a stage of the ring
 //   warp 2         MMAs (M = 256, N = 2 half, K = 16) of the pair's first CTA
-//   warps 4 ..     epilogue, 16 (fp32: 8) warps: 32 rows and a share of the
+//   warps 4 ..     epilogue, 16 (drained accumulators: 8) warps: 32 rows and a share of the
 //                  columns each, straight from tensor memory to global memory
 //
 // A step is 512 SM cycles of MMAs at 256 columns (fp32: six times that). Waiting for a
@@ -79,17 +79,20 @@ namespace {
 constexpr int KC = 64;                        // columns of K per chunk
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's A tile
 constexpr int kEpiWarp0 = 4, kMmaWarp = 2;
-constexpr int epi_warps(bool f32) { return f32 ? 8 : 16; }
-constexpr int threads_of(bool f32) { return 32 * (kEpiWarp0 + epi_warps(f32)); }
+constexpr int epi_warps(bool drained) { return drained ? 8 : 16; }
+constexpr int threads_of(bool drained) { return 32 * (kEpiWarp0 + epi_warps(drained)); }
+// Drained accumulators go into registers every so many steps: fp32's after each, those
+// of a gated mode with bf16 sums of more than kMostSteps after 512 columns.
+constexpr int drain_steps(bool f32) { return f32 ? 1 : 8; }
 constexpr int kStages = 8;
 constexpr uint32_t kBiasBytes = 8 * 128 * 4;  // a warp's share of bg and bu: 64 (fp32), 32 features
 constexpr uint32_t kMaxSmem = 227 * 1024 - 1024;
 constexpr uint32_t kAccCols = 256;
 constexpr int kProducers = 3;
-// Steps of a bf16 product's unit at most: the accumulators lose about 7e-9 of a sum of
+// Steps of a bf16 sum in the accumulators at most: the accumulators lose about 7e-9 of a sum of
 // one sign with each column, always towards zero, over so many (16384 columns) 2^-13, a
-// sixteenth of the most that a bf16 result is rounded by; longer sums are split, their
-// parts added in fp32.
+// sixteenth of the most that a bf16 result is rounded by. Longer sums of plain products
+// are split, their parts added in fp32; those of the gated modes are drained.
 constexpr int kMostSteps = 256;
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
 
@@ -453,10 +456,10 @@ __device__ __forceinline__ void put_product(const Args &a, const Job &job, const
     }
 }
 
-template <int MODE, typename T>
-__global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(const __grid_constant__ Args a) {
+template <int MODE, typename T, bool DRAIN>
+__global__ void __launch_bounds__(threads_of(DRAIN), 1) k_gated_mma(const __grid_constant__ Args a) {
     constexpr bool F32 = sizeof(T) == 4;
-    constexpr int kEpiWarps = epi_warps(F32);
+    constexpr int kEpiWarps = epi_warps(DRAIN), kDrain = drain_steps(F32);
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
     const int ns = a.ns;
@@ -602,7 +605,8 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 const uint32_t a_step = a_side ? 128 : 2, b_step = b_side ? 128 : 2, idesc = job.idesc;
                 for (i = un.i0; ok && i < un.i1; i++) {
                     const uint32_t d = tmem + (uint32_t)ab * kAccCols;
-                    if (F32 || i == un.i0) {   // into a fresh accumulator buffer
+                    const bool fresh = DRAIN ? (i - un.i0) % kDrain == 0 : i == un.i0;
+                    if (fresh) {   // into a fresh accumulator buffer
                         ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[ab], aphase, a.wait_ns, &stop));
                         if (!ok) break;
                     }
@@ -620,7 +624,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
 #pragma unroll
                             for (int j = 0; j < KC / 16; j++)
                                 tc5::mma_ss_pair(d, ad + j * a_step, bd + j * b_step, idesc,
-                                                 (!F32 && i > un.i0) | (t > 0) | (j > 0));
+                                                 !fresh | (t > 0) | (j > 0));
                         }
                         tc5::commit_pair(&empty[s]);
                     }
@@ -630,7 +634,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                         s = 0;
                         fphase ^= 1;
                     }
-                    if (F32 || i + 1 == un.i1) {
+                    if (i + 1 == un.i1 || (DRAIN && (i + 1 - un.i0) % kDrain == 0)) {
                         if (elected) tc5::commit_pair(&acc_full[ab]);
                         __syncwarp();
                         n_handed++;
@@ -738,8 +742,8 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
         };
         // bf16: dH of the unit to come (it is read from DRAM, 3000 cycles when the
         // loads of the operands are in its way)
-        Eight<T> ahead[F32 ? 1 : kMost][2];
-        if constexpr (MODE == GM_BACKWARD && !F32) {
+        Eight<T> ahead[DRAIN ? 1 : kMost][2];
+        if constexpr (MODE == GM_BACKWARD && !DRAIN) {
             if (v < a.units) {
                 un = unit_at<MODE>(a, v);
 #pragma unroll
@@ -761,7 +765,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 }
                 __syncwarp();
             }
-            if constexpr (!F32) {
+            if constexpr (!DRAIN) {
                 const uint32_t tm = wait_acc(un);
                 if (!ok) break;
                 if (pieces == 0) hand_back();
@@ -787,7 +791,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                     put(job, p, x, y, dh);
                 }
             } else {
-                float g[kMost][16], w[kMost][16];   // the sums of the steps so far
+                float g[kMost][16], w[kMost][16];   // the sums of what was drained so far
                 if constexpr (MODE == GM_BACKWARD) {   // dH comes from DRAM: into L2 meanwhile
                     for (int p = 0; p < pieces; p++)
                         for (int h = 0; h < 2; h++) {
@@ -799,7 +803,7 @@ __global__ void __launch_bounds__(threads_of(sizeof(T) == 4), 1) k_gated_mma(con
                 for (int p = 0; p < kMost; p++)
 #pragma unroll
                     for (int j = 0; j < 16; j++) g[p][j] = w[p][j] = 0.f;
-                for (int b = un.i0; b < un.i1; b++) {
+                for (int b = un.i0; b < un.i1; b += kDrain) {
                     const uint32_t tm = wait_acc(un);
                     if (!ok) break;
 #pragma unroll
@@ -1008,7 +1012,7 @@ cudaError_t finish(const Args &a, int64_t joins, const GatedBias &b, cudaStream_
     return launch_kernel(k_gated_finish<T>, dim3((unsigned)(joins + sums)), dim3(256), 0, s, a, (unsigned)joins, b.rows, b.F, b.dbg, b.dbu);
 }
 
-template <int MODE, typename T>
+template <int MODE, typename T, bool DRAIN>
 cudaError_t launch(const GatedMma *g, const GatedPlan &p, const GatedBias &b, cudaStream_t s) {
     Args a = {};
     if (p.units > INT32_MAX) return cudaErrorInvalidConfiguration;
@@ -1035,10 +1039,10 @@ cudaError_t launch(const GatedMma *g, const GatedPlan &p, const GatedBias &b, cu
         a.job[1].whole = a.job[1].split_units = 0;
     }
     static std::atomic<uint64_t> attr_set{0};
-    if (e == cudaSuccess) e = allow_smem(k_gated_mma<MODE, T>, kMaxSmem, attr_set);
+    if (e == cudaSuccess) e = allow_smem(k_gated_mma<MODE, T, DRAIN>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(p.units, pairs_of_sms());
-    e = launch_clusters(k_gated_mma<MODE, T>, 2, dim3(grid), dim3(threads_of(sizeof(T) == 4)),
+    e = launch_clusters(k_gated_mma<MODE, T, DRAIN>, 2, dim3(grid), dim3(threads_of(DRAIN)),
                         a.ns * a.stage_bytes + kBiasBytes + 1024, s, a);
     if (MODE != GM_PRODUCT || e != cudaSuccess) return e;
     int64_t joins = 0;
@@ -1113,6 +1117,7 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
             sh.tiles_n = product ? (g[i].N + 2 * half - 1) / (2 * half) : (g[i].Fp + half - 1) / half;
             sh.tiles = (g[i].M + 255) / 256 * sh.tiles_n;
         }
+        p.drained = groups == 6 || (!product && p.shape[0].steps > kMostSteps);
         // the first `whole` tiles of each job as one unit, the others split
         auto consider = [&](const int64_t (&whole)[2], const int (&splits)[2]) {
             GatedPlan q = p;
@@ -1165,9 +1170,15 @@ GatedPlan plan_gated_mma(const GatedMma *g, int n, int64_t most_bytes) {
 cudaError_t launch_gated_mma(const GatedMma *g, const GatedPlan &p, cudaStream_t s, const GatedBias &b) {
     const bool f32 = g->dt == BSR_F32;
     switch (g->mode) {
-        case GM_FORWARD: return f32 ? launch<GM_FORWARD, float>(g, p, b, s) : launch<GM_FORWARD, uint16_t>(g, p, b, s);
-        case GM_BACKWARD: return f32 ? launch<GM_BACKWARD, float>(g, p, b, s) : launch<GM_BACKWARD, uint16_t>(g, p, b, s);
-        default: return f32 ? launch<GM_PRODUCT, float>(g, p, b, s) : launch<GM_PRODUCT, uint16_t>(g, p, b, s);
+        case GM_FORWARD:
+            return f32         ? launch<GM_FORWARD, float, true>(g, p, b, s)
+                   : p.drained ? launch<GM_FORWARD, uint16_t, true>(g, p, b, s)
+                               : launch<GM_FORWARD, uint16_t, false>(g, p, b, s);
+        case GM_BACKWARD:
+            return f32         ? launch<GM_BACKWARD, float, true>(g, p, b, s)
+                   : p.drained ? launch<GM_BACKWARD, uint16_t, true>(g, p, b, s)
+                               : launch<GM_BACKWARD, uint16_t, false>(g, p, b, s);
+        default: return f32 ? launch<GM_PRODUCT, float, true>(g, p, b, s) : launch<GM_PRODUCT, uint16_t, false>(g, p, b, s);
     }
 }
 

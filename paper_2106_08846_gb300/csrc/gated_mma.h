@@ -54,6 +54,7 @@ struct GatedShape {
 // split into how many parts.
 struct GatedPlan {
     int jobs, half;
+    bool drained;                    // accumulators are added up in registers
     int order[2];                    // shape[i] is g[order[i]]'s
     GatedShape shape[2];
     int64_t units, part_bytes;
@@ -61,7 +62,7 @@ struct GatedPlan {
 };
 
 // Rows of GatedMma::sums: one for so many rows of dG and dU.
-inline int sum_rows(const GatedPlan &p, bsr_dtype_t dt) { return p.half == 128 || (dt == BSR_F32 && p.half == 64) ? 32 : 16; }
+inline int sum_rows(const GatedPlan &p) { return p.half == 128 || (p.drained && p.half == 64) ? 32 : 16; }
 
 // The plan of g, or of two GM_PRODUCTs (as many parts each) in one launch, from
 // the modes and sizes, with at most so many part_bytes.
