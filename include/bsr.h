@@ -392,9 +392,7 @@ bsr_status_t bsr_residual_norm_backward(const bsr_residual_norm_t *p, const void
  *
  * fp32 operands run on the tensor cores as three bf16 parts each, whose sum they
  * are, and a product as the six part products that are not below 2^-24 of it,
- * added in fp32: |dG| <= 1e-5 (sum |x||w| + |b|), as for bsr_spmm. A sum with
- * fp32 values that are not finite gives NaN where plain arithmetic might give an
- * infinity.
+ * added in fp32: |dG| <= 1e-5 (sum |x||w| + |b|), as for bsr_spmm.
  */
 typedef enum {
     BSR_ACT_SILU = 0,      /* g / (1 + e^-g) */

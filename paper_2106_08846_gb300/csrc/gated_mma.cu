@@ -365,20 +365,39 @@ __device__ __forceinline__ void put_gated(const Args &a, const Job &job, int64_t
             }
         }
         if (c >= a.Fp) return;
+        // 0 past the features, whatever a row of X with an infinity makes of weights of 0
+        if (c + 8 > job.N) {
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const float2 x = unpack2(v[h][j]), y = unpack2(w[h][j]);
+                    const bool one = c + 2 * j < job.N, two = c + 2 * j + 1 < job.N;
+                    v[h][j] = pack2(one ? x.x : 0.f, two ? x.y : 0.f);
+                    w[h][j] = pack2(one ? y.x : 0.f, two ? y.y : 0.f);
+                }
+        }
 #pragma unroll
         for (int h = 0; h < 2; h++) {
             if (row + 8 * h >= job.M) continue;
             uint16_t *at = a.D + (row + 8 * h) * 2 * a.Fp + c;
             if constexpr (FAST) {
-                store8(at, 8, 16, eight_of<uint16_t>(v[h]));
-                store8(at + a.Fp, 8, 16, eight_of<uint16_t>(w[h]));
-                if (a.d_planes == 2) {   // what the rounding left
-                    auto rest = [](float x) { return x - __bfloat162float(__float2bfloat16_rn(x)); };
-#pragma unroll
-                    for (int j = 0; j < 4; j++) v[h][j] = each2(v[h][j], rest), w[h][j] = each2(w[h][j], rest);
-                    at += 2 * a.Fp * job.M;
+                if (a.d_planes == 1) {
                     store8(at, 8, 16, eight_of<uint16_t>(v[h]));
                     store8(at + a.Fp, 8, 16, eight_of<uint16_t>(w[h]));
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2; k++) {
+                        uint32_t p[4][2];
+#pragma unroll
+                        for (int j = 0; j < 4; j++) {
+                            const float2 x = unpack2(k ? w[h][j] : v[h][j]);
+                            parts_of(x.x, x.y, p[j]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 2; i++)
+                            *reinterpret_cast<uint4 *>(at + k * a.Fp + i * 2 * a.Fp * job.M) = make_uint4(p[0][i], p[1][i], p[2][i], p[3][i]);
+                    }
                 }
             } else {
 #pragma unroll
