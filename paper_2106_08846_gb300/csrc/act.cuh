@@ -96,7 +96,9 @@ __device__ __forceinline__ F2 activate_slope(F2 g, F2 &slope) {
         return mul2(g, p);
     } else if constexpr (ACT == BSR_ACT_GELU_TANH) {
         const F2 p = logistic<FAST>(gelu_2u(g)), a = mul2(g, p);
-        const F2 rise = mul2(all2(2.f * kGeluA), fma2(mul2(all2(3.f * kGeluB), g), g, one));
+        // (2u)'; where p is 0 or 1 any finite value does, and g^2 may overflow
+        const F2 x = each2(g, [](float t) { return fminf(fabsf(t), 1e4f); });
+        const F2 rise = mul2(all2(2.f * kGeluA), fma2(mul2(all2(3.f * kGeluB), x), x, one));
         slope = fma2(mul2(a, fma2(p, minus, one)), rise, p);
         return a;
     } else if constexpr (ACT == BSR_ACT_RELU) {

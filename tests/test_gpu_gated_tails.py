@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2106_08846_gb300 as bsr
-from tests.test_gpu_gated import DT
+from tests.test_gpu_gated import ACTS, DT
 
 pytestmark = pytest.mark.gpu
 # an activation in fp32: some 20 roundings at most; with the exponential for bf16 results:
@@ -61,3 +61,17 @@ def test_sigmoid_where_the_exponential_overflows(dtype):
     H, dG, dU = on_a_grid(g, "sigmoid", dtype, 40)
     want = (g > 0).double()
     assert ((H - want).abs() <= 1e-37).all() and ((dU - want).abs() <= 1e-37).all() and (dG.abs() <= 1e-37).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("N", [1, 40])
+def test_gates_whose_square_overflows(N, act, dtype):
+    """Where an activation is g, 0 or 1 and its slope 1 or 0."""
+    g = torch.tensor([-3e38, -1e25, -2e19, -1e4, 1e4, 2e19, 1e25, 3e38], device="cuda").repeat(8)
+    H, dG, dU = on_a_grid(g, act, dtype, N)
+    x = g.double()
+    value, slope = ((x > 0).double(), 0 * x) if act == "sigmoid" else (x.clamp(min=0), (x > 0).double())
+    sums = torch.where(value * N > torch.finfo(torch.float32).max, float("inf"), value)   # (dU's sum may overflow)
+    for got, want, rel in ((H, value, 2.0 ** -8), (dU, sums, 2.0 ** -19), (dG, slope, 2.0 ** -19)):
+        assert ((got == want) | ((got - want).abs() <= rel * value + 1e-37)).all(), (got[:8], want[:8])
