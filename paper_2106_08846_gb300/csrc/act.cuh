@@ -7,8 +7,9 @@
 
 namespace bsr {
 
-// e^(s x); FAST: the hardware's exponential, whose relative error of about 2^-21 is
-// lost in a result rounded to bf16.
+// e^(s x); FAST: the hardware's exponential. Its relative error, about 2^-21 and that of
+// rounding the argument, 2^-24 |s x| / ln 2 (2^-18 at 80), is lost in a result rounded
+// to bf16.
 template <bool FAST>
 __device__ __forceinline__ F2 exp_of(float s, F2 x) {
     if constexpr (!FAST) return each2(x, [s](float t) { return expf(s * t); });
@@ -38,7 +39,8 @@ constexpr float kGeluB = 0.044715f;
 // coefficients are those with the least largest error of e^(x^2 / 2) Phi(-x), taken
 // relative to it and over 1 + x: 3.2e-8 (1 + x). So a tail has as many correct bits as
 // the middle. With the exponential that the derivative takes anyway; where it has all of
-// fp32's bits, with what the rounding of g^2 left out of it.
+// fp32's bits, with what the rounding of g^2 left out of it. (fp32, 1000 tokens of 768 into
+// 2048: 34.3 us, with normcdff 38.9.)
 template <bool FAST>
 __device__ __forceinline__ F2 normal_cdf(F2 g, F2 &e) {
     const F2 x = each2(g, [](float t) { return fminf(fabsf(t), 16.f); });   // (beyond, all of it is 0 in fp32)

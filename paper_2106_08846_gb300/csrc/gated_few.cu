@@ -12,12 +12,13 @@
 // fp32: likewise, values split into the three bf16 parts whose sum they are, and a product
 // as the six part products that are not below 2^-24 of it; one token or two by
 // multiply-adds, two columns of K to an instruction and four lanes to a feature. (768 into
-// 2048: one token 4.4 us, by parts 6.6; four tokens 6.3, by parts 6.6.)
+// 2048: one token 4.5 us, two 4.7, by parts 7.3. Three and four tokens by multiply-adds
+// 6.3 there, 8.4 against 8.9 for 1024 into 4096, and 8.4 against 7.9 for 770 into 1000.)
 //
 // What bounds it: DRAM, and for small weights the time of a launch and of one read.
 // 1024 into 4096, bf16: 1 to 8 tokens 4.5 us (16.8 MB, 2.5 us at the copy rate), 16
-// tokens 6.1, 32 tokens 7.8 (the products' own kernel 9.7); fp32: 1 token 6.7 us
-// (33.6 MB, 5.0 us), 8 tokens 8.8, 32 tokens 17.2 (30.6). Four CTAs to an SM, so that
+// tokens 6.2, 32 tokens 7.8 (the products' own kernel 9.7); fp32: 1 token 6.6 us
+// (33.6 MB, 5.0 us), 3 to 8 tokens 9.0, 32 tokens 17.6 (30.6). Four CTAs to an SM, so that
 // all of them run at once: three took 0.3 us more.
 #include <algorithm>
 

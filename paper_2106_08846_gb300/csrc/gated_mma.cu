@@ -26,10 +26,10 @@
 // their K split.
 //
 // What bounds it: the MMAs, at the power limit's clocks in long runs; 1024 features
-// into 4096, bf16, 8192 tokens: forward 73 us (1.89 PFLOP/s) in calls back to back; the
-// backward pass's first product with its epilogue, which reads dH and writes dG and
-// dU, 94 us; its plain products, 275 GFLOP, 152 us (1.81 PFLOP/s, the tensor pipe busy
-// 85% of the time). Few tokens: the weights' bytes and the latency of one tile (128
+// into 4096, bf16, 8192 tokens: forward 73 us (1.89 PFLOP/s) for the kernel in short
+// runs, 85 in a long run of calls; the backward pass's first product with its epilogue,
+// which reads dH and writes dG and dU, 94 us; its plain products, 275 GFLOP, 147 us
+// (1.87 PFLOP/s, the tensor pipe busy 84% of the time). Few tokens: the weights' bytes and the latency of one tile (128
 // tokens of 768 into 2048 9 us). fp32 forward, 1000 tokens of 768 into 2048: 34 us,
 // 19.6 at six part products of bf16 each, the rest laying out the operands and, with
 // one tile a pair, its start and epilogue.

@@ -1,5 +1,7 @@
 // C entry points of the operators beside the product (include/bsr.h): argument
-// checks and launches on the current device. They keep nothing between calls.
+// checks and launches on the current device. They keep nothing between calls but the
+// gated block's choice of tiles for the last few sizes, per thread, and the device's
+// status word, until bsr_check_status.
 #include <algorithm>
 #include <cmath>
 

@@ -9,8 +9,7 @@
 // from h' before h' is rounded. Arithmetic is on pairs of features.
 //
 // Forward, up to 1024 features a row is one warp's: no barriers, every load of the
-// row on its way at once. Wider rows are a group of threads', eight or sixteen
-// features each.
+// row on its way at once. Wider rows are a group of threads', sixteen features each.
 //
 // What bounds it: DRAM (y and h in, h' and z out) and, with more parameters, L1, from
 // which they are read. 16384 x 1024 bf16: one RMSNorm 21.4 us, 134 MB at 92% of the copy
@@ -18,7 +17,8 @@
 // and a gate 34.7 us, 57%. 16384 x 768 fp32, LayerNorms with biases 41 us, 72%; 4096 x
 // 4096 bf16, RMSNorms 26 us, 75%. One row of 1024: 2.5 us, the launch and one read's
 // latency. Rows that are no runs of eight on 16-byte boundaries pay for shifting them
-// into place and for stores of single words (5000 x 1193 bf16: 22%).
+// into place and for stores of single words (5000 x 1193 bf16: one RMSNorm 17.5 us, 40%,
+// two LayerNorms with biases, scale and gate 32 us, 22%; 16384 x 1023 fp32 72% and 46%).
 #include <algorithm>
 #include <type_traits>
 

@@ -175,8 +175,9 @@ __device__ __forceinline__ float *stage() {
 }
 // By whole warps. ANY: a warp's fp32 runs, which are contiguous, change lanes through
 // shared memory, so that an instruction's stores lie side by side: a lane's eight
-// values one by one cost a write of their 32-byte sector each (3000 x 771 fp32 30.0 us,
-// so 26.3). bf16 runs go in four stores and lose by the detour (5000 x 1193 32.3 and 34.9).
+// values one by one cost a write of their 32-byte sector each (3000 x 771 fp32, one norm
+// 21.5 us, so 15.6; 16384 x 1023 114 and 55). bf16 runs go in four stores and gain nothing
+// by the detour.
 template <typename T, int L, int WARPS>
 __device__ __forceinline__ void store_run(T *row, int D, int i, int t, int NT, const Run &r) {
     const int lane = threadIdx.x & 31, left = D - feature(i, 0, t, NT);   // values of the row from this lane's on
