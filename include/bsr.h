@@ -42,8 +42,8 @@
  *    MB + 1, KB and nnzb below 2^31.
  *  - One handle must not run bsr_spmm on two streams at once (the split-row
  *    workspace and staging buffers belong to the handle).
- *  - bsr_residual_norm, bsr_gated and their backward calls have no handle: they
- *    work on the current device and keep nothing between calls but the choice of
+ *  - bsr_residual_norm, bsr_gated and their backward calls, bsr_expert_* and bsr_fp8_*
+ *    have no handle: they work on the current device and keep nothing between calls but the choice of
  *    tiles for the last 16 sizes (per thread; a size that is not among them costs a
  *    forward call of the gated block 0.5 us more, a backward call 5 to 14, one of
  *    65536 tokens 22). Scratch memory is the caller's, a buffer to each call in
@@ -443,8 +443,140 @@ bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, c
                                 int64_t K, bsr_dtype_t dt, bsr_act_t act, void *ws, size_t ws_bytes, void *stream);
 
 /*
+ * ---- Rows sorted by expert
+ *
+ * A layer of E experts sends every token to k of them. Sorted by expert, an
+ * expert's tokens are one run of rows, which one product takes (bsr_fp8_product
+ * with groups, or bsr_gated on the run); the results are added up again with the
+ * router's weights:
+ *
+ *   c_e = number of choices of expert e,  offsets[0] = 0,
+ *   offsets[e + 1] = offsets[e] + align * ceil(c_e / align)
+ *   place[n, j]  = offsets[e] + the number of earlier choices of e, in the order
+ *                  of n k + j; -1 if the choice is no expert (outside 0 .. E - 1)
+ *   source[r]    = the n k + j of row r, -1 where there is none
+ *   Xs[r] = X[source[r] / k], zeros in the rows of an expert's run behind its last
+ *   Y[n]  = sum_j weights[n, j] Ys[place[n, j]]     (j with a place only)
+ */
+typedef struct {
+    int64_t N;         /* tokens, below 2^30 */
+    int64_t R;         /* rows of source, Xs and Ys: at least bsr_expert_capacity's, below 2^31 */
+    int k, E, align;   /* 1 .. 64 choices of a token, 1 .. 1024 experts, 1 .. 1024 */
+    int32_t *offsets;  /* device [E + 1] */
+    int32_t *place;    /* device [N, k] */
+    int32_t *source;   /* device [R] */
+} bsr_experts_t;
+
+/* The rows that N tokens take at most: the least R of bsr_experts_t. */
+bsr_status_t bsr_expert_capacity(int64_t N, int k, int E, int align, int64_t *rows);
+
+/*
+ * bsr_expert_order -- offsets, place and source from each token's choices.
+ *
+ * experts  device int32 [N, k]; a value outside 0 .. E - 1 is a dropped choice, an
+ *          expert may be chosen twice. R below the capacity: BSR_ERR_CAPACITY.
+ * Nothing is read back: the arrays are used on the device by the calls below and
+ * by bsr_fp8_product. Asynchronous on `stream`; allocates nothing. Same input, same bits.
+ */
+bsr_status_t bsr_expert_order(const bsr_experts_t *p, const int32_t *experts, void *stream);
+
+/*
+ * bsr_expert_rows -- Xs [R, D] from X [N, D] (device, 16-byte aligned, type dt,
+ * D in 1 .. 2^20, D R below 2^38).
+ * Rows from offsets[E] on are left as they were. Its gradient is bsr_expert_sum of
+ * dXs without weights. Entries of place outside 0 .. R - 1 are not sent, here and
+ * in the calls below. N == 0 is a no-op. Nothing overlaps.
+ */
+bsr_status_t bsr_expert_rows(const bsr_experts_t *p, const void *X, void *Xs, int64_t D, bsr_dtype_t dt, void *stream);
+
+/*
+ * bsr_expert_sum -- Y [N, D] from Ys [R, D]; weights: device fp32 [N, k], or NULL for
+ * 1. Sums in fp32, in the order of j, rounded once; a token without a place gets
+ * zeros. Rows that no choice has are not read.
+ */
+bsr_status_t bsr_expert_sum(const bsr_experts_t *p, const void *Ys, const float *weights, void *Y, int64_t D, bsr_dtype_t dt,
+                            void *stream);
+
+/*
+ * bsr_expert_sum_backward -- dYs[place[n, j]] = weights[n, j] dY[n], zeros in an
+ * expert's rows behind its last, and dweights[n, j] = the product of dY[n] and
+ * Ys[place[n, j]] summed over features (0 without a place). dYs or dweights may be
+ * NULL; dweights needs weights and Ys (else unused). Rows from offsets[E] on are left as they were.
+ */
+bsr_status_t bsr_expert_sum_backward(const bsr_experts_t *p, const void *Ys, const float *weights, const void *dY, void *dYs,
+                                     float *dweights, int64_t D, bsr_dtype_t dt, void *stream);
+
+/*
+ * ---- Products in 8-bit floating point
+ *
+ * An operand is a matrix of 8-bit values with an fp32 scale for each block of 128
+ * columns (the axis that the product sums over) of a row, or of 128 rows:
+ *
+ *   x[r, c] is q[r, c] * scale[c / 128, r / tile]
+ *
+ * Y = a b' + bias:  Y[n, m] = bias[m] + sum_k a[n, k] b[m, k], the sum of a block in
+ * the tensor cores' fp32 accumulators, blocks scaled and added in fp32.
+ * A layer X W': a = X by rows, b = W by rows with tiles of 128. Its gradients:
+ * dX = dY W: b = W by columns; dW = dY' X: a = dY and b = X, both by columns.
+ */
+typedef enum { BSR_E4M3 = 0, BSR_E5M2 = 1 } bsr_fp8_t;
+typedef struct {
+    int64_t batch;         /* matrices, one behind the other; 1 but for the weights of experts */
+    int64_t rows, cols;    /* below 2^31; batch * rows * (cols rounded up to 128) up to 2^38 */
+    int tile;              /* rows that share a scale: 1 or 128 */
+    bsr_fp8_t type;
+    void *q;               /* device, 16-byte aligned: [batch, rows, cols rounded up to 128], zeros past cols */
+    float *scale;          /* device [batch, ceil(cols / 128), ceil(rows / tile)] */
+} bsr_fp8_matrix_t;
+
+/*
+ * bsr_fp8_quantize -- x [batch, R, C] (device, 16-byte aligned, type dt) in 8 bits.
+ *
+ * rows     [batch, R, C]: blocks along C. columns: [batch, C, R], x transposed, blocks
+ *          along R. Either may be NULL; with both, their batch, tile and type agree.
+ * A block's scale is the least power of two that brings its largest |x| to at most
+ * 448 (e4m3) or 57344 (e5m2), at least 2^-126; 1 for a block of zeros. So each value is rounded
+ * once, to nearest even. Values that are not finite become NaN, and do not count
+ * for the scale.
+ * used     device int32 [1], or NULL for R (batch 1): rows of x from *used on are not read
+ *          and count as zeros of a block; in rows, they and their scales are left as they
+ *          were, in columns the blocks of 128 that begin at or after *used.
+ * Asynchronous on `stream`; allocates nothing. Nothing overlaps.
+ */
+bsr_status_t bsr_fp8_quantize(const void *x, bsr_dtype_t dt, const bsr_fp8_matrix_t *rows, const bsr_fp8_matrix_t *columns,
+                              const int32_t *used, void *stream);
+
+typedef enum {
+    BSR_GROUP_NONE = 0,
+    BSR_GROUP_ROWS = 1,     /* rows offsets[e] .. offsets[e + 1] - 1 of a meet b's matrix e */
+    BSR_GROUP_COLUMNS = 2   /* Y[e] sums over the columns offsets[e] .. offsets[e + 1] - 1, multiples of 128 */
+} bsr_group_t;
+
+/* Bytes of workspace of a product; may be 0. a and b: their sizes, no arrays. */
+bsr_status_t bsr_fp8_product_workspace(const bsr_fp8_matrix_t *a, const bsr_fp8_matrix_t *b, bsr_dtype_t dt, bsr_group_t group,
+                                       int64_t groups, size_t *bytes);
+
+/*
+ * bsr_fp8_product -- Y = a b' + bias.
+ *
+ * a, b     of as many columns; types may differ; a.batch is 1.
+ * Y        device, 16-byte aligned, type dt: [a.rows, b.rows], by BSR_GROUP_COLUMNS
+ *          [groups, a.rows, b.rows]. Overlaps nothing.
+ * bias     device fp32 [b.batch, b.rows], or NULL; not by BSR_GROUP_COLUMNS.
+ * groups   1 .. 1024 experts, offsets: device int32 [groups + 1], ascending, within a's rows
+ *          (columns, where 128 columns from a multiple of 128 are taken or left as a whole); read on the device.
+ *          BSR_GROUP_ROWS: b.batch is groups; rows in no expert's run are left as they were.
+ *          BSR_GROUP_NONE: offsets NULL, groups unused, b.batch 1.
+ * ws       device, 16-byte aligned, of at least the bytes that bsr_fp8_product_workspace
+ *          gives (else BSR_ERR_CAPACITY); used until the call's kernels have run.
+ * Asynchronous on `stream`; allocates nothing. Same input, same bits.
+ */
+bsr_status_t bsr_fp8_product(const bsr_fp8_matrix_t *a, const bsr_fp8_matrix_t *b, const float *bias, void *Y, bsr_dtype_t dt,
+                             bsr_group_t group, const int32_t *offsets, int64_t groups, void *ws, size_t ws_bytes, void *stream);
+
+/*
  * bsr_check_status -- synchronise the current device and return the first error
- * that a kernel of bsr_gated or bsr_gated_backward recorded there
+ * that a kernel of bsr_gated, bsr_gated_backward or bsr_fp8_product recorded there
  * (BSR_ERR_TIMEOUT when a bounded wait gave up), then clear it. BSR_OK if none.
  */
 bsr_status_t bsr_check_status(void);

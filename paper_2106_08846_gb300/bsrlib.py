@@ -41,6 +41,13 @@ BSR_NORM_NONE = 0
 BSR_NORM_LAYER = 1
 BSR_NORM_RMS = 2
 
+BSR_E4M3 = 0
+BSR_E5M2 = 1
+
+BSR_GROUP_NONE = 0
+BSR_GROUP_ROWS = 1
+BSR_GROUP_COLUMNS = 2
+
 BSR_ACT_SILU = 0
 BSR_ACT_GELU = 1
 BSR_ACT_GELU_TANH = 2
@@ -50,6 +57,9 @@ BSR_ACT_SIGMOID = 4
 _ACT = {"silu": BSR_ACT_SILU, "gelu": BSR_ACT_GELU, "gelu_tanh": BSR_ACT_GELU_TANH, "relu": BSR_ACT_RELU,
         "sigmoid": BSR_ACT_SIGMOID}
 _NORM = {"none": BSR_NORM_NONE, "layer": BSR_NORM_LAYER, "rms": BSR_NORM_RMS}
+
+_FP8 = {"e4m3": BSR_E4M3, "e5m2": BSR_E5M2}
+_FP8_TYPE = {"e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2}
 
 _lib = None
 
@@ -66,6 +76,18 @@ class _ResidualNorm(ctypes.Structure):
 class _ResidualNormGrads(ctypes.Structure):
     """bsr_residual_norm_grads_t"""
     _fields_ = [(k, ctypes.c_void_p) for k in ("dgate", "dscale", "dpost_w", "dpost_b", "dpre_w", "dpre_b")]
+
+
+class _Experts(ctypes.Structure):
+    """bsr_experts_t"""
+    _fields_ = [("N", ctypes.c_int64), ("R", ctypes.c_int64), ("k", ctypes.c_int), ("E", ctypes.c_int), ("align", ctypes.c_int),
+                ("offsets", ctypes.c_void_p), ("place", ctypes.c_void_p), ("source", ctypes.c_void_p)]
+
+
+class _Fp8Matrix(ctypes.Structure):
+    """bsr_fp8_matrix_t"""
+    _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("tile", ctypes.c_int),
+                ("type", ctypes.c_int), ("q", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class BsrError(RuntimeError):
@@ -127,6 +149,23 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
         lib.bsr_gated.restype = U
         lib.bsr_gated_backward.argtypes = [P] * 11 + [I64, I64, I64, U, I, P, ctypes.c_size_t, P]
         lib.bsr_gated_backward.restype = U
+        EX, M8, SIZE = ctypes.POINTER(_Experts), ctypes.POINTER(_Fp8Matrix), ctypes.c_size_t
+        lib.bsr_expert_capacity.argtypes = [I64, I, I, I, ctypes.POINTER(I64)]
+        lib.bsr_expert_capacity.restype = U
+        lib.bsr_expert_order.argtypes = [EX, P, P]
+        lib.bsr_expert_order.restype = U
+        lib.bsr_expert_rows.argtypes = [EX, P, P, I64, U, P]
+        lib.bsr_expert_rows.restype = U
+        lib.bsr_expert_sum.argtypes = [EX, P, P, P, I64, U, P]
+        lib.bsr_expert_sum.restype = U
+        lib.bsr_expert_sum_backward.argtypes = [EX, P, P, P, P, P, I64, U, P]
+        lib.bsr_expert_sum_backward.restype = U
+        lib.bsr_fp8_quantize.argtypes = [P, U, M8, M8, P, P]
+        lib.bsr_fp8_quantize.restype = U
+        lib.bsr_fp8_product_workspace.argtypes = [M8, M8, U, U, I64, ctypes.POINTER(SIZE)]
+        lib.bsr_fp8_product_workspace.restype = U
+        lib.bsr_fp8_product.argtypes = [M8, M8, P, P, U, U, P, I64, P, SIZE, P]
+        lib.bsr_fp8_product.restype = U
         lib.bsr_check_status.argtypes = []
         lib.bsr_check_status.restype = U
         lib.bsr_destroy.argtypes = [P]
@@ -434,7 +473,8 @@ def bsr_check_device_status(h: Handle) -> int:
 
 
 def bsr_check_status() -> int:
-    """The first error that a kernel of bsr_gated or bsr_gated_backward recorded on the current device (synchronises it)."""
+    """The first error that a kernel of bsr_gated, bsr_gated_backward or bsr_fp8_product recorded on the current device
+    (synchronises it)."""
     return load().bsr_check_status()
 
 
@@ -663,6 +703,209 @@ def bsr_gated_backward(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, bg: 
     if status:
         _check(status, "bsr_gated_backward")
     return out
+
+
+class ExpertOrder:
+    """Which rows N tokens' k choices of E experts have (bsr_expert_order fills it in):
+    `offsets` [E + 1], `place` [N, k] and `source` [rows], int32 on the device; see
+    include/bsr.h. `rows` is what the sorted tensors must have; `used` is a view of
+    the number that is in use, offsets[E]."""
+
+    def __init__(self, N: int, k: int, E: int, align: int = 1, device="cuda"):
+        rows = ctypes.c_int64(0)
+        _check(load().bsr_expert_capacity(N, k, E, align, ctypes.byref(rows)), "bsr_expert_capacity")
+        self.N, self.k, self.E, self.align, self.rows = N, k, E, align, rows.value
+        self._offsets = torch.empty(E + 1, dtype=torch.int32, device=device)
+        self._place = torch.empty((N, k), dtype=torch.int32, device=device)
+        self._source = torch.empty(self.rows, dtype=torch.int32, device=device)
+        self._used = self._offsets[E:]
+        self._c = _Experts(N, self.rows, k, E, align, _ptr(self._offsets), _ptr(self._place) if N else None,
+                           _ptr(self._source) if self.rows else None)
+
+    # (not to be replaced: the calls have their addresses)
+    offsets = property(lambda self: self._offsets)
+    place = property(lambda self: self._place)
+    source = property(lambda self: self._source)
+    used = property(lambda self: self._used)
+
+
+def bsr_expert_order(experts: torch.Tensor, E: int, align: int = 1, order: Optional[ExpertOrder] = None, stream=None) -> ExpertOrder:
+    """The order of the tokens' choices `experts` [N, k] (int32; a value outside
+    0 .. E - 1 is a dropped choice), each expert's rows from a multiple of `align` on.
+    Fills `order` if given. Nothing is read back to the host."""
+    if experts.dim() != 2:
+        raise ValueError("experts must be [N, k]")
+    N, k = experts.shape
+    if not _is_rows(experts, experts.shape, torch.int32):
+        _check_rows("experts", experts, experts.shape, torch.int32)
+    if order is None:
+        order = ExpertOrder(N, k, E, align, experts.device)
+        _lend(stream, experts.device, order.offsets, order.place, order.source)
+    elif (order.N, order.k, order.E, order.align) != (N, k, E, align):
+        raise ValueError("order is of other sizes")
+    status = _lib.bsr_expert_order(order._c, experts.data_ptr(), _stream(stream))
+    if status:
+        _check(status, "bsr_expert_order")
+    return order
+
+
+def _check_sorted(order: ExpertOrder, **tensors) -> None:
+    """Tensors of one type, each (rows, tensor or None) and of as many features."""
+    given = [(name, n, t) for name, (n, t) in tensors.items() if t is not None]
+    shape, dt = given[0][2].shape, given[0][2].dtype
+    if len(shape) != 2:
+        raise ValueError(f"{given[0][0]} must be [{given[0][1]}, D]")
+    for name, n, t in given:
+        if not _is_rows(t, (n, shape[1]), dt):
+            _check_rows(name, t, (n, shape[1]), dt)
+
+
+def _made(t: Optional[torch.Tensor], rows: int, like: torch.Tensor, stream) -> torch.Tensor:
+    if t is None:
+        t = torch.empty((rows, like.shape[1]), dtype=like.dtype, device=like.device)
+        _lend(stream, like.device, t)
+    return t
+
+
+def bsr_expert_rows(X: torch.Tensor, order: ExpertOrder, Xs: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Xs [order.rows, D]: the tokens' rows X [N, D] in the experts' order, zeros behind
+    an expert's last one; rows from order.used on are left as they were (of an Xs
+    that the call makes: without a value). Its gradient is bsr_expert_sum without weights."""
+    _check_sorted(order, X=(order.N, X), Xs=(order.rows, Xs))
+    dt = dtype_code(X.dtype)
+    Xs = _made(Xs, order.rows, X, stream)
+    status = _lib.bsr_expert_rows(order._c, X.data_ptr(), Xs.data_ptr(), X.shape[1], dt, _stream(stream))
+    if status:
+        _check(status, "bsr_expert_rows")
+    return Xs
+
+
+def bsr_expert_sum(Ys: torch.Tensor, order: ExpertOrder, weights: Optional[torch.Tensor] = None, Y: Optional[torch.Tensor] = None,
+                   stream=None) -> torch.Tensor:
+    """Y [N, D]: for each token the sum of its choices' rows of Ys [order.rows, D], with
+    the router's weights (fp32 [N, k], None: 1)."""
+    _check_sorted(order, Ys=(order.rows, Ys), Y=(order.N, Y))
+    dt = dtype_code(Ys.dtype)
+    _check_rows("weights", weights, (order.N, order.k), torch.float32)
+    Y = _made(Y, order.N, Ys, stream)
+    status = _lib.bsr_expert_sum(order._c, Ys.data_ptr(), _ptr(weights), Y.data_ptr(), Ys.shape[1], dt, _stream(stream))
+    if status:
+        _check(status, "bsr_expert_sum")
+    return Y
+
+
+def bsr_expert_sum_backward(Ys: Optional[torch.Tensor], order: ExpertOrder, weights: Optional[torch.Tensor], dY: torch.Tensor,
+                            dYs: Optional[torch.Tensor] = None, stream=None) -> dict:
+    """Gradients of bsr_expert_sum: "dYs" (rows from order.used on as in bsr_expert_rows),
+    and "dweights" where weights are given; without them Ys is not needed."""
+    _check_sorted(order, dY=(order.N, dY), Ys=(order.rows, Ys), dYs=(order.rows, dYs))
+    dt = dtype_code(dY.dtype)
+    _check_rows("weights", weights, (order.N, order.k), torch.float32)
+    if weights is not None and Ys is None:
+        raise ValueError("the gradient of the weights needs Ys")
+    out = {"dYs": _made(dYs, order.rows, dY, stream)}
+    if weights is not None:
+        out["dweights"] = torch.empty_like(weights)
+        _lend(stream, dY.device, out["dweights"])
+    status = _lib.bsr_expert_sum_backward(order._c, _ptr(Ys), _ptr(weights), dY.data_ptr(), out["dYs"].data_ptr(),
+                                          _ptr(out.get("dweights")), dY.shape[1], dt, _stream(stream))
+    if status:
+        _check(status, "bsr_expert_sum_backward")
+    return out
+
+
+class Fp8Matrix:
+    """[rows, cols] values in 8 bits (batch: that many, of shape [batch, rows, cols]) with
+    a scale for each block of 128 columns of `tile` rows: x[r, c] is
+    q[r, c] * scale[c // 128, r // tile]. `q` has cols rounded up to 128, zeros past
+    them. fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
+
+    def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda"):
+        if fmt not in _FP8 or tile not in (1, 128):
+            raise ValueError("fmt is 'e4m3' or 'e5m2', tile 1 or 128")
+        self.rows, self.cols, self.tile, self.fmt, self.batch = rows, cols, tile, fmt, batch
+        each, blocks = () if batch is None else (batch,), -(-cols // 128)
+        self._q = torch.empty((*each, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
+        self._scale = torch.empty((*each, blocks, -(-rows // tile)), dtype=torch.float32, device=device)
+        full = self._q.numel() > 0
+        self._c = _Fp8Matrix(1 if batch is None else batch, rows, cols, tile, _FP8[fmt], _ptr(self._q) if full else None,
+                             _ptr(self._scale) if full else None)
+
+    # (to be filled, not replaced: the calls have their addresses)
+    q = property(lambda self: self._q)
+    scale = property(lambda self: self._scale)
+
+
+def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: str = "rows", used: Optional[torch.Tensor] = None,
+                     out=None, stream=None):
+    """x [R, C] (or a batch of them) in 8 bits, with the least power of two that fits as
+    each block's scale. form "rows": as it lies, an Fp8Matrix of [R, C]; "columns":
+    transposed, of [C, R], its blocks along R (an operand of a product that sums over
+    rows); "both": the two, from one reading. tile 128: blocks of 128 x 128, as for
+    weights. used (device int32 [1], as ExpertOrder.used): rows from there on are not
+    read. `out`: what to fill, as it would be returned."""
+    if form not in ("rows", "columns", "both"):
+        raise ValueError("form is 'rows', 'columns' or 'both'")
+    if x.dim() not in (2, 3) or not x.is_contiguous():
+        raise ValueError("x must be contiguous, [R, C] or [batch, R, C]")
+    dt = dtype_code(x.dtype)
+    batch = x.shape[0] if x.dim() == 3 else None
+    R, C = x.shape[-2:]
+    _check_rows("used", used, (1,), torch.int32)
+    sizes = [(R, C)] if form == "rows" else [(C, R)] if form == "columns" else [(R, C), (C, R)]
+    if out is None:
+        m = [Fp8Matrix(r, c, tile, fmt, batch, x.device) for r, c in sizes]
+        for f in m:
+            _lend(stream, x.device, f.q, f.scale)
+    else:
+        m = list(out) if form == "both" else [out]
+        if [(f.rows, f.cols, f.tile, f.fmt, f.batch) for f in m] != [(r, c, tile, fmt, batch) for r, c in sizes]:
+            raise ValueError("out is of other sizes")
+    rows, columns = (m[0], None) if form == "rows" else (None, m[0]) if form == "columns" else m
+    status = (_lib or load()).bsr_fp8_quantize(x.data_ptr() if x.numel() else None, dt, rows and rows._c, columns and columns._c,
+                                               _ptr(used), _stream(stream))
+    if status:
+        _check(status, "bsr_fp8_quantize")
+    return m[0] if len(m) == 1 else tuple(m)
+
+
+def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
+                    offsets: Optional[torch.Tensor] = None, over: str = "rows", Y: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Y [a.rows, b.rows] = a b' + bias, of `dtype` (or that of a given Y).
+    offsets (int32 [E + 1] on the device, as ExpertOrder.offsets): over "rows", b is a
+    batch of E matrices and each run of a's rows meets its expert's (bias [E, b.rows];
+    rows in no run are left as they were); over "columns", Y [E, a.rows, b.rows] has a
+    sum over each run of columns, whose offsets are multiples of 128."""
+    if over not in ("rows", "columns"):
+        raise ValueError("over is 'rows' or 'columns'")
+    dtype = dtype if Y is None else Y.dtype
+    dt = dtype_code(dtype)
+    if offsets is None:
+        group, E = BSR_GROUP_NONE, 0
+    else:
+        E = offsets.shape[0] - 1
+        _check_rows("offsets", offsets, (E + 1,), torch.int32)
+        group = BSR_GROUP_ROWS if over == "rows" else BSR_GROUP_COLUMNS
+    if a.batch is not None or b.batch != (E if group == BSR_GROUP_ROWS else None):
+        raise ValueError("a is one matrix, b one for each expert by rows, else one")
+    _check_rows("bias", bias, (b.rows,) if b.batch is None else (E, b.rows), torch.float32)
+    shape = (E, a.rows, b.rows) if group == BSR_GROUP_COLUMNS else (a.rows, b.rows)
+    if Y is None:
+        Y = torch.empty(shape, dtype=dtype, device=a.q.device)
+        _lend(stream, Y.device, Y)
+    else:
+        _check_rows("Y", Y, shape, dtype)
+    lib, n = _lib or load(), ctypes.c_size_t(0)
+    status = lib.bsr_fp8_product_workspace(a._c, b._c, dt, group, E, ctypes.byref(n))
+    if status:
+        _check(status, "bsr_fp8_product_workspace")
+    ws = _workspace(n.value, Y.device, stream)
+    status = lib.bsr_fp8_product(a._c, b._c, _ptr(bias), Y.data_ptr() if Y.numel() else None, dt, group, _ptr(offsets), E, _ptr(ws),
+                                 n.value, _stream(stream))
+    if status:
+        _check(status, "bsr_fp8_product")
+    return Y
 
 
 def parse_schedule(text: str) -> dict:

@@ -1,0 +1,325 @@
+// Tokens sorted by expert and added up again with the router's weights.
+//
+//   c_e = #{(n, j): x_nj = e},  o_0 = 0,  o_{e+1} = o_e + align ceil(c_e / align)
+//   place[n, j] = o_e + the rank of (n, j) among the choices of e = x_nj
+//   Xs[place[n, j]] = X[n];   Y[n] = sum_j w_nj Ys[place[n, j]]
+//
+// Order: one launch. A warp takes a contiguous run of the choices twice, 32 at a
+// time: lanes with equal experts find each other, the first adds their number to
+// the warp's count of that expert (no atomics: the order is by index, the same in
+// every call). Between the passes the counts of the warps, and of a cluster's CTAs
+// through distributed shared memory, become first rows.
+//
+// Rows and sums: one pass over the data, a warp to a token's 2 KB (backward: to a
+// choice's row). What bounds them: DRAM.
+#include <algorithm>
+#include <atomic>
+
+#include "elem.cuh"
+#include "experts.h"
+#include "launch.cuh"
+#include "ptx.cuh"
+
+namespace bsr {
+
+namespace {
+
+constexpr int kOrderThreads = 1024, kWarps = kOrderThreads / 32;
+
+__device__ __forceinline__ int32_t load_cluster(uint32_t addr) {
+    int32_t v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// Dynamic shared memory: counts[warps][E], then totals of this CTA [E], of all [E], first rows [E].
+__global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_constant__ bsr_experts_t p, const int32_t *experts,
+                                                                   unsigned ctas) {
+    extern __shared__ int32_t words[];
+    __shared__ int32_t sums[kWarps];
+    const int E = p.E, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int32_t *count = words, *mine = words + kWarps * E, *all = mine + E, *first = all + E;
+    const uint32_t rank = ctas > 1 ? ptx::cluster_rank() : 0;
+    const int64_t pairs = p.N * p.k, warps = (int64_t)ctas * kWarps, per = ((pairs + warps - 1) / warps + 31) / 32 * 32;
+    const int64_t lo = min(pairs, (rank * kWarps + warp) * per), hi = min(pairs, lo + per);
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    for (int i = threadIdx.x; i < kWarps * E; i += kOrderThreads) count[i] = 0;
+    __syncthreads();
+    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
+        const int64_t i = i0 + lane;
+        const int32_t x = i < hi ? __ldg(experts + i) : -1;
+        const bool is = (uint32_t)x < (uint32_t)E;
+        const uint32_t same = __match_any_sync(0xffffffffu, is ? x : -1);
+        if (is && lane == __ffs((int)same) - 1) count[warp * E + x] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    const int e = threadIdx.x;
+    if (e < E) {   // the warps' counts become what the warps before have
+        int32_t run = 0;
+        for (int w = 0; w < kWarps; w++) {
+            const int32_t c = count[w * E + e];
+            count[w * E + e] = run;
+            run += c;
+        }
+        mine[e] = run;
+    }
+    if (ctas > 1) ptx::cluster_barrier();
+    else __syncthreads();
+    int32_t before = 0, total = 0;
+    if (e < E) {
+        for (uint32_t r = 0; r < ctas; r++) {
+            const int32_t c = r == rank ? mine[e] : load_cluster(ptx::map_to_cta(mine + e, r));
+            before += r < rank ? c : 0;
+            total += c;
+        }
+    }
+    const int32_t padded = (total + p.align - 1) / p.align * p.align;
+    int32_t upto = padded;   // inclusive sums: of the warp's experts, then of the warps'
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int32_t v = __shfl_up_sync(0xffffffffu, upto, d);
+        if (lane >= d) upto += v;
+    }
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    if (warp == 0) {
+        int32_t v = sums[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int32_t u = __shfl_up_sync(0xffffffffu, v, d);
+            if (lane >= d) v += u;
+        }
+        sums[lane] = v;
+    }
+    __syncthreads();
+    const int32_t used = sums[kWarps - 1];
+    if (e < E) {
+        const int32_t at = upto - padded + (warp ? sums[warp - 1] : 0);
+        all[e] = total;
+        first[e] = at;
+        for (int w = 0; w < kWarps; w++) count[w * E + e] += at + before;
+        if (rank == 0) p.offsets[e] = at;
+    }
+    if (rank == 0 && threadIdx.x == 0) p.offsets[E] = used;
+    __syncthreads();
+    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
+        const int64_t i = i0 + lane;
+        const int32_t x = i < hi ? __ldg(experts + i) : -1;
+        const bool is = (uint32_t)x < (uint32_t)E;
+        const uint32_t same = __match_any_sync(0xffffffffu, is ? x : -1);
+        const int32_t row = is ? count[warp * E + x] + __popc(same & ((1u << lane) - 1)) : -1;
+        __syncwarp();
+        if (is && lane == __ffs((int)same) - 1) count[warp * E + x] += __popc(same);
+        __syncwarp();
+        if (i < hi) p.place[i] = row;
+        if (is) p.source[row] = (int32_t)i;
+    }
+    // rows that nobody was sent to: behind an expert's, and behind the last one's
+    for (int f = (int)rank * kWarps + warp; f < E; f += (int)ctas * kWarps) {
+        const int32_t end = f + 1 < E ? first[f + 1] : used;
+        for (int32_t r = first[f] + all[f] + lane; r < end; r += 32) p.source[r] = -1;
+    }
+    for (int64_t r = used + (int64_t)rank * kOrderThreads + threadIdx.x; r < p.R; r += (int64_t)ctas * kOrderThreads) p.source[r] = -1;
+    if (ctas > 1) ptx::cluster_barrier();   // nobody reads this CTA's counts any more
+}
+
+// ---- rows in words of 2 to 16 bytes, as their addresses allow
+
+template <typename T, typename W>
+struct Word {
+    static constexpr int n = sizeof(W) / sizeof(T);
+    union {
+        W w;
+        T v[n];
+    };
+};
+
+constexpr int kWords = 4;   // of a row, a lane holds at once
+
+__device__ __forceinline__ int32_t row_of(const bsr_experts_t &p, int64_t pair) {
+    const int32_t r = __ldg(p.place + pair);
+    return r >= 0 && r < p.R ? r : -1;   // (rows out of range: not sent)
+}
+
+// Zeros in the rows below offsets[E] that nobody was sent to, 32 rows to the warp.
+template <typename W>
+__device__ __forceinline__ void zero_rows(const bsr_experts_t &p, W *out, int64_t words, int64_t first) {
+    const int lane = threadIdx.x & 31;
+    const int64_t used = min((int64_t)__ldg(p.offsets + p.E), p.R), r = first + lane;
+    uint32_t mask = __ballot_sync(0xffffffffu, r < used && __ldg(p.source + r) < 0);
+    while (mask) {
+        W *row = out + (first + __ffs((int)mask) - 1) * words;
+        mask &= mask - 1;
+        for (int64_t w = lane; w < words; w += 32) row[w] = W{};
+    }
+}
+
+template <typename W>
+__global__ void __launch_bounds__(256) k_expert_rows(const __grid_constant__ bsr_experts_t p, const W *X, W *Xs, int64_t words,
+                                                     int64_t parts) {
+    const int lane = threadIdx.x & 31;
+    const int64_t copies = p.N * parts, units = copies + (p.R + 31) / 32;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
+        if (u >= copies) {
+            zero_rows(p, Xs, words, (u - copies) * 32);
+            continue;
+        }
+        const int64_t n = u / parts, at = (u - n * parts) * 32 * kWords + lane;
+        W x[kWords];
+#pragma unroll
+        for (int v = 0; v < kWords; v++)
+            if (at + 32 * v < words) x[v] = __ldg(X + n * words + at + 32 * v);
+        for (int j = 0; j < p.k; j++) {
+            const int64_t r = row_of(p, n * p.k + j);
+            if (r < 0) continue;
+#pragma unroll
+            for (int v = 0; v < kWords; v++)
+                if (at + 32 * v < words) Xs[r * words + at + 32 * v] = x[v];
+        }
+    }
+}
+
+template <typename T, typename W>
+__global__ void __launch_bounds__(256) k_expert_sum(const __grid_constant__ bsr_experts_t p, const W *Ys, const float *weights, W *Y,
+                                                    int64_t words, int64_t parts) {
+    constexpr int n_w = Word<T, W>::n;
+    const int lane = threadIdx.x & 31;
+    const int64_t units = p.N * parts;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
+        const int64_t n = u / parts, at = (u - n * parts) * 32 * kWords + lane;
+        float sum[kWords][n_w] = {};
+        for (int j = 0; j < p.k; j++) {
+            const int64_t r = row_of(p, n * p.k + j);
+            if (r < 0) continue;
+            const float w = weights ? __ldg(weights + n * p.k + j) : 1.f;
+#pragma unroll
+            for (int v = 0; v < kWords; v++) {
+                if (at + 32 * v >= words) break;
+                Word<T, W> y;
+                y.w = __ldg(Ys + r * words + at + 32 * v);
+#pragma unroll
+                for (int i = 0; i < n_w; i++) sum[v][i] = fmaf(w, to_f32(y.v[i]), sum[v][i]);
+            }
+        }
+#pragma unroll
+        for (int v = 0; v < kWords; v++) {
+            if (at + 32 * v >= words) break;
+            Word<T, W> y;
+#pragma unroll
+            for (int i = 0; i < n_w; i++) y.v[i] = from_f32<T>(sum[v][i]);
+            Y[n * words + at + 32 * v] = y.w;
+        }
+    }
+}
+
+// dYs = w dY, dw = <Ys, dY>: a warp to a choice.
+template <typename T, typename W>
+__global__ void __launch_bounds__(256) k_expert_sum_backward(const __grid_constant__ bsr_experts_t p, const W *Ys, const float *weights,
+                                                             const W *dY, W *dYs, float *dweights, int64_t words) {
+    constexpr int n_w = Word<T, W>::n;
+    const int lane = threadIdx.x & 31;
+    const int64_t pairs = p.N * p.k, units = pairs + (dYs ? (p.R + 31) / 32 : 0);
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
+        if (u >= pairs) {
+            zero_rows(p, dYs, words, (u - pairs) * 32);
+            continue;
+        }
+        const int64_t n = u / p.k, r = row_of(p, u);
+        if (r < 0) {
+            if (dweights && lane == 0) dweights[u] = 0.f;
+            continue;
+        }
+        const float w = __ldg(weights + u);
+        float dot = 0.f;
+        for (int64_t at = lane; at < words; at += 32 * kWords) {
+            Word<T, W> d[kWords], y[kWords];
+#pragma unroll
+            for (int v = 0; v < kWords; v++) {
+                if (at + 32 * v >= words) break;
+                d[v].w = __ldg(dY + n * words + at + 32 * v);
+                if (dweights) y[v].w = __ldg(Ys + r * words + at + 32 * v);
+            }
+#pragma unroll
+            for (int v = 0; v < kWords; v++) {
+                if (at + 32 * v >= words) break;
+                Word<T, W> o;
+#pragma unroll
+                for (int i = 0; i < n_w; i++) {
+                    const float g = to_f32(d[v].v[i]);
+                    if (dweights) dot = fmaf(g, to_f32(y[v].v[i]), dot);
+                    o.v[i] = from_f32<T>(w * g);
+                }
+                if (dYs) dYs[r * words + at + 32 * v] = o.w;
+            }
+        }
+        if (!dweights) continue;
+#pragma unroll
+        for (int m = 16; m; m /= 2) dot += __shfl_xor_sync(0xffffffffu, dot, m);
+        if (lane == 0) dweights[u] = dot;
+    }
+}
+
+unsigned grid_of(int64_t units) { return (unsigned)std::min<int64_t>(std::max<int64_t>((units + 7) / 8, 1), 1 << 20); }
+
+// f(T(), W()) with the element type and the widest word that rows of D are made of.
+template <typename F>
+cudaError_t by_word(int64_t D, bsr_dtype_t dt, F f) {
+    const int64_t bytes = D * (dt == BSR_F32 ? 4 : 2);
+    if (dt == BSR_F32) return bytes % 16 == 0 ? f(float(), uint4()) : bytes % 8 == 0 ? f(float(), uint2()) : f(float(), uint32_t());
+    return bytes % 16 == 0  ? f(uint16_t(), uint4())
+           : bytes % 8 == 0 ? f(uint16_t(), uint2())
+           : bytes % 4 == 0 ? f(uint16_t(), uint32_t())
+                            : f(uint16_t(), uint16_t());
+}
+
+}  // namespace
+
+cudaError_t launch_expert_order(const bsr_experts_t &p, const int32_t *experts, cudaStream_t s) {
+    static std::atomic<uint64_t> attr_set{0};
+    const int most = (kWarps + 3) * kMostExperts * 4;
+    const cudaError_t e = allow_smem(k_expert_order, most, attr_set);
+    if (e != cudaSuccess) return e;
+    const unsigned ctas = p.N * p.k > 4 * kOrderThreads ? 8 : 1;
+    return launch_clusters(k_expert_order, ctas, dim3(ctas), dim3(kOrderThreads), (size_t)(kWarps + 3) * p.E * 4, s, p, experts, ctas);
+}
+
+cudaError_t launch_expert_rows(const bsr_experts_t &p, const void *X, void *Xs, int64_t D, bsr_dtype_t dt, cudaStream_t s) {
+    return by_word(D, dt, [&](auto t, auto w) {
+        using W = decltype(w);
+        const int64_t words = D * (int64_t)sizeof(t) / (int64_t)sizeof(W), parts = (words + 32 * kWords - 1) / (32 * kWords);
+        return launch_kernel(k_expert_rows<W>, dim3(grid_of(p.N * parts + (p.R + 31) / 32)), dim3(256), 0, s, p, static_cast<const W *>(X),
+                             static_cast<W *>(Xs), words, parts);
+    });
+}
+
+cudaError_t launch_expert_sum(const bsr_experts_t &p, const void *Ys, const float *weights, void *Y, int64_t D, bsr_dtype_t dt,
+                              cudaStream_t s) {
+    return by_word(D, dt, [&](auto t, auto w) {
+        using T = decltype(t);
+        using W = decltype(w);
+        const int64_t words = D * (int64_t)sizeof(T) / (int64_t)sizeof(W), parts = (words + 32 * kWords - 1) / (32 * kWords);
+        return launch_kernel(k_expert_sum<T, W>, dim3(grid_of(p.N * parts)), dim3(256), 0, s, p, static_cast<const W *>(Ys), weights,
+                             static_cast<W *>(Y), words, parts);
+    });
+}
+
+cudaError_t launch_expert_sum_backward(const bsr_experts_t &p, const void *Ys, const float *weights, const void *dY, void *dYs,
+                                       float *dweights, int64_t D, bsr_dtype_t dt, cudaStream_t s) {
+    return by_word(D, dt, [&](auto t, auto w) {
+        using T = decltype(t);
+        using W = decltype(w);
+        const int64_t words = D * (int64_t)sizeof(T) / (int64_t)sizeof(W);
+        return launch_kernel(k_expert_sum_backward<T, W>, dim3(grid_of(p.N * p.k + (p.R + 31) / 32)), dim3(256), 0, s, p,
+                             static_cast<const W *>(Ys), weights, static_cast<const W *>(dY), static_cast<W *>(dYs), dweights, words);
+    });
+}
+
+}  // namespace bsr

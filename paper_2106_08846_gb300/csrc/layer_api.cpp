@@ -5,68 +5,17 @@
 #include <algorithm>
 #include <cmath>
 
-#include "bsr_internal.h"
+#include "buffers.h"
+#include "fp8.h"
 #include "gated.h"
 #include "gated_mma.h"
-#include "host.h"
 #include "residual_norm.h"
 
 using namespace bsr;
 
 namespace {
 
-// The buffers of one call, checked together: alignment, where they live, and
-// that no output overlaps another buffer, but for the input whose place it may
-// take (`over`: the same address).
-struct Buffers {
-    struct One {
-        const void *p;
-        size_t bytes;
-        const void *over[2];
-        bool out;
-    };
-    One all[24];
-    int n = 0;
-    bool misaligned = false;
-
-    void add(const void *p, size_t bytes, size_t align, bool out, const void *over0 = nullptr, const void *over1 = nullptr) {
-        if (!p) return;
-        misaligned |= reinterpret_cast<uintptr_t>(p) % align != 0;
-        all[n++] = One{p, bytes, {over0, over1}, out};
-    }
-    void in(const void *p, size_t bytes, size_t align = 16) { add(p, bytes, align, false); }
-    void out(const void *p, size_t bytes, size_t align = 16, const void *over0 = nullptr, const void *over1 = nullptr) {
-        add(p, bytes, align, true, over0, over1);
-    }
-    bsr_status_t check() const {
-        if (misaligned) return BSR_ERR_ALIGNMENT;
-        for (int i = 0; i < n; i++) {
-            if (!all[i].out) continue;
-            for (int j = 0; j < n; j++) {
-                if (j == i || (all[j].out && j < i)) continue;
-                if (!overlaps(all[i].p, all[i].bytes, all[j].p, all[j].bytes)) continue;
-                const bool same = all[i].p == all[j].p && all[i].bytes == all[j].bytes && !all[j].out;
-                if (!same || (all[i].p != all[i].over[0] && all[i].p != all[i].over[1])) return BSR_ERR_INVALID_ARG;
-            }
-        }
-        int device = 0;
-        if (cudaGetDevice(&device) != cudaSuccess) {
-            cudaGetLastError();
-            return BSR_ERR_CUDA;
-        }
-        for (int i = 0; i < n; i++)
-            if (all[i].bytes && classify(all[i].p, device) != PK_DEVICE) return BSR_ERR_INVALID_ARG;
-        return BSR_OK;
-    }
-};
-
-bsr_status_t launched(cudaError_t e) {
-    if (e == cudaSuccess) return BSR_OK;
-    cudaGetLastError();
-    return BSR_ERR_CUDA;
-}
-
-bool known(bsr_dtype_t dt) { return dt == BSR_F32 || dt == BSR_BF16; }
+using bsr::known;
 bool known(bsr_norm_t n) { return n == BSR_NORM_NONE || n == BSR_NORM_LAYER || n == BSR_NORM_RMS; }
 
 // What all calls of the residual step check; with a gate, its rows too.
@@ -242,9 +191,10 @@ bsr_status_t bsr_gated_backward(const void *X, const void *Wg, const void *Wu, c
 }
 
 bsr_status_t bsr_check_status(void) {
-    int code = DEV_OK;
-    const bsr_status_t st = launched(gated_mma_status(&code));
-    return st == BSR_OK && code == DEV_TIMEOUT ? BSR_ERR_TIMEOUT : st;
+    int gated = DEV_OK, product = DEV_OK;
+    bsr_status_t st = launched(gated_mma_status(&gated));
+    if (st == BSR_OK) st = launched(fp8_product_status(&product));
+    return st == BSR_OK && (gated == DEV_TIMEOUT || product == DEV_TIMEOUT) ? BSR_ERR_TIMEOUT : st;
 }
 
 }  // extern "C"
