@@ -40,6 +40,11 @@ __host__ __device__ constexpr uint32_t idesc(bool tf32, int M, int N) {
            ((uint32_t)(M >> 4) << 24);
 }
 
+// The same for 8-bit operands: formats 0 (e4m3) or 1 (e5m2).
+__host__ __device__ constexpr uint32_t idesc_8bit(int a, int b, int M, int N) {
+    return (1u << 4) | ((uint32_t)a << 7) | ((uint32_t)b << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
 // bits of the instruction descriptor for operands contiguous along M and N
 constexpr uint32_t kIdescAmn = 1u << 15, kIdescBmn = 1u << 16;
 
@@ -94,6 +99,12 @@ __device__ __forceinline__ void dealloc(uint32_t taddr, uint32_t cols) {
 __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc));
+}
+// The same of 8-bit floating-point operands (K = 32).
+__device__ __forceinline__ void mma_ss_pair_8bit(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc));
 }
 // One arrival on the barrier at this offset in both CTAs of the pair (of a
