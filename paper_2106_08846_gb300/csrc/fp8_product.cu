@@ -3,19 +3,30 @@
 //   Y[n, m] = bias[m] + sum_b sa[b, n] sb[b, m] sum_{k in block b} qa[n, k] qb[m, k]
 //
 // A cluster of two CTAs works on a tile of 256 rows of a by 2 `half` rows of b. A
-// block of 128 columns is a step: four MMAs (M = 256, N = 2 half, K = 32) into a
-// fresh accumulator buffer, which the epilogue takes out, scales and adds in
-// registers while the next step's MMAs fill the other buffer.
+// block of 128 columns is a step: four MMAs (M = 256, N = 2 half, K = 32), which
+// multiply by the rows' scales themselves, powers of two as bytes in tensor memory.
 //
 //   warps 0, 1, 3  producers, a step each in turn: 128 rows of a and `half` of b a
 //                  CTA, 128 bytes each, by TMA (128-byte swizzle) into a stage of the ring
 //   warp 2         MMAs of the pair's first CTA
-//   warps 4 .. 11  epilogue: 32 rows and half of the columns each, up to 128 sums a thread
-//                  (registers handed over by the other four warps)
+//   warps 4, 5, 6  scales of 128 rows each (of a, of b, of b) and four steps: their exponents
+//                  go to shared memory, a word a row, and from there to tensor memory by
+//                  the thread that issues the MMAs
+//   warps 8 ..     epilogue, 16 (drained accumulators: 8) warps: 32 rows and a share of
+//                  the columns each, straight from tensor memory to global memory
 //
-// A step of 256 columns is 512 SM cycles of MMAs; its epilogue reads 128 KB of
-// tensor memory an SM and makes a multiply-add of each value (256 cycles, packed).
-// Where each of b's rows has a scale of its own, one more multiplication.
+// Scaling outside the MMAs (a fresh accumulator for each step, scaled and added in
+// registers) takes every value of a step out of tensor memory: 16384 tokens of 1024
+// features into 4096 174 us.
+//
+// A step is 512 SM cycles of MMAs at 256 columns. Two accumulators of 256 columns and
+// the scales do not fit 512 columns: the second begins at column 224, and the
+// epilogue takes the 32 columns that they share first, before the next tile's MMAs.
+//
+// The accumulators lose bits with every addition, always towards zero: about 7e-9 of a sum of
+// one sign with each column. bf16 results: up to 16384 columns (2^-13 of such a
+// sum, a sixteenth of what the result is rounded by); fp32 ones: up to 1024 (7e-6). Longer sums
+// are drained every 1024 columns into registers, up to 128 a thread (handed over by the other warps).
 //
 // Persistent: one CTA per SM. Runs of rows: tiles of 256 rows from each run's first
 // one on; the table of the runs' tiles is made by every CTA from the offsets on the device.
@@ -42,15 +53,23 @@ namespace bsr {
 
 namespace {
 
-constexpr int kEpiWarp0 = 4, kMmaWarp = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kScaleWarp0 = 4, kScaleWarps = 3, kEpiWarp0 = 8, kMmaWarp = 2;
+constexpr int epi_warps(bool drained) { return drained ? 8 : 16; }
+constexpr int threads_of(bool drained) { return 32 * (kEpiWarp0 + epi_warps(drained)); }
 constexpr int kProducers = 3, kStages = 8;
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's rows of a, a step
-constexpr uint32_t kAccCols = 256;
-constexpr uint32_t kScaleBytes = kEpiWarps * 128 * 4;
+constexpr uint32_t kOverlap = 32;             // columns that the accumulators of 256 columns share
+// Tensor memory behind them: two sets of scales, of a in the first four of 16 columns.
+constexpr uint32_t kScaleCol = 512 - kOverlap, kScaleCols = 16, kAllCols = 512;
+constexpr int kScaleSteps = 4;                // bytes of a word
+constexpr int kScaleSlots = 4;                // in shared memory
+constexpr uint32_t kScaleSlot = kScaleWarps * 512, kScaleBytes = kScaleSlots * kScaleSlot;
+constexpr int kDrainSteps = 8;                // steps of a drained accumulator, and of fp32 sums that are not drained
+constexpr int kMostSteps = 128;               // of bf16 ones
 constexpr uint32_t kMaxSmem = 227 * 1024 - 12 * 1024;   // (static: the runs' table, barriers)
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
-// Registers of a thread: (4 warps * 72 + 8 warps * 216) * 32 is what 384 threads are launched with (168 each).
-constexpr int kFewRegs = 72, kManyRegs = 216;
+// Registers of a thread, drained: 8 warps of 56 and 8 of 200 are what 512 threads are launched with (128 each).
+constexpr int kFewRegs = 56, kManyRegs = 200;
 
 __device__ int g_status;
 
@@ -59,7 +78,7 @@ struct Args {
     const float *sa, *sb, *bias;
     int64_t rows, M;          // of a; of b (columns of Y)
     int64_t sa_cols, sb_cols, KB;
-    int a_shift;              // rows of a that share a scale: 1 << a_shift
+    int a_shift, b_shift;     // rows that share a scale: 1 << shift
     int group, E;
     const int32_t *offsets;
     unsigned tiles_m, tiles_n;
@@ -134,23 +153,77 @@ __device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsig
     return round * pairs + (round ? pairs - 1 - pair : pair);
 }
 
-// Scales of a step as a thread loads them: of its own row of a, and of its warp's
-// columns' rows of b (COL: of columns 4 lane .. 4 lane + 3).
-template <bool COL>
-struct Scales {
-    float a, b[COL ? 4 : 1];
-};
+// 32 rows of the result from `row` on (of this thread: row + lane / 4 + 8 h) x 32 columns
+// from c on: x[h][j], columns 8 j + 2 (lane % 4), + 1.
+template <typename T>
+__device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, int64_t c, const F2 (&x)[4][4]) {
+    const int lane = threadIdx.x & 31, c4 = lane & 3;
+    row += lane >> 2;
+    if (un.part >= 0) {
+#pragma unroll
+        for (int h = 0; h < 4; h++) {
+            float *at = a.parts + ((int64_t)un.part * 256 + (row - un.m0) + 8 * h) * 2 * a.half + (c - un.n0) + 2 * c4;
+#pragma unroll
+            for (int j = 0; j < 4; j++) *reinterpret_cast<float2 *>(at + 8 * j) = unpack2(x[h][j]);
+        }
+        return;
+    }
+    F2 add[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++) add[j] = all2(0.f);
+    if (a.bias) {
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const int64_t at = c + 8 * j + 2 * c4;
+            const float *bias = a.bias + (int64_t)un.batch * a.M + at;
+            add[j] = pack2(at < a.M ? __ldg(bias) : 0.f, at + 1 < a.M ? __ldg(bias + 1) : 0.f);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 4; h++) {
+        F2 y[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) y[j] = add2(x[h][j], add[j]);
+        uint32_t w[4];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; j++) w[j] = pack_bf16(y[j]);
+            turn_words(w);
+        }
+        if (row + 8 * h >= un.m1) continue;
+        T *out = static_cast<T *>(a.Y) + (un.out + row + 8 * h) * a.M;
+        if constexpr (sizeof(T) == 2) {
+            Eight<T> e;
+#pragma unroll
+            for (int j = 0; j < 4; j++) e.w[j] = w[j];
+            store8(out + c + 8 * c4, a.M - (c + 8 * c4), a.align, e);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const int64_t at = c + 8 * j + 2 * c4;
+                const float2 z = unpack2(y[j]);
+                if (at + 2 <= a.M && a.align >= 8) {
+                    *reinterpret_cast<float2 *>(out + at) = z;
+                } else {
+                    if (at < a.M) out[at] = z.x;
+                    if (at + 1 < a.M) out[at + 1] = z.y;
+                }
+            }
+        }
+    }
+}
 
-// COL: each row of b has a scale of its own, else 128 of them share one.
-template <typename T, bool COL>
-__global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_constant__ Args a) {
+template <typename T, bool DRAIN>
+__global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __grid_constant__ Args a) {
+    constexpr int kEpiWarps = epi_warps(DRAIN);
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
     const int ns = a.ns;
     const uint32_t stage_bytes = a.stage_bytes;
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], done;
+    __shared__ uint64_t scales_full[kScaleSlots], scales_empty[kScaleSlots];
     __shared__ int stop, loads[kProducers][2];   // loads[producer][CTA of the pair]: steps loaded
-    __shared__ int freed, handed;                // commits issued to `empty` and to `acc_full`
+    __shared__ int freed, handed, copied;        // commits issued to `empty`, `acc_full` and `scales_empty`
     __shared__ uint32_t tmem_s;
     __shared__ Runs runs;
 
@@ -167,11 +240,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             ptx::mbar_init(&acc_full[i], 1);
             ptx::mbar_init(&acc_empty[i], 2 * kEpiWarps);
         }
+        for (int i = 0; i < kScaleSlots; i++) {
+            ptx::mbar_init(&scales_full[i], 2 * kScaleWarps);
+            ptx::mbar_init(&scales_empty[i], 1);
+        }
         ptx::mbar_init(&done, 1);
-        stop = freed = handed = 0;
+        stop = freed = handed = copied = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, 2 * kAccCols);
+    if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, kAllCols);
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tensormap(&a.a);
         ptx::prefetch_tensormap(&a.b);
@@ -186,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     if (a.group != BSR_GROUP_NONE) {
         // within what there is, in steps for columns
         const bool by_rows = a.group == BSR_GROUP_ROWS;
-        for (int e = threadIdx.x; e <= a.E; e += kThreads) {
+        for (int e = threadIdx.x; e <= a.E; e += threads_of(DRAIN)) {
             const int64_t o = max(0, __ldg(a.offsets + e));
             runs.at[e] = (int32_t)(by_rows ? min(o, a.rows) : min(o / kFp8Block, a.KB));
         }
@@ -211,6 +288,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         units = by_rows ? runs.first[a.E] * a.tiles_n : units * (unsigned)a.E;
     }
     const uint32_t tmem = tmem_s;
+    unsigned char *scales_s = base + (size_t)ns * stage_bytes;
     const bool elected = ptx::elect_one();
     // stops every role of this pair; a timeout is recorded
     auto halt = [&]() {
@@ -227,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     // parity, would let it pass a round early; its last wait, for step
     // g - np - ns, tells it so if np <= ns.
     const int prod = warp < kMmaWarp ? warp : kMmaWarp, np = min(kProducers, ns);
-    const bool producer = warp < kEpiWarp0 && warp != kMmaWarp && prod < np;
+    const bool producer = warp < kScaleWarp0 && warp != kMmaWarp && prod < np;
     unsigned round = 0, v = pair;
     Unit un = {};
     int i = 0, s = prod % ns, issued = 0;
@@ -261,164 +339,114 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         return seek();
     };
     bool more = false;
-    // (each in its role's own branch, so that the compiler knows what a role has)
+    // Accumulators: of 256 columns they share kOverlap, and the epilogue hands those of
+    // one tile over for the next tile's; narrower ones are handed back for the next but one.
+    const bool shared_cols = a.half == 128;
+    const uint32_t acc_step = shared_cols ? 256 - kOverlap : 128;
     if (warp >= kEpiWarp0) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
-        const int q = warp & 3, share = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., columns from half * share on
-        const int groups = a.half / 32;                            // of 32 columns
-        float *col_s = reinterpret_cast<float *>(base + (size_t)ns * stage_bytes) + (warp - kEpiWarp0) * 128;
+        if constexpr (DRAIN) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
+        const int q = warp & 3, share = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., a share of the columns
+        const int all = a.half / 16, each = (all + kEpiWarps / 4 - 1) / (kEpiWarps / 4), first = share * each,
+                  groups = max(0, min(each, all - first));          // of 32 columns
         int ab = 0;
         uint32_t fphase = 0;
         bool ok = true;
+        auto wait_acc = [&](const Unit &u) {
+            ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, a.wait_ns * (uint64_t)(u.i1 - u.i0 + 2), &stop));
+            if (!ok) halt();
+            tc5::fence_after();
+            return tmem + (uint32_t)ab * acc_step + ((uint32_t)(32 * q) << 16) + 32 * first;
+        };
+        auto hand_back = [&]() {
+            tc5::fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(&acc_empty[ab], 0));
+        };
+        auto next_acc = [&]() {
+            ab ^= 1;
+            if (ab == 0) fphase ^= 1;
+        };
+        auto load = [&](uint32_t tm, uint32_t (&r)[2][16]) {
+            tc5::ld_16x32(tm, r[0]);
+            tc5::ld_16x32(tm + (16u << 16), r[1]);
+        };
+        auto loaded = [&](uint32_t (&r)[2][16]) {
+            tc5::ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
+                asm volatile("" : "+r"(r[0][j]));
+                asm volatile("" : "+r"(r[1][j]));
+            }
+        };
+        // rows lane / 4 + 8 h, columns 8 j + 2 (lane % 4), + 1 of what was loaded
+        auto at = [&](const uint32_t (&r)[2][16], int h, int j) {
+            const uint32_t *x = &r[h >> 1][4 * j + 2 * (h & 1)];
+            return pack2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+        };
         for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
             un = unit_at(a, runs, v);
-            const int64_t row0 = un.m0 + rank * 128 + 32 * q, col0 = un.n0 + share * a.half;
-            // where this thread's scales lie; rows and columns that are not there take another's
-            const float *sa = a.sa + (min(row0 + lane, a.rows - 1) >> a.a_shift);
-            const float *sb = a.sb + (int64_t)un.batch * a.KB * a.sb_cols + (COL ? 0 : min(col0 >> 7, a.sb_cols - 1));
-            auto fetch = [&](int b, Scales<COL> &f) {
-                if (b >= un.i1) return;
-                f.a = __ldg(sa + b * a.sa_cols);
-                if constexpr (COL) {
-#pragma unroll
-                    for (int j = 0; j < 4; j++) f.b[j] = __ldg(sb + b * a.sb_cols + min(col0 + 4 * lane + j, a.M - 1));
-                } else {
-                    f.b[0] = __ldg(sb + b * a.sb_cols);
+            const int64_t row = un.m0 + rank * 128 + 32 * q, col = un.n0 + 32 * first;
+            if constexpr (!DRAIN) {
+                const bool any = un.i1 > un.i0;
+                uint32_t tm = 0;
+                // the columns that the next tile's accumulator has too, first
+                const bool back = shared_cols && ab == 0, mine = !shared_cols || (ab == 0 ? first + groups == all : first == 0);
+                if (any) {
+                    tm = wait_acc(un);
+                    if (!ok) break;
+                    if (groups == 0 || !mine) hand_back();
                 }
-            };
-            F2 acc[4][2][2][4];   // [group][16 rows][8 rows][pair of columns]
-#pragma unroll
-            for (int g = 0; g < 4; g++)
-#pragma unroll
-                for (int j = 0; j < 16; j++) acc[g][j >> 3][(j >> 2) & 1][j & 3] = all2(0.f);
-            Scales<COL> f0, f1;   // of even and odd steps, two steps ahead
-            fetch(un.i0, f0);
-            fetch(un.i0 + 1, f1);
-            for (int b = un.i0; b < un.i1; b++) {
-                float fa;
-                auto take = [&](Scales<COL> &f) {
-                    fa = COL ? f.a : f.a * f.b[0];
-                    if constexpr (COL) {
-                        __syncwarp();
-                        *reinterpret_cast<float4 *>(col_s + 4 * lane) = make_float4(f.b[0], f.b[1], f.b[2], f.b[3]);
-                        __syncwarp();
+                for (int p = 0; p < groups; p++) {
+                    const int g = back ? groups - 1 - p : p;
+                    uint32_t r[2][16];
+                    if (any) {
+                        load(tm + 32 * g, r);
+                        loaded(r);
+                        if (mine && p == (shared_cols ? 0 : groups - 1)) hand_back();
                     }
-                    fetch(b + 2, f);
-                };
-                if ((b - un.i0) & 1) take(f1);
-                else take(f0);
-                F2 fr[4];   // factors of rows lane / 4 + 8 h
+                    F2 x[4][4];
 #pragma unroll
-                for (int h = 0; h < 4; h++) fr[h] = all2(__shfl_sync(0xffffffffu, fa, (lane >> 2) + 8 * h));
-                ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, a.wait_ns * (uint64_t)(un.i1 - un.i0 + 2), &stop));
-                if (!ok) {
-                    halt();
-                    break;
+                    for (int h = 0; h < 4; h++)
+#pragma unroll
+                        for (int j = 0; j < 4; j++) x[h][j] = any ? at(r, h, j) : all2(0.f);
+                    put<T>(a, un, row, col + 32 * g, x);
                 }
-                tc5::fence_after();
-                const uint32_t tm = tmem + (uint32_t)ab * kAccCols + ((uint32_t)(32 * q) << 16) + share * a.half;
-                uint32_t r[2][2][16];   // a group ahead
-                tc5::ld_16x32(tm, r[0][0]);
-                tc5::ld_16x32(tm + (16u << 16), r[0][1]);
+                if (any) next_acc();
+            } else {
+                F2 sum[4][4][4];   // [group]
 #pragma unroll
-                for (int g = 0; g < 4; g++) {
-                    if (g >= groups) break;
-                    tc5::ld_wait();
+                for (int g = 0; g < 4; g++)
 #pragma unroll
-                    for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
-                        asm volatile("" : "+r"(r[g & 1][0][j]));
-                        asm volatile("" : "+r"(r[g & 1][1][j]));
+                    for (int j = 0; j < 16; j++) sum[g][j >> 2][j & 3] = all2(0.f);
+                for (int b = un.i0; b < un.i1; b += kDrainSteps) {
+                    const uint32_t tm = wait_acc(un);
+                    if (!ok) break;
+                    if (groups == 0) hand_back();
+                    // both ends first: one of them is shared
+                    constexpr int order[4] = {0, 3, 1, 2};
+#pragma unroll
+                    for (int p = 0; p < 4; p++) {
+                        const int g = order[p];
+                        if (g >= groups) continue;
+                        uint32_t r[2][16];
+                        load(tm + 32 * g, r);
+                        loaded(r);
+                        if (shared_cols ? p == 1 : g == groups - 1) hand_back();
+#pragma unroll
+                        for (int h = 0; h < 4; h++)
+#pragma unroll
+                            for (int j = 0; j < 4; j++) sum[g][h][j] = add2(sum[g][h][j], at(r, h, j));
                     }
-                    if (g + 1 < groups) {
-                        if (g < 3) {
-                            tc5::ld_16x32(tm + 32 * (g + 1), r[(g + 1) & 1][0]);
-                            tc5::ld_16x32(tm + (16u << 16) + 32 * (g + 1), r[(g + 1) & 1][1]);
-                        }
-                    } else {   // the last columns are in registers: the buffer is handed back
-                        tc5::fence_before();
-                        __syncwarp();
-                        if (lane == 0) ptx::mbar_arrive_remote(ptx::map_to_cta(&acc_empty[ab], 0));
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; j++) {
-                        F2 fc;
-                        if constexpr (COL) {
-                            const float2 c = *reinterpret_cast<const float2 *>(col_s + 32 * g + 8 * j + 2 * (lane & 3));
-                            fc = pack2(c.x, c.y);
-                        }
-#pragma unroll
-                        for (int h = 0; h < 4; h++) {
-                            const uint32_t *x = &r[g & 1][h >> 1][4 * j + 2 * (h & 1)];
-                            F2 p = pack2(__uint_as_float(x[0]), __uint_as_float(x[1]));
-                            if constexpr (COL) p = mul2(p, fc);
-                            acc[g][h >> 1][h & 1][j] = fma2(p, fr[h], acc[g][h >> 1][h & 1][j]);
-                        }
-                    }
+                    next_acc();
                 }
-                ab ^= 1;
-                if (ab == 0) fphase ^= 1;
-            }
-            if (!ok) break;
-            // rows lane / 4 + 8 h, columns 32 g + 8 j + 2 (lane % 4), + 1
-            const int c4 = lane & 3;
+                if (!ok) break;
 #pragma unroll
-            for (int g = 0; g < 4; g++) {
-                if (g >= groups) break;
-                const int64_t c = col0 + 32 * g;
-                if (un.part >= 0) {
-#pragma unroll
-                    for (int h = 0; h < 4; h++) {
-                        const int64_t row = row0 - un.m0 + (lane >> 2) + 8 * h;
-                        float *at = a.parts + ((int64_t)un.part * 256 + row) * 2 * a.half + (c - un.n0) + 2 * c4;
-#pragma unroll
-                        for (int j = 0; j < 4; j++) *reinterpret_cast<float2 *>(at + 8 * j) = unpack2(acc[g][h >> 1][h & 1][j]);
-                    }
-                    continue;
-                }
-                F2 add[4];
-#pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    const int64_t at = c + 8 * j + 2 * c4;
-                    const float *bias = a.bias + (int64_t)un.batch * a.M + at;
-                    add[j] = a.bias ? pack2(at < a.M ? __ldg(bias) : 0.f, at + 1 < a.M ? __ldg(bias + 1) : 0.f) : all2(0.f);
-                }
-#pragma unroll
-                for (int h = 0; h < 4; h++) {
-                    F2 x[4];
-#pragma unroll
-                    for (int j = 0; j < 4; j++) x[j] = add2(acc[g][h >> 1][h & 1][j], add[j]);
-                    uint32_t w[4];
-                    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-                        for (int j = 0; j < 4; j++) w[j] = pack_bf16(x[j]);
-                        turn_words(w);
-                    }
-                    const int64_t row = row0 + (lane >> 2) + 8 * h;
-                    if (row >= un.m1) continue;
-                    T *out = static_cast<T *>(a.Y) + (un.out + row) * a.M;
-                    if constexpr (sizeof(T) == 2) {
-                        Eight<T> e;
-#pragma unroll
-                        for (int j = 0; j < 4; j++) e.w[j] = w[j];
-                        store8(out + c + 8 * c4, a.M - (c + 8 * c4), a.align, e);
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; j++) {
-                            const int64_t at = c + 8 * j + 2 * c4;
-                            const float2 y = unpack2(x[j]);
-                            if (at + 2 <= a.M && a.align >= 8) {
-                                *reinterpret_cast<float2 *>(out + at) = y;
-                            } else {
-                                if (at < a.M) out[at] = y.x;
-                                if (at + 1 < a.M) out[at + 1] = y.y;
-                            }
-                        }
-                    }
-                }
+                for (int g = 0; g < 4; g++)
+                    if (g < groups) put<T>(a, un, row, col + 32 * g, sum[g]);
             }
         }
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
+        if constexpr (DRAIN) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
         if (producer) {
             if (v < units) {
                 un = unit_at(a, runs, v);
@@ -437,49 +465,115 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 loads[prod][rank] = issued;
                 ptx::store_cluster(ptx::map_to_cta(&loads[prod][rank], rank ^ 1), (uint32_t)issued);
             }
-        } else if (warp == kMmaWarp) {
-            if (rank == 0) {
-                int ab = 0, n_steps = 0;
-                uint32_t fphase = 0, aphase = 1;
-                bool ok = true;
-                s = 0;
-                const uint64_t ad0 = tc5::desc_sw128(smem0), bd0 = tc5::desc_sw128(smem0 + kABytes);
-                for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-                    un = unit_at(a, runs, v);
-                    for (i = un.i0; i < un.i1; i++) {
-                        ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[ab], aphase, a.wait_ns, &stop) &&
-                                                         wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
-                        if (!ok) break;
-                        tc5::fence_after();
-                        if (elected) {
-                            const uint64_t at = (uint64_t)((s * stage_bytes) >> 4);
-    #pragma unroll
-                            for (int j = 0; j < kFp8Block / 32; j++)   // (32 bytes along the rows)
-                                tc5::mma_ss_pair_8bit(tmem + (uint32_t)ab * kAccCols, ad0 + at + 2 * j, bd0 + at + 2 * j, a.idesc, j > 0);
-                            tc5::commit_pair(&empty[s]);
-                            tc5::commit_pair(&acc_full[ab]);
-                        }
-                        __syncwarp();
-                        n_steps++;
-                        if (++s == ns) {
-                            s = 0;
-                            fphase ^= 1;
-                        }
-                        ab ^= 1;
-                        if (ab == 0) aphase ^= 1;
+        } else if (warp >= kScaleWarp0 && warp < kScaleWarp0 + kScaleWarps) {
+            // row r of this warp's 128 is word 4 (r % 32) + r / 32 of its 512 bytes
+            const int which = warp - kScaleWarp0, shift = which ? a.b_shift : a.a_shift;
+            const bool needed = which < 2 || a.half == 128;   // (all three arrive at the barrier)
+            const uint32_t full0 = ptx::map_to_cta(&scales_full[0], 0);
+            int slot = 0;
+            uint32_t sphase = 1;
+            bool ok = true;
+            for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
+                un = unit_at(a, runs, v);
+                const int64_t row0 = which ? un.n0 + (which - 1) * 128 : un.m0 + rank * 128, rows = which ? a.M : a.rows,
+                              cols = which ? a.sb_cols : a.sa_cols;
+                const float *from = which ? a.sb + (int64_t)un.batch * a.KB * cols : a.sa;
+                int64_t at[4];   // (rows that are not there take another's)
+#pragma unroll
+                for (int c = 0; c < 4; c++) at[c] = min(row0 + 32 * c + lane, rows - 1) >> shift;
+                for (int b = un.i0; b < un.i1; b += kScaleSteps) {
+                    uint32_t x[kScaleSteps][4];
+#pragma unroll
+                    for (int k = 0; k < kScaleSteps; k++)
+#pragma unroll
+                        for (int c = 0; c < 4; c++) x[k][c] = needed && b + k < un.i1 ? __float_as_uint(__ldg(from + (b + k) * cols + at[c])) : 0;
+                    ok = __all_sync(0xffffffffu, wait_or_abort(&scales_empty[slot], sphase, a.wait_ns, &stop));
+                    if (!ok) {
+                        halt();
+                        break;
                     }
-                    if (!ok) halt();
+                    uint32_t w[4];
+#pragma unroll
+                    for (int c = 0; c < 4; c++)   // (a scale's bits are its exponent's byte, above 23 zeros)
+                        w[c] = ((x[0][c] >> 23) & 0xff) | ((x[1][c] >> 23) & 0xff) << 8 | ((x[2][c] >> 23) & 0xff) << 16 | ((x[3][c] >> 23) & 0xff) << 24;
+                    *reinterpret_cast<uint4 *>(scales_s + slot * kScaleSlot + which * 512 + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+                    ptx::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive_cluster(full0 + 8 * slot);
+                    if (++slot == kScaleSlots) slot = 0, sphase ^= 1;
                 }
-                // every MMA issued has completed before the tensor memory is freed
-                if (elected) {
-                    tc5::commit_pair(&done);
-                    freed = handed = n_steps;
-                    ptx::store_cluster(ptx::map_to_cta(&freed, 1), (uint32_t)n_steps);
-                    ptx::store_cluster(ptx::map_to_cta(&handed, 1), (uint32_t)n_steps);
-                }
-                __syncwarp();
-                ptx::mbar_wait_bounded(&done, 0, kDrainNs);
             }
+        } else if (warp == kMmaWarp && rank == 0) {
+            int n_steps = 0, n_acc = 0, n_scales = 0;
+            uint32_t fphase = 0;
+            bool ok = true;
+            s = 0;
+            const uint64_t ad0 = tc5::desc_sw128(smem0), bd0 = tc5::desc_sw128(smem0 + kABytes);
+            const uint64_t sd0 = tc5::desc(ptx::smem_addr(scales_s), 16, 128);   // (eight rows of 16 bytes side by side)
+            for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
+                un = unit_at(a, runs, v);
+                for (i = un.i0; i < un.i1; i++) {
+                    const int b = i - un.i0;
+                    const bool fresh = DRAIN ? b % kDrainSteps == 0 : b == 0, last = i + 1 == un.i1 || (DRAIN && (b + 1) % kDrainSteps == 0);
+                    if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
+                        const int wait_for = n_acc - (shared_cols ? 1 : 2);
+                        if (wait_for >= 0)
+                            ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[wait_for & 1], (uint32_t)(wait_for >> 1) & 1, a.wait_ns, &stop));
+                        if (!ok) break;
+                    }
+                    const int slot = n_scales % kScaleSlots;
+                    const uint32_t set = tmem + kScaleCol + (uint32_t)(n_scales & 1) * kScaleCols;
+                    if (b % kScaleSteps == 0) {
+                        const uint32_t sphase = (uint32_t)(n_scales / kScaleSlots) & 1;
+                        ok = wait_or_abort(&scales_full[slot], sphase, a.wait_ns, &stop) && ptx::mbar_try_wait_cluster(&scales_full[slot], sphase);
+                        // (tensor memory's set of two words before has been read: a copy does not wait for MMAs)
+                        const int before = n_scales - 2;
+                        if (before >= 0)
+                            ok = ok && wait_or_abort(&scales_empty[before % kScaleSlots], (uint32_t)(before / kScaleSlots) & 1, a.wait_ns, &stop);
+                        ok = __all_sync(0xffffffffu, ok);
+                        if (!ok) break;
+                    }
+                    ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
+                    if (!ok) break;
+                    tc5::fence_after();
+                    if (elected) {
+                        if (b % kScaleSteps == 0) {
+                            const uint64_t sd = sd0 + (uint64_t)((slot * kScaleSlot) >> 4);
+                            tc5::copy_pair_32x16(set, sd);
+                            tc5::copy_pair_32x16(set + 4, sd + (512 >> 4));
+                            if (shared_cols) tc5::copy_pair_32x16(set + 8, sd + (1024 >> 4));
+                        }
+                        const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
+                        const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)b % kScaleSteps);
+#pragma unroll
+                        for (int j = 0; j < kFp8Block / 32; j++)   // (32 bytes along the rows)
+                            tc5::mma_ss_pair_scaled(tmem + (uint32_t)(n_acc & 1) * acc_step, ad0 + stage + 2 * j, bd0 + stage + 2 * j, idesc, set,
+                                                    set + 4, !fresh | (j > 0));
+                        tc5::commit_pair(&empty[s]);
+                        if (last) tc5::commit_pair(&acc_full[n_acc & 1]);
+                        if (b % kScaleSteps == kScaleSteps - 1 || i + 1 == un.i1) tc5::commit_pair(&scales_empty[slot]);
+                    }
+                    __syncwarp();
+                    n_steps++;
+                    if (last) n_acc++;
+                    if (b % kScaleSteps == kScaleSteps - 1 || i + 1 == un.i1) n_scales++;
+                    if (++s == ns) {
+                        s = 0;
+                        fphase ^= 1;
+                    }
+                }
+                if (!ok) halt();
+            }
+            // every MMA issued has completed before the tensor memory is freed
+            if (elected) {
+                tc5::commit_pair(&done);
+                freed = n_steps, handed = n_acc, copied = n_scales;
+                ptx::store_cluster(ptx::map_to_cta(&freed, 1), (uint32_t)n_steps);
+                ptx::store_cluster(ptx::map_to_cta(&handed, 1), (uint32_t)n_acc);
+                ptx::store_cluster(ptx::map_to_cta(&copied, 1), (uint32_t)n_scales);
+            }
+            __syncwarp();
+            ptx::mbar_wait_bounded(&done, 0, kDrainNs);
         }
     }
     // every MMA completed (the issuer waited for `done`), and neither CTA reads
@@ -517,6 +611,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         if (lane < ns && lane < freed) {
             bar = &empty[lane];
             last = (freed - 1 - lane) / ns;
+        } else if (lane >= kStages && lane - kStages < min(kScaleSlots, copied)) {
+            bar = &scales_empty[lane - kStages];
+            last = (copied - 1 - (lane - kStages)) / kScaleSlots;
         } else if (lane >= 29 && lane - 29 < min(2, handed)) {
             bar = &acc_full[lane - 29];
             last = (handed - 1 - (lane - 29)) / 2;
@@ -526,7 +623,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         if (bar) ptx::mbar_wait_bounded(bar, (uint32_t)last & 1, kDrainNs);
         __syncwarp();
         tc5::fence_after();
-        tc5::dealloc_pair(tmem, 2 * kAccCols);
+        tc5::dealloc_pair(tmem, kAllCols);
     }
 }
 
@@ -607,12 +704,12 @@ cudaError_t encode(const bsr_fp8_matrix_t &m, bool batch, int rows, CUtensorMap 
                : cudaErrorInvalidValue;
 }
 
-template <typename T, bool COL>
+template <typename T, bool DRAIN>
 cudaError_t launch(const Args &a, unsigned grid, cudaStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
-    cudaError_t e = allow_smem(k_fp8_product<T, COL>, kMaxSmem, attr_set);
+    cudaError_t e = allow_smem(k_fp8_product<T, DRAIN>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
-    return launch_clusters(k_fp8_product<T, COL>, 2, dim3(grid), dim3(kThreads), a.ns * a.stage_bytes + kScaleBytes + 1024, s, a);
+    return launch_clusters(k_fp8_product<T, DRAIN>, 2, dim3(grid), dim3(threads_of(DRAIN)), a.ns * a.stage_bytes + kScaleBytes + 1024, s, a);
 }
 
 }  // namespace
@@ -631,7 +728,7 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     a.rows = p.a.rows, a.M = p.b.rows;
     a.sa_cols = fp8_scale_cols(p.a), a.sb_cols = fp8_scale_cols(p.b);
     a.KB = fp8_blocks(p.a.cols);
-    a.a_shift = p.a.tile == 1 ? 0 : 7;
+    a.a_shift = p.a.tile == 1 ? 0 : 7, a.b_shift = p.b.tile == 1 ? 0 : 7;
     a.group = p.group, a.E = p.groups;
     a.offsets = p.offsets;
     a.tiles_m = (unsigned)q.tiles_m, a.tiles_n = (unsigned)q.tiles_n;
@@ -639,7 +736,7 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     a.half = q.half;
     a.stage_bytes = kABytes + (uint32_t)q.half * kFp8Block;
     a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 1024 - kScaleBytes) / a.stage_bytes);
-    a.idesc = tc5::idesc_8bit(p.a.type, p.b.type, 256, 2 * q.half);
+    a.idesc = tc5::idesc_scaled(p.a.type, p.b.type, 256, 2 * q.half);
     a.Y = p.Y;
     a.parts = p.ws;
     const uintptr_t addresses = reinterpret_cast<uintptr_t>(p.Y) | (uintptr_t)(p.b.rows * (p.dt == BSR_F32 ? 4 : 2)) | 16;
@@ -654,9 +751,9 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     }
     if (e != cudaSuccess) return e;
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(q.units, pairs_of_sms());
-    const bool f32 = p.dt == BSR_F32, col = p.b.tile == 1;
-    e = f32 ? (col ? launch<float, true>(a, grid, s) : launch<float, false>(a, grid, s))
-            : (col ? launch<uint16_t, true>(a, grid, s) : launch<uint16_t, false>(a, grid, s));
+    const bool f32 = p.dt == BSR_F32, drained = (a.KB + q.splits - 1) / q.splits > (f32 ? kDrainSteps : kMostSteps);
+    e = f32 ? (drained ? launch<float, true>(a, grid, s) : launch<float, false>(a, grid, s))
+            : (drained ? launch<uint16_t, true>(a, grid, s) : launch<uint16_t, false>(a, grid, s));
     if (e != cudaSuccess || q.splits == 1) return e;
     const dim3 joins((unsigned)(q.tiles_m * q.tiles_n * (q.half / 2)));
     return launch_kernel(f32 ? k_fp8_join<float> : k_fp8_join<uint16_t>, joins, dim3(256), 0, s, a);

@@ -40,10 +40,12 @@ __host__ __device__ constexpr uint32_t idesc(bool tf32, int M, int N) {
            ((uint32_t)(M >> 4) << 24);
 }
 
-// The same for 8-bit operands: formats 0 (e4m3) or 1 (e5m2).
-__host__ __device__ constexpr uint32_t idesc_8bit(int a, int b, int M, int N) {
-    return (1u << 4) | ((uint32_t)a << 7) | ((uint32_t)b << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+// The same for scaled 8-bit operands: formats 0 (e4m3) or 1 (e5m2), scales that are
+// exponents; and the bits that name byte i of the scales' words.
+__host__ __device__ constexpr uint32_t idesc_scaled(int a, int b, int M, int N) {
+    return ((uint32_t)a << 7) | ((uint32_t)b << 10) | ((uint32_t)(N >> 3) << 17) | (1u << 23) | ((uint32_t)(M >> 4) << 24);
 }
+__host__ __device__ constexpr uint32_t idesc_byte(uint32_t i) { return (i << 4) | (i << 29); }
 
 // bits of the instruction descriptor for operands contiguous along M and N
 constexpr uint32_t kIdescAmn = 1u << 15, kIdescBmn = 1u << 16;
@@ -101,11 +103,20 @@ __device__ __forceinline__ void mma_ss_pair(uint32_t d, uint64_t a, uint64_t b, 
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc));
 }
-// The same of 8-bit floating-point operands (K = 32).
-__device__ __forceinline__ void mma_ss_pair_8bit(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+// The same of 8-bit floating-point operands (K = 32), each row of A and of B times a
+// power of two (an exponent's byte, biased by 127) in tensor memory: that of row r in
+// lane r % 32 of each 32 lanes, column r / 32; the byte of the word is named in the
+// instruction descriptor. Each CTA has those of its 128 rows of A and of all rows of B.
+__device__ __forceinline__ void mma_ss_pair_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t scale_a, uint32_t scale_b,
+                                                   uint32_t acc) {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc));
+                 "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%5], [%6], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(id), "r"(acc), "r"(scale_a), "r"(scale_b));
+}
+// In both CTAs: 32 rows of 16 bytes of shared memory (contiguous) into four columns of
+// tensor memory, the same for each 32 lanes; in order with the thread's MMAs.
+__device__ __forceinline__ void copy_pair_32x16(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 // One arrival on the barrier at this offset in both CTAs of the pair (of a
 // cluster of two), once every MMA this thread issued so far completed.
