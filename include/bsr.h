@@ -509,13 +509,20 @@ bsr_status_t bsr_expert_sum_backward(const bsr_experts_t *p, const void *Ys, con
 /*
  * ---- Products in 8-bit floating point
  *
- * An operand is a matrix of 8-bit values with an fp32 scale for each block of 128
- * columns (the axis that the product sums over) of a row, or of 128 rows:
+ * An operand is a matrix of 8-bit values with a scale, a power of two, for each block
+ * of 128 columns (the axis that the product sums over) of a row, or of 128 rows:
  *
  *   x[r, c] is q[r, c] * scale[c / 128, r / tile]
  *
- * Y = a b' + bias:  Y[n, m] = bias[m] + sum_k a[n, k] b[m, k], the sum of a block in
- * the tensor cores' fp32 accumulators, blocks scaled and added in fp32.
+ * The product reads the scales as exponents, a byte 127 + log2(scale) for each row and
+ * block in the order that the tensor cores take them: with w = ceil(rows / 128), that of
+ * row r and block b at byte
+ *
+ *   ((b / 4) * w + r / 128) * 512 + (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4
+ *
+ * Y = a b' + bias:  Y[n, m] = bias[m] + sum_k a[n, k] b[m, k], in the tensor cores'
+ * fp32 accumulators, which lose up to 7e-9 of a sum of one sign with each column; they are added up
+ * in fp32 every 1024 columns, for bf16 results at most every 16384.
  * A layer X W': a = X by rows, b = W by rows with tiles of 128. Its gradients:
  * dX = dY W: b = W by columns; dW = dY' X: a = dY and b = X, both by columns.
  */
@@ -526,7 +533,9 @@ typedef struct {
     int tile;              /* rows that share a scale: 1 or 128 */
     bsr_fp8_t type;
     void *q;               /* device, 16-byte aligned: [batch, rows, cols rounded up to 128], zeros past cols */
-    float *scale;          /* device [batch, ceil(cols / 128), ceil(rows / tile)] */
+    uint8_t *exponent;     /* device, 16-byte aligned: [batch, ceil(cols / 512), ceil(rows / 128), 512] */
+    float *scale;          /* device [batch, ceil(cols / 128), ceil(rows / tile)], or NULL: written by
+                              bsr_fp8_quantize for who reads q, not read by the product */
 } bsr_fp8_matrix_t;
 
 /*

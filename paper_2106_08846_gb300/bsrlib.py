@@ -87,7 +87,7 @@ class _Experts(ctypes.Structure):
 class _Fp8Matrix(ctypes.Structure):
     """bsr_fp8_matrix_t"""
     _fields_ = [("batch", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("tile", ctypes.c_int),
-                ("type", ctypes.c_int), ("q", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+                ("type", ctypes.c_int), ("q", ctypes.c_void_p), ("exponent", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
 
 
 class BsrError(RuntimeError):
@@ -818,7 +818,7 @@ class Fp8Matrix:
     """[rows, cols] values in 8 bits (batch: that many, of shape [batch, rows, cols]) with
     a scale for each block of 128 columns of `tile` rows: x[r, c] is
     q[r, c] * scale[c // 128, r // tile]. `q` has cols rounded up to 128, zeros past
-    them. fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
+    them; `exponent` is what the product reads of the scales, powers of two (include/bsr.h). fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
 
     def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda"):
         if fmt not in _FP8 or tile not in (1, 128):
@@ -827,12 +827,14 @@ class Fp8Matrix:
         each, blocks = () if batch is None else (batch,), -(-cols // 128)
         self._q = torch.empty((*each, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
         self._scale = torch.empty((*each, blocks, -(-rows // tile)), dtype=torch.float32, device=device)
+        self._exponent = torch.empty((*each, -(-blocks // 4), -(-rows // 128), 512), dtype=torch.uint8, device=device)
         full = self._q.numel() > 0
         self._c = _Fp8Matrix(1 if batch is None else batch, rows, cols, tile, _FP8[fmt], _ptr(self._q) if full else None,
-                             _ptr(self._scale) if full else None)
+                             _ptr(self._exponent) if full else None, _ptr(self._scale) if full else None)
 
     # (to be filled, not replaced: the calls have their addresses)
     q = property(lambda self: self._q)
+    exponent = property(lambda self: self._exponent)
     scale = property(lambda self: self._scale)
 
 
@@ -856,7 +858,7 @@ def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: st
     if out is None:
         m = [Fp8Matrix(r, c, tile, fmt, batch, x.device) for r, c in sizes]
         for f in m:
-            _lend(stream, x.device, f.q, f.scale)
+            _lend(stream, x.device, f._q, f._scale, f._exponent)
     else:
         m = list(out) if form == "both" else [out]
         if [(f.rows, f.cols, f.tile, f.fmt, f.batch) for f in m] != [(r, c, tile, fmt, batch) for r, c in sizes]:

@@ -57,7 +57,8 @@ bsr_status_t check_matrix(const bsr_fp8_matrix_t *m) {
 }
 void add_matrix(Buffers &b, const bsr_fp8_matrix_t *m, bool out) {
     b.add(m->q, (size_t)fp8_bytes(*m), 16, out);
-    b.add(m->scale, (size_t)fp8_scales(*m) * 4, 4, out);
+    b.add(m->exponent, (size_t)fp8_exponents(*m), 16, out);
+    if (out) b.add(m->scale, (size_t)fp8_scales(*m) * 4, 4, out);
 }
 
 // What both calls of the product check.
@@ -170,7 +171,7 @@ bsr_status_t bsr_fp8_quantize(const void *x, bsr_dtype_t dt, const bsr_fp8_matri
     b.in(used, 4, 4);
     for (const bsr_fp8_matrix_t *c : {rows, columns}) {
         if (!c) continue;
-        if (!c->q || !c->scale) return BSR_ERR_INVALID_ARG;
+        if (!c->q || !c->exponent) return BSR_ERR_INVALID_ARG;
         add_matrix(b, c, true);
     }
     const bsr_status_t st = b.check();
@@ -194,7 +195,7 @@ bsr_status_t bsr_fp8_product(const bsr_fp8_matrix_t *a, const bsr_fp8_matrix_t *
     if ((group == BSR_GROUP_NONE) != (offsets == nullptr) || (bias && group == BSR_GROUP_COLUMNS)) return BSR_ERR_INVALID_ARG;
     const int64_t each = group == BSR_GROUP_COLUMNS ? groups : 1;
     if (a->rows == 0 || b->rows == 0) return BSR_OK;
-    if (!Y || (a->cols > 0 && (!a->q || !a->scale || !b->q || !b->scale))) return BSR_ERR_INVALID_ARG;
+    if (!Y || (a->cols > 0 && (!a->q || !a->exponent || !b->q || !b->exponent))) return BSR_ERR_INVALID_ARG;
     Fp8Product p = {*a, *b, bias, Y, dt, group, offsets, (int)groups, static_cast<float *>(ws)};
     const size_t need = (size_t)fp8_product_workspace(p);
     if (need > ws_bytes) return BSR_ERR_CAPACITY;

@@ -14,6 +14,8 @@ constexpr int kFp8Block = 128;   // columns that share a scale
 inline int64_t fp8_blocks(int64_t cols) { return (cols + kFp8Block - 1) / kFp8Block; }
 inline int64_t fp8_scale_cols(const bsr_fp8_matrix_t &m) { return (m.rows + m.tile - 1) / m.tile; }
 inline int64_t fp8_bytes(const bsr_fp8_matrix_t &m) { return m.batch * m.rows * fp8_blocks(m.cols) * kFp8Block; }
+inline int64_t fp8_words(int64_t cols) { return (fp8_blocks(cols) + 3) / 4; }   // of four blocks' exponents
+inline int64_t fp8_exponents(const bsr_fp8_matrix_t &m) { return m.batch * fp8_words(m.cols) * fp8_blocks(m.rows) * 512; }
 inline int64_t fp8_scales(const bsr_fp8_matrix_t &m) { return m.batch * fp8_blocks(m.cols) * fp8_scale_cols(m); }
 
 // x [batch, R, C] as `rows` [batch, R, C] and as `columns` [batch, C, R]; either may be NULL.

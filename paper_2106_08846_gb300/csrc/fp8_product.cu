@@ -7,17 +7,19 @@
 // multiply by the rows' scales themselves, powers of two as bytes in tensor memory.
 //
 //   warps 0, 1, 3  producers, a step each in turn: 128 rows of a and `half` of b a
-//                  CTA, 128 bytes each, by TMA (128-byte swizzle) into a stage of the ring
-//   warp 2         MMAs of the pair's first CTA
-//   warps 4, 5, 6  scales of 128 rows each (of a, of b, of b) and four steps: their exponents
-//                  go to shared memory, a word a row, and from there to tensor memory by
-//                  the thread that issues the MMAs
-//   warps 8 ..     epilogue, 16 (drained accumulators: 8) warps: 32 rows and a share of
-//                  the columns each, straight from tensor memory to global memory
+//                  CTA, 128 bytes each, by TMA (128-byte swizzle) into a stage of the
+//                  ring; every fourth block the rows' exponents of four blocks with it
+//   warp 2         MMAs of the pair's first CTA, and before them the exponents' copy
+//                  from shared to tensor memory
+//   warps 4 .. 11  epilogue: 32 rows and half of the columns each, through 2 KB of
+//                  shared memory a warp, so that four lanes store 64 bytes of a row
 //
 // Scaling outside the MMAs (a fresh accumulator for each step, scaled and added in
 // registers) takes every value of a step out of tensor memory: 16384 tokens of 1024
-// features into 4096 174 us.
+// features into 4096 174 us. Exponents made of fp32 scales by three more warps: 102 us, a
+// step waiting for their way from the other CTA's registers; so bsr_fp8_quantize lays
+// them out as tensor memory has them. The epilogue from registers to 64 bytes of a row by
+// shuffles took 9000 cycles a tile of 4096 cycles of MMAs.
 //
 // A step is 512 SM cycles of MMAs at 256 columns. Two accumulators of 256 columns and
 // the scales do not fit 512 columns: the second begins at column 224, and the
@@ -26,10 +28,10 @@
 // The accumulators lose bits with every addition, always towards zero: about 7e-9 of a sum of
 // one sign with each column. bf16 results: up to 16384 columns (2^-13 of such a
 // sum, a sixteenth of what the result is rounded by); fp32 ones: up to 1024 (7e-6). Longer sums
-// are drained every 1024 columns into registers, up to 128 a thread (handed over by the other warps).
+// are drained every 1024 columns into registers, 128 a thread (handed over by the other warps).
 //
-// Persistent: one CTA per SM. Runs of rows: tiles of 256 rows from each run's first
-// one on; the table of the runs' tiles is made by every CTA from the offsets on the device.
+// Persistent: one CTA per SM. Runs of rows: tiles of 256 rows from a multiple of 128 on,
+// as the exponents lie, the rows of other runs left out; the table of the runs' tiles is made by every CTA from the offsets on the device.
 // Runs of columns: a tile's steps are the run's. Tiles of sums too few to fill the
 // GPU have them split; the parts are added in their order by a second launch.
 //
@@ -53,36 +55,32 @@ namespace bsr {
 
 namespace {
 
-constexpr int kScaleWarp0 = 4, kScaleWarps = 3, kEpiWarp0 = 8, kMmaWarp = 2;
-constexpr int epi_warps(bool drained) { return drained ? 8 : 16; }
-constexpr int threads_of(bool drained) { return 32 * (kEpiWarp0 + epi_warps(drained)); }
-constexpr int kProducers = 3, kStages = 8;
+constexpr int kEpiWarp0 = 4, kMmaWarp = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kProducers = 3, kStages = 8, kLeastStages = 6;
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's rows of a, a step
 constexpr uint32_t kOverlap = 32;             // columns that the accumulators of 256 columns share
 // Tensor memory behind them: two sets of scales, of a in the first four of 16 columns.
 constexpr uint32_t kScaleCol = 512 - kOverlap, kScaleCols = 16, kAllCols = 512;
-constexpr int kScaleSteps = 4;                // bytes of a word
-constexpr int kScaleSlots = 4;                // in shared memory
-constexpr uint32_t kScaleSlot = kScaleWarps * 512, kScaleBytes = kScaleSlots * kScaleSlot;
+constexpr int kScaleSteps = 4;                // blocks whose exponents make a word
+constexpr uint32_t kScaleBytes = 3 * 512;     // a stage's exponents: of 128 rows of a, 256 of b
 constexpr int kDrainSteps = 8;                // steps of a drained accumulator, and of fp32 sums that are not drained
 constexpr int kMostSteps = 128;               // of bf16 ones
-constexpr uint32_t kMaxSmem = 227 * 1024 - 12 * 1024;   // (static: the runs' table, barriers)
+constexpr uint32_t kTurnBytes = 2048;         // of an epilogue warp: 32 rows of 64 bytes
+constexpr uint32_t kMaxSmem = 227 * 1024 - 9 * 1024;   // (static: the runs' table, barriers)
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
-// Registers of a thread, drained: 8 warps of 56 and 8 of 200 are what 512 threads are launched with (128 each).
-constexpr int kFewRegs = 56, kManyRegs = 200;
+// Registers of a thread: 4 warps of 72 and 8 of 216 are what 384 threads are launched with (168 each).
+constexpr int kFewRegs = 72, kManyRegs = 216;
 
 __device__ int g_status;
 
 struct Args {
-    CUtensorMap a, b;
-    const float *sa, *sb, *bias;
-    int64_t rows, M;          // of a; of b (columns of Y)
-    int64_t sa_cols, sb_cols, KB;
-    int a_shift, b_shift;     // rows that share a scale: 1 << shift
+    CUtensorMap a, b, ea, eb; // values; exponents
+    const float *bias;
+    int64_t rows, M, KB;      // of a; of b (columns of Y); blocks
     int group, E;
     const int32_t *offsets;
     unsigned tiles_m, tiles_n;
-    int splits;               // of a tile's steps
+    int splits;               // of a tile's steps, each a multiple of kScaleSteps
     int half, ns;
     uint32_t stage_bytes, idesc;
     void *Y;
@@ -93,10 +91,10 @@ struct Args {
 };
 
 struct Unit {
-    int64_t m0, m1, n0;   // first row, end of the rows, first column
-    int64_t out;          // rows of Y before this unit's matrix
+    int64_t m0, r0, r1, n0;   // first row; the rows that are the unit's; first column
+    int64_t out;              // rows of Y before this unit's matrix
     int batch, part;
-    int i0, i1;           // steps
+    int i0, i1;               // steps
 };
 
 // The runs: their ends, and the tiles of rows before each.
@@ -105,7 +103,7 @@ struct Runs {
     uint32_t first[kMostExperts + 1];
 };
 
-__device__ __forceinline__ Unit unit_at(const Args &a, const Runs &r, unsigned v) {
+__device__ __forceinline__ Unit unit_of(const Args &a, const Runs &r, unsigned v) {
     Unit u;
     u.out = 0;
     u.batch = 0;
@@ -121,8 +119,9 @@ __device__ __forceinline__ Unit unit_at(const Args &a, const Runs &r, unsigned v
             else hi = mid;
         }
         u.batch = lo;
-        u.m0 = r.at[lo] + (int64_t)(t - r.first[lo]) * 256;
-        u.m1 = r.at[lo + 1];
+        u.r0 = r.at[lo];
+        u.r1 = r.at[lo + 1];
+        u.m0 = u.r0 / 128 * 128 + (int64_t)(t - r.first[lo]) * 256;
         u.n0 = (int64_t)(v - t * a.tiles_n) * 2 * a.half;
         return u;
     }
@@ -137,14 +136,29 @@ __device__ __forceinline__ Unit unit_at(const Args &a, const Runs &r, unsigned v
         u.part = (int)v;
         tile = v / (unsigned)a.splits;
         const unsigned k = v - tile * (unsigned)a.splits;
-        u.i0 = (int)(a.KB * k / a.splits);
-        u.i1 = (int)(a.KB * (k + 1) / a.splits);
+        const int64_t words = (a.KB + kScaleSteps - 1) / kScaleSteps;
+        u.i0 = (int)(words * k / a.splits) * kScaleSteps;
+        u.i1 = (int)min(a.KB, words * (k + 1) / a.splits * kScaleSteps);
     }
     const unsigned tm = tile / a.tiles_n;
     u.m0 = (int64_t)tm * 256;
-    u.m1 = a.rows;
+    u.r0 = 0;
+    u.r1 = a.rows;
     u.n0 = (int64_t)(tile - tm * a.tiles_n) * 2 * a.half;
     return u;
+}
+
+// One copy of the code for all roles, as cold instructions are what a short call waits
+// for; but for drained sums, whose registers a call would push out.
+__device__ __noinline__ Unit unit_call(const Args &a, const Runs &r, unsigned v) { return unit_of(a, r, v); }
+template <bool DRAIN>
+__device__ __forceinline__ Unit unit_at(const Args &a, const Runs &r, unsigned v) {
+    return DRAIN ? unit_of(a, r, v) : unit_call(a, r, v);
+}
+
+// Tiles of the rows o .. p - 1, from a multiple of 128 on.
+__device__ __forceinline__ uint32_t tiles_of(int32_t o, int32_t p) {
+    return p > o ? ((uint32_t)p - (uint32_t)o / 128 * 128 + 255) / 256 : 0;
 }
 
 // The unit of a pair in a round of them: all rounds but the first are taken
@@ -153,77 +167,83 @@ __device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsig
     return round * pairs + (round ? pairs - 1 - pair : pair);
 }
 
-// 32 rows of the result from `row` on (of this thread: row + lane / 4 + 8 h) x 32 columns
-// from c on: x[h][j], columns 8 j + 2 (lane % 4), + 1.
+// Where 16 bytes of the 64 of a row lie, so that eight lanes' rows, and the four runs of two rows, fall on different banks.
+__device__ __forceinline__ uint4 *turned(unsigned char *buf, int row, int chunk) {
+    return reinterpret_cast<uint4 *>(buf + row * 64 + 16 * (chunk ^ ((row >> 1) & 3)));
+}
+
+// 32 rows of the result from `row` on x 32 columns from c on; x: those of row + lane.
 template <typename T>
-__device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, int64_t c, const F2 (&x)[4][4]) {
-    const int lane = threadIdx.x & 31, c4 = lane & 3;
-    row += lane >> 2;
-    if (un.part >= 0) {
+__device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, int64_t c, float (&x)[32], unsigned char *buf) {
+    const int lane = threadIdx.x & 31, up = lane >> 2, chunk = lane & 3;
+    const bool part = un.part >= 0;
+    if (a.bias && !part) {
+        const float *bias = a.bias + (int64_t)un.batch * a.M + c;
 #pragma unroll
-        for (int h = 0; h < 4; h++) {
-            float *at = a.parts + ((int64_t)un.part * 256 + (row - un.m0) + 8 * h) * 2 * a.half + (c - un.n0) + 2 * c4;
-#pragma unroll
-            for (int j = 0; j < 4; j++) *reinterpret_cast<float2 *>(at + 8 * j) = unpack2(x[h][j]);
-        }
-        return;
+        for (int j = 0; j < 32; j++) x[j] += c + j < a.M ? __ldg(bias + j) : 0.f;
     }
-    F2 add[4];
+    if (sizeof(T) == 2 && !part) {
 #pragma unroll
-    for (int j = 0; j < 4; j++) add[j] = all2(0.f);
-    if (a.bias) {
+        for (int j = 0; j < 4; j++)
+            *turned(buf, lane, j) = make_uint4(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]),
+                                               pack_bf16(x[8 * j + 4], x[8 * j + 5]), pack_bf16(x[8 * j + 6], x[8 * j + 7]));
+        __syncwarp();
+        T *out = static_cast<T *>(a.Y) + (un.out + row + up) * a.M + c + 8 * chunk;
+        const int64_t n = a.M - (c + 8 * chunk);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const int64_t at = c + 8 * j + 2 * c4;
-            const float *bias = a.bias + (int64_t)un.batch * a.M + at;
-            add[j] = pack2(at < a.M ? __ldg(bias) : 0.f, at + 1 < a.M ? __ldg(bias + 1) : 0.f);
+        for (int i = 0; i < 4; i++) {
+            const uint4 w = *turned(buf, up + 8 * i, chunk);
+            const int64_t r = row + up + 8 * i;
+            if (r >= un.r0 && r < un.r1) {
+                Eight<uint16_t> e;
+                e.w[0] = w.x, e.w[1] = w.y, e.w[2] = w.z, e.w[3] = w.w;
+                store8(reinterpret_cast<uint16_t *>(out + 8 * i * a.M), n, a.align, e);
+            }
         }
-    }
+        __syncwarp();
+    } else {
+        // (fp32: 16 columns at a time)
 #pragma unroll
-    for (int h = 0; h < 4; h++) {
-        F2 y[4];
-#pragma unroll
-        for (int j = 0; j < 4; j++) y[j] = add2(x[h][j], add[j]);
-        uint32_t w[4];
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int j = 0; j < 4; j++) w[j] = pack_bf16(y[j]);
-            turn_words(w);
-        }
-        if (row + 8 * h >= un.m1) continue;
-        T *out = static_cast<T *>(a.Y) + (un.out + row + 8 * h) * a.M;
-        if constexpr (sizeof(T) == 2) {
-            Eight<T> e;
-#pragma unroll
-            for (int j = 0; j < 4; j++) e.w[j] = w[j];
-            store8(out + c + 8 * c4, a.M - (c + 8 * c4), a.align, e);
-        } else {
+        for (int half = 0; half < 2; half++) {
 #pragma unroll
             for (int j = 0; j < 4; j++) {
-                const int64_t at = c + 8 * j + 2 * c4;
-                const float2 z = unpack2(y[j]);
-                if (at + 2 <= a.M && a.align >= 8) {
-                    *reinterpret_cast<float2 *>(out + at) = z;
-                } else {
-                    if (at < a.M) out[at] = z.x;
-                    if (at + 1 < a.M) out[at + 1] = z.y;
+                const float *v = x + 16 * half + 4 * j;
+                *turned(buf, lane, j) = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            }
+            __syncwarp();
+            const int64_t at = c + 16 * half + 4 * chunk;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                const uint4 w = *turned(buf, up + 8 * i, chunk);
+                const int64_t r = row + up + 8 * i;
+                if (part) {
+                    *reinterpret_cast<uint4 *>(a.parts + ((int64_t)un.part * 256 + (r - un.m0)) * 2 * a.half + (at - un.n0)) = w;
+                } else if (r >= un.r0 && r < un.r1) {
+                    float *out = static_cast<float *>(a.Y) + (un.out + r) * a.M + at;
+                    if (at + 4 <= a.M && a.align == 16) {
+                        *reinterpret_cast<uint4 *>(out) = w;
+                    } else {
+                        const uint32_t v[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                        for (int j = 0; j < 4; j++)
+                            if (at + j < a.M) out[j] = __uint_as_float(v[j]);
+                    }
                 }
             }
+            __syncwarp();
         }
     }
 }
 
 template <typename T, bool DRAIN>
-__global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __grid_constant__ Args a) {
-    constexpr int kEpiWarps = epi_warps(DRAIN);
+__global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_constant__ Args a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
     const int ns = a.ns;
     const uint32_t stage_bytes = a.stage_bytes;
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], done;
-    __shared__ uint64_t scales_full[kScaleSlots], scales_empty[kScaleSlots];
     __shared__ int stop, loads[kProducers][2];   // loads[producer][CTA of the pair]: steps loaded
-    __shared__ int freed, handed, copied;        // commits issued to `empty`, `acc_full` and `scales_empty`
+    __shared__ int freed, handed;                // commits issued to `empty` and to `acc_full`
     __shared__ uint32_t tmem_s;
     __shared__ Runs runs;
 
@@ -240,18 +260,16 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             ptx::mbar_init(&acc_full[i], 1);
             ptx::mbar_init(&acc_empty[i], 2 * kEpiWarps);
         }
-        for (int i = 0; i < kScaleSlots; i++) {
-            ptx::mbar_init(&scales_full[i], 2 * kScaleWarps);
-            ptx::mbar_init(&scales_empty[i], 1);
-        }
         ptx::mbar_init(&done, 1);
-        stop = freed = handed = copied = 0;
+        stop = freed = handed = 0;
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, kAllCols);
     if (warp == 0 && ptx::elect_one()) {
         ptx::prefetch_tensormap(&a.a);
         ptx::prefetch_tensormap(&a.b);
+        ptx::prefetch_tensormap(&a.ea);
+        ptx::prefetch_tensormap(&a.eb);
     }
     tc5::fence_before();
     __syncthreads();
@@ -263,7 +281,7 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
     if (a.group != BSR_GROUP_NONE) {
         // within what there is, in steps for columns
         const bool by_rows = a.group == BSR_GROUP_ROWS;
-        for (int e = threadIdx.x; e <= a.E; e += threads_of(DRAIN)) {
+        for (int e = threadIdx.x; e <= a.E; e += kThreads) {
             const int64_t o = max(0, __ldg(a.offsets + e));
             runs.at[e] = (int32_t)(by_rows ? min(o, a.rows) : min(o / kFp8Block, a.KB));
         }
@@ -272,7 +290,7 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             uint32_t before = 0;
             for (int e0 = 0; e0 < a.E; e0 += 32) {
                 const int e = e0 + lane;
-                const uint32_t tiles = e < a.E ? (uint32_t)(max(0, runs.at[e + 1] - runs.at[e]) + 255) / 256 : 0;
+                const uint32_t tiles = e < a.E ? tiles_of(runs.at[e], runs.at[e + 1]) : 0;
                 uint32_t upto = tiles;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
@@ -288,7 +306,6 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
         units = by_rows ? runs.first[a.E] * a.tiles_n : units * (unsigned)a.E;
     }
     const uint32_t tmem = tmem_s;
-    unsigned char *scales_s = base + (size_t)ns * stage_bytes;
     const bool elected = ptx::elect_one();
     // stops every role of this pair; a timeout is recorded
     auto halt = [&]() {
@@ -305,7 +322,7 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
     // parity, would let it pass a round early; its last wait, for step
     // g - np - ns, tells it so if np <= ns.
     const int prod = warp < kMmaWarp ? warp : kMmaWarp, np = min(kProducers, ns);
-    const bool producer = warp < kScaleWarp0 && warp != kMmaWarp && prod < np;
+    const bool producer = warp < kEpiWarp0 && warp != kMmaWarp && prod < np;
     unsigned round = 0, v = pair;
     Unit un = {};
     int i = 0, s = prod % ns, issued = 0;
@@ -319,7 +336,7 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             const int over = i - un.i1;
             v = unit_in(++round, pair, pairs);
             if (v >= units) return false;
-            un = unit_at(a, runs, v);
+            un = unit_at<DRAIN>(a, runs, v);
             i = un.i0 + over;
         }
         return true;
@@ -329,9 +346,16 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             stalled |= 1u << s;
         } else if (elected) {
             const uint32_t dst = smem0 + s * stage_bytes, bar = first0 + 8 * s;
-            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * stage_bytes);
-            ptx::tma_load_2d_pair_at(dst, &a.a, i * kFp8Block, (int)(un.m0 + rank * 128), bar);
-            ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, (int)(un.n0 + rank * a.half), un.batch, bar);
+            const bool scales = i == un.i0 || i % kScaleSteps == 0;
+            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (stage_bytes + (scales ? (a.half == 128 ? 3 : 2) * 512 : 0)));
+            const int m = (int)(un.m0 + rank * 128), n = (int)un.n0;
+            ptx::tma_load_2d_pair_at(dst, &a.a, i * kFp8Block, m, bar);
+            ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, n + (int)rank * a.half, un.batch, bar);
+            if (scales) {
+                const uint32_t to = smem0 + ns * stage_bytes + s * kScaleBytes;
+                ptx::tma_load_3d_pair_at(to, &a.ea, 0, m / 128, i / kScaleSteps, bar);
+                ptx::tma_load_4d_pair_at(to + 512, &a.eb, 0, n / 128, i / kScaleSteps, un.batch, bar);
+            }
         }
         issued++;
         for (s += np; s >= ns; s -= ns) phase ^= 1;
@@ -345,9 +369,9 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
     const uint32_t acc_step = shared_cols ? 256 - kOverlap : 128;
     if (warp >= kEpiWarp0) {
         if constexpr (DRAIN) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegs));
-        const int q = warp & 3, share = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., a share of the columns
-        const int all = a.half / 16, each = (all + kEpiWarps / 4 - 1) / (kEpiWarps / 4), first = share * each,
-                  groups = max(0, min(each, all - first));          // of 32 columns
+        const int q = warp & 3, share = (warp - kEpiWarp0) >> 2;   // tensor-memory lanes 32 q .., half the columns
+        const int groups = a.half / 32, first = share * groups;      // of 32 columns
+        unsigned char *buf = base + (size_t)ns * (stage_bytes + kScaleBytes) + (warp - kEpiWarp0) * kTurnBytes;
         int ab = 0;
         uint32_t fphase = 0;
         bool ok = true;
@@ -366,90 +390,81 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             ab ^= 1;
             if (ab == 0) fphase ^= 1;
         };
-        auto load = [&](uint32_t tm, uint32_t (&r)[2][16]) {
-            tc5::ld_16x32(tm, r[0]);
-            tc5::ld_16x32(tm + (16u << 16), r[1]);
-        };
-        auto loaded = [&](uint32_t (&r)[2][16]) {
+        auto load = [&](uint32_t tm, uint32_t (&r)[32]) {
+            tc5::ld32(tm, r);
             tc5::ld_wait();
 #pragma unroll
-            for (int j = 0; j < 16; j++) {   // no use of a loaded register moves above the wait
-                asm volatile("" : "+r"(r[0][j]));
-                asm volatile("" : "+r"(r[1][j]));
-            }
-        };
-        // rows lane / 4 + 8 h, columns 8 j + 2 (lane % 4), + 1 of what was loaded
-        auto at = [&](const uint32_t (&r)[2][16], int h, int j) {
-            const uint32_t *x = &r[h >> 1][4 * j + 2 * (h & 1)];
-            return pack2(__uint_as_float(x[0]), __uint_as_float(x[1]));
+            for (int j = 0; j < 32; j++) asm volatile("" : "+r"(r[j]));   // no use of a loaded register moves above the wait
         };
         for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-            un = unit_at(a, runs, v);
+            un = unit_at<DRAIN>(a, runs, v);
             const int64_t row = un.m0 + rank * 128 + 32 * q, col = un.n0 + 32 * first;
             if constexpr (!DRAIN) {
                 const bool any = un.i1 > un.i0;
                 uint32_t tm = 0;
                 // the columns that the next tile's accumulator has too, first
-                const bool back = shared_cols && ab == 0, mine = !shared_cols || (ab == 0 ? first + groups == all : first == 0);
+                const bool back = shared_cols && ab == 0, mine = !shared_cols || (ab == 0 ? share == 1 : share == 0);
                 if (any) {
                     tm = wait_acc(un);
                     if (!ok) break;
-                    if (groups == 0 || !mine) hand_back();
+                    if (!mine) hand_back();
                 }
+#pragma unroll 1
                 for (int p = 0; p < groups; p++) {
                     const int g = back ? groups - 1 - p : p;
-                    uint32_t r[2][16];
+                    uint32_t r[32];
+                    float x[32];
+#pragma unroll
+                    for (int j = 0; j < 32; j++) r[j] = 0;
                     if (any) {
                         load(tm + 32 * g, r);
-                        loaded(r);
                         if (mine && p == (shared_cols ? 0 : groups - 1)) hand_back();
                     }
-                    F2 x[4][4];
 #pragma unroll
-                    for (int h = 0; h < 4; h++)
-#pragma unroll
-                        for (int j = 0; j < 4; j++) x[h][j] = any ? at(r, h, j) : all2(0.f);
-                    put<T>(a, un, row, col + 32 * g, x);
+                    for (int j = 0; j < 32; j++) x[j] = __uint_as_float(r[j]);
+                    put<T>(a, un, row, col + 32 * g, x, buf);
                 }
                 if (any) next_acc();
             } else {
-                F2 sum[4][4][4];   // [group]
+                float sum[4][32];   // [group]
 #pragma unroll
                 for (int g = 0; g < 4; g++)
 #pragma unroll
-                    for (int j = 0; j < 16; j++) sum[g][j >> 2][j & 3] = all2(0.f);
+                    for (int j = 0; j < 32; j++) sum[g][j] = 0.f;
                 for (int b = un.i0; b < un.i1; b += kDrainSteps) {
                     const uint32_t tm = wait_acc(un);
                     if (!ok) break;
-                    if (groups == 0) hand_back();
                     // both ends first: one of them is shared
                     constexpr int order[4] = {0, 3, 1, 2};
 #pragma unroll
                     for (int p = 0; p < 4; p++) {
                         const int g = order[p];
                         if (g >= groups) continue;
-                        uint32_t r[2][16];
+                        uint32_t r[32];
                         load(tm + 32 * g, r);
-                        loaded(r);
                         if (shared_cols ? p == 1 : g == groups - 1) hand_back();
 #pragma unroll
-                        for (int h = 0; h < 4; h++)
-#pragma unroll
-                            for (int j = 0; j < 4; j++) sum[g][h][j] = add2(sum[g][h][j], at(r, h, j));
+                        for (int j = 0; j < 32; j++) sum[g][j] += __uint_as_float(r[j]);
                     }
                     next_acc();
                 }
                 if (!ok) break;
+                // one copy of the code, the sums handed on from group to group
+#pragma unroll 1
+                for (int g = 0; g < groups; g++) {
+                    put<T>(a, un, row, col + 32 * g, sum[0], buf);
 #pragma unroll
-                for (int g = 0; g < 4; g++)
-                    if (g < groups) put<T>(a, un, row, col + 32 * g, sum[g]);
+                    for (int k = 0; k < 3; k++)
+#pragma unroll
+                        for (int j = 0; j < 32; j++) sum[k][j] = sum[k + 1][j];
+                }
             }
         }
     } else {
         if constexpr (DRAIN) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
         if (producer) {
             if (v < units) {
-                un = unit_at(a, runs, v);
+                un = unit_at<DRAIN>(a, runs, v);
                 i = un.i0 + prod;
                 more = seek();
             }
@@ -465,98 +480,59 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
                 loads[prod][rank] = issued;
                 ptx::store_cluster(ptx::map_to_cta(&loads[prod][rank], rank ^ 1), (uint32_t)issued);
             }
-        } else if (warp >= kScaleWarp0 && warp < kScaleWarp0 + kScaleWarps) {
-            // row r of this warp's 128 is word 4 (r % 32) + r / 32 of its 512 bytes
-            const int which = warp - kScaleWarp0, shift = which ? a.b_shift : a.a_shift;
-            const bool needed = which < 2 || a.half == 128;   // (all three arrive at the barrier)
-            const uint32_t full0 = ptx::map_to_cta(&scales_full[0], 0);
-            int slot = 0;
-            uint32_t sphase = 1;
-            bool ok = true;
-            for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-                un = unit_at(a, runs, v);
-                const int64_t row0 = which ? un.n0 + (which - 1) * 128 : un.m0 + rank * 128, rows = which ? a.M : a.rows,
-                              cols = which ? a.sb_cols : a.sa_cols;
-                const float *from = which ? a.sb + (int64_t)un.batch * a.KB * cols : a.sa;
-                int64_t at[4];   // (rows that are not there take another's)
-#pragma unroll
-                for (int c = 0; c < 4; c++) at[c] = min(row0 + 32 * c + lane, rows - 1) >> shift;
-                for (int b = un.i0; b < un.i1; b += kScaleSteps) {
-                    uint32_t x[kScaleSteps][4];
-#pragma unroll
-                    for (int k = 0; k < kScaleSteps; k++)
-#pragma unroll
-                        for (int c = 0; c < 4; c++) x[k][c] = needed && b + k < un.i1 ? __float_as_uint(__ldg(from + (b + k) * cols + at[c])) : 0;
-                    ok = __all_sync(0xffffffffu, wait_or_abort(&scales_empty[slot], sphase, a.wait_ns, &stop));
-                    if (!ok) {
-                        halt();
-                        break;
-                    }
-                    uint32_t w[4];
-#pragma unroll
-                    for (int c = 0; c < 4; c++)   // (a scale's bits are its exponent's byte, above 23 zeros)
-                        w[c] = ((x[0][c] >> 23) & 0xff) | ((x[1][c] >> 23) & 0xff) << 8 | ((x[2][c] >> 23) & 0xff) << 16 | ((x[3][c] >> 23) & 0xff) << 24;
-                    *reinterpret_cast<uint4 *>(scales_s + slot * kScaleSlot + which * 512 + 16 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
-                    ptx::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0) ptx::mbar_arrive_cluster(full0 + 8 * slot);
-                    if (++slot == kScaleSlots) slot = 0, sphase ^= 1;
-                }
-            }
         } else if (warp == kMmaWarp && rank == 0) {
-            int n_steps = 0, n_acc = 0, n_scales = 0;
+            int n_steps = 0, n_acc = 0, n_sets = 0;
+            int set_end[2] = {-1, -1};   // the last step that has read each set of exponents
             uint32_t fphase = 0;
             bool ok = true;
             s = 0;
             const uint64_t ad0 = tc5::desc_sw128(smem0), bd0 = tc5::desc_sw128(smem0 + kABytes);
-            const uint64_t sd0 = tc5::desc(ptx::smem_addr(scales_s), 16, 128);   // (eight rows of 16 bytes side by side)
+            const uint64_t sd0 = tc5::desc(smem0 + ns * stage_bytes, 16, 128);   // (eight rows of 16 bytes side by side)
             for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-                un = unit_at(a, runs, v);
+                un = unit_at<DRAIN>(a, runs, v);
                 for (i = un.i0; i < un.i1; i++) {
                     const int b = i - un.i0;
                     const bool fresh = DRAIN ? b % kDrainSteps == 0 : b == 0, last = i + 1 == un.i1 || (DRAIN && (b + 1) % kDrainSteps == 0);
+                    const bool scales = b == 0 || i % kScaleSteps == 0;
                     if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
                         const int wait_for = n_acc - (shared_cols ? 1 : 2);
                         if (wait_for >= 0)
                             ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[wait_for & 1], (uint32_t)(wait_for >> 1) & 1, a.wait_ns, &stop));
                         if (!ok) break;
                     }
-                    const int slot = n_scales % kScaleSlots;
-                    const uint32_t set = tmem + kScaleCol + (uint32_t)(n_scales & 1) * kScaleCols;
-                    if (b % kScaleSteps == 0) {
-                        const uint32_t sphase = (uint32_t)(n_scales / kScaleSlots) & 1;
-                        ok = wait_or_abort(&scales_full[slot], sphase, a.wait_ns, &stop) && ptx::mbar_try_wait_cluster(&scales_full[slot], sphase);
-                        // (tensor memory's set of two words before has been read: a copy does not wait for MMAs)
-                        const int before = n_scales - 2;
+                    if (scales) {
+                        // the set's last readers are done (a copy does not wait for MMAs): at most five
+                        // steps back, fewer than the ring has stages, so that the stage's barrier tells
+                        const int before = set_end[n_sets & 1];
                         if (before >= 0)
-                            ok = ok && wait_or_abort(&scales_empty[before % kScaleSlots], (uint32_t)(before / kScaleSlots) & 1, a.wait_ns, &stop);
-                        ok = __all_sync(0xffffffffu, ok);
+                            ok = __all_sync(0xffffffffu, wait_or_abort(&empty[before % ns], (uint32_t)(before / ns) & 1, a.wait_ns, &stop));
                         if (!ok) break;
+                        n_sets++;
                     }
                     ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
                     if (!ok) break;
                     tc5::fence_after();
+                    const uint32_t set = tmem + kScaleCol + (uint32_t)((n_sets - 1) & 1) * kScaleCols;
                     if (elected) {
-                        if (b % kScaleSteps == 0) {
-                            const uint64_t sd = sd0 + (uint64_t)((slot * kScaleSlot) >> 4);
+                        const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
+                        if (scales) {
+                            const uint64_t sd = sd0 + (uint64_t)((s * kScaleBytes) >> 4);
                             tc5::copy_pair_32x16(set, sd);
                             tc5::copy_pair_32x16(set + 4, sd + (512 >> 4));
                             if (shared_cols) tc5::copy_pair_32x16(set + 8, sd + (1024 >> 4));
                         }
-                        const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
-                        const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)b % kScaleSteps);
+                        const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)i % kScaleSteps);
 #pragma unroll
                         for (int j = 0; j < kFp8Block / 32; j++)   // (32 bytes along the rows)
                             tc5::mma_ss_pair_scaled(tmem + (uint32_t)(n_acc & 1) * acc_step, ad0 + stage + 2 * j, bd0 + stage + 2 * j, idesc, set,
                                                     set + 4, !fresh | (j > 0));
                         tc5::commit_pair(&empty[s]);
                         if (last) tc5::commit_pair(&acc_full[n_acc & 1]);
-                        if (b % kScaleSteps == kScaleSteps - 1 || i + 1 == un.i1) tc5::commit_pair(&scales_empty[slot]);
                     }
                     __syncwarp();
+                    set_end[(n_sets - 1) & 1] = n_steps;
                     n_steps++;
                     if (last) n_acc++;
-                    if (b % kScaleSteps == kScaleSteps - 1 || i + 1 == un.i1) n_scales++;
                     if (++s == ns) {
                         s = 0;
                         fphase ^= 1;
@@ -567,10 +543,9 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
             // every MMA issued has completed before the tensor memory is freed
             if (elected) {
                 tc5::commit_pair(&done);
-                freed = n_steps, handed = n_acc, copied = n_scales;
+                freed = n_steps, handed = n_acc;
                 ptx::store_cluster(ptx::map_to_cta(&freed, 1), (uint32_t)n_steps);
                 ptx::store_cluster(ptx::map_to_cta(&handed, 1), (uint32_t)n_acc);
-                ptx::store_cluster(ptx::map_to_cta(&copied, 1), (uint32_t)n_scales);
             }
             __syncwarp();
             ptx::mbar_wait_bounded(&done, 0, kDrainNs);
@@ -611,9 +586,6 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_fp8_product(const __gr
         if (lane < ns && lane < freed) {
             bar = &empty[lane];
             last = (freed - 1 - lane) / ns;
-        } else if (lane >= kStages && lane - kStages < min(kScaleSlots, copied)) {
-            bar = &scales_empty[lane - kStages];
-            last = (copied - 1 - (lane - kStages)) / kScaleSlots;
         } else if (lane >= 29 && lane - 29 < min(2, handed)) {
             bar = &acc_full[lane - 29];
             last = (handed - 1 - (lane - 29)) / 2;
@@ -663,19 +635,19 @@ struct Plan {
 // Half the columns of a tile, and the parts of its steps, by the cycles that the
 // busiest pair takes: a step, a unit's start and end, and a second launch that adds parts.
 Plan plan_of(const Fp8Product &p) {
-    const int64_t pairs = pairs_of_sms(), KB = fp8_blocks(p.a.cols);
+    const int64_t pairs = pairs_of_sms(), KB = fp8_blocks(p.a.cols), words = (KB + kScaleSteps - 1) / kScaleSteps;
     Plan best = {};
     double best_t = 0;
-    for (int half : {128, 64, 32}) {
+    for (int half : {128, 64}) {
         Plan q = {half, 1, (p.a.rows + 255) / 256, (p.b.rows + 2 * half - 1) / (2 * half), 0};
-        const double step = half == 128 ? 560 : half == 64 ? 400 : 330, unit = 1500 + 10 * half;
+        const double step = half == 128 ? 540 : 400, unit = 1000 + 10 * half;
         for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-            if (s > 1 && (p.group != BSR_GROUP_NONE || s > KB)) break;
+            if (s > 1 && (p.group != BSR_GROUP_NONE || s > words)) break;
             q.splits = s;
             int64_t tiles = q.tiles_m * q.tiles_n;
-            double steps = (double)((KB + s - 1) / s);
+            double steps = s == 1 ? (double)KB : (double)((words + s - 1) / s * kScaleSteps);
             if (p.group == BSR_GROUP_ROWS) {   // (as if every run ended in the middle of a tile)
-                tiles = (p.a.rows / 256 + std::min<int64_t>(p.groups, p.a.rows)) * q.tiles_n;
+                tiles = (p.a.rows / 256 + 2 * std::min<int64_t>(p.groups, p.a.rows)) * q.tiles_n;
             } else if (p.group == BSR_GROUP_COLUMNS) {
                 tiles *= p.groups;
                 steps = std::max(1.0, (double)KB / p.groups);
@@ -704,12 +676,26 @@ cudaError_t encode(const bsr_fp8_matrix_t &m, bool batch, int rows, CUtensorMap 
                : cudaErrorInvalidValue;
 }
 
+cudaError_t encode_exponents(const bsr_fp8_matrix_t &m, bool batch, int rows, CUtensorMap *map) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t runs = (cuuint64_t)fp8_blocks(m.rows), words = (cuuint64_t)fp8_words(m.cols);
+    const cuuint64_t dims[4] = {128, runs, words, (cuuint64_t)m.batch};
+    const cuuint64_t strides[3] = {512, 512 * runs, 512 * runs * words};
+    const cuuint32_t box[4] = {128, (cuuint32_t)(rows / 128), 1, 1};
+    const cuuint32_t estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, batch ? 4 : 3, m.exponent, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
 template <typename T, bool DRAIN>
 cudaError_t launch(const Args &a, unsigned grid, cudaStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
     cudaError_t e = allow_smem(k_fp8_product<T, DRAIN>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
-    return launch_clusters(k_fp8_product<T, DRAIN>, 2, dim3(grid), dim3(threads_of(DRAIN)), a.ns * a.stage_bytes + kScaleBytes + 1024, s, a);
+    return launch_clusters(k_fp8_product<T, DRAIN>, 2, dim3(grid), dim3(kThreads), a.ns * (a.stage_bytes + kScaleBytes) + kEpiWarps * kTurnBytes + 1024, s, a);
 }
 
 }  // namespace
@@ -724,18 +710,17 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     const Plan q = plan_of(p);
     if (q.units > INT32_MAX) return cudaErrorInvalidConfiguration;
     Args a = {};
-    a.sa = p.a.scale, a.sb = p.b.scale, a.bias = p.bias;
+    a.bias = p.bias;
     a.rows = p.a.rows, a.M = p.b.rows;
-    a.sa_cols = fp8_scale_cols(p.a), a.sb_cols = fp8_scale_cols(p.b);
     a.KB = fp8_blocks(p.a.cols);
-    a.a_shift = p.a.tile == 1 ? 0 : 7, a.b_shift = p.b.tile == 1 ? 0 : 7;
     a.group = p.group, a.E = p.groups;
     a.offsets = p.offsets;
     a.tiles_m = (unsigned)q.tiles_m, a.tiles_n = (unsigned)q.tiles_n;
     a.splits = q.splits;
     a.half = q.half;
     a.stage_bytes = kABytes + (uint32_t)q.half * kFp8Block;
-    a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 1024 - kScaleBytes) / a.stage_bytes);
+    static_assert(kLeastStages * (2 * kABytes + kScaleBytes) + kEpiWarps * kTurnBytes + 1024 <= kMaxSmem, "stages");
+    a.ns = (int)std::min<uint32_t>(kStages, (kMaxSmem - 1024 - kEpiWarps * kTurnBytes) / (a.stage_bytes + kScaleBytes));
     a.idesc = tc5::idesc_scaled(p.a.type, p.b.type, 256, 2 * q.half);
     a.Y = p.Y;
     a.parts = p.ws;
@@ -748,10 +733,13 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     if (a.KB > 0) {   // (sums of nothing load nothing)
         e = encode(p.a, false, 128, &a.a);
         if (e == cudaSuccess) e = encode(p.b, true, q.half, &a.b);
+        if (e == cudaSuccess) e = encode_exponents(p.a, false, 128, &a.ea);
+        if (e == cudaSuccess) e = encode_exponents(p.b, true, q.half == 128 ? 256 : 128, &a.eb);
     }
     if (e != cudaSuccess) return e;
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(q.units, pairs_of_sms());
-    const bool f32 = p.dt == BSR_F32, drained = (a.KB + q.splits - 1) / q.splits > (f32 ? kDrainSteps : kMostSteps);
+    const int64_t steps = q.splits == 1 ? a.KB : (fp8_words(p.a.cols) + q.splits - 1) / q.splits * kScaleSteps;
+    const bool f32 = p.dt == BSR_F32, drained = steps > (f32 ? kDrainSteps : kMostSteps);
     e = f32 ? (drained ? launch<float, true>(a, grid, s) : launch<float, false>(a, grid, s))
             : (drained ? launch<uint16_t, true>(a, grid, s) : launch<uint16_t, false>(a, grid, s));
     if (e != cudaSuccess || q.splits == 1) return e;

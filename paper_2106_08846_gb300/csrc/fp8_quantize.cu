@@ -29,7 +29,9 @@ struct QArgs {
     const void *x;
     int64_t R, C, KB, RB;   // blocks of columns and of rows
     uint8_t *q, *qt;        // rows of 128 KB and of 128 RB bytes
-    float *s, *st;
+    int64_t e_bytes, et_bytes;   // of a matrix's exponents
+    float *s, *st;          // (NULL: not wanted)
+    uint8_t *e, *et;        // exponents as bytes, in the tensor cores' order
     const int32_t *used;
     int align;              // bytes (at most 16) that rows of x are aligned to
 };
@@ -43,6 +45,11 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
     return max(e, -126);
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+
+// Where the exponent of block b of row r is (matrices of `runs` x 128 rows).
+__device__ __forceinline__ int64_t exponent_at(int64_t r, int64_t b, int64_t runs) {
+    return ((b >> 2) * runs + (r >> 7)) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4 + (b & 3);
+}
 
 // |x| as bits, 0 where it is not finite
 __device__ __forceinline__ uint32_t size_bits(float x) {
@@ -126,12 +133,17 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QA
         for (int w = 1; w < 8; w++) t = max(t, tops[w][0]);
         tile_e = scale_exponent<E5M2>(t);
         if (threadIdx.x == 0) {
-            if (ROWS) a.s[(batch * a.KB + kb) * a.RB + rb] = power_of_two(tile_e);
-            if (COLUMNS) a.st[(batch * a.RB + rb) * a.KB + kb] = power_of_two(tile_e);
+            if (ROWS && a.s) a.s[(batch * a.KB + kb) * a.RB + rb] = power_of_two(tile_e);
+            if (COLUMNS && a.st) a.st[(batch * a.RB + rb) * a.KB + kb] = power_of_two(tile_e);
+        }
+        const int r = threadIdx.x;   // of the block
+        if (r < kFp8Block) {
+            if (ROWS) a.e[batch * a.e_bytes + exponent_at(rb * kFp8Block + r, kb, a.RB)] = (uint8_t)(tile_e + 127);
+            if (COLUMNS) a.et[batch * a.et_bytes + exponent_at(kb * kFp8Block + r, rb, a.KB)] = (uint8_t)(tile_e + 127);
         }
     }
     if constexpr (ROWS) {
-        float mine = 1.f;   // of row l, for lanes l < 8
+        int mine = 0;   // of row l, for lanes l < 8
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             int e = tile_e;
@@ -139,14 +151,17 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QA
 #pragma unroll
                 for (int m = 8; m; m /= 2) row_top[i] = max(row_top[i], __shfl_xor_sync(0xffffffffu, row_top[i], m));
                 e = scale_exponent<E5M2>(row_top[i]);
-                if (l == i) mine = power_of_two(e);
+                if (l == i) mine = e;
             }
             const float inv = power_of_two(-e);
             const uint32_t w0 = round2<E5M2>(x[i][0], x[i][1], inv) | round2<E5M2>(x[i][2], x[i][3], inv) << 16,
                            w1 = round2<E5M2>(x[i][4], x[i][5], inv) | round2<E5M2>(x[i][6], x[i][7], inv) << 16;
             if (row0 + i < R) *reinterpret_cast<uint2 *>(a.q + ((batch * a.R + row0 + i) * a.KB + kb) * kFp8Block + 8 * l) = make_uint2(w0, w1);
         }
-        if (!TILE && l < 8 && row0 + l < R) a.s[(batch * a.KB + kb) * a.R + row0 + l] = mine;
+        if (!TILE && l < 8 && row0 + l < R) {
+            if (a.s) a.s[(batch * a.KB + kb) * a.R + row0 + l] = power_of_two(mine);
+            a.e[batch * a.e_bytes + exponent_at(row0 + l, kb, a.RB)] = (uint8_t)(mine + 127);
+        }
     }
     if constexpr (COLUMNS) {
         if constexpr (!TILE) {
@@ -162,7 +177,10 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QA
                 for (int w = 1; w < 8; w++) t = max(t, tops[w][threadIdx.x]);
                 const int e = scale_exponent<E5M2>(t);
                 const int64_t c = kb * kFp8Block + threadIdx.x;
-                if (c < a.C) a.st[(batch * a.RB + rb) * a.C + c] = power_of_two(e);
+                if (c < a.C) {
+                    if (a.st) a.st[(batch * a.RB + rb) * a.C + c] = power_of_two(e);
+                    a.et[batch * a.et_bytes + exponent_at(c, rb, a.KB)] = (uint8_t)(e + 127);
+                }
                 tops[0][threadIdx.x] = __float_as_uint(power_of_two(-e));
             }
             __syncthreads();
@@ -210,8 +228,9 @@ cudaError_t launch_fp8_quantize(const void *x, bsr_dtype_t dt, int64_t batch, in
     a.x = x;
     a.R = R, a.C = C;
     a.KB = fp8_blocks(C), a.RB = fp8_blocks(R);
-    if (rows) a.q = static_cast<uint8_t *>(rows->q), a.s = rows->scale;
-    if (columns) a.qt = static_cast<uint8_t *>(columns->q), a.st = columns->scale;
+    if (rows) a.q = static_cast<uint8_t *>(rows->q), a.s = rows->scale, a.e = rows->exponent;
+    if (columns) a.qt = static_cast<uint8_t *>(columns->q), a.st = columns->scale, a.et = columns->exponent;
+    a.e_bytes = fp8_words(C) * a.RB * 512, a.et_bytes = fp8_words(R) * a.KB * 512;
     a.used = used;
     const int64_t bytes = C * (dt == BSR_F32 ? 4 : 2) | 16;
     a.align = (int)(bytes & -bytes);

@@ -63,13 +63,13 @@ def test_fp8_refusals(lib):
     n = ctypes.c_size_t(7)
     d, e, f = ctypes.c_void_p(256), ctypes.c_void_p(1 << 30), ctypes.c_void_p(1 << 32)
 
-    def m(rows=64, cols=256, tile=1, type=0, batch=1, q=1 << 20, scale=1 << 24):
-        return b._Fp8Matrix(batch, rows, cols, tile, type, q, scale)
+    def m(rows=64, cols=256, tile=1, type=0, batch=1, q=1 << 20, exponent=1 << 24, scale=1 << 27):
+        return b._Fp8Matrix(batch, rows, cols, tile, type, q, exponent, scale)
 
     def quantize(rows=None, columns=None, x=d, dt=0, used=None):
         return lib.bsr_fp8_quantize(x, dt, rows, columns, used, None)
 
-    assert quantize() == quantize(m(), x=None) == quantize(m(q=None)) == quantize(m(scale=None)) == b.BSR_ERR_INVALID_ARG
+    assert quantize() == quantize(m(), x=None) == quantize(m(q=None)) == quantize(m(exponent=None)) == b.BSR_ERR_INVALID_ARG
     assert quantize(m(rows=-1)) == quantize(m(), m(rows=256, cols=-1)) == b.BSR_ERR_INVALID_ARG
     assert quantize(m(tile=64)) == quantize(m(type=2)) == quantize(m(), dt=2) == b.BSR_ERR_UNSUPPORTED
     for other in (m(rows=256, cols=65), m(rows=255, cols=64), m(rows=256, cols=64, tile=128), m(rows=256, cols=64, type=1),
@@ -78,11 +78,11 @@ def test_fp8_refusals(lib):
     assert quantize(m(batch=2), used=d) == quantize(m(batch=65536)) == quantize(m(rows=1 << 31)) == b.BSR_ERR_SHAPE
     assert quantize(m(rows=1 << 30, cols=1 << 20)) == b.BSR_ERR_SHAPE
     assert quantize(m(rows=0), x=None) == quantize(m(cols=0), x=None) == b.BSR_OK
-    assert quantize(m(), x=ctypes.c_void_p(264)) == quantize(m(q=(1 << 20) + 8)) == b.BSR_ERR_ALIGNMENT
+    assert quantize(m(), x=ctypes.c_void_p(264)) == quantize(m(q=(1 << 20) + 8)) == quantize(m(exponent=(1 << 24) + 8)) == b.BSR_ERR_ALIGNMENT
     assert quantize(m(q=512)) == b.BSR_ERR_INVALID_ARG   # over x
 
     def product(a=None, w=None, bias=None, Y=f, dt=1, group=0, offsets=None, groups=0, ws=None, size=0):
-        a, w = a or m(), w or m(rows=32, tile=128, q=1 << 25, scale=1 << 26)
+        a, w = a or m(), w or m(rows=32, tile=128, q=1 << 25, exponent=1 << 26)
         return lib.bsr_fp8_product(a, w, bias, Y, dt, group, offsets, groups, ws, size, None)
 
     for bad in (dict(w=m(cols=255)), dict(a=m(batch=2)), dict(w=m(batch=2)), dict(group=1, groups=0, offsets=d),
@@ -92,7 +92,7 @@ def test_fp8_refusals(lib):
     for bad in (dict(dt=2), dict(group=3), dict(a=m(tile=2)), dict(w=m(type=-1))):
         assert product(**bad) == b.BSR_ERR_UNSUPPORTED
     for bad in (dict(offsets=d), dict(group=2, groups=2), dict(group=2, groups=2, offsets=d, bias=d), dict(Y=None),
-                dict(a=m(q=None)), dict(w=m(scale=None))):
+                dict(a=m(q=None)), dict(w=m(exponent=None))):
         assert product(**bad) == b.BSR_ERR_INVALID_ARG
     assert lib.bsr_fp8_product(None, m(), None, f, 1, 0, None, 0, None, 0, None) == b.BSR_ERR_INVALID_ARG
     assert product(Y=ctypes.c_void_p((1 << 32) + 8), size=1 << 40, ws=e) == b.BSR_ERR_ALIGNMENT

@@ -43,6 +43,16 @@ def same(m, q, scale):
     assert torch.equal(torch.signbit(m.q.float()) & ~got.isnan(), torch.signbit(q) & ~q.isnan())
 
 
+def check_exponents(m, rows=None, blocks=None):
+    """A byte for each row and block, in the order that include/bsr.h gives."""
+    rows, blocks = m.rows if rows is None else rows, -(-m.cols // 128) if blocks is None else blocks
+    r, b = torch.arange(rows, device="cuda").view(-1, 1), torch.arange(blocks, device="cuda")
+    runs = -(-m.rows // 128)
+    at = ((b // 4) * runs + r // 128) * 512 + (r % 32) * 16 + (r // 32 % 4) * 4 + b % 4
+    want = 127 + torch.log2(m.scale.double()).round().long()[:blocks, :].repeat_interleave(m.tile, 1)[:, :rows].T
+    assert torch.equal(m.exponent.view(-1)[at.reshape(-1)].long().view(rows, blocks), want)
+
+
 def filled(m):
     m.q.view(torch.uint8).fill_(0x55)
     m.scale.fill_(-7.0)
@@ -61,6 +71,8 @@ def test_quantize(R, C, dtype, tile, fmt):
     assert got == (rows, columns)
     same(rows, *quantized(x, tile, fmt))
     same(columns, *quantized(x.T, tile, fmt))
+    check_exponents(rows)
+    check_exponents(columns)
     for form, of in (("rows", rows), ("columns", columns)):
         one = bsr.bsr_fp8_quantize(x, tile, fmt, form)
         assert torch.equal(one.q.view(torch.uint8), of.q.view(torch.uint8)) and torch.equal(one.scale, of.scale)
@@ -108,6 +120,8 @@ def test_quantize_rows_in_use(used):
     whole = -(-n // 128)
     assert torch.equal(columns.q[:, :128 * whole].double(), q[:, :128 * whole]) and torch.equal(columns.scale[:whole].double(), scale[:whole])
     assert (columns.q[:, 128 * whole:].view(torch.uint8) == 0x55).all() and (columns.scale[whole:] == -7).all()
+    check_exponents(rows, rows=n)
+    check_exponents(columns, blocks=whole)
 
 
 def test_quantize_a_batch():
