@@ -22,8 +22,8 @@
 // shuffles took 9000 cycles a tile of 4096 cycles of MMAs.
 //
 // A step is 512 SM cycles of MMAs at 256 columns. Two accumulators of 256 columns and
-// the scales do not fit 512 columns: the second begins at column 224, and the
-// epilogue takes the 32 columns that they share first, before the next tile's MMAs.
+// the exponents do not fit 512 columns: the second begins at column 192, and the
+// epilogue takes the 64 columns that they share first, before the next tile's MMAs.
 //
 // The accumulators lose bits with every addition, always towards zero: about 7e-9 of a sum of
 // one sign with each column. bf16 results: up to 16384 columns (2^-13 of such a
@@ -58,9 +58,10 @@ namespace {
 constexpr int kEpiWarp0 = 4, kMmaWarp = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
 constexpr int kProducers = 3, kStages = 8, kLeastStages = 6;
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's rows of a, a step
-constexpr uint32_t kOverlap = 32;             // columns that the accumulators of 256 columns share
-// Tensor memory behind them: two sets of scales, of a in the first four of 16 columns.
+constexpr uint32_t kOverlap = 64;             // columns that the accumulators of 256 columns share
+// Tensor memory behind them: sets of exponents, of a in the first four of 16 columns.
 constexpr uint32_t kScaleCol = 512 - kOverlap, kScaleCols = 16, kAllCols = 512;
+constexpr int kScaleSets = kOverlap / kScaleCols;
 constexpr int kScaleSteps = 4;                // blocks whose exponents make a word
 constexpr uint32_t kScaleBytes = 3 * 512;     // a stage's exponents: of 128 rows of a, 256 of b
 constexpr int kDrainSteps = 8;                // steps of a drained accumulator, and of fp32 sums that are not drained
@@ -189,15 +190,21 @@ __device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, 
                                                pack_bf16(x[8 * j + 4], x[8 * j + 5]), pack_bf16(x[8 * j + 6], x[8 * j + 7]));
         __syncwarp();
         T *out = static_cast<T *>(a.Y) + (un.out + row + up) * a.M + c + 8 * chunk;
-        const int64_t n = a.M - (c + 8 * chunk);
+        uint4 w[4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint4 w = *turned(buf, up + 8 * i, chunk);
-            const int64_t r = row + up + 8 * i;
-            if (r >= un.r0 && r < un.r1) {
+        for (int i = 0; i < 4; i++) w[i] = *turned(buf, up + 8 * i, chunk);
+        const int lo = (int)max((int64_t)-1, min((int64_t)32, un.r0 - row - up)), hi = (int)max((int64_t)-1, min((int64_t)32, un.r1 - row - up));
+        const int64_t n = a.M - (c + 8 * chunk);
+        if (a.align == 16 && n >= 8) {
+#pragma unroll
+            for (int i = 0; i < 4; i++)
+                if (8 * i >= lo && 8 * i < hi) *reinterpret_cast<uint4 *>(out + 8 * i * a.M) = w[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
                 Eight<uint16_t> e;
-                e.w[0] = w.x, e.w[1] = w.y, e.w[2] = w.z, e.w[3] = w.w;
-                store8(reinterpret_cast<uint16_t *>(out + 8 * i * a.M), n, a.align, e);
+                e.w[0] = w[i].x, e.w[1] = w[i].y, e.w[2] = w[i].z, e.w[3] = w[i].w;
+                if (8 * i >= lo && 8 * i < hi) store8(reinterpret_cast<uint16_t *>(out + 8 * i * a.M), n, a.align, e);
             }
         }
         __syncwarp();
@@ -390,9 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             ab ^= 1;
             if (ab == 0) fphase ^= 1;
         };
-        auto load = [&](uint32_t tm, uint32_t (&r)[32]) {
-            tc5::ld32(tm, r);
-            tc5::ld_wait();
+        auto loaded = [&](uint32_t (&r)[32]) {
 #pragma unroll
             for (int j = 0; j < 32; j++) asm volatile("" : "+r"(r[j]));   // no use of a loaded register moves above the wait
         };
@@ -402,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             if constexpr (!DRAIN) {
                 const bool any = un.i1 > un.i0;
                 uint32_t tm = 0;
-                // the columns that the next tile's accumulator has too, first
+                // the columns that the next tile's accumulator has too, first: two groups of one share
                 const bool back = shared_cols && ab == 0, mine = !shared_cols || (ab == 0 ? share == 1 : share == 0);
                 if (any) {
                     tm = wait_acc(un);
@@ -410,19 +415,26 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                     if (!mine) hand_back();
                 }
 #pragma unroll 1
-                for (int p = 0; p < groups; p++) {
-                    const int g = back ? groups - 1 - p : p;
-                    uint32_t r[32];
-                    float x[32];
+                for (int p = 0; p < groups; p += 2) {
+                    const int g = back ? groups - 2 - p : p;
+                    uint32_t r[2][32];
 #pragma unroll
-                    for (int j = 0; j < 32; j++) r[j] = 0;
+                    for (int j = 0; j < 32; j++) r[0][j] = r[1][j] = 0;
                     if (any) {
-                        load(tm + 32 * g, r);
-                        if (mine && p == (shared_cols ? 0 : groups - 1)) hand_back();
+                        tc5::ld32(tm + 32 * g, r[0]);
+                        tc5::ld32(tm + 32 * g + 32, r[1]);
+                        tc5::ld_wait();
+                        loaded(r[0]);
+                        loaded(r[1]);
+                        if (mine && p == 0) hand_back();   // (narrow tiles: all columns)
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; j++) x[j] = __uint_as_float(r[j]);
-                    put<T>(a, un, row, col + 32 * g, x, buf);
+                    for (int k = 0; k < 2; k++) {
+                        float x[32];
+#pragma unroll
+                        for (int j = 0; j < 32; j++) x[j] = __uint_as_float(r[k][j]);
+                        put<T>(a, un, row, col + 32 * (g + k), x, buf);
+                    }
                 }
                 if (any) next_acc();
             } else {
@@ -434,15 +446,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 for (int b = un.i0; b < un.i1; b += kDrainSteps) {
                     const uint32_t tm = wait_acc(un);
                     if (!ok) break;
-                    // both ends first: one of them is shared
-                    constexpr int order[4] = {0, 3, 1, 2};
+                    // handed back after its shared columns, if it has them (the last group's at the end)
+                    const int back = !shared_cols ? groups - 1 : share == ab ? -1 : share == 0 ? 1 : 3;
+                    if (back < 0) hand_back();
 #pragma unroll
-                    for (int p = 0; p < 4; p++) {
-                        const int g = order[p];
-                        if (g >= groups) continue;
+                    for (int g = 0; g < 4; g++) {
+                        if (g >= groups) break;
                         uint32_t r[32];
-                        load(tm + 32 * g, r);
-                        if (shared_cols ? p == 1 : g == groups - 1) hand_back();
+                        tc5::ld32(tm + 32 * g, r);
+                        tc5::ld_wait();
+                        loaded(r);
+                        if (g == back) hand_back();
 #pragma unroll
                         for (int j = 0; j < 32; j++) sum[g][j] += __uint_as_float(r[j]);
                     }
@@ -481,67 +495,67 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 ptx::store_cluster(ptx::map_to_cta(&loads[prod][rank], rank ^ 1), (uint32_t)issued);
             }
         } else if (warp == kMmaWarp && rank == 0) {
-            int n_steps = 0, n_acc = 0, n_sets = 0;
-            int set_end[2] = {-1, -1};   // the last step that has read each set of exponents
-            uint32_t fphase = 0;
-            bool ok = true;
-            s = 0;
-            const uint64_t ad0 = tc5::desc_sw128(smem0), bd0 = tc5::desc_sw128(smem0 + kABytes);
-            const uint64_t sd0 = tc5::desc(smem0 + ns * stage_bytes, 16, 128);   // (eight rows of 16 bytes side by side)
-            for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-                un = unit_at<DRAIN>(a, runs, v);
-                for (i = un.i0; i < un.i1; i++) {
-                    const int b = i - un.i0;
-                    const bool fresh = DRAIN ? b % kDrainSteps == 0 : b == 0, last = i + 1 == un.i1 || (DRAIN && (b + 1) % kDrainSteps == 0);
-                    const bool scales = b == 0 || i % kScaleSteps == 0;
-                    if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
-                        const int wait_for = n_acc - (shared_cols ? 1 : 2);
-                        if (wait_for >= 0)
-                            ok = __all_sync(0xffffffffu, wait_or_abort(&acc_empty[wait_for & 1], (uint32_t)(wait_for >> 1) & 1, a.wait_ns, &stop));
+            if (elected) {   // (one thread throughout: what the others would cost is in the MMAs' way)
+                int n_steps = 0, n_acc = 0, n_sets = 0;
+                uint32_t fphase = 0;
+                // the last steps of the last sets of exponents, the oldest first, with their stages and phases
+                int end_step[kScaleSets], end_stage[kScaleSets];
+                uint32_t end_phase[kScaleSets];
+                bool ok = true;
+                s = 0;
+                const uint64_t ad0 = tc5::desc_sw128(smem0), bd0 = tc5::desc_sw128(smem0 + kABytes);
+                const uint64_t sd0 = tc5::desc(smem0 + ns * stage_bytes, 16, 128);   // (eight rows of 16 bytes side by side)
+                uint32_t set = tmem + kScaleCol - kScaleCols;
+                for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
+                    un = unit_at<DRAIN>(a, runs, v);
+                    for (i = un.i0; i < un.i1; i++) {
+                        const int b = i - un.i0;
+                        const bool fresh = DRAIN ? b % kDrainSteps == 0 : b == 0, last = i + 1 == un.i1 || (DRAIN && (b + 1) % kDrainSteps == 0);
+                        const bool scales = b == 0 || i % kScaleSteps == 0;
+                        if (scales) {
+                            // the set's last readers are done (a copy does not wait for MMAs): so the stage's
+                            // barrier says, or the stage has been filled again since
+                            set = n_sets % kScaleSets == 0 ? tmem + kScaleCol : set + kScaleCols;
+                            if (n_sets >= kScaleSets && n_steps - end_step[0] <= ns)
+                                ok = wait_or_abort(&empty[end_stage[0]], end_phase[0], a.wait_ns, &stop);
+                            n_sets++;
+#pragma unroll
+                            for (int k = 0; k + 1 < kScaleSets; k++)
+                                end_step[k] = end_step[k + 1], end_stage[k] = end_stage[k + 1], end_phase[k] = end_phase[k + 1];
+                        }
+                        if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
+                            const int before = n_acc - (shared_cols ? 1 : 2);
+                            if (before >= 0) ok = ok && wait_or_abort(&acc_empty[before & 1], (uint32_t)(before >> 1) & 1, a.wait_ns, &stop);
+                        }
+                        ok = ok && wait_or_abort(&full[s], fphase, a.wait_ns, &stop);
                         if (!ok) break;
-                    }
-                    if (scales) {
-                        // the set's last readers are done (a copy does not wait for MMAs): at most five
-                        // steps back, fewer than the ring has stages, so that the stage's barrier tells
-                        const int before = set_end[n_sets & 1];
-                        if (before >= 0)
-                            ok = __all_sync(0xffffffffu, wait_or_abort(&empty[before % ns], (uint32_t)(before / ns) & 1, a.wait_ns, &stop));
-                        if (!ok) break;
-                        n_sets++;
-                    }
-                    ok = __all_sync(0xffffffffu, wait_or_abort(&full[s], fphase, a.wait_ns, &stop));
-                    if (!ok) break;
-                    tc5::fence_after();
-                    const uint32_t set = tmem + kScaleCol + (uint32_t)((n_sets - 1) & 1) * kScaleCols;
-                    if (elected) {
-                        const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
+                        tc5::fence_after();
                         if (scales) {
                             const uint64_t sd = sd0 + (uint64_t)((s * kScaleBytes) >> 4);
                             tc5::copy_pair_32x16(set, sd);
                             tc5::copy_pair_32x16(set + 4, sd + (512 >> 4));
                             if (shared_cols) tc5::copy_pair_32x16(set + 8, sd + (1024 >> 4));
                         }
-                        const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)i % kScaleSteps);
+                        const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
+                        const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)i % kScaleSteps), acc = tmem + (uint32_t)(n_acc & 1) * acc_step;
 #pragma unroll
                         for (int j = 0; j < kFp8Block / 32; j++)   // (32 bytes along the rows)
-                            tc5::mma_ss_pair_scaled(tmem + (uint32_t)(n_acc & 1) * acc_step, ad0 + stage + 2 * j, bd0 + stage + 2 * j, idesc, set,
-                                                    set + 4, !fresh | (j > 0));
+                            tc5::mma_ss_pair_scaled(acc, ad0 + stage + 2 * j, bd0 + stage + 2 * j, idesc, set, set + 4, !fresh | (j > 0));
                         tc5::commit_pair(&empty[s]);
-                        if (last) tc5::commit_pair(&acc_full[n_acc & 1]);
+                        if (last) {
+                            tc5::commit_pair(&acc_full[n_acc & 1]);
+                            n_acc++;
+                        }
+                        end_step[kScaleSets - 1] = n_steps, end_stage[kScaleSets - 1] = s, end_phase[kScaleSets - 1] = fphase;
+                        n_steps++;
+                        if (++s == ns) {
+                            s = 0;
+                            fphase ^= 1;
+                        }
                     }
-                    __syncwarp();
-                    set_end[(n_sets - 1) & 1] = n_steps;
-                    n_steps++;
-                    if (last) n_acc++;
-                    if (++s == ns) {
-                        s = 0;
-                        fphase ^= 1;
-                    }
+                    if (!ok) halt();
                 }
-                if (!ok) halt();
-            }
-            // every MMA issued has completed before the tensor memory is freed
-            if (elected) {
+                // every MMA issued has completed before the tensor memory is freed
                 tc5::commit_pair(&done);
                 freed = n_steps, handed = n_acc;
                 ptx::store_cluster(ptx::map_to_cta(&freed, 1), (uint32_t)n_steps);
