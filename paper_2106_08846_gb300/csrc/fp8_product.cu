@@ -11,15 +11,18 @@
 //                  ring; every fourth block the rows' exponents of four blocks with it
 //   warp 2         MMAs of the pair's first CTA, and before them the exponents' copy
 //                  from shared to tensor memory
-//   warps 4 .. 11  epilogue: 32 rows and half of the columns each, through 2 KB of
-//                  shared memory a warp, so that four lanes store 64 bytes of a row
+//   warps 4 .. 11  epilogue: 32 rows and half of the columns each. Where 128 of b's rows
+//                  share their scales, its rows are loaded in the order that leaves a thread 16
+//                  columns side by side, and four lanes store 128 bytes of a row (bf16) straight from
+//                  tensor memory; else through 2 KB of shared memory a warp
 //
 // Scaling outside the MMAs (a fresh accumulator for each step, scaled and added in
 // registers) takes every value of a step out of tensor memory: 16384 tokens of 1024
 // features into 4096 174 us. Exponents made of fp32 scales by three more warps: 102 us, a
 // step waiting for their way from the other CTA's registers; so bsr_fp8_quantize lays
-// them out as tensor memory has them. The epilogue from registers to 64 bytes of a row by
-// shuffles took 9000 cycles a tile of 4096 cycles of MMAs.
+// them out as tensor memory has them. The MMAs' operands take all of shared memory's
+// bandwidth (64 bytes a cycle in, 64 out), so what the epilogue moves through it is in their
+// way: by shuffles 9000 cycles a tile of 4096 cycles of MMAs, through buffers 6900.
 //
 // A step is 512 SM cycles of MMAs at 256 columns. Two accumulators of 256 columns and
 // the exponents do not fit 512 columns: the second begins at column 192, and the
@@ -104,13 +107,20 @@ struct Runs {
     uint32_t first[kMostExperts + 1];
 };
 
-__device__ __forceinline__ Unit unit_of(const Args &a, const Runs &r, unsigned v) {
+// What the units follow from, in registers.
+struct Sizes {
+    int64_t rows;
+    int KB, group, E, splits, width;   // width: columns of a tile
+    unsigned tiles_m, tiles_n;
+};
+
+__device__ __forceinline__ Unit unit_of(const Sizes &a, const Runs &r, unsigned v) {
     Unit u;
     u.out = 0;
     u.batch = 0;
     u.part = -1;
     u.i0 = 0;
-    u.i1 = (int)a.KB;
+    u.i1 = a.KB;
     if (a.group == BSR_GROUP_ROWS) {
         const unsigned t = v / a.tiles_n;
         int lo = 0, hi = a.E;   // the last run whose tiles begin at or before t
@@ -123,7 +133,7 @@ __device__ __forceinline__ Unit unit_of(const Args &a, const Runs &r, unsigned v
         u.r0 = r.at[lo];
         u.r1 = r.at[lo + 1];
         u.m0 = u.r0 / 128 * 128 + (int64_t)(t - r.first[lo]) * 256;
-        u.n0 = (int64_t)(v - t * a.tiles_n) * 2 * a.half;
+        u.n0 = (int64_t)(v - t * a.tiles_n) * a.width;
         return u;
     }
     unsigned tile = v;
@@ -136,24 +146,23 @@ __device__ __forceinline__ Unit unit_of(const Args &a, const Runs &r, unsigned v
     } else if (a.splits > 1) {
         u.part = (int)v;
         tile = v / (unsigned)a.splits;
-        const unsigned k = v - tile * (unsigned)a.splits;
-        const int64_t words = (a.KB + kScaleSteps - 1) / kScaleSteps;
-        u.i0 = (int)(words * k / a.splits) * kScaleSteps;
-        u.i1 = (int)min(a.KB, words * (k + 1) / a.splits * kScaleSteps);
+        const unsigned k = v - tile * (unsigned)a.splits, words = (unsigned)(a.KB + kScaleSteps - 1) / kScaleSteps;
+        u.i0 = (int)(words * k / (unsigned)a.splits) * kScaleSteps;
+        u.i1 = min(a.KB, (int)(words * (k + 1) / (unsigned)a.splits) * kScaleSteps);
     }
     const unsigned tm = tile / a.tiles_n;
     u.m0 = (int64_t)tm * 256;
     u.r0 = 0;
     u.r1 = a.rows;
-    u.n0 = (int64_t)(tile - tm * a.tiles_n) * 2 * a.half;
+    u.n0 = (int64_t)(tile - tm * a.tiles_n) * a.width;
     return u;
 }
 
 // One copy of the code for all roles, as cold instructions are what a short call waits
 // for; but for drained sums, whose registers a call would push out.
-__device__ __noinline__ Unit unit_call(const Args &a, const Runs &r, unsigned v) { return unit_of(a, r, v); }
+__device__ __noinline__ Unit unit_call(Sizes a, const Runs &r, unsigned v) { return unit_of(a, r, v); }
 template <bool DRAIN>
-__device__ __forceinline__ Unit unit_at(const Args &a, const Runs &r, unsigned v) {
+__device__ __forceinline__ Unit unit_at(const Sizes &a, const Runs &r, unsigned v) {
     return DRAIN ? unit_of(a, r, v) : unit_call(a, r, v);
 }
 
@@ -171,6 +180,44 @@ __device__ __forceinline__ unsigned unit_in(unsigned round, unsigned pair, unsig
 // Where 16 bytes of the 64 of a row lie, so that eight lanes' rows, and the four runs of two rows, fall on different banks.
 __device__ __forceinline__ uint4 *turned(unsigned char *buf, int row, int chunk) {
     return reinterpret_cast<uint4 *>(buf + row * 64 + 16 * (chunk ^ ((row >> 1) & 3)));
+}
+
+// 16 rows of the result from `row` on x 64 columns from c on, of b's rows in order: x as
+// tc5::ld_16x64 leaves it is 16 columns from c + 16 (lane % 4) on of this thread, of rows
+// lane / 4 and + 8.
+template <typename T>
+__device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64_t row, int64_t c, float (&x)[32]) {
+    const int lane = threadIdx.x & 31;
+    c += 16 * (lane & 3);
+    if (c >= a.M) return;   // (64 columns are there or not)
+    row += lane >> 2;
+    if (a.bias) {
+        const float *bias = a.bias + (int64_t)un.batch * a.M + c;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float b0 = __ldg(bias + 2 * i), b1 = __ldg(bias + 2 * i + 1);
+            x[4 * i] += b0, x[4 * i + 1] += b1, x[4 * i + 2] += b0, x[4 * i + 3] += b1;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        if (row + 8 * h < un.r0 || row + 8 * h >= un.r1) continue;
+        T *out = static_cast<T *>(a.Y) + (un.out + row + 8 * h) * a.M + c;
+        uint32_t w[8];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; i++) w[i] = pack_bf16(x[4 * i + 2 * h], x[4 * i + 2 * h + 1]);
+            ptx::st_global_32(out, w);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 2; k++) {
+#pragma unroll
+                for (int i = 0; i < 4; i++)
+                    w[2 * i] = __float_as_uint(x[16 * k + 4 * i + 2 * h]), w[2 * i + 1] = __float_as_uint(x[16 * k + 4 * i + 2 * h + 1]);
+                ptx::st_global_32(out + 8 * k, w);
+            }
+        }
+    }
 }
 
 // 32 rows of the result from `row` on x 32 columns from c on; x: those of row + lane.
@@ -242,7 +289,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, 
     }
 }
 
-template <typename T, bool DRAIN>
+template <typename T, bool DRAIN, bool ORDERED>
 __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_constant__ Args a) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char *base = ptx::align_smem(smem_raw);
@@ -258,21 +305,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t rank = ptx::cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < ns; s++) {
-            ptx::mbar_init(&full[s], 1);   // a producer's arrival, and its bytes
-            ptx::mbar_init(&empty[s], 1);
-        }
-        for (int i = 0; i < 2; i++) {
-            ptx::mbar_init(&acc_full[i], 1);
-            ptx::mbar_init(&acc_empty[i], 2 * kEpiWarps);
-        }
-        ptx::mbar_init(&done, 1);
-        stop = freed = handed = 0;
+    if (threadIdx.x == 0) stop = freed = handed = 0;
+    if (threadIdx.x < 32) {   // a barrier a lane: a producer's arrival with its bytes, commits, the epilogue warps of both CTAs
+        if (lane < kStages) ptx::mbar_init(&full[lane], 1);
+        else if (lane < 2 * kStages) ptx::mbar_init(&empty[lane - kStages], 1);
+        else if (lane < 2 * kStages + 2) ptx::mbar_init(&acc_full[lane & 1], 1);
+        else if (lane < 2 * kStages + 4) ptx::mbar_init(&acc_empty[lane & 1], 2 * kEpiWarps);
+        else if (lane == 31) ptx::mbar_init(&done, 1);
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, kAllCols);
-    if (warp == 0 && ptx::elect_one()) {
+    if (warp == 1 && ptx::elect_one()) {
         ptx::prefetch_tensormap(&a.a);
         ptx::prefetch_tensormap(&a.b);
         ptx::prefetch_tensormap(&a.ea);
@@ -312,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         __syncthreads();
         units = by_rows ? runs.first[a.E] * a.tiles_n : units * (unsigned)a.E;
     }
+    const Sizes sizes = {a.rows, (int)a.KB, a.group, a.E, a.splits, 2 * a.half, a.tiles_m, a.tiles_n};
     const uint32_t tmem = tmem_s;
     const bool elected = ptx::elect_one();
     // stops every role of this pair; a timeout is recorded
@@ -343,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             const int over = i - un.i1;
             v = unit_in(++round, pair, pairs);
             if (v >= units) return false;
-            un = unit_at<DRAIN>(a, runs, v);
+            un = unit_at<DRAIN>(sizes, runs, v);
             i = un.i0 + over;
         }
         return true;
@@ -357,7 +401,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (stage_bytes + (scales ? (a.half == 128 ? 3 : 2) * 512 : 0)));
             const int m = (int)(un.m0 + rank * 128), n = (int)un.n0;
             ptx::tma_load_2d_pair_at(dst, &a.a, i * kFp8Block, m, bar);
-            ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, n + (int)rank * a.half, un.batch, bar);
+            const int nb = n + (int)rank * a.half;
+            if constexpr (ORDERED) ptx::tma_load_5d_pair_at(dst + kABytes, &a.b, i * kFp8Block, 0, 0, 0, (int)((un.batch * a.M + nb) / 64), bar);
+            else ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, nb, un.batch, bar);
             if (scales) {
                 const uint32_t to = smem0 + ns * stage_bytes + s * kScaleBytes;
                 ptx::tma_load_3d_pair_at(to, &a.ea, 0, m / 128, i / kScaleSteps, bar);
@@ -402,7 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
             for (int j = 0; j < 32; j++) asm volatile("" : "+r"(r[j]));   // no use of a loaded register moves above the wait
         };
         for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-            un = unit_at<DRAIN>(a, runs, v);
+            un = unit_at<DRAIN>(sizes, runs, v);
             const int64_t row = un.m0 + rank * 128 + 32 * q, col = un.n0 + 32 * first;
             if constexpr (!DRAIN) {
                 const bool any = un.i1 > un.i0;
@@ -421,8 +467,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
 #pragma unroll
                     for (int j = 0; j < 32; j++) r[0][j] = r[1][j] = 0;
                     if (any) {
-                        tc5::ld32(tm + 32 * g, r[0]);
-                        tc5::ld32(tm + 32 * g + 32, r[1]);
+                        if constexpr (ORDERED) {
+                            tc5::ld_16x64(tm + 32 * g, r[0]);
+                            tc5::ld_16x64(tm + (16u << 16) + 32 * g, r[1]);
+                        } else {
+                            tc5::ld32(tm + 32 * g, r[0]);
+                            tc5::ld32(tm + 32 * g + 32, r[1]);
+                        }
                         tc5::ld_wait();
                         loaded(r[0]);
                         loaded(r[1]);
@@ -433,12 +484,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                         float x[32];
 #pragma unroll
                         for (int j = 0; j < 32; j++) x[j] = __uint_as_float(r[k][j]);
-                        put<T>(a, un, row, col + 32 * (g + k), x, buf);
+                        if constexpr (ORDERED) put_ordered<T>(a, un, row + 16 * k, col + 32 * g, x);
+                        else put<T>(a, un, row, col + 32 * (g + k), x, buf);
                     }
                 }
                 if (any) next_acc();
             } else {
-                float sum[4][32];   // [group]
+                float sum[4][32];   // [32 columns, or ORDERED 16 rows of 64]
 #pragma unroll
                 for (int g = 0; g < 4; g++)
 #pragma unroll
@@ -453,7 +505,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                     for (int g = 0; g < 4; g++) {
                         if (g >= groups) break;
                         uint32_t r[32];
-                        tc5::ld32(tm + 32 * g, r);
+                        if constexpr (ORDERED) tc5::ld_16x64(tm + ((uint32_t)(16 * (g & 1)) << 16) + 64 * (g / 2), r);
+                        else tc5::ld32(tm + 32 * g, r);
                         tc5::ld_wait();
                         loaded(r);
                         if (g == back) hand_back();
@@ -466,7 +519,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 // one copy of the code, the sums handed on from group to group
 #pragma unroll 1
                 for (int g = 0; g < groups; g++) {
-                    put<T>(a, un, row, col + 32 * g, sum[0], buf);
+                    if constexpr (ORDERED) put_ordered<T>(a, un, row + 16 * (g & 1), col + 64 * (g / 2), sum[0]);
+                    else put<T>(a, un, row, col + 32 * g, sum[0], buf);
 #pragma unroll
                     for (int k = 0; k < 3; k++)
 #pragma unroll
@@ -478,7 +532,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         if constexpr (DRAIN) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegs));
         if (producer) {
             if (v < units) {
-                un = unit_at<DRAIN>(a, runs, v);
+                un = unit_at<DRAIN>(sizes, runs, v);
                 i = un.i0 + prod;
                 more = seek();
             }
@@ -507,7 +561,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 const uint64_t sd0 = tc5::desc(smem0 + ns * stage_bytes, 16, 128);   // (eight rows of 16 bytes side by side)
                 uint32_t set = tmem + kScaleCol - kScaleCols;
                 for (; ok && v < units; v = unit_in(++round, pair, pairs)) {
-                    un = unit_at<DRAIN>(a, runs, v);
+                    un = unit_at<DRAIN>(sizes, runs, v);
                     for (i = un.i0; i < un.i1; i++) {
                         const int b = i - un.i0;
                         const bool fresh = DRAIN ? b % kDrainSteps == 0 : b == 0, last = i + 1 == un.i1 || (DRAIN && (b + 1) % kDrainSteps == 0);
@@ -690,6 +744,22 @@ cudaError_t encode(const bsr_fp8_matrix_t &m, bool batch, int rows, CUtensorMap 
                : cudaErrorInvalidValue;
 }
 
+// b's rows in groups of 64, a group's in the order that gives a thread 16 columns side by
+// side (row 8 i + 2 q + e of a box: 16 q + 2 i + e of the group; i < 8, q < 4, e < 2).
+cudaError_t encode_ordered(const bsr_fp8_matrix_t &m, int rows, CUtensorMap *map) {
+    auto enc = tensor_map_encoder();
+    if (!enc) return cudaErrorNotSupported;
+    const cuuint64_t ld = (cuuint64_t)fp8_blocks(m.cols) * kFp8Block;
+    const cuuint64_t dims[5] = {ld, 2, 4, 8, (cuuint64_t)(m.batch * m.rows / 64)};
+    const cuuint64_t strides[4] = {ld, 16 * ld, 2 * ld, 64 * ld};
+    const cuuint32_t box[5] = {kFp8Block, 2, 4, 8, (cuuint32_t)(rows / 64)};
+    const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, m.q, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? cudaSuccess
+               : cudaErrorInvalidValue;
+}
+
 cudaError_t encode_exponents(const bsr_fp8_matrix_t &m, bool batch, int rows, CUtensorMap *map) {
     auto enc = tensor_map_encoder();
     if (!enc) return cudaErrorNotSupported;
@@ -704,12 +774,18 @@ cudaError_t encode_exponents(const bsr_fp8_matrix_t &m, bool batch, int rows, CU
                : cudaErrorInvalidValue;
 }
 
-template <typename T, bool DRAIN>
+// Whether results go to memory straight from tensor memory: the order of b's rows must not
+// matter to their exponents, tiles' 64 columns be all there, and rows of Y start on 32 bytes.
+bool ordered(const Fp8Product &p, const Plan &q) {
+    return p.b.tile == kFp8Block && p.b.rows % 64 == 0 && q.splits == 1 && reinterpret_cast<uintptr_t>(p.Y) % 32 == 0;
+}
+
+template <typename T, bool DRAIN, bool ORDERED>
 cudaError_t launch(const Args &a, unsigned grid, cudaStream_t s) {
     static std::atomic<uint64_t> attr_set{0};
-    cudaError_t e = allow_smem(k_fp8_product<T, DRAIN>, kMaxSmem, attr_set);
+    cudaError_t e = allow_smem(k_fp8_product<T, DRAIN, ORDERED>, kMaxSmem, attr_set);
     if (e != cudaSuccess) return e;
-    return launch_clusters(k_fp8_product<T, DRAIN>, 2, dim3(grid), dim3(kThreads), a.ns * (a.stage_bytes + kScaleBytes) + kEpiWarps * kTurnBytes + 1024, s, a);
+    return launch_clusters(k_fp8_product<T, DRAIN, ORDERED>, 2, dim3(grid), dim3(kThreads), a.ns * (a.stage_bytes + kScaleBytes) + kEpiWarps * kTurnBytes + 1024, s, a);
 }
 
 }  // namespace
@@ -743,10 +819,11 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     const char *limit = std::getenv("BSR_WAIT_LIMIT_NS"), *stall = std::getenv("BSR_TEST_STALL_CHUNK");
     a.wait_ns = limit ? std::strtoull(limit, nullptr, 10) : 1000000000ull;
     a.stall_step = stall ? std::atoi(stall) : -1;
+    const bool order = ordered(p, q);
     cudaError_t e = cudaSuccess;
     if (a.KB > 0) {   // (sums of nothing load nothing)
         e = encode(p.a, false, 128, &a.a);
-        if (e == cudaSuccess) e = encode(p.b, true, q.half, &a.b);
+        if (e == cudaSuccess) e = order ? encode_ordered(p.b, q.half, &a.b) : encode(p.b, true, q.half, &a.b);
         if (e == cudaSuccess) e = encode_exponents(p.a, false, 128, &a.ea);
         if (e == cudaSuccess) e = encode_exponents(p.b, true, q.half == 128 ? 256 : 128, &a.eb);
     }
@@ -754,8 +831,12 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     const unsigned grid = 2 * (unsigned)std::min<int64_t>(q.units, pairs_of_sms());
     const int64_t steps = q.splits == 1 ? a.KB : (fp8_words(p.a.cols) + q.splits - 1) / q.splits * kScaleSteps;
     const bool f32 = p.dt == BSR_F32, drained = steps > (f32 ? kDrainSteps : kMostSteps);
-    e = f32 ? (drained ? launch<float, true>(a, grid, s) : launch<float, false>(a, grid, s))
-            : (drained ? launch<uint16_t, true>(a, grid, s) : launch<uint16_t, false>(a, grid, s));
+    auto run = [&](auto t) {
+        using T = decltype(t);
+        if (order) return drained ? launch<T, true, true>(a, grid, s) : launch<T, false, true>(a, grid, s);
+        return drained ? launch<T, true, false>(a, grid, s) : launch<T, false, false>(a, grid, s);
+    };
+    e = f32 ? run(float()) : run(uint16_t());
     if (e != cudaSuccess || q.splits == 1) return e;
     const dim3 joins((unsigned)(q.tiles_m * q.tiles_n * (q.half / 2)));
     return launch_kernel(f32 ? k_fp8_join<float> : k_fp8_join<uint16_t>, joins, dim3(256), 0, s, a);
