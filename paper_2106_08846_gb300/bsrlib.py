@@ -821,21 +821,42 @@ class Fp8Matrix:
     them; `exponent` is what the product reads of the scales, powers of two (include/bsr.h). fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
 
     def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda"):
-        if fmt not in _FP8 or tile not in (1, 128):
+        code = _FP8.get(fmt)
+        if code is None or (tile != 1 and tile != 128):
             raise ValueError("fmt is 'e4m3' or 'e5m2', tile 1 or 128")
         self.rows, self.cols, self.tile, self.fmt, self.batch = rows, cols, tile, fmt, batch
-        each, blocks = () if batch is None else (batch,), -(-cols // 128)
-        self._q = torch.empty((*each, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
-        self._scale = torch.empty((*each, blocks, -(-rows // tile)), dtype=torch.float32, device=device)
-        self._exponent = torch.empty((*each, -(-blocks // 4), -(-rows // 128), 512), dtype=torch.uint8, device=device)
-        full = self._q.numel() > 0
-        self._c = _Fp8Matrix(1 if batch is None else batch, rows, cols, tile, _FP8[fmt], _ptr(self._q) if full else None,
-                             _ptr(self._exponent) if full else None, _ptr(self._scale) if full else None)
+        n, blocks = 1 if batch is None else batch, (cols + 127) // 128
+        # one allocation: the values, the exponents and the scales; views of it are made when they are asked for
+        values = n * rows * blocks * 128
+        exponents = n * ((blocks + 3) // 4) * ((rows + 127) // 128) * 512
+        self._first = (values, (values + exponents) // 4)   # of the exponents, in bytes, and of the scales, in fours
+        self._base = torch.empty(values + exponents + 4 * n * blocks * ((rows + tile - 1) // tile), dtype=_FP8_TYPE[fmt], device=device)
+        self._q = self._scale = None
+        p = self._base.data_ptr() if values else 0
+        self._c = _Fp8Matrix(n, rows, cols, tile, code, p, p and p + values, p and p + values + exponents)
+
+    def _strided(self, flat: torch.Tensor, first: int, r: int, c: int) -> torch.Tensor:
+        if self.batch is None:
+            return flat.as_strided((r, c), (c, 1), first)
+        return flat.as_strided((self.batch, r, c), (r * c, c, 1), first)
 
     # (to be filled, not replaced: the calls have their addresses)
-    q = property(lambda self: self._q)
-    exponent = property(lambda self: self._exponent)
-    scale = property(lambda self: self._scale)
+    @property
+    def q(self) -> torch.Tensor:
+        if self._q is None:
+            self._q = self._strided(self._base, 0, self.rows, (self.cols + 127) // 128 * 128)
+        return self._q
+
+    @property
+    def scale(self) -> torch.Tensor:
+        if self._scale is None:
+            self._scale = self._strided(self._base.view(torch.float32), self._first[1], (self.cols + 127) // 128,
+                                        (self.rows + self.tile - 1) // self.tile)
+        return self._scale
+
+    @property
+    def exponent(self) -> torch.Tensor:
+        return self._strided(self._base.view(torch.uint8), self._first[0], (self.cols + 511) // 512, (self.rows + 127) // 128 * 512)
 
 
 def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: str = "rows", used: Optional[torch.Tensor] = None,
@@ -846,26 +867,38 @@ def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: st
     rows); "both": the two, from one reading. tile 128: blocks of 128 x 128, as for
     weights. used (device int32 [1], as ExpertOrder.used): rows from there on are not
     read. `out`: what to fill, as it would be returned."""
-    if form not in ("rows", "columns", "both"):
-        raise ValueError("form is 'rows', 'columns' or 'both'")
-    if x.dim() not in (2, 3) or not x.is_contiguous():
-        raise ValueError("x must be contiguous, [R, C] or [batch, R, C]")
+    shape = x.shape
+    if len(shape) == 2:
+        (R, C), batch = shape, None
+    elif len(shape) == 3:
+        batch, R, C = shape
+    else:
+        raise ValueError("x must be [R, C] or [batch, R, C]")
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
     dt = dtype_code(x.dtype)
-    batch = x.shape[0] if x.dim() == 3 else None
-    R, C = x.shape[-2:]
-    _check_rows("used", used, (1,), torch.int32)
-    sizes = [(R, C)] if form == "rows" else [(C, R)] if form == "columns" else [(R, C), (C, R)]
+    if used is not None:
+        _check_rows("used", used, (1,), torch.int32)
+    if form == "both":
+        sizes = ((R, C), (C, R))
+    elif form == "rows":
+        sizes = ((R, C),)
+    elif form == "columns":
+        sizes = ((C, R),)
+    else:
+        raise ValueError("form is 'rows', 'columns' or 'both'")
     if out is None:
         m = [Fp8Matrix(r, c, tile, fmt, batch, x.device) for r, c in sizes]
-        for f in m:
-            _lend(stream, x.device, f._q, f._scale, f._exponent)
+        if stream is not None:
+            _lend(stream, x.device, *[f._base for f in m])
     else:
         m = list(out) if form == "both" else [out]
         if [(f.rows, f.cols, f.tile, f.fmt, f.batch) for f in m] != [(r, c, tile, fmt, batch) for r, c in sizes]:
             raise ValueError("out is of other sizes")
-    rows, columns = (m[0], None) if form == "rows" else (None, m[0]) if form == "columns" else m
-    status = (_lib or load()).bsr_fp8_quantize(x.data_ptr() if x.numel() else None, dt, rows and rows._c, columns and columns._c,
-                                               _ptr(used), _stream(stream))
+    first = m[0]._c
+    rows, columns = (first, None) if form == "rows" else (None, first) if form == "columns" else (first, m[1]._c)
+    status = (_lib or load()).bsr_fp8_quantize(x.data_ptr(), dt, rows, columns, None if used is None else used.data_ptr(),
+                                               _stream(stream))
     if status:
         _check(status, "bsr_fp8_quantize")
     return m[0] if len(m) == 1 else tuple(m)
@@ -891,12 +924,13 @@ def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = N
         group = BSR_GROUP_ROWS if over == "rows" else BSR_GROUP_COLUMNS
     if a.batch is not None or b.batch != (E if group == BSR_GROUP_ROWS else None):
         raise ValueError("a is one matrix, b one for each expert by rows, else one")
-    _check_rows("bias", bias, (b.rows,) if b.batch is None else (E, b.rows), torch.float32)
+    if bias is not None:
+        _check_rows("bias", bias, (b.rows,) if b.batch is None else (E, b.rows), torch.float32)
     shape = (E, a.rows, b.rows) if group == BSR_GROUP_COLUMNS else (a.rows, b.rows)
     if Y is None:
-        Y = torch.empty(shape, dtype=dtype, device=a.q.device)
+        Y = torch.empty(shape, dtype=dtype, device=a._base.device)
         _lend(stream, Y.device, Y)
-    else:
+    elif not _is_rows(Y, shape, dtype):
         _check_rows("Y", Y, shape, dtype)
     lib, n = _lib or load(), ctypes.c_size_t(0)
     status = lib.bsr_fp8_product_workspace(a._c, b._c, dt, group, E, ctypes.byref(n))

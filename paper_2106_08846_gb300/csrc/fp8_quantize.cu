@@ -8,12 +8,15 @@
 // exponent a finer scale would keep no more bits of the others. s = 1 for a block of zeros, at
 // least 2^-126. Values that are not finite become NaN and have no part in s.
 //
-// One pass: a CTA holds 128 x 128 values in registers, takes the largest of each
-// row's 128 (16 lanes) and of each column's (the lanes' eight rows, then the eight
+// One pass: a CTA holds 128 x 128 values in registers (bf16 in pairs, as they lie), takes
+// the largest of each row's 128 (16 lanes) and of each column's (the lanes' eight rows, then the eight
 // warps'), and writes them as they lie and transposed, through shared memory, so
-// that both operands of a later product have the sum's axis contiguous.
+// that both operands of a later product have the sum's axis contiguous. Blocks with
+// an infinity, which would be the largest, go through a second copy of the code.
 //
 // What bounds it: DRAM.
+#include <cuda_bf16.h>
+
 #include <algorithm>
 
 #include "elem.cuh"
@@ -51,81 +54,109 @@ __device__ __forceinline__ int64_t exponent_at(int64_t r, int64_t b, int64_t run
     return ((b >> 2) * runs + (r >> 7)) * 512 + (r & 31) * 16 + (r >> 5 & 3) * 4 + (b & 3);
 }
 
-// |x| as bits, 0 where it is not finite
-__device__ __forceinline__ uint32_t size_bits(float x) {
-    const uint32_t b = __float_as_uint(x) & 0x7fffffffu;
-    return b < 0x7f800000u ? b : 0;
-}
-
-// Two values times a power of two, in 8 bits each (the first one's low).
+// Two values in 8 bits each (the first one's low).
 template <bool E5M2>
-__device__ __forceinline__ uint32_t round2(float x0, float x1, float inv) {
-    float y0 = x0 * inv, y1 = x1 * inv;
-    y0 = fmaf(y0, 0.f, y0), y1 = fmaf(y1, 0.f, y1);   // infinities become NaN
+__device__ __forceinline__ uint32_t round2(float y0, float y1) {
     uint16_t r;
     if constexpr (E5M2) asm("cvt.rn.satfinite.e5m2x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y1), "f"(y0));
     else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y1), "f"(y0));
     return r;
 }
+// Infinities become NaN; all else stays.
+__device__ __forceinline__ float no_inf(float y) { return fmaf(y, 0.f, y); }
 
-// Eight values of a row from p on, n of which are there (the others 0).
+// Eight values of a row: bf16 in pairs, fp32 one by one. Sizes: of pairs or values,
+// a maximum with a NaN is the other operand.
 template <typename T>
-__device__ __forceinline__ void load_eight(const T *p, int64_t n, int align, float (&x)[8]) {
-    if (n >= 8 && align == 16) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int j = 0; j < 4; j++) x[2 * j] = __uint_as_float(w[j] << 16), x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        } else {
-            const float4 u = __ldg(reinterpret_cast<const float4 *>(p)), v = __ldg(reinterpret_cast<const float4 *>(p) + 1);
-            x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = v.x, x[5] = v.y, x[6] = v.z, x[7] = v.w;
-        }
-    } else if (sizeof(T) == 2 && n >= 8 && align >= 4) {
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint32_t w = __ldg(reinterpret_cast<const uint32_t *>(p) + j);
-            x[2 * j] = __uint_as_float(w << 16), x[2 * j + 1] = __uint_as_float(w & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; j++) x[j] = j < n ? to_f32(__ldg(p + j)) : 0.f;
-    }
-}
+struct Row;
 
-// 256 threads: warp w, half h of it, lane l of the half: rows 16 w + 8 h + i, columns 8 l + j.
-template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS>
-__global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QArgs a) {
-    __shared__ uint32_t tops[8][kFp8Block];
-    __shared__ __align__(16) unsigned char turned[COLUMNS ? kFp8Block * kFp8Block : 16];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, l = lane & 15;
-    const int64_t kb = blockIdx.x % a.KB, rb = blockIdx.x / a.KB, batch = blockIdx.y;
-    const int64_t row0 = rb * kFp8Block + 16 * warp + 8 * h, col0 = kb * kFp8Block + 8 * l;
-    ptx::pdl_launch_dependents();
-    ptx::pdl_wait();
-    const int64_t R = a.used ? min(a.R, (int64_t)max(0, __ldg(a.used))) : a.R;
-    if (rb * kFp8Block >= R) return;
-    float x[8][8];
-    const T *from = static_cast<const T *>(a.x) + (batch * a.R + row0) * a.C + col0;
+template <>
+struct Row<uint16_t> {
+    static constexpr int words = 4, each = 2;
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const uint16_t *p, int n, int align) {
+        if (n >= 8 && align == 16) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p));
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w;
+        } else if (n >= 8 && align >= 4) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) load_eight(from + i * a.C, row0 + i < R ? a.C - col0 : 0, a.align, x[i]);
-    uint32_t row_top[8], col_top[8] = {};
+            for (int j = 0; j < 4; j++) w[j] = __ldg(reinterpret_cast<const uint32_t *>(p) + j);
+        } else {
 #pragma unroll
-    for (int i = 0; i < 8; i++) {
-        row_top[i] = 0;
-#pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const uint32_t b = size_bits(x[i][j]);
-            row_top[i] = max(row_top[i], b);
-            if (COLUMNS && !TILE) col_top[j] = max(col_top[j], b);
+            for (int j = 0; j < 4; j++)
+                w[j] = (2 * j < n ? (uint32_t)__ldg(p + 2 * j) : 0) | (2 * j + 1 < n ? (uint32_t)__ldg(p + 2 * j + 1) : 0) << 16;
         }
     }
+    static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t v) { return *reinterpret_cast<const __nv_bfloat162 *>(&v); }
+    static __device__ __forceinline__ uint32_t word(__nv_bfloat162 v) { return *reinterpret_cast<const uint32_t *>(&v); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return word(__hmax2(pair(a), pair(b))); }
+    // the size of word j; ODD: 0 for infinities
+    template <bool ODD>
+    __device__ __forceinline__ uint32_t size(int j) const {
+        uint32_t a = w[j] & 0x7fff7fffu;
+        if (ODD) a &= ((a & 0xffffu) == 0x7f80u ? 0xffff0000u : ~0u) & (a >> 16 == 0x7f80u ? 0xffffu : ~0u);
+        return a;
+    }
+    // the bits, as fp32, of the larger value of a pair of sizes; a NaN is no size
+    static __device__ __forceinline__ uint32_t top(uint32_t a) {
+        const uint32_t t = larger(a, a >> 16 | a << 16) & 0xffffu;
+        return t > 0x7f80u ? 0 : t << 16;
+    }
+    static __device__ __forceinline__ uint32_t low(uint32_t a) { return (a & 0xffffu) > 0x7f80u ? 0 : a << 16; }
+    static __device__ __forceinline__ uint32_t high(uint32_t a) { return a >> 16 > 0x7f80u ? 0 : a & 0xffff0000u; }
+    // 2^-e, and word j times it (exact, but for values that 8 bits do not have)
+    static __device__ __forceinline__ uint32_t factor(int e0, int e1) { return (uint32_t)(127 - e0) << 7 | (uint32_t)(127 - e1) << 23; }
+    __device__ __forceinline__ float2 scaled(int j, uint32_t f) const {
+        const uint32_t y = word(__hmul2(pair(w[j]), pair(f)));
+        return make_float2(__uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
+    }
+};
+
+template <>
+struct Row<float> {
+    static constexpr int words = 8, each = 1;
+    float w[8];
+    __device__ __forceinline__ void load(const float *p, int n, int align) {
+        if (n >= 8 && align == 16) {
+            const float4 u = __ldg(reinterpret_cast<const float4 *>(p)), v = __ldg(reinterpret_cast<const float4 *>(p) + 1);
+            w[0] = u.x, w[1] = u.y, w[2] = u.z, w[3] = u.w, w[4] = v.x, w[5] = v.y, w[6] = v.z, w[7] = v.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; j++) w[j] = j < n ? __ldg(p + j) : 0.f;
+        }
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    template <bool ODD>
+    __device__ __forceinline__ uint32_t size(int j) const {
+        const uint32_t a = __float_as_uint(w[j]) & 0x7fffffffu;
+        return ODD && a == 0x7f800000u ? 0 : a;
+    }
+    static __device__ __forceinline__ uint32_t top(uint32_t a) { return a > 0x7f800000u ? 0 : a; }
+    static __device__ __forceinline__ uint32_t low(uint32_t a) { return top(a); }
+    static __device__ __forceinline__ float factor(int e0, int) { return power_of_two(-e0); }
+    __device__ __forceinline__ float scaled(int j, float f) const { return w[j] * f; }
+};
+
+struct Place {
+    int64_t kb, rb, batch, row0, R;   // row0: this thread's first row; R: rows in use
+};
+
+// What is left when the values are in registers: 256 threads, warp w, half h of it, lane l
+// of the half: rows 16 w + 8 h + i, columns 8 l + j.
+template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS, bool ODD>
+__device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const Row<T> (&x)[8], uint32_t (&tops)[8][kFp8Block], unsigned char *turned) {
+    using X = Row<T>;
+    constexpr int words = X::words, each = X::each;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, l = lane & 15;
+    auto half = [](float y) { return ODD ? no_inf(y) : y; };
     int tile_e = 0;
     if constexpr (TILE) {
-        uint32_t t = row_top[0];
+        uint32_t t = 0;
 #pragma unroll
-        for (int i = 1; i < 8; i++) t = max(t, row_top[i]);
-        t = __reduce_max_sync(0xffffffffu, t);
+        for (int i = 0; i < 8; i++)
+#pragma unroll
+            for (int j = 0; j < words; j++) t = X::larger(t, x[i].template size<ODD>(j));
+        t = __reduce_max_sync(0xffffffffu, X::top(t));
         if (lane == 0) tops[warp][0] = t;
         __syncthreads();
         t = tops[0][0];
@@ -133,55 +164,76 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QA
         for (int w = 1; w < 8; w++) t = max(t, tops[w][0]);
         tile_e = scale_exponent<E5M2>(t);
         if (threadIdx.x == 0) {
-            if (ROWS && a.s) a.s[(batch * a.KB + kb) * a.RB + rb] = power_of_two(tile_e);
-            if (COLUMNS && a.st) a.st[(batch * a.RB + rb) * a.KB + kb] = power_of_two(tile_e);
+            if (ROWS && a.s) a.s[(at.batch * a.KB + at.kb) * a.RB + at.rb] = power_of_two(tile_e);
+            if (COLUMNS && a.st) a.st[(at.batch * a.RB + at.rb) * a.KB + at.kb] = power_of_two(tile_e);
         }
         const int r = threadIdx.x;   // of the block
         if (r < kFp8Block) {
-            if (ROWS) a.e[batch * a.e_bytes + exponent_at(rb * kFp8Block + r, kb, a.RB)] = (uint8_t)(tile_e + 127);
-            if (COLUMNS) a.et[batch * a.et_bytes + exponent_at(kb * kFp8Block + r, rb, a.KB)] = (uint8_t)(tile_e + 127);
+            if (ROWS) a.e[at.batch * a.e_bytes + exponent_at(at.rb * kFp8Block + r, at.kb, a.RB)] = (uint8_t)(tile_e + 127);
+            if (COLUMNS) a.et[at.batch * a.et_bytes + exponent_at(at.kb * kFp8Block + r, at.rb, a.KB)] = (uint8_t)(tile_e + 127);
         }
     }
     if constexpr (ROWS) {
         int mine = 0;   // of row l, for lanes l < 8
+        uint8_t *q = a.q + ((at.batch * a.R + at.row0) * a.KB + at.kb) * kFp8Block + 8 * l;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
             int e = tile_e;
             if constexpr (!TILE) {
+                uint32_t t = x[i].template size<ODD>(0);
 #pragma unroll
-                for (int m = 8; m; m /= 2) row_top[i] = max(row_top[i], __shfl_xor_sync(0xffffffffu, row_top[i], m));
-                e = scale_exponent<E5M2>(row_top[i]);
+                for (int j = 1; j < words; j++) t = X::larger(t, x[i].template size<ODD>(j));
+                t = X::top(t);
+#pragma unroll
+                for (int m = 8; m; m /= 2) t = max(t, __shfl_xor_sync(0xffffffffu, t, m));
+                e = scale_exponent<E5M2>(t);
                 if (l == i) mine = e;
             }
-            const float inv = power_of_two(-e);
-            const uint32_t w0 = round2<E5M2>(x[i][0], x[i][1], inv) | round2<E5M2>(x[i][2], x[i][3], inv) << 16,
-                           w1 = round2<E5M2>(x[i][4], x[i][5], inv) | round2<E5M2>(x[i][6], x[i][7], inv) << 16;
-            if (row0 + i < R) *reinterpret_cast<uint2 *>(a.q + ((batch * a.R + row0 + i) * a.KB + kb) * kFp8Block + 8 * l) = make_uint2(w0, w1);
+            const auto f = X::factor(e, e);
+            uint32_t b[4];   // two bytes each
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                if constexpr (each == 2) {
+                    const float2 y = x[i].scaled(j, f);
+                    b[j] = round2<E5M2>(half(y.x), half(y.y));
+                } else {
+                    b[j] = round2<E5M2>(half(x[i].scaled(2 * j, f)), half(x[i].scaled(2 * j + 1, f)));
+                }
+            }
+            if (at.row0 + i < at.R) *reinterpret_cast<uint2 *>(q + i * a.KB * kFp8Block) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
         }
-        if (!TILE && l < 8 && row0 + l < R) {
-            if (a.s) a.s[(batch * a.KB + kb) * a.R + row0 + l] = power_of_two(mine);
-            a.e[batch * a.e_bytes + exponent_at(row0 + l, kb, a.RB)] = (uint8_t)(mine + 127);
+        if (!TILE && l < 8 && at.row0 + l < at.R) {
+            if (a.s) a.s[(at.batch * a.KB + at.kb) * a.R + at.row0 + l] = power_of_two(mine);
+            a.e[at.batch * a.e_bytes + exponent_at(at.row0 + l, at.kb, a.RB)] = (uint8_t)(mine + 127);
         }
     }
     if constexpr (COLUMNS) {
         if constexpr (!TILE) {
 #pragma unroll
-            for (int j = 0; j < 8; j++) {
-                col_top[j] = max(col_top[j], __shfl_xor_sync(0xffffffffu, col_top[j], 16));
-                if (h == 0) tops[warp][8 * l + j] = col_top[j];
+            for (int j = 0; j < words; j++) {
+                uint32_t t = x[0].template size<ODD>(j);
+#pragma unroll
+                for (int i = 1; i < 8; i++) t = X::larger(t, x[i].template size<ODD>(j));
+                t = X::larger(t, __shfl_xor_sync(0xffffffffu, t, 16));
+                if (h == 0) tops[warp][words * l + j] = t;
             }
             __syncthreads();
-            if (threadIdx.x < kFp8Block) {
+            if (threadIdx.x < words * 16) {   // a word's columns
                 uint32_t t = tops[0][threadIdx.x];
 #pragma unroll
-                for (int w = 1; w < 8; w++) t = max(t, tops[w][threadIdx.x]);
-                const int e = scale_exponent<E5M2>(t);
-                const int64_t c = kb * kFp8Block + threadIdx.x;
-                if (c < a.C) {
-                    if (a.st) a.st[(batch * a.RB + rb) * a.C + c] = power_of_two(e);
-                    a.et[batch * a.et_bytes + exponent_at(c, rb, a.KB)] = (uint8_t)(e + 127);
+                for (int w = 1; w < 8; w++) t = X::larger(t, tops[w][threadIdx.x]);
+                int e[each];
+                e[0] = scale_exponent<E5M2>(X::low(t));
+                if constexpr (each == 2) e[1] = scale_exponent<E5M2>(X::high(t));
+#pragma unroll
+                for (int k = 0; k < each; k++) {
+                    const int64_t c = at.kb * kFp8Block + each * threadIdx.x + k;
+                    if (c >= a.C) break;
+                    if (a.st) a.st[(at.batch * a.RB + at.rb) * a.C + c] = power_of_two(e[k]);
+                    a.et[at.batch * a.et_bytes + exponent_at(c, at.rb, a.KB)] = (uint8_t)(e[k] + 127);
                 }
-                tops[0][threadIdx.x] = __float_as_uint(power_of_two(-e));
+                const auto f = X::factor(e[0], e[each - 1]);
+                tops[0][threadIdx.x] = *reinterpret_cast<const uint32_t *>(&f);
             }
             __syncthreads();
         }
@@ -189,20 +241,65 @@ __global__ void __launch_bounds__(256) k_fp8_quantize(const __grid_constant__ QA
         // eight are turned by the column's group: 16 lanes write to 16 different banks' pairs
         const int run = 2 * warp + h;
 #pragma unroll
-        for (int j = 0; j < 8; j++) {
-            const float inv = TILE ? power_of_two(-tile_e) : __uint_as_float(tops[0][8 * l + j]);
-            const uint32_t w0 = round2<E5M2>(x[0][j], x[1][j], inv) | round2<E5M2>(x[2][j], x[3][j], inv) << 16,
-                           w1 = round2<E5M2>(x[4][j], x[5][j], inv) | round2<E5M2>(x[6][j], x[7][j], inv) << 16;
-            *reinterpret_cast<uint2 *>(turned + (8 * l + j) * kFp8Block + 8 * (run ^ l)) = make_uint2(w0, w1);
+        for (int j = 0; j < words; j++) {
+            auto f = X::factor(tile_e, tile_e);
+            if constexpr (!TILE) f = *reinterpret_cast<const decltype(f) *>(&tops[0][words * l + j]);
+            uint32_t b[each][4];
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                if constexpr (each == 2) {
+                    const float2 y = x[i].scaled(j, f), z = x[i + 1].scaled(j, f);
+                    b[0][i / 2] = round2<E5M2>(half(y.x), half(z.x));
+                    b[each - 1][i / 2] = round2<E5M2>(half(y.y), half(z.y));
+                } else {
+                    b[0][i / 2] = round2<E5M2>(half(x[i].scaled(j, f)), half(x[i + 1].scaled(j, f)));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < each; k++)
+                *reinterpret_cast<uint2 *>(turned + (8 * l + each * j + k) * kFp8Block + 8 * (run ^ l)) =
+                    make_uint2(b[k][0] | b[k][1] << 16, b[k][2] | b[k][3] << 16);
         }
         __syncthreads();
-        for (int c = 2 * warp + h; c < kFp8Block; c += 16) {
-            const int64_t col = kb * kFp8Block + c;
-            if (col >= a.C) break;
-            const uint2 w = *reinterpret_cast<const uint2 *>(turned + c * kFp8Block + 8 * (l ^ (c >> 3)));
-            *reinterpret_cast<uint2 *>(a.qt + ((batch * a.C + col) * a.RB + rb) * kFp8Block + 8 * l) = w;
-        }
+        uint8_t *qt = a.qt + ((at.batch * a.C + at.kb * kFp8Block) * a.RB + at.rb) * kFp8Block + 8 * l;
+        const int left = (int)min((int64_t)kFp8Block, a.C - at.kb * kFp8Block);
+        for (int c = 2 * warp + h; c < left; c += 16)
+            *reinterpret_cast<uint2 *>(qt + c * a.RB * kFp8Block) = *reinterpret_cast<const uint2 *>(turned + c * kFp8Block + 8 * (l ^ (c >> 3)));
     }
+}
+
+template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 3 : 2) k_fp8_quantize(const __grid_constant__ QArgs a) {
+    using X = Row<T>;
+    __shared__ uint32_t tops[8][kFp8Block];
+    __shared__ __align__(16) unsigned char turned[COLUMNS ? kFp8Block * kFp8Block : 16];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, l = lane & 15;
+    Place at;
+    const unsigned rb = blockIdx.x / (unsigned)a.KB;
+    at.rb = rb, at.kb = blockIdx.x - rb * (unsigned)a.KB, at.batch = blockIdx.y;
+    at.row0 = at.rb * kFp8Block + 16 * warp + 8 * h;
+    ptx::pdl_launch_dependents();
+    ptx::pdl_wait();
+    at.R = a.used ? min(a.R, (int64_t)max(0, __ldg(a.used))) : a.R;
+    if (at.rb * kFp8Block >= at.R) return;
+    X x[8];
+    const int64_t col0 = at.kb * kFp8Block + 8 * l;
+    const T *from = static_cast<const T *>(a.x) + (at.batch * a.R + at.row0) * a.C + col0;
+    if (a.align == 16 && (at.rb + 1) * kFp8Block <= at.R && (at.kb + 1) * kFp8Block <= a.C) {   // (no test between the loads)
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i].load(from + i * a.C, 8, 16);
+    } else {
+        const int n = (int)max((int64_t)0, min((int64_t)8, a.C - col0));
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i].load(from + i * a.C, at.row0 + i < at.R ? n : 0, a.align);
+    }
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+#pragma unroll
+        for (int j = 0; j < X::words; j++) t = X::larger(t, x[i].template size<false>(j));
+    if (__syncthreads_or(X::top(t) == 0x7f800000u)) quantize<T, E5M2, TILE, ROWS, COLUMNS, true>(a, at, x, tops, turned);
+    else quantize<T, E5M2, TILE, ROWS, COLUMNS, false>(a, at, x, tops, turned);
 }
 
 template <typename T, bool E5M2, bool TILE>
