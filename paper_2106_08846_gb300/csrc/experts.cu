@@ -5,7 +5,7 @@
 //   Xs[place[n, j]] = X[n];   Y[n] = sum_j w_nj Ys[place[n, j]]
 //
 // Order: one launch. A warp takes a contiguous run of the choices twice, 32 at a
-// time: lanes with equal experts find each other, the first adds their number to
+// time (eight times 32 on their way): lanes with equal experts find each other, the first adds their number to
 // the warp's count of that expert (no atomics: the order is by index, the same in
 // every call). Between the passes the counts of the warps, and of a cluster's CTAs
 // through distributed shared memory, become first rows.
@@ -24,7 +24,7 @@ namespace bsr {
 
 namespace {
 
-constexpr int kOrderThreads = 1024, kWarps = kOrderThreads / 32;
+constexpr int kOrderThreads = 1024, kWarps = kOrderThreads / 32, kAtOnce = 8;
 
 __device__ __forceinline__ int32_t load_cluster(uint32_t addr) {
     int32_t v;
@@ -32,7 +32,23 @@ __device__ __forceinline__ int32_t load_cluster(uint32_t addr) {
     return v;
 }
 
+// The lanes with the same expert (below 2^bits) as this one; none for lanes without one
+// (-1). A bit at a time: the instruction that compares values takes as long as there are
+// different ones (65536 choices of 64 experts: 16.5 us for the whole kernel).
+template <int BITS>
+__device__ __forceinline__ uint32_t lanes_with(int32_t x) {
+    uint32_t same = __ballot_sync(0xffffffffu, x >= 0);
+#pragma unroll
+    for (int b = 0; b < BITS; b++) {
+        const int32_t mine = x << (31 - b) >> 31;   // the bit, in all bits
+        same &= ~(__ballot_sync(0xffffffffu, mine < 0) ^ (uint32_t)mine);
+    }
+    return x >= 0 ? same : 0;
+}
+
 // Dynamic shared memory: counts[warps][E], then totals of this CTA [E], of all [E], first rows [E].
+// BITS: of experts' numbers.
+template <int BITS>
 __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_constant__ bsr_experts_t p, const int32_t *experts,
                                                                    unsigned ctas) {
     extern __shared__ int32_t words[];
@@ -46,18 +62,30 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_
     ptx::pdl_wait();
     for (int i = threadIdx.x; i < kWarps * E; i += kOrderThreads) count[i] = 0;
     __syncthreads();
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const int32_t x = i < hi ? __ldg(experts + i) : -1;
-        const bool is = (uint32_t)x < (uint32_t)E;
-        const uint32_t same = __match_any_sync(0xffffffffu, is ? x : -1);
-        if (is && lane == __ffs((int)same) - 1) count[warp * E + x] += __popc(same);
-        __syncwarp();
+    int32_t x[kAtOnce];   // (kept for the second pass if they are all)
+    auto fetch = [&](int64_t i0) {
+#pragma unroll
+        for (int t = 0; t < kAtOnce; t++) {
+            const int64_t i = i0 + 32 * t + lane;
+            const int32_t v = i < hi ? __ldg(experts + i) : -1;
+            x[t] = (uint32_t)v < (uint32_t)E ? v : -1;
+        }
+    };
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAtOnce) {
+        fetch(i0);
+#pragma unroll
+        for (int t = 0; t < kAtOnce; t++) {
+            if (i0 + 32 * t >= hi) break;
+            const uint32_t same = lanes_with<BITS>(x[t]);
+            if (x[t] >= 0 && lane == __ffs((int)same) - 1) count[warp * E + x[t]] += __popc(same);
+            __syncwarp();
+        }
     }
     __syncthreads();
     const int e = threadIdx.x;
     if (e < E) {   // the warps' counts become what the warps before have
         int32_t run = 0;
+#pragma unroll 8
         for (int w = 0; w < kWarps; w++) {
             const int32_t c = count[w * E + e];
             count[w * E + e] = run;
@@ -99,22 +127,26 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_
         const int32_t at = upto - padded + (warp ? sums[warp - 1] : 0);
         all[e] = total;
         first[e] = at;
+#pragma unroll 8
         for (int w = 0; w < kWarps; w++) count[w * E + e] += at + before;
         if (rank == 0) p.offsets[e] = at;
     }
     if (rank == 0 && threadIdx.x == 0) p.offsets[E] = used;
     __syncthreads();
-    for (int64_t i0 = lo; i0 < hi; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const int32_t x = i < hi ? __ldg(experts + i) : -1;
-        const bool is = (uint32_t)x < (uint32_t)E;
-        const uint32_t same = __match_any_sync(0xffffffffu, is ? x : -1);
-        const int32_t row = is ? count[warp * E + x] + __popc(same & ((1u << lane) - 1)) : -1;
-        __syncwarp();
-        if (is && lane == __ffs((int)same) - 1) count[warp * E + x] += __popc(same);
-        __syncwarp();
-        if (i < hi) p.place[i] = row;
-        if (is) p.source[row] = (int32_t)i;
+    for (int64_t i0 = lo; i0 < hi; i0 += 32 * kAtOnce) {
+        if (hi - lo > 32 * kAtOnce) fetch(i0);
+#pragma unroll
+        for (int t = 0; t < kAtOnce; t++) {
+            if (i0 + 32 * t >= hi) break;
+            const int64_t i = i0 + 32 * t + lane;
+            const uint32_t same = lanes_with<BITS>(x[t]);
+            const int32_t row = x[t] >= 0 ? count[warp * E + x[t]] + __popc(same & ((1u << lane) - 1)) : -1;
+            __syncwarp();
+            if (x[t] >= 0 && lane == __ffs((int)same) - 1) count[warp * E + x[t]] += __popc(same);
+            __syncwarp();
+            if (i < hi) p.place[i] = row;
+            if (row >= 0) p.source[row] = (int32_t)i;
+        }
     }
     // rows that nobody was sent to: behind an expert's, and behind the last one's
     for (int f = (int)rank * kWarps + warp; f < E; f += (int)ctas * kWarps) {
@@ -137,6 +169,7 @@ struct Word {
 };
 
 constexpr int kWords = 4;   // of a row, a lane holds at once
+constexpr int kRows = 4;    // rows of a sum on their way at once
 
 __device__ __forceinline__ int32_t row_of(const bsr_experts_t &p, int64_t pair) {
     const int32_t r = __ldg(p.place + pair);
@@ -194,17 +227,26 @@ __global__ void __launch_bounds__(256) k_expert_sum(const __grid_constant__ bsr_
     for (int64_t u = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); u < units; u += (int64_t)gridDim.x * 8) {
         const int64_t n = u / parts, at = (u - n * parts) * 32 * kWords + lane;
         float sum[kWords][n_w] = {};
-        for (int j = 0; j < p.k; j++) {
-            const int64_t r = row_of(p, n * p.k + j);
-            if (r < 0) continue;
-            const float w = weights ? __ldg(weights + n * p.k + j) : 1.f;
+        for (int j0 = 0; j0 < p.k; j0 += kRows) {
+            Word<T, W> y[kRows][kWords];
+            int64_t r[kRows];
 #pragma unroll
-            for (int v = 0; v < kWords; v++) {
-                if (at + 32 * v >= words) break;
-                Word<T, W> y;
-                y.w = __ldg(Ys + r * words + at + 32 * v);
+            for (int j = 0; j < kRows; j++) r[j] = j0 + j < p.k ? row_of(p, n * p.k + j0 + j) : -1;
 #pragma unroll
-                for (int i = 0; i < n_w; i++) sum[v][i] = fmaf(w, to_f32(y.v[i]), sum[v][i]);
+            for (int j = 0; j < kRows; j++)
+#pragma unroll
+                for (int v = 0; v < kWords; v++)
+                    if (r[j] >= 0 && at + 32 * v < words) y[j][v].w = __ldg(Ys + r[j] * words + at + 32 * v);
+#pragma unroll
+            for (int j = 0; j < kRows; j++) {
+                if (r[j] < 0) continue;
+                const float w = weights ? __ldg(weights + n * p.k + j0 + j) : 1.f;
+#pragma unroll
+                for (int v = 0; v < kWords; v++)
+                    if (at + 32 * v < words) {
+#pragma unroll
+                        for (int i = 0; i < n_w; i++) sum[v][i] = fmaf(w, to_f32(y[j][v].v[i]), sum[v][i]);
+                    }
             }
         }
 #pragma unroll
@@ -267,6 +309,23 @@ __global__ void __launch_bounds__(256) k_expert_sum_backward(const __grid_consta
     }
 }
 
+template <int BITS>
+cudaError_t order(const bsr_experts_t &p, const int32_t *experts, cudaStream_t s) {
+    static std::atomic<uint64_t> attr_set{0}, wide_set{0};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    const uint64_t bit = 1ull << (dev & 63);
+    cudaError_t e = allow_smem(k_expert_order<BITS>, (kWarps + 3) * (1 << BITS) * 4, attr_set);
+    if (e == cudaSuccess && !(wide_set.load() & bit)) {
+        e = cudaFuncSetAttribute(k_expert_order<BITS>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) wide_set.fetch_or(bit);
+    }
+    if (e != cudaSuccess) return e;
+    const int64_t pairs = p.N * p.k;
+    const unsigned ctas = pairs <= 4 * kOrderThreads ? 1 : pairs <= 16 * kOrderThreads ? 8 : 16;
+    return launch_clusters(k_expert_order<BITS>, ctas, dim3(ctas), dim3(kOrderThreads), (size_t)(kWarps + 3) * p.E * 4, s, p, experts, ctas);
+}
+
 unsigned grid_of(int64_t units) { return (unsigned)std::min<int64_t>(std::max<int64_t>((units + 7) / 8, 1), 1 << 20); }
 
 // f(T(), W()) with the element type and the widest word that rows of D are made of.
@@ -283,12 +342,7 @@ cudaError_t by_word(int64_t D, bsr_dtype_t dt, F f) {
 }  // namespace
 
 cudaError_t launch_expert_order(const bsr_experts_t &p, const int32_t *experts, cudaStream_t s) {
-    static std::atomic<uint64_t> attr_set{0};
-    const int most = (kWarps + 3) * kMostExperts * 4;
-    const cudaError_t e = allow_smem(k_expert_order, most, attr_set);
-    if (e != cudaSuccess) return e;
-    const unsigned ctas = p.N * p.k > 4 * kOrderThreads ? 8 : 1;
-    return launch_clusters(k_expert_order, ctas, dim3(ctas), dim3(kOrderThreads), (size_t)(kWarps + 3) * p.E * 4, s, p, experts, ctas);
+    return p.E <= 16 ? order<4>(p, experts, s) : p.E <= 64 ? order<6>(p, experts, s) : order<10>(p, experts, s);
 }
 
 cudaError_t launch_expert_rows(const bsr_experts_t &p, const void *X, void *Xs, int64_t D, bsr_dtype_t dt, cudaStream_t s) {
