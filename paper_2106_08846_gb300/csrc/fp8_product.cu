@@ -166,6 +166,22 @@ __device__ __forceinline__ Unit unit_at(const Sizes &a, const Runs &r, unsigned 
     return DRAIN ? unit_of(a, r, v) : unit_call(a, r, v);
 }
 
+// A bounded wait, its long form once for all roles (as unit_call).
+__device__ __noinline__ bool wait_call(uint64_t *bar, uint32_t parity, uint64_t limit_ns, const int *flag) {
+    return wait_or_abort(bar, parity, limit_ns, flag);
+}
+template <bool DRAIN>
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, uint64_t limit_ns, const int *flag) {
+    if (DRAIN) return wait_or_abort(bar, parity, limit_ns, flag);
+    return ptx::mbar_try_wait(bar, parity) || wait_call(bar, parity, limit_ns, flag);
+}
+// Stops every role of the pair; a timeout is recorded.
+__device__ __noinline__ void halt_pair(int *stop, uint32_t rank) {
+    if (!aborted(stop)) set_status(&g_status, DEV_TIMEOUT);
+    atomicExch(stop, 1);
+    ptx::store_cluster(ptx::map_to_cta(stop, rank ^ 1), 1);
+}
+
 // Tiles of the rows o .. p - 1, from a multiple of 128 on.
 __device__ __forceinline__ uint32_t tiles_of(int32_t o, int32_t p) {
     return p > o ? ((uint32_t)p - (uint32_t)o / 128 * 128 + 255) / 256 : 0;
@@ -182,6 +198,18 @@ __device__ __forceinline__ uint4 *turned(unsigned char *buf, int row, int chunk)
     return reinterpret_cast<uint4 *>(buf + row * 64 + 16 * (chunk ^ ((row >> 1) & 3)));
 }
 
+// (a call, as few have a bias)
+__device__ __noinline__ void bias_of(const float *bias, float (&b)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16; j++) b[j] = __ldg(bias + j);
+}
+__device__ __forceinline__ void add_bias(const float *bias, float (&x)[32]) {
+    float b[16];
+    bias_of(bias, b);
+#pragma unroll
+    for (int i = 0; i < 8; i++) x[4 * i] += b[2 * i], x[4 * i + 1] += b[2 * i + 1], x[4 * i + 2] += b[2 * i], x[4 * i + 3] += b[2 * i + 1];
+}
+
 // 16 rows of the result from `row` on x 64 columns from c on, of b's rows in order: x as
 // tc5::ld_16x64 leaves it is 16 columns from c + 16 (lane % 4) on of this thread, of rows
 // lane / 4 and + 8.
@@ -191,14 +219,7 @@ __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64
     c += 16 * (lane & 3);
     if (c >= a.M) return;   // (64 columns are there or not)
     row += lane >> 2;
-    if (a.bias) {
-        const float *bias = a.bias + (int64_t)un.batch * a.M + c;
-#pragma unroll
-        for (int i = 0; i < 8; i++) {
-            const float b0 = __ldg(bias + 2 * i), b1 = __ldg(bias + 2 * i + 1);
-            x[4 * i] += b0, x[4 * i + 1] += b1, x[4 * i + 2] += b0, x[4 * i + 3] += b1;
-        }
-    }
+    if (a.bias) add_bias(a.bias + (int64_t)un.batch * a.M + c, x);
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         if (row + 8 * h < un.r0 || row + 8 * h >= un.r1) continue;
@@ -358,13 +379,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     const Sizes sizes = {a.rows, (int)a.KB, a.group, a.E, a.splits, 2 * a.half, a.tiles_m, a.tiles_n};
     const uint32_t tmem = tmem_s;
     const bool elected = ptx::elect_one();
-    // stops every role of this pair; a timeout is recorded
     auto halt = [&]() {
-        if (elected) {
-            if (!aborted(&stop)) set_status(&g_status, DEV_TIMEOUT);
-            atomicExch(&stop, 1);
-            ptx::store_cluster(ptx::map_to_cta(&stop, rank ^ 1), 1);
-        }
+        if (elected) halt_pair(&stop, rank);
     };
 
     // ---- producers: the pair's steps prod, prod + np, ... No more producers
@@ -429,7 +445,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         uint32_t fphase = 0;
         bool ok = true;
         auto wait_acc = [&](const Unit &u) {
-            ok = __all_sync(0xffffffffu, wait_or_abort(&acc_full[ab], fphase, a.wait_ns * (uint64_t)(u.i1 - u.i0 + 2), &stop));
+            ok = __all_sync(0xffffffffu, wait_for<DRAIN>(&acc_full[ab], fphase, a.wait_ns * (uint64_t)(u.i1 - u.i0 + 2), &stop));
             if (!ok) halt();
             tc5::fence_after();
             return tmem + (uint32_t)ab * acc_step + ((uint32_t)(32 * q) << 16) + 32 * first;
@@ -537,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 more = seek();
             }
             while (more) {
-                const bool got = wait_or_abort(&empty[s], phase, a.wait_ns, &stop);
+                const bool got = wait_for<DRAIN>(&empty[s], phase, a.wait_ns, &stop);
                 if (!__all_sync(0xffffffffu, got && !aborted(&stop))) {
                     halt();
                     break;
@@ -571,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                             // barrier says, or the stage has been filled again since
                             set = n_sets % kScaleSets == 0 ? tmem + kScaleCol : set + kScaleCols;
                             if (n_sets >= kScaleSets && n_steps - end_step[0] <= ns)
-                                ok = wait_or_abort(&empty[end_stage[0]], end_phase[0], a.wait_ns, &stop);
+                                ok = wait_for<DRAIN>(&empty[end_stage[0]], end_phase[0], a.wait_ns, &stop);
                             n_sets++;
 #pragma unroll
                             for (int k = 0; k + 1 < kScaleSets; k++)
@@ -579,9 +595,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                         }
                         if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
                             const int before = n_acc - (shared_cols ? 1 : 2);
-                            if (before >= 0) ok = ok && wait_or_abort(&acc_empty[before & 1], (uint32_t)(before >> 1) & 1, a.wait_ns, &stop);
+                            if (before >= 0) ok = ok && wait_for<DRAIN>(&acc_empty[before & 1], (uint32_t)(before >> 1) & 1, a.wait_ns, &stop);
                         }
-                        ok = ok && wait_or_abort(&full[s], fphase, a.wait_ns, &stop);
+                        ok = ok && wait_for<DRAIN>(&full[s], fphase, a.wait_ns, &stop);
                         if (!ok) break;
                         tc5::fence_after();
                         if (scales) {
