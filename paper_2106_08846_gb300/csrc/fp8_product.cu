@@ -6,12 +6,13 @@
 // block of 128 columns is a step: four MMAs (M = 256, N = 2 half, K = 32), which
 // multiply by the rows' scales themselves, powers of two as bytes in tensor memory.
 //
-//   warps 0, 1, 3  producers, a step each in turn: 128 rows of a and `half` of b a
-//                  CTA, 128 bytes each, by TMA (128-byte swizzle) into a stage of the
-//                  ring; every fourth block the rows' exponents of four blocks with it
+//   warps 0, 1     128 rows of a a CTA, 128 bytes each, by TMA (128-byte swizzle) into a
+//                  stage of the ring, a step each in turn; every fourth block the
+//                  rows' exponents of four blocks with it
+//   warps 3, 4     the same of `half` rows of b
 //   warp 2         MMAs of the pair's first CTA, and before them the exponents' copy
 //                  from shared to tensor memory
-//   warps 4 .. 11  epilogue: 32 rows and half of the columns each. Where 128 of b's rows
+//   warps 8 .. 15  epilogue: 32 rows and half of the columns each. Where 128 of b's rows
 //                  share their scales, its rows are loaded in the order that leaves a thread 16
 //                  columns side by side, and four lanes store 128 bytes of a row (bf16) straight from
 //                  tensor memory; else through 2 KB of shared memory a warp
@@ -58,8 +59,8 @@ namespace bsr {
 
 namespace {
 
-constexpr int kEpiWarp0 = 4, kMmaWarp = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
-constexpr int kProducers = 3, kStages = 8, kLeastStages = 6;
+constexpr int kEpiWarp0 = 8, kMmaWarp = 2, kEpiWarps = 8, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kProducers = 2, kStages = 8, kLeastStages = 6;   // producers: of a, and of b
 constexpr uint32_t kABytes = 128 * 128;       // a CTA's rows of a, a step
 constexpr uint32_t kOverlap = 64;             // columns that the accumulators of 256 columns share
 // Tensor memory behind them: sets of exponents, of a in the first four of 16 columns.
@@ -72,8 +73,8 @@ constexpr int kMostSteps = 128;               // of bf16 ones
 constexpr uint32_t kTurnBytes = 2048;         // of an epilogue warp: 32 rows of 64 bytes
 constexpr uint32_t kMaxSmem = 227 * 1024 - 9 * 1024;   // (static: the runs' table, barriers)
 constexpr uint64_t kDrainNs = 200000000ull;   // bound for copies and MMAs already issued
-// Registers of a thread: 4 warps of 72 and 8 of 216 are what 384 threads are launched with (168 each).
-constexpr int kFewRegs = 72, kManyRegs = 216;
+// Registers of a thread: 8 warps of 56 and 8 of 200 are what 512 threads are launched with (128 each).
+constexpr int kFewRegs = 56, kManyRegs = 200;
 
 __device__ int g_status;
 
@@ -166,21 +167,35 @@ __device__ __forceinline__ Unit unit_at(const Sizes &a, const Runs &r, unsigned 
     return DRAIN ? unit_of(a, r, v) : unit_call(a, r, v);
 }
 
-// A bounded wait, its long form once for all roles (as unit_call).
+// A bounded wait that gives up when another role stopped; the timer is read every 64 tries.
+__device__ __forceinline__ bool wait_long(uint64_t *bar, uint32_t parity, uint64_t limit_ns, const int *flag) {
+    uint64_t t0 = 0;
+    while (true) {
+#pragma unroll 1
+        for (int k = 0; k < 64; k++)
+            if (ptx::mbar_try_wait(bar, parity)) return true;
+        if (aborted(flag)) return false;
+        const uint64_t t = ptx::globaltimer();
+        if (t0 == 0) t0 = t;
+        else if (t - t0 > limit_ns) return false;
+    }
+}
+// (its code once for all roles, as unit_call)
 __device__ __noinline__ bool wait_call(uint64_t *bar, uint32_t parity, uint64_t limit_ns, const int *flag) {
-    return wait_or_abort(bar, parity, limit_ns, flag);
+    return wait_long(bar, parity, limit_ns, flag);
 }
 template <bool DRAIN>
 __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, uint64_t limit_ns, const int *flag) {
-    if (DRAIN) return wait_or_abort(bar, parity, limit_ns, flag);
-    return ptx::mbar_try_wait(bar, parity) || wait_call(bar, parity, limit_ns, flag);
+    return ptx::mbar_try_wait(bar, parity) || (DRAIN ? wait_long(bar, parity, limit_ns, flag) : wait_call(bar, parity, limit_ns, flag));
 }
 // Stops every role of the pair; a timeout is recorded.
-__device__ __noinline__ void halt_pair(int *stop, uint32_t rank) {
+__device__ __forceinline__ void halt_pair(int *stop, uint32_t rank) {
     if (!aborted(stop)) set_status(&g_status, DEV_TIMEOUT);
     atomicExch(stop, 1);
     ptx::store_cluster(ptx::map_to_cta(stop, rank ^ 1), 1);
 }
+
+__device__ __noinline__ void halt_call(int *stop, uint32_t rank) { halt_pair(stop, rank); }
 
 // Tiles of the rows o .. p - 1, from a multiple of 128 on.
 __device__ __forceinline__ uint32_t tiles_of(int32_t o, int32_t p) {
@@ -198,18 +213,6 @@ __device__ __forceinline__ uint4 *turned(unsigned char *buf, int row, int chunk)
     return reinterpret_cast<uint4 *>(buf + row * 64 + 16 * (chunk ^ ((row >> 1) & 3)));
 }
 
-// (a call, as few have a bias)
-__device__ __noinline__ void bias_of(const float *bias, float (&b)[16]) {
-#pragma unroll
-    for (int j = 0; j < 16; j++) b[j] = __ldg(bias + j);
-}
-__device__ __forceinline__ void add_bias(const float *bias, float (&x)[32]) {
-    float b[16];
-    bias_of(bias, b);
-#pragma unroll
-    for (int i = 0; i < 8; i++) x[4 * i] += b[2 * i], x[4 * i + 1] += b[2 * i + 1], x[4 * i + 2] += b[2 * i], x[4 * i + 3] += b[2 * i + 1];
-}
-
 // 16 rows of the result from `row` on x 64 columns from c on, of b's rows in order: x as
 // tc5::ld_16x64 leaves it is 16 columns from c + 16 (lane % 4) on of this thread, of rows
 // lane / 4 and + 8.
@@ -219,7 +222,14 @@ __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64
     c += 16 * (lane & 3);
     if (c >= a.M) return;   // (64 columns are there or not)
     row += lane >> 2;
-    if (a.bias) add_bias(a.bias + (int64_t)un.batch * a.M + c, x);
+    if (a.bias) {
+        const float *bias = a.bias + (int64_t)un.batch * a.M + c;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            const float b0 = __ldg(bias + 2 * i), b1 = __ldg(bias + 2 * i + 1);
+            x[4 * i] += b0, x[4 * i + 1] += b1, x[4 * i + 2] += b0, x[4 * i + 3] += b1;
+        }
+    }
 #pragma unroll
     for (int h = 0; h < 2; h++) {
         if (row + 8 * h < un.r0 || row + 8 * h >= un.r1) continue;
@@ -317,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     const int ns = a.ns;
     const uint32_t stage_bytes = a.stage_bytes;
     __shared__ uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], done;
-    __shared__ int stop, loads[kProducers][2];   // loads[producer][CTA of the pair]: steps loaded
+    __shared__ int stop, loads[2][kProducers][2];   // loads[a or b][producer][CTA of the pair]: steps loaded
     __shared__ int freed, handed;                // commits issued to `empty` and to `acc_full`
     __shared__ uint32_t tmem_s;
     __shared__ Runs runs;
@@ -327,8 +337,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     const uint32_t rank = ptx::cluster_rank();
     const unsigned pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     if (threadIdx.x == 0) stop = freed = handed = 0;
-    if (threadIdx.x < 32) {   // a barrier a lane: a producer's arrival with its bytes, commits, the epilogue warps of both CTAs
-        if (lane < kStages) ptx::mbar_init(&full[lane], 1);
+    if (threadIdx.x < 32) {   // a barrier a lane: two producers' arrivals with their bytes, commits, the epilogue warps of both CTAs
+        if (lane < kStages) ptx::mbar_init(&full[lane], 2);
         else if (lane < 2 * kStages) ptx::mbar_init(&empty[lane - kStages], 1);
         else if (lane < 2 * kStages + 2) ptx::mbar_init(&acc_full[lane & 1], 1);
         else if (lane < 2 * kStages + 4) ptx::mbar_init(&acc_empty[lane & 1], 2 * kEpiWarps);
@@ -380,7 +390,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     const uint32_t tmem = tmem_s;
     const bool elected = ptx::elect_one();
     auto halt = [&]() {
-        if (elected) halt_pair(&stop, rank);
+        if (!elected) return;
+        if (DRAIN) halt_pair(&stop, rank);
+        else halt_call(&stop, rank);
     };
 
     // ---- producers: the pair's steps prod, prod + np, ... No more producers
@@ -388,8 +400,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     // step g - 2 ns was, or the stage's barrier, which tells phases apart by their
     // parity, would let it pass a round early; its last wait, for step
     // g - np - ns, tells it so if np <= ns.
-    const int prod = warp < kMmaWarp ? warp : kMmaWarp, np = min(kProducers, ns);
-    const bool producer = warp < kEpiWarp0 && warp != kMmaWarp && prod < np;
+    constexpr int np = kProducers;
+    const bool producer = warp < 5 && warp != kMmaWarp, of_b = warp > kMmaWarp;
+    const int prod = of_b ? warp - 3 : warp;
     unsigned round = 0, v = pair;
     Unit un = {};
     int i = 0, s = prod % ns, issued = 0;
@@ -414,16 +427,17 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         } else if (elected) {
             const uint32_t dst = smem0 + s * stage_bytes, bar = first0 + 8 * s;
             const bool scales = i == un.i0 || i % kScaleSteps == 0;
-            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * (stage_bytes + (scales ? (a.half == 128 ? 3 : 2) * 512 : 0)));
-            const int m = (int)(un.m0 + rank * 128), n = (int)un.n0;
-            ptx::tma_load_2d_pair_at(dst, &a.a, i * kFp8Block, m, bar);
-            const int nb = n + (int)rank * a.half;
-            if constexpr (ORDERED) ptx::tma_load_5d_pair_at(dst + kABytes, &a.b, i * kFp8Block, 0, 0, 0, (int)((un.batch * a.M + nb) / 64), bar);
-            else ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, nb, un.batch, bar);
-            if (scales) {
-                const uint32_t to = smem0 + ns * stage_bytes + s * kScaleBytes;
-                ptx::tma_load_3d_pair_at(to, &a.ea, 0, m / 128, i / kScaleSteps, bar);
-                ptx::tma_load_4d_pair_at(to + 512, &a.eb, 0, n / 128, i / kScaleSteps, un.batch, bar);
+            const int m = (int)(un.m0 + rank * 128), n = (int)un.n0, nb = n + (int)rank * a.half;
+            const uint32_t words = of_b ? (a.half == 128 ? 1024 : 512) : 512;
+            if (rank == 0) ptx::mbar_arrive_expect_tx_at(bar0 + 8 * s, 2 * ((of_b ? stage_bytes - kABytes : kABytes) + (scales ? words : 0)));
+            const uint32_t to = smem0 + ns * stage_bytes + s * kScaleBytes;
+            if (!of_b) {
+                ptx::tma_load_2d_pair_at(dst, &a.a, i * kFp8Block, m, bar);
+                if (scales) ptx::tma_load_3d_pair_at(to, &a.ea, 0, m / 128, i / kScaleSteps, bar);
+            } else {
+                if constexpr (ORDERED) ptx::tma_load_5d_pair_at(dst + kABytes, &a.b, i * kFp8Block, 0, 0, 0, (int)((un.batch * a.M + nb) / 64), bar);
+                else ptx::tma_load_3d_pair_at(dst + kABytes, &a.b, i * kFp8Block, nb, un.batch, bar);
+                if (scales) ptx::tma_load_4d_pair_at(to + 512, &a.eb, 0, n / 128, i / kScaleSteps, un.batch, bar);
             }
         }
         issued++;
@@ -561,8 +575,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                 more = load_step();
             }
             if (elected) {
-                loads[prod][rank] = issued;
-                ptx::store_cluster(ptx::map_to_cta(&loads[prod][rank], rank ^ 1), (uint32_t)issued);
+                loads[of_b][prod][rank] = issued;
+                ptx::store_cluster(ptx::map_to_cta(&loads[of_b][prod][rank], rank ^ 1), (uint32_t)issued);
             }
         } else if (warp == kMmaWarp && rank == 0) {
             if (elected) {   // (one thread throughout: what the others would cost is in the MMAs' way)
@@ -593,10 +607,6 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                             for (int k = 0; k + 1 < kScaleSets; k++)
                                 end_step[k] = end_step[k + 1], end_stage[k] = end_stage[k + 1], end_phase[k] = end_phase[k + 1];
                         }
-                        if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
-                            const int before = n_acc - (shared_cols ? 1 : 2);
-                            if (before >= 0) ok = ok && wait_for<DRAIN>(&acc_empty[before & 1], (uint32_t)(before >> 1) & 1, a.wait_ns, &stop);
-                        }
                         ok = ok && wait_for<DRAIN>(&full[s], fphase, a.wait_ns, &stop);
                         if (!ok) break;
                         tc5::fence_after();
@@ -605,6 +615,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                             tc5::copy_pair_32x16(set, sd);
                             tc5::copy_pair_32x16(set + 4, sd + (512 >> 4));
                             if (shared_cols) tc5::copy_pair_32x16(set + 8, sd + (1024 >> 4));
+                        }
+                        if (fresh) {   // the accumulator before (the next but one) is taken out as far as it must be
+                            const int before = n_acc - (shared_cols ? 1 : 2);
+                            if (before >= 0) {
+                                ok = wait_for<DRAIN>(&acc_empty[before & 1], (uint32_t)(before >> 1) & 1, a.wait_ns, &stop);
+                                if (!ok) break;
+                                tc5::fence_after();
+                            }
                         }
                         const uint64_t stage = (uint64_t)((s * stage_bytes) >> 4);
                         const uint32_t idesc = a.idesc | tc5::idesc_byte((uint32_t)i % kScaleSteps), acc = tmem + (uint32_t)(n_acc & 1) * acc_step;
@@ -644,14 +662,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     tc5::fence_before();
     meet();
     if (aborted(&stop)) {
-        // (the same for both CTAs.) The loads that only one CTA's producer
-        // issued are completed by the other's, so that every barrier phase can
+        // (the same for both CTAs.) The loads that only some of a step's producers
+        // issued are completed by the others, so that every barrier phase can
         // finish, and the CTA whose barriers count the bytes waits for those
         // that no later load of their stage shows to be complete: no copy
         // outlives the CTAs
         if (producer) {
             int most[kProducers];
-            for (int p = 0; p < np; p++) most[p] = max(loads[p][0], loads[p][1]);
+            for (int p = 0; p < np; p++) most[p] = max(max(loads[0][p][0], loads[0][p][1]), max(loads[1][p][0], loads[1][p][1]));
             while (more && issued < most[prod]) more = load_step();
             for (int k = max(0, issued - ns); rank == 0 && k < issued; k++) {
                 const int g = prod + np * k, later = g + ns;
