@@ -208,6 +208,12 @@ __device__ __forceinline__ void st_global_32(void *p, const uint32_t (&v)[8]) {
                  "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
                  : "memory");
 }
+// The same for results that push operands which are read again out of L2 last.
+__device__ __forceinline__ void st_global_32_first_out(void *p, const uint32_t (&v)[8]) {
+    asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
 // True for one lane of a converged warp.
 __device__ __forceinline__ bool elect_one() {
     uint32_t p;
