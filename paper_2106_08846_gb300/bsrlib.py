@@ -820,57 +820,44 @@ class Fp8Matrix:
     q[r, c] * scale[c // 128, r // tile]. `q` has cols rounded up to 128, zeros past
     them; `exponent` is what the product reads of the scales, powers of two (include/bsr.h). fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
 
-    def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda",
-                 apart: bool = False):
+    __slots__ = ("rows", "cols", "tile", "fmt", "batch", "_q", "_base", "_first", "_scale", "_c", "__weakref__")
+
+    def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda"):
         code = _FP8.get(fmt)
         if code is None or (tile != 1 and tile != 128):
             raise ValueError("fmt is 'e4m3' or 'e5m2', tile 1 or 128")
         self.rows, self.cols, self.tile, self.fmt, self.batch = rows, cols, tile, fmt, batch
-        n, blocks, runs = 1 if batch is None else batch, (cols + 127) // 128, rows if tile == 1 else (rows + 127) // 128
-        values, exponents, scales = n * rows * blocks * 128, n * ((blocks + 3) // 4) * ((rows + 127) // 128) * 512, n * blocks * runs
-        each = () if batch is None else (batch,)
-        self._q = self._scale = None
-        # One allocation, of which views are made when they are asked for, takes the host 3 us less than
-        # a tensor for each, and the views 9 more: `apart` is for who reads them.
-        if apart:
-            self._q = torch.empty((*each, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
-            self._scale = torch.empty((*each, blocks, runs), dtype=torch.float32, device=device)
-            self._base, self._first = torch.empty(exponents, dtype=torch.uint8, device=device), 0
-            p = (self._q.data_ptr(), self._base.data_ptr(), self._scale.data_ptr()) if values else (None, None, None)
-            self._made = (self._q, self._scale, self._base)
-        else:
-            self._base, self._first = torch.empty(values + exponents + 4 * scales, dtype=_FP8_TYPE[fmt], device=device), values
+        blocks, runs, n = (cols + 127) // 128, rows if tile == 1 else (rows + 127) // 128, 1 if batch is None else batch
+        # the scales, and before them as many rows as the exponents take (a tensor less, and a view only for who reads scales)
+        first = -(-n * ((blocks + 3) // 4) * ((rows + 127) // 128) * 128 // runs) if runs else 0
+        self._q = torch.empty((rows, blocks * 128) if batch is None else (batch, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
+        self._base = torch.empty((first + n * blocks, runs), dtype=torch.float32, device=device)
+        self._first, self._scale = first, None
+        if n and rows and cols:
             at = self._base.data_ptr()
-            p = (at, at + values, at + values + exponents) if values else (None, None, None)
-            self._made = (self._base,)
-        self._c = _Fp8Matrix(n, rows, cols, tile, code, *p)
+            self._c = _Fp8Matrix(n, rows, cols, tile, code, self._q.data_ptr(), at, at + 4 * first * runs)
+        else:
+            self._c = _Fp8Matrix(n, rows, cols, tile, code, None, None, None)
 
     # (to be filled, not replaced: the calls have their addresses)
     @property
     def q(self) -> torch.Tensor:
-        if self._q is None:
-            r, c = self.rows, (self.cols + 127) // 128 * 128
-            self._q = (self._base.as_strided((r, c), (c, 1)) if self.batch is None else
-                       self._base.as_strided((self.batch, r, c), (r * c, c, 1)))
         return self._q
 
     @property
     def scale(self) -> torch.Tensor:
         if self._scale is None:
-            b, r = (self.cols + 127) // 128, self.rows if self.tile == 1 else (self.rows + 127) // 128
-            flat, n = self._base.view(torch.float32), b * r * (1 if self.batch is None else self.batch)
-            first = flat.shape[0] - n
-            self._scale = (flat.as_strided((b, r), (r, 1), first) if self.batch is None else
-                           flat.as_strided((self.batch, b, r), (b * r, r, 1), first))
+            scale = self._base[self._first:]
+            self._scale = scale if self.batch is None else scale.view(self.batch, -1, scale.shape[1])
         return self._scale
 
     @property
     def exponent(self) -> torch.Tensor:
-        w, r = (self.cols + 511) // 512, (self.rows + 127) // 128
-        flat = self._base.view(torch.uint8)
-        if self.batch is None:
-            return flat.as_strided((w, r, 512), (r * 512, 512, 1), self._first)
-        return flat.as_strided((self.batch, w, r, 512), (w * r * 512, r * 512, 512, 1), self._first)
+        shape = ((self.cols + 511) // 512, (self.rows + 127) // 128, 512)
+        if self.batch is not None:
+            shape = (self.batch, *shape)
+        words = 128 * self._c.batch * ((self.cols + 511) // 512) * ((self.rows + 127) // 128)
+        return self._base.view(-1)[:words].view(torch.uint8).view(shape)
 
 
 def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: str = "rows", used: Optional[torch.Tensor] = None,
@@ -890,32 +877,33 @@ def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: st
         raise ValueError("x must be [R, C] or [batch, R, C]")
     if not x.is_contiguous():
         raise ValueError("x must be contiguous")
-    dt = dtype_code(x.dtype)
+    dt = _DT.get(x.dtype)
+    if dt is None:
+        dt = dtype_code(x.dtype)   # (raises)
     if used is not None:
         _check_rows("used", used, (1,), torch.int32)
-    if form == "both":
-        sizes = ((R, C), (C, R))
-    elif form == "rows":
-        sizes = ((R, C),)
-    elif form == "columns":
-        sizes = ((C, R),)
-    else:
+    if form not in ("rows", "columns", "both"):
         raise ValueError("form is 'rows', 'columns' or 'both'")
+    rows = columns = None
     if out is None:
-        m = [Fp8Matrix(r, c, tile, fmt, batch, x.device, form == "both") for r, c in sizes]
+        device = x.device
+        if form != "columns":
+            rows = Fp8Matrix(R, C, tile, fmt, batch, device)
+        if form != "rows":
+            columns = Fp8Matrix(C, R, tile, fmt, batch, device)
+        out = rows if columns is None else columns if rows is None else (rows, columns)
         if stream is not None:
-            _lend(stream, x.device, *[t for f in m for t in f._made])
+            _lend(stream, device, *[t for m in (rows, columns) if m is not None for t in (m._q, m._base)])
     else:
-        m = list(out) if form == "both" else [out]
-        if [(f.rows, f.cols, f.tile, f.fmt, f.batch) for f in m] != [(r, c, tile, fmt, batch) for r, c in sizes]:
-            raise ValueError("out is of other sizes")
-    first = m[0]._c
-    rows, columns = (first, None) if form == "rows" else (None, first) if form == "columns" else (first, m[1]._c)
-    status = (_lib or load()).bsr_fp8_quantize(x.data_ptr(), dt, rows, columns, None if used is None else used.data_ptr(),
-                                               _stream(stream))
+        rows, columns = (out, None) if form == "rows" else (None, out) if form == "columns" else out
+        for m, size in ((rows, (R, C)), (columns, (C, R))):
+            if m is not None and (m.rows, m.cols, m.tile, m.fmt, m.batch) != (*size, tile, fmt, batch):
+                raise ValueError("out is of other sizes")
+    status = (_lib or load()).bsr_fp8_quantize(x.data_ptr(), dt, None if rows is None else rows._c, None if columns is None else columns._c,
+                                               None if used is None else used.data_ptr(), _stream(stream))
     if status:
         _check(status, "bsr_fp8_quantize")
-    return m[0] if len(m) == 1 else tuple(m)
+    return out
 
 
 def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = None, dtype: torch.dtype = torch.bfloat16,
@@ -926,33 +914,39 @@ def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = N
     batch of E matrices and each run of a's rows meets its expert's (bias [E, b.rows];
     rows in no run are left as they were); over "columns", Y [E, a.rows, b.rows] has a
     sum over each run of columns, whose offsets are multiples of 128."""
-    if over not in ("rows", "columns"):
+    if over != "rows" and over != "columns":
         raise ValueError("over is 'rows' or 'columns'")
-    dtype = dtype if Y is None else Y.dtype
-    dt = dtype_code(dtype)
-    if offsets is None:
-        group, E = BSR_GROUP_NONE, 0
-    else:
+    if Y is not None:
+        dtype = Y.dtype
+    dt = _DT.get(dtype)
+    if dt is None:
+        dt = dtype_code(dtype)   # (raises)
+    group, E, batch, shape = BSR_GROUP_NONE, 0, None, (a.rows, b.rows)
+    if offsets is not None:
         E = offsets.shape[0] - 1
         _check_rows("offsets", offsets, (E + 1,), torch.int32)
-        group = BSR_GROUP_ROWS if over == "rows" else BSR_GROUP_COLUMNS
-    if a.batch is not None or b.batch != (E if group == BSR_GROUP_ROWS else None):
+        if over == "rows":
+            group, batch = BSR_GROUP_ROWS, E
+        else:
+            group, shape = BSR_GROUP_COLUMNS, (E, a.rows, b.rows)
+    if a.batch is not None or b.batch != batch:
         raise ValueError("a is one matrix, b one for each expert by rows, else one")
     if bias is not None:
-        _check_rows("bias", bias, (b.rows,) if b.batch is None else (E, b.rows), torch.float32)
-    shape = (E, a.rows, b.rows) if group == BSR_GROUP_COLUMNS else (a.rows, b.rows)
+        _check_rows("bias", bias, (b.rows,) if batch is None else (E, b.rows), torch.float32)
     if Y is None:
-        Y = torch.empty(shape, dtype=dtype, device=a._base.device)
+        Y = torch.empty(shape, dtype=dtype, device=a._q.device)
         _lend(stream, Y.device, Y)
-    elif not _is_rows(Y, shape, dtype):
+    elif Y.shape != shape or not Y.is_contiguous():
         _check_rows("Y", Y, shape, dtype)
-    lib, n = _lib or load(), ctypes.c_size_t(0)
-    status = lib.bsr_fp8_product_workspace(a._c, b._c, dt, group, E, ctypes.byref(n))
-    if status:
-        _check(status, "bsr_fp8_product_workspace")
-    ws = _workspace(n.value, Y.device, stream)
-    status = lib.bsr_fp8_product(a._c, b._c, _ptr(bias), Y.data_ptr() if Y.numel() else None, dt, group, _ptr(offsets), E, _ptr(ws),
-                                 n.value, _stream(stream))
+    lib, ac, bc, s = _lib or load(), a._c, b._c, _stream(stream)
+    ptrs = (None if bias is None else bias.data_ptr(), Y.data_ptr(), dt, group, None if offsets is None else offsets.data_ptr(), E)
+    # (most calls need no workspace: it is asked for when a call is refused for want of it)
+    status = lib.bsr_fp8_product(ac, bc, *ptrs, None, 0, s)
+    if status == BSR_ERR_CAPACITY:
+        n = ctypes.c_size_t(0)
+        _check(lib.bsr_fp8_product_workspace(ac, bc, dt, group, E, ctypes.byref(n)), "bsr_fp8_product_workspace")
+        ws = _workspace(n.value, Y.device, stream)
+        status = lib.bsr_fp8_product(ac, bc, *ptrs, ws.data_ptr(), n.value, s)
     if status:
         _check(status, "bsr_fp8_product")
     return Y
