@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         ptx::fence_barrier_init();
     }
     if (warp == kMmaWarp) tc5::alloc_pair(&tmem_s, kAllCols);
-    if (warp == 1 && ptx::elect_one()) {
+    if (warp == 1 && a.KB > 0 && ptx::elect_one()) {
         ptx::prefetch_tensormap(&a.a);
         ptx::prefetch_tensormap(&a.b);
         ptx::prefetch_tensormap(&a.ea);
