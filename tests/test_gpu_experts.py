@@ -55,6 +55,11 @@ def draw(N, D, dtype, seed=0):
     return torch.randn(N, D, device="cuda", generator=g).to(DT[dtype])
 
 
+def uniform(N, k):
+    # (a generator of its own: a capture in another test may have left the default one unusable)
+    return torch.rand(N, k, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+
+
 def make(N, k, E, align, drop):
     x = choices(N, k, E, drop)
     order = bsr.ExpertOrder(N, k, E, align)
@@ -105,7 +110,7 @@ def test_rows_and_back(N, k, E, D, align, drop, dtype):
     want[sent] = X[(source.cuda()[sent] // k).long()]
     assert torch.equal(Xs, want) and unharmed(buf)
 
-    Ys, w = draw(R, D, dtype, 1), torch.rand(N, k, device="cuda", generator=torch.Generator(device="cuda").manual_seed(3)) - 0.2
+    Ys, w = draw(R, D, dtype, 1), uniform(N, k) - 0.2
     Ys[~sent] = float("nan")   # rows that no choice has are not read
     at = place.cuda().clamp(min=0).long()
     has = (place >= 0).cuda().unsqueeze(2)
@@ -140,7 +145,7 @@ def test_rows_and_back(N, k, E, D, align, drop, dtype):
 def test_gradients_against_differences():
     N, k, E, D = 9, 2, 4, 12
     x, order, _ = make(N, k, E, 4, 0.2)
-    X, w, dY = draw(N, D, "f32"), torch.rand(N, k, device="cuda"), draw(N, D, "f32", 1)
+    X, w, dY = draw(N, D, "f32"), uniform(N, k), draw(N, D, "f32", 1)
 
     def out(X, w):   # every expert doubles its rows and adds up with the weights
         Ys = 2 * bsr.bsr_expert_rows(X, order, Xs=torch.zeros(order.rows, D, device="cuda"))
@@ -178,7 +183,7 @@ def test_rows_beyond_32_bits():
 def test_streams_and_a_captured_graph():
     N, k, E, D = 500, 2, 8, 768
     xs = [choices(N, k, E, 0.1, seed).cuda() for seed in (0, 1)]
-    X, w = draw(N, D, "bf16"), torch.rand(N, k, device="cuda")
+    X, w = draw(N, D, "bf16"), uniform(N, k)
     order, x = bsr.ExpertOrder(N, k, E, 16), xs[0].clone()
     Xs, Y = torch.zeros(order.rows, D, dtype=torch.bfloat16, device="cuda"), torch.empty_like(X)
 
