@@ -11,7 +11,14 @@
 // through distributed shared memory, become first rows.
 //
 // Rows and sums: one pass over the data, a warp to a token's 2 KB (backward: to a
-// choice's row). What bounds them: DRAM.
+// choice's row).
+//
+// What bounds them: DRAM, and the order the choices' bits (16384 tokens of 4 of 64
+// experts 8.8 us, a ballot a bit and choice, on 16 SMs). 16384 x 1024 bf16: rows of 4
+// choices 29.3 us, 168 MB at 84% of the copy rate; their sum 29.5, 84%; the sum's gradients for 2 choices
+// 31, 80%. 9920 x 1344 fp32, 2 choices: 27 us, 88%. One token: order 3.6, rows 1.5,
+// launches and a read's latency. Rows that are no multiples of 16 bytes go in smaller words
+// (8192 x 1023 bf16, 2 choices 21 us, 35%).
 #include <algorithm>
 #include <atomic>
 

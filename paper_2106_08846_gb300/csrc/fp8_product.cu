@@ -17,13 +17,20 @@
 //                  columns side by side, and four lanes store 128 bytes of a row (bf16) straight from
 //                  tensor memory; else through 2 KB of shared memory a warp
 //
-// Scaling outside the MMAs (a fresh accumulator for each step, scaled and added in
-// registers) takes every value of a step out of tensor memory: 16384 tokens of 1024
-// features into 4096 174 us. Exponents made of fp32 scales by three more warps: 102 us, a
-// step waiting for their way from the other CTA's registers; so bsr_fp8_quantize lays
-// them out as tensor memory has them. The MMAs' operands take all of shared memory's
-// bandwidth (64 bytes a cycle in, 64 out), so what the epilogue moves through it is in their
-// way: by shuffles 9000 cycles a tile of 4096 cycles of MMAs, through buffers 6900.
+// Measured at 16384 tokens of 1024 features into 4096: scaling outside the MMAs (a fresh
+// accumulator for each step, every value of it taken out, scaled and added in registers)
+// 174 us; exponents made of fp32 scales by three more warps, whose way from the other CTA's
+// registers every step waited for, 102, so bsr_fp8_quantize lays them out as tensor memory
+// has them; results by shuffles 60, through buffers 55, straight 54, and put out of L2
+// before the operands 48 to 50.
+//
+// What bounds it: 48 to 50 us there (2.75 to 2.85 PFLOP/s), the tensor pipe busy 54% of the
+// time: with eight steps to a tile, the hand-over of an accumulator (1300 of 6600
+// cycles: the commit, the shared columns' way out, the other CTA's word) and loads that
+// take up to 3200 cycles while all CTAs store, as long as the ring's six steps; shared
+// memory is at 27% of its rate, L2 at 38%. Sums of 4096 and 8192 columns: 2.65 and 2.75
+// PFLOP/s, 560 to 600 cycles a step and the last round in part empty. Few tokens: 6 to
+// 7 us, 5000 cycles until the first load, one tile's steps, and the way out.
 //
 // A step is 512 SM cycles of MMAs at 256 columns. Two accumulators of 256 columns and
 // the exponents do not fit 512 columns: the second begins at column 192, and the
@@ -36,7 +43,8 @@
 // columns into registers, 128 a thread (handed over by the other warps).
 //
 // Persistent: one CTA per SM. Runs of rows: tiles of 256 rows from a multiple of 128 on,
-// as the exponents lie, the rows of other runs left out; the table of the runs' tiles is made by every CTA from the offsets on the device.
+// as the exponents lie, the rows of other runs left out; the table of the runs' tiles is
+// made by every CTA from the offsets on the device.
 // Runs of columns: a tile's steps are the run's. Tiles of sums too few to fill the
 // GPU have them split; the parts are added in their order by a second launch.
 //

@@ -14,7 +14,10 @@
 // that both operands of a later product have the sum's axis contiguous. Blocks with
 // an infinity, which would be the largest, go through a second copy of the code.
 //
-// What bounds it: DRAM.
+// What bounds it: DRAM, and the arithmetic between a tile's loads and stores, which only
+// the other CTA of an SM overlaps. bf16, both ways: 16384 x 1024 11.6 us (68 MB, 86% of the copy
+// rate, part of it from L2), 8192 x 4096 29 (68%); by rows 16384 x 1024 8.0; fp32 both ways 8192 x 4096
+// 39.5 (76%). Rows that are not aligned are read value by value (8192 x 1023 bf16 11.4, x 1024 7.2).
 #include <algorithm>
 
 #include "elem.cuh"

@@ -213,6 +213,26 @@ def test_streams_and_a_captured_graph():
     assert torch.equal(Y, got[1]) and torch.equal(g["dweights"], got[2])
 
 
+def test_nobody_is_sent_and_invalid_orders():
+    """All choices dropped; and places and sources that are no rows, which are left out."""
+    N, k, E, D = 40, 2, 6, 64
+    X = draw(N, D, "bf16")
+    order = bsr.bsr_expert_order(torch.full((N, k), -1, dtype=torch.int32, device="cuda"), E, 16)
+    assert int(order.used) == 0 and (order.place == -1).all() and (order.source == -1).all()
+    Xs = torch.full((order.rows, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert (bsr.bsr_expert_rows(X, order, Xs=Xs) == 7).all()
+    assert (bsr.bsr_expert_sum(Xs, order, uniform(N, k)) == 0).all()
+    g = bsr.bsr_expert_sum_backward(Xs, order, uniform(N, k), X, dYs=Xs.clone())
+    assert (g["dYs"] == 7).all() and (g["dweights"] == 0).all()
+    with pytest.raises(bsr.BsrError):   # (not in place)
+        bsr.bsr_expert_sum_backward(Xs, order, uniform(N, k), X, dYs=Xs)
+    bsr.bsr_expert_order(torch.zeros(N, k, dtype=torch.int32, device="cuda"), E, 16, order=order)
+    order.place[3, 1], order.place[4, 0] = order.rows, -5
+    order.offsets[E] = 2 ** 31 - 1
+    bsr.bsr_expert_rows(X, order, Xs=Xs)
+    assert (bsr.bsr_expert_sum(Xs, order)[4] == X[4]).all()
+
+
 def test_no_tokens():
     order = bsr.bsr_expert_order(torch.empty(0, 2, dtype=torch.int32, device="cuda"), 4, 128)
     assert order.rows == 0 and order.offsets.tolist() == [0] * 5

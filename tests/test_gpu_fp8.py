@@ -193,7 +193,8 @@ def test_long_sums_of_one_sign(K, dtype):
 
 RUNS = [(1, 64, 128, [0, 1]), (300, 130, 200, [0, 0, 100, 100, 257, 300]), (1000, 1024, 768, [0, 256, 256, 768, 896]),
         (777, 2050, 513, [5, 5, 6, 300, 301, 700]), (5000, 512, 256, [0, 4000, 4001, 4128, 4999]), (64, 256, 1024, list(range(0, 65, 4))),
-        (2000, 300, 384, [0] * 20 + [1999] + [2000] * 43), (40, 1024, 2048, [0, 1, 3, 4, 5, 9, 40])]
+        (2000, 300, 384, [0] * 20 + [1999] + [2000] * 43), (40, 1024, 2048, [0, 1, 3, 4, 5, 9, 40]), (50, 64, 128, [7, 7, 7]),
+        (300, 128, 3000, [0, 129, 300])]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -322,6 +323,44 @@ def test_streams_and_a_captured_graph():
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(got, Y) and torch.equal(made, Y)
     assert bsr.bsr_check_status() == BSR_OK
+
+
+def test_two_graphs_and_a_call_that_needs_a_workspace():
+    """Sums that are split: their parts' memory is each call's own."""
+    N, M, K = 64, 1024, 4096
+    a, b = bsr.bsr_fp8_quantize(normal(N, K)), bsr.bsr_fp8_quantize(normal(M, K, seed=1), 128)
+    c, d = bsr.bsr_fp8_quantize(normal(N, K, seed=2)), bsr.bsr_fp8_quantize(normal(M, K, seed=3), 128)
+    want = [bsr.bsr_fp8_product(a, b), bsr.bsr_fp8_product(c, d)]
+    near(want[0], values(a), values(b))
+    graphs, got = [], []
+    for x, w in ((a, b), (c, d)):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got.append(bsr.bsr_fp8_product(x, w))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = bsr.bsr_fp8_product(a, d)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    near(eager, values(a), values(d))
+    assert bsr.bsr_check_status() == BSR_OK
+
+
+def test_other_devices_memory_and_the_host_are_refused():
+    a, b = bsr.bsr_fp8_quantize(normal(8, 128)), bsr.bsr_fp8_quantize(normal(8, 128))
+    with pytest.raises(bsr.BsrError):
+        bsr.bsr_fp8_product(a, b, Y=torch.empty(8, 8))
+    with pytest.raises(bsr.BsrError):
+        bsr.bsr_fp8_product(a, b, offsets=torch.tensor([0, 128], dtype=torch.int32), over="columns")
+    with pytest.raises(bsr.BsrError):
+        bsr.bsr_fp8_quantize(torch.zeros(8, 128), out=a)
+    with pytest.raises(bsr.BsrError):   # rows that do not start on 16 bytes
+        bsr.bsr_fp8_quantize(torch.zeros(8 * 128 + 1, device="cuda")[1:].view(8, 128), out=a)
 
 
 def test_beyond_32_bits():
