@@ -14,10 +14,10 @@
 // that both operands of a later product have the sum's axis contiguous. Blocks with
 // an infinity, which would be the largest, go through a second copy of the code.
 //
-// What bounds it: DRAM, and the arithmetic between a tile's loads and stores, which only
-// the other CTA of an SM overlaps. bf16, both ways: 16384 x 1024 11.6 us (68 MB, 86% of the copy
-// rate, part of it from L2), 8192 x 4096 29 (68%); by rows 16384 x 1024 8.0; fp32 both ways 8192 x 4096
-// 39.5 (76%). Rows that are not aligned are read value by value (8192 x 1023 bf16 11.4, x 1024 7.2).
+// What bounds it: DRAM. bf16, both ways: 16384 x 1024 10.3 us (68 MB, 97% of the copy rate,
+// part of it from L2), 8192 x 4096 22.8 (88%); by rows 16384 x 1024 6.0; fp32 both ways
+// 8192 x 4096 36.7 (82%). Rows that are not aligned are read value by value (8192 x 1023
+// bf16 10.6, x 1024 6.5).
 #include <algorithm>
 
 #include "elem.cuh"
@@ -63,9 +63,6 @@ __device__ __forceinline__ uint32_t round2(float y0, float y1) {
     else asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(y1), "f"(y0));
     return r;
 }
-// Infinities become NaN; all else stays.
-__device__ __forceinline__ float no_inf(float y) { return fmaf(y, 0.f, y); }
-
 // Eight values of a row: bf16 in pairs, fp32 one by one. Sizes: of pairs or values,
 // a maximum with a NaN is the other operand.
 template <typename T>
@@ -93,13 +90,14 @@ struct Row<uint16_t> {
         asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
-    // the size of word j; ODD: 0 for infinities
-    template <bool ODD>
     __device__ __forceinline__ uint32_t size(int j) const {
         uint32_t a;
         asm("abs.bf16x2 %0, %1;" : "=r"(a) : "r"(w[j]));
-        if (ODD) a &= ((a & 0xffffu) == 0x7f80u ? 0xffff0000u : ~0u) & (a >> 16 == 0x7f80u ? 0xffffu : ~0u);
         return a;
+    }
+    __device__ __forceinline__ void no_infinities() {   // (they become NaN)
+#pragma unroll
+        for (int j = 0; j < words; j++) w[j] |= ((w[j] & 0x7fffu) == 0x7f80u ? 0x7fffu : 0) | ((w[j] & 0x7fff0000u) == 0x7f800000u ? 0x7fff0000u : 0);
     }
     // the bits, as fp32, of the larger value of a pair of sizes; a NaN is no size
     static __device__ __forceinline__ uint32_t top(uint32_t a) {
@@ -131,10 +129,11 @@ struct Row<float> {
         }
     }
     static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
-    template <bool ODD>
-    __device__ __forceinline__ uint32_t size(int j) const {
-        const uint32_t a = __float_as_uint(w[j]) & 0x7fffffffu;
-        return ODD && a == 0x7f800000u ? 0 : a;
+    __device__ __forceinline__ uint32_t size(int j) const { return __float_as_uint(w[j]) & 0x7fffffffu; }
+    __device__ __forceinline__ void no_infinities() {
+#pragma unroll
+        for (int j = 0; j < words; j++)
+            if (size(j) == 0x7f800000u) w[j] = __uint_as_float(0x7fffffffu);
     }
     static __device__ __forceinline__ uint32_t top(uint32_t a) { return a > 0x7f800000u ? 0 : a; }
     static __device__ __forceinline__ uint32_t low(uint32_t a) { return top(a); }
@@ -147,13 +146,13 @@ struct Place {
 };
 
 // The largest sizes of a thread's eight rows, as words of two columns' or one's.
-template <typename T, bool ODD>
+template <typename T>
 __device__ __forceinline__ void row_tops(const Row<T> (&x)[8], uint32_t (&t)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-        t[i] = x[i].template size<ODD>(0);
+        t[i] = x[i].size(0);
 #pragma unroll
-        for (int j = 1; j < Row<T>::words; j++) t[i] = Row<T>::larger(t[i], x[i].template size<ODD>(j));
+        for (int j = 1; j < Row<T>::words; j++) t[i] = Row<T>::larger(t[i], x[i].size(j));
     }
 }
 
@@ -171,14 +170,12 @@ __device__ __forceinline__ void halve(uint32_t (&w)[n], int m, int lane) {
 
 // What is left when the values and the rows' largest sizes are in registers: 256 threads,
 // warp w, half h of it, lane l of the half: rows 16 w + 8 h + i, columns 8 l + j.
-template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS, bool ODD>
+template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS>
 __device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const Row<T> (&x)[8], uint32_t (&t)[8],
                                          uint32_t (&tops)[8][kFp8Block], unsigned char *turned) {
     using X = Row<T>;
     constexpr int words = X::words, each = X::each;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = lane >> 4, l = lane & 15;
-    auto half = [](float y) { return ODD ? no_inf(y) : y; };
-    if (ODD) row_tops<T, true>(x, t);
     int tile_e = 0;
     if constexpr (TILE) {
         uint32_t top = t[0];
@@ -256,9 +253,9 @@ __device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const 
             for (int j = 0; j < 4; j++) {
                 if constexpr (each == 2) {
                     const float2 y = x[i].scaled(j, g);
-                    b[j] = round2<E5M2>(half(y.x), half(y.y));
+                    b[j] = round2<E5M2>(y.x, y.y);
                 } else {
-                    b[j] = round2<E5M2>(half(x[i].scaled(2 * j, g)), half(x[i].scaled(2 * j + 1, g)));
+                    b[j] = round2<E5M2>(x[i].scaled(2 * j, g), x[i].scaled(2 * j + 1, g));
                 }
             }
             if (i < rows) *reinterpret_cast<uint2 *>(q) = make_uint2(b[0] | b[1] << 16, b[2] | b[3] << 16);
@@ -269,9 +266,9 @@ __device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const 
         if constexpr (!TILE) {
 #pragma unroll
             for (int j = 0; j < words; j++) {
-                uint32_t top = x[0].template size<ODD>(j);
+                uint32_t top = x[0].size(j);
 #pragma unroll
-                for (int i = 1; i < 8; i++) top = X::larger(top, x[i].template size<ODD>(j));
+                for (int i = 1; i < 8; i++) top = X::larger(top, x[i].size(j));
                 top = X::larger(top, __shfl_xor_sync(0xffffffffu, top, 16));
                 if (h == 0) tops[warp][words * l + j] = top;
             }
@@ -307,10 +304,10 @@ __device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const 
             for (int i = 0; i < 8; i += 2) {
                 if constexpr (each == 2) {
                     const float2 y = x[i].scaled(j, f), z = x[i + 1].scaled(j, f);
-                    b[0][i / 2] = round2<E5M2>(half(y.x), half(z.x));
-                    b[each - 1][i / 2] = round2<E5M2>(half(y.y), half(z.y));
+                    b[0][i / 2] = round2<E5M2>(y.x, z.x);
+                    b[each - 1][i / 2] = round2<E5M2>(y.y, z.y);
                 } else {
-                    b[0][i / 2] = round2<E5M2>(half(x[i].scaled(j, f)), half(x[i + 1].scaled(j, f)));
+                    b[0][i / 2] = round2<E5M2>(x[i].scaled(j, f), x[i + 1].scaled(j, f));
                 }
             }
 #pragma unroll
@@ -332,9 +329,10 @@ __device__ __forceinline__ void quantize(const QArgs &a, const Place &at, const 
     }
 }
 
-// (three CTAs an SM, of 80 registers: 8192 x 4096 bf16 both ways 30.8 us, two 28.4; 16384 x 1024 15.2 and 11.6)
+// (CTAs an SM, registers a thread: bf16 both ways 8192 x 4096 four, 64: 22.8 us, three 24.8, two 29; fp32 two, 128: 36.7,
+// three 40.4)
 template <typename T, bool E5M2, bool TILE, bool ROWS, bool COLUMNS>
-__global__ void __launch_bounds__(256, 2) k_fp8_quantize(const __grid_constant__ QArgs a) {
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 2) k_fp8_quantize(const __grid_constant__ QArgs a) {
     using X = Row<T>;
     __shared__ uint32_t tops[8][kFp8Block];
     __shared__ __align__(16) unsigned char turned[COLUMNS ? kFp8Block * kFp8Block : 16];
@@ -359,12 +357,16 @@ __global__ void __launch_bounds__(256, 2) k_fp8_quantize(const __grid_constant__
         for (int i = 0; i < 8; i++) x[i].load(from + i * a.C, at.row0 + i < at.R ? n : 0, a.align);
     }
     uint32_t t[8];
-    row_tops<T, false>(x, t);
+    row_tops(x, t);
     uint32_t top = t[0];
 #pragma unroll
     for (int i = 1; i < 8; i++) top = X::larger(top, t[i]);
-    if (__syncthreads_or(X::top(top) == 0x7f800000u)) quantize<T, E5M2, TILE, ROWS, COLUMNS, true>(a, at, x, t, tops, turned);
-    else quantize<T, E5M2, TILE, ROWS, COLUMNS, false>(a, at, x, t, tops, turned);
+    if (__syncthreads_or(X::top(top) == 0x7f800000u)) {   // (an infinity would be the largest)
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[i].no_infinities();
+        row_tops(x, t);
+    }
+    quantize<T, E5M2, TILE, ROWS, COLUMNS>(a, at, x, t, tops, turned);
 }
 
 template <typename T, bool E5M2, bool TILE>
