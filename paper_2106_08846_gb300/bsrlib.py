@@ -820,7 +820,7 @@ class Fp8Matrix:
     q[r, c] * scale[c // 128, r // tile]. `q` has cols rounded up to 128, zeros past
     them; `exponent` is what the product reads of the scales, powers of two (include/bsr.h). fmt: "e4m3" or "e5m2"; bsr_fp8_quantize fills it in."""
 
-    __slots__ = ("rows", "cols", "tile", "fmt", "batch", "_q", "_base", "_first", "_scale", "_c", "__weakref__")
+    __slots__ = ("rows", "cols", "tile", "fmt", "batch", "_base", "_q", "_scale", "_c", "__weakref__")
 
     def __init__(self, rows: int, cols: int, tile: int = 1, fmt: str = "e4m3", batch: Optional[int] = None, device="cuda"):
         code = _FP8.get(fmt)
@@ -828,36 +828,41 @@ class Fp8Matrix:
             raise ValueError("fmt is 'e4m3' or 'e5m2', tile 1 or 128")
         self.rows, self.cols, self.tile, self.fmt, self.batch = rows, cols, tile, fmt, batch
         blocks, runs, n = (cols + 127) // 128, rows if tile == 1 else (rows + 127) // 128, 1 if batch is None else batch
-        # the scales, and before them as many rows as the exponents take (a tensor less, and a view only for who reads scales)
-        first = -(-n * ((blocks + 3) // 4) * ((rows + 127) // 128) * 128 // runs) if runs else 0
-        self._q = torch.empty((rows, blocks * 128) if batch is None else (batch, rows, blocks * 128), dtype=_FP8_TYPE[fmt], device=device)
-        self._base = torch.empty((first + n * blocks, runs), dtype=torch.float32, device=device)
-        self._first, self._scale = first, None
-        if n and rows and cols:
-            at = self._base.data_ptr()
-            self._c = _Fp8Matrix(n, rows, cols, tile, code, self._q.data_ptr(), at, at + 4 * first * runs)
-        else:
-            self._c = _Fp8Matrix(n, rows, cols, tile, code, None, None, None)
+        # One allocation, of the values, the exponents and the scales, in words (a tensor for each takes the
+        # host 3 us more, with their release); views of it are made when they are asked for.
+        values, exponents = n * rows * blocks * 32, n * ((blocks + 3) // 4) * ((rows + 127) // 128) * 128
+        self._base = torch.empty(values + exponents + n * blocks * runs, dtype=torch.float32, device=device)
+        self._q = self._scale = None
+        at = self._base.data_ptr() if values else 0
+        self._c = _Fp8Matrix(n, rows, cols, tile, code, at, at and at + 4 * values, at and at + 4 * (values + exponents))
 
     # (to be filled, not replaced: the calls have their addresses)
     @property
     def q(self) -> torch.Tensor:
+        if self._q is None:
+            r, c = self.rows, (self.cols + 127) // 128 * 128
+            flat = self._base.view(_FP8_TYPE[self.fmt])
+            self._q = flat.as_strided((r, c), (c, 1)) if self.batch is None else flat.as_strided((self.batch, r, c), (r * c, c, 1))
         return self._q
 
     @property
     def scale(self) -> torch.Tensor:
         if self._scale is None:
-            scale = self._base[self._first:]
-            self._scale = scale if self.batch is None else scale.view(self.batch, -1, scale.shape[1])
+            flat, b = self._base, (self.cols + 127) // 128
+            r = self.rows if self.tile == 1 else (self.rows + 127) // 128
+            if self.batch is None:
+                self._scale = flat.as_strided((b, r), (r, 1), flat.shape[0] - b * r)
+            else:
+                self._scale = flat.as_strided((self.batch, b, r), (b * r, r, 1), flat.shape[0] - self.batch * b * r)
         return self._scale
 
     @property
     def exponent(self) -> torch.Tensor:
-        shape = ((self.cols + 511) // 512, (self.rows + 127) // 128, 512)
-        if self.batch is not None:
-            shape = (self.batch, *shape)
-        words = 128 * self._c.batch * ((self.cols + 511) // 512) * ((self.rows + 127) // 128)
-        return self._base.view(-1)[:words].view(torch.uint8).view(shape)
+        w, r = (self.cols + 511) // 512, (self.rows + 127) // 128
+        flat, first = self._base.view(torch.uint8), self._c.batch * self.rows * ((self.cols + 127) // 128) * 128
+        if self.batch is None:
+            return flat.as_strided((w, r, 512), (r * 512, 512, 1), first)
+        return flat.as_strided((self.batch, w, r, 512), (w * r * 512, r * 512, 512, 1), first)
 
 
 def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: str = "rows", used: Optional[torch.Tensor] = None,
@@ -893,7 +898,7 @@ def bsr_fp8_quantize(x: torch.Tensor, tile: int = 1, fmt: str = "e4m3", form: st
             columns = Fp8Matrix(C, R, tile, fmt, batch, device)
         out = rows if columns is None else columns if rows is None else (rows, columns)
         if stream is not None:
-            _lend(stream, device, *[t for m in (rows, columns) if m is not None for t in (m._q, m._base)])
+            _lend(stream, device, *[m._base for m in (rows, columns) if m is not None])
     else:
         rows, columns = (out, None) if form == "rows" else (None, out) if form == "columns" else out
         for m, size in ((rows, (R, C)), (columns, (C, R))):
@@ -934,7 +939,7 @@ def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = N
     if bias is not None:
         _check_rows("bias", bias, (b.rows,) if batch is None else (E, b.rows), torch.float32)
     if Y is None:
-        Y = torch.empty(shape, dtype=dtype, device=a._q.device)
+        Y = torch.empty(shape, dtype=dtype, device=a._base.device)
         _lend(stream, Y.device, Y)
     elif Y.shape != shape or not Y.is_contiguous():
         _check_rows("Y", Y, shape, dtype)
