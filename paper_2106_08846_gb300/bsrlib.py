@@ -733,15 +733,16 @@ def bsr_expert_order(experts: torch.Tensor, E: int, align: int = 1, order: Optio
     """The order of the tokens' choices `experts` [N, k] (int32; a value outside
     0 .. E - 1 is a dropped choice), each expert's rows from a multiple of `align` on.
     Fills `order` if given. Nothing is read back to the host."""
-    if experts.dim() != 2:
+    shape = experts.shape
+    if len(shape) != 2:
         raise ValueError("experts must be [N, k]")
-    N, k = experts.shape
-    if not _is_rows(experts, experts.shape, torch.int32):
-        _check_rows("experts", experts, experts.shape, torch.int32)
+    N, k = shape
+    if experts.dtype is not torch.int32 or not experts.is_contiguous():
+        _check_rows("experts", experts, shape, torch.int32)
     if order is None:
         order = ExpertOrder(N, k, E, align, experts.device)
         _lend(stream, experts.device, order.offsets, order.place, order.source)
-    elif (order.N, order.k, order.E, order.align) != (N, k, E, align):
+    elif order.N != N or order.k != k or order.E != E or order.align != align:
         raise ValueError("order is of other sizes")
     status = _lib.bsr_expert_order(order._c, experts.data_ptr(), _stream(stream))
     if status:
@@ -749,21 +750,33 @@ def bsr_expert_order(experts: torch.Tensor, E: int, align: int = 1, order: Optio
     return order
 
 
-def _check_sorted(order: ExpertOrder, **tensors) -> None:
-    """Tensors of one type, each (rows, tensor or None) and of as many features."""
-    given = [(name, n, t) for name, (n, t) in tensors.items() if t is not None]
-    shape, dt = given[0][2].shape, given[0][2].dtype
+def _check_sorted(of: str, t: torch.Tensor, rows: int, *others) -> Tuple[int, int]:
+    """The features and the type of t, which must have `rows` rows, and the checks of others
+    (name, tensor or None, shape's rows), of as many features and its type."""
+    shape, dtype = t.shape, t.dtype
     if len(shape) != 2:
-        raise ValueError(f"{given[0][0]} must be [{given[0][1]}, D]")
-    for name, n, t in given:
-        if not _is_rows(t, (n, shape[1]), dt):
-            _check_rows(name, t, (n, shape[1]), dt)
+        raise ValueError(f"{of} must be [{rows}, D]")
+    if shape[0] != rows or not t.is_contiguous():
+        _check_rows(of, t, (rows, shape[1]), dtype)
+    for name, o, n in others:
+        if o is not None and not _is_rows(o, (n, shape[1]), dtype):
+            _check_rows(name, o, (n, shape[1]), dtype)
+    dt = _DT.get(dtype)
+    return shape[1], dtype_code(dtype) if dt is None else dt   # (dtype_code raises)
 
 
-def _made(t: Optional[torch.Tensor], rows: int, like: torch.Tensor, stream) -> torch.Tensor:
-    if t is None:
-        t = torch.empty((rows, like.shape[1]), dtype=like.dtype, device=like.device)
-        _lend(stream, like.device, t)
+def _check_weights(order: ExpertOrder, weights: Optional[torch.Tensor]) -> Optional[int]:
+    if weights is None:
+        return None
+    shape = (order.N, order.k)
+    if not _is_rows(weights, shape, torch.float32):
+        _check_rows("weights", weights, shape, torch.float32)
+    return weights.data_ptr()
+
+
+def _made(rows: int, like: torch.Tensor, stream) -> torch.Tensor:
+    t = torch.empty((rows, like.shape[1]), dtype=like.dtype, device=like.device)
+    _lend(stream, like.device, t)
     return t
 
 
@@ -771,10 +784,10 @@ def bsr_expert_rows(X: torch.Tensor, order: ExpertOrder, Xs: Optional[torch.Tens
     """Xs [order.rows, D]: the tokens' rows X [N, D] in the experts' order, zeros behind
     an expert's last one; rows from order.used on are left as they were (of an Xs
     that the call makes: without a value). Its gradient is bsr_expert_sum without weights."""
-    _check_sorted(order, X=(order.N, X), Xs=(order.rows, Xs))
-    dt = dtype_code(X.dtype)
-    Xs = _made(Xs, order.rows, X, stream)
-    status = _lib.bsr_expert_rows(order._c, X.data_ptr(), Xs.data_ptr(), X.shape[1], dt, _stream(stream))
+    D, dt = _check_sorted("X", X, order.N, ("Xs", Xs, order.rows))
+    if Xs is None:
+        Xs = _made(order.rows, X, stream)
+    status = _lib.bsr_expert_rows(order._c, X.data_ptr(), Xs.data_ptr(), D, dt, _stream(stream))
     if status:
         _check(status, "bsr_expert_rows")
     return Xs
@@ -784,11 +797,11 @@ def bsr_expert_sum(Ys: torch.Tensor, order: ExpertOrder, weights: Optional[torch
                    stream=None) -> torch.Tensor:
     """Y [N, D]: for each token the sum of its choices' rows of Ys [order.rows, D], with
     the router's weights (fp32 [N, k], None: 1)."""
-    _check_sorted(order, Ys=(order.rows, Ys), Y=(order.N, Y))
-    dt = dtype_code(Ys.dtype)
-    _check_rows("weights", weights, (order.N, order.k), torch.float32)
-    Y = _made(Y, order.N, Ys, stream)
-    status = _lib.bsr_expert_sum(order._c, Ys.data_ptr(), _ptr(weights), Y.data_ptr(), Ys.shape[1], dt, _stream(stream))
+    D, dt = _check_sorted("Ys", Ys, order.rows, ("Y", Y, order.N))
+    w = _check_weights(order, weights)
+    if Y is None:
+        Y = _made(order.N, Ys, stream)
+    status = _lib.bsr_expert_sum(order._c, Ys.data_ptr(), w, Y.data_ptr(), D, dt, _stream(stream))
     if status:
         _check(status, "bsr_expert_sum")
     return Y
@@ -798,17 +811,16 @@ def bsr_expert_sum_backward(Ys: Optional[torch.Tensor], order: ExpertOrder, weig
                             dYs: Optional[torch.Tensor] = None, stream=None) -> dict:
     """Gradients of bsr_expert_sum: "dYs" (rows from order.used on as in bsr_expert_rows),
     and "dweights" where weights are given; without them Ys is not needed."""
-    _check_sorted(order, dY=(order.N, dY), Ys=(order.rows, Ys), dYs=(order.rows, dYs))
-    dt = dtype_code(dY.dtype)
-    _check_rows("weights", weights, (order.N, order.k), torch.float32)
-    if weights is not None and Ys is None:
+    D, dt = _check_sorted("dY", dY, order.N, ("Ys", Ys, order.rows), ("dYs", dYs, order.rows))
+    w = _check_weights(order, weights)
+    if w is not None and Ys is None:
         raise ValueError("the gradient of the weights needs Ys")
-    out = {"dYs": _made(dYs, order.rows, dY, stream)}
-    if weights is not None:
+    out = {"dYs": _made(order.rows, dY, stream) if dYs is None else dYs}
+    if w is not None:
         out["dweights"] = torch.empty_like(weights)
         _lend(stream, dY.device, out["dweights"])
-    status = _lib.bsr_expert_sum_backward(order._c, _ptr(Ys), _ptr(weights), dY.data_ptr(), out["dYs"].data_ptr(),
-                                          _ptr(out.get("dweights")), dY.shape[1], dt, _stream(stream))
+    status = _lib.bsr_expert_sum_backward(order._c, _ptr(Ys), w, dY.data_ptr(), out["dYs"].data_ptr(), _ptr(out.get("dweights")), D, dt,
+                                          _stream(stream))
     if status:
         _check(status, "bsr_expert_sum_backward")
     return out
