@@ -15,10 +15,13 @@
 //
 // What bounds them: DRAM, and the order the choices' bits (16384 tokens of 4 of 64
 // experts 8.8 us, a ballot a bit and choice, on 16 SMs). 16384 x 1024 bf16: rows of 4
-// choices 29.3 us, 168 MB at 84% of the copy rate; their sum 29.5, 84%; the sum's gradients for 2 choices
-// 31, 80%. 9920 x 1344 fp32, 2 choices: 27 us, 88%. One token: order 3.6, rows 1.5,
+// choices 29.3 us, 168 MB at 84% of the copy rate; their sum 30, 83%; the sum's gradients for 2 choices
+// 31, 80%. 9920 x 1344 fp32, 2 choices: 30 us, 79%, bf16 12.4, 95%. One token: order 3.6, rows 1.5,
 // launches and a read's latency. Rows that are no multiples of 16 bytes go in smaller words
-// (8192 x 1023 bf16, 2 choices 21 us, 35%).
+// (8192 x 1023 bf16, 2 choices: order and rows 16, their sum 15 us, 48%).
+//
+// Inputs are read by plain loads, none by the read-only path: a kernel starts while the
+// one before it, whose output they may be, still runs.
 #include <algorithm>
 #include <atomic>
 
@@ -74,7 +77,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_
 #pragma unroll
         for (int t = 0; t < kAtOnce; t++) {
             const int64_t i = i0 + 32 * t + lane;
-            const int32_t v = i < hi ? __ldg(experts + i) : -1;
+            const int32_t v = i < hi ? experts[i] : -1;
             x[t] = (uint32_t)v < (uint32_t)E ? v : -1;
         }
     };
@@ -175,10 +178,29 @@ struct Word {
     };
 };
 
-constexpr int kWords = 4;   // of a row, a lane holds at once
+// w = *p where `on` (else w has no value), without a branch: with one, the compiler puts each load where it
+// is used, one behind the other (16384 x 1024 bf16, 4 choices: 42 us for 29.5).
+__device__ __forceinline__ void load_if(uint4 &w, const uint4 *p, bool on) {
+    asm volatile("{\n.reg .pred on;\nsetp.ne.u32 on, %5, 0;\n@on ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n}"
+                 : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+__device__ __forceinline__ void load_if(uint2 &w, const uint2 *p, bool on) {
+    asm volatile("{\n.reg .pred on;\nsetp.ne.u32 on, %3, 0;\n@on ld.global.v2.u32 {%0, %1}, [%2];\n}"
+                 : "=r"(w.x), "=r"(w.y) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+__device__ __forceinline__ void load_if(uint32_t &w, const uint32_t *p, bool on) {
+    asm volatile("{\n.reg .pred on;\nsetp.ne.u32 on, %2, 0;\n@on ld.global.u32 %0, [%1];\n}" : "=r"(w) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+__device__ __forceinline__ void load_if(uint16_t &w, const uint16_t *p, bool on) {
+    asm volatile("{\n.reg .pred on;\nsetp.ne.u32 on, %2, 0;\n@on ld.global.u16 %0, [%1];\n}" : "=h"(w) : "l"(p), "r"((uint32_t)on) : "memory");
+}
+
+// Of a row, a lane holds at once (words of 2 bytes, 8192 x 1023 bf16 of one choice: four 17.9 us, eight 13.7).
+template <typename W>
+constexpr int kWords = sizeof(W) == 16 ? 4 : 8;
 
 __device__ __forceinline__ int32_t row_of(const bsr_experts_t &p, int64_t pair) {
-    const int32_t r = __ldg(p.place + pair);
+    const int32_t r = p.place[pair];
     return r >= 0 && r < p.R ? r : -1;   // (rows out of range: not sent)
 }
 
@@ -188,14 +210,14 @@ constexpr int kZeroRows = 8;
 template <typename W>
 __device__ __forceinline__ void zero_rows(const bsr_experts_t &p, W *out, int64_t words, int64_t u, int64_t parts) {
     const int lane = threadIdx.x & 31;
-    const int64_t first = u / parts * kZeroRows, at = u % parts * 32 * kWords + lane;
-    const int64_t used = min((int64_t)__ldg(p.offsets + p.E), p.R), r = first + lane;
-    uint32_t mask = __ballot_sync(0xffffffffu, lane < kZeroRows && r < used && __ldg(p.source + r) < 0);
+    const int64_t first = u / parts * kZeroRows, at = u % parts * 32 * kWords<W> + lane;
+    const int64_t used = min((int64_t)p.offsets[p.E], p.R), r = first + lane;
+    uint32_t mask = __ballot_sync(0xffffffffu, lane < kZeroRows && r < used && p.source[r] < 0);
     while (mask) {
         W *row = out + (first + __ffs((int)mask) - 1) * words + at;
         mask &= mask - 1;
 #pragma unroll
-        for (int v = 0; v < kWords; v++)
+        for (int v = 0; v < kWords<W>; v++)
             if (at + 32 * v < words) row[32 * v] = W{};
     }
 }
@@ -212,25 +234,29 @@ __global__ void __launch_bounds__(256) k_expert_rows(const __grid_constant__ bsr
             zero_rows(p, Xs, words, u - copies, parts);
             continue;
         }
-        const int64_t n = u / parts, at = (u - n * parts) * 32 * kWords + lane;
-        W x[kWords];
+        const int64_t n = u / parts, at = (u - n * parts) * 32 * kWords<W> + lane;
+        W x[kWords<W>];
 #pragma unroll
-        for (int v = 0; v < kWords; v++)
-            if (at + 32 * v < words) x[v] = __ldg(X + n * words + at + 32 * v);
+        for (int v = 0; v < kWords<W>; v++)
+            if (at + 32 * v < words) x[v] = X[n * words + at + 32 * v];
+        int32_t row = -1;
         for (int j = 0; j < p.k; j++) {
-            const int64_t r = row_of(p, n * p.k + j);
+            if (j % 32 == 0) row = j + lane < p.k ? row_of(p, n * p.k + j + lane) : -1;
+            const int64_t r = __shfl_sync(0xffffffffu, row, j % 32);
             if (r < 0) continue;
 #pragma unroll
-            for (int v = 0; v < kWords; v++)
+            for (int v = 0; v < kWords<W>; v++)
                 if (at + 32 * v < words) Xs[r * words + at + 32 * v] = x[v];
         }
     }
 }
 
-// ROWS: choices whose rows are on their way at once; WORDS of each a lane. (With four words of
-// four rows for all, 9920 rows of 1344 fp32 features of one choice 28 us, 53% of the copy rate.)
+// ROWS: choices whose rows are on their way at once; WORDS of each a lane: eight of one choice, 32 bytes of
+// two, four words of four. (Four of four for all: 9920 rows of 1344 fp32 features of one choice 28 us for 20; four of
+// two choices: bf16 15 for 12.4, fp32 31.6 for 29.9; four words of 2 bytes, 8192 x 1023: 19.8 for 15.4.
+// Two CTAs an SM: 128 registers, or one of 140.)
 template <typename T, typename W, int WORDS, int ROWS>
-__global__ void __launch_bounds__(256) k_expert_sum(const __grid_constant__ bsr_experts_t p, const W *Ys, const float *weights, W *Y,
+__global__ void __launch_bounds__(256, 2) k_expert_sum(const __grid_constant__ bsr_experts_t p, const W *Ys, const float *weights, W *Y,
                                                     int64_t words, int64_t parts) {
     constexpr int n_w = Word<T, W>::n;
     const int lane = threadIdx.x & 31;
@@ -243,22 +269,27 @@ __global__ void __launch_bounds__(256) k_expert_sum(const __grid_constant__ bsr_
         for (int j0 = 0; j0 < p.k; j0 += ROWS) {
             Word<T, W> y[ROWS][WORDS];
             int64_t r[ROWS];
+            float w[ROWS];
 #pragma unroll
-            for (int j = 0; j < ROWS; j++) r[j] = j0 + j < p.k ? row_of(p, n * p.k + j0 + j) : -1;
+            for (int j = 0; j < ROWS; j++) {
+                const int64_t pair = n * p.k + min(j0 + j, p.k - 1);
+                const int32_t row = row_of(p, pair);
+                r[j] = j0 + j < p.k ? row : -1;
+                w[j] = weights ? weights[pair] : 1.f;
+            }
 #pragma unroll
             for (int j = 0; j < ROWS; j++)
 #pragma unroll
                 for (int v = 0; v < WORDS; v++)
-                    if (r[j] >= 0 && at + 32 * v < words) y[j][v].w = __ldg(Ys + r[j] * words + at + 32 * v);
+                    load_if(y[j][v].w, Ys + r[j] * words + at + 32 * v, r[j] >= 0 && at + 32 * v < words);
 #pragma unroll
             for (int j = 0; j < ROWS; j++) {
                 if (r[j] < 0) continue;
-                const float w = weights ? __ldg(weights + n * p.k + j0 + j) : 1.f;
 #pragma unroll
                 for (int v = 0; v < WORDS; v++)
                     if (at + 32 * v < words) {
 #pragma unroll
-                        for (int i = 0; i < n_w; i++) sum[v][i] = fmaf(w, to_f32(y[j][v].v[i]), sum[v][i]);
+                        for (int i = 0; i < n_w; i++) sum[v][i] = fmaf(w[j], to_f32(y[j][v].v[i]), sum[v][i]);
                     }
             }
         }
@@ -293,18 +324,18 @@ __global__ void __launch_bounds__(256) k_expert_sum_backward(const __grid_consta
             if (dweights && lane == 0) dweights[u] = 0.f;
             continue;
         }
-        const float w = __ldg(weights + u);
+        const float w = weights[u];
         float dot = 0.f;
-        for (int64_t at = lane; at < words; at += 32 * kWords) {
-            Word<T, W> d[kWords], y[kWords];
+        for (int64_t at = lane; at < words; at += 32 * kWords<W>) {
+            Word<T, W> d[kWords<W>], y[kWords<W>];
 #pragma unroll
-            for (int v = 0; v < kWords; v++) {
+            for (int v = 0; v < kWords<W>; v++) {
                 if (at + 32 * v >= words) break;
-                d[v].w = __ldg(dY + n * words + at + 32 * v);
-                if (dweights) y[v].w = __ldg(Ys + r * words + at + 32 * v);
+                d[v].w = dY[n * words + at + 32 * v];
+                if (dweights) y[v].w = Ys[r * words + at + 32 * v];
             }
 #pragma unroll
-            for (int v = 0; v < kWords; v++) {
+            for (int v = 0; v < kWords<W>; v++) {
                 if (at + 32 * v >= words) break;
                 Word<T, W> o;
 #pragma unroll
@@ -362,7 +393,7 @@ cudaError_t launch_expert_order(const bsr_experts_t &p, const int32_t *experts, 
 cudaError_t launch_expert_rows(const bsr_experts_t &p, const void *X, void *Xs, int64_t D, bsr_dtype_t dt, cudaStream_t s) {
     return by_word(D, dt, [&](auto t, auto w) {
         using W = decltype(w);
-        const int64_t words = D * (int64_t)sizeof(t) / (int64_t)sizeof(W), parts = (words + 32 * kWords - 1) / (32 * kWords);
+        const int64_t words = D * (int64_t)sizeof(t) / (int64_t)sizeof(W), parts = (words + 32 * kWords<W> - 1) / (32 * kWords<W>);
         return launch_kernel(k_expert_rows<W>, dim3(grid_of((p.N + (p.R + kZeroRows - 1) / kZeroRows) * parts)), dim3(256), 0, s, p,
                              static_cast<const W *>(X), static_cast<W *>(Xs), words, parts);
     });
@@ -379,7 +410,8 @@ cudaError_t launch_expert_sum(const bsr_experts_t &p, const void *Ys, const floa
             return launch_kernel(kernel, dim3(grid_of(p.N * parts)), dim3(256), 0, s, p, static_cast<const W *>(Ys), weights, static_cast<W *>(Y),
                                  words, parts);
         };
-        return p.k == 1 ? run(k_expert_sum<T, W, 8, 1>, 8) : p.k == 2 ? run(k_expert_sum<T, W, 4, 2>, 4) : run(k_expert_sum<T, W, 4, 4>, 4);
+        constexpr int two = sizeof(W) >= 4 ? 32 / (int)sizeof(W) : 8;
+        return p.k == 1 ? run(k_expert_sum<T, W, 8, 1>, 8) : p.k == 2 ? run(k_expert_sum<T, W, two, 2>, two) : run(k_expert_sum<T, W, 4, 4>, 4);
     });
 }
 
@@ -388,7 +420,7 @@ cudaError_t launch_expert_sum_backward(const bsr_experts_t &p, const void *Ys, c
     return by_word(D, dt, [&](auto t, auto w) {
         using T = decltype(t);
         using W = decltype(w);
-        const int64_t words = D * (int64_t)sizeof(T) / (int64_t)sizeof(W), parts = (words + 32 * kWords - 1) / (32 * kWords);
+        const int64_t words = D * (int64_t)sizeof(T) / (int64_t)sizeof(W), parts = (words + 32 * kWords<W> - 1) / (32 * kWords<W>);
         const int64_t units = p.N * p.k + (dYs ? (p.R + kZeroRows - 1) / kZeroRows * parts : 0);
         return launch_kernel(k_expert_sum_backward<T, W>, dim3(grid_of(units)), dim3(256), 0, s, p, static_cast<const W *>(Ys), weights,
                              static_cast<const W *>(dY), static_cast<W *>(dYs), dweights, words, parts);

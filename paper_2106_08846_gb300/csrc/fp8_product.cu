@@ -236,7 +236,7 @@ __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64
         const float *bias = a.bias + (int64_t)un.batch * a.M + c;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
-            const float b0 = __ldg(bias + 2 * i), b1 = __ldg(bias + 2 * i + 1);
+            const float b0 = bias[2 * i], b1 = bias[2 * i + 1];
             x[4 * i] += b0, x[4 * i + 1] += b1, x[4 * i + 2] += b0, x[4 * i + 3] += b1;
         }
     }
@@ -269,7 +269,7 @@ __device__ __forceinline__ void put(const Args &a, const Unit &un, int64_t row, 
     if (a.bias && !part) {
         const float *bias = a.bias + (int64_t)un.batch * a.M + c;
 #pragma unroll
-        for (int j = 0; j < 32; j++) x[j] += c + j < a.M ? __ldg(bias + j) : 0.f;
+        for (int j = 0; j < 32; j++) x[j] += c + j < a.M ? bias[j] : 0.f;
     }
     if (sizeof(T) == 2 && !part) {
 #pragma unroll
@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
         // within what there is, in steps for columns
         const bool by_rows = a.group == BSR_GROUP_ROWS;
         for (int e = threadIdx.x; e <= a.E; e += kThreads) {
-            const int64_t o = max(0, __ldg(a.offsets + e));
+            const int64_t o = max(0, a.offsets[e]);
             runs.at[e] = (int32_t)(by_rows ? min(o, a.rows) : min(o / kFp8Block, a.KB));
         }
         __syncthreads();
@@ -729,7 +729,7 @@ __global__ void __launch_bounds__(256) k_fp8_join(const __grid_constant__ Args a
     T *out = static_cast<T *>(a.Y) + row * a.M + c;
 #pragma unroll
     for (int j = 0; j < 4; j++)
-        if (c + j < a.M) out[j] = from_f32<T>(f[j] + (a.bias ? __ldg(a.bias + c + j) : 0.f));
+        if (c + j < a.M) out[j] = from_f32<T>(f[j] + (a.bias ? a.bias[c + j] : 0.f));
 }
 
 int pairs_of_sms() {
