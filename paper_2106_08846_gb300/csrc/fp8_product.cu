@@ -225,14 +225,15 @@ __device__ __forceinline__ uint4 *turned(unsigned char *buf, int row, int chunk)
 // 16 rows of the result from `row` on x 64 columns from c on, of b's rows in order: x as
 // tc5::ld_16x64 leaves it is 16 columns from c + 16 (lane % 4) on of this thread, of rows
 // lane / 4 and + 8. The stores ask to be put out of L2 before the operands, which other
-// CTAs read (16384 tokens of 1024 into 4096: 54 us without, 49.5 so).
+// CTAs read (16384 tokens of 1024 into 4096: 54 us without, 49.5 so). The lanes, parted by
+// their rows, meet at the end: the next tc5::ld_16x64 is one instruction of the warp.
 template <typename T>
 __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64_t row, int64_t c, float (&x)[32]) {
     const int lane = threadIdx.x & 31;
     c += 16 * (lane & 3);
-    if (c >= a.M) return;   // (64 columns are there or not)
     row += lane >> 2;
-    if (a.bias) {
+    const bool there = c < a.M;   // (64 columns are there or not)
+    if (there && a.bias) {
         const float *bias = a.bias + (int64_t)un.batch * a.M + c;
 #pragma unroll
         for (int i = 0; i < 8; i++) {
@@ -242,7 +243,7 @@ __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64
     }
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        if (row + 8 * h < un.r0 || row + 8 * h >= un.r1) continue;
+        if (!there || row + 8 * h < un.r0 || row + 8 * h >= un.r1) continue;
         T *out = static_cast<T *>(a.Y) + (un.out + row + 8 * h) * a.M + c;
         uint32_t w[8];
         if constexpr (sizeof(T) == 2) {
@@ -259,6 +260,7 @@ __device__ __forceinline__ void put_ordered(const Args &a, const Unit &un, int64
             }
         }
     }
+    __syncwarp();
 }
 
 // 32 rows of the result from `row` on x 32 columns from c on; x: those of row + lane.
@@ -665,12 +667,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     }
     // every MMA completed (the issuer waited for `done`), and neither CTA reads
     // or signals the other's shared memory any more
-    auto meet = [&]() {
-        __syncwarp();
-        ptx::cluster_barrier();
-    };
     tc5::fence_before();
-    meet();
+    ptx::cluster_barrier();
     if (aborted(&stop)) {
         // (the same for both CTAs.) The loads that only some of a step's producers
         // issued are completed by the others, so that every barrier phase can
@@ -687,7 +685,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                     ptx::mbar_wait_bounded(&full[g % ns], (uint32_t)(g / ns) & 1, kDrainNs);
             }
         }
-        meet();
+        ptx::cluster_barrier();
     }
     if (warp == kMmaWarp) {
         // a commit arrives by itself, at both CTAs: each waits for the last

@@ -610,6 +610,7 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_gated_mma(const __grid
         };
         // a piece of the accumulators at tm
         auto load_piece = [&](uint32_t tm, int p, uint32_t (&r0)[16], uint32_t (&r1)[16]) {
+            __syncwarp();   // (the piece before may have parted the lanes by their rows)
             if constexpr (MODE == GM_PRODUCT) {
                 tc5::ld_16x32(tm + 32 * (first + p), r0);
                 tc5::ld_16x32(tm + (16u << 16) + 32 * (first + p), r1);

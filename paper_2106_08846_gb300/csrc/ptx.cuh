@@ -131,8 +131,10 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 // Barrier over every thread of the cluster, with release and acquire of
-// shared-memory writes (each CTA's and each other's).
+// shared-memory writes (each CTA's and each other's). Its instructions want a warp's
+// lanes side by side, which tests and loops by lane before it may have parted.
 __device__ __forceinline__ void cluster_barrier() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }

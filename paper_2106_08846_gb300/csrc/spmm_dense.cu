@@ -513,6 +513,7 @@ k_dense(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ DnBatc
             for (int gq = 0; gq < gn; gq += 4) {               // 64 columns: four row groups
                 const int cnt = min(4, gn - gq);
                 uint32_t r[64] = {};
+                __syncwarp();   // (the groups before may have parted the lanes by their tokens)
                 if (un.n > 0) {
                     tc5::ld32(tm + 16 * gq, *reinterpret_cast<uint32_t(*)[32]>(&r[0]));
                     if (cnt > 2) tc5::ld32(tm + 16 * gq + 32, *reinterpret_cast<uint32_t(*)[32]>(&r[32]));
