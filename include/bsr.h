@@ -558,7 +558,7 @@ bsr_status_t bsr_fp8_quantize(const void *x, bsr_dtype_t dt, const bsr_fp8_matri
 typedef enum {
     BSR_GROUP_NONE = 0,
     BSR_GROUP_ROWS = 1,     /* rows offsets[e] .. offsets[e + 1] - 1 of a meet b's matrix e */
-    BSR_GROUP_COLUMNS = 2   /* Y[e] sums over the columns offsets[e] .. offsets[e + 1] - 1, multiples of 128 */
+    BSR_GROUP_COLUMNS = 2   /* Y[e] sums over the columns offsets[e] .. offsets[e + 1] - 1, multiples of 128 or the end */
 } bsr_group_t;
 
 /* Bytes of workspace of a product; may be 0. a and b: their sizes, no arrays. */
@@ -573,7 +573,9 @@ bsr_status_t bsr_fp8_product_workspace(const bsr_fp8_matrix_t *a, const bsr_fp8_
  *          [groups, a.rows, b.rows]. Overlaps nothing.
  * bias     device fp32 [b.batch, b.rows], or NULL; not by BSR_GROUP_COLUMNS.
  * groups   1 .. 1024 experts, offsets: device int32 [groups + 1], ascending, within a's rows
- *          (columns, where 128 columns from a multiple of 128 are taken or left as a whole); read on the device.
+ *          or columns; read on the device. Of columns, multiples of 128 (orders of align 128, 256, ...), or a.cols
+ *          and more, the end: at any other, the matrices Y[e] of the runs that it ends are NaN, and
+ *          bsr_check_status returns BSR_ERR_INVALID_ARG.
  *          BSR_GROUP_ROWS: b.batch is groups; rows in no expert's run are left as they were.
  *          BSR_GROUP_NONE: offsets NULL, groups unused, b.batch 1.
  * ws       device, 16-byte aligned, of at least the bytes that bsr_fp8_product_workspace
@@ -586,7 +588,8 @@ bsr_status_t bsr_fp8_product(const bsr_fp8_matrix_t *a, const bsr_fp8_matrix_t *
 /*
  * bsr_check_status -- synchronise the current device and return the first error
  * that a kernel of bsr_gated, bsr_gated_backward or bsr_fp8_product recorded there
- * (BSR_ERR_TIMEOUT when a bounded wait gave up), then clear it. BSR_OK if none.
+ * (BSR_ERR_TIMEOUT when a bounded wait gave up, BSR_ERR_INVALID_ARG for offsets inside a
+ * block of columns), then clear it. BSR_OK if none.
  */
 bsr_status_t bsr_check_status(void);
 

@@ -930,7 +930,8 @@ def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = N
     offsets (int32 [E + 1] on the device, as ExpertOrder.offsets): over "rows", b is a
     batch of E matrices and each run of a's rows meets its expert's (bias [E, b.rows];
     rows in no run are left as they were); over "columns", Y [E, a.rows, b.rows] has a
-    sum over each run of columns, whose offsets are multiples of 128."""
+    sum over each run of columns, whose offsets are multiples of 128 (an order of align
+    128) or the end: at any other the runs beside it are NaN, and bsr_check_status tells."""
     if over != "rows" and over != "columns":
         raise ValueError("over is 'rows' or 'columns'")
     if Y is not None:

@@ -45,7 +45,7 @@
 // Persistent: one CTA per SM. Runs of rows: tiles of 256 rows from a multiple of 128 on,
 // as the exponents lie, the rows of other runs left out; the table of the runs' tiles is
 // made by every CTA from the offsets on the device.
-// Runs of columns: a tile's steps are the run's. Tiles of sums too few to fill the
+// Runs of columns: a tile's steps are the run's, which ends where blocks do. Tiles of sums too few to fill the
 // GPU have them split; the parts are added in their order by a second launch.
 //
 // Every wait is bounded by the global timer; a timeout is recorded, stops every
@@ -91,6 +91,7 @@ struct Args {
     CUtensorMap a, b, ea, eb; // values; exponents
     const float *bias;
     int64_t rows, M, KB;      // of a; of b (columns of Y); blocks
+    int64_t cols;             // of a and b
     int group, E;
     const int32_t *offsets;
     unsigned tiles_m, tiles_n;
@@ -109,9 +110,10 @@ struct Unit {
     int64_t out;              // rows of Y before this unit's matrix
     int batch, part;
     int i0, i1;               // steps
+    float fill;               // the result of no steps
 };
 
-// The runs: their ends, and the tiles of rows before each.
+// The runs: their ends, and the tiles of rows before each; of columns, whether the end is none.
 struct Runs {
     int32_t at[kMostExperts + 1];
     uint32_t first[kMostExperts + 1];
@@ -131,6 +133,7 @@ __device__ __forceinline__ Unit unit_of(const Sizes &a, const Runs &r, unsigned 
     u.part = -1;
     u.i0 = 0;
     u.i1 = a.KB;
+    u.fill = 0.f;
     if (a.group == BSR_GROUP_ROWS) {
         const unsigned t = v / a.tiles_n;
         int lo = 0, hi = a.E;   // the last run whose tiles begin at or before t
@@ -153,6 +156,7 @@ __device__ __forceinline__ Unit unit_of(const Sizes &a, const Runs &r, unsigned 
         u.out = (int64_t)e * a.rows;
         u.i0 = r.at[e];
         u.i1 = max(r.at[e], r.at[e + 1]);
+        if (r.first[e] | r.first[e + 1]) u.i1 = u.i0, u.fill = __uint_as_float(0x7fffffffu);   // NaN
     } else if (a.splits > 1) {
         u.part = (int)v;
         tile = v / (unsigned)a.splits;
@@ -372,11 +376,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
     ptx::pdl_wait();                // operands and offsets may be an earlier kernel's, and Y may be read by one
     unsigned units = a.tiles_m * a.tiles_n * (unsigned)a.splits;
     if (a.group != BSR_GROUP_NONE) {
-        // within what there is, in steps for columns
+        // within what there is, in steps for columns: an offset inside a block, whose columns
+        // share scales and MMAs, is reported, and the runs that it ends are NaN
         const bool by_rows = a.group == BSR_GROUP_ROWS;
         for (int e = threadIdx.x; e <= a.E; e += kThreads) {
             const int64_t o = max(0, a.offsets[e]);
-            runs.at[e] = (int32_t)(by_rows ? min(o, a.rows) : min(o / kFp8Block, a.KB));
+            if (by_rows) {
+                runs.at[e] = (int32_t)min(o, a.rows);
+                continue;
+            }
+            runs.at[e] = (int32_t)(o < a.cols ? o / kFp8Block : a.KB);
+            runs.first[e] = o < a.cols && o % kFp8Block != 0;
+            if (runs.first[e]) set_status(&g_status, DEV_OFFSETS);
         }
         __syncthreads();
         if (warp == 0 && by_rows) {
@@ -507,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
                     const int g = back ? groups - 2 - p : p;
                     uint32_t r[2][32];
 #pragma unroll
-                    for (int j = 0; j < 32; j++) r[0][j] = r[1][j] = 0;
+                    for (int j = 0; j < 32; j++) r[0][j] = r[1][j] = __float_as_uint(un.fill);
                     if (any) {
                         if constexpr (ORDERED) {
                             tc5::ld_16x64(tm + 32 * g, r[0]);
@@ -536,7 +547,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_fp8_product(const __grid_consta
 #pragma unroll
                 for (int g = 0; g < 4; g++)
 #pragma unroll
-                    for (int j = 0; j < 32; j++) sum[g][j] = 0.f;
+                    for (int j = 0; j < 32; j++) sum[g][j] = un.fill;
                 for (int b = un.i0; b < un.i1; b += kDrainSteps) {
                     const uint32_t tm = wait_acc(un);
                     if (!ok) break;
@@ -844,7 +855,7 @@ cudaError_t launch_fp8_product(const Fp8Product &p, cudaStream_t s) {
     Args a = {};
     a.bias = p.bias;
     a.rows = p.a.rows, a.M = p.b.rows;
-    a.KB = fp8_blocks(p.a.cols);
+    a.KB = fp8_blocks(p.a.cols), a.cols = p.a.cols;
     a.group = p.group, a.E = p.groups;
     a.offsets = p.offsets;
     a.tiles_m = (unsigned)q.tiles_m, a.tiles_n = (unsigned)q.tiles_n;

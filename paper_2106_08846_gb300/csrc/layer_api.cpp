@@ -194,7 +194,8 @@ bsr_status_t bsr_check_status(void) {
     int gated = DEV_OK, product = DEV_OK;
     bsr_status_t st = launched(gated_mma_status(&gated));
     if (st == BSR_OK) st = launched(fp8_product_status(&product));
-    return st == BSR_OK && (gated == DEV_TIMEOUT || product == DEV_TIMEOUT) ? BSR_ERR_TIMEOUT : st;
+    if (st != BSR_OK) return st;
+    return gated == DEV_TIMEOUT || product == DEV_TIMEOUT ? BSR_ERR_TIMEOUT : product == DEV_OFFSETS ? BSR_ERR_INVALID_ARG : BSR_OK;
 }
 
 }  // extern "C"
