@@ -947,6 +947,8 @@ def bsr_fp8_product(a: Fp8Matrix, b: Fp8Matrix, bias: Optional[torch.Tensor] = N
             group, batch = BSR_GROUP_ROWS, E
         else:
             group, shape = BSR_GROUP_COLUMNS, (E, a.rows, b.rows)
+    elif over == "columns":
+        raise ValueError("sums over runs of columns need offsets")
     if a.batch is not None or b.batch != batch:
         raise ValueError("a is one matrix, b one for each expert by rows, else one")
     if bias is not None:
