@@ -1,5 +1,5 @@
 """Products of runs of columns whose offsets are not multiples of 128: a run to the last
-column is whole, one that ends inside a block of columns is NaN and reported."""
+column is whole, one that ends inside a block of columns is NaN and reported; and of long runs in bf16."""
 import pytest
 import torch
 
@@ -72,3 +72,24 @@ def test_gradients_of_runs_that_are_not_aligned_for_them(align):
         else:
             near(dW[e], values(d)[:, at[e]:at[e + 1]], values(x)[:, at[e]:at[e + 1]])
     assert bsr.bsr_check_status() == BSR_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("M,tile", [(192, 128), (320, 128), (320, 1), (77, 128)])   # straight from tensor memory, or through shared memory
+@pytest.mark.parametrize("N,R,at", [(70, 16512, [0, 16512]), (130, 17000, [0, 0, 256, 1408, 1408, 17000]), (300, 40000, [0, 18560, 18560, 39936, 40000]),
+                                    (600, 20000, [128, 19200])])
+def test_drained_sums_with_bf16_results(N, R, at, M, tile):
+    """More than 128 blocks of columns, of runs that are empty, short, longer than that and no multiples
+    of the eight blocks of a drained sum: bf16 results are those in fp32, rounded once."""
+    a, b = operands(N, M, R, tile)
+    E = len(at) - 1
+    buf, Y = guarded("bf16", E, N, M)
+    product(a, b, at, Y)
+    wide = torch.full((E, N, M), 7.0, device="cuda")
+    product(a, b, at, wide)
+    assert torch.equal(Y, wide.to(torch.bfloat16))
+    A, B = values(a), values(b)
+    for e in range(E):
+        near(Y[e], A[:, at[e]:at[e + 1]], B[:, at[e]:at[e + 1]])
+        near(wide[e], A[:, at[e]:at[e + 1]], B[:, at[e]:at[e + 1]])
+    assert (buf[:32] == 7).all() and (buf[-32:] == 7).all()
+    assert bsr.bsr_check_status() == BSR_OK
