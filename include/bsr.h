@@ -521,8 +521,8 @@ bsr_status_t bsr_expert_sum_backward(const bsr_experts_t *p, const void *Ys, con
  *   ((b / 4) * w + r / 128) * 512 + (r % 32) * 16 + (r / 32 % 4) * 4 + b % 4
  *
  * Y = a b' + bias:  Y[n, m] = bias[m] + sum_k a[n, k] b[m, k], in the tensor cores'
- * fp32 accumulators, which lose at most 4e-9 of a sum of one sign with each column (2e-10
- * on average); they are added up in fp32 every 1024 columns, for bf16 results every 16384 at least.
+ * fp32 accumulators, which lose at most 4e-9 of a sum of one sign with each column (on
+ * average 2e-10 of 1024 columns, 6e-10 of 16384); they are added up in fp32 every 1024 columns, for bf16 results every 16384 at least.
  * A layer X W': a = X by rows, b = W by rows with tiles of 128. Its gradients:
  * dX = dY W: b = W by columns; dW = dY' X: a = dY and b = X, both by columns.
  */
