@@ -74,26 +74,26 @@ __device__ __forceinline__ void load8(const T *p, int64_t n, int align, Eight<T>
     if (n >= 8 && align == 16) {
 #pragma unroll
         for (int h = 0; h < words / 4; h++) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + h);
+            const uint4 u = reinterpret_cast<const uint4 *>(p)[h];
             r.w[4 * h] = u.x, r.w[4 * h + 1] = u.y, r.w[4 * h + 2] = u.z, r.w[4 * h + 3] = u.w;
         }
     } else if (n >= 8 && align >= 8) {
 #pragma unroll
         for (int h = 0; h < words / 2; h++) {
-            const uint2 u = __ldg(reinterpret_cast<const uint2 *>(p) + h);
+            const uint2 u = reinterpret_cast<const uint2 *>(p)[h];
             r.w[2 * h] = u.x, r.w[2 * h + 1] = u.y;
         }
     } else if (n >= 8 && align >= 4) {
 #pragma unroll
-        for (int h = 0; h < words; h++) r.w[h] = __ldg(reinterpret_cast<const uint32_t *>(p) + h);
+        for (int h = 0; h < words; h++) r.w[h] = reinterpret_cast<const uint32_t *>(p)[h];
     } else {
 #pragma unroll
         for (int j = 0; j < words; j++) r.w[j] = 0;
 #pragma unroll
         for (int j = 0; j < 8; j++) {
             if (j >= n) break;
-            if constexpr (sizeof(T) == 2) r.w[j / 2] |= (uint32_t)__ldg(p + j) << (16 * (j & 1));
-            else r.w[j] = __float_as_uint(__ldg(p + j));
+            if constexpr (sizeof(T) == 2) r.w[j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+            else r.w[j] = __float_as_uint(p[j]);
         }
     }
 }

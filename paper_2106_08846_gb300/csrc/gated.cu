@@ -54,17 +54,17 @@ __global__ void __launch_bounds__(256) k_lay_out(const __grid_constant__ Sources
         if constexpr (PARTS == 1) {
 #pragma unroll
             for (int j = 0; j < 8; j++) {
-                const uint32_t v = there && c + j < a.K ? __ldg(src + j) : (uint16_t)0;
+                const uint32_t v = there && c + j < a.K ? src[j] : (uint16_t)0;
                 w[0][j / 2] = j & 1 ? w[0][j / 2] | v << 16 : v;
             }
         } else {
             float v[8];
             if (a.vec && there) {
-                const float4 p = __ldg(reinterpret_cast<const float4 *>(src)), q = __ldg(reinterpret_cast<const float4 *>(src) + 1);
+                const float4 p = reinterpret_cast<const float4 *>(src)[0], q = reinterpret_cast<const float4 *>(src)[1];
                 v[0] = p.x, v[1] = p.y, v[2] = p.z, v[3] = p.w, v[4] = q.x, v[5] = q.y, v[6] = q.z, v[7] = q.w;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; j++) v[j] = there && c + j < a.K ? __ldg(src + j) : 0.f;
+                for (int j = 0; j < 8; j++) v[j] = there && c + j < a.K ? src[j] : 0.f;
             }
 #pragma unroll
             for (int j = 0; j < 4; j++) {

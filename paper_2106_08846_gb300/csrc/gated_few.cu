@@ -59,11 +59,11 @@ __device__ __forceinline__ uint4 load16(const T *row, int k, int K) {
         uint4 v = make_uint4(0, 0, 0, 0);
         if (!CHECK || k < K) {
             if constexpr (STREAM)
-                asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                              : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                              : "l"(row + k));
             else
-                v = __ldg(reinterpret_cast<const uint4 *>(row + k));
+                v = *reinterpret_cast<const uint4 *>(row + k);
         }
         return v;
     } else {
@@ -72,8 +72,8 @@ __device__ __forceinline__ uint4 load16(const T *row, int k, int K) {
 #pragma unroll
         for (int j = 0; j < 4 * per; j++)
             if (!CHECK || k + j < K) {
-                if constexpr (per == 2) w[j / 2] |= (uint32_t)__ldg(row + k + j) << (16 * (j & 1));
-                else w[j] = __float_as_uint(__ldg(row + k + j));
+                if constexpr (per == 2) w[j / 2] |= (uint32_t)row[k + j] << (16 * (j & 1));
+                else w[j] = __float_as_uint(row[k + j]);
             }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 4 : NT == 2 ? 3 : 2) k_
             const float4 v = sums[k][n][l];
             s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
         }
-        const float bg = c.bg ? __ldg(c.bg + fe) : 0.f, bu = c.bu ? __ldg(c.bu + fe) : 0.f;
+        const float bg = c.bg ? c.bg[fe] : 0.f, bu = c.bu ? c.bu[fe] : 0.f;
         float2 h;
         with_act(c.act, [&](auto tag) {
             h = unpack2(mul2(activate<decltype(tag)::value, sizeof(T) == 2>(pack2(s.x + bg, s.y + bg)), pack2(s.z + bu, s.w + bu)));
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) k_gated_few_f32(const __grid_c
     const int e = threadIdx.x, fl = e & 7, n = e >> 3;
     const int64_t fe = (int64_t)blockIdx.x * 8 + fl;
     if (n >= tokens || fe >= c.F) return;
-    float2 s = make_float2(c.bg ? __ldg(c.bg + fe) : 0.f, c.bu ? __ldg(c.bu + fe) : 0.f);
+    float2 s = make_float2(c.bg ? c.bg[fe] : 0.f, c.bu ? c.bu[fe] : 0.f);
 #pragma unroll
     for (int k = 0; k < kWarps; k++) s.x += sums[k][fl][n].x, s.y += sums[k][fl][n].y;
     with_act(c.act, [&](auto tag) {

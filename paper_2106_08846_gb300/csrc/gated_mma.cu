@@ -681,8 +681,8 @@ __global__ void __launch_bounds__(threads_of(DRAIN), 1) k_gated_mma(const __grid
                 __syncwarp();   // (the last unit's biases have been read)
                 for (int j = lane; j < 16 * kMost; j += 32) {
                     const int64_t f = un.n0 + 32 * (first >> 1) + j;
-                    bs[j] = a.bg && f < job.N ? __ldg(a.bg + f) : 0.f;
-                    bs[16 * kMost + j] = a.bu && f < job.N ? __ldg(a.bu + f) : 0.f;
+                    bs[j] = a.bg && f < job.N ? a.bg[f] : 0.f;
+                    bs[16 * kMost + j] = a.bu && f < job.N ? a.bu[f] : 0.f;
                 }
                 __syncwarp();
             }

@@ -7,7 +7,11 @@
 // and the next kernel runs its prologue -- barrier set-up, fetching the
 // handle's own schedule and block values -- on the SMs that free up, then
 // waits (griddepcontrol.wait) before it touches anything an earlier kernel
-// may write: X, the bias, Y and the split-row workspace. A chain of products
+// may write: X, the bias, Y and the split-row workspace. What an earlier kernel may
+// have written is read by plain loads or TMA: the read-only path (ld.global.nc, __ldg,
+// const __restrict__) wants memory that nobody writes while the kernel runs, and it
+// runs from before the earlier one's end. The same holds for the operators without a
+// handle, whose every input may be an earlier kernel's output. A chain of products
 // on one stream (layers, or the block-shape sweep) thus overlaps each
 // kernel's start with the previous one's tail, with the stream's ordering
 // intact. BSR_PDL=0 in the environment turns it off (plain stream order).

@@ -146,7 +146,7 @@ __device__ __forceinline__ void kept_sums(float (&acc)[kDnGroup], const uint16_t
     uint4 x_next = {};
     auto fetch = [&](int v) {
         if (v < 8 * n) col_next = min(K, (int64_t)__ldg(list + (v >> 3)) * KC + 8 * (v & 7));
-        if (col_next < K) x_next = __ldg(reinterpret_cast<const uint4 *>(x + col_next));
+        if (col_next < K) x_next = *reinterpret_cast<const uint4 *>(x + col_next);
     };
     fetch(first);
     for (int v = first, k = 0; v < 8 * n; v += step, k++) {
@@ -175,7 +175,7 @@ __device__ __forceinline__ void kept_sums(float (&acc)[kDnGroup], const uint16_t
         } else {
 #pragma unroll 1
             for (int e = 0; e < 8; e++) {
-                const float xv = to_f32(__ldg(x + col + e));
+                const float xv = to_f32(x[col + e]);
 #pragma unroll
                 for (int r = 0; r < kDnGroup; r++) {
                     const uint16_t wv = __ldg(w + r * K + col + e);
@@ -227,7 +227,7 @@ __device__ __noinline__ void compute_again(const DnArgs &a, const uint16_t *X, i
 #pragma unroll
                 for (int r = 0; r < kDnGroup; r++)
                     if ((y[r] & 0x7fffu) > 0x7f80u)
-                        y[r] = from_f32<uint16_t>(acc[r] + (a.bias ? __ldg(a.bias + row0 + r) : 0.f));
+                        y[r] = from_f32<uint16_t>(acc[r] + (a.bias ? a.bias[row0 + r] : 0.f));
             }
         } else {
             for (uint32_t left = tokens; left; left &= left - 1) {
@@ -243,7 +243,7 @@ __device__ __noinline__ void compute_again(const DnArgs &a, const uint16_t *X, i
                 }
                 uint16_t *y = a.Y + t * a.M + row0 + lane;
                 if (lane < kDnGroup && (*y & 0x7fffu) > 0x7f80u)
-                    *y = from_f32<uint16_t>(mine + (a.bias ? __ldg(a.bias + row0 + lane) : 0.f));
+                    *y = from_f32<uint16_t>(mine + (a.bias ? a.bias[row0 + lane] : 0.f));
             }
         }
         __syncwarp();
@@ -491,7 +491,7 @@ k_dense(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ DnBatc
 #pragma unroll
             for (int j = 0; j < 8; j++) {   // unit columns lane + 32 j
                 const int gj = __shfl_sync(0xffffffffu, gl, 2 * j + (lane >> 4) & 15);
-                bv[j] = a.bias && gj >= 0 ? __ldg(a.bias + gj * 16 + (lane & 15)) : 0.f;
+                bv[j] = a.bias && gj >= 0 ? a.bias[gj * 16 + (lane & 15)] : 0.f;
             }
             if (un.n > 0) {
                 const bool got = wait_or_abort(&acc_full[ab], fphase, a.wait_ns * (uint64_t)(un.n + 2), &stop, &beat);

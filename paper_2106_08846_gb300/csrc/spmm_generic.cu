@@ -16,8 +16,8 @@ namespace {
 template <typename T>
 __global__ void __launch_bounds__(256)
 k_generic(const Item *__restrict__ items, int n_items, const int32_t *__restrict__ indices,
-          const T *__restrict__ data, const T *__restrict__ X, const float *__restrict__ bias,
-          T *__restrict__ Y, float *__restrict__ ws, int64_t N, int64_t K, int64_t M, int R, int C,
+          const T *__restrict__ data, const T *X, const float *bias,
+          T *Y, float *ws, int64_t N, int64_t K, int64_t M, int R, int C,
           int tn, int64_t n_tiles) {
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();   // X, the bias, Y and the workspace may be an earlier kernel's
@@ -54,8 +54,8 @@ k_generic(const Item *__restrict__ items, int n_items, const int32_t *__restrict
 // inside it.
 template <typename T>
 __global__ void __launch_bounds__(256)
-k_reduce(const Split *__restrict__ splits, int n_splits, const float *__restrict__ ws,
-         const float *__restrict__ bias, T *__restrict__ Y, int64_t N, int64_t M, int R, int tn, int64_t n_tiles) {
+k_reduce(const Split *__restrict__ splits, int n_splits, const float *ws,
+         const float *bias, T *Y, int64_t N, int64_t M, int R, int tn, int64_t n_tiles) {
     ptx::pdl_launch_dependents();
     ptx::pdl_wait();   // the partials come from the product kernel just before
     const int64_t work = (int64_t)n_splits * n_tiles;

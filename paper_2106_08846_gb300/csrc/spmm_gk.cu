@@ -493,7 +493,7 @@ k_gk(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ GkArgs a)
                 float *B = bias_s(j);
                 for (int e = et; e < I[0] * R; e += 32 * NEW) {
                     const int g = e / R, r = e - g * R;
-                    B[e] = a.bias ? __ldg(a.bias + (int64_t)I[be_at + pad4(I[1] + 1) + 4 * g] * R + r) : 0.f;
+                    B[e] = a.bias ? a.bias[(int64_t)I[be_at + pad4(I[1] + 1) + 4 * g] * R + r] : 0.f;
                 }
                 ptx::named_barrier(2, 32 * NEW);
             }

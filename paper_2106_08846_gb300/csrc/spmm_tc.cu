@@ -363,7 +363,7 @@ __device__ __forceinline__ void tc_cta(const CUtensorMap &xmap, const TcArgs &a,
         ptx::pdl_wait();   // the bias, Y and the workspace may be an earlier kernel's
         for (int e = et; e < g_count * R; e += 128) {
             const int g = e / R, r = e - g * R;
-            B_s[e] = a.bias ? __ldg(a.bias + (int64_t)itab[6 * g + 0] * R + r) : 0.f;
+            B_s[e] = a.bias ? a.bias[(int64_t)itab[6 * g + 0] * R + r] : 0.f;
         }
         bool split_ok = true;
         if constexpr (F32) {

@@ -448,7 +448,7 @@ k_tcp(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ TcpArgs 
                 float *B = bias_s(j);
                 for (int e = et; e < I[1] * R; e += 32 * NEW) {
                     const int g = e / R, r = e - g * R;
-                    B[e] = a.bias && I[items_at + 4 * g + 3] < 0 ? __ldg(a.bias + (int64_t)I[items_at + 4 * g] * R + r)
+                    B[e] = a.bias && I[items_at + 4 * g + 3] < 0 ? a.bias[(int64_t)I[items_at + 4 * g] * R + r]
                                                                   : 0.f;   // split rows: the reduce pass adds it
                 }
                 ptx::named_barrier(1, 32 * NEW);
