@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_
             total += c;
         }
     }
-    const int32_t padded = (total + p.align - 1) / p.align * p.align;
+    const int32_t padded = (int32_t)(((uint32_t)total + (uint32_t)p.align - 1) / (uint32_t)p.align * (uint32_t)p.align);   // (below 2^31, not so the sum)
     int32_t upto = padded;   // inclusive sums: of the warp's experts, then of the warps'
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
@@ -160,8 +160,8 @@ __global__ void __launch_bounds__(kOrderThreads, 1) k_expert_order(const __grid_
     }
     // rows that nobody was sent to: behind an expert's, and behind the last one's
     for (int f = (int)rank * kWarps + warp; f < E; f += (int)ctas * kWarps) {
-        const int32_t end = f + 1 < E ? first[f + 1] : used;
-        for (int32_t r = first[f] + all[f] + lane; r < end; r += 32) p.source[r] = -1;
+        const int64_t end = f + 1 < E ? first[f + 1] : used;   // (rows up to 2^31 - 1: past them 32 bits end)
+        for (int64_t r = (int64_t)first[f] + all[f] + lane; r < end; r += 32) p.source[r] = -1;
     }
     for (int64_t r = used + (int64_t)rank * kOrderThreads + threadIdx.x; r < p.R; r += (int64_t)ctas * kOrderThreads) p.source[r] = -1;
     if (ctas > 1) ptx::cluster_barrier();   // nobody reads this CTA's counts any more
