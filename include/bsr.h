@@ -528,7 +528,7 @@ bsr_status_t bsr_expert_sum_backward(const bsr_experts_t *p, const void *Ys, con
  */
 typedef enum { BSR_E4M3 = 0, BSR_E5M2 = 1 } bsr_fp8_t;
 typedef struct {
-    int64_t batch;         /* matrices, one behind the other; 1 but for the weights of experts */
+    int64_t batch;         /* matrices, one behind the other, at most 65535; 1 but for the weights of experts */
     int64_t rows, cols;    /* below 2^31; batch * rows * (cols rounded up to 128) up to 2^38 */
     int tile;              /* rows that share a scale: 1 or 128 */
     bsr_fp8_t type;
@@ -549,7 +549,8 @@ typedef struct {
  * for the scale.
  * used     device int32 [1], or NULL for R (batch 1): rows of x from *used on are not read
  *          and count as zeros of a block; in rows, they and their scales are left as they
- *          were, in columns the blocks of 128 that begin at or after *used.
+ *          were (with tile 128, a block in use in part has one scale: that of its rows in
+ *          use), in columns the blocks of 128 that begin at or after *used.
  * Asynchronous on `stream`; allocates nothing. Nothing overlaps.
  */
 bsr_status_t bsr_fp8_quantize(const void *x, bsr_dtype_t dt, const bsr_fp8_matrix_t *rows, const bsr_fp8_matrix_t *columns,

@@ -10,13 +10,13 @@
 // every call). Between the passes the counts of the warps, and of a cluster's CTAs
 // through distributed shared memory, become first rows.
 //
-// Rows and sums: one pass over the data, a warp to a token's 2 KB (backward: to a
-// choice's row).
+// Rows and sums: one pass over the data, a warp to 2 KB of a token's row (16-byte words; sums of
+// one choice: 4 KB, of two: 1 KB; backward: to a choice's whole row).
 //
 // What bounds them: DRAM, and the order the choices' bits (16384 tokens of 4 of 64
 // experts 8.8 us, a ballot a bit and choice, on 16 SMs). 16384 x 1024 bf16: rows of 4
 // choices 29.3 us, 168 MB at 84% of the copy rate; their sum 30, 83%; the sum's gradients for 2 choices
-// 31, 80%. 9920 x 1344 fp32, 2 choices: 30 us, 79%, bf16 12.4, 95%. One token: order 3.6, rows 1.5,
+// 31, 80%. 9920 x 1344 fp32, 2 choices: 29.9 us, 79%, bf16 12.0, 98%, their gradients 41.8, 94%, and 25.0, 78%. One token: order 3.6, rows 1.5,
 // launches and a read's latency. Rows that are no multiples of 16 bytes go in smaller words
 // (8192 x 1023 bf16, 2 choices: order and rows 16, their sum 15 us, 48%).
 //
