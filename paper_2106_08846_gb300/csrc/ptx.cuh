@@ -31,6 +31,15 @@ __device__ __forceinline__ unsigned char *align_smem(unsigned char *p) {
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// A value that an earlier kernel may have written (no read-only load): behind pdl_wait, in
+// no order with stores (the biases of k_xcol by plain C++ loads: 16384 tokens of 1024 into 1024,
+// 32x1 blocks 96.6 us for 96.3).
+__device__ __forceinline__ float load_input(const float *p) {
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+
 __device__ __forceinline__ uint64_t globaltimer() {
     uint64_t t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));

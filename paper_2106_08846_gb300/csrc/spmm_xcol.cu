@@ -419,7 +419,7 @@ k_xcol(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ XcBatch
             const float *bias = a.bias && !partial ? a.bias + (int64_t)it.row * R : nullptr;
             float bv[NR];
 #pragma unroll
-            for (int j = 0; j < NR; j++) bv[j] = bias ? bias[j < 4 ? 4 * rg + j : 16 + 4 * rg + j - 4] : 0.f;
+            for (int j = 0; j < NR; j++) bv[j] = bias ? ptx::load_input(bias + (j < 4 ? 4 * rg + j : 16 + 4 * rg + j - 4)) : 0.f;
 #pragma unroll
             for (int i = 0; i < TT; i++) {
                 float v[NR];
